@@ -665,6 +665,73 @@ int shifter_compact_batch_masked(shifter_ctx* ctx, const shifter_model* model, c
                                  shifter_vec_desc* h_out_vecs, uint64_t* h_elems_w,
                                  uint64_t* h_elems_v);
 
+/* --- 8-bit matrices ------------------------------------------------------------------ */
+
+/* Linear layers of a rebuilt variant in 8 bits, and 8-bit activations as the checkpoint that
+ * training between two prunings reads in its backward pass (Phase 1, Sec. III-C: weights stay
+ * masked while the network trains on).  None of these calls needs a model; all of them only
+ * enqueue kernels, allocate nothing and can be recorded into a HIP graph.
+ *
+ * An 8-bit matrix of rows x cols is int8 codes, row r at d_q + r * ld_q, and one fp32 scale a
+ * row: value = code * scale.  d_q and ld_q are multiples of 16, ld_q is at least cols rounded up
+ * to 16 and at most 2^22.  A call that writes codes writes zeros behind a row's last column up to the
+ * next multiple of 16 and nothing further; a call that reads them does not rely on that.
+ * Element matrices (fp32, bf16, fp16) may start at any element and have any stride from a row's
+ * length on; strides are in elements, of the 8-bit rows and the mask in bytes.  Zero rows
+ * or columns are allowed everywhere.
+ *
+ * shifter_quantize_q8    each row of x by itself: a = max |f(x)|, scale = a / 127,
+ *                        code = 127 f(x) / a rounded to the nearest whole number, ties to even;
+ *                        f is the identity, or ReLU with SHIFTER_Q8_RELU.  Codes are exact:
+ *                        the rounding is that of the real quotient.  A row of zeros has
+ *                        scale 0; a row with a value that is not finite (behind f) has codes 0
+ *                        and scale NaN, so that every use of it becomes NaN.
+ *                        Rows are a linear tensor's output channels (d_w + offset, stride
+ *                        in_ch) or a batch's tokens.
+ * shifter_dequantize_q8  x = code * scale, rounded to the element type.
+ * shifter_rms_norm_q8    h = x + residual, rounded to the element type and written to d_h (which
+ *                        may be d_x or d_residual); without a residual h is x and d_h NULL.
+ *                        y = h * weight / sqrt(mean(h^2) + eps) as an 8-bit matrix: codes and the row's
+ *                        a as above, of p = fl32(h * weight), and
+ *                        scale = a / (127 sqrt(mean(h^2) + eps)); the mean of squares is summed in
+ *                        64 bits.  A row of zeros has scale 0 (also where eps is 0).
+ * shifter_matmul_q8      c[m][n] = sa[m] sb[n] sum_k qa[m][k] qb[n][k] + bias[n], ReLU with
+ *                        SHIFTER_Q8_RELU, rounded to the element type.  The sum is exact in 32-bit integers:
+ *                        k up to SHIFTER_Q8_MAX_SUM, else SHIFTER_ERR_CAPACITY.  d_bias may be NULL.
+ *                        For k = 0 the sum is 0.  The result does not depend on the device's state or on how the
+ *                        work is split.
+ * shifter_weight_grad_q8 dw[n][k] = sum over the m rows of g[m][n] scale[m] q[m][k], the gradient of a linear
+ *                        layer's weights from the gradient g of its outputs and its input as an 8-bit matrix;
+ *                        where d_mask (n rows of k bytes, ld_mask apart, as shifter_apply_mask writes them) is
+ *                        not NULL, entries whose byte is 0 are 0; with SHIFTER_Q8_ACCUMULATE the sum is added to
+ *                        what d_dw holds (masked entries keep what they hold).
+ *                        p = fl32(g * scale) is held as a 24-bit whole number relative to the largest |p| of its
+ *                        column n and summed exactly: the error of an entry is at most that largest |p| / 8355711
+ *                        times the sum of |q| over its column k, plus a few roundings of the terms and of the result.  A column with
+ *                        a p that is not finite has NaN in its whole row of dw (masked entries aside).
+ *                        m up to SHIFTER_Q8_MAX_SUM, else SHIFTER_ERR_CAPACITY; more rows go in several calls with
+ *                        SHIFTER_Q8_ACCUMULATE.
+ *                        d_work: work_bytes of shifter_weight_grad_q8_layout, 256-byte aligned. */
+typedef enum { SHIFTER_F32 = 0, SHIFTER_BF16 = 1, SHIFTER_F16 = 2 } shifter_dtype;
+#define SHIFTER_Q8_RELU 1u
+#define SHIFTER_Q8_ACCUMULATE 2u
+#define SHIFTER_Q8_MAX_SUM 131071u
+int shifter_quantize_q8(shifter_ctx* ctx, const void* d_x, int dtype, uint64_t ld_x, uint64_t rows,
+                        uint64_t cols, uint32_t flags, int8_t* d_q, uint64_t ld_q, float* d_scale);
+int shifter_dequantize_q8(shifter_ctx* ctx, const int8_t* d_q, uint64_t ld_q, const float* d_scale,
+                          uint64_t rows, uint64_t cols, void* d_x, int dtype, uint64_t ld_x);
+int shifter_rms_norm_q8(shifter_ctx* ctx, const void* d_x, uint64_t ld_x, const void* d_residual,
+                        uint64_t ld_r, int dtype, uint64_t rows, uint64_t cols, const float* d_weight,
+                        float eps, void* d_h, uint64_t ld_h, int8_t* d_q, uint64_t ld_q, float* d_scale);
+int shifter_matmul_q8(shifter_ctx* ctx, const int8_t* d_qa, uint64_t ld_a, const float* d_sa,
+                      const int8_t* d_qb, uint64_t ld_b, const float* d_sb, uint64_t m, uint64_t n,
+                      uint64_t k, const float* d_bias, uint32_t flags, void* d_c, int dtype, uint64_t ld_c);
+int shifter_weight_grad_q8_layout(uint64_t m, uint64_t n, uint64_t k, uint64_t* h_work_bytes);
+int shifter_weight_grad_q8(shifter_ctx* ctx, const void* d_g, int dtype, uint64_t ld_g, const int8_t* d_q,
+                           uint64_t ld_q, const float* d_scale, uint64_t m, uint64_t n, uint64_t k,
+                           const uint8_t* d_mask, uint64_t ld_mask, uint32_t flags, float* d_dw,
+                           uint64_t ld_dw, void* d_work, uint64_t work_bytes);
+
 /* --- measurement ------------------------------------------------------------------- */
 
 /* Per-kernel timing with HIP events on the context's stream.  While enabled every

@@ -11,6 +11,7 @@
 
 #include "chain.h"
 #include "internal.h"
+#include "q8.h"
 
 using namespace shifter;
 
@@ -21,7 +22,8 @@ const char* const kKernelNames[K_COUNT] = {
     "copy", "kernel_scan", "fix_round", "fold_scale", "fold_apply",
     "deflate_chunk", "codec_scan", "codec_pack", "inflate_chunk",
     "mask_scan_batch", "expand_levels",
-    "spec_sample", "spec_pass", "spec_hist_locate", "spec_filter_rank", "spec_fixup"};
+    "spec_sample", "spec_pass", "spec_hist_locate", "spec_filter_rank", "spec_fixup",
+    "q8_rows", "q8_read", "q8_norm", "q8_product", "q8_digits", "q8_gradient"};
 
 ProfileScope::ProfileScope(shifter_ctx* c, int id) : ctx(c), idx(-1) {
     if (!c->profiling) return;
@@ -1669,4 +1671,140 @@ extern "C" int shifter_copy_f32(shifter_ctx* ctx, const float* d_src, float* d_d
     HIP_TRY(ctx, hipSetDevice(ctx->device));
     launch_copy(ctx, d_src, d_dst, n);
     return after_launch(ctx, "copy_f32");
+}
+
+// ---- 8-bit matrices -----------------------------------------------------------------
+
+static_assert(SHIFTER_Q8_MAX_SUM == Q8_MAX_K, "the limit the header names");
+
+static int q8_enter(shifter_ctx* ctx, const char* fn, int dtype, uint32_t flags, uint32_t known) {
+    if (!ctx) return fail(nullptr, SHIFTER_ERR_INVALID_ARG, std::string(fn) + ": ctx is NULL");
+    if (dtype != SHIFTER_F32 && dtype != SHIFTER_BF16 && dtype != SHIFTER_F16)
+        return fail(ctx, SHIFTER_ERR_INVALID_ARG, std::string(fn) + ": unknown element type");
+    if (flags & ~known) return fail(ctx, SHIFTER_ERR_INVALID_ARG, std::string(fn) + ": unknown flag bits");
+    HIP_TRY(ctx, hipSetDevice(ctx->device));
+    return SHIFTER_OK;
+}
+
+static uintptr_t element_size(int dtype) { return dtype == SHIFTER_F32 ? 4 : 2; }
+
+#define Q8_REFUSE(fn, expr)                                                                     \
+    do {                                                                                        \
+        if (const char* why_ = (expr))                                                          \
+            return fail(ctx, SHIFTER_ERR_INVALID_ARG, std::string(fn ": ") + why_);             \
+    } while (0)
+
+extern "C" int shifter_quantize_q8(shifter_ctx* ctx, const void* d_x, int dtype, uint64_t ld_x, uint64_t rows,
+                                   uint64_t cols, uint32_t flags, int8_t* d_q, uint64_t ld_q, float* d_scale) {
+    int rc = q8_enter(ctx, "quantize_q8", dtype, flags, SHIFTER_Q8_RELU);
+    if (rc) return rc;
+    Q8_REFUSE("quantize_q8", q8_bad_rows(d_x, element_size(dtype), rows, cols, ld_x));
+    Q8_REFUSE("quantize_q8", q8_bad_codes(d_q, d_scale, rows, cols, ld_q));
+    Q8RowsArgs a{};
+    a.x = d_x; a.ld_x = ld_x; a.rows = (uint32_t)rows; a.cols = (uint32_t)cols;
+    a.q = d_q; a.ld_q = ld_q; a.scale = d_scale; a.relu = (flags & SHIFTER_Q8_RELU) != 0;
+    launch_q8_rows(ctx, dtype, a);
+    return after_launch(ctx, "quantize_q8");
+}
+
+extern "C" int shifter_dequantize_q8(shifter_ctx* ctx, const int8_t* d_q, uint64_t ld_q, const float* d_scale,
+                                     uint64_t rows, uint64_t cols, void* d_x, int dtype, uint64_t ld_x) {
+    int rc = q8_enter(ctx, "dequantize_q8", dtype, 0, 0);
+    if (rc) return rc;
+    Q8_REFUSE("dequantize_q8", q8_bad_rows(d_x, element_size(dtype), rows, cols, ld_x));
+    Q8_REFUSE("dequantize_q8", q8_bad_codes(d_q, d_scale, rows, cols, ld_q));
+    launch_q8_read(ctx, dtype, d_q, ld_q, d_scale, (uint32_t)rows, (uint32_t)cols, d_x, ld_x);
+    return after_launch(ctx, "dequantize_q8");
+}
+
+extern "C" int shifter_rms_norm_q8(shifter_ctx* ctx, const void* d_x, uint64_t ld_x, const void* d_residual,
+                                   uint64_t ld_r, int dtype, uint64_t rows, uint64_t cols, const float* d_weight,
+                                   float eps, void* d_h, uint64_t ld_h, int8_t* d_q, uint64_t ld_q,
+                                   float* d_scale) {
+    int rc = q8_enter(ctx, "rms_norm_q8", dtype, 0, 0);
+    if (rc) return rc;
+    const uintptr_t size = element_size(dtype);
+    if (!(eps >= 0.0f) || !std::isfinite(eps))
+        return fail(ctx, SHIFTER_ERR_INVALID_ARG, "rms_norm_q8: eps must be finite and not negative");
+    Q8_REFUSE("rms_norm_q8", q8_bad_rows(d_x, size, rows, cols, ld_x));
+    if (d_residual) {
+        Q8_REFUSE("rms_norm_q8", q8_bad_rows(d_residual, size, rows, cols, ld_r));
+        Q8_REFUSE("rms_norm_q8", q8_bad_rows(d_h, size, rows, cols, ld_h));
+    } else if (d_h) {
+        return fail(ctx, SHIFTER_ERR_INVALID_ARG, "rms_norm_q8: d_h without d_residual (the stream is d_x itself)");
+    }
+    Q8_REFUSE("rms_norm_q8", q8_bad_codes(d_q, d_scale, rows, cols, ld_q));
+    if (rows && cols && !d_weight) return fail(ctx, SHIFTER_ERR_INVALID_ARG, "rms_norm_q8: NULL pointer argument");
+    if (misaligned(d_weight, 4))
+        return fail(ctx, SHIFTER_ERR_INVALID_ARG, "rms_norm_q8: a pointer is not aligned to its elements");
+    Q8RowsArgs a{};
+    a.x = d_x; a.residual = d_residual; a.weight = d_weight; a.h = d_h;
+    a.ld_x = ld_x; a.ld_r = ld_r; a.ld_h = ld_h; a.rows = (uint32_t)rows; a.cols = (uint32_t)cols;
+    a.q = d_q; a.ld_q = ld_q; a.scale = d_scale; a.eps = eps;
+    launch_q8_rows(ctx, dtype, a);
+    return after_launch(ctx, "rms_norm_q8");
+}
+
+extern "C" int shifter_matmul_q8(shifter_ctx* ctx, const int8_t* d_qa, uint64_t ld_a, const float* d_sa,
+                                 const int8_t* d_qb, uint64_t ld_b, const float* d_sb, uint64_t m, uint64_t n,
+                                 uint64_t k, const float* d_bias, uint32_t flags, void* d_c, int dtype,
+                                 uint64_t ld_c) {
+    int rc = q8_enter(ctx, "matmul_q8", dtype, flags, SHIFTER_Q8_RELU);
+    if (rc) return rc;
+    Q8_REFUSE("matmul_q8", q8_bad_codes(d_qa, d_sa, m, k, ld_a));
+    Q8_REFUSE("matmul_q8", q8_bad_codes(d_qb, d_sb, n, k, ld_b));
+    Q8_REFUSE("matmul_q8", q8_bad_rows(d_c, element_size(dtype), m, n, ld_c));
+    if (misaligned(d_bias, 4))
+        return fail(ctx, SHIFTER_ERR_INVALID_ARG, "matmul_q8: a pointer is not aligned to its elements");
+    if (k > SHIFTER_Q8_MAX_SUM)
+        return fail(ctx, SHIFTER_ERR_CAPACITY, "matmul_q8: sums of more than 131071 products do not fit 32 bits");
+    if (m == 0 || n == 0) return SHIFTER_OK;
+    Q8ProductArgs a{};
+    a.a = d_qa; a.b = d_qb; a.sa = d_sa; a.sb = d_sb; a.bias = d_bias;
+    a.ld_a = ld_a; a.ld_b = ld_b; a.ld_c = ld_c;
+    a.m = (uint32_t)m; a.n = (uint32_t)n; a.k = (uint32_t)k; a.c = d_c;
+    a.relu = (flags & SHIFTER_Q8_RELU) != 0;
+    launch_q8_product(ctx, dtype, a);
+    return after_launch(ctx, "matmul_q8");
+}
+
+extern "C" int shifter_weight_grad_q8_layout(uint64_t m, uint64_t n, uint64_t k, uint64_t* h_work_bytes) {
+    if (!h_work_bytes) return fail(nullptr, SHIFTER_ERR_INVALID_ARG, "weight_grad_q8_layout: NULL argument");
+    *h_work_bytes = 0;
+    if (m > SHIFTER_Q8_MAX_SUM)
+        return fail(nullptr, SHIFTER_ERR_CAPACITY, "weight_grad_q8_layout: sums of more than 131071 products do not fit 32 bits");
+    if (n > Q8_MAX_ROWS || k > Q8_MAX_ROWS)
+        return fail(nullptr, SHIFTER_ERR_INVALID_ARG, "weight_grad_q8_layout: more than 2^31 - 1 rows or columns");
+    *h_work_bytes = q8_gradient_plan(m, n, k).bytes;
+    return SHIFTER_OK;
+}
+
+extern "C" int shifter_weight_grad_q8(shifter_ctx* ctx, const void* d_g, int dtype, uint64_t ld_g,
+                                      const int8_t* d_q, uint64_t ld_q, const float* d_scale, uint64_t m,
+                                      uint64_t n, uint64_t k, const uint8_t* d_mask, uint64_t ld_mask,
+                                      uint32_t flags, float* d_dw, uint64_t ld_dw, void* d_work,
+                                      uint64_t work_bytes) {
+    int rc = q8_enter(ctx, "weight_grad_q8", dtype, flags, SHIFTER_Q8_ACCUMULATE);
+    if (rc) return rc;
+    Q8_REFUSE("weight_grad_q8", q8_bad_rows(d_g, element_size(dtype), m, n, ld_g));
+    Q8_REFUSE("weight_grad_q8", q8_bad_codes(d_q, d_scale, m, k, ld_q));
+    Q8_REFUSE("weight_grad_q8", q8_bad_rows(d_dw, 4, n, k, ld_dw));
+    if (d_mask) Q8_REFUSE("weight_grad_q8", q8_bad_rows(d_mask, 1, n, k, ld_mask));
+    if (m > SHIFTER_Q8_MAX_SUM)
+        return fail(ctx, SHIFTER_ERR_CAPACITY, "weight_grad_q8: sums of more than 131071 products do not fit 32 bits");
+    const uint64_t need = q8_gradient_plan(m, n, k).bytes;
+    if (work_bytes < need)
+        return fail(ctx, SHIFTER_ERR_INVALID_ARG,
+                    "weight_grad_q8: workspace too small, needs " + std::to_string(need) + " bytes");
+    if (need && (!d_work || misaligned(d_work, 256)))
+        return fail(ctx, SHIFTER_ERR_INVALID_ARG, "weight_grad_q8: the workspace must be 256-byte aligned");
+    if (n == 0 || k == 0) return SHIFTER_OK;
+    Q8GradientArgs a{};
+    a.g = d_g; a.q = d_q; a.s = d_scale; a.mask = d_mask;
+    a.ld_g = ld_g; a.ld_q = ld_q; a.ld_mask = ld_mask; a.ld_dw = ld_dw;
+    a.m = (uint32_t)m; a.n = (uint32_t)n; a.k = (uint32_t)k; a.dw = d_dw;
+    a.accumulate = (flags & SHIFTER_Q8_ACCUMULATE) != 0;
+    a.work = static_cast<uint8_t*>(d_work);
+    launch_q8_gradient(ctx, dtype, a);
+    return after_launch(ctx, "weight_grad_q8");
 }

@@ -173,6 +173,7 @@ enum KernelId {
     K_DEFLATE_CHUNK, K_CODEC_SCAN, K_CODEC_PACK, K_INFLATE_CHUNK,
     K_MASK_SCAN_BATCH, K_EXPAND_LEVELS,
     K_SPEC_SAMPLE, K_SPEC_PASS, K_SPEC_FINISH, K_SPEC_FINISH2, K_SPEC_FIXUP,
+    K_Q8_ROWS, K_Q8_READ, K_Q8_NORM, K_Q8_PRODUCT, K_Q8_DIGITS, K_Q8_GRADIENT,
     K_COUNT
 };
 extern const char* const kKernelNames[K_COUNT];

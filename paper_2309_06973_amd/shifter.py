@@ -118,6 +118,21 @@ EXPORTS = {
     "shifter_inflate": [C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p, C.c_void_p, C.c_void_p,
                         C.c_uint64, C.c_void_p, C.c_int],
     "shifter_codec_status": [C.c_void_p, C.POINTER(C.c_uint64), C.POINTER(C.c_uint32)],
+    "shifter_quantize_q8": [C.c_void_p, C.c_void_p, C.c_int, C.c_uint64, C.c_uint64, C.c_uint64,
+                            C.c_uint32, C.c_void_p, C.c_uint64, C.c_void_p],
+    "shifter_dequantize_q8": [C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p, C.c_uint64,
+                              C.c_uint64, C.c_void_p, C.c_int, C.c_uint64],
+    "shifter_rms_norm_q8": [C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p, C.c_uint64, C.c_int,
+                            C.c_uint64, C.c_uint64, C.c_void_p, C.c_float, C.c_void_p, C.c_uint64,
+                            C.c_void_p, C.c_uint64, C.c_void_p],
+    "shifter_matmul_q8": [C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p, C.c_void_p, C.c_uint64,
+                          C.c_void_p, C.c_uint64, C.c_uint64, C.c_uint64, C.c_void_p, C.c_uint32,
+                          C.c_void_p, C.c_int, C.c_uint64],
+    "shifter_weight_grad_q8_layout": [C.c_uint64, C.c_uint64, C.c_uint64, C.POINTER(C.c_uint64)],
+    "shifter_weight_grad_q8": [C.c_void_p, C.c_void_p, C.c_int, C.c_uint64, C.c_void_p, C.c_uint64,
+                               C.c_void_p, C.c_uint64, C.c_uint64, C.c_uint64, C.c_void_p,
+                               C.c_uint64, C.c_uint32, C.c_void_p, C.c_uint64, C.c_void_p,
+                               C.c_uint64],
     "shifter_apply_mask": [C.c_void_p] * 8,
     "shifter_dead_channel_scan": [C.c_void_p] * 5,
     "shifter_propagate_groups": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint32,
@@ -426,6 +441,58 @@ def shifter_codec_status(ctx: Context):
     total, bad = C.c_uint64(), C.c_uint32()
     _check(load_library().shifter_codec_status(ctx.handle, C.byref(total), C.byref(bad)), ctx.handle)
     return int(total.value), bool(bad.value)
+
+
+SHIFTER_F32, SHIFTER_BF16, SHIFTER_F16 = 0, 1, 2
+SHIFTER_Q8_RELU = 1
+SHIFTER_Q8_ACCUMULATE = 2
+SHIFTER_Q8_MAX_SUM = 131071
+SHIFTER_Q8_ALIGN = 16
+
+
+def shifter_quantize_q8(ctx: Context, d_x, dtype: int, ld_x: int, rows: int, cols: int, flags: int,
+                        d_q, ld_q: int, d_scale) -> None:
+    """Rows of ``d_x`` (dtype one of SHIFTER_F32, _BF16, _F16) as an 8-bit matrix."""
+    _check(load_library().shifter_quantize_q8(ctx.handle, _ptr(d_x), dtype, ld_x, rows, cols, flags,
+                                              _ptr(d_q), ld_q, _ptr(d_scale)), ctx.handle)
+
+
+def shifter_dequantize_q8(ctx: Context, d_q, ld_q: int, d_scale, rows: int, cols: int, d_x,
+                          dtype: int, ld_x: int) -> None:
+    _check(load_library().shifter_dequantize_q8(ctx.handle, _ptr(d_q), ld_q, _ptr(d_scale), rows,
+                                                cols, _ptr(d_x), dtype, ld_x), ctx.handle)
+
+
+def shifter_rms_norm_q8(ctx: Context, d_x, ld_x: int, d_residual, ld_r: int, dtype: int, rows: int,
+                        cols: int, d_weight, eps: float, d_h, ld_h: int, d_q, ld_q: int,
+                        d_scale) -> None:
+    """d_residual and d_h: both, or None."""
+    _check(load_library().shifter_rms_norm_q8(ctx.handle, _ptr(d_x), ld_x, _ptr(d_residual), ld_r,
+                                              dtype, rows, cols, _ptr(d_weight), eps, _ptr(d_h),
+                                              ld_h, _ptr(d_q), ld_q, _ptr(d_scale)), ctx.handle)
+
+
+def shifter_matmul_q8(ctx: Context, d_qa, ld_a: int, d_sa, d_qb, ld_b: int, d_sb, m: int, n: int,
+                      k: int, d_bias, flags: int, d_c, dtype: int, ld_c: int) -> None:
+    _check(load_library().shifter_matmul_q8(ctx.handle, _ptr(d_qa), ld_a, _ptr(d_sa), _ptr(d_qb),
+                                            ld_b, _ptr(d_sb), m, n, k, _ptr(d_bias), flags,
+                                            _ptr(d_c), dtype, ld_c), ctx.handle)
+
+
+def shifter_weight_grad_q8_layout(m: int, n: int, k: int) -> int:
+    """Bytes of workspace that shifter_weight_grad_q8 takes for these sizes."""
+    out = C.c_uint64()
+    _check(load_library().shifter_weight_grad_q8_layout(m, n, k, C.byref(out)))
+    return int(out.value)
+
+
+def shifter_weight_grad_q8(ctx: Context, d_g, dtype: int, ld_g: int, d_q, ld_q: int, d_scale,
+                           m: int, n: int, k: int, d_mask, ld_mask: int, flags: int, d_dw,
+                           ld_dw: int, d_work, work_bytes: int) -> None:
+    _check(load_library().shifter_weight_grad_q8(ctx.handle, _ptr(d_g), dtype, ld_g, _ptr(d_q),
+                                                 ld_q, _ptr(d_scale), m, n, k, _ptr(d_mask),
+                                                 ld_mask, flags, _ptr(d_dw), ld_dw, _ptr(d_work),
+                                                 work_bytes), ctx.handle)
 
 
 def shifter_portfolio_begin(ctx: Context, model: Model, d_w, d_vecs, n_prune: Sequence[int],
