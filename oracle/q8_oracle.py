@@ -60,8 +60,8 @@ def rms_norm(x, weight, eps, residual=None):
 
 
 def product(qa, sa, qb, sb, bias=None, relu=False):
-    """(result in 64 bits, its magnitude before the bias): whole-number sums."""
-    s = qa.astype(np.int64) @ qb.astype(np.int64).T
+    """(result in 64 bits, its magnitude before the bias): whole-number sums, exact in float64."""
+    s = qa.astype(np.float64) @ qb.astype(np.float64).T
     c = s * sa.astype(np.float64)[:, None] * sb.astype(np.float64)
     mag = np.abs(c)
     if bias is not None:

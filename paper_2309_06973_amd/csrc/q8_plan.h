@@ -43,6 +43,50 @@ inline const char* q8_bad_codes(const void* q, const void* scale, uint64_t rows,
     return nullptr;
 }
 
+// The product's kernels.  Tiles of rows x columns, a block each; Q8_FEW: no tiles, the weights are read straight into
+// registers by blocks of 16 columns and all rows.
+enum Q8Kernel { Q8_FEW, Q8_TILE_64x64, Q8_TILE_64x128, Q8_TILE_128x256, Q8_TILE_256x256, Q8_KERNELS };
+struct Q8TileCost {
+    uint32_t rows, cols;
+    double start, alone, full;    // us: a launch and a tile's ends; a stage of 128 bytes on an empty chip, on a full one
+    bool shared;                  // two blocks to a compute unit: rounds are no whole numbers
+};
+// Measured on 256 compute units, us a call by kernel (the four tiles):
+//    m x n x k            64x64   64x128  128x256  256x256         m x n x k           64x64   64x128  128x256  256x256
+//    128 x 4096 x 4096     10.2     13.1     29.3     40.3         2048 x 2048 x 2048   18.9     17.8     18.5     26.1
+//    512 x 4096 x 4096     17.7     15.7     29.3     41.3         4096 x 2048 x 2048   33.2     27.7     22.6     29.4
+//    1024 x 4096 x 4096    32.1     26.6     30.8     42.7         4096 x 4096 x 4096    115       90       79       62
+//    2048 x 4096 x 4096    60.9     47.5     38.0     48.6         4096 x 1024 x 8192   57.9     44.5     55.1     77.3
+//    777 x 1873 x 977       7.1      6.9     11.5     17.4         16384 x 100 x 2048   12.7     11.1     18.1     26.8
+// The costs below say these within 15 %; the kernel of the least cost is taken.
+constexpr Q8TileCost Q8_TILES[] = {{64, 64, 3.2, 0.215, 0.235, true},
+                                   {64, 128, 3.5, 0.30, 0.375, true},
+                                   {128, 256, 5.0, 0.76, 1.03, false},
+                                   {256, 256, 7.0, 1.04, 1.72, false}};
+constexpr double Q8_UNITS = 256.0;      // compute units
+
+inline double q8_tile_us(const Q8TileCost& c, uint64_t m, uint64_t n, uint64_t k) {
+    const double tiles = (double)((m + c.rows - 1u) / c.rows) * (double)((n + c.cols - 1u) / c.cols);
+    const double stages = (double)((k + 127u) / 128u), share = tiles < Q8_UNITS ? tiles / Q8_UNITS : 1.0;
+    double rounds = tiles / Q8_UNITS;
+    if (!c.shared && rounds > 1.0) rounds = (double)((uint64_t)((tiles + Q8_UNITS - 1.0) / Q8_UNITS));
+    return c.start + stages * (c.alone + (c.full - c.alone) * share) * (rounds < 1.0 ? 1.0 : rounds);
+}
+
+// Up to 16 rows the reading of the weights is all there is, and the kernel without LDS does it best: 1 x 4096 x 4096 5.4 us
+// against 9.8 with tiles, 1 x 256 x 8192 6.4 / 16.3, 1 x 8192 x 8192 13.5 / 16.6.  Its blocks read all of A: up to 48 rows it still
+// wins where the weights are few (17 x 1000 x 1000 4.0 / 4.7, 32 x 4096 x 4096 8.3 / 10.0, 48 x 3541 x 3277 7.5 / 9.4; but
+// 32 x 8192 x 8192 24.1 / 16.8, 64 x 4096 x 4096 12.2 / 10.1).
+constexpr uint64_t Q8_FEW_ROWS = 16, Q8_FEW_ROWS_MOST = 48, Q8_FEW_WEIGHTS = 1ull << 24;
+
+inline Q8Kernel q8_kernel_for(uint64_t m, uint64_t n, uint64_t k) {
+    if (m <= Q8_FEW_ROWS || (m <= Q8_FEW_ROWS_MOST && n * k <= Q8_FEW_WEIGHTS)) return Q8_FEW;
+    int best = 0;
+    for (int i = 1; i < 4; ++i)
+        if (q8_tile_us(Q8_TILES[i], m, n, k) < q8_tile_us(Q8_TILES[best], m, n, k)) best = i;
+    return (Q8Kernel)(Q8_TILE_64x64 + best);
+}
+
 // The gradient's workspace: the largest |g s| of every column by slices of rows, then the columns' three
 // planes of digits, then the codes, both with the rows of a call side by side.
 constexpr uint32_t Q8_SLICES = 64;

@@ -11,6 +11,7 @@
 // with the same Q give the sum to fp32 accuracy at 1.5 times the cost of one bf16 product (the
 // matrix units take 8-bit integers twice as fast), where fp32 products run at a sixteenth.
 #include <algorithm>
+#include <type_traits>
 
 #include "dev_common.h"
 #include "q8.h"
@@ -20,7 +21,6 @@ namespace shifter {
 typedef int v4i __attribute__((ext_vector_type(4)));
 typedef int v16i __attribute__((ext_vector_type(16)));
 
-constexpr uint32_t STEP = 128;     // bytes of a row per stage
 constexpr uint32_t UNIT = 16;      // bytes a lane moves
 
 // 16 bytes a lane from global memory to LDS: lane l's go to base + 16 l, base the same in all lanes.
@@ -30,19 +30,37 @@ __device__ __forceinline__ void to_lds(const int8_t* from, int8_t* base) {
     __builtin_amdgcn_global_load_lds((gptr*)from, (lptr*)base, 16, 0, 0);
 }
 
+// Waits until at most N of this wavefront's moves are under way, and until its LDS reads are done.
+template <uint32_t N>
+__device__ __forceinline__ void wait_moves() {
+    static_assert(N < 64, "six bits");
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((N & 15u) | (N >> 4) << 14 | 7u << 4);      // a builtin: the compiler knows what is done
+    asm volatile("" ::: "memory");
+}
+
 // The tiled loop: WA x WB wavefronts, each with FA x FB tiles of 32 x 32 (FA for each of P planes of A).
 // A stage holds STEP bytes of every row of the block's tile, the 16-byte units of a row permuted by its
-// number so that the 8 lanes that LDS serves at once read 8 different units.
-template <uint32_t P, uint32_t WA, uint32_t WB, uint32_t FA, uint32_t FB>
+// number so that 16 lanes of a read meet 64 different banks.  NS stages are in LDS or on their
+// way to it.  A stage is worked off in steps of 32 bytes, whose operands are read one step
+// ahead: the first ones of the next stage before the last step of this one, behind the stage's only barrier.
+template <uint32_t P, uint32_t WA, uint32_t WB, uint32_t FA, uint32_t FB, uint32_t NS, uint32_t STEP>
 struct Tile {
+    static constexpr uint32_t UNITS = STEP / UNIT, STEPS = STEP / 32;
+    static constexpr uint32_t COLS = 32 * FB;                            // columns of a wavefront
     static constexpr uint32_t THREADS = 64 * WA * WB;
     static constexpr uint32_t RA = 32 * WA * FA, RB = 32 * WB * FB;      // rows of A (per plane) and of B
     static constexpr uint32_t ROWS = P * RA + RB;
     static constexpr uint32_t BYTES = ROWS * STEP;
-    static constexpr uint32_t PER = ROWS * (STEP / UNIT) / THREADS;      // units a thread moves per stage
-    static constexpr uint32_t PASS = THREADS / (STEP / UNIT);            // rows per pass of all threads
-    static_assert(ROWS * (STEP / UNIT) % THREADS == 0 && RA % PASS == 0 && RB % PASS == 0, "whole passes");
+    static constexpr uint32_t LDS = NS * BYTES;
+    static constexpr uint32_t PER = ROWS * UNITS / THREADS;              // units a thread moves per stage
+    static constexpr uint32_t PASS = THREADS / UNITS;                    // rows per pass of all threads
+    // a row's turn: rows that share the 256 bytes of all banks have the same one
+    __device__ __forceinline__ static uint32_t turn_of(uint32_t row) { return row / (256u / STEP) & (UNITS - 1u); }
+    static_assert(STEPS % 2 == 0 && PASS % 16 == 0 && ROWS * UNITS % THREADS == 0 && RA % PASS == 0 && RB % PASS == 0, "whole passes");
     v16i acc[P][FA][FB];
+
+    struct Operands { v4i a[P][FA], b[FB]; };
 
     // a, b: first rows of the block; rows_a, rows_b: how many of them there are (1 at least); k: bytes of a row
     __device__ __forceinline__ void run(const int8_t* a, uint64_t ld_a, uint64_t plane, uint32_t rows_a,
@@ -58,8 +76,8 @@ struct Tile {
         if (k == 0) return;
         const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = uniform_u32(tid >> 6);
         const uint32_t wa = wave % WA, wb = wave / WA;
-        const uint32_t row_in_pass = tid / (STEP / UNIT);
-        const uint32_t unit = ((tid % (STEP / UNIT)) ^ (row_in_pass & 7u)) * UNIT;    // PASS is a multiple of 8
+        const uint32_t row_in_pass = tid / UNITS;
+        const uint32_t unit = ((tid % UNITS) ^ turn_of(row_in_pass)) * UNIT;    // PASS is a multiple of 16
         const uint32_t pad = (k + UNIT - 1u) & ~(UNIT - 1u);
         const uint32_t stages = (k + STEP - 1u) / STEP;
         uint32_t off[PER];
@@ -70,58 +88,96 @@ struct Tile {
             off[j] = j * PASS < P * RA ? min(r % RA, rows_a - 1u) * (uint32_t)ld_a
                                        : min(r - P * RA, rows_b - 1u) * (uint32_t)ld_b;
         }
-        auto fetch = [&](uint32_t s, int8_t* to) {
+        auto fetch = [&](uint32_t s, uint32_t buf) {
             const uint32_t at = s * STEP;
             const uint32_t u = at + min(unit, pad - UNIT - at);
 #pragma unroll
             for (uint32_t j = 0; j < PER; ++j) {
                 const int8_t* base = j * PASS < P * RA ? a + (uint64_t)(j * PASS / RA) * plane : b;
-                to_lds(base + (uint64_t)(off[j] + u), to + (j * THREADS + wave * 64u) * UNIT);
+                to_lds(base + (uint64_t)(off[j] + u), lds + buf + (j * THREADS + wave * 64u) * UNIT);
             }
         };
         const uint32_t half = lane >> 5;
-        const uint32_t turn = (half ^ (lane & 7u)) * UNIT;
+        const uint32_t turn = (half ^ turn_of(lane & 31u)) * UNIT;
         const int8_t* lane_a = lds + (wa * FA * 32u + (lane & 31u)) * STEP;
         const int8_t* lane_b = lds + (P * RA + wb * FB * 32u + (lane & 31u)) * STEP;
-        fetch(0, lds);
-        for (uint32_t s = 0; s < stages; ++s) {
-            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");   // this wavefront's part has come, its reads are done
-            __builtin_amdgcn_s_barrier();          // the stage is there, and the other half is free
-            asm volatile("" ::: "memory");
-            if (s + 1u < stages) fetch(s + 1u, lds + ((s + 1u) & 1u) * BYTES);
-            const uint32_t buf = (s & 1u) * BYTES;
-            const uint32_t left = k - s * STEP;
+        auto read = [&](Operands& o, uint32_t buf, uint32_t x) {
+            const uint32_t at = buf + (turn ^ (x * 32u));
 #pragma unroll
-            for (uint32_t x = 0; x < STEP / 32u; ++x) {
-                const uint32_t at = buf + (turn ^ (x * 32u));
-                v4i fa[P][FA], fb[FB];
+            for (uint32_t j = 0; j < FB; ++j) o.b[j] = *reinterpret_cast<const v4i*>(lane_b + at + j * 32u * STEP);
 #pragma unroll
-                for (uint32_t j = 0; j < FB; ++j) fb[j] = *reinterpret_cast<const v4i*>(lane_b + at + j * 32u * STEP);
+            for (uint32_t p = 0; p < P; ++p)
 #pragma unroll
-                for (uint32_t p = 0; p < P; ++p)
+                for (uint32_t i = 0; i < FA; ++i)
+                    o.a[p][i] = *reinterpret_cast<const v4i*>(lane_a + at + (p * RA + i * 32u) * STEP);
+        };
+        auto multiply = [&](const Operands& o) {
 #pragma unroll
-                    for (uint32_t i = 0; i < FA; ++i)
-                        fa[p][i] = *reinterpret_cast<const v4i*>(lane_a + at + (p * RA + i * 32u) * STEP);
-                if (left < STEP) {                 // bytes behind the row's end count as zero in A
-                    const int32_t n = (int32_t)left - (int32_t)(x * 32u + half * UNIT);
+            for (uint32_t p = 0; p < P; ++p)
 #pragma unroll
-                    for (int32_t e = 0; e < 4; ++e) {
-                        const int32_t m = min(max(n - 4 * e, 0), 4);
-                        const int32_t keep = m == 4 ? -1 : (1 << (8 * m)) - 1;
+                for (uint32_t i = 0; i < FA; ++i)
 #pragma unroll
-                        for (uint32_t p = 0; p < P; ++p)
+                    for (uint32_t j = 0; j < FB; ++j)
+                        acc[p][i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(o.a[p][i], o.b[j], acc[p][i][j], 0, 0, 0);
+        };
+
 #pragma unroll
-                            for (uint32_t i = 0; i < FA; ++i) fa[p][i][e] &= keep;
-                    }
+        for (uint32_t s = 0; s < NS; ++s)
+            if (s < stages) fetch(s, s * BYTES);
+        Operands o[2];
+        if (stages >= NS) wait_moves<(NS - 1u) * PER>(); else wait_moves<0>();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        uint32_t buf = 0, s = 0;
+        read(o[0], 0, 0);
+        auto stage = [&](auto more) {              // more: there is a stage to be fetched
+            const uint32_t next = buf + BYTES == LDS ? 0u : buf + BYTES;
+#pragma unroll
+            for (uint32_t x = 0; x < STEPS; ++x) {
+                if (x + 1u < STEPS) {
+                    read(o[(x + 1) & 1], buf, x + 1);
+                } else {
+                    // the next stage's parts have come and this one's reads are done, in this wavefront and, behind
+                    // the barrier, in all: the buffer is free
+                    wait_moves<more.value ? (NS - 2u) * PER : 0u>();
+                    __builtin_amdgcn_s_barrier();
+                    asm volatile("" ::: "memory");
+                    read(o[0], next, 0);
+                    if (more.value) fetch(s + NS, buf);
                 }
+                multiply(o[x & 1]);
+                // one LDS read, then its share of the products, in turn
+                constexpr int READS = P * FA + FB, PRODUCTS = P * FA * FB;
 #pragma unroll
-                for (uint32_t p = 0; p < P; ++p)
-#pragma unroll
-                    for (uint32_t i = 0; i < FA; ++i)
-#pragma unroll
-                        for (uint32_t j = 0; j < FB; ++j)
-                            acc[p][i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fa[p][i], fb[j], acc[p][i][j], 0, 0, 0);
+                for (int z = 0; z < READS; ++z) {
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x8, PRODUCTS / READS, 0);
+                }
+                __builtin_amdgcn_sched_group_barrier(0x8, PRODUCTS % READS, 0);
+                __builtin_amdgcn_sched_barrier(0);
             }
+            buf = next;
+        };
+        for (; s + NS < stages; ++s) stage(std::true_type{});
+        for (; s + 1u < stages; ++s) stage(std::false_type{});
+        const uint32_t left = k - (stages - 1u) * STEP;      // bytes of the last stage, 1 at least
+#pragma unroll
+        for (uint32_t x = 0; x < STEPS; ++x) {
+            if (x * 32u >= left) break;
+            if (x + 1u < STEPS) read(o[(x + 1) & 1], buf, x + 1);
+            if (left < x * 32u + 32u) {                      // bytes behind the row's end count as zero in A
+                const int32_t n = (int32_t)left - (int32_t)(x * 32u + half * UNIT);
+#pragma unroll
+                for (int32_t e = 0; e < 4; ++e) {
+                    const int32_t m = min(max(n - 4 * e, 0), 4);
+                    const int32_t keep = m == 4 ? -1 : (1 << (8 * m)) - 1;
+#pragma unroll
+                    for (uint32_t p = 0; p < P; ++p)
+#pragma unroll
+                        for (uint32_t i = 0; i < FA; ++i) o[x & 1].a[p][i][e] &= keep;
+                }
+            }
+            multiply(o[x & 1]);
         }
     }
 
@@ -136,40 +192,197 @@ struct Tile {
     }
 };
 
-template <typename T, uint32_t WA, uint32_t WB, uint32_t FA, uint32_t FB>
+// The tile of a block, of `tiles_a` x `tiles_b`: blocks go to the 8 chiplets in turn, and each of those takes a
+// run of tiles in bands of GROUP along a, so that the 32 tiles it works on share rows of both factors in its L2.
+template <uint32_t GROUP>
+__device__ __forceinline__ void tile_of_block(uint32_t tiles_a, uint32_t tiles_b, uint32_t* ta, uint32_t* tb) {
+    const uint32_t all = tiles_a * tiles_b, xcd = blockIdx.x % 8u, nth = blockIdx.x / 8u;
+    const uint32_t each = all / 8u, more = all % 8u;
+    const uint32_t t = xcd * each + min(xcd, more) + nth;
+    const uint32_t band = t / (GROUP * tiles_b), in = t - band * GROUP * tiles_b;
+    const uint32_t high = min(GROUP, tiles_a - band * GROUP);
+    *tb = in / high;
+    *ta = band * GROUP + in - *tb * high;
+}
+
+// Writes a wavefront's 32 rows x COLS values of LDS (rows `pitch` bytes apart) to c: 16 bytes a lane, rows and
+// columns behind the matrix' end left out.
+template <typename T, uint32_t COLS>
+__device__ __forceinline__ void store_rows(const int8_t* from, uint32_t pitch, T* c, uint64_t ld, uint32_t rows, uint32_t cols) {
+    constexpr uint32_t E = 16 / sizeof(T), LANES = COLS / E;             // elements of a lane, lanes of a row
+    typedef T vec __attribute__((ext_vector_type(E)));
+    typedef T loose __attribute__((ext_vector_type(E), aligned(sizeof(T))));
+    const uint32_t lane = threadIdx.x & 63u, n = lane % LANES * E;
+#pragma unroll
+    for (uint32_t r = lane / LANES; r < 32u; r += 64u / LANES) {
+        const vec v = *reinterpret_cast<const vec*>(from + r * pitch + n * sizeof(T));
+        if (r >= rows) continue;
+        T* to = c + (uint64_t)r * ld + n;
+        if (n + E <= cols) {
+            *reinterpret_cast<loose*>(to) = v;
+        } else {
+#pragma unroll
+            for (uint32_t i = 0; i < E; ++i)
+                if (n + i < cols) to[i] = v[i];
+        }
+    }
+}
+
+template <typename T, uint32_t WA, uint32_t WB, uint32_t FA, uint32_t FB, uint32_t NS, uint32_t STEP, uint32_t GROUP>
 __global__ __launch_bounds__(64 * WA * WB) void q8_product_kernel(Q8ProductArgs g) {
-    using Tl = Tile<1, WA, WB, FA, FB>;
-    extern __shared__ __align__(16) int8_t lds[];
-    const uint32_t tiles_m = (g.m + Tl::RA - 1u) / Tl::RA;
-    const uint32_t m0 = (blockIdx.x % tiles_m) * Tl::RA, n0 = (blockIdx.x / tiles_m) * Tl::RB;
-    Tl t;
-    t.run(g.a + (uint64_t)m0 * g.ld_a, g.ld_a, 0, g.m - m0, g.b + (uint64_t)n0 * g.ld_b, g.ld_b, g.n - n0, g.k, lds);
-    T* c = static_cast<T*>(g.c);
+    using Tl = Tile<1, WA, WB, FA, FB, NS, STEP>;
+    constexpr uint32_t PITCH = Tl::COLS * sizeof(T) + 16u;               // of the results' rows, in bytes
+    constexpr uint32_t OUT = WA * WB * 32u * PITCH;
+    constexpr uint32_t BEHIND = OUT + 4u * Tl::RA;                       // the tokens' scales lie behind them
+    __shared__ __align__(16) int8_t lds[Tl::LDS > BEHIND ? Tl::LDS : BEHIND];
+    static_assert(Tl::THREADS >= Tl::RA, "a scale a thread");
+    uint32_t ta, tb;
+    tile_of_block<GROUP>((g.m + Tl::RA - 1u) / Tl::RA, (g.n + Tl::RB - 1u) / Tl::RB, &ta, &tb);
+    const uint32_t m0 = ta * Tl::RA, n0 = tb * Tl::RB;
+    const float mine = g.sa[min(m0 + threadIdx.x % Tl::RA, g.m - 1u)];
+    float sb[FB], bias[FB];
 #pragma unroll
     for (uint32_t j = 0; j < FB; ++j) {
-        const uint32_t n = n0 + Tl::col(j);
-        if (n >= g.n) continue;
-        const float sb = g.sb[n], bias = g.bias ? g.bias[n] : 0.0f;
-#pragma unroll
-        for (uint32_t i = 0; i < FA; ++i)
-#pragma unroll
-            for (uint32_t e = 0; e < 16; ++e) {
-                const uint32_t m = m0 + Tl::row(i, e);
-                if (m >= g.m) continue;
-                // the token's scale first: the product of both could leave the range that their values stay in
-                float v = fmaf((float)t.acc[0][i][j][e] * g.sa[m], sb, bias);
-                if (g.relu) v = v < 0.0f ? 0.0f : v;
-                c[(uint64_t)m * g.ld_c + n] = (T)v;
-            }
+        const uint32_t n = min(n0 + Tl::col(j), g.n - 1u);
+        sb[j] = g.sb[n];
+        bias[j] = g.bias ? g.bias[n] : 0.0f;
     }
+    Tl t;
+    t.run(g.a + (uint64_t)m0 * g.ld_a, g.ld_a, 0, g.m - m0, g.b + (uint64_t)n0 * g.ld_b, g.ld_b, g.n - n0, g.k, lds);
+    // results go through LDS, each wavefront by itself, so that rows are written in long pieces
+    __syncthreads();
+    float* s_a = reinterpret_cast<float*>(lds + OUT);
+    if (threadIdx.x < Tl::RA) s_a[threadIdx.x] = mine;
+    __syncthreads();
+    const uint32_t lane = threadIdx.x & 63u;
+    int8_t* out = lds + uniform_u32(threadIdx.x >> 6) * 32u * PITCH;
+    T* c = static_cast<T*>(g.c);
+#pragma unroll
+    for (uint32_t i = 0; i < FA; ++i) {
+        const uint32_t first = Tl::row(i, 0) - 4u * (lane >> 5), m = m0 + first, n = n0 + Tl::col(0) - (lane & 31u);
+#pragma unroll
+        for (uint32_t e4 = 0; e4 < 4; ++e4) {
+            const float4 sa = *reinterpret_cast<const float4*>(&s_a[Tl::row(i, 4 * e4)]);
+            const float s[4] = {sa.x, sa.y, sa.z, sa.w};
+#pragma unroll
+            for (uint32_t e = 0; e < 4; ++e)
+#pragma unroll
+                for (uint32_t j = 0; j < FB; ++j) {
+                    // the token's scale first: the product of both could leave the range that their values stay in
+                    float v = fmaf((float)t.acc[0][i][j][4 * e4 + e] * s[e], sb[j], bias[j]);
+                    if (g.relu) v = v < 0.0f ? 0.0f : v;
+                    *reinterpret_cast<T*>(out + (8u * e4 + 4u * (lane >> 5) + e) * PITCH + (j * 32u + (lane & 31u)) * sizeof(T)) = (T)v;
+                }
+        }
+        __builtin_amdgcn_wave_barrier();       // a wavefront's LDS accesses are done in order
+        if (m < g.m && n < g.n)
+            store_rows<T, Tl::COLS>(out, PITCH, c + (uint64_t)m * g.ld_c + n, g.ld_c, g.m - m, g.n - n);
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+template <typename T, uint32_t WA, uint32_t WB, uint32_t FA, uint32_t FB, uint32_t NS, uint32_t STEP, uint32_t GROUP>
+static void launch_product_as(shifter_ctx* ctx, const Q8ProductArgs& g) {
+    using Tl = Tile<1, WA, WB, FA, FB, NS, STEP>;
+    const uint64_t tiles = (uint64_t)((g.m + Tl::RA - 1u) / Tl::RA) * ((g.n + Tl::RB - 1u) / Tl::RB);
+    q8_product_kernel<T, WA, WB, FA, FB, NS, STEP, GROUP><<<(uint32_t)tiles, Tl::THREADS, 0, ctx->stream>>>(g);
+}
+
+// Few tokens: the weights are read once, straight into registers, and that read is the time.  A block has 16
+// columns of the result and all of the up to 16 F tokens; its WAVES wavefronts take pieces of 128 bytes of the
+// rows in turn and join their sums in LDS.  (Weights are the first factor of the 16 x 16 x 64 products: a
+// lane then holds four neighbouring columns of one token.)
+template <typename T, uint32_t F, uint32_t WAVES>
+__global__ __launch_bounds__(64 * WAVES) void q8_product_few_kernel(Q8ProductArgs g) {
+    constexpr uint32_t PIECE = 128, DEPTH = 4;                           // bytes; pieces under way
+    __shared__ v4i s_sum[WAVES][F][64];
+    const uint32_t lane = threadIdx.x & 63u, wave = uniform_u32(threadIdx.x >> 6);
+    const uint32_t n0 = blockIdx.x * 16u, at = lane / 16u * UNIT;
+    const int8_t* b = g.b + (uint64_t)min(n0 + (lane & 15u), g.n - 1u) * g.ld_b;
+    const int8_t* a[F];
+#pragma unroll
+    for (uint32_t f = 0; f < F; ++f) a[f] = g.a + (uint64_t)min(16u * f + (lane & 15u), g.m - 1u) * g.ld_a;
+    v4i acc[F];
+#pragma unroll
+    for (uint32_t f = 0; f < F; ++f) acc[f] = v4i{0, 0, 0, 0};
+    const uint32_t whole = g.k / PIECE;
+    uint32_t p = wave;
+    for (; p + (DEPTH - 1u) * WAVES < whole; p += DEPTH * WAVES) {
+        v4i vb[DEPTH][2], va[DEPTH][F][2];
+#pragma unroll
+        for (uint32_t d = 0; d < DEPTH; ++d)
+#pragma unroll
+            for (uint32_t x = 0; x < 2; ++x) {
+                const uint32_t k = (p + d * WAVES) * PIECE + x * 64u + at;
+                vb[d][x] = *reinterpret_cast<const v4i*>(b + k);
+#pragma unroll
+                for (uint32_t f = 0; f < F; ++f) va[d][f][x] = *reinterpret_cast<const v4i*>(a[f] + k);
+            }
+#pragma unroll
+        for (uint32_t d = 0; d < DEPTH; ++d)
+#pragma unroll
+            for (uint32_t x = 0; x < 2; ++x)
+#pragma unroll
+                for (uint32_t f = 0; f < F; ++f)
+                    acc[f] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vb[d][x], va[d][f][x], acc[f], 0, 0, 0);
+    }
+    for (; p * PIECE < g.k; p += WAVES) {
+#pragma unroll
+        for (uint32_t x = 0; x < 2; ++x) {
+            const uint32_t k = p * PIECE + x * 64u + at;
+            const uint32_t from = min(k, (g.k - 1u) & ~(UNIT - 1u));     // behind the row's end: its last unit again
+            const v4i vb = *reinterpret_cast<const v4i*>(b + from);
+#pragma unroll
+            for (uint32_t f = 0; f < F; ++f) {
+                v4i va = *reinterpret_cast<const v4i*>(a[f] + from);
+#pragma unroll
+                for (int32_t e = 0; e < 4; ++e) {                        // bytes behind it count as zero
+                    const int32_t n = min(max((int32_t)g.k - (int32_t)k - 4 * e, 0), 4);
+                    va[e] &= n == 4 ? -1 : (1 << (8 * n)) - 1;
+                }
+                acc[f] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vb, va, acc[f], 0, 0, 0);
+            }
+        }
+    }
+#pragma unroll
+    for (uint32_t f = 0; f < F; ++f) s_sum[wave][f][lane] = acc[f];
+    __syncthreads();
+    static_assert(WAVES >= F, "a wavefront for 16 tokens' sums");
+    if (wave >= F) return;
+    const uint32_t m = wave * 16u + (lane & 15u), n = n0 + lane / 16u * 4u;
+    v4i sum = s_sum[0][wave][lane];
+#pragma unroll
+    for (uint32_t w = 1; w < WAVES; ++w) sum += s_sum[w][wave][lane];
+    if (m >= g.m) return;
+    const float sa = g.sa[m];
+    T* c = static_cast<T*>(g.c) + (uint64_t)m * g.ld_c + n;
+#pragma unroll
+    for (uint32_t e = 0; e < 4; ++e) {
+        if (n + e >= g.n) break;
+        float v = fmaf((float)sum[e] * sa, g.sb[n + e], g.bias ? g.bias[n + e] : 0.0f);
+        if (g.relu) v = v < 0.0f ? 0.0f : v;
+        c[e] = (T)v;
+    }
+}
+
+template <typename T, uint32_t F, uint32_t WAVES>
+static void launch_product_few(shifter_ctx* ctx, const Q8ProductArgs& g) {
+    q8_product_few_kernel<T, F, WAVES><<<(g.n + 15u) / 16u, 64 * WAVES, 0, ctx->stream>>>(g);
 }
 
 template <typename T>
 static void launch_product_of(shifter_ctx* ctx, const Q8ProductArgs& g) {
-    constexpr uint32_t WA = 2, WB = 2, FA = 1, FB = 1;
-    using Tl = Tile<1, WA, WB, FA, FB>;
-    const uint64_t tiles = (uint64_t)((g.m + Tl::RA - 1u) / Tl::RA) * ((g.n + Tl::RB - 1u) / Tl::RB);
-    q8_product_kernel<T, WA, WB, FA, FB><<<(uint32_t)tiles, Tl::THREADS, 2 * Tl::BYTES, ctx->stream>>>(g);
+    switch (q8_kernel_for(g.m, g.n, g.k)) {
+        case Q8_FEW:
+            if (g.m <= 16) launch_product_few<T, 1, 8>(ctx, g);
+            else if (g.m <= 32) launch_product_few<T, 2, 16>(ctx, g);
+            else launch_product_few<T, 3, 16>(ctx, g);
+            break;
+        case Q8_TILE_64x64: launch_product_as<T, 2, 2, 1, 1, 4, 128, 16>(ctx, g); break;
+        case Q8_TILE_64x128: launch_product_as<T, 2, 2, 1, 2, 3, 128, 8>(ctx, g); break;
+        case Q8_TILE_128x256: launch_product_as<T, 2, 4, 2, 2, 2, 128, 8>(ctx, g); break;
+        default: launch_product_as<T, 2, 4, 4, 2, 2, 128, 4>(ctx, g); break;
+    }
 }
 
 void launch_q8_product(shifter_ctx* ctx, int dtype, const Q8ProductArgs& g) {
@@ -266,10 +479,10 @@ __global__ __launch_bounds__(BLOCK) void q8_turn_kernel(Q8GradientArgs a, Q8Grad
     }
 }
 
-template <uint32_t WA, uint32_t WB, uint32_t FA, uint32_t FB>
+template <uint32_t WA, uint32_t WB, uint32_t FA, uint32_t FB, uint32_t NS>
 __global__ __launch_bounds__(64 * WA * WB) void q8_gradient_kernel(Q8GradientArgs g, Q8GradientPlan pl) {
-    using Tl = Tile<3, WA, WB, FA, FB>;
-    extern __shared__ __align__(16) int8_t lds[];
+    using Tl = Tile<3, WA, WB, FA, FB, NS, 128>;
+    __shared__ __align__(16) int8_t lds[Tl::LDS];
     const uint32_t tiles_n = (g.n + Tl::RA - 1u) / Tl::RA;
     const uint32_t n0 = (blockIdx.x % tiles_n) * Tl::RA, k0 = (blockIdx.x / tiles_n) * Tl::RB;
     const int8_t* digits = reinterpret_cast<const int8_t*>(g.work + pl.digits);
@@ -320,10 +533,10 @@ void launch_q8_gradient(shifter_ctx* ctx, int dtype, const Q8GradientArgs& g) {
         else launch_digits<_Float16>(ctx, g, pl);
     }
     ProfileScope ps(ctx, K_Q8_GRADIENT);
-    constexpr uint32_t WA = 2, WB = 2, FA = 1, FB = 1;
-    using Tl = Tile<3, WA, WB, FA, FB>;
+    constexpr uint32_t WA = 2, WB = 2, FA = 1, FB = 1, NS = 2;
+    using Tl = Tile<3, WA, WB, FA, FB, NS, 128>;
     const uint64_t tiles = (uint64_t)((g.n + Tl::RA - 1u) / Tl::RA) * ((g.k + Tl::RB - 1u) / Tl::RB);
-    q8_gradient_kernel<WA, WB, FA, FB><<<(uint32_t)tiles, Tl::THREADS, 2 * Tl::BYTES, ctx->stream>>>(g, pl);
+    q8_gradient_kernel<WA, WB, FA, FB, NS><<<(uint32_t)tiles, Tl::THREADS, 0, ctx->stream>>>(g, pl);
 }
 
 }  // namespace shifter

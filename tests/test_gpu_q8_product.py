@@ -73,7 +73,8 @@ def test_product_sums(ops, k):
 
 
 @pytest.mark.parametrize("m,n,k", [(1, 4096, 1000), (16, 2049, 640), (40, 515, 3000), (64, 1000, 999), (130, 1000, 999),
-                                   (300, 4000, 70), (1000, 1100, 300), (2100, 2300, 260), (5000, 20, 100), (3, 40000, 48)])
+                                   (300, 4000, 70), (1000, 1100, 300), (2100, 2300, 260), (5000, 20, 100), (3, 40000, 48),
+                                   (4000, 2047, 500), (4090, 4001, 1003)])
 def test_product_sizes(ops, m, n, k):
     for dtype in Q.DTYPES:
         check_product(ops, m, n, k, dtype, seed=m, bias=True, relu=dtype == "fp16")

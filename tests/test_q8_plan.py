@@ -69,6 +69,18 @@ int main() {
                 ok = ok && g.codes >= g.digits + 3 * n * g.ld && g.codes % 128 == 0 && g.bytes >= g.codes + k * g.ld;
                 if (!ok) { printf("plan of %llu %llu %llu\n", (unsigned long long)m, (unsigned long long)n, (unsigned long long)k); ++bad; }
             }
+    // kernels: few rows take the one without tiles, and every kernel is taken somewhere
+    int taken[Q8_KERNELS] = {0};
+    for (uint64_t m = 1; m <= 20000; m += 1 + m / 7)
+        for (uint64_t n = 1; n <= 20000; n += 1 + n / 5)
+            for (uint64_t k = 0; k <= Q8_MAX_K; k = k * 3 + 17) {
+                const Q8Kernel q = q8_kernel_for(m, n, k);
+                taken[q] += 1;
+                const bool few = m <= Q8_FEW_ROWS || (m <= Q8_FEW_ROWS_MOST && n * k <= Q8_FEW_WEIGHTS);
+                if (q >= Q8_KERNELS || (q == Q8_FEW) != few) { printf("kernel of %llu %llu %llu\n", (unsigned long long)m, (unsigned long long)n, (unsigned long long)k); ++bad; }
+            }
+    for (int q = 0; q < Q8_KERNELS; ++q) if (!taken[q]) { printf("kernel %d is never taken\n", q); ++bad; }
+    if (q8_kernel_for(8192, 8192, 8192) != Q8_TILE_256x256 || q8_kernel_for(128, 4096, 4096) != Q8_TILE_64x64) { printf("ends\n"); ++bad; }
     printf("%d bad\n", bad);
     return bad != 0;
 }
