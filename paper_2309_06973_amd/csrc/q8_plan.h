@@ -65,9 +65,10 @@ constexpr Q8TileCost Q8_TILES[] = {{64, 64, 3.2, 0.215, 0.235, true},
                                    {256, 256, 7.0, 1.04, 1.72, false}};
 constexpr double Q8_UNITS = 256.0;      // compute units
 
-inline double q8_tile_us(const Q8TileCost& c, uint64_t m, uint64_t n, uint64_t k) {
-    const double tiles = (double)((m + c.rows - 1u) / c.rows) * (double)((n + c.cols - 1u) / c.cols);
-    const double stages = (double)((k + 127u) / 128u), share = tiles < Q8_UNITS ? tiles / Q8_UNITS : 1.0;
+// us of a product of m x n sums over k bytes, each made by `parts` blocks.
+inline double q8_tile_us(const Q8TileCost& c, uint64_t m, uint64_t n, uint64_t k, uint64_t parts = 1) {
+    const double tiles = (double)((m + c.rows - 1u) / c.rows) * (double)((n + c.cols - 1u) / c.cols) * (double)parts;
+    const double stages = (double)(((k + 127u) / 128u + parts - 1u) / parts), share = tiles < Q8_UNITS ? tiles / Q8_UNITS : 1.0;
     double rounds = tiles / Q8_UNITS;
     if (!c.shared && rounds > 1.0) rounds = (double)((uint64_t)((tiles + Q8_UNITS - 1.0) / Q8_UNITS));
     return c.start + stages * (c.alone + (c.full - c.alone) * share) * (rounds < 1.0 ? 1.0 : rounds);
@@ -87,25 +88,57 @@ inline Q8Kernel q8_kernel_for(uint64_t m, uint64_t n, uint64_t k) {
     return (Q8Kernel)(Q8_TILE_64x64 + best);
 }
 
-// The gradient's workspace: the largest |g s| of every column by slices of rows, then the columns' three
-// planes of digits, then the codes, both with the rows of a call side by side.
-constexpr uint32_t Q8_SLICES = 64;
+// The gradient's workspace: the largest |g s| of every column by slices of rows and of all rows, then the columns'
+// three planes of digits, then the codes, both with the rows of a call side by side.
+constexpr uint32_t Q8_SLICES = 128, Q8_SLICE_ROWS = 32;      // most slices; a slice's rows are a multiple of the other
+// Up to so many rows a block that makes digits finds its columns' largest itself, one launch less; beyond, the rows
+// are read in slices for that first.
+constexpr uint32_t Q8_SELF_ROWS = 512;
+// The gradient's kernels, tiles of (columns of g) x (columns of the checkpoint), the costs as above.  Measured, us of the tiles' kernel:
+//    m x n x k             64x64   64x128   64x256  128x256         m x n x k             64x64   64x128   64x256  128x256
+//    16384 x 4096 x 4096     886      695      683      593         512 x 4096 x 1024      14.0     12.5     11.9     18.0
+//    2048 x 2048 x 2048     33.8     28.5     26.3     36.1         2048 x 1873 x 977      18.1     19.5     21.7     36.5
+//    16384 x 512 x 512      76.2     89.0      113      196         64 x 512 x 512          5.3      6.9      7.2     11.0
+enum Q8GradientKernel { Q8_GRAD_64x64, Q8_GRAD_64x128, Q8_GRAD_64x256, Q8_GRAD_128x256, Q8_GRAD_KERNELS };
+constexpr Q8TileCost Q8_GRAD_TILES[] = {{64, 64, 3.5, 0.57, 0.43, true},
+                                        {64, 128, 4.0, 0.67, 0.67, true},
+                                        {64, 256, 5.0, 0.85, 1.32, false},
+                                        {128, 256, 7.0, 1.50, 2.29, false}};
+// Where tiles are few the rows are split among `parts` blocks a tile; their sums, fp32, are joined by a launch of its own,
+// which costs that and the traffic.
+constexpr uint64_t Q8_PARTS = 32;
+constexpr double q8_join_us(uint64_t parts, uint64_t n, uint64_t k) {
+    return parts > 1 ? 3.5 + 2.0e-6 * (double)parts * (double)n * (double)k : 0.0;
+}
 struct Q8GradientPlan {
+    Q8GradientKernel kernel;
+    uint32_t parts, part_rows;                // blocks a tile, and the rows (a multiple of 128) that each has
     uint64_t ld;                              // bytes of a transposed row: the call's rows, rounded up to 128
-    uint32_t slices, slice_rows;
-    uint64_t tops, digits, codes, bytes;      // offsets, and the whole
+    uint32_t slices, slice_rows;              // 0 slices: up to Q8_SELF_ROWS rows
+    uint64_t tops, slice_tops, digits, codes, sums, bytes;      // offsets, and the whole
 };
 inline Q8GradientPlan q8_gradient_plan(uint64_t m, uint64_t n, uint64_t k) {
     Q8GradientPlan p;
     p.ld = (m + 127u) & ~(uint64_t)127u;
-    const uint64_t tiles = p.ld / 128u;                       // slices are whole tiles of 128 rows
-    const uint64_t per = (tiles + Q8_SLICES - 1u) / Q8_SLICES;
-    p.slice_rows = (uint32_t)(128u * (per ? per : 1u));
-    p.slices = (uint32_t)((m + p.slice_rows - 1u) / p.slice_rows);
+    const uint64_t per = (m + Q8_SLICES * Q8_SLICE_ROWS - 1u) / (Q8_SLICES * Q8_SLICE_ROWS);
+    p.slice_rows = (uint32_t)(Q8_SLICE_ROWS * (per ? per : 1u));
+    p.slices = m <= Q8_SELF_ROWS ? 0u : (uint32_t)((m + p.slice_rows - 1u) / p.slice_rows);
     p.tops = 0;
-    p.digits = (4u * n * p.slices + 255u) & ~(uint64_t)255u;
+    p.slice_tops = 4u * n;
+    p.digits = (p.slice_tops + 4u * n * p.slices + 255u) & ~(uint64_t)255u;
     p.codes = p.digits + 3u * n * p.ld;
-    p.bytes = p.codes + k * p.ld;
+    p.sums = p.codes + k * p.ld;
+    p.kernel = Q8_GRAD_64x64;
+    uint64_t parts = 1;
+    double least = 0.0;
+    for (int i = 0; i < Q8_GRAD_KERNELS; ++i)
+        for (uint64_t x = 1; x <= Q8_PARTS && (x == 1 || 2u * 128u * x <= p.ld); x *= 2) {
+            const double us = q8_tile_us(Q8_GRAD_TILES[i], n, k, m, x) + q8_join_us(x, n, k);
+            if ((i == 0 && x == 1) || us < least) { least = us; p.kernel = (Q8GradientKernel)i; parts = x; }
+        }
+    p.part_rows = (uint32_t)((p.ld / 128u + parts - 1u) / parts * 128u);
+    p.parts = p.ld ? (uint32_t)((p.ld + p.part_rows - 1u) / p.part_rows) : 1u;
+    p.bytes = m ? p.sums + (p.parts > 1 ? 4u * (uint64_t)p.parts * n * k : 0u) : 0u;
     return p;
 }
 

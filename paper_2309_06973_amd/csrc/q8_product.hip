@@ -401,127 +401,331 @@ constexpr float DIGITS_TOP = 8355711.0f;     // 127 * (2^16 + 2^8 + 1): the larg
 __device__ __forceinline__ float digits_up(float c) { return c < 0x1p-90f ? 0x1p90f : 1.0f; }
 __device__ __forceinline__ float digits_down(float c) { return c < 0x1p-90f ? 0x1p-90f : 1.0f; }
 
-// p = fl(g s) as 32 bits of magnitude: the order of |p|, with infinity and NaN on top.
+// Eight neighbours of a row, zeros behind the n that there are.
 template <typename T>
-__device__ __forceinline__ float scaled(const T* g, float s) { return __fmul_rn((float)*g, s); }
+__device__ __forceinline__ void load_up_to_8(const T* p, uint32_t n, float (&f)[8]) {
+    typedef T vec __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+    if (n >= 8u) {
+        const vec v = *reinterpret_cast<const vec*>(p);
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) f[i] = (float)v[i];
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) f[i] = i < n ? (float)p[i] : 0.0f;
+    }
+}
 
-// Largest |p| of every column over a slice of rows.  One column a thread.
+// Four words of four bytes, turned: byte i of word j becomes byte j of word i.
+__device__ __forceinline__ void turn_bytes(uint32_t& a, uint32_t& b, uint32_t& c, uint32_t& d) {
+    const uint32_t ab0 = __builtin_amdgcn_perm(b, a, 0x05010400u), ab1 = __builtin_amdgcn_perm(b, a, 0x07030602u);
+    const uint32_t cd0 = __builtin_amdgcn_perm(d, c, 0x05010400u), cd1 = __builtin_amdgcn_perm(d, c, 0x07030602u);
+    a = __builtin_amdgcn_perm(cd0, ab0, 0x05040100u);
+    b = __builtin_amdgcn_perm(cd0, ab0, 0x07060302u);
+    c = __builtin_amdgcn_perm(cd1, ab1, 0x05040100u);
+    d = __builtin_amdgcn_perm(cd1, ab1, 0x07060302u);
+}
+
+constexpr uint32_t TURN_ROWS = 128, TURN_PITCH = TURN_ROWS / 4 + 1;      // words of a turned row in LDS
+
+// `rows` turned rows of 128 bytes from LDS to memory, 16 bytes a thread.
+__device__ __forceinline__ void store_turned(const uint32_t* s, uint32_t rows, int8_t* to, uint64_t ld) {
+    for (uint32_t i = threadIdx.x; i < rows * 8u; i += BLOCK) {
+        const uint32_t* w = s + (i / 8u) * TURN_PITCH + (i & 7u) * 4u;
+        *reinterpret_cast<uint4*>(to + (uint64_t)(i / 8u) * ld + (i & 7u) * 16u) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+// 128 columns and 128 rows of the checkpoint, turned: a thread has 16 columns of four rows.
+__device__ __forceinline__ void turn_codes(const Q8GradientArgs& a, const Q8GradientPlan& pl, uint32_t block, uint32_t* lds) {
+    const uint32_t across = (a.k + 127u) / 128u, k0 = block % across * 128u, m0 = block / across * TURN_ROWS;
+    const uint32_t kg = threadIdx.x & 7u, rg = threadIdx.x >> 3, k = k0 + kg * 16u;
+    uint32_t w[4][4];                                                    // [row][word of its columns]
+#pragma unroll
+    for (uint32_t r = 0; r < 4; ++r) {
+        const uint32_t m = m0 + rg * 4u + r;
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (m < a.m && k < a.k) v = *reinterpret_cast<const uint4*>(a.q + (uint64_t)m * a.ld_q + k);
+        w[r][0] = v.x; w[r][1] = v.y; w[r][2] = v.z; w[r][3] = v.w;
+    }
+#pragma unroll
+    for (uint32_t x = 0; x < 4; ++x) {
+        turn_bytes(w[0][x], w[1][x], w[2][x], w[3][x]);
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) lds[(kg * 16u + x * 4u + i) * TURN_PITCH + rg] = w[i][x];
+    }
+    __syncthreads();
+    store_turned(lds, min(128u, a.k - k0), reinterpret_cast<int8_t*>(a.work + pl.codes) + (uint64_t)k0 * pl.ld + m0, pl.ld);
+}
+static uint32_t turn_blocks(const Q8GradientArgs& a, const Q8GradientPlan& pl) {
+    return (a.k + 127u) / 128u * (uint32_t)(pl.ld / TURN_ROWS);
+}
+
+// Largest |p| of eight columns over the rows from r0 on, every `step`-th.  As magnitudes' bits: infinity and NaN are on top.
 template <typename T>
-__global__ __launch_bounds__(BLOCK) void q8_tops_kernel(Q8GradientArgs a, uint32_t slice_rows, uint32_t* __restrict__ tops) {
-    const uint32_t n = blockIdx.x * BLOCK + threadIdx.x, r0 = blockIdx.y * slice_rows;
+__device__ __forceinline__ void column_tops(const Q8GradientArgs& a, uint32_t n, uint32_t r0, uint32_t r1, uint32_t step, uint32_t (&top)[8]) {
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) top[i] = 0;
     if (n >= a.n) return;
-    const T* g = static_cast<const T*>(a.g) + (uint64_t)r0 * a.ld_g + n;
-    const uint32_t rows = min(slice_rows, a.m - r0);
-    uint32_t top = 0;
-    for (uint32_t r = 0; r < rows; ++r) top = max(top, key_of(scaled(g + (uint64_t)r * a.ld_g, a.s[r0 + r])));
-    tops[(uint64_t)blockIdx.y * a.n + n] = top;
-}
-
-// The digits of 64 columns and 128 rows, the rows of a column side by side.
-template <typename T>
-__global__ __launch_bounds__(BLOCK) void q8_digits_kernel(Q8GradientArgs a, Q8GradientPlan pl) {
-    __shared__ float s_factor[64];
-    __shared__ float s_up[64];
-    __shared__ int8_t s_d[3][64][128 + 4];
-    uint32_t* tops = reinterpret_cast<uint32_t*>(a.work + pl.tops);
-    const uint32_t n0 = blockIdx.x * 64u, m0 = blockIdx.y * 128u;
-    if (threadIdx.x < 64u) {
-        const uint32_t n = n0 + threadIdx.x;
-        uint32_t top = 0;
-        if (n < a.n)
-            for (uint32_t s = 0; s < pl.slices; ++s) top = max(top, tops[(uint64_t)s * a.n + n]);
-        const float c = __uint_as_float(top);
-        const float up = digits_up(c);
-        s_up[threadIdx.x] = up;
-        s_factor[threadIdx.x] = top == 0u || top >= 0x7f800000u ? 0.0f : DIGITS_TOP / (c * up);
-    }
-    __syncthreads();
-    const uint32_t col = threadIdx.x & 63u, n = n0 + col;
-    const float f = s_factor[col], up = s_up[col];
-    for (uint32_t r = threadIdx.x / 64u; r < 128u; r += BLOCK / 64u) {
-        const uint32_t m = m0 + r;
-        int32_t v = 0;
-        if (m < a.m && n < a.n && f != 0.0f) {
-            const float p = scaled(static_cast<const T*>(a.g) + (uint64_t)m * a.ld_g + n, a.s[m]);
-            v = (int32_t)fminf(fmaxf(rintf(p * up * f), -DIGITS_TOP), DIGITS_TOP);
+    const T* g = static_cast<const T*>(a.g) + n;
+    for (uint32_t r = r0; r < r1; r += 8u * step) {                      // eight rows under way
+        float f[8][8], s[8];
+#pragma unroll
+        for (uint32_t x = 0; x < 8; ++x) {
+            const uint32_t at = min(r + x * step, r1 - 1u);              // behind the last one: it again
+            load_up_to_8(g + (uint64_t)at * a.ld_g, a.n - n, f[x]);
+            s[x] = a.s[at];
         }
-        const int32_t d0 = (int8_t)v, w = (v - d0) >> 8, d1 = (int8_t)w;
-        s_d[0][col][r] = (int8_t)d0;
-        s_d[1][col][r] = (int8_t)d1;
-        s_d[2][col][r] = (int8_t)((w - d1) >> 8);
+#pragma unroll
+        for (uint32_t x = 0; x < 8; ++x)
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i) top[i] = max(top[i], key_of(__fmul_rn(f[x][i], s[x])));
+    }
+}
+
+// The columns' largest over one slice of rows, 512 columns a block and eight a thread; behind those blocks, the
+// ones that turn the checkpoint.
+template <typename T>
+__global__ __launch_bounds__(BLOCK) void q8_tops_kernel(Q8GradientArgs a, Q8GradientPlan pl, uint32_t blocks) {
+    __shared__ uint32_t lds[128 * TURN_PITCH];
+    if (blockIdx.x >= blocks) return turn_codes(a, pl, blockIdx.x - blocks, lds);
+    const uint32_t across = blocks / pl.slices, slice = blockIdx.x / across, lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+    const uint32_t n = blockIdx.x % across * 512u + lane * 8u, r0 = slice * pl.slice_rows;
+    uint32_t top[8];
+    column_tops<T>(a, n, r0 + wave, min(r0 + pl.slice_rows, a.m), BLOCK / 64u, top);
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) lds[(wave * 8u + i) * 64u + lane] = top[i];
+    __syncthreads();
+    if (wave != 0) return;
+    uint32_t* to = reinterpret_cast<uint32_t*>(a.work + pl.slice_tops) + (uint64_t)slice * a.n;
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) {
+        for (uint32_t w = 1; w < BLOCK / 64u; ++w) top[i] = max(top[i], lds[(w * 8u + i) * 64u + lane]);
+        if (n + i < a.n) to[n + i] = top[i];
+    }
+}
+
+// The digits of 64 columns and `deep` times 128 rows, the rows of a column side by side: a thread has eight columns
+// of four rows at a time, and the next ones on their way while it works.  SELF: the columns' largest are found
+// here, and behind the blocks for digits come those that turn the checkpoint.
+template <typename T, bool SELF>
+__global__ __launch_bounds__(BLOCK) void q8_digits_kernel(Q8GradientArgs a, Q8GradientPlan pl, uint32_t blocks, uint32_t deep) {
+    __shared__ uint32_t lds[3 * 64 * TURN_PITCH];
+    __shared__ uint32_t s_top[64];
+    if (SELF && blockIdx.x >= blocks) return turn_codes(a, pl, blockIdx.x - blocks, lds);
+    const uint32_t across = (a.n + 63u) / 64u, n0 = blockIdx.x % across * 64u;
+    const uint32_t first = blockIdx.x / across * deep * TURN_ROWS, last = min(first + deep * TURN_ROWS, (uint32_t)pl.ld);
+    const uint32_t cg = threadIdx.x & 7u, rg = threadIdx.x >> 3, n = n0 + cg * 8u;
+    float f[4][8], s[4];
+    auto fetch = [&](uint32_t m0) {
+#pragma unroll
+        for (uint32_t r = 0; r < 4; ++r) {
+            const uint32_t m = m0 + rg * 4u + r;
+            const bool there = m < a.m && n < a.n;                           // the others read as zero
+            load_up_to_8(static_cast<const T*>(a.g) + (there ? (uint64_t)m * a.ld_g + n : 0u), there ? a.n - n : 0u, f[r]);
+            s[r] = there ? a.s[m] : 0.0f;
+        }
+    };
+    fetch(first);
+    if (threadIdx.x < 64u) s_top[threadIdx.x] = 0;
+    __syncthreads();
+    if constexpr (SELF) {
+        uint32_t top[8];
+        column_tops<T>(a, n, rg, a.m, BLOCK / 8u, top);
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) {
+            for (uint32_t d = 8; d < 64; d <<= 1) top[i] = max(top[i], (uint32_t)__shfl_xor((int)top[i], (int)d, 64));
+            if ((threadIdx.x & 63u) < 8u) atomicMax(&s_top[cg * 8u + i], top[i]);
+        }
+    } else {
+        const uint32_t* tops = reinterpret_cast<const uint32_t*>(a.work + pl.slice_tops);
+        const uint32_t col = threadIdx.x & 63u;
+        uint32_t top = 0;
+        if (n0 + col < a.n) {
+#pragma unroll 8
+            for (uint32_t x = threadIdx.x / 64u; x < pl.slices; x += BLOCK / 64u) top = max(top, tops[(uint64_t)x * a.n + n0 + col]);
+            atomicMax(&s_top[col], top);
+        }
     }
     __syncthreads();
+    if (first == 0 && threadIdx.x < 64u && n0 + threadIdx.x < a.n)
+        reinterpret_cast<uint32_t*>(a.work + pl.tops)[n0 + threadIdx.x] = s_top[threadIdx.x];
+    float up[8], factor[8];
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) {
+        const uint32_t top = s_top[cg * 8u + i];
+        const float c = __uint_as_float(top);
+        up[i] = digits_up(c);
+        factor[i] = top == 0u || top >= 0x7f800000u ? 0.0f : DIGITS_TOP / (c * up[i]);
+    }
     int8_t* out = reinterpret_cast<int8_t*>(a.work + pl.digits);
-    for (uint32_t i = threadIdx.x; i < 3u * 64u * 32u; i += BLOCK) {
-        const uint32_t word = i & 31u, c = (i >> 5) & 63u, p = i >> 11;
-        if (n0 + c < a.n)
-            *reinterpret_cast<uint32_t*>(out + ((uint64_t)p * a.n + n0 + c) * pl.ld + m0 + 4u * word) =
-                *reinterpret_cast<const uint32_t*>(&s_d[p][c][4u * word]);
+    for (uint32_t m0 = first; m0 < last; m0 += TURN_ROWS) {
+        uint32_t d[3][8] = {};
+#pragma unroll
+        for (uint32_t r = 0; r < 4; ++r)
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i) {
+                // a column that is not finite has factor 0, and NaN in its own place alone
+                const float t = rintf(__fmul_rn(__fmul_rn(__fmul_rn(f[r][i], s[r]), up[i]), factor[i]));
+                const int32_t v = (int32_t)fminf(fmaxf(t, -DIGITS_TOP), DIGITS_TOP);
+                const int32_t v1 = (v + 128) >> 8, v2 = (v1 + 128) >> 8;     // what the digits from d1, from d2 on stand for
+                d[0][i] |= ((uint32_t)v & 255u) << (8u * r);
+                d[1][i] |= ((uint32_t)v1 & 255u) << (8u * r);
+                d[2][i] |= ((uint32_t)v2 & 255u) << (8u * r);
+            }
+        if (m0 + TURN_ROWS < last) fetch(m0 + TURN_ROWS);
+#pragma unroll
+        for (uint32_t p = 0; p < 3; ++p)
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i) lds[(p * 64u + cg * 8u + i) * TURN_PITCH + rg] = d[p][i];
+        __syncthreads();
+#pragma unroll
+        for (uint32_t p = 0; p < 3; ++p)
+            store_turned(lds + p * 64u * TURN_PITCH, min(64u, a.n - n0), out + ((uint64_t)p * a.n + n0) * pl.ld + m0, pl.ld);
+        __syncthreads();
     }
 }
 
-// 64 columns and 128 rows of the checkpoint, turned.
-__global__ __launch_bounds__(BLOCK) void q8_turn_kernel(Q8GradientArgs a, Q8GradientPlan pl) {
-    __shared__ int8_t s_q[64][128 + 4];
-    const uint32_t k0 = blockIdx.x * 64u, m0 = blockIdx.y * 128u;
-    const uint32_t col = threadIdx.x & 63u;
-    for (uint32_t r = threadIdx.x / 64u; r < 128u; r += BLOCK / 64u) {
-        const uint32_t m = m0 + r, k = k0 + col;
-        s_q[col][r] = m < a.m && k < a.k ? a.q[(uint64_t)m * a.ld_q + k] : (int8_t)0;
-    }
-    __syncthreads();
-    int8_t* out = reinterpret_cast<int8_t*>(a.work + pl.codes);
-    for (uint32_t i = threadIdx.x; i < 64u * 32u; i += BLOCK) {
-        const uint32_t word = i & 31u, c = i >> 5;
-        if (k0 + c < a.k)
-            *reinterpret_cast<uint32_t*>(out + (uint64_t)(k0 + c) * pl.ld + m0 + 4u * word) =
-                *reinterpret_cast<const uint32_t*>(&s_q[c][4u * word]);
-    }
-}
-
-template <uint32_t WA, uint32_t WB, uint32_t FA, uint32_t FB, uint32_t NS>
-__global__ __launch_bounds__(64 * WA * WB) void q8_gradient_kernel(Q8GradientArgs g, Q8GradientPlan pl) {
-    using Tl = Tile<3, WA, WB, FA, FB, NS, 128>;
-    __shared__ __align__(16) int8_t lds[Tl::LDS];
-    const uint32_t tiles_n = (g.n + Tl::RA - 1u) / Tl::RA;
-    const uint32_t n0 = (blockIdx.x % tiles_n) * Tl::RA, k0 = (blockIdx.x / tiles_n) * Tl::RB;
-    const int8_t* digits = reinterpret_cast<const int8_t*>(g.work + pl.digits);
-    const int8_t* codes = reinterpret_cast<const int8_t*>(g.work + pl.codes);
-    const uint32_t* tops = reinterpret_cast<const uint32_t*>(g.work + pl.tops);
-    Tl t;
-    t.run(digits + (uint64_t)n0 * pl.ld, pl.ld, (uint64_t)g.n * pl.ld, g.n - n0, codes + (uint64_t)k0 * pl.ld, pl.ld,
-          g.k - k0, (uint32_t)pl.ld, lds);
+// A wavefront's 32 rows x COLS values of LDS to dw, under the mask, or added to it.
+template <uint32_t COLS>
+__device__ __forceinline__ void store_gradient(const int8_t* from, uint32_t pitch, const Q8GradientArgs& g, uint32_t n0, uint32_t k0) {
+    constexpr uint32_t LANES = COLS / 4;
+    typedef float vec __attribute__((ext_vector_type(4)));
+    typedef float loose __attribute__((ext_vector_type(4), aligned(4)));
+    const uint32_t lane = threadIdx.x & 63u, k = k0 + lane % LANES * 4u;
+    if (k >= g.k) return;
+    const bool whole = k + 4u <= g.k;
+#pragma unroll 4
+    for (uint32_t r = lane / LANES; r < 32u; r += 64u / LANES) {
+        vec v = *reinterpret_cast<const vec*>(from + r * pitch + (k - k0) * 4u);
+        const uint32_t n = n0 + r;
+        if (n >= g.n) continue;
+        float* to = g.dw + (uint64_t)n * g.ld_dw + k;
+        const uint8_t* mask = g.mask + (uint64_t)n * g.ld_mask + k;
+        if (whole) {
+            uint32_t keep = 0xffffffffu;
+            if (g.mask) keep = *reinterpret_cast<const u32_a1*>(mask);
+            vec old = {0.0f, 0.0f, 0.0f, 0.0f};
+            if (g.accumulate) old = *reinterpret_cast<const loose*>(to);
 #pragma unroll
-    for (uint32_t i = 0; i < FA; ++i)
+            for (uint32_t i = 0; i < 4; ++i) v[i] = keep >> (8u * i) & 255u ? (g.accumulate ? old[i] + v[i] : v[i]) : old[i];
+            *reinterpret_cast<loose*>(to) = v;
+        } else {
 #pragma unroll
-        for (uint32_t e = 0; e < 16; ++e) {
-            const uint32_t n = n0 + Tl::row(i, e);
-            if (n >= g.n) continue;
-            uint32_t top = 0;
-            for (uint32_t s = 0; s < pl.slices; ++s) top = max(top, tops[(uint64_t)s * g.n + n]);
-            const float c = __uint_as_float(top), unit = c * digits_up(c) / DIGITS_TOP, down = digits_down(c);
-            const bool bad = top >= 0x7f800000u;
-#pragma unroll
-            for (uint32_t j = 0; j < FB; ++j) {
-                const uint32_t k = k0 + Tl::col(j);
-                if (k >= g.k) continue;
-                const bool keep = !g.mask || g.mask[(uint64_t)n * g.ld_mask + k];
-                float v = fmaf((float)t.acc[2][i][j][e], 65536.0f, fmaf((float)t.acc[1][i][j][e], 256.0f, (float)t.acc[0][i][j][e]));
-                v = bad ? __uint_as_float(0x7fc00000u) : v * unit * down;
-                float* out = g.dw + (uint64_t)n * g.ld_dw + k;
-                if (g.accumulate) { if (keep) *out += v; }
-                else *out = keep ? v : 0.0f;
+            for (uint32_t i = 0; i < 4; ++i) {
+                if (k + i >= g.k) break;
+                const float old = g.accumulate ? to[i] : 0.0f;
+                to[i] = !g.mask || mask[i] ? (g.accumulate ? old + v[i] : v[i]) : old;
             }
         }
+    }
+}
+
+template <uint32_t WA, uint32_t WB, uint32_t FA, uint32_t FB, uint32_t NS, uint32_t STEP, uint32_t GROUP>
+__global__ __launch_bounds__(64 * WA * WB) void q8_gradient_kernel(Q8GradientArgs g, Q8GradientPlan pl) {
+
+    using Tl = Tile<3, WA, WB, FA, FB, NS, STEP>;
+    constexpr uint32_t PITCH = Tl::COLS * 4u + 16u, OUT = WA * WB * 32u * PITCH, BEHIND = OUT + 8u * Tl::RA;
+    __shared__ __align__(16) int8_t lds[Tl::LDS > BEHIND ? Tl::LDS : BEHIND];
+    static_assert(Tl::THREADS >= Tl::RA, "a column's unit a thread");
+    uint32_t ta, tb;
+    tile_of_block<GROUP>((g.n + Tl::RA - 1u) / Tl::RA, (g.k + Tl::RB - 1u) / Tl::RB, &ta, &tb);
+    const uint32_t n0 = ta * Tl::RA, k0 = tb * Tl::RB;
+    const int8_t* digits = reinterpret_cast<const int8_t*>(g.work + pl.digits);
+    const int8_t* codes = reinterpret_cast<const int8_t*>(g.work + pl.codes);
+    const float top = pl.ld ? reinterpret_cast<const float*>(g.work + pl.tops)[min(n0 + threadIdx.x % Tl::RA, g.n - 1u)] : 0.0f;
+    Tl t;
+    const uint32_t m0 = blockIdx.y * pl.part_rows;
+    t.run(digits + (uint64_t)n0 * pl.ld + m0, pl.ld, (uint64_t)g.n * pl.ld, g.n - n0, codes + (uint64_t)k0 * pl.ld + m0, pl.ld,
+          g.k - k0, min(pl.part_rows, (uint32_t)pl.ld - m0), lds);
+    if (pl.parts > 1) {                        // one part of the rows: its sums go to the workspace as they are
+        g.dw = reinterpret_cast<float*>(g.work + pl.sums) + (uint64_t)blockIdx.y * g.n * g.k;
+        g.ld_dw = g.k;
+        g.mask = nullptr;
+        g.accumulate = 0;
+    }
+    __syncthreads();
+    float* s_unit = reinterpret_cast<float*>(lds + OUT);
+    float* s_down = s_unit + Tl::RA;
+    if (threadIdx.x < Tl::RA) {
+        s_unit[threadIdx.x] = key_of(top) >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : top * digits_up(top) / DIGITS_TOP;
+        s_down[threadIdx.x] = digits_down(top);
+    }
+    __syncthreads();
+    const uint32_t lane = threadIdx.x & 63u;
+    int8_t* out = lds + uniform_u32(threadIdx.x >> 6) * 32u * PITCH;
+#pragma unroll
+    for (uint32_t i = 0; i < FA; ++i) {
+#pragma unroll
+        for (uint32_t e = 0; e < 16; ++e) {
+            const uint32_t row = Tl::row(i, e);
+            const float unit = s_unit[row], down = s_down[row];
+#pragma unroll
+            for (uint32_t j = 0; j < FB; ++j) {
+                const float v = fmaf((float)t.acc[2][i][j][e], 65536.0f, fmaf((float)t.acc[1][i][j][e], 256.0f, (float)t.acc[0][i][j][e]));
+                *reinterpret_cast<float*>(out + (8u * (e / 4u) + 4u * (lane >> 5) + (e & 3u)) * PITCH + (j * 32u + (lane & 31u)) * 4u) = v * unit * down;
+            }
+        }
+        __builtin_amdgcn_wave_barrier();       // a wavefront's LDS accesses are done in order
+        store_gradient<Tl::COLS>(out, PITCH, g, n0 + Tl::row(i, 0) - 4u * (lane >> 5), k0 + Tl::col(0) - (lane & 31u));
+        __builtin_amdgcn_wave_barrier();
+    }
 }
 
 template <typename T>
 static void launch_digits(shifter_ctx* ctx, const Q8GradientArgs& g, const Q8GradientPlan& pl) {
-    if (pl.slices == 0) return;
-    q8_tops_kernel<T><<<dim3((g.n + BLOCK - 1u) / BLOCK, pl.slices), BLOCK, 0, ctx->stream>>>(
-        g, pl.slice_rows, reinterpret_cast<uint32_t*>(g.work + pl.tops));
-    q8_digits_kernel<T><<<dim3((g.n + 63u) / 64u, (uint32_t)(pl.ld / 128u)), BLOCK, 0, ctx->stream>>>(g, pl);
-    q8_turn_kernel<<<dim3((g.k + 63u) / 64u, (uint32_t)(pl.ld / 128u)), BLOCK, 0, ctx->stream>>>(g, pl);
+    if (pl.ld == 0) return;
+    const uint32_t turns = turn_blocks(g, pl), across = (g.n + 63u) / 64u, tiles = (uint32_t)(pl.ld / TURN_ROWS);
+    if (pl.slices == 0) {
+        q8_digits_kernel<T, true><<<across * tiles + turns, BLOCK, 0, ctx->stream>>>(g, pl, across * tiles, 1u);
+    } else {
+        const uint32_t tops = (g.n + 511u) / 512u * pl.slices;
+        q8_tops_kernel<T><<<tops + turns, BLOCK, 0, ctx->stream>>>(g, pl, tops);
+        // every block reads its columns' slices: as many rows a block as leave 2048 blocks
+        const uint32_t deep = std::min(8u, std::max(1u, (uint32_t)((uint64_t)across * tiles / 2048u)));
+        const uint32_t blocks = across * ((tiles + deep - 1u) / deep);
+        q8_digits_kernel<T, false><<<blocks, BLOCK, 0, ctx->stream>>>(g, pl, blocks, deep);
+    }
+}
+
+// The parts' sums joined, in 64 bits so that only the parts' own roundings count; under the mask, or added to dw.
+__global__ __launch_bounds__(BLOCK) void q8_join_kernel(Q8GradientArgs g, Q8GradientPlan pl) {
+    const float* sums = reinterpret_cast<const float*>(g.work + pl.sums);
+    const uint64_t all = (uint64_t)g.n * g.k;
+    for (uint64_t i = ((uint64_t)blockIdx.x * BLOCK + threadIdx.x) * 4u; i < all; i += (uint64_t)gridDim.x * BLOCK * 4u) {
+        double v[4] = {0.0, 0.0, 0.0, 0.0};
+        const uint32_t there = (uint32_t)min(all - i, (uint64_t)4u);
+#pragma unroll 4
+        for (uint32_t p = 0; p < pl.parts; ++p) {
+            const float* from = sums + p * all + i;
+            if (there == 4u) {
+                const uint4 f = load_u4<false>(from);
+                v[0] += __uint_as_float(f.x); v[1] += __uint_as_float(f.y); v[2] += __uint_as_float(f.z); v[3] += __uint_as_float(f.w);
+            } else {
+                for (uint32_t e = 0; e < there; ++e) v[e] += from[e];
+            }
+        }
+        const uint64_t row = i / g.k;
+        uint32_t k = (uint32_t)(i - row * g.k);
+        float* to = g.dw + row * g.ld_dw;
+        const uint8_t* mask = g.mask + row * g.ld_mask;
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e) {
+            if (e >= there) break;
+            if (k == g.k) { k = 0; to += g.ld_dw; mask += g.ld_mask; }
+            const float old = g.accumulate ? to[k] : 0.0f;
+            to[k] = !g.mask || mask[k] ? (g.accumulate ? old + (float)v[e] : (float)v[e]) : old;
+            ++k;
+        }
+    }
+}
+
+template <uint32_t WA, uint32_t WB, uint32_t FA, uint32_t FB, uint32_t NS, uint32_t STEP, uint32_t GROUP>
+static void launch_gradient_as(shifter_ctx* ctx, const Q8GradientArgs& g, const Q8GradientPlan& pl) {
+    using Tl = Tile<3, WA, WB, FA, FB, NS, STEP>;
+    const uint64_t tiles = (uint64_t)((g.n + Tl::RA - 1u) / Tl::RA) * ((g.k + Tl::RB - 1u) / Tl::RB);
+    q8_gradient_kernel<WA, WB, FA, FB, NS, STEP, GROUP><<<dim3((uint32_t)tiles, pl.parts), Tl::THREADS, 0, ctx->stream>>>(g, pl);
+    if (pl.parts > 1)
+        q8_join_kernel<<<(uint32_t)std::min<uint64_t>(((uint64_t)g.n * g.k + 4u * BLOCK - 1u) / (4u * BLOCK), 4096u), BLOCK, 0, ctx->stream>>>(g, pl);
 }
 
 void launch_q8_gradient(shifter_ctx* ctx, int dtype, const Q8GradientArgs& g) {
@@ -533,10 +737,12 @@ void launch_q8_gradient(shifter_ctx* ctx, int dtype, const Q8GradientArgs& g) {
         else launch_digits<_Float16>(ctx, g, pl);
     }
     ProfileScope ps(ctx, K_Q8_GRADIENT);
-    constexpr uint32_t WA = 2, WB = 2, FA = 1, FB = 1, NS = 2;
-    using Tl = Tile<3, WA, WB, FA, FB, NS, 128>;
-    const uint64_t tiles = (uint64_t)((g.n + Tl::RA - 1u) / Tl::RA) * ((g.k + Tl::RB - 1u) / Tl::RB);
-    q8_gradient_kernel<WA, WB, FA, FB, NS><<<(uint32_t)tiles, Tl::THREADS, 0, ctx->stream>>>(g, pl);
+    switch (pl.kernel) {
+        case Q8_GRAD_64x64: launch_gradient_as<2, 2, 1, 1, 2, 128, 8>(ctx, g, pl); break;
+        case Q8_GRAD_64x128: launch_gradient_as<2, 2, 1, 2, 2, 128, 8>(ctx, g, pl); break;
+        case Q8_GRAD_64x256: launch_gradient_as<2, 4, 1, 2, 2, 128, 8>(ctx, g, pl); break;
+        default: launch_gradient_as<4, 2, 1, 4, 2, 128, 4>(ctx, g, pl); break;
+    }
 }
 
 }  // namespace shifter

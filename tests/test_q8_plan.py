@@ -58,17 +58,24 @@ int main() {
     WANT(q8_bad_codes(p, p, 1ull << 31, 17, 32), "rows or columns");
     // workspace: the parts follow one another, every slice has rows, the rows are all in slices
     const uint64_t ms[] = {0, 1, 127, 128, 129, 8191, 8192, 8193, 16384, 20000, 131071};
-    const uint64_t ns[] = {1, 63, 4097};
+    const uint64_t ns[] = {1, 63, 500, 2048, 4097};
+    int used[Q8_GRAD_KERNELS] = {0}, split = 0;
     for (uint64_t m : ms)
         for (uint64_t n : ns)
             for (uint64_t k : ns) {
                 const Q8GradientPlan g = q8_gradient_plan(m, n, k);
-                bool ok = g.ld >= m && g.ld < m + 128 && g.ld % 128 == 0 && g.slices <= Q8_SLICES && g.slice_rows % 128 == 0;
-                ok = ok && (uint64_t)g.slices * g.slice_rows >= m && (m == 0 ? g.slices == 0 : (uint64_t)(g.slices - 1) * g.slice_rows < m);
-                ok = ok && g.tops == 0 && g.digits >= 4 * n * g.slices && g.digits % 256 == 0;
-                ok = ok && g.codes >= g.digits + 3 * n * g.ld && g.codes % 128 == 0 && g.bytes >= g.codes + k * g.ld;
+                bool ok = g.ld >= m && g.ld < m + 128 && g.ld % 128 == 0 && g.slices <= Q8_SLICES && g.slice_rows % Q8_SLICE_ROWS == 0;
+                ok = ok && (m <= Q8_SELF_ROWS ? g.slices == 0 : (uint64_t)g.slices * g.slice_rows >= m && (uint64_t)(g.slices - 1) * g.slice_rows < m);
+                ok = ok && g.tops == 0 && g.slice_tops >= 4 * n && g.digits >= g.slice_tops + 4 * n * g.slices && g.digits % 256 == 0;
+                ok = ok && g.kernel < Q8_GRAD_KERNELS && g.parts >= 1 && g.parts <= Q8_PARTS && g.part_rows % 128 == 0;
+                ok = ok && (uint64_t)g.parts * g.part_rows >= g.ld && (g.ld == 0 || (uint64_t)(g.parts - 1) * g.part_rows < g.ld);
+                ok = ok && g.sums == g.codes + k * g.ld && g.sums % 128 == 0 && (m == 0 || g.bytes == g.sums + (g.parts > 1 ? 4 * g.parts * n * k : 0));
+                if (ok) { ++used[g.kernel]; split += g.parts > 1; }
+                ok = ok && g.codes >= g.digits + 3 * n * g.ld && g.codes % 128 == 0 && g.bytes >= (m ? g.codes + k * g.ld : 0);
                 if (!ok) { printf("plan of %llu %llu %llu\n", (unsigned long long)m, (unsigned long long)n, (unsigned long long)k); ++bad; }
             }
+    for (int q = 0; q < Q8_GRAD_KERNELS; ++q) if (!used[q]) { printf("gradient kernel %d is never taken\n", q); ++bad; }
+    if (!split) { printf("rows are never split\n"); ++bad; }
     // kernels: few rows take the one without tiles, and every kernel is taken somewhere
     int taken[Q8_KERNELS] = {0};
     for (uint64_t m = 1; m <= 20000; m += 1 + m / 7)
