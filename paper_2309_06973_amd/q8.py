@@ -12,6 +12,13 @@ import torch
 from . import shifter as S
 
 _DTYPES = {torch.float32: S.SHIFTER_F32, torch.bfloat16: S.SHIFTER_BF16, torch.float16: S.SHIFTER_F16}
+# a call's kernel takes a few microseconds: the checks around it are kept short (the stream object of
+# torch.cuda.current_stream alone costs 1.9 us, this 0.1)
+_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else None
+
+
+def _pad(cols: int) -> int:
+    return -(-cols // S.SHIFTER_Q8_ALIGN) * S.SHIFTER_Q8_ALIGN
 
 
 class Q8Matrix:
@@ -27,7 +34,7 @@ class Q8Matrix:
         if scale.shape[0] != q.shape[0] or not 0 <= cols <= q.shape[1] or q.device != scale.device:
             raise ValueError("codes, scales and cols do not belong together")
         self.q, self.scale, self.rows, self.cols = q, scale, q.shape[0], cols
-        pad = -(-cols // S.SHIFTER_Q8_ALIGN) * S.SHIFTER_Q8_ALIGN
+        pad = _pad(cols)
         self.ld = q.stride(0) if self.rows > 1 and cols else pad
         if self.rows and cols and q.storage_offset() + (self.rows - 1) * self.ld + pad > q.untyped_storage().nbytes():
             raise ValueError("the last row's buffer ends before its columns rounded up to 16")
@@ -57,19 +64,22 @@ class Q8:
     # ---- checks -------------------------------------------------------------------
     def _enter(self):
         """New tensors belong to torch's current stream; the kernels run on the handle's."""
-        if torch.cuda.current_stream(self.dev).cuda_stream != self.stream:
+        if _raw_stream(self.dev.index) != self.stream:
             raise RuntimeError("this handle runs on the stream it was made on: make one under the other stream")
 
     def _matrix(self, x: torch.Tensor, what: str):
         """(dtype code, rows, cols, stride)"""
-        if x.dim() != 2 or x.dtype not in _DTYPES:
+        code = _DTYPES.get(x.dtype)
+        if code is None or x.dim() != 2:
             raise ValueError(f"{what} must be a two-dimensional fp32, bf16 or fp16 tensor")
         rows, cols = x.shape
-        ld = x.stride(0) if rows > 1 else cols
-        if (cols > 1 and x.stride(1) != 1) or ld < cols:
+        ld, side = x.stride()
+        if rows < 2:
+            ld = cols
+        if (cols > 1 and side != 1) or ld < cols:
             raise ValueError(f"the columns of {what} must lie side by side, rows one after another")
         self._here(x, what)
-        return _DTYPES[x.dtype], rows, cols, ld
+        return code, rows, cols, ld
 
     def _here(self, x: torch.Tensor, what: str):
         if x.device != self.dev:
@@ -81,18 +91,31 @@ class Q8:
         self._here(v, what)
 
     def _same(self, a: torch.Tensor, shape, dtype, what: str):
-        if tuple(a.shape) != tuple(shape) or a.dtype != dtype:
+        if a.shape != shape or a.dtype != dtype:
             raise ValueError(f"{what} must have shape {tuple(shape)} and type {dtype}")
 
     def _room(self, rows: int, cols: int, out: Optional[Q8Matrix]) -> Q8Matrix:
         if out is None:
-            ld = -(-cols // S.SHIFTER_Q8_ALIGN) * S.SHIFTER_Q8_ALIGN
-            return Q8Matrix(torch.empty((rows, ld), dtype=torch.int8, device=self.dev),
-                            torch.empty(rows, dtype=torch.float32, device=self.dev), cols)
+            m = Q8Matrix.__new__(Q8Matrix)             # as __init__ would leave it
+            m.rows, m.cols, m.ld = rows, cols, _pad(cols)
+            m.q = torch.empty((rows, m.ld), dtype=torch.int8, device=self.dev)
+            m.scale = torch.empty(rows, dtype=torch.float32, device=self.dev)
+            return m
         self._here(out.q, "out")
         if out.rows != rows or out.cols != cols:
             raise ValueError("out is an 8-bit matrix of another size")
         return out
+
+    def _result(self, rows: int, cols: int, dtype: torch.dtype, out: Optional[torch.Tensor]):
+        """(out or a new matrix, dtype code, stride)"""
+        if out is None:
+            code = _DTYPES.get(dtype)
+            if code is None:
+                raise ValueError("dtype must be fp32, bf16 or fp16")
+            return torch.empty((rows, cols), dtype=dtype, device=self.dev), code, cols
+        code, _, _, ld = self._matrix(out, "out")
+        self._same(out, (rows, cols), out.dtype, "out")
+        return out, code, ld
 
     # ---- the operators --------------------------------------------------------------
     def quantize(self, x: torch.Tensor, relu: bool = False, out: Optional[Q8Matrix] = None) -> Q8Matrix:
@@ -105,16 +128,11 @@ class Q8:
         return m
 
     def dequantize(self, m: Q8Matrix, dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None):
-        """code * scale in the element type."""
+        """code * scale in the element type (that of ``out`` where it is given)."""
         self._enter()
         self._here(m.q, "m")
-        if out is None:
-            if dtype not in _DTYPES:
-                raise ValueError("dtype must be fp32, bf16 or fp16")
-            out = torch.empty((m.rows, m.cols), dtype=dtype, device=self.dev)
-        t, rows, cols, ld = self._matrix(out, "out")
-        self._same(out, (m.rows, m.cols), out.dtype, "out")
-        S.shifter_dequantize_q8(self.ctx, m.q, m.ld, m.scale, rows, cols, out, t, ld)
+        out, t, ld = self._result(m.rows, m.cols, dtype, out)
+        S.shifter_dequantize_q8(self.ctx, m.q, m.ld, m.scale, m.rows, m.cols, out, t, ld)
         return out
 
     def rms_norm(self, x: torch.Tensor, weight: torch.Tensor, eps: float, residual: Optional[torch.Tensor] = None,
@@ -129,9 +147,10 @@ class Q8:
             self._same(residual, x.shape, x.dtype, "residual")
             _, _, _, ld_r = self._matrix(residual, "residual")
             if h is None:
-                h = torch.empty((rows, cols), dtype=x.dtype, device=self.dev)
-            self._same(h, x.shape, x.dtype, "h")
-            _, _, _, ld_h = self._matrix(h, "h")
+                h, ld_h = torch.empty((rows, cols), dtype=x.dtype, device=self.dev), cols
+            else:
+                self._same(h, x.shape, x.dtype, "h")
+                _, _, _, ld_h = self._matrix(h, "h")
         elif h is not None:
             raise ValueError("h without a residual: the stream is x itself")
         m = self._room(rows, cols, out)
@@ -148,13 +167,8 @@ class Q8:
             raise ValueError("a and b have different numbers of columns")
         if bias is not None:
             self._vector(bias, b.rows, "bias")
-        if out is None:
-            if dtype not in _DTYPES:
-                raise ValueError("dtype must be fp32, bf16 or fp16")
-            out = torch.empty((a.rows, b.rows), dtype=dtype, device=self.dev)
-        t, m, n, ld = self._matrix(out, "out")
-        self._same(out, (a.rows, b.rows), out.dtype, "out")
-        S.shifter_matmul_q8(self.ctx, a.q, a.ld, a.scale, b.q, b.ld, b.scale, m, n, a.cols, bias,
+        out, t, ld = self._result(a.rows, b.rows, dtype, out)
+        S.shifter_matmul_q8(self.ctx, a.q, a.ld, a.scale, b.q, b.ld, b.scale, a.rows, b.rows, a.cols, bias,
                             S.SHIFTER_Q8_RELU if relu else 0, out, t, ld)
         return out
 
@@ -175,12 +189,11 @@ class Q8:
             ld_mask = mask.stride(0) if n > 1 else k
             if (k > 1 and mask.stride(1) != 1) or ld_mask < k:
                 raise ValueError("the columns of mask must lie side by side, rows one after another")
-        if out is None:
-            if accumulate:
-                raise ValueError("accumulate without out")
-            out = torch.empty((n, k), dtype=torch.float32, device=self.dev)
-        self._same(out, (n, k), torch.float32, "out")
-        _, _, _, ld_out = self._matrix(out, "out")
+        if accumulate and out is None:
+            raise ValueError("accumulate without out")
+        if out is not None and out.dtype != torch.float32:
+            raise ValueError("out must be float32")
+        out, _, ld_out = self._result(n, k, torch.float32, out)
         need = S.shifter_weight_grad_q8_layout(m, n, k)
         if self.work is None or self.work.numel() < need:
             self.work = torch.empty(need, dtype=torch.uint8, device=self.dev)
