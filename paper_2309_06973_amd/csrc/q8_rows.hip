@@ -10,84 +10,189 @@
 //
 // Streaming work: each row is read once into registers, reduced and written.
 #include <algorithm>
+#include <type_traits>
 
 #include "dev_common.h"
 #include "q8.h"
 
 namespace shifter {
 
+// Eight neighbouring elements as they lie in memory, at any element's address.
 template <typename T>
-__device__ __forceinline__ void load8(const T* p, float (&f)[8]) {
-    if constexpr (sizeof(T) == 4) {
-        const uint4 a = load_u4<false>(reinterpret_cast<const float*>(p));
-        const uint4 b = load_u4<false>(reinterpret_cast<const float*>(p) + 4);
-        f[0] = __uint_as_float(a.x); f[1] = __uint_as_float(a.y); f[2] = __uint_as_float(a.z); f[3] = __uint_as_float(a.w);
-        f[4] = __uint_as_float(b.x); f[5] = __uint_as_float(b.y); f[6] = __uint_as_float(b.z); f[7] = __uint_as_float(b.w);
-    } else {
-        typedef T vec __attribute__((ext_vector_type(8), aligned(2)));
-        const vec v = *reinterpret_cast<const vec*>(p);
+struct Eight {
+    static constexpr uint32_t WORDS = 2 * sizeof(T);
+    uint32_t w[WORDS];
+    __device__ __forceinline__ void load(const T* p) {
+        typedef uint32_t vec __attribute__((ext_vector_type(4), aligned(2)));
+        const vec* q = reinterpret_cast<const vec*>(p);
+#pragma unroll
+        for (uint32_t x = 0; x < WORDS / 4u; ++x) {
+            const vec v = q[x];
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i) w[4u * x + i] = v[i];
+        }
+    }
+    __device__ __forceinline__ void store(T* p) const {
+        typedef uint32_t vec __attribute__((ext_vector_type(4), aligned(2)));
+        vec* q = reinterpret_cast<vec*>(p);
+#pragma unroll
+        for (uint32_t x = 0; x < WORDS / 4u; ++x) q[x] = vec{w[4u * x], w[4u * x + 1u], w[4u * x + 2u], w[4u * x + 3u]};
+    }
+    // the elements from the n-th on, zeros behind them: n < 8
+    __device__ __forceinline__ void drop(uint32_t n) {
+        const uint32_t bits = n * 8u * sizeof(T), words = bits / 32u, rest = bits % 32u;
+#pragma unroll
+        for (uint32_t d = WORDS / 2u; d > 0; d >>= 1)
+#pragma unroll
+            for (uint32_t i = 0; i < WORDS; ++i)
+                if (words & d) w[i] = i + d < WORDS ? w[i + d] : 0u;
+        if (sizeof(T) == 2 && rest) {
+#pragma unroll
+            for (uint32_t i = 0; i < WORDS; ++i) w[i] = w[i] >> 16 | (i + 1u < WORDS ? w[i + 1u] << 16 : 0u);
+        }
+    }
+    __device__ __forceinline__ void floats(float (&f)[8]) const {
+        typedef T vec __attribute__((ext_vector_type(8)));
+        vec v;
+        __builtin_memcpy(&v, w, sizeof(v));
 #pragma unroll
         for (int i = 0; i < 8; ++i) f[i] = (float)v[i];
     }
-}
-
-template <typename T>
-__device__ __forceinline__ void store8(T* p, const float (&f)[8]) {
-    if constexpr (sizeof(T) == 4) {
-        store_u4<false>(reinterpret_cast<float*>(p),
-                        make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])));
-        store_u4<false>(reinterpret_cast<float*>(p) + 4,
-                        make_uint4(__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7])));
-    } else {
-        typedef T vec __attribute__((ext_vector_type(8), aligned(2)));
+    __device__ __forceinline__ void from(const float (&f)[8]) {
+        typedef T vec __attribute__((ext_vector_type(8)));
         vec v;
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = (T)f[i];
-        *reinterpret_cast<vec*>(p) = v;
+        __builtin_memcpy(w, &v, sizeof(v));
+    }
+};
+
+// The elements from column c on of a row of `cols`, zeros behind its end.  A row's last elements are fetched
+// with the ones before them and moved into place, so that no load stands in a branch and all of a row's are under way
+// together; only rows of less than eight elements are read one by one.
+template <typename T>
+__device__ __forceinline__ void fetch8(const T* row, uint32_t c, uint32_t cols, Eight<T>& e) {
+    if (cols >= 8u) {
+        e.load(row + min(c, cols - 8u));
+    } else {
+        float f[8];
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) f[i] = c + i < cols ? (float)row[c + i] : 0.0f;
+        e.from(f);
+    }
+}
+template <typename T>
+__device__ __forceinline__ void place8(uint32_t c, uint32_t cols, Eight<T>& e) {
+    if (c + 8u > cols && cols >= 8u) {
+        if (c < cols) e.drop(c + 8u - cols);
+        else {
+#pragma unroll
+            for (uint32_t i = 0; i < Eight<T>::WORDS; ++i) e.w[i] = 0u;
+        }
+    }
+}
+template <typename T>
+__device__ __forceinline__ void store_up_to_8(T* p, uint32_t n, const float (&f)[8]) {
+    if (n >= 8u) {
+        Eight<T> e;
+        e.from(f);
+        e.store(p);
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i)
+            if (i < n) p[i] = (T)f[i];
     }
 }
 
-// The first n < 8 elements alone; the others read as zero.
-template <typename T>
-__device__ __forceinline__ void load_part(const T* p, uint32_t n, float (&f)[8]) {
-#pragma unroll
-    for (uint32_t i = 0; i < 8; ++i) f[i] = i < n ? (float)p[i] : 0.0f;
-}
-template <typename T>
-__device__ __forceinline__ void store_part(T* p, uint32_t n, const float (&f)[8]) {
-#pragma unroll
-    for (uint32_t i = 0; i < 8; ++i)
-        if (i < n) p[i] = (T)f[i];
-}
-
-// 127 p / a to the nearest whole number, ties to even, exactly.  r = fl(127 / a), or 0 where a is so small
-// that it could overflow (every value then takes the long way).  t = fl(p r) is within 127 * 2^-23 = 1.6e-5 of the
-// quotient, so the nearest whole number is certain unless t lies within 2e-5 of a half; there one division
-// in 64 bits decides: 127 p is exact in them, and the quotient of 24-bit numbers that is no tie is
-// further than 2^-32 from one.
-__device__ __forceinline__ float q8_code(float p, float a, float r) {
-    const float t = __fmul_rn(p, r);
-    float n = rintf(t);
-    if (fabsf(fabsf(t - n) - 0.5f) < (r > 0.0f ? 4e-5f : 1.0f)) n = (float)rint(127.0 * (double)p / (double)a);
-    return n;
-}
-__device__ __forceinline__ float q8_factor(float a) { return a >= 0x1p-100f ? 127.0f / a : 0.0f; }
-
-// Eight codes as two words.
+// 127 p / a to the nearest whole number, ties to even, exactly, for eight p, as two words; r = fl(127 / a).
+// t = fl(p r) is within 127 * 2^-23 = 1.6e-5 of the quotient, so the nearest whole number is certain unless t lies
+// within 2e-5 of a half.  There 254 |p| is compared with the odd multiple of a: both are exact in 64 bits.  (One
+// question for all eight: a branch for each cost the norm of 16384 x 4096 a tenth.)
 __device__ __forceinline__ uint2 q8_codes(const float (&p)[8], float a, float r) {
+    float t[8], n[8], near = 1.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        t[i] = __fmul_rn(p[i], r);
+        n[i] = rintf(t[i]);
+        near = fminf(near, fabsf(fabsf(t[i] - n[i]) - 0.5f));
+    }
+    if (near < 4e-5f) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (fabsf(fabsf(t[i] - n[i]) - 0.5f) >= 4e-5f) continue;
+            const float low = floorf(fabsf(t[i]));
+            const double over = 254.0 * (double)fabsf(p[i]) - (2.0 * (double)low + 1.0) * (double)a;
+            n[i] = copysignf(over > 0.0 || (over == 0.0 && ((int)low & 1)) ? low + 1.0f : low, t[i]);
+        }
+    }
     uint32_t w[2] = {0u, 0u};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w[i / 4] |= ((uint32_t)(int)q8_code(p[i], a, r) & 255u) << (8 * (i % 4));
+    for (int i = 0; i < 8; ++i) w[i / 4] |= ((uint32_t)(int)n[i] & 255u) << (8 * (i % 4));
     return make_uint2(w[0], w[1]);
+}
+
+// What a row's codes are made with.  A row of zeros and one that is not finite have none; one of tiny values is worked on
+// times 2^100, exactly, or 127 / a could overflow.
+struct RowCoder {
+    float a, r, up;
+    bool none;
+    __device__ __forceinline__ explicit RowCoder(uint32_t top) {
+        none = top == 0u || top >= 0x7f800000u;
+        a = none ? 1.0f : __uint_as_float(top);
+        up = a < 0x1p-100f ? 0x1p100f : 1.0f;
+        a *= up;
+        r = 127.0f / a;
+    }
+    __device__ __forceinline__ uint2 operator()(float (&p)[8]) const {
+        if (none) return make_uint2(0u, 0u);
+        if (up != 1.0f) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) p[i] *= up;
+        }
+        return q8_codes(p, a, r);
+    }
+};
+
+// v of the lane that DPP pattern CTRL pairs a lane with: neighbours by 1 and 2, mirrors of 8 and 16.
+template <int CTRL>
+__device__ __forceinline__ uint32_t paired(uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
+}
+template <int CTRL>
+__device__ __forceinline__ double paired(double v) {
+    uint32_t w[2];
+    __builtin_memcpy(w, &v, 8);
+    w[0] = paired<CTRL>(w[0]);
+    w[1] = paired<CTRL>(w[1]);
+    __builtin_memcpy(&v, w, 8);
+    return v;
+}
+__device__ __forceinline__ double of_lane(double v, int lane) {
+    uint32_t w[2];
+    __builtin_memcpy(w, &v, 8);
+    w[0] = (uint32_t)__builtin_amdgcn_readlane((int)w[0], lane);
+    w[1] = (uint32_t)__builtin_amdgcn_readlane((int)w[1], lane);
+    __builtin_memcpy(&v, w, 8);
+    return v;
 }
 
 // Largest and sum over the TPR threads of a row, in every one of them.
 template <uint32_t TPR, bool SUM>
 __device__ __forceinline__ void row_reduce(uint32_t& top, double& sum) {
+    top = max(top, paired<0xB1>(top));
+    top = max(top, paired<0x4E>(top));
+    top = max(top, paired<0x141>(top));
+    top = max(top, paired<0x140>(top));
+    uint32_t all = 0;
 #pragma unroll
-    for (uint32_t d = 32; d > 0; d >>= 1) {
-        top = max(top, (uint32_t)__shfl_xor((int)top, d, 64));
-        if (SUM) sum += __shfl_xor(sum, d, 64);
+    for (int i = 0; i < 4; ++i) all = max(all, (uint32_t)__builtin_amdgcn_readlane((int)top, 16 * i));
+    top = all;
+    if constexpr (SUM) {
+        sum += paired<0xB1>(sum);
+        sum += paired<0x4E>(sum);
+        sum += paired<0x141>(sum);
+        sum += paired<0x140>(sum);
+        sum = (of_lane(sum, 0) + of_lane(sum, 16)) + (of_lane(sum, 32) + of_lane(sum, 48));
     }
     if constexpr (TPR > 64) {
         __shared__ uint32_t s_top[TPR / 64];
@@ -120,72 +225,92 @@ __device__ __forceinline__ float row_scale(uint32_t top, double sum, const Q8Row
 
 enum Q8Form { Q8_PLAIN, Q8_NORM, Q8_NORM_ADD };
 
-// p of the eight elements from column c on; what lies behind the row's end is zero.  Adds to the sum of squares.
+// A row's own part: eight elements from column c on as p, the stream written, squares added up.
 template <typename T, int FORM>
-__device__ __forceinline__ void row_values(const Q8RowsArgs& g, uint64_t row, uint32_t c, float (&p)[8], double& sum,
-                                           bool again = false) {
-    const T* x = (again && FORM == Q8_NORM_ADD ? static_cast<const T*>(g.h) + row * g.ld_h
-                                               : static_cast<const T*>(g.x) + row * g.ld_x) + c;
-    const uint32_t n = c < g.cols ? min(g.cols - c, 8u) : 0u;
-    if (n == 8) load8(x, p); else load_part(x, n, p);
+__device__ __forceinline__ void row_values(const Q8RowsArgs& g, uint64_t row, uint32_t c, Eight<T>& x, Eight<T>& res,
+                                           const float (&w)[8], float (&p)[8], uint32_t& top, double& sum) {
+    place8(c, g.cols, x);
+    x.floats(p);
     if constexpr (FORM == Q8_PLAIN) {
         if (g.relu) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) p[i] = p[i] < 0.0f ? 0.0f : p[i];
         }
     } else {
-        if (FORM == Q8_NORM_ADD && !again) {
+        if constexpr (FORM == Q8_NORM_ADD) {
             float r[8];
-            const T* res = static_cast<const T*>(g.residual) + row * g.ld_r + c;
-            T* h = static_cast<T*>(g.h) + row * g.ld_h + c;
-            if (n == 8) load8(res, r); else load_part(res, n, r);
+            place8(c, g.cols, res);
+            res.floats(r);
             // the stream is held in its own type, and the norm is of what is held; the sum in 32 bits
             // first is rounded as the exact one would be (24 bits are more than twice 11 and two)
 #pragma unroll
             for (int i = 0; i < 8; ++i) p[i] = (float)(T)(p[i] + r[i]);
-            if (n == 8) store8(h, p); else store_part(h, n, p);
+            if (c < g.cols) store_up_to_8(static_cast<T*>(g.h) + row * g.ld_h + c, g.cols - c, p);
         }
-        float w[8];
-        if (n == 8) load8(g.weight + c, w); else load_part(g.weight + c, n, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            if (!again) sum = fma((double)p[i], (double)p[i], sum);
+            sum = fma((double)p[i], (double)p[i], sum);
             p[i] = __fmul_rn(p[i], w[i]);
         }
     }
-}
-
-__device__ __forceinline__ uint32_t top8(const float (&p)[8], uint32_t top) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) top = max(top, key_of(p[i]));      // NaN and infinity come out on top
-    return top;
 }
 
-// TPR threads a row, NV times eight elements in the registers of each.
+// TPR threads a row, NV times eight elements in the registers of each.  A block takes rows in turn: the norm's
+// weights stay in registers, and the next row is on its way while this one is reduced and coded.
 template <typename T, int FORM, uint32_t TPR, uint32_t NV>
 __global__ __launch_bounds__(TPR < BLOCK ? BLOCK : TPR) void q8_rows_kernel(Q8RowsArgs g) {
     constexpr uint32_t AT_ONCE = TPR < BLOCK ? BLOCK / TPR : 1u;      // rows of a block
     const uint32_t t = threadIdx.x % TPR, pad = (g.cols + Q8_ALIGN - 1u) & ~(Q8_ALIGN - 1u);
-    for (uint64_t row = (uint64_t)blockIdx.x * AT_ONCE + threadIdx.x / TPR; row < g.rows;
-         row += (uint64_t)gridDim.x * AT_ONCE) {
+    const uint64_t turn = (uint64_t)gridDim.x * AT_ONCE;
+    uint64_t row = (uint64_t)blockIdx.x * AT_ONCE + threadIdx.x / TPR;
+    if (row >= g.rows) return;            // whole wavefronts; a block of one row's threads stays together
+    Eight<T> x[NV], res[NV];
+    auto fetch = [&](uint64_t from) {
+        if (g.cols == 0) return;
+#pragma unroll
+        for (uint32_t v = 0; v < NV; ++v) {
+            const uint32_t c = (v * TPR + t) * 8u;
+            fetch8(static_cast<const T*>(g.x) + from * g.ld_x, c, g.cols, x[v]);
+            if constexpr (FORM == Q8_NORM_ADD) fetch8(static_cast<const T*>(g.residual) + from * g.ld_r, c, g.cols, res[v]);
+        }
+    };
+    fetch(row);
+    float w[NV][8];
+    if constexpr (FORM != Q8_PLAIN) {
+        Eight<float> e[NV];
+#pragma unroll
+        for (uint32_t v = 0; v < NV; ++v)
+            if (g.cols) fetch8(g.weight, (v * TPR + t) * 8u, g.cols, e[v]);
+#pragma unroll
+        for (uint32_t v = 0; v < NV; ++v) {
+            place8((v * TPR + t) * 8u, g.cols, e[v]);
+            e[v].floats(w[v]);
+        }
+    }
+    for (;;) {
         float p[NV][8];
         uint32_t top = 0;
         double sum = 0.0;
+        if (g.cols) {
 #pragma unroll
-        for (uint32_t v = 0; v < NV; ++v) {
-            row_values<T, FORM>(g, row, (v * TPR + t) * 8u, p[v], sum);
-            top = top8(p[v], top);
+            for (uint32_t v = 0; v < NV; ++v)
+                row_values<T, FORM>(g, row, (v * TPR + t) * 8u, x[v], res[v], w[v], p[v], top, sum);
         }
+        const uint64_t next = row + turn;
+        if (next < g.rows) fetch(next);
         row_reduce<TPR, FORM != Q8_PLAIN>(top, sum);
         if (t == 0) g.scale[row] = row_scale<FORM != Q8_PLAIN>(top, sum, g);
-        const bool none = top == 0u || top >= 0x7f800000u;
-        const float a = __uint_as_float(top), r = none ? 0.0f : q8_factor(a);
+        const RowCoder coder(top);
         uint2* q = reinterpret_cast<uint2*>(g.q + row * g.ld_q);
 #pragma unroll
         for (uint32_t v = 0; v < NV; ++v) {
             const uint32_t c = (v * TPR + t) * 8u;
-            if (c < pad) q[c / 8u] = none ? make_uint2(0u, 0u) : q8_codes(p[v], a, r);
+            if (c < pad) q[c / 8u] = coder(p[v]);
         }
+        if (next >= g.rows) break;
+        row = next;
     }
 }
 
@@ -197,38 +322,56 @@ __global__ __launch_bounds__(1024) void q8_long_rows_kernel(Q8RowsArgs g) {
     for (uint64_t row = blockIdx.x; row < g.rows; row += gridDim.x) {
         uint32_t top = 0;
         double sum = 0.0;
-        for (uint32_t c = threadIdx.x * 8u; c < pad; c += TPR * 8u) {
-            float p[8];
-            row_values<T, FORM>(g, row, c, p, sum);
-            top = top8(p, top);
-        }
+        auto values = [&](auto form, const void* from, uint64_t ld, uint32_t c, float (&p)[8]) {
+            Eight<T> x, res;
+            Eight<float> e;
+            float w[8];
+            fetch8(static_cast<const T*>(from) + row * ld, c, g.cols, x);
+            if constexpr (form.value == Q8_NORM_ADD) fetch8(static_cast<const T*>(g.residual) + row * g.ld_r, c, g.cols, res);
+            if constexpr (form.value != Q8_PLAIN) {
+                fetch8(g.weight, c, g.cols, e);
+                place8(c, g.cols, e);
+                e.floats(w);
+            }
+            row_values<T, form.value>(g, row, c, x, res, w, p, top, sum);
+        };
+        float p[8];
+        for (uint32_t c = threadIdx.x * 8u; c < pad; c += TPR * 8u)
+            values(std::integral_constant<int, FORM>{}, g.x, g.ld_x, c, p);
         row_reduce<TPR, FORM != Q8_PLAIN>(top, sum);
         if (threadIdx.x == 0) g.scale[row] = row_scale<FORM != Q8_PLAIN>(top, sum, g);
-        const bool none = top == 0u || top >= 0x7f800000u;
-        const float a = __uint_as_float(top), r = none ? 0.0f : q8_factor(a);
+        const RowCoder coder(top);
         uint2* q = reinterpret_cast<uint2*>(g.q + row * g.ld_q);
+        // the second time the stream comes from what this thread wrote
         for (uint32_t c = threadIdx.x * 8u; c < pad; c += TPR * 8u) {
-            float p[8];
-            row_values<T, FORM>(g, row, c, p, sum, true);     // the stream comes from what this thread wrote
-            q[c / 8u] = none ? make_uint2(0u, 0u) : q8_codes(p, a, r);
+            if constexpr (FORM == Q8_NORM_ADD) values(std::integral_constant<int, Q8_NORM>{}, g.h, g.ld_h, c, p);
+            else values(std::integral_constant<int, FORM>{}, g.x, g.ld_x, c, p);
+            q[c / 8u] = coder(p);
         }
     }
 }
 
 // A launch holds less than 2^32 threads; blocks take further rows in turn.
 constexpr uint32_t Q8_MAX_BLOCKS = 1u << 21;
+// Up to so many rows a row of 1025 to 2048 elements gets 256 threads with eight each, a longer one up to 8192 gets 1024; then a
+// wavefront, or 256, with more each.  us of norms in bf16, more threads / fewer: 1 x 2048 2.8 / 5.0, 777 x 1873 6.2 / 8.0,
+// 2048 x 2048 9.4 / 10.5, 8192 x 2048 23.8 / 27.2, 32768 x 2048 96.9 / 91.5; 256 x 4096 4.8 / 5.2, 512 x 4096 7.9 / 6.6.
+constexpr uint32_t Q8_ROWS_WIDE = 8192, Q8_ROWS_WIDER = 256;
+constexpr uint32_t Q8_ROWS_THREADS = 256u * 2048u;      // of the rows' kernel: all that the chip holds
 
 template <typename T, int FORM, uint32_t TPR, uint32_t NV>
 static void launch_rows_as(shifter_ctx* ctx, const Q8RowsArgs& g) {
-    constexpr uint32_t AT_ONCE = TPR < BLOCK ? BLOCK / TPR : 1u;
-    const uint32_t blocks = std::min((g.rows + AT_ONCE - 1u) / AT_ONCE, Q8_MAX_BLOCKS);
+    constexpr uint32_t AT_ONCE = TPR < BLOCK ? BLOCK / TPR : 1u, MOST = Q8_ROWS_THREADS / (AT_ONCE * TPR);
+    const uint32_t blocks = std::min((g.rows + AT_ONCE - 1u) / AT_ONCE, MOST);
     q8_rows_kernel<T, FORM, TPR, NV><<<blocks, TPR < BLOCK ? BLOCK : TPR, 0, ctx->stream>>>(g);
 }
 
 template <typename T, int FORM>
 static void launch_rows(shifter_ctx* ctx, const Q8RowsArgs& g) {
     const uint32_t units = (uint32_t)(q8_pad(g.cols) / 8u);
-    if (units <= 64) launch_rows_as<T, FORM, 64, 1>(ctx, g);
+    if (g.rows <= Q8_ROWS_WIDE && units > 128 && units <= 256) launch_rows_as<T, FORM, 256, 1>(ctx, g);
+    else if (g.rows <= Q8_ROWS_WIDER && units > 256 && units <= 1024) launch_rows_as<T, FORM, 1024, 1>(ctx, g);
+    else if (units <= 64) launch_rows_as<T, FORM, 64, 1>(ctx, g);
     else if (units <= 128) launch_rows_as<T, FORM, 64, 2>(ctx, g);
     else if (units <= 256) launch_rows_as<T, FORM, 64, 4>(ctx, g);
     else if (units <= 512) launch_rows_as<T, FORM, 256, 2>(ctx, g);
@@ -269,7 +412,7 @@ __global__ __launch_bounds__(BLOCK) void q8_read_kernel(const int8_t* __restrict
 #pragma unroll
         for (int j = 0; j < 8; ++j) f[j] = (float)(int8_t)((j < 4 ? w.x : w.y) >> (8 * (j % 4))) * s;
         T* out = x + row * ld_x + c;
-        if (c + 8u <= cols) store8(out, f); else store_part(out, cols - c, f);
+        store_up_to_8(out, cols - c, f);
     }
 }
 

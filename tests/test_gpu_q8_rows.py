@@ -75,7 +75,8 @@ def test_quantize(ops, cols, dtype):
         check_values(ops, m, dtype)
 
 
-@pytest.mark.parametrize("rows,cols", [(0, 7), (3, 0), (0, 0), (1000, 40), (777, 130)])
+@pytest.mark.parametrize("rows,cols", [(0, 7), (3, 0), (0, 0), (1000, 40), (777, 130),
+                                       (9000, 700), (9001, 1100), (2500, 4000), (300, 3001), (300, 8000), (600, 9000), (9, 2000)])
 def test_quantize_shapes(ops, rows, cols):
     x = make(rows, cols, "bf16", 3)
     m = ops.quantize(x)
@@ -198,6 +199,20 @@ def test_rms_norm(ops, cols, dtype):
                 m2, h2 = ops.rms_norm(a, w, 1e-5, residual=b, h=(a, b)[at])
                 assert h2 is (a, b)[at] and torch.equal(h2.cpu(), want_h)
                 assert torch.equal(m2.q, m.q) and torch.equal(m2.scale, m.scale)
+
+
+@pytest.mark.parametrize("rows,cols", [(9000, 300), (9000, 700), (9001, 1100), (2500, 4000), (300, 3001), (300, 8000), (600, 9000),
+                                       (9, 2000), (530, 20000)])
+def test_rms_norm_many_rows(ops, rows, cols):
+    """More rows than a launch's blocks hold at once, and both sides of the rules on rows."""
+    for dtype in Q.DTYPES:
+        x, r = make(rows, cols, dtype, 1), make(rows, cols, dtype, 2, gap=3)
+        w = (1.0 + 0.3 * torch.randn(cols, generator=torch.Generator().manual_seed(3))).to(DEV)
+        q, s, want_h = Q.rms_norm(x, w, float(np.float32(1e-6)), r)
+        m, h = ops.rms_norm(x, w, 1e-6, residual=r, h=x)          # in place
+        assert h is x and torch.equal(h.cpu(), want_h)
+        check_codes(m, q)
+        check_scales(m.scale, s)
 
 
 def test_rms_norm_ends(ops):
