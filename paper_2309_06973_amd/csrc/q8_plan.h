@@ -48,8 +48,9 @@ inline const char* q8_bad_codes(const void* q, const void* scale, uint64_t rows,
 enum Q8Kernel { Q8_FEW, Q8_TILE_64x64, Q8_TILE_64x128, Q8_TILE_128x256, Q8_TILE_256x256, Q8_KERNELS };
 struct Q8TileCost {
     uint32_t rows, cols;
-    double start, alone, full;    // us: a launch and a tile's ends; a stage of 128 bytes on an empty chip, on a full one
-    bool shared;                  // two blocks to a compute unit: rounds are no whole numbers
+    // us: a launch and a tile's ends; then a stage of 128 bytes: a tile alone on the chip, one on each compute unit, and, where
+    // two share a unit, a tile's part of it (0: they do not, and rounds are whole numbers)
+    double start, alone, one, shared;
 };
 // Measured on 256 compute units, us a call by kernel (the four tiles):
 //    m x n x k            64x64   64x128  128x256  256x256         m x n x k           64x64   64x128  128x256  256x256
@@ -59,19 +60,19 @@ struct Q8TileCost {
 //    2048 x 4096 x 4096    60.9     47.5     38.0     48.6         4096 x 1024 x 8192   57.9     44.5     55.1     77.3
 //    777 x 1873 x 977       7.1      6.9     11.5     17.4         16384 x 100 x 2048   12.7     11.1     18.1     26.8
 // The costs below say these within 15 %; the kernel of the least cost is taken.
-constexpr Q8TileCost Q8_TILES[] = {{64, 64, 3.2, 0.215, 0.235, true},
-                                   {64, 128, 3.5, 0.30, 0.375, true},
-                                   {128, 256, 5.0, 0.76, 1.03, false},
-                                   {256, 256, 7.0, 1.04, 1.72, false}};
+constexpr Q8TileCost Q8_TILES[] = {{64, 64, 3.2, 0.215, 0.235, 0.235},
+                                   {64, 128, 3.5, 0.30, 0.38, 0.37},
+                                   {128, 256, 5.0, 0.76, 1.03, 0.0},
+                                   {256, 256, 7.0, 1.04, 1.72, 0.0}};
 constexpr double Q8_UNITS = 256.0;      // compute units
 
 // us of a product of m x n sums over k bytes, each made by `parts` blocks.
 inline double q8_tile_us(const Q8TileCost& c, uint64_t m, uint64_t n, uint64_t k, uint64_t parts = 1) {
     const double tiles = (double)((m + c.rows - 1u) / c.rows) * (double)((n + c.cols - 1u) / c.cols) * (double)parts;
-    const double stages = (double)(((k + 127u) / 128u + parts - 1u) / parts), share = tiles < Q8_UNITS ? tiles / Q8_UNITS : 1.0;
-    double rounds = tiles / Q8_UNITS;
-    if (!c.shared && rounds > 1.0) rounds = (double)((uint64_t)((tiles + Q8_UNITS - 1.0) / Q8_UNITS));
-    return c.start + stages * (c.alone + (c.full - c.alone) * share) * (rounds < 1.0 ? 1.0 : rounds);
+    const double stages = (double)(((k + 127u) / 128u + parts - 1u) / parts), rounds = tiles / Q8_UNITS;
+    if (rounds <= 1.0) return c.start + stages * (c.alone + (c.one - c.alone) * rounds);
+    if (c.shared > 0.0) return c.start + stages * (c.shared * rounds > c.one ? c.shared * rounds : c.one);
+    return c.start + stages * c.one * (double)((uint64_t)((tiles + Q8_UNITS - 1.0) / Q8_UNITS));
 }
 
 // Up to 16 rows the reading of the weights is all there is, and the kernel without LDS does it best: 1 x 4096 x 4096 5.4 us
@@ -100,10 +101,10 @@ constexpr uint32_t Q8_SELF_ROWS = 512;
 //    2048 x 2048 x 2048     33.8     28.5     26.3     36.1         2048 x 1873 x 977      18.1     19.5     21.7     36.5
 //    16384 x 512 x 512      76.2     89.0      113      196         64 x 512 x 512          5.3      6.9      7.2     11.0
 enum Q8GradientKernel { Q8_GRAD_64x64, Q8_GRAD_64x128, Q8_GRAD_64x256, Q8_GRAD_128x256, Q8_GRAD_KERNELS };
-constexpr Q8TileCost Q8_GRAD_TILES[] = {{64, 64, 3.5, 0.57, 0.43, true},
-                                        {64, 128, 4.0, 0.67, 0.67, true},
-                                        {64, 256, 5.0, 0.85, 1.32, false},
-                                        {128, 256, 7.0, 1.50, 2.29, false}};
+constexpr Q8TileCost Q8_GRAD_TILES[] = {{64, 64, 3.5, 0.57, 0.62, 0.43},
+                                        {64, 128, 4.0, 0.67, 0.97, 0.67},
+                                        {64, 256, 5.0, 0.85, 1.32, 0.0},
+                                        {128, 256, 7.0, 1.50, 2.29, 0.0}};
 // Where tiles are few the rows are split among `parts` blocks a tile; their sums, fp32, are joined by a launch of its own,
 // which costs that and the traffic.
 constexpr uint64_t Q8_PARTS = 32;

@@ -14,7 +14,7 @@
 #include <type_traits>
 
 #include "dev_common.h"
-#include "q8.h"
+#include "q8_eight.h"
 
 namespace shifter {
 
@@ -401,20 +401,6 @@ constexpr float DIGITS_TOP = 8355711.0f;     // 127 * (2^16 + 2^8 + 1): the larg
 __device__ __forceinline__ float digits_up(float c) { return c < 0x1p-90f ? 0x1p90f : 1.0f; }
 __device__ __forceinline__ float digits_down(float c) { return c < 0x1p-90f ? 0x1p-90f : 1.0f; }
 
-// Eight neighbours of a row, zeros behind the n that there are.
-template <typename T>
-__device__ __forceinline__ void load_up_to_8(const T* p, uint32_t n, float (&f)[8]) {
-    typedef T vec __attribute__((ext_vector_type(8), aligned(sizeof(T))));
-    if (n >= 8u) {
-        const vec v = *reinterpret_cast<const vec*>(p);
-#pragma unroll
-        for (uint32_t i = 0; i < 8; ++i) f[i] = (float)v[i];
-    } else {
-#pragma unroll
-        for (uint32_t i = 0; i < 8; ++i) f[i] = i < n ? (float)p[i] : 0.0f;
-    }
-}
-
 // Four words of four bytes, turned: byte i of word j becomes byte j of word i.
 __device__ __forceinline__ void turn_bytes(uint32_t& a, uint32_t& b, uint32_t& c, uint32_t& d) {
     const uint32_t ab0 = __builtin_amdgcn_perm(b, a, 0x05010400u), ab1 = __builtin_amdgcn_perm(b, a, 0x07030602u);
@@ -466,19 +452,24 @@ __device__ __forceinline__ void column_tops(const Q8GradientArgs& a, uint32_t n,
 #pragma unroll
     for (uint32_t i = 0; i < 8; ++i) top[i] = 0;
     if (n >= a.n) return;
-    const T* g = static_cast<const T*>(a.g) + n;
+    const T* g = static_cast<const T*>(a.g);
     for (uint32_t r = r0; r < r1; r += 8u * step) {                      // eight rows under way
-        float f[8][8], s[8];
+        Eight<T> e[8];
+        float s[8];
 #pragma unroll
         for (uint32_t x = 0; x < 8; ++x) {
             const uint32_t at = min(r + x * step, r1 - 1u);              // behind the last one: it again
-            load_up_to_8(g + (uint64_t)at * a.ld_g, a.n - n, f[x]);
+            fetch8(g + (uint64_t)at * a.ld_g, n, a.n, e[x]);
             s[x] = a.s[at];
         }
 #pragma unroll
-        for (uint32_t x = 0; x < 8; ++x)
+        for (uint32_t x = 0; x < 8; ++x) {
+            float f[8];
+            place8(n, a.n, e[x]);
+            e[x].floats(f);
 #pragma unroll
-            for (uint32_t i = 0; i < 8; ++i) top[i] = max(top[i], key_of(__fmul_rn(f[x][i], s[x])));
+            for (uint32_t i = 0; i < 8; ++i) top[i] = max(top[i], key_of(__fmul_rn(f[i], s[x])));
+        }
     }
 }
 
@@ -515,22 +506,34 @@ __global__ __launch_bounds__(BLOCK) void q8_digits_kernel(Q8GradientArgs a, Q8Gr
     const uint32_t across = (a.n + 63u) / 64u, n0 = blockIdx.x % across * 64u;
     const uint32_t first = blockIdx.x / across * deep * TURN_ROWS, last = min(first + deep * TURN_ROWS, (uint32_t)pl.ld);
     const uint32_t cg = threadIdx.x & 7u, rg = threadIdx.x >> 3, n = n0 + cg * 8u;
-    float f[4][8], s[4];
+    Eight<T> e[4];
+    float s[4];
     auto fetch = [&](uint32_t m0) {
 #pragma unroll
         for (uint32_t r = 0; r < 4; ++r) {
-            const uint32_t m = m0 + rg * 4u + r;
-            const bool there = m < a.m && n < a.n;                           // the others read as zero
-            load_up_to_8(static_cast<const T*>(a.g) + (there ? (uint64_t)m * a.ld_g + n : 0u), there ? a.n - n : 0u, f[r]);
-            s[r] = there ? a.s[m] : 0.0f;
+            const uint32_t m = min(m0 + rg * 4u + r, a.m - 1u);              // behind the last one: it again
+            fetch8(static_cast<const T*>(a.g) + (uint64_t)m * a.ld_g, n, a.n, e[r]);
+            s[r] = a.s[m];
         }
     };
     fetch(first);
     if (threadIdx.x < 64u) s_top[threadIdx.x] = 0;
     __syncthreads();
     if constexpr (SELF) {
-        uint32_t top[8];
-        column_tops<T>(a, n, rg, a.m, BLOCK / 8u, top);
+        uint32_t top[8] = {};
+        if (a.m > TURN_ROWS) {
+            column_tops<T>(a, n, rg, a.m, BLOCK / 8u, top);
+        } else {                               // all the rows there are have been fetched
+#pragma unroll
+            for (uint32_t r = 0; r < 4; ++r) {
+                Eight<T> x = e[r];
+                float f[8];
+                place8(n, a.n, x);
+                x.floats(f);
+#pragma unroll
+                for (uint32_t i = 0; i < 8; ++i) top[i] = max(top[i], key_of(__fmul_rn(f[i], s[r])));
+            }
+        }
 #pragma unroll
         for (uint32_t i = 0; i < 8; ++i) {
             for (uint32_t d = 8; d < 64; d <<= 1) top[i] = max(top[i], (uint32_t)__shfl_xor((int)top[i], (int)d, 64));
@@ -561,17 +564,22 @@ __global__ __launch_bounds__(BLOCK) void q8_digits_kernel(Q8GradientArgs a, Q8Gr
     for (uint32_t m0 = first; m0 < last; m0 += TURN_ROWS) {
         uint32_t d[3][8] = {};
 #pragma unroll
-        for (uint32_t r = 0; r < 4; ++r)
+        for (uint32_t r = 0; r < 4; ++r) {
+            const bool there = m0 + rg * 4u + r < a.m;                       // rows behind the last one count as zero
+            float f[8];
+            place8(n, a.n, e[r]);
+            e[r].floats(f);
 #pragma unroll
             for (uint32_t i = 0; i < 8; ++i) {
                 // a column that is not finite has factor 0, and NaN in its own place alone
-                const float t = rintf(__fmul_rn(__fmul_rn(__fmul_rn(f[r][i], s[r]), up[i]), factor[i]));
-                const int32_t v = (int32_t)fminf(fmaxf(t, -DIGITS_TOP), DIGITS_TOP);
+                const float t = rintf(__fmul_rn(__fmul_rn(__fmul_rn(f[i], s[r]), up[i]), factor[i]));
+                const int32_t v = there ? (int32_t)fminf(fmaxf(t, -DIGITS_TOP), DIGITS_TOP) : 0;
                 const int32_t v1 = (v + 128) >> 8, v2 = (v1 + 128) >> 8;     // what the digits from d1, from d2 on stand for
                 d[0][i] |= ((uint32_t)v & 255u) << (8u * r);
                 d[1][i] |= ((uint32_t)v1 & 255u) << (8u * r);
                 d[2][i] |= ((uint32_t)v2 & 255u) << (8u * r);
             }
+        }
         if (m0 + TURN_ROWS < last) fetch(m0 + TURN_ROWS);
 #pragma unroll
         for (uint32_t p = 0; p < 3; ++p)
