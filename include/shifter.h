@@ -711,7 +711,8 @@ int shifter_compact_batch_masked(shifter_ctx* ctx, const shifter_model* model, c
  *                        a p that is not finite has NaN in its whole row of dw (masked entries aside).
  *                        m up to SHIFTER_Q8_MAX_SUM, else SHIFTER_ERR_CAPACITY; more rows go in several calls with
  *                        SHIFTER_Q8_ACCUMULATE.
- *                        d_work: work_bytes of shifter_weight_grad_q8_layout, 256-byte aligned. */
+ *                        d_work: work_bytes of shifter_weight_grad_q8_layout, 256-byte aligned; NULL where that says
+ *                        0, as it does for few rows. */
 typedef enum { SHIFTER_F32 = 0, SHIFTER_BF16 = 1, SHIFTER_F16 = 2 } shifter_dtype;
 #define SHIFTER_Q8_RELU 1u
 #define SHIFTER_Q8_ACCUMULATE 2u

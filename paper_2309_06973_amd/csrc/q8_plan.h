@@ -100,7 +100,8 @@ constexpr uint32_t Q8_SELF_ROWS = 512;
 //    16384 x 4096 x 4096     886      695      683      593         512 x 4096 x 1024      14.0     12.5     11.9     18.0
 //    2048 x 2048 x 2048     33.8     28.5     26.3     36.1         2048 x 1873 x 977      18.1     19.5     21.7     36.5
 //    16384 x 512 x 512      76.2     89.0      113      196         64 x 512 x 512          5.3      6.9      7.2     11.0
-enum Q8GradientKernel { Q8_GRAD_64x64, Q8_GRAD_64x128, Q8_GRAD_64x256, Q8_GRAD_128x256, Q8_GRAD_KERNELS };
+// Q8_GRAD_SMALL: no digits and no workspace, sums in 64-bit floating point (which the vector units add as fast as 32-bit).
+enum Q8GradientKernel { Q8_GRAD_SMALL = -1, Q8_GRAD_64x64, Q8_GRAD_64x128, Q8_GRAD_64x256, Q8_GRAD_128x256, Q8_GRAD_KERNELS };
 constexpr Q8TileCost Q8_GRAD_TILES[] = {{64, 64, 3.5, 0.57, 0.62, 0.43},
                                         {64, 128, 4.0, 0.67, 0.97, 0.67},
                                         {64, 256, 5.0, 0.85, 1.32, 0.0},
@@ -108,6 +109,13 @@ constexpr Q8TileCost Q8_GRAD_TILES[] = {{64, 64, 3.5, 0.57, 0.62, 0.43},
 // Where tiles are few the rows are split among `parts` blocks a tile; their sums, fp32, are joined by a launch of its own,
 // which costs that and the traffic.
 constexpr uint64_t Q8_PARTS = 32;
+// Few rows, and few products in all, go to the small kernel's one launch.  us, that / digits and tiles: 1 x 64 x 64 4.1 / 10.7,
+// 1 x 4096 x 4096 17.3 / 34.5, 16 x 4096 x 4096 24.5 / 34.4, 32 x 4096 x 4096 36.3 / 34.4; 64 x 512 x 512 9.3 / 11.7,
+// 64 x 2048 x 2048 20.6 / 17.2, 128 x 1024 x 1024 16.9 / 12.3.
+constexpr uint64_t Q8_SMALL_ROWS = 16, Q8_SMALL_ROWS_MOST = 64, Q8_SMALL_WORK = 1ull << 27;
+constexpr bool q8_small(uint64_t m, uint64_t n, uint64_t k) {
+    return m <= Q8_SMALL_ROWS || (m <= Q8_SMALL_ROWS_MOST && m * n * k <= Q8_SMALL_WORK);
+}
 constexpr double q8_join_us(uint64_t parts, uint64_t n, uint64_t k) {
     return parts > 1 ? 3.5 + 2.0e-6 * (double)parts * (double)n * (double)k : 0.0;
 }
@@ -129,6 +137,13 @@ inline Q8GradientPlan q8_gradient_plan(uint64_t m, uint64_t n, uint64_t k) {
     p.digits = (p.slice_tops + 4u * n * p.slices + 255u) & ~(uint64_t)255u;
     p.codes = p.digits + 3u * n * p.ld;
     p.sums = p.codes + k * p.ld;
+    p.parts = 1;
+    p.part_rows = (uint32_t)p.ld;
+    if (q8_small(m, n, k)) {
+        p.kernel = Q8_GRAD_SMALL;
+        p.bytes = 0;
+        return p;
+    }
     p.kernel = Q8_GRAD_64x64;
     uint64_t parts = 1;
     double least = 0.0;
@@ -138,8 +153,8 @@ inline Q8GradientPlan q8_gradient_plan(uint64_t m, uint64_t n, uint64_t k) {
             if ((i == 0 && x == 1) || us < least) { least = us; p.kernel = (Q8GradientKernel)i; parts = x; }
         }
     p.part_rows = (uint32_t)((p.ld / 128u + parts - 1u) / parts * 128u);
-    p.parts = p.ld ? (uint32_t)((p.ld + p.part_rows - 1u) / p.part_rows) : 1u;
-    p.bytes = m ? p.sums + (p.parts > 1 ? 4u * (uint64_t)p.parts * n * k : 0u) : 0u;
+    p.parts = (uint32_t)((p.ld + p.part_rows - 1u) / p.part_rows);
+    p.bytes = p.sums + (p.parts > 1 ? 4u * (uint64_t)p.parts * n * k : 0u);
     return p;
 }
 

@@ -640,7 +640,7 @@ __global__ __launch_bounds__(64 * WA * WB) void q8_gradient_kernel(Q8GradientArg
     const uint32_t n0 = ta * Tl::RA, k0 = tb * Tl::RB;
     const int8_t* digits = reinterpret_cast<const int8_t*>(g.work + pl.digits);
     const int8_t* codes = reinterpret_cast<const int8_t*>(g.work + pl.codes);
-    const float top = pl.ld ? reinterpret_cast<const float*>(g.work + pl.tops)[min(n0 + threadIdx.x % Tl::RA, g.n - 1u)] : 0.0f;
+    const float top = reinterpret_cast<const float*>(g.work + pl.tops)[min(n0 + threadIdx.x % Tl::RA, g.n - 1u)];
     Tl t;
     const uint32_t m0 = blockIdx.y * pl.part_rows;
     t.run(digits + (uint64_t)n0 * pl.ld + m0, pl.ld, (uint64_t)g.n * pl.ld, g.n - n0, codes + (uint64_t)k0 * pl.ld + m0, pl.ld,
@@ -679,9 +679,94 @@ __global__ __launch_bounds__(64 * WA * WB) void q8_gradient_kernel(Q8GradientArg
     }
 }
 
+// Few rows or few products: one launch, no digits.  A block has 16 columns of g and 256 of the checkpoint, a thread
+// four by four of the sums, which are 64-bit.  Products of a p and a code are exact in them.
+template <typename T>
+__global__ __launch_bounds__(BLOCK) void q8_gradient_small_kernel(Q8GradientArgs a) {
+    constexpr uint32_t DEEP = 32;                                        // rows of p in LDS at a time
+    __shared__ __align__(16) double s_p[DEEP][16];
+    const uint32_t across = (a.k + 255u) / 256u, n0 = blockIdx.x / across * 16u, k0 = blockIdx.x % across * 256u;
+    const uint32_t lane = threadIdx.x & 63u, wave = uniform_u32(threadIdx.x >> 6), k = k0 + lane * 4u;
+    const uint32_t n_of = n0 + (threadIdx.x & 15u), r_of = threadIdx.x >> 4;      // the p that this thread makes
+    const bool there = k < a.k;                                          // the codes behind the last column are in the row's padding
+    double acc[4][4] = {};
+    for (uint32_t m0 = 0; m0 < a.m; m0 += DEEP) {
+        const uint32_t rows = min(DEEP, a.m - m0);
+        uint32_t q[DEEP / 4];
+        auto codes = [&](uint32_t from) {
+#pragma unroll
+            for (uint32_t r = 0; r < DEEP / 4; ++r)
+                q[r] = there ? *reinterpret_cast<const uint32_t*>(a.q + (uint64_t)(m0 + min(from + r, rows - 1u)) * a.ld_q + k) : 0u;
+        };
+        codes(0);
+        if (m0) __syncthreads();
+#pragma unroll
+        for (uint32_t r = r_of; r < DEEP; r += BLOCK / 16u) {
+            const uint32_t m = m0 + min(r, rows - 1u);
+            const float p = __fmul_rn((float)static_cast<const T*>(a.g)[(uint64_t)m * a.ld_g + min(n_of, a.n - 1u)], a.s[m]);
+            s_p[r][threadIdx.x & 15u] = r < rows ? (double)p : 0.0;
+        }
+        __syncthreads();
+#pragma unroll
+        for (uint32_t from = 0; from < DEEP; from += DEEP / 4) {
+            if (from >= rows) break;
+            uint32_t now[DEEP / 4];
+#pragma unroll
+            for (uint32_t r = 0; r < DEEP / 4; ++r) now[r] = q[r];
+            if (from + DEEP / 4 < rows) codes(from + DEEP / 4);
+#pragma unroll
+            for (uint32_t r = 0; r < DEEP / 4; ++r) {
+                double p[4];
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i) p[i] = s_p[from + r][wave * 4u + i];
+#pragma unroll
+                for (uint32_t j = 0; j < 4; ++j) {
+                    const double c = (double)(int8_t)(now[r] >> (8u * j));
+#pragma unroll
+                    for (uint32_t i = 0; i < 4; ++i) acc[i][j] = fma(p[i], c, acc[i][j]);
+                }
+            }
+        }
+    }
+    if (!there) return;
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i) {
+        const uint32_t n = n0 + wave * 4u + i;
+        if (n >= a.n) break;
+        float* to = a.dw + (uint64_t)n * a.ld_dw + k;
+        const uint8_t* mask = a.mask + (uint64_t)n * a.ld_mask + k;
+        typedef float loose __attribute__((ext_vector_type(4), aligned(4)));
+        float v[4];
+        uint32_t keep = 0xffffffffu;
+        const bool whole = k + 4u <= a.k;
+        if (a.mask) {
+            keep = 0;
+            if (whole) keep = *reinterpret_cast<const u32_a1*>(mask);
+            else
+                for (uint32_t j = 0; k + j < a.k; ++j) keep |= (uint32_t)mask[j] << (8u * j);
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) {
+            // a column with a p that is not finite: NaN in the whole row, as where digits are made
+            v[j] = isfinite(acc[i][j]) ? (float)acc[i][j] : __uint_as_float(0x7fc00000u);
+            const float old = a.accumulate && k + j < a.k ? to[j] : 0.0f;
+            v[j] = keep >> (8u * j) & 255u ? (a.accumulate ? old + v[j] : v[j]) : old;
+        }
+        if (whole) *reinterpret_cast<loose*>(to) = loose{v[0], v[1], v[2], v[3]};
+        else
+            for (uint32_t j = 0; k + j < a.k; ++j) to[j] = v[j];
+    }
+}
+
+template <typename T>
+static void launch_gradient_small(shifter_ctx* ctx, const Q8GradientArgs& g) {
+    ProfileScope ps(ctx, K_Q8_GRADIENT);
+    const uint64_t blocks = (uint64_t)((g.n + 15u) / 16u) * ((g.k + 255u) / 256u);
+    q8_gradient_small_kernel<T><<<(uint32_t)blocks, BLOCK, 0, ctx->stream>>>(g);
+}
+
 template <typename T>
 static void launch_digits(shifter_ctx* ctx, const Q8GradientArgs& g, const Q8GradientPlan& pl) {
-    if (pl.ld == 0) return;
     const uint32_t turns = turn_blocks(g, pl), across = (g.n + 63u) / 64u, tiles = (uint32_t)(pl.ld / TURN_ROWS);
     if (pl.slices == 0) {
         q8_digits_kernel<T, true><<<across * tiles + turns, BLOCK, 0, ctx->stream>>>(g, pl, across * tiles, 1u);
@@ -738,6 +823,12 @@ static void launch_gradient_as(shifter_ctx* ctx, const Q8GradientArgs& g, const 
 
 void launch_q8_gradient(shifter_ctx* ctx, int dtype, const Q8GradientArgs& g) {
     const Q8GradientPlan pl = q8_gradient_plan(g.m, g.n, g.k);
+    if (pl.kernel == Q8_GRAD_SMALL) {
+        if (dtype == SHIFTER_F32) launch_gradient_small<float>(ctx, g);
+        else if (dtype == SHIFTER_BF16) launch_gradient_small<__bf16>(ctx, g);
+        else launch_gradient_small<_Float16>(ctx, g);
+        return;
+    }
     {
         ProfileScope ps(ctx, K_Q8_DIGITS);
         if (dtype == SHIFTER_F32) launch_digits<float>(ctx, g, pl);

@@ -195,13 +195,15 @@ class Q8:
             raise ValueError("out must be float32")
         out, _, ld_out = self._result(n, k, torch.float32, out)
         need = S.shifter_weight_grad_q8_layout(m, n, k)
-        if self.work is None or self.work.numel() < need:
-            self.work = torch.empty(need, dtype=torch.uint8, device=self.dev)
-        if torch.cuda.is_current_stream_capturing() and not any(w is self.work for w in self.recorded):
-            self.recorded.append(self.work)
+        work = None
+        if need:
+            if self.work is None or self.work.numel() < need:
+                self.work = torch.empty(need, dtype=torch.uint8, device=self.dev)
+            work = self.work
+            if torch.cuda.is_current_stream_capturing() and not any(w is work for w in self.recorded):
+                self.recorded.append(work)
         S.shifter_weight_grad_q8(self.ctx, g, t, ld, x.q, x.ld, x.scale, m, n, k, mask, ld_mask,
-                                 S.SHIFTER_Q8_ACCUMULATE if accumulate else 0, out, ld_out, self.work,
-                                 self.work.numel())
+                                 S.SHIFTER_Q8_ACCUMULATE if accumulate else 0, out, ld_out, work, need)
         return out
 
 

@@ -181,7 +181,8 @@ def test_gradient_columns(ops, n):
 
 
 @pytest.mark.parametrize("m,n,k", [(64, 512, 512), (1000, 700, 900), (300, 1500, 100), (40, 100, 3000), (4100, 260, 520),
-                                   (128, 2500, 2600), (700, 20, 5000)])
+                                   (128, 2500, 2600), (700, 20, 5000), (100, 2400, 2410), (30, 4300, 4301),
+                                   (256, 1500, 1401), (256, 1400, 1300)])
 def test_gradient_sizes(ops, m, n, k):
     for dtype in Q.DTYPES:
         check_gradient(ops, m, n, k, dtype, seed=m, mask=dtype != "fp32")
@@ -255,6 +256,7 @@ def test_refusals(ops):
                dict(out=torch.zeros((4, 7), device=DEV)), dict(out=torch.zeros((6, 4), device=DEV).t())):
         with pytest.raises(ValueError):
             ops.matmul(a, b, **kw)
+    tall, _, _ = matrix(300, 40, 3)
     g = torch.zeros((4, 6), device=DEV)
     for kw in (dict(mask=torch.zeros((6, 39), dtype=torch.uint8, device=DEV)), dict(mask=torch.zeros((6, 40), device=DEV)),
                dict(mask=torch.zeros((6, 40), dtype=torch.uint8)), dict(accumulate=True),
@@ -276,7 +278,8 @@ def test_refusals(ops):
     d = torch.zeros((6, 40), device=DEV)
     for w, n, what in ((work, 100, "too small"), (None, 1 << 20, "256"), (work[1:], 1 << 19, "256")):
         with pytest.raises(S.ShifterError) as e:
-            S.shifter_weight_grad_q8(ops.ctx, g, 0, 6, a.q, 48, a.scale, 4, 6, 40, None, 0, 0, d, 40, w, n)
+            S.shifter_weight_grad_q8(ops.ctx, torch.zeros((300, 6), device=DEV), 0, 6, tall.q, 48, tall.scale, 300, 6, 40,
+                                     None, 0, 0, d, 40, w, n)
         assert e.value.code == S.SHIFTER_ERR_INVALID_ARG and what in str(e.value)
 
 

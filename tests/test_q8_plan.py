@@ -57,17 +57,20 @@ int main() {
     WANT(q8_bad_codes(p, p, 3, 17, (1u << 22) + 16), "2^22");
     WANT(q8_bad_codes(p, p, 1ull << 31, 17, 32), "rows or columns");
     // workspace: the parts follow one another, every slice has rows, the rows are all in slices
-    const uint64_t ms[] = {0, 1, 127, 128, 129, 8191, 8192, 8193, 16384, 20000, 131071};
+    const uint64_t ms[] = {0, 1, 64, 127, 128, 129, 8191, 8192, 8193, 16384, 20000, 131071};
     const uint64_t ns[] = {1, 63, 500, 2048, 4097};
     int used[Q8_GRAD_KERNELS] = {0}, split = 0;
     for (uint64_t m : ms)
         for (uint64_t n : ns)
             for (uint64_t k : ns) {
                 const Q8GradientPlan g = q8_gradient_plan(m, n, k);
-                bool ok = g.ld >= m && g.ld < m + 128 && g.ld % 128 == 0 && g.slices <= Q8_SLICES && g.slice_rows % Q8_SLICE_ROWS == 0;
+                const bool is_small = m <= 16 || (m <= 64 && m * n * k <= 1ull << 27);
+                if ((g.kernel == Q8_GRAD_SMALL) != is_small || (is_small && g.bytes != 0)) { printf("small %llu %llu %llu\n", (unsigned long long)m, (unsigned long long)n, (unsigned long long)k); ++bad; }
+                if (is_small) continue;
+                bool ok = m > 0 && g.ld >= m && g.ld < m + 128 && g.ld % 128 == 0 && g.slices <= Q8_SLICES && g.slice_rows % Q8_SLICE_ROWS == 0;
                 ok = ok && (m <= Q8_SELF_ROWS ? g.slices == 0 : (uint64_t)g.slices * g.slice_rows >= m && (uint64_t)(g.slices - 1) * g.slice_rows < m);
                 ok = ok && g.tops == 0 && g.slice_tops >= 4 * n && g.digits >= g.slice_tops + 4 * n * g.slices && g.digits % 256 == 0;
-                ok = ok && g.kernel < Q8_GRAD_KERNELS && g.parts >= 1 && g.parts <= Q8_PARTS && g.part_rows % 128 == 0;
+                ok = ok && g.kernel >= 0 && g.kernel < Q8_GRAD_KERNELS && g.parts >= 1 && g.parts <= Q8_PARTS && g.part_rows % 128 == 0;
                 ok = ok && (uint64_t)g.parts * g.part_rows >= g.ld && (g.ld == 0 || (uint64_t)(g.parts - 1) * g.part_rows < g.ld);
                 ok = ok && g.sums == g.codes + k * g.ld && g.sums % 128 == 0 && (m == 0 || g.bytes == g.sums + (g.parts > 1 ? 4 * g.parts * n * k : 0));
                 if (ok) { ++used[g.kernel]; split += g.parts > 1; }
@@ -105,7 +108,8 @@ def test_checks_and_plan(tmp_path):
 
 def test_layout_call_and_calls_without_a_context():
     assert S.shifter_weight_grad_q8_layout(0, 5, 5) == 0
-    assert S.shifter_weight_grad_q8_layout(100, 5, 7) >= 128 * (3 * 5 + 7)
+    assert S.shifter_weight_grad_q8_layout(16, 5000, 7000) == S.shifter_weight_grad_q8_layout(60, 50, 70) == 0
+    assert S.shifter_weight_grad_q8_layout(1000, 5, 7) >= 1024 * (3 * 5 + 7)
     with pytest.raises(S.ShifterError) as e:
         S.shifter_weight_grad_q8_layout(S.SHIFTER_Q8_MAX_SUM + 1, 5, 5)
     assert e.value.code == S.SHIFTER_ERR_CAPACITY
