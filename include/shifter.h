@@ -697,7 +697,8 @@ int shifter_compact_batch_masked(shifter_ctx* ctx, const shifter_model* model, c
  *                        64 bits.  A row of zeros has scale 0 (also where eps is 0).
  * shifter_matmul_q8      c[m][n] = sa[m] sb[n] sum_k qa[m][k] qb[n][k] + bias[n], ReLU with
  *                        SHIFTER_Q8_RELU, rounded to the element type.  The sum is exact in 32-bit integers:
- *                        k up to SHIFTER_Q8_MAX_SUM, else SHIFTER_ERR_CAPACITY.  d_bias may be NULL.
+ *                        k up to SHIFTER_Q8_MAX_SUM, else SHIFTER_ERR_CAPACITY (also for m x n of about 2^35 and more,
+ *                        or n of 2^26, which a launch does not hold).  d_bias may be NULL.
  *                        For k = 0 the sum is 0.  The result does not depend on the device's state or on how the
  *                        work is split.
  * shifter_weight_grad_q8 dw[n][k] = sum over the m rows of g[m][n] scale[m] q[m][k], the gradient of a linear

@@ -1759,6 +1759,7 @@ extern "C" int shifter_matmul_q8(shifter_ctx* ctx, const int8_t* d_qa, uint64_t 
     if (k > SHIFTER_Q8_MAX_SUM)
         return fail(ctx, SHIFTER_ERR_CAPACITY, "matmul_q8: sums of more than 131071 products do not fit 32 bits");
     if (m == 0 || n == 0) return SHIFTER_OK;
+    if (const char* why = q8_too_many(m, n)) return fail(ctx, SHIFTER_ERR_CAPACITY, std::string("matmul_q8: ") + why);
     Q8ProductArgs a{};
     a.a = d_qa; a.b = d_qb; a.sa = d_sa; a.sb = d_sb; a.bias = d_bias;
     a.ld_a = ld_a; a.ld_b = ld_b; a.ld_c = ld_c;
@@ -1799,6 +1800,7 @@ extern "C" int shifter_weight_grad_q8(shifter_ctx* ctx, const void* d_g, int dty
     if (need && (!d_work || misaligned(d_work, 256)))
         return fail(ctx, SHIFTER_ERR_INVALID_ARG, "weight_grad_q8: the workspace must be 256-byte aligned");
     if (n == 0 || k == 0) return SHIFTER_OK;
+    if (const char* why = q8_too_many(n, k)) return fail(ctx, SHIFTER_ERR_CAPACITY, std::string("weight_grad_q8: ") + why);
     Q8GradientArgs a{};
     a.g = d_g; a.q = d_q; a.s = d_scale; a.mask = d_mask;
     a.ld_g = ld_g; a.ld_q = ld_q; a.ld_mask = ld_mask; a.ld_dw = ld_dw;

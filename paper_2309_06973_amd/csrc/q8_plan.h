@@ -20,6 +20,14 @@ constexpr uint64_t q8_pad(uint64_t cols) { return (cols + Q8_ALIGN - 1u) & ~(uin
 
 inline bool q8_off(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1u)) != 0; }
 
+// A launch holds less than 2^32 threads.  The largest tiles that could be meant have 64 x 64 results and 512 threads, the
+// smallest blocks 16 columns; results of so many do not fit that.
+inline const char* q8_too_many(uint64_t rows, uint64_t cols) {
+    const uint64_t tiles = ((rows + 63u) / 64u) * ((cols + 63u) / 64u), strips = (cols + 15u) / 16u;
+    return tiles >= (1ull << 23) || strips >= (1ull << 22) || (rows + 15u) / 16u * ((cols + 255u) / 256u) >= (1ull << 24)
+               ? "a result of more tiles than a launch holds" : nullptr;
+}
+
 // What is wrong with a matrix of elements of `size` bytes, or nullptr.
 inline const char* q8_bad_rows(const void* p, uintptr_t size, uint64_t rows, uint64_t cols, uint64_t ld) {
     if (rows > Q8_MAX_ROWS || cols > Q8_MAX_ROWS) return "more than 2^31 - 1 rows or columns";
@@ -45,25 +53,31 @@ inline const char* q8_bad_codes(const void* q, const void* scale, uint64_t rows,
 
 // The product's kernels.  Tiles of rows x columns, a block each; Q8_FEW: no tiles, the weights are read straight into
 // registers by blocks of 16 columns and all rows.
-enum Q8Kernel { Q8_FEW, Q8_TILE_64x64, Q8_TILE_64x128, Q8_TILE_128x256, Q8_TILE_256x256, Q8_KERNELS };
+enum Q8Kernel { Q8_FEW, Q8_TILE_64x64, Q8_TILE_64x128, Q8_TILE_128x128, Q8_TILE_128x256, Q8_TILE_256x256, Q8_KERNELS };
 struct Q8TileCost {
     uint32_t rows, cols;
     // us: a launch and a tile's ends; then a stage of 128 bytes: a tile alone on the chip, one on each compute unit, and, where
     // two share a unit, a tile's part of it (0: they do not, and rounds are whole numbers)
     double start, alone, one, shared;
 };
-// Measured on 256 compute units, us a call by kernel (the four tiles):
-//    m x n x k            64x64   64x128  128x256  256x256         m x n x k           64x64   64x128  128x256  256x256
-//    128 x 4096 x 4096     10.2     13.1     29.3     40.3         2048 x 2048 x 2048   18.9     17.8     18.5     26.1
-//    512 x 4096 x 4096     17.7     15.7     29.3     41.3         4096 x 2048 x 2048   33.2     27.7     22.6     29.4
-//    1024 x 4096 x 4096    32.1     26.6     30.8     42.7         4096 x 4096 x 4096    115       90       79       62
-//    2048 x 4096 x 4096    60.9     47.5     38.0     48.6         4096 x 1024 x 8192   57.9     44.5     55.1     77.3
-//    777 x 1873 x 977       7.1      6.9     11.5     17.4         16384 x 100 x 2048   12.7     11.1     18.1     26.8
+// Measured on 256 compute units, us a call by tile:
+//    m x n x k            64x64   64x128  128x128  128x256  256x256
+//    128 x 4096 x 4096     10.5     13.1     16.8     29.3     40.3
+//    512 x 4096 x 4096     17.5     15.5     17.6     29.4     41.3
+//    1024 x 4096 x 4096    32.3     25.9     22.8     31.2     42.7
+//    2048 x 4096 x 4096    60.9     47.5       44     38.0     48.6
+//    4096 x 4096 x 4096     115       90       80       79       62
+//    777 x 1873 x 977       7.3      7.0      8.0     11.4     17.4
+//    2048 x 2048 x 2048    18.4     15.4     14.5     18.7     26.1
+//    4096 x 1024 x 8192    61.0     46.5     41.2     55.0     77.3
+//    16384 x 100 x 2048    12.7     11.1     11.7     18.1     26.8
 // The costs below say these within 15 %; the kernel of the least cost is taken.
-constexpr Q8TileCost Q8_TILES[] = {{64, 64, 3.2, 0.215, 0.235, 0.235},
-                                   {64, 128, 3.5, 0.30, 0.38, 0.37},
-                                   {128, 256, 5.0, 0.76, 1.03, 0.0},
-                                   {256, 256, 7.0, 1.04, 1.72, 0.0}};
+constexpr int Q8_TILES_N = 5;
+constexpr Q8TileCost Q8_TILES[Q8_TILES_N] = {{64, 64, 3.2, 0.215, 0.235, 0.235},
+                                             {64, 128, 3.5, 0.30, 0.38, 0.37},
+                                             {128, 128, 4.0, 0.40, 0.59, 0.0},
+                                             {128, 256, 5.0, 0.76, 1.03, 0.0},
+                                             {256, 256, 7.0, 1.04, 1.72, 0.0}};
 constexpr double Q8_UNITS = 256.0;      // compute units
 
 // us of a product of m x n sums over k bytes, each made by `parts` blocks.
@@ -84,7 +98,7 @@ constexpr uint64_t Q8_FEW_ROWS = 16, Q8_FEW_ROWS_MOST = 48, Q8_FEW_WEIGHTS = 1ul
 inline Q8Kernel q8_kernel_for(uint64_t m, uint64_t n, uint64_t k) {
     if (m <= Q8_FEW_ROWS || (m <= Q8_FEW_ROWS_MOST && n * k <= Q8_FEW_WEIGHTS)) return Q8_FEW;
     int best = 0;
-    for (int i = 1; i < 4; ++i)
+    for (int i = 1; i < Q8_TILES_N; ++i)
         if (q8_tile_us(Q8_TILES[i], m, n, k) < q8_tile_us(Q8_TILES[best], m, n, k)) best = i;
     return (Q8Kernel)(Q8_TILE_64x64 + best);
 }

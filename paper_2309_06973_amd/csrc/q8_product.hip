@@ -380,6 +380,7 @@ static void launch_product_of(shifter_ctx* ctx, const Q8ProductArgs& g) {
             break;
         case Q8_TILE_64x64: launch_product_as<T, 2, 2, 1, 1, 4, 128, 16>(ctx, g); break;
         case Q8_TILE_64x128: launch_product_as<T, 2, 2, 1, 2, 3, 128, 8>(ctx, g); break;
+        case Q8_TILE_128x128: launch_product_as<T, 2, 4, 2, 1, 3, 128, 8>(ctx, g); break;
         case Q8_TILE_128x256: launch_product_as<T, 2, 4, 2, 2, 2, 128, 8>(ctx, g); break;
         default: launch_product_as<T, 2, 4, 4, 2, 2, 128, 4>(ctx, g); break;
     }

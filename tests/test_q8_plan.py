@@ -56,6 +56,12 @@ int main() {
     WANT(q8_bad_codes(p, p, 1, 17, 16), "smaller than a row");
     WANT(q8_bad_codes(p, p, 3, 17, (1u << 22) + 16), "2^22");
     WANT(q8_bad_codes(p, p, 1ull << 31, 17, 32), "rows or columns");
+    WANT(q8_too_many(1u << 20, 1u << 14), nullptr);
+    WANT(q8_too_many(1u << 20, 1u << 15), "more tiles");
+    WANT(q8_too_many(0x7fffffff, 16), "more tiles");
+    WANT(q8_too_many(1u << 27, 16), nullptr);
+    WANT(q8_too_many(1, 1u << 26), "more tiles");
+    WANT(q8_too_many(16, (1u << 26) - 16), nullptr);
     // workspace: the parts follow one another, every slice has rows, the rows are all in slices
     const uint64_t ms[] = {0, 1, 64, 127, 128, 129, 8191, 8192, 8193, 16384, 20000, 131071};
     const uint64_t ns[] = {1, 63, 500, 2048, 4097};
