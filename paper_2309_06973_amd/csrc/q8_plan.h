@@ -106,9 +106,9 @@ inline Q8Kernel q8_kernel_for(uint64_t m, uint64_t n, uint64_t k) {
 // The gradient's workspace: the largest |g s| of every column by slices of rows and of all rows, then the columns'
 // three planes of digits, then the codes, both with the rows of a call side by side.
 constexpr uint32_t Q8_SLICES = 128, Q8_SLICE_ROWS = 32;      // most slices; a slice's rows are a multiple of the other
-// Up to so many rows a block that makes digits finds its columns' largest itself, one launch less; beyond, the rows
-// are read in slices for that first.
-constexpr uint32_t Q8_SELF_ROWS = 512;
+// Up to so many rows a block holds its columns whole in registers and makes their digits from there, in one launch that
+// reads g once; beyond, the rows are read in slices for the columns' largest first.
+constexpr uint32_t Q8_WHOLE_ROWS = 4096;
 // The gradient's kernels, tiles of (columns of g) x (columns of the checkpoint), the costs as above.  Measured, us of the tiles' kernel:
 //    m x n x k             64x64   64x128   64x256  128x256         m x n x k             64x64   64x128   64x256  128x256
 //    16384 x 4096 x 4096     886      695      683      593         512 x 4096 x 1024      14.0     12.5     11.9     18.0
@@ -137,7 +137,7 @@ struct Q8GradientPlan {
     Q8GradientKernel kernel;
     uint32_t parts, part_rows;                // blocks a tile, and the rows (a multiple of 128) that each has
     uint64_t ld;                              // bytes of a transposed row: the call's rows, rounded up to 128
-    uint32_t slices, slice_rows;              // 0 slices: up to Q8_SELF_ROWS rows
+    uint32_t slices, slice_rows;              // 0 slices: up to Q8_WHOLE_ROWS rows
     uint64_t tops, slice_tops, digits, codes, sums, bytes;      // offsets, and the whole
 };
 inline Q8GradientPlan q8_gradient_plan(uint64_t m, uint64_t n, uint64_t k) {
@@ -145,7 +145,7 @@ inline Q8GradientPlan q8_gradient_plan(uint64_t m, uint64_t n, uint64_t k) {
     p.ld = (m + 127u) & ~(uint64_t)127u;
     const uint64_t per = (m + Q8_SLICES * Q8_SLICE_ROWS - 1u) / (Q8_SLICES * Q8_SLICE_ROWS);
     p.slice_rows = (uint32_t)(Q8_SLICE_ROWS * (per ? per : 1u));
-    p.slices = m <= Q8_SELF_ROWS ? 0u : (uint32_t)((m + p.slice_rows - 1u) / p.slice_rows);
+    p.slices = m <= Q8_WHOLE_ROWS ? 0u : (uint32_t)((m + p.slice_rows - 1u) / p.slice_rows);
     p.tops = 0;
     p.slice_tops = 4u * n;
     p.digits = (p.slice_tops + 4u * n * p.slices + 255u) & ~(uint64_t)255u;

@@ -414,24 +414,30 @@ __device__ __forceinline__ void turn_bytes(uint32_t& a, uint32_t& b, uint32_t& c
 
 constexpr uint32_t TURN_ROWS = 128, TURN_PITCH = TURN_ROWS / 4 + 1;      // words of a turned row in LDS
 
-// `rows` turned rows of 128 bytes from LDS to memory, 16 bytes a thread.
-__device__ __forceinline__ void store_turned(const uint32_t* s, uint32_t rows, int8_t* to, uint64_t ld) {
-    for (uint32_t i = threadIdx.x; i < rows * 8u; i += BLOCK) {
+// `rows` turned rows of 128 bytes from LDS to memory, 16 bytes a thread of 256.
+__device__ __forceinline__ void store_turned(uint32_t tid, const uint32_t* s, uint32_t rows, int8_t* to, uint64_t ld) {
+    for (uint32_t i = tid; i < rows * 8u; i += BLOCK) {
         const uint32_t* w = s + (i / 8u) * TURN_PITCH + (i & 7u) * 4u;
         *reinterpret_cast<uint4*>(to + (uint64_t)(i / 8u) * ld + (i & 7u) * 16u) = make_uint4(w[0], w[1], w[2], w[3]);
     }
 }
 
-// 128 columns and 128 rows of the checkpoint, turned: a thread has 16 columns of four rows.
+// 128 columns and 128 rows of the checkpoint, turned, by each 256 threads of a block: a thread has 16 columns of
+// four rows.  lds: 128 rows of TURN_PITCH words for each.
+template <uint32_t THREADS>
 __device__ __forceinline__ void turn_codes(const Q8GradientArgs& a, const Q8GradientPlan& pl, uint32_t block, uint32_t* lds) {
-    const uint32_t across = (a.k + 127u) / 128u, k0 = block % across * 128u, m0 = block / across * TURN_ROWS;
-    const uint32_t kg = threadIdx.x & 7u, rg = threadIdx.x >> 3, k = k0 + kg * 16u;
+    const uint32_t across = (a.k + 127u) / 128u, tid = threadIdx.x % BLOCK, group = threadIdx.x / BLOCK;
+    const uint32_t tile = block * (THREADS / BLOCK) + group;
+    const bool there = tile < across * (uint32_t)(pl.ld / TURN_ROWS);
+    const uint32_t k0 = tile % across * 128u, m0 = tile / across * TURN_ROWS;
+    const uint32_t kg = tid & 7u, rg = tid >> 3, k = k0 + kg * 16u;
+    lds += group * (128u * TURN_PITCH);
     uint32_t w[4][4];                                                    // [row][word of its columns]
 #pragma unroll
     for (uint32_t r = 0; r < 4; ++r) {
         const uint32_t m = m0 + rg * 4u + r;
         uint4 v = make_uint4(0u, 0u, 0u, 0u);
-        if (m < a.m && k < a.k) v = *reinterpret_cast<const uint4*>(a.q + (uint64_t)m * a.ld_q + k);
+        if (there && m < a.m && k < a.k) v = *reinterpret_cast<const uint4*>(a.q + (uint64_t)m * a.ld_q + k);
         w[r][0] = v.x; w[r][1] = v.y; w[r][2] = v.z; w[r][3] = v.w;
     }
 #pragma unroll
@@ -441,10 +447,104 @@ __device__ __forceinline__ void turn_codes(const Q8GradientArgs& a, const Q8Grad
         for (uint32_t i = 0; i < 4; ++i) lds[(kg * 16u + x * 4u + i) * TURN_PITCH + rg] = w[i][x];
     }
     __syncthreads();
-    store_turned(lds, min(128u, a.k - k0), reinterpret_cast<int8_t*>(a.work + pl.codes) + (uint64_t)k0 * pl.ld + m0, pl.ld);
+    if (there)
+        store_turned(tid, lds, min(128u, a.k - k0), reinterpret_cast<int8_t*>(a.work + pl.codes) + (uint64_t)k0 * pl.ld + m0, pl.ld);
 }
-static uint32_t turn_blocks(const Q8GradientArgs& a, const Q8GradientPlan& pl) {
-    return (a.k + 127u) / 128u * (uint32_t)(pl.ld / TURN_ROWS);
+static uint32_t turn_blocks(const Q8GradientArgs& a, const Q8GradientPlan& pl, uint32_t threads) {
+    const uint32_t tiles = (a.k + 127u) / 128u * (uint32_t)(pl.ld / TURN_ROWS), each = threads / BLOCK;
+    return (tiles + each - 1u) / each;
+}
+
+// What a column's digits are made with, from its largest |p|.  No factor: zeros, or a column that is not finite.
+struct ColumnScale {
+    float up, factor;
+    __device__ __forceinline__ explicit ColumnScale(uint32_t top) {
+        const float c = __uint_as_float(top);
+        up = digits_up(c);
+        // a little less than the quotient, so that the largest p stays at DIGITS_TOP with both roundings
+        factor = top == 0u || top >= 0x7f800000u ? 0.0f : DIGITS_TOP / (c * up) * (1.0f - 0x1p-22f);
+    }
+    // 0x808080 + the whole number of p: with 128 added to each, the balanced digits are the number's bytes
+    __device__ __forceinline__ uint32_t operator()(float p) const {
+        // a column that is not finite has factor 0; its NaN become some number, in their own column alone
+        return (uint32_t)((int32_t)rintf(__fmul_rn(__fmul_rn(p, up), factor)) + 0x808080);
+    }
+    // what a whole number of 1 stands for, without `up`; NaN for a column that is not finite
+    __device__ __forceinline__ static float unit(uint32_t top) {
+        return top >= 0x7f800000u ? __uint_as_float(0x7fc00000u)
+                                  : __uint_as_float(top) * digits_up(__uint_as_float(top)) / DIGITS_TOP * (1.0f + 0x1p-22f);
+    }
+};
+
+// Four of its numbers as the digits' three words, the first number's in the lowest bytes.
+__device__ __forceinline__ void digit_words(uint32_t a, uint32_t b, uint32_t c, uint32_t d, uint32_t& d0, uint32_t& d1, uint32_t& d2) {
+    const uint32_t ab = __builtin_amdgcn_perm(b, a, 0x05010400u), cd = __builtin_amdgcn_perm(d, c, 0x05010400u);
+    d0 = __builtin_amdgcn_perm(cd, ab, 0x05040100u) ^ 0x80808080u;
+    d1 = __builtin_amdgcn_perm(cd, ab, 0x07060302u) ^ 0x80808080u;
+    const uint32_t hi = __builtin_amdgcn_perm(b, a, 0x0c0c0602u), lo = __builtin_amdgcn_perm(d, c, 0x06020c0cu);
+    d2 = (hi | lo) ^ 0x80808080u;
+}
+
+// Digits of 16 columns and all rows by a block that holds them in registers, eight columns of eight rows a thread: g is
+// read once, and what a thread has of a column leaves as eight bytes.  Neighbouring blocks, which share lines of g, are
+// on one chiplet.  Behind the blocks for digits come those that turn the checkpoint.
+template <typename T, uint32_t THREADS>
+__global__ __launch_bounds__(THREADS) void q8_columns_kernel(Q8GradientArgs a, Q8GradientPlan pl, uint32_t blocks) {
+    constexpr uint32_t DEEP = 8;
+    __shared__ uint32_t lds[THREADS / BLOCK * 128 * TURN_PITCH];
+    if (blockIdx.x >= blocks) return turn_codes<THREADS>(a, pl, blockIdx.x - blocks, lds);
+    const uint32_t xcd = blockIdx.x % 8u, block = xcd * (blocks / 8u) + min(xcd, blocks % 8u) + blockIdx.x / 8u;
+    const uint32_t cg = threadIdx.x & 1u, m0 = (threadIdx.x >> 1) * DEEP, n = block * 16u + cg * 8u;
+    Eight<T> e[DEEP];
+    float s[DEEP];
+#pragma unroll
+    for (uint32_t r = 0; r < DEEP; ++r) {
+        const uint32_t m = min(m0 + r, a.m - 1u);                        // behind the last one: it again
+        fetch8(static_cast<const T*>(a.g) + (uint64_t)m * a.ld_g, n, a.n, e[r]);
+        s[r] = a.s[m];
+    }
+    if (threadIdx.x < 16u) lds[threadIdx.x] = 0;
+    __syncthreads();
+    uint32_t top[8] = {};
+#pragma unroll
+    for (uint32_t r = 0; r < DEEP; ++r) {
+        float f[8];
+        place8(n, a.n, e[r]);
+        e[r].floats(f);
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) top[i] = max(top[i], key_of(__fmul_rn(f[i], s[r])));
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) {                                   // lanes of the same columns: every other one
+        top[i] = max(top[i], (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top[i], 0x4E, 0xf, 0xf, true));
+        top[i] = max(top[i], (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top[i], 0x124, 0xf, 0xf, true));
+        top[i] = max(top[i], (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top[i], 0x128, 0xf, 0xf, true));
+        if ((threadIdx.x & 15u) < 2u) atomicMax(&lds[cg * 8u + i], top[i]);
+    }
+    __syncthreads();
+    if (threadIdx.x < 16u && block * 16u + threadIdx.x < a.n)
+        reinterpret_cast<uint32_t*>(a.work + pl.tops)[block * 16u + threadIdx.x] = lds[threadIdx.x];
+    if (m0 >= (uint32_t)pl.ld) return;
+    int8_t* out = reinterpret_cast<int8_t*>(a.work + pl.digits) + m0;
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) {
+        if (n + i >= a.n) break;
+        const ColumnScale scale(lds[cg * 8u + i]);
+        uint32_t u[DEEP];
+#pragma unroll
+        for (uint32_t r = 0; r < DEEP; ++r) {
+            float f[8];
+            e[r].floats(f);
+            u[r] = scale(m0 + r < a.m ? __fmul_rn(f[i], s[r]) : 0.0f);       // rows behind the last one count as zero
+        }
+        uint32_t d[3][2];
+#pragma unroll
+        for (uint32_t x = 0; x < 2; ++x)
+            digit_words(u[4 * x], u[4 * x + 1], u[4 * x + 2], u[4 * x + 3], d[0][x], d[1][x], d[2][x]);
+#pragma unroll
+        for (uint32_t p = 0; p < 3; ++p)
+            *reinterpret_cast<uint2*>(out + ((uint64_t)p * a.n + n + i) * pl.ld) = make_uint2(d[p][0], d[p][1]);
+    }
 }
 
 // Largest |p| of eight columns over the rows from r0 on, every `step`-th.  As magnitudes' bits: infinity and NaN are on top.
@@ -479,7 +579,7 @@ __device__ __forceinline__ void column_tops(const Q8GradientArgs& a, uint32_t n,
 template <typename T>
 __global__ __launch_bounds__(BLOCK) void q8_tops_kernel(Q8GradientArgs a, Q8GradientPlan pl, uint32_t blocks) {
     __shared__ uint32_t lds[128 * TURN_PITCH];
-    if (blockIdx.x >= blocks) return turn_codes(a, pl, blockIdx.x - blocks, lds);
+    if (blockIdx.x >= blocks) return turn_codes<BLOCK>(a, pl, blockIdx.x - blocks, lds);
     const uint32_t across = blocks / pl.slices, slice = blockIdx.x / across, lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
     const uint32_t n = blockIdx.x % across * 512u + lane * 8u, r0 = slice * pl.slice_rows;
     uint32_t top[8];
@@ -497,13 +597,11 @@ __global__ __launch_bounds__(BLOCK) void q8_tops_kernel(Q8GradientArgs a, Q8Grad
 }
 
 // The digits of 64 columns and `deep` times 128 rows, the rows of a column side by side: a thread has eight columns
-// of four rows at a time, and the next ones on their way while it works.  SELF: the columns' largest are found
-// here, and behind the blocks for digits come those that turn the checkpoint.
-template <typename T, bool SELF>
-__global__ __launch_bounds__(BLOCK) void q8_digits_kernel(Q8GradientArgs a, Q8GradientPlan pl, uint32_t blocks, uint32_t deep) {
+// of four rows at a time, and the next ones on their way while it works.
+template <typename T>
+__global__ __launch_bounds__(BLOCK) void q8_digits_kernel(Q8GradientArgs a, Q8GradientPlan pl, uint32_t deep) {
     __shared__ uint32_t lds[3 * 64 * TURN_PITCH];
     __shared__ uint32_t s_top[64];
-    if (SELF && blockIdx.x >= blocks) return turn_codes(a, pl, blockIdx.x - blocks, lds);
     const uint32_t across = (a.n + 63u) / 64u, n0 = blockIdx.x % across * 64u;
     const uint32_t first = blockIdx.x / across * deep * TURN_ROWS, last = min(first + deep * TURN_ROWS, (uint32_t)pl.ld);
     const uint32_t cg = threadIdx.x & 7u, rg = threadIdx.x >> 3, n = n0 + cg * 8u;
@@ -520,50 +618,23 @@ __global__ __launch_bounds__(BLOCK) void q8_digits_kernel(Q8GradientArgs a, Q8Gr
     fetch(first);
     if (threadIdx.x < 64u) s_top[threadIdx.x] = 0;
     __syncthreads();
-    if constexpr (SELF) {
-        uint32_t top[8] = {};
-        if (a.m > TURN_ROWS) {
-            column_tops<T>(a, n, rg, a.m, BLOCK / 8u, top);
-        } else {                               // all the rows there are have been fetched
-#pragma unroll
-            for (uint32_t r = 0; r < 4; ++r) {
-                Eight<T> x = e[r];
-                float f[8];
-                place8(n, a.n, x);
-                x.floats(f);
-#pragma unroll
-                for (uint32_t i = 0; i < 8; ++i) top[i] = max(top[i], key_of(__fmul_rn(f[i], s[r])));
-            }
-        }
-#pragma unroll
-        for (uint32_t i = 0; i < 8; ++i) {
-            for (uint32_t d = 8; d < 64; d <<= 1) top[i] = max(top[i], (uint32_t)__shfl_xor((int)top[i], (int)d, 64));
-            if ((threadIdx.x & 63u) < 8u) atomicMax(&s_top[cg * 8u + i], top[i]);
-        }
-    } else {
-        const uint32_t* tops = reinterpret_cast<const uint32_t*>(a.work + pl.slice_tops);
-        const uint32_t col = threadIdx.x & 63u;
+    const uint32_t* tops = reinterpret_cast<const uint32_t*>(a.work + pl.slice_tops);
+    const uint32_t col = threadIdx.x & 63u;
+    if (n0 + col < a.n) {
         uint32_t top = 0;
-        if (n0 + col < a.n) {
 #pragma unroll 8
-            for (uint32_t x = threadIdx.x / 64u; x < pl.slices; x += BLOCK / 64u) top = max(top, tops[(uint64_t)x * a.n + n0 + col]);
-            atomicMax(&s_top[col], top);
-        }
+        for (uint32_t x = threadIdx.x / 64u; x < pl.slices; x += BLOCK / 64u) top = max(top, tops[(uint64_t)x * a.n + n0 + col]);
+        atomicMax(&s_top[col], top);
     }
     __syncthreads();
     if (first == 0 && threadIdx.x < 64u && n0 + threadIdx.x < a.n)
         reinterpret_cast<uint32_t*>(a.work + pl.tops)[n0 + threadIdx.x] = s_top[threadIdx.x];
-    float up[8], factor[8];
-#pragma unroll
-    for (uint32_t i = 0; i < 8; ++i) {
-        const uint32_t top = s_top[cg * 8u + i];
-        const float c = __uint_as_float(top);
-        up[i] = digits_up(c);
-        factor[i] = top == 0u || top >= 0x7f800000u ? 0.0f : DIGITS_TOP / (c * up[i]);
-    }
     int8_t* out = reinterpret_cast<int8_t*>(a.work + pl.digits);
+    const ColumnScale scale[8] = {ColumnScale(s_top[cg * 8u]), ColumnScale(s_top[cg * 8u + 1u]), ColumnScale(s_top[cg * 8u + 2u]),
+                                  ColumnScale(s_top[cg * 8u + 3u]), ColumnScale(s_top[cg * 8u + 4u]), ColumnScale(s_top[cg * 8u + 5u]),
+                                  ColumnScale(s_top[cg * 8u + 6u]), ColumnScale(s_top[cg * 8u + 7u])};
     for (uint32_t m0 = first; m0 < last; m0 += TURN_ROWS) {
-        uint32_t d[3][8] = {};
+        uint32_t u[4][8];
 #pragma unroll
         for (uint32_t r = 0; r < 4; ++r) {
             const bool there = m0 + rg * 4u + r < a.m;                       // rows behind the last one count as zero
@@ -571,25 +642,20 @@ __global__ __launch_bounds__(BLOCK) void q8_digits_kernel(Q8GradientArgs a, Q8Gr
             place8(n, a.n, e[r]);
             e[r].floats(f);
 #pragma unroll
-            for (uint32_t i = 0; i < 8; ++i) {
-                // a column that is not finite has factor 0, and NaN in its own place alone
-                const float t = rintf(__fmul_rn(__fmul_rn(__fmul_rn(f[i], s[r]), up[i]), factor[i]));
-                const int32_t v = there ? (int32_t)fminf(fmaxf(t, -DIGITS_TOP), DIGITS_TOP) : 0;
-                const int32_t v1 = (v + 128) >> 8, v2 = (v1 + 128) >> 8;     // what the digits from d1, from d2 on stand for
-                d[0][i] |= ((uint32_t)v & 255u) << (8u * r);
-                d[1][i] |= ((uint32_t)v1 & 255u) << (8u * r);
-                d[2][i] |= ((uint32_t)v2 & 255u) << (8u * r);
-            }
+            for (uint32_t i = 0; i < 8; ++i) u[r][i] = scale[i](there ? __fmul_rn(f[i], s[r]) : 0.0f);
         }
         if (m0 + TURN_ROWS < last) fetch(m0 + TURN_ROWS);
 #pragma unroll
-        for (uint32_t p = 0; p < 3; ++p)
+        for (uint32_t i = 0; i < 8; ++i) {
+            uint32_t d[3];
+            digit_words(u[0][i], u[1][i], u[2][i], u[3][i], d[0], d[1], d[2]);
 #pragma unroll
-            for (uint32_t i = 0; i < 8; ++i) lds[(p * 64u + cg * 8u + i) * TURN_PITCH + rg] = d[p][i];
+            for (uint32_t p = 0; p < 3; ++p) lds[(p * 64u + cg * 8u + i) * TURN_PITCH + rg] = d[p];
+        }
         __syncthreads();
 #pragma unroll
         for (uint32_t p = 0; p < 3; ++p)
-            store_turned(lds + p * 64u * TURN_PITCH, min(64u, a.n - n0), out + ((uint64_t)p * a.n + n0) * pl.ld + m0, pl.ld);
+            store_turned(threadIdx.x, lds + p * 64u * TURN_PITCH, min(64u, a.n - n0), out + ((uint64_t)p * a.n + n0) * pl.ld + m0, pl.ld);
         __syncthreads();
     }
 }
@@ -656,7 +722,7 @@ __global__ __launch_bounds__(64 * WA * WB) void q8_gradient_kernel(Q8GradientArg
     float* s_unit = reinterpret_cast<float*>(lds + OUT);
     float* s_down = s_unit + Tl::RA;
     if (threadIdx.x < Tl::RA) {
-        s_unit[threadIdx.x] = key_of(top) >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : top * digits_up(top) / DIGITS_TOP;
+        s_unit[threadIdx.x] = ColumnScale::unit(key_of(top));
         s_down[threadIdx.x] = digits_down(top);
     }
     __syncthreads();
@@ -766,19 +832,22 @@ static void launch_gradient_small(shifter_ctx* ctx, const Q8GradientArgs& g) {
     q8_gradient_small_kernel<T><<<(uint32_t)blocks, BLOCK, 0, ctx->stream>>>(g);
 }
 
+template <typename T, uint32_t THREADS>
+static void launch_columns(shifter_ctx* ctx, const Q8GradientArgs& g, const Q8GradientPlan& pl) {
+    const uint32_t blocks = (g.n + 15u) / 16u;
+    q8_columns_kernel<T, THREADS><<<blocks + turn_blocks(g, pl, THREADS), THREADS, 0, ctx->stream>>>(g, pl, blocks);
+}
+
 template <typename T>
 static void launch_digits(shifter_ctx* ctx, const Q8GradientArgs& g, const Q8GradientPlan& pl) {
-    const uint32_t turns = turn_blocks(g, pl), across = (g.n + 63u) / 64u, tiles = (uint32_t)(pl.ld / TURN_ROWS);
-    if (pl.slices == 0) {
-        q8_digits_kernel<T, true><<<across * tiles + turns, BLOCK, 0, ctx->stream>>>(g, pl, across * tiles, 1u);
-    } else {
-        const uint32_t tops = (g.n + 511u) / 512u * pl.slices;
-        q8_tops_kernel<T><<<tops + turns, BLOCK, 0, ctx->stream>>>(g, pl, tops);
-        // every block reads its columns' slices: as many rows a block as leave 2048 blocks
-        const uint32_t deep = std::min(8u, std::max(1u, (uint32_t)((uint64_t)across * tiles / 2048u)));
-        const uint32_t blocks = across * ((tiles + deep - 1u) / deep);
-        q8_digits_kernel<T, false><<<blocks, BLOCK, 0, ctx->stream>>>(g, pl, blocks, deep);
-    }
+    if (pl.ld <= 1024) return launch_columns<T, 256>(ctx, g, pl);
+    if (pl.ld <= 2048) return launch_columns<T, 512>(ctx, g, pl);
+    if (pl.ld <= Q8_WHOLE_ROWS) return launch_columns<T, 1024>(ctx, g, pl);
+    const uint32_t across = (g.n + 63u) / 64u, tiles = (uint32_t)(pl.ld / TURN_ROWS), tops = (g.n + 511u) / 512u * pl.slices;
+    q8_tops_kernel<T><<<tops + turn_blocks(g, pl, BLOCK), BLOCK, 0, ctx->stream>>>(g, pl, tops);
+    // every block reads its columns' slices: as many rows a block as leave 2048 blocks
+    const uint32_t deep = std::min(8u, std::max(1u, (uint32_t)((uint64_t)across * tiles / 2048u)));
+    q8_digits_kernel<T><<<across * ((tiles + deep - 1u) / deep), BLOCK, 0, ctx->stream>>>(g, pl, deep);
 }
 
 // The parts' sums joined, in 64 bits so that only the parts' own roundings count; under the mask, or added to dw.

@@ -55,6 +55,8 @@ class Q8:
         self.ctx = ctx or S.shifter_create(device, self.stream)
         self.work = None
         self.recorded = []                 # workspaces that a recorded call holds
+        self._int8 = torch.empty(0, dtype=torch.int8, device=self.dev)        # new_empty is the shortest way to a new tensor
+        self._float = torch.empty(0, dtype=torch.float32, device=self.dev)
 
     def close(self):
         if self.own and self.ctx is not None:
@@ -98,8 +100,8 @@ class Q8:
         if out is None:
             m = Q8Matrix.__new__(Q8Matrix)             # as __init__ would leave it
             m.rows, m.cols, m.ld = rows, cols, _pad(cols)
-            m.q = torch.empty((rows, m.ld), dtype=torch.int8, device=self.dev)
-            m.scale = torch.empty(rows, dtype=torch.float32, device=self.dev)
+            m.q = self._int8.new_empty(rows, m.ld)
+            m.scale = self._float.new_empty(rows)
             return m
         self._here(out.q, "out")
         if out.rows != rows or out.cols != cols:
@@ -147,7 +149,7 @@ class Q8:
             self._same(residual, x.shape, x.dtype, "residual")
             _, _, _, ld_r = self._matrix(residual, "residual")
             if h is None:
-                h, ld_h = torch.empty((rows, cols), dtype=x.dtype, device=self.dev), cols
+                h, ld_h = x.new_empty(rows, cols), cols
             else:
                 self._same(h, x.shape, x.dtype, "h")
                 _, _, _, ld_h = self._matrix(h, "h")

@@ -63,7 +63,7 @@ int main() {
     WANT(q8_too_many(1, 1u << 26), "more tiles");
     WANT(q8_too_many(16, (1u << 26) - 16), nullptr);
     // workspace: the parts follow one another, every slice has rows, the rows are all in slices
-    const uint64_t ms[] = {0, 1, 64, 127, 128, 129, 8191, 8192, 8193, 16384, 20000, 131071};
+    const uint64_t ms[] = {0, 1, 64, 127, 128, 129, 4095, 4096, 4097, 8191, 8192, 8193, 16384, 20000, 131071};
     const uint64_t ns[] = {1, 63, 500, 2048, 4097};
     int used[Q8_GRAD_KERNELS] = {0}, split = 0;
     for (uint64_t m : ms)
@@ -74,7 +74,7 @@ int main() {
                 if ((g.kernel == Q8_GRAD_SMALL) != is_small || (is_small && g.bytes != 0)) { printf("small %llu %llu %llu\n", (unsigned long long)m, (unsigned long long)n, (unsigned long long)k); ++bad; }
                 if (is_small) continue;
                 bool ok = m > 0 && g.ld >= m && g.ld < m + 128 && g.ld % 128 == 0 && g.slices <= Q8_SLICES && g.slice_rows % Q8_SLICE_ROWS == 0;
-                ok = ok && (m <= Q8_SELF_ROWS ? g.slices == 0 : (uint64_t)g.slices * g.slice_rows >= m && (uint64_t)(g.slices - 1) * g.slice_rows < m);
+                ok = ok && (m <= Q8_WHOLE_ROWS ? g.slices == 0 : (uint64_t)g.slices * g.slice_rows >= m && (uint64_t)(g.slices - 1) * g.slice_rows < m);
                 ok = ok && g.tops == 0 && g.slice_tops >= 4 * n && g.digits >= g.slice_tops + 4 * n * g.slices && g.digits % 256 == 0;
                 ok = ok && g.kernel >= 0 && g.kernel < Q8_GRAD_KERNELS && g.parts >= 1 && g.parts <= Q8_PARTS && g.part_rows % 128 == 0;
                 ok = ok && (uint64_t)g.parts * g.part_rows >= g.ld && (g.ld == 0 || (uint64_t)(g.parts - 1) * g.part_rows < g.ld);
