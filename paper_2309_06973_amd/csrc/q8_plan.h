@@ -107,8 +107,9 @@ inline Q8Kernel q8_kernel_for(uint64_t m, uint64_t n, uint64_t k) {
 // three planes of digits, then the codes, both with the rows of a call side by side.
 constexpr uint32_t Q8_SLICES = 128, Q8_SLICE_ROWS = 32;      // most slices; a slice's rows are a multiple of the other
 // Up to so many rows a block holds its columns whole in registers and makes their digits from there, in one launch that
-// reads g once; beyond, the rows are read in slices for the columns' largest first.
-constexpr uint32_t Q8_WHOLE_ROWS = 4096;
+// reads g once; beyond, the rows are read in slices for the columns' largest first.  us a call, one launch / two: 966 x 232 x 320
+// 15.2 / 19.2, 1000 x 4096 x 4096 70.7 / 75.9; equal at 2048 rows; 4096 x 64 x 1024 30.8 / 26.2, 4096 x 4096 x 1024 74.5 / 82.3.
+constexpr uint32_t Q8_WHOLE_ROWS = 2048;
 // The gradient's kernels, tiles of (columns of g) x (columns of the checkpoint), the costs as above.  Measured, us of the tiles' kernel:
 //    m x n x k             64x64   64x128   64x256  128x256         m x n x k             64x64   64x128   64x256  128x256
 //    16384 x 4096 x 4096     886      695      683      593         512 x 4096 x 1024      14.0     12.5     11.9     18.0

@@ -841,8 +841,7 @@ static void launch_columns(shifter_ctx* ctx, const Q8GradientArgs& g, const Q8Gr
 template <typename T>
 static void launch_digits(shifter_ctx* ctx, const Q8GradientArgs& g, const Q8GradientPlan& pl) {
     if (pl.ld <= 1024) return launch_columns<T, 256>(ctx, g, pl);
-    if (pl.ld <= 2048) return launch_columns<T, 512>(ctx, g, pl);
-    if (pl.ld <= Q8_WHOLE_ROWS) return launch_columns<T, 1024>(ctx, g, pl);
+    if (pl.ld <= Q8_WHOLE_ROWS) return launch_columns<T, 512>(ctx, g, pl);
     const uint32_t across = (g.n + 63u) / 64u, tiles = (uint32_t)(pl.ld / TURN_ROWS), tops = (g.n + 511u) / 512u * pl.slices;
     q8_tops_kernel<T><<<tops + turn_blocks(g, pl, BLOCK), BLOCK, 0, ctx->stream>>>(g, pl, tops);
     // every block reads its columns' slices: as many rows a block as leave 2048 blocks
