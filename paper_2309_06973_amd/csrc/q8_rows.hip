@@ -102,23 +102,25 @@ __device__ __forceinline__ double of_lane(double v, int lane) {
     return v;
 }
 
-// Largest and sum over the TPR threads of a row, in every one of them.
+// Largest and sum over the TPR threads of a row, 16 or a multiple of 64, in every one of them.
 template <uint32_t TPR, bool SUM>
 __device__ __forceinline__ void row_reduce(uint32_t& top, double& sum) {
     top = max(top, paired<0xB1>(top));
     top = max(top, paired<0x4E>(top));
     top = max(top, paired<0x141>(top));
     top = max(top, paired<0x140>(top));
-    uint32_t all = 0;
+    if constexpr (TPR >= 64) {
+        uint32_t all = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) all = max(all, (uint32_t)__builtin_amdgcn_readlane((int)top, 16 * i));
-    top = all;
+        for (int i = 0; i < 4; ++i) all = max(all, (uint32_t)__builtin_amdgcn_readlane((int)top, 16 * i));
+        top = all;
+    }
     if constexpr (SUM) {
         sum += paired<0xB1>(sum);
         sum += paired<0x4E>(sum);
         sum += paired<0x141>(sum);
         sum += paired<0x140>(sum);
-        sum = (of_lane(sum, 0) + of_lane(sum, 16)) + (of_lane(sum, 32) + of_lane(sum, 48));
+        if constexpr (TPR >= 64) sum = (of_lane(sum, 0) + of_lane(sum, 16)) + (of_lane(sum, 32) + of_lane(sum, 48));
     }
     if constexpr (TPR > 64) {
         __shared__ uint32_t s_top[TPR / 64];
@@ -191,7 +193,7 @@ __global__ __launch_bounds__(TPR < BLOCK ? BLOCK : TPR) void q8_rows_kernel(Q8Ro
     const uint32_t t = threadIdx.x % TPR, pad = (g.cols + Q8_ALIGN - 1u) & ~(Q8_ALIGN - 1u);
     const uint64_t turn = (uint64_t)gridDim.x * AT_ONCE;
     uint64_t row = (uint64_t)blockIdx.x * AT_ONCE + threadIdx.x / TPR;
-    if (row >= g.rows) return;            // whole wavefronts; a block of one row's threads stays together
+    if (row >= g.rows) return;            // all the threads of a row together
     Eight<T> x[NV], res[NV];
     auto fetch = [&](uint64_t from) {
         if (g.cols == 0) return;
@@ -283,11 +285,14 @@ constexpr uint32_t Q8_MAX_BLOCKS = 1u << 21;
 // wavefront, or 256, with more each.  us of norms in bf16, more threads / fewer: 1 x 2048 2.8 / 5.0, 777 x 1873 6.2 / 8.0,
 // 2048 x 2048 9.4 / 10.5, 8192 x 2048 23.8 / 27.2, 32768 x 2048 96.9 / 91.5; 256 x 4096 4.8 / 5.2, 512 x 4096 7.9 / 6.6.
 constexpr uint32_t Q8_ROWS_WIDE = 8192, Q8_ROWS_WIDER = 256;
-constexpr uint32_t Q8_ROWS_THREADS = 256u * 2048u;      // of the rows' kernel: all that the chip holds
+// Threads of the rows' kernel: all that the chip holds, and as many again where blocks are short, which evens out their ends
+// (quantise 65536 x 1024 bf16 40.8 -> 37.0 us, 8192 x 4096 22.3 -> 20.7; of 1024 threads 51 -> 52, norm 4096 x 16384 90 -> 94).
+constexpr uint32_t Q8_ROWS_THREADS = 256u * 2048u;
 
 template <typename T, int FORM, uint32_t TPR, uint32_t NV>
 static void launch_rows_as(shifter_ctx* ctx, const Q8RowsArgs& g) {
-    constexpr uint32_t AT_ONCE = TPR < BLOCK ? BLOCK / TPR : 1u, MOST = Q8_ROWS_THREADS / (AT_ONCE * TPR);
+    constexpr uint32_t AT_ONCE = TPR < BLOCK ? BLOCK / TPR : 1u;
+    constexpr uint32_t MOST = Q8_ROWS_THREADS * (TPR == 1024 ? 1u : 2u) / (AT_ONCE * TPR);
     const uint32_t blocks = std::min((g.rows + AT_ONCE - 1u) / AT_ONCE, MOST);
     q8_rows_kernel<T, FORM, TPR, NV><<<blocks, TPR < BLOCK ? BLOCK : TPR, 0, ctx->stream>>>(g);
 }
@@ -297,6 +302,8 @@ static void launch_rows(shifter_ctx* ctx, const Q8RowsArgs& g) {
     const uint32_t units = (uint32_t)(q8_pad(g.cols) / 8u);
     if (g.rows <= Q8_ROWS_WIDE && units > 128 && units <= 256) launch_rows_as<T, FORM, 256, 1>(ctx, g);
     else if (g.rows <= Q8_ROWS_WIDER && units > 256 && units <= 1024) launch_rows_as<T, FORM, 1024, 1>(ctx, g);
+    else if (units <= 16) launch_rows_as<T, FORM, 16, 1>(ctx, g);
+    else if (units <= 32) launch_rows_as<T, FORM, 16, 2>(ctx, g);
     else if (units <= 64) launch_rows_as<T, FORM, 64, 1>(ctx, g);
     else if (units <= 128) launch_rows_as<T, FORM, 64, 2>(ctx, g);
     else if (units <= 256) launch_rows_as<T, FORM, 64, 4>(ctx, g);

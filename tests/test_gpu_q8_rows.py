@@ -58,7 +58,7 @@ def check_values(ops, m, dtype):
     assert (np.abs(got[ok] - want[ok]) <= (Q.HALF_STEP[dtype] + 1.01 * Q.U32) * np.abs(want[ok]) + 1.01 * Q.LEAST[dtype]).all()
 
 
-COLS = [1, 2, 7, 8, 9, 15, 16, 17, 100, 511, 512, 513, 1024, 1025, 2047, 2048, 2049, 4096, 4097, 8192, 8193,
+COLS = [1, 2, 7, 8, 9, 15, 16, 17, 100, 127, 128, 129, 255, 256, 257, 511, 512, 513, 1024, 1025, 2047, 2048, 2049, 4096, 4097, 8192, 8193,
         16384, 16385, 32768, 32769, 50001]
 
 
@@ -76,7 +76,8 @@ def test_quantize(ops, cols, dtype):
 
 
 @pytest.mark.parametrize("rows,cols", [(0, 7), (3, 0), (0, 0), (1000, 40), (777, 130),
-                                       (9000, 700), (9001, 1100), (2500, 4000), (300, 3001), (300, 8000), (600, 9000), (9, 2000)])
+                                       (9000, 700), (9001, 1100), (2500, 4000), (300, 3001), (300, 8000), (600, 9000), (9, 2000),
+                                       (70001, 3), (66000, 200), (17000, 300)])
 def test_quantize_shapes(ops, rows, cols):
     x = make(rows, cols, "bf16", 3)
     m = ops.quantize(x)
@@ -201,7 +202,7 @@ def test_rms_norm(ops, cols, dtype):
                 assert torch.equal(m2.q, m.q) and torch.equal(m2.scale, m.scale)
 
 
-@pytest.mark.parametrize("rows,cols", [(9000, 300), (9000, 700), (9001, 1100), (2500, 4000), (300, 3001), (300, 8000), (600, 9000),
+@pytest.mark.parametrize("rows,cols", [(70001, 3), (66000, 150), (17000, 300), (9000, 700), (9001, 1100), (2500, 4000), (300, 3001), (300, 8000), (600, 9000),
                                        (9, 2000), (530, 20000)])
 def test_rms_norm_many_rows(ops, rows, cols):
     """More rows than a launch's blocks hold at once, and both sides of the rules on rows."""
