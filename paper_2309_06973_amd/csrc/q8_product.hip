@@ -746,59 +746,57 @@ __global__ __launch_bounds__(64 * WA * WB) void q8_gradient_kernel(Q8GradientArg
     }
 }
 
-// Few rows or few products: one launch, no digits.  A block has 16 columns of g and 256 of the checkpoint, a thread
-// four by four of the sums, which are 64-bit.  Products of a p and a code are exact in them.
-template <typename T>
+// Few rows: one launch, no digits.  A block has 4 I columns of g and 256 of the checkpoint, a thread I by four of the
+// sums, which are 64-bit: products of a p and a code are exact in them, and the vector units add them fast enough.
+// All p of the block's columns lie in LDS; the codes come 16 rows at a time, the next ones on their way.
+template <typename T, uint32_t I>
 __global__ __launch_bounds__(BLOCK) void q8_gradient_small_kernel(Q8GradientArgs a) {
-    constexpr uint32_t DEEP = 32;                                        // rows of p in LDS at a time
-    __shared__ __align__(16) double s_p[DEEP][16];
-    const uint32_t across = (a.k + 255u) / 256u, n0 = blockIdx.x / across * 16u, k0 = blockIdx.x % across * 256u;
+    constexpr uint32_t MOST = Q8_SMALL_ROWS_MOST, COLS = 4 * I, DEEP = 16;
+    __shared__ double s_p[MOST][COLS];
+    const uint32_t across = (a.k + 255u) / 256u, n0 = blockIdx.x / across * COLS, k0 = blockIdx.x % across * 256u;
     const uint32_t lane = threadIdx.x & 63u, wave = uniform_u32(threadIdx.x >> 6), k = k0 + lane * 4u;
-    const uint32_t n_of = n0 + (threadIdx.x & 15u), r_of = threadIdx.x >> 4;      // the p that this thread makes
     const bool there = k < a.k;                                          // the codes behind the last column are in the row's padding
-    double acc[4][4] = {};
-    for (uint32_t m0 = 0; m0 < a.m; m0 += DEEP) {
-        const uint32_t rows = min(DEEP, a.m - m0);
-        uint32_t q[DEEP / 4];
-        auto codes = [&](uint32_t from) {
+    uint32_t q[DEEP];
+    auto codes = [&](uint32_t from) {
 #pragma unroll
-            for (uint32_t r = 0; r < DEEP / 4; ++r)
-                q[r] = there ? *reinterpret_cast<const uint32_t*>(a.q + (uint64_t)(m0 + min(from + r, rows - 1u)) * a.ld_q + k) : 0u;
-        };
-        codes(0);
-        if (m0) __syncthreads();
+        for (uint32_t r = 0; r < DEEP; ++r)
+            q[r] = there ? *reinterpret_cast<const uint32_t*>(a.q + (uint64_t)min(from + r, a.m - 1u) * a.ld_q + k) : 0u;
+    };
+    if (a.m) codes(0);
+    const uint32_t rows = (a.m + DEEP - 1u) / DEEP * DEEP;               // those behind the last one count as zero
 #pragma unroll
-        for (uint32_t r = r_of; r < DEEP; r += BLOCK / 16u) {
-            const uint32_t m = m0 + min(r, rows - 1u);
-            const float p = __fmul_rn((float)static_cast<const T*>(a.g)[(uint64_t)m * a.ld_g + min(n_of, a.n - 1u)], a.s[m]);
-            s_p[r][threadIdx.x & 15u] = r < rows ? (double)p : 0.0;
-        }
-        __syncthreads();
+    for (uint32_t i = 0; i < MOST * COLS; i += BLOCK) {
+        const uint32_t r = (i + threadIdx.x) / COLS, c = (i + threadIdx.x) % COLS;
+        if (i / COLS >= rows || r >= MOST) break;
+        const uint32_t m = min(r, a.m - 1u);
+        const float p = __fmul_rn((float)static_cast<const T*>(a.g)[(uint64_t)m * a.ld_g + min(n0 + c, a.n - 1u)], a.s[m]);
+        s_p[r][c] = r < a.m ? (double)p : 0.0;
+    }
+    __syncthreads();
+    double acc[I][4] = {};
+    for (uint32_t from = 0; from < rows; from += DEEP) {
+        uint32_t now[DEEP];
 #pragma unroll
-        for (uint32_t from = 0; from < DEEP; from += DEEP / 4) {
-            if (from >= rows) break;
-            uint32_t now[DEEP / 4];
+        for (uint32_t r = 0; r < DEEP; ++r) now[r] = q[r];
+        if (from + DEEP < rows) codes(from + DEEP);
 #pragma unroll
-            for (uint32_t r = 0; r < DEEP / 4; ++r) now[r] = q[r];
-            if (from + DEEP / 4 < rows) codes(from + DEEP / 4);
+        for (uint32_t r = 0; r < DEEP; ++r) {
+            if (r % 4u == 0 && from + r >= a.m) break;
+            double p[I];
 #pragma unroll
-            for (uint32_t r = 0; r < DEEP / 4; ++r) {
-                double p[4];
+            for (uint32_t i = 0; i < I; ++i) p[i] = s_p[from + r][wave * I + i];
 #pragma unroll
-                for (uint32_t i = 0; i < 4; ++i) p[i] = s_p[from + r][wave * 4u + i];
+            for (uint32_t j = 0; j < 4; ++j) {
+                const double c = (double)(int8_t)(now[r] >> (8u * j));
 #pragma unroll
-                for (uint32_t j = 0; j < 4; ++j) {
-                    const double c = (double)(int8_t)(now[r] >> (8u * j));
-#pragma unroll
-                    for (uint32_t i = 0; i < 4; ++i) acc[i][j] = fma(p[i], c, acc[i][j]);
-                }
+                for (uint32_t i = 0; i < I; ++i) acc[i][j] = fma(p[i], c, acc[i][j]);
             }
         }
     }
     if (!there) return;
 #pragma unroll
-    for (uint32_t i = 0; i < 4; ++i) {
-        const uint32_t n = n0 + wave * 4u + i;
+    for (uint32_t i = 0; i < I; ++i) {
+        const uint32_t n = n0 + wave * I + i;
         if (n >= a.n) break;
         float* to = a.dw + (uint64_t)n * a.ld_dw + k;
         const uint8_t* mask = a.mask + (uint64_t)n * a.ld_mask + k;
@@ -825,11 +823,19 @@ __global__ __launch_bounds__(BLOCK) void q8_gradient_small_kernel(Q8GradientArgs
     }
 }
 
+template <typename T, uint32_t I>
+static void launch_gradient_small_as(shifter_ctx* ctx, const Q8GradientArgs& g) {
+    const uint64_t blocks = (uint64_t)((g.n + 4u * I - 1u) / (4u * I)) * ((g.k + 255u) / 256u);
+    q8_gradient_small_kernel<T, I><<<(uint32_t)blocks, BLOCK, 0, ctx->stream>>>(g);
+}
 template <typename T>
 static void launch_gradient_small(shifter_ctx* ctx, const Q8GradientArgs& g) {
     ProfileScope ps(ctx, K_Q8_GRADIENT);
-    const uint64_t blocks = (uint64_t)((g.n + 15u) / 16u) * ((g.k + 255u) / 256u);
-    q8_gradient_small_kernel<T><<<(uint32_t)blocks, BLOCK, 0, ctx->stream>>>(g);
+    // the fewer blocks there would be, the narrower they are: a compute unit each, as far as the columns go
+    const uint64_t sixteens = (uint64_t)((g.n + 15u) / 16u) * ((g.k + 255u) / 256u);
+    if (sixteens >= 256u) launch_gradient_small_as<T, 4>(ctx, g);
+    else if (sixteens >= 128u) launch_gradient_small_as<T, 2>(ctx, g);
+    else launch_gradient_small_as<T, 1>(ctx, g);
 }
 
 template <typename T, uint32_t THREADS>
