@@ -115,6 +115,7 @@ constexpr uint32_t Q8_WHOLE_ROWS = 2048;
 //    16384 x 4096 x 4096     886      695      683      593         512 x 4096 x 1024      14.0     12.5     11.9     18.0
 //    2048 x 2048 x 2048     33.8     28.5     26.3     36.1         2048 x 1873 x 977      18.1     19.5     21.7     36.5
 //    16384 x 512 x 512      76.2     89.0      113      196         64 x 512 x 512          5.3      6.9      7.2     11.0
+// (the last without the launch of the digits; the first on random digits, on those of a real gradient 690 with 128x256)
 // Q8_GRAD_SMALL: no digits and no workspace, sums in 64-bit floating point (which the vector units add as fast as 32-bit).
 enum Q8GradientKernel { Q8_GRAD_SMALL = -1, Q8_GRAD_64x64, Q8_GRAD_64x128, Q8_GRAD_64x256, Q8_GRAD_128x256, Q8_GRAD_KERNELS };
 constexpr Q8TileCost Q8_GRAD_TILES[] = {{64, 64, 3.5, 0.57, 0.62, 0.43},
@@ -125,7 +126,7 @@ constexpr Q8TileCost Q8_GRAD_TILES[] = {{64, 64, 3.5, 0.57, 0.62, 0.43},
 // which costs that and the traffic.
 constexpr uint64_t Q8_PARTS = 32;
 // Few rows, and few products in all, go to the small kernel's one launch.  us, that / digits and tiles: 1 x 64 x 64 4.1 / 10.7,
-// 1 x 4096 x 4096 17.3 / 34.5, 16 x 4096 x 4096 24.5 / 34.4, 32 x 4096 x 4096 36.3 / 34.4; 64 x 512 x 512 9.3 / 11.7,
+// 1 x 4096 x 4096 17.7 / 34.5, 16 x 4096 x 4096 24.3 / 34.4, 32 x 4096 x 4096 36.3 / 34.4; 64 x 512 x 512 6.6 / 11.7,
 // 64 x 2048 x 2048 20.6 / 17.2, 128 x 1024 x 1024 16.9 / 12.3.
 constexpr uint64_t Q8_SMALL_ROWS = 16, Q8_SMALL_ROWS_MOST = 64, Q8_SMALL_WORK = 1ull << 27;
 constexpr bool q8_small(uint64_t m, uint64_t n, uint64_t k) {

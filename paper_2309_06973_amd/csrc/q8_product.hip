@@ -228,6 +228,11 @@ __device__ __forceinline__ void store_rows(const int8_t* from, uint32_t pitch, T
     }
 }
 
+// c[m][n] = (sum over k of A[m][k] B[n][k]) sa[m] sb[n] + bias[n]: the sum exact, then two roundings in fp32 and the one to
+// c's type.  8192 x 8192 x 8192 to bf16 takes 446 us, 2.46 POP/s, against 2.42 of the library's bare integer product:
+// the matrix units are busy 69 % of the time and the card lowers its clock to 1.6 GHz under them, so that power is the
+// bound.  A band of GROUP tiles keeps memory out of the way: 0.8 GB are read, 1.8 TB/s.  Eight wavefronts of 128 x 64 each
+// for 256 x 256: four of 128 x 128 would read a fifth less LDS but spill (505 us or more).
 template <typename T, uint32_t WA, uint32_t WB, uint32_t FA, uint32_t FB, uint32_t NS, uint32_t STEP, uint32_t GROUP>
 __global__ __launch_bounds__(64 * WA * WB) void q8_product_kernel(Q8ProductArgs g) {
     using Tl = Tile<1, WA, WB, FA, FB, NS, STEP>;
@@ -291,7 +296,8 @@ static void launch_product_as(shifter_ctx* ctx, const Q8ProductArgs& g) {
 // Few tokens: the weights are read once, straight into registers, and that read is the time.  A block has 16
 // columns of the result and all of the up to 16 F tokens; its WAVES wavefronts take pieces of 128 bytes of the
 // rows in turn and join their sums in LDS.  (Weights are the first factor of the 16 x 16 x 64 products: a
-// lane then holds four neighbouring columns of one token.)
+// lane then holds four neighbouring columns of one token.)  1 x 4096 x 4096 takes 5.3 us, of which 3.0 are the weights' 16.8 MB at
+// a large copy's rate; 48 x 3277 x 3541 7.6 us.  Four pieces of each wavefront are under way: 16 KB to 64 KB a block.
 template <typename T, uint32_t F, uint32_t WAVES>
 __global__ __launch_bounds__(64 * WAVES) void q8_product_few_kernel(Q8ProductArgs g) {
     constexpr uint32_t PIECE = 128, DEPTH = 4;                           // bytes; pieces under way
@@ -487,7 +493,9 @@ __device__ __forceinline__ void digit_words(uint32_t a, uint32_t b, uint32_t c, 
 
 // Digits of 16 columns and all rows by a block that holds them in registers, eight columns of eight rows a thread: g is
 // read once, and what a thread has of a column leaves as eight bytes.  Neighbouring blocks, which share lines of g, are
-// on one chiplet.  Behind the blocks for digits come those that turn the checkpoint.
+// on one chiplet.  Behind the blocks for digits come those that turn the checkpoint.  2048 x 1873 (bf16, odd stride) and 977
+// columns of checkpoint take 13 us: 23 MB, but only 118 blocks for the digits, each of which waits for its reads once,
+// for the columns' largest, and then codes; latency bounds it.
 template <typename T, uint32_t THREADS>
 __global__ __launch_bounds__(THREADS) void q8_columns_kernel(Q8GradientArgs a, Q8GradientPlan pl, uint32_t blocks) {
     constexpr uint32_t DEEP = 8;
@@ -575,7 +583,7 @@ __device__ __forceinline__ void column_tops(const Q8GradientArgs& a, uint32_t n,
 }
 
 // The columns' largest over one slice of rows, 512 columns a block and eight a thread; behind those blocks, the
-// ones that turn the checkpoint.
+// ones that turn the checkpoint.  16384 x 4096 bf16 and as much checkpoint take 54 us: 271 MB, 5 TB/s.
 template <typename T>
 __global__ __launch_bounds__(BLOCK) void q8_tops_kernel(Q8GradientArgs a, Q8GradientPlan pl, uint32_t blocks) {
     __shared__ uint32_t lds[128 * TURN_PITCH];
@@ -597,7 +605,8 @@ __global__ __launch_bounds__(BLOCK) void q8_tops_kernel(Q8GradientArgs a, Q8Grad
 }
 
 // The digits of 64 columns and `deep` times 128 rows, the rows of a column side by side: a thread has eight columns
-// of four rows at a time, and the next ones on their way while it works.
+// of four rows at a time, and the next ones on their way while it works.  g is read again here because a column's unit is not
+// known before its last row: 16384 x 4096 bf16 takes 70 us, 341 MB, 4.9 TB/s.
 template <typename T>
 __global__ __launch_bounds__(BLOCK) void q8_digits_kernel(Q8GradientArgs a, Q8GradientPlan pl, uint32_t deep) {
     __shared__ uint32_t lds[3 * 64 * TURN_PITCH];
@@ -695,6 +704,11 @@ __device__ __forceinline__ void store_gradient(const int8_t* from, uint32_t pitc
     }
 }
 
+// dW[n][k] = unit[n] (2^16 D2 + 2^8 D1 + D0), Dp the exact sum of digit plane p of column n times column k of the codes.  One
+// tile of Q serves the three planes, whose sums all stay in registers: 128 x 256 of them fill eight wavefronts' 192
+// accumulators.  16384 x 4096 x 4096 takes 690 us, 2.39 POP/s over the three products, with the matrix units 56 % busy at
+// 2.0 GHz: power, as in the product.  2048 x 1873 x 977 takes 20 us on tiles of 64 x 64: less than two a compute unit,
+// whose stages are bound by the latency of LDS and of the fetches.
 template <uint32_t WA, uint32_t WB, uint32_t FA, uint32_t FB, uint32_t NS, uint32_t STEP, uint32_t GROUP>
 __global__ __launch_bounds__(64 * WA * WB) void q8_gradient_kernel(Q8GradientArgs g, Q8GradientPlan pl) {
 
@@ -748,7 +762,9 @@ __global__ __launch_bounds__(64 * WA * WB) void q8_gradient_kernel(Q8GradientArg
 
 // Few rows: one launch, no digits.  A block has 4 I columns of g and 256 of the checkpoint, a thread I by four of the
 // sums, which are 64-bit: products of a p and a code are exact in them, and the vector units add them fast enough.
-// All p of the block's columns lie in LDS; the codes come 16 rows at a time, the next ones on their way.
+// All p of the block's columns lie in LDS; the codes come 16 rows at a time, the next ones on their way.  64 x 512 x 512
+// takes 6.6 us, a third of it the launch and the rest four trips to memory and 64 rows of additions in a thread; 1 x 4096 x
+// 4096 17.7 us, the 67 MB of dW at 3.8 TB/s.  The same with the rows split over blocks and joined was slower (9 us).
 template <typename T, uint32_t I>
 __global__ __launch_bounds__(BLOCK) void q8_gradient_small_kernel(Q8GradientArgs a) {
     constexpr uint32_t MOST = Q8_SMALL_ROWS_MOST, COLS = 4 * I, DEEP = 16;
@@ -856,6 +872,7 @@ static void launch_digits(shifter_ctx* ctx, const Q8GradientArgs& g, const Q8Gra
 }
 
 // The parts' sums joined, in 64 bits so that only the parts' own roundings count; under the mask, or added to dw.
+// One pass over parts x n x k fp32 that are mostly still in cache: q8_join_us, 3.5 us and 2 us per million of them.
 __global__ __launch_bounds__(BLOCK) void q8_join_kernel(Q8GradientArgs g, Q8GradientPlan pl) {
     const float* sums = reinterpret_cast<const float*>(g.work + pl.sums);
     const uint64_t all = (uint64_t)g.n * g.k;
