@@ -1,9 +1,11 @@
-"""Builds libshifter.so (HIP, gfx950) in-tree with hipcc."""
+"""Builds libshifter.so (HIP, gfx950) with hipcc and _q8.so (the 8-bit operators' calls from Python,
+host code over torch's headers) with g++, both in-tree."""
 from __future__ import annotations
 
 import os
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -11,6 +13,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libshifter.so")
+BINDING = os.path.join(PKG, "_q8.so")
 SOURCES = ["api.hip", "select.hip", "spec_select.hip", "spec_multi.hip", "mask_scan.hip", "batch.hip", "plan_compact.hip",
            "fixpoint.hip", "fold.hip", "codec.hip", "q8_rows.hip", "q8_product.hip"]
 FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-Wall",
@@ -24,6 +27,26 @@ def _hipcc() -> str:
         if c and (os.path.isabs(c) and os.path.exists(c) or not os.path.isabs(c)):
             return c
     return "hipcc"
+
+
+def _binding_commands():
+    """(compile, link): the binding is linked once libshifter.so is there."""
+    import torch
+    from torch.utils import cpp_extension
+    obj = os.path.join(OBJ, "q8_bind.o")
+    headers = [sysconfig.get_paths()["include"], *cpp_extension.include_paths()]
+    compile_ = ["g++", "-O2", "-std=c++17", "-fPIC", "-Wall", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
+                *(a for h in headers for a in ("-isystem", h)), "-I", os.path.join(ROOT, "include"),
+                "-c", os.path.join(CSRC, "q8_bind.cpp"), "-o", obj]
+    link = ["g++", "-shared", obj, "-L", PKG, "-lshifter", *("-L" + p for p in cpp_extension.library_paths()),
+            "-lc10", "-ltorch_cpu", "-ltorch_python", "-Wl,-rpath,$ORIGIN", "-Wl,--allow-shlib-undefined", "-o", BINDING]
+    return compile_, link
+
+
+def _run(cmd, what: str):
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"{what} failed:\n{r.stdout}\n{r.stderr}")
 
 
 def build_library(verbose: bool = True) -> str:
@@ -43,14 +66,16 @@ def build_library(verbose: bool = True) -> str:
                 print(l, file=sys.stderr)
         return obj
 
+    bind, link_binding = _binding_commands()
     with ThreadPoolExecutor(max_workers=4) as ex:
+        binding = ex.submit(_run, bind, "g++ for q8_bind.cpp")
         objs = list(ex.map(compile_one, SOURCES))
-    cmd = [hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", LIB]
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if r.returncode != 0:
-        raise RuntimeError(f"link failed:\n{r.stdout}\n{r.stderr}")
+        binding.result()
+    _run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", LIB], "link")
+    _run(link_binding, "link of the binding")
     if verbose:
         print(f"built {LIB}")
+        print(f"built {BINDING}")
     return LIB
 
 
