@@ -8,6 +8,8 @@
 
 #include <stdint.h>
 
+#include <cmath>
+
 namespace shifter {
 
 constexpr uint32_t Q8_ALIGN = 16;                  // bytes: a row's start, and the granule of its stride
@@ -80,13 +82,17 @@ constexpr Q8TileCost Q8_TILES[Q8_TILES_N] = {{64, 64, 3.2, 0.215, 0.235, 0.235},
                                              {256, 256, 7.0, 1.04, 1.72, 0.0}};
 constexpr double Q8_UNITS = 256.0;      // compute units
 
-// us of a product of m x n sums over k bytes, each made by `parts` blocks.
+// Blocks a compute unit of m x n sums, each made by `parts` of them.
+inline double q8_rounds(const Q8TileCost& c, uint64_t m, uint64_t n, uint64_t parts) {
+    return (double)((m + c.rows - 1u) / c.rows) * (double)((n + c.cols - 1u) / c.cols) * (double)parts / Q8_UNITS;
+}
+
+// us of these sums, over k bytes.
 inline double q8_tile_us(const Q8TileCost& c, uint64_t m, uint64_t n, uint64_t k, uint64_t parts = 1) {
-    const double tiles = (double)((m + c.rows - 1u) / c.rows) * (double)((n + c.cols - 1u) / c.cols) * (double)parts;
-    const double stages = (double)(((k + 127u) / 128u + parts - 1u) / parts), rounds = tiles / Q8_UNITS;
+    const double rounds = q8_rounds(c, m, n, parts), stages = (double)(((k + 127u) / 128u + parts - 1u) / parts);
     if (rounds <= 1.0) return c.start + stages * (c.alone + (c.one - c.alone) * rounds);
     if (c.shared > 0.0) return c.start + stages * (c.shared * rounds > c.one ? c.shared * rounds : c.one);
-    return c.start + stages * c.one * (double)((uint64_t)((tiles + Q8_UNITS - 1.0) / Q8_UNITS));
+    return c.start + stages * c.one * std::ceil(rounds);
 }
 
 // Up to 16 rows the reading of the weights is all there is, and the kernel without LDS does it best: 1 x 4096 x 4096 5.4 us
@@ -110,16 +116,26 @@ constexpr uint32_t Q8_SLICES = 128, Q8_SLICE_ROWS = 32;      // most slices; a s
 // reads g once; beyond, the rows are read in slices for the columns' largest first.  us a call, one launch / two: 966 x 232 x 320
 // 15.2 / 19.2, 1000 x 4096 x 4096 70.7 / 75.9; equal at 2048 rows; 4096 x 64 x 1024 30.8 / 26.2, 4096 x 4096 x 1024 74.5 / 82.3.
 constexpr uint32_t Q8_WHOLE_ROWS = 2048;
-// The gradient's kernels, tiles of (columns of g) x (columns of the checkpoint), the costs as above.  Measured, us of the tiles' kernel:
-//    m x n x k             64x64   64x128   64x256  128x256         m x n x k             64x64   64x128   64x256  128x256
-//    16384 x 4096 x 4096     886      695      683      593         512 x 4096 x 1024      14.0     12.5     11.9     18.0
-//    2048 x 2048 x 2048     33.8     28.5     26.3     36.1         2048 x 1873 x 977      18.1     19.5     21.7     36.5
-//    16384 x 512 x 512      76.2     89.0      113      196         64 x 512 x 512          5.3      6.9      7.2     11.0
-// (the last without the launch of the digits; the first on random digits, on those of a real gradient 690 with 128x256)
+// The gradient's kernels, tiles of (columns of g) x (columns of the checkpoint), the costs as above.  DEEP: three stages in LDS
+// for two, so that one block fills a compute unit: taken where there is a unit for every block.  Measured, us of the tiles' kernel:
+//    m x n x k             64x64  deep  64x128  deep  64x256  128x256
+//    16384 x 4096 x 4096     912  1066     703   797     689      638
+//    2048 x 2048 x 2048     32.9  41.7    27.5  30.2    26.5     37.1
+//    2048 x 1873 x 977      18.8  25.1    18.2  17.2    23.0     37.3
+//    512 x 4096 x 1024      14.2  21.7    11.4  13.7    12.2     18.1
+//    3000 x 1500 x 700      20.6  28.9    22.0  18.6    28.0     47.4
+//    8192 x 1000 x 300      40.9  31.9    47.0  38.9    61.0      106
+//    16384 x 512 x 512      76.0  57.2    83.9  72.0     113      198
+//    256 x 2048 x 512        5.8   6.0     6.1   6.2     8.3     13.0
+// (on random digits; the first on those of a real gradient 690 with 128x256)
 // Q8_GRAD_SMALL: no digits and no workspace, sums in 64-bit floating point (which the vector units add as fast as 32-bit).
-enum Q8GradientKernel { Q8_GRAD_SMALL = -1, Q8_GRAD_64x64, Q8_GRAD_64x128, Q8_GRAD_64x256, Q8_GRAD_128x256, Q8_GRAD_KERNELS };
+enum Q8GradientKernel { Q8_GRAD_SMALL = -1, Q8_GRAD_64x64, Q8_GRAD_64x64_DEEP, Q8_GRAD_64x128, Q8_GRAD_64x128_DEEP,
+                        Q8_GRAD_64x256, Q8_GRAD_128x256, Q8_GRAD_KERNELS };
+constexpr double Q8_ALONE = -1.0;       // in the place of `shared`: only where every block has a unit
 constexpr Q8TileCost Q8_GRAD_TILES[] = {{64, 64, 3.5, 0.57, 0.62, 0.43},
-                                        {64, 128, 4.0, 0.67, 0.97, 0.67},
+                                        {64, 64, 3.5, 0.41, 0.50, Q8_ALONE},
+                                        {64, 128, 4.3, 0.60, 0.86, 0.72},
+                                        {64, 128, 4.3, 0.52, 0.74, Q8_ALONE},
                                         {64, 256, 5.0, 0.85, 1.32, 0.0},
                                         {128, 256, 7.0, 1.50, 2.29, 0.0}};
 // Where tiles are few the rows are split among `parts` blocks a tile; their sums, fp32, are joined by a launch of its own,
@@ -165,6 +181,7 @@ inline Q8GradientPlan q8_gradient_plan(uint64_t m, uint64_t n, uint64_t k) {
     double least = 0.0;
     for (int i = 0; i < Q8_GRAD_KERNELS; ++i)
         for (uint64_t x = 1; x <= Q8_PARTS && (x == 1 || 2u * 128u * x <= p.ld); x *= 2) {
+            if (Q8_GRAD_TILES[i].shared == Q8_ALONE && q8_rounds(Q8_GRAD_TILES[i], n, k, x) > 1.0) continue;
             const double us = q8_tile_us(Q8_GRAD_TILES[i], n, k, m, x) + q8_join_us(x, n, k);
             if ((i == 0 && x == 1) || us < least) { least = us; p.kernel = (Q8GradientKernel)i; parts = x; }
         }

@@ -464,6 +464,7 @@ static uint32_t turn_blocks(const Q8GradientArgs& a, const Q8GradientPlan& pl, u
 // What a column's digits are made with, from its largest |p|.  No factor: zeros, or a column that is not finite.
 struct ColumnScale {
     float up, factor;
+    ColumnScale() = default;
     __device__ __forceinline__ explicit ColumnScale(uint32_t top) {
         const float c = __uint_as_float(top);
         up = digits_up(c);
@@ -491,18 +492,19 @@ __device__ __forceinline__ void digit_words(uint32_t a, uint32_t b, uint32_t c, 
     d2 = (hi | lo) ^ 0x80808080u;
 }
 
-// Digits of 16 columns and all rows by a block that holds them in registers, eight columns of eight rows a thread: g is
-// read once, and what a thread has of a column leaves as eight bytes.  Neighbouring blocks, which share lines of g, are
-// on one chiplet.  Behind the blocks for digits come those that turn the checkpoint.  2048 x 1873 (bf16, odd stride) and 977
-// columns of checkpoint take 13 us: 23 MB, but only 118 blocks for the digits, each of which waits for its reads once,
-// for the columns' largest, and then codes; latency bounds it.
+// Digits of 16 columns and all rows by a block that holds them in registers, eight columns of four rows a thread: g is
+// read once, and what a thread has of a column leaves as four bytes.  Neighbouring blocks, which share lines of g, are
+// on one chiplet.  Behind the blocks for digits come those that turn the checkpoint.  100 x 512 with 512 columns of checkpoint
+// takes 3.5 us, little more than a launch (with eight rows a thread, and a column's unit made by every thread, 5.5);
+// 2048 x 1873 (bf16, odd stride) and 977 10.4 us for 23 MB, 2048 x 4096 and 4096 13 us for 58 MB, 4.5 TB/s.
 template <typename T, uint32_t THREADS>
 __global__ __launch_bounds__(THREADS) void q8_columns_kernel(Q8GradientArgs a, Q8GradientPlan pl, uint32_t blocks) {
-    constexpr uint32_t DEEP = 8;
+    constexpr uint32_t COLS = 16, DEEP = 4;                              // a block's columns, a thread's rows
+    static_assert(THREADS / 2 * DEEP <= Q8_WHOLE_ROWS, "all rows");
     __shared__ uint32_t lds[THREADS / BLOCK * 128 * TURN_PITCH];
     if (blockIdx.x >= blocks) return turn_codes<THREADS>(a, pl, blockIdx.x - blocks, lds);
     const uint32_t xcd = blockIdx.x % 8u, block = xcd * (blocks / 8u) + min(xcd, blocks % 8u) + blockIdx.x / 8u;
-    const uint32_t cg = threadIdx.x & 1u, m0 = (threadIdx.x >> 1) * DEEP, n = block * 16u + cg * 8u;
+    const uint32_t cg = threadIdx.x % 2u, m0 = threadIdx.x / 2u * DEEP, n = block * COLS + cg * 8u;
     Eight<T> e[DEEP];
     float s[DEEP];
 #pragma unroll
@@ -511,7 +513,7 @@ __global__ __launch_bounds__(THREADS) void q8_columns_kernel(Q8GradientArgs a, Q
         fetch8(static_cast<const T*>(a.g) + (uint64_t)m * a.ld_g, n, a.n, e[r]);
         s[r] = a.s[m];
     }
-    if (threadIdx.x < 16u) lds[threadIdx.x] = 0;
+    if (threadIdx.x < COLS) lds[threadIdx.x] = 0;
     __syncthreads();
     uint32_t top[8] = {};
 #pragma unroll
@@ -530,14 +532,22 @@ __global__ __launch_bounds__(THREADS) void q8_columns_kernel(Q8GradientArgs a, Q
         if ((threadIdx.x & 15u) < 2u) atomicMax(&lds[cg * 8u + i], top[i]);
     }
     __syncthreads();
-    if (threadIdx.x < 16u && block * 16u + threadIdx.x < a.n)
-        reinterpret_cast<uint32_t*>(a.work + pl.tops)[block * 16u + threadIdx.x] = lds[threadIdx.x];
+    float* s_scale = reinterpret_cast<float*>(lds + COLS);               // factor and up of every column
+    if (threadIdx.x < COLS) {
+        const ColumnScale scale(lds[threadIdx.x]);
+        s_scale[2u * threadIdx.x] = scale.factor;
+        s_scale[2u * threadIdx.x + 1u] = scale.up;
+        if (block * COLS + threadIdx.x < a.n) reinterpret_cast<uint32_t*>(a.work + pl.tops)[block * COLS + threadIdx.x] = lds[threadIdx.x];
+    }
+    __syncthreads();
     if (m0 >= (uint32_t)pl.ld) return;
     int8_t* out = reinterpret_cast<int8_t*>(a.work + pl.digits) + m0;
 #pragma unroll
     for (uint32_t i = 0; i < 8; ++i) {
         if (n + i >= a.n) break;
-        const ColumnScale scale(lds[cg * 8u + i]);
+        ColumnScale scale;
+        scale.factor = s_scale[2u * (cg * 8u + i)];
+        scale.up = s_scale[2u * (cg * 8u + i) + 1u];
         uint32_t u[DEEP];
 #pragma unroll
         for (uint32_t r = 0; r < DEEP; ++r) {
@@ -545,13 +555,11 @@ __global__ __launch_bounds__(THREADS) void q8_columns_kernel(Q8GradientArgs a, Q
             e[r].floats(f);
             u[r] = scale(m0 + r < a.m ? __fmul_rn(f[i], s[r]) : 0.0f);       // rows behind the last one count as zero
         }
-        uint32_t d[3][2];
-#pragma unroll
-        for (uint32_t x = 0; x < 2; ++x)
-            digit_words(u[4 * x], u[4 * x + 1], u[4 * x + 2], u[4 * x + 3], d[0][x], d[1][x], d[2][x]);
+        uint32_t d[3];
+        digit_words(u[0], u[1], u[2], u[3], d[0], d[1], d[2]);
 #pragma unroll
         for (uint32_t p = 0; p < 3; ++p)
-            *reinterpret_cast<uint2*>(out + ((uint64_t)p * a.n + n + i) * pl.ld) = make_uint2(d[p][0], d[p][1]);
+            *reinterpret_cast<uint32_t*>(out + ((uint64_t)p * a.n + n + i) * pl.ld) = d[p];
     }
 }
 
@@ -862,8 +870,9 @@ static void launch_columns(shifter_ctx* ctx, const Q8GradientArgs& g, const Q8Gr
 
 template <typename T>
 static void launch_digits(shifter_ctx* ctx, const Q8GradientArgs& g, const Q8GradientPlan& pl) {
-    if (pl.ld <= 1024) return launch_columns<T, 256>(ctx, g, pl);
-    if (pl.ld <= Q8_WHOLE_ROWS) return launch_columns<T, 512>(ctx, g, pl);
+    if (pl.ld <= 512) return launch_columns<T, 256>(ctx, g, pl);
+    if (pl.ld <= 1024) return launch_columns<T, 512>(ctx, g, pl);
+    if (pl.ld <= Q8_WHOLE_ROWS) return launch_columns<T, 1024>(ctx, g, pl);
     const uint32_t across = (g.n + 63u) / 64u, tiles = (uint32_t)(pl.ld / TURN_ROWS), tops = (g.n + 511u) / 512u * pl.slices;
     q8_tops_kernel<T><<<tops + turn_blocks(g, pl, BLOCK), BLOCK, 0, ctx->stream>>>(g, pl, tops);
     // every block reads its columns' slices: as many rows a block as leave 2048 blocks
@@ -930,9 +939,11 @@ void launch_q8_gradient(shifter_ctx* ctx, int dtype, const Q8GradientArgs& g) {
     ProfileScope ps(ctx, K_Q8_GRADIENT);
     switch (pl.kernel) {
         case Q8_GRAD_64x64: launch_gradient_as<2, 2, 1, 1, 2, 128, 8>(ctx, g, pl); break;
-        case Q8_GRAD_64x128: launch_gradient_as<2, 2, 1, 2, 2, 128, 8>(ctx, g, pl); break;
+        case Q8_GRAD_64x64_DEEP: launch_gradient_as<2, 2, 1, 1, 3, 128, 8>(ctx, g, pl); break;
+        case Q8_GRAD_64x128: launch_gradient_as<2, 4, 1, 1, 2, 128, 8>(ctx, g, pl); break;
+        case Q8_GRAD_64x128_DEEP: launch_gradient_as<2, 4, 1, 1, 3, 128, 8>(ctx, g, pl); break;
         case Q8_GRAD_64x256: launch_gradient_as<2, 4, 1, 2, 2, 128, 8>(ctx, g, pl); break;
-        default: launch_gradient_as<4, 2, 1, 4, 2, 128, 4>(ctx, g, pl); break;
+        default: launch_gradient_as<4, 2, 1, 4, 4, 64, 4>(ctx, g, pl); break;
     }
 }
 
