@@ -62,24 +62,24 @@ struct Q8TileCost {
     // two share a unit, a tile's part of it (0: they do not, and rounds are whole numbers)
     double start, alone, one, shared;
 };
-// Measured on 256 compute units, us a call by tile:
-//    m x n x k            64x64   64x128  128x128  128x256  256x256
-//    128 x 4096 x 4096     10.5     13.1     16.8     29.3     40.3
-//    512 x 4096 x 4096     17.5     15.5     17.6     29.4     41.3
-//    1024 x 4096 x 4096    32.3     25.9     22.8     31.2     42.7
-//    2048 x 4096 x 4096    60.9     47.5       44     38.0     48.6
-//    4096 x 4096 x 4096     115       90       80       79       62
-//    777 x 1873 x 977       7.3      7.0      8.0     11.4     17.4
-//    2048 x 2048 x 2048    18.4     15.4     14.5     18.7     26.1
-//    4096 x 1024 x 8192    61.0     46.5     41.2     55.0     77.3
-//    16384 x 100 x 2048    12.7     11.1     11.7     18.1     26.8
+// Measured on 256 compute units, us of the kernel by tile:
+//    m x n x k             64x64   64x128  128x128  128x256  256x256
+//    128 x 4096 x 4096     10.5     12.0     16.1     24.8     39.5
+//    512 x 4096 x 4096     15.7     14.7     18.1     25.2     40.4
+//    1024 x 4096 x 4096    30.1     24.1     21.5     26.2     41.3
+//    2048 x 4096 x 4096    55.2     44.3     39.8     33.8     42.5
+//    4096 x 4096 x 4096     106     85.4     77.7     65.0     57.4
+//    777 x 1873 x 977       6.8      6.1      7.6     10.8     17.4
+//    2048 x 2048 x 2048    16.9     13.4     12.8     16.2     24.8
+//    4096 x 1024 x 8192    53.0     43.7     37.7     45.5     73.4
+//    16384 x 100 x 2048     9.4      9.1     11.4     16.8     26.4
 // The costs below say these within 15 %; the kernel of the least cost is taken.
 constexpr int Q8_TILES_N = 5;
-constexpr Q8TileCost Q8_TILES[Q8_TILES_N] = {{64, 64, 3.2, 0.215, 0.235, 0.235},
-                                             {64, 128, 3.5, 0.30, 0.38, 0.37},
-                                             {128, 128, 4.0, 0.40, 0.59, 0.0},
-                                             {128, 256, 5.0, 0.76, 1.03, 0.0},
-                                             {256, 256, 7.0, 1.04, 1.72, 0.0}};
+constexpr Q8TileCost Q8_TILES[Q8_TILES_N] = {{64, 64, 3.2, 0.21, 0.235, 0.20},
+                                             {64, 128, 3.2, 0.265, 0.36, 0.325},
+                                             {128, 128, 4.0, 0.37, 0.56, 0.0},
+                                             {128, 256, 5.0, 0.60, 0.88, 0.0},
+                                             {256, 256, 7.0, 0.99, 1.58, 0.0}};
 constexpr double Q8_UNITS = 256.0;      // compute units
 
 // Blocks a compute unit of m x n sums, each made by `parts` of them.

@@ -311,61 +311,71 @@ __global__ __launch_bounds__(64 * WAVES) void q8_product_few_kernel(Q8ProductArg
     v4i acc[F];
 #pragma unroll
     for (uint32_t f = 0; f < F; ++f) acc[f] = v4i{0, 0, 0, 0};
-    const uint32_t whole = g.k / PIECE;
-    uint32_t p = wave;
-    for (; p + (DEPTH - 1u) * WAVES < whole; p += DEPTH * WAVES) {
-        v4i vb[DEPTH][2], va[DEPTH][F][2];
+    // what the sums are finished with is on its way while they are made
+    const uint32_t m = wave * 16u + (lane & 15u), n = n0 + lane / 16u * 4u;
+    float sa = 0.0f, sb[4], bias[4];
+    if (wave < F) {
+        sa = g.sa[min(m, g.m - 1u)];
 #pragma unroll
-        for (uint32_t d = 0; d < DEPTH; ++d)
+        for (uint32_t e = 0; e < 4; ++e) {
+            sb[e] = g.sb[min(n + e, g.n - 1u)];
+            bias[e] = g.bias ? g.bias[min(n + e, g.n - 1u)] : 0.0f;
+        }
+    }
+    const uint32_t whole = g.k / PIECE, pieces = (g.k + PIECE - 1u) / PIECE;
+    uint32_t p = wave;
+    // D pieces, `ends`: the row may end in or before them
+    auto round = [&](auto depth, auto ends) {
+        constexpr uint32_t D = depth.value;
+        v4i vb[D][2], va[D][F][2];
+#pragma unroll
+        for (uint32_t d = 0; d < D; ++d)
 #pragma unroll
             for (uint32_t x = 0; x < 2; ++x) {
-                const uint32_t k = (p + d * WAVES) * PIECE + x * 64u + at;
+                uint32_t k = (p + d * WAVES) * PIECE + x * 64u + at;
+                if (ends.value) k = min(k, (g.k - 1u) & ~(UNIT - 1u));   // behind the row's end: its last unit again
                 vb[d][x] = *reinterpret_cast<const v4i*>(b + k);
 #pragma unroll
                 for (uint32_t f = 0; f < F; ++f) va[d][f][x] = *reinterpret_cast<const v4i*>(a[f] + k);
             }
 #pragma unroll
-        for (uint32_t d = 0; d < DEPTH; ++d)
+        for (uint32_t d = 0; d < D; ++d)
 #pragma unroll
-            for (uint32_t x = 0; x < 2; ++x)
+            for (uint32_t x = 0; x < 2; ++x) {
+                if (ends.value) {                                        // bytes behind it count as zero
+                    const int32_t left = (int32_t)g.k - (int32_t)((p + d * WAVES) * PIECE + x * 64u + at);
+#pragma unroll
+                    for (int32_t e = 0; e < 4; ++e) {
+                        const int32_t c = min(max(left - 4 * e, 0), 4), keep = c == 4 ? -1 : (1 << (8 * c)) - 1;
+                        vb[d][x][e] &= keep;
+                    }
+                }
 #pragma unroll
                 for (uint32_t f = 0; f < F; ++f)
                     acc[f] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vb[d][x], va[d][f][x], acc[f], 0, 0, 0);
-    }
-    for (; p * PIECE < g.k; p += WAVES) {
-#pragma unroll
-        for (uint32_t x = 0; x < 2; ++x) {
-            const uint32_t k = p * PIECE + x * 64u + at;
-            const uint32_t from = min(k, (g.k - 1u) & ~(UNIT - 1u));     // behind the row's end: its last unit again
-            const v4i vb = *reinterpret_cast<const v4i*>(b + from);
-#pragma unroll
-            for (uint32_t f = 0; f < F; ++f) {
-                v4i va = *reinterpret_cast<const v4i*>(a[f] + from);
-#pragma unroll
-                for (int32_t e = 0; e < 4; ++e) {                        // bytes behind it count as zero
-                    const int32_t n = min(max((int32_t)g.k - (int32_t)k - 4 * e, 0), 4);
-                    va[e] &= n == 4 ? -1 : (1 << (8 * n)) - 1;
-                }
-                acc[f] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vb, va, acc[f], 0, 0, 0);
             }
-        }
+        p += D * WAVES;
+    };
+    while (p + (DEPTH - 1u) * WAVES < whole) round(std::integral_constant<uint32_t, DEPTH>{}, std::false_type{});
+    while (p < pieces) {
+        if (p + 2u * WAVES < pieces) round(std::integral_constant<uint32_t, DEPTH>{}, std::true_type{});
+        else if (p + WAVES < pieces) round(std::integral_constant<uint32_t, 2>{}, std::true_type{});
+        else round(std::integral_constant<uint32_t, 1>{}, std::true_type{});
     }
 #pragma unroll
     for (uint32_t f = 0; f < F; ++f) s_sum[wave][f][lane] = acc[f];
     __syncthreads();
     static_assert(WAVES >= F, "a wavefront for 16 tokens' sums");
     if (wave >= F) return;
-    const uint32_t m = wave * 16u + (lane & 15u), n = n0 + lane / 16u * 4u;
     v4i sum = s_sum[0][wave][lane];
 #pragma unroll
     for (uint32_t w = 1; w < WAVES; ++w) sum += s_sum[w][wave][lane];
     if (m >= g.m) return;
-    const float sa = g.sa[m];
     T* c = static_cast<T*>(g.c) + (uint64_t)m * g.ld_c + n;
 #pragma unroll
     for (uint32_t e = 0; e < 4; ++e) {
         if (n + e >= g.n) break;
-        float v = fmaf((float)sum[e] * sa, g.sb[n + e], g.bias ? g.bias[n + e] : 0.0f);
+        float v = fmaf((float)sum[e] * sa, sb[e], bias[e]);
         if (g.relu) v = v < 0.0f ? 0.0f : v;
         c[e] = (T)v;
     }
@@ -385,9 +395,9 @@ static void launch_product_of(shifter_ctx* ctx, const Q8ProductArgs& g) {
             else launch_product_few<T, 3, 16>(ctx, g);
             break;
         case Q8_TILE_64x64: launch_product_as<T, 2, 2, 1, 1, 4, 128, 16>(ctx, g); break;
-        case Q8_TILE_64x128: launch_product_as<T, 2, 2, 1, 2, 3, 128, 8>(ctx, g); break;
+        case Q8_TILE_64x128: launch_product_as<T, 2, 4, 1, 1, 3, 128, 8>(ctx, g); break;
         case Q8_TILE_128x128: launch_product_as<T, 2, 4, 2, 1, 3, 128, 8>(ctx, g); break;
-        case Q8_TILE_128x256: launch_product_as<T, 2, 4, 2, 2, 2, 128, 8>(ctx, g); break;
+        case Q8_TILE_128x256: launch_product_as<T, 2, 4, 2, 2, 3, 128, 8>(ctx, g); break;
         default: launch_product_as<T, 2, 4, 4, 2, 2, 128, 4>(ctx, g); break;
     }
 }
