@@ -229,7 +229,7 @@ __device__ __forceinline__ void store_rows(const int8_t* from, uint32_t pitch, T
 }
 
 // c[m][n] = (sum over k of A[m][k] B[n][k]) sa[m] sb[n] + bias[n]: the sum exact, then two roundings in fp32 and the one to
-// c's type.  8192 x 8192 x 8192 to bf16 takes 446 us, 2.46 POP/s, against 2.42 of the library's bare integer product:
+// c's type.  8192 x 8192 x 8192 to bf16 takes 420 to 445 us, 2.5 to 2.6 POP/s, against 2.42 of the library's bare integer product:
 // the matrix units are busy 69 % of the time and the card lowers its clock to 1.6 GHz under them, so that power is the
 // bound.  A band of GROUP tiles keeps memory out of the way: 0.8 GB are read, 1.8 TB/s.  Eight wavefronts of 128 x 64 each
 // for 256 x 256: four of 128 x 128 would read a fifth less LDS but spill (505 us or more).
@@ -296,8 +296,9 @@ static void launch_product_as(shifter_ctx* ctx, const Q8ProductArgs& g) {
 // Few tokens: the weights are read once, straight into registers, and that read is the time.  A block has 16
 // columns of the result and all of the up to 16 F tokens; its WAVES wavefronts take pieces of 128 bytes of the
 // rows in turn and join their sums in LDS.  (Weights are the first factor of the 16 x 16 x 64 products: a
-// lane then holds four neighbouring columns of one token.)  1 x 4096 x 4096 takes 5.3 us, of which 3.0 are the weights' 16.8 MB at
-// a large copy's rate; 48 x 3277 x 3541 7.6 us.  Four pieces of each wavefront are under way: 16 KB to 64 KB a block.
+// lane then holds four neighbouring columns of one token.)  1 x 4096 x 4096 takes 5.3 us, 6.3 with the weights in no cache, of
+// which 3.4 are their 16.8 MB at a large copy's rate, 5.0 TB/s; 1 x 8192 x 8192 14.6 us, 4.6 TB/s; 48 x 3277 x 3541 7.6 and 9.6 us.
+// Four pieces of each wavefront are under way: 16 KB to 64 KB a block.
 template <typename T, uint32_t F, uint32_t WAVES>
 __global__ __launch_bounds__(64 * WAVES) void q8_product_few_kernel(Q8ProductArgs g) {
     constexpr uint32_t PIECE = 128, DEPTH = 4;                           // bytes; pieces under way
@@ -390,7 +391,10 @@ template <typename T>
 static void launch_product_of(shifter_ctx* ctx, const Q8ProductArgs& g) {
     switch (q8_kernel_for(g.m, g.n, g.k)) {
         case Q8_FEW:
-            if (g.m <= 16) launch_product_few<T, 1, 8>(ctx, g);
+            // long rows and a block a compute unit: more wavefronts (1 x 4096 x 14336 14.1 -> 13.6 us, 8 x 1024 x 16384 15.6 -> 14.5;
+            // but 1 x 8192 x 4200 9.0 -> 10.0, 16 x 8192 x 8192 20.1 -> 20.5)
+            if (g.m <= 16 && g.k >= 8192 && g.n <= 4096) launch_product_few<T, 1, 16>(ctx, g);
+            else if (g.m <= 16) launch_product_few<T, 1, 8>(ctx, g);
             else if (g.m <= 32) launch_product_few<T, 2, 16>(ctx, g);
             else launch_product_few<T, 3, 16>(ctx, g);
             break;
@@ -724,9 +728,10 @@ __device__ __forceinline__ void store_gradient(const int8_t* from, uint32_t pitc
 
 // dW[n][k] = unit[n] (2^16 D2 + 2^8 D1 + D0), Dp the exact sum of digit plane p of column n times column k of the codes.  One
 // tile of Q serves the three planes, whose sums all stay in registers: 128 x 256 of them fill eight wavefronts' 192
-// accumulators.  16384 x 4096 x 4096 takes 690 us, 2.39 POP/s over the three products, with the matrix units 56 % busy at
-// 2.0 GHz: power, as in the product.  2048 x 1873 x 977 takes 20 us on tiles of 64 x 64: less than two a compute unit,
-// whose stages are bound by the latency of LDS and of the fetches.
+// accumulators.  16384 x 4096 x 4096 takes 640 to 675 us, 2.5 POP/s over the three products: power, as in the product (with
+// stages of 128 bytes, two for four of 64, 650 to 690).  2048 x 1873 x 977 takes 19 us on tiles of 64 x 128, one on a compute
+// unit: its LDS is read and written 0.5 us for each of 16 stages, so eight wavefronts, of which one reads while another
+// multiplies, take 16.4 us where four with half as many reads take 19 to 20; the rest is a launch, the digits' and the mask's way from memory.
 template <uint32_t WA, uint32_t WB, uint32_t FA, uint32_t FB, uint32_t NS, uint32_t STEP, uint32_t GROUP>
 __global__ __launch_bounds__(64 * WA * WB) void q8_gradient_kernel(Q8GradientArgs g, Q8GradientPlan pl) {
 
