@@ -61,7 +61,9 @@ def load_calls():
 class Q8:
     """The 8-bit operators on one device and stream.  Matrices of elements are two-dimensional
     fp32, bf16 or fp16 tensors whose columns lie side by side; their rows may have any stride.
-    Results are new tensors unless ``out`` (or ``h``) says where they go."""
+    Results are new tensors unless ``out`` (or ``h``) says where they go.  Recorded into a graph,
+    calls of one handle share a workspace apart from that of calls made at once: replays of such graphs
+    go one after another, on whatever stream."""
 
     def __init__(self, device: int = 0, ctx=None):
         if not torch.cuda.is_available():
@@ -72,7 +74,7 @@ class Q8:
         self.own = ctx is None
         self.ctx = ctx or S.shifter_create(device, self.stream)
         self.work = None
-        self.recorded = []                 # workspaces that a recorded call holds
+        self.recorded = []                 # workspaces of recorded calls, which use them at every replay
         self._calls = load_calls()
 
     def close(self):
@@ -87,11 +89,13 @@ class Q8:
         return self.ctx.handle.value, self.dev.index
 
     def _room(self, need: int) -> torch.Tensor:
-        """A workspace of `need` bytes at least, kept from call to call."""
+        """A workspace of `need` bytes at least, kept from call to call; recorded calls have their own."""
+        if torch.cuda.is_current_stream_capturing():
+            if not self.recorded or self.recorded[-1].numel() < need:
+                self.recorded.append(torch.empty(need, dtype=torch.uint8, device=self.dev))
+            return self.recorded[-1]
         if self.work is None or self.work.numel() < need:
             self.work = torch.empty(need, dtype=torch.uint8, device=self.dev)
-        if torch.cuda.is_current_stream_capturing() and not any(w is self.work for w in self.recorded):
-            self.recorded.append(self.work)
         return self.work
 
     # ---- the operators --------------------------------------------------------------

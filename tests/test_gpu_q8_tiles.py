@@ -84,3 +84,31 @@ def test_digits(ops, m, dtype):
     """Digits of all rows at once by 256, 512 and 1024 threads, and in slices."""
     check_gradient(ops, m, 250, 260, dtype, seed=m, gap=m % 3, shift=m % 2)
     check_gradient(ops, m, 5, 300, dtype, seed=m)
+
+
+@pytest.mark.gpu
+def test_recorded_workspace():
+    """A recorded gradient keeps its workspace to itself: replays on another stream than the handle's, with calls made at once
+    of other sizes under way beside them, give what they gave alone."""
+    stream, other = torch.cuda.Stream(), torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        ops = Q8()
+        gen = torch.Generator(device="cuda").manual_seed(5)
+        rand = lambda *s: torch.randn(*s, generator=gen, device="cuda")
+        g, x = rand(700, 300), ops.quantize(rand(700, 200))
+        g2, x2 = rand(900, 310), ops.quantize(rand(900, 190))
+        want, want2 = ops.weight_grad(g, x), ops.weight_grad(g2, x2)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            recorded = ops.weight_grad(g, x)
+        assert len(ops.recorded) == 1 and ops.recorded[0].data_ptr() != ops.work.data_ptr()
+        torch.cuda.synchronize()
+        for _ in range(20):
+            recorded.zero_()
+            other.wait_stream(stream)
+            with torch.cuda.stream(other):
+                graph.replay()
+            got2 = ops.weight_grad(g2, x2)
+            torch.cuda.synchronize()
+            assert torch.equal(recorded, want) and torch.equal(got2, want2)
+        ops.close()
