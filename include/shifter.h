@@ -713,7 +713,7 @@ int shifter_compact_batch_masked(shifter_ctx* ctx, const shifter_model* model, c
  *                        m up to SHIFTER_Q8_MAX_SUM, else SHIFTER_ERR_CAPACITY; more rows go in several calls with
  *                        SHIFTER_Q8_ACCUMULATE.
  *                        d_work: work_bytes of shifter_weight_grad_q8_layout, 256-byte aligned; NULL where that says
- *                        0, as it does for few rows. */
+ *                        0, as it does for few rows and for little work. */
 typedef enum { SHIFTER_F32 = 0, SHIFTER_BF16 = 1, SHIFTER_F16 = 2 } shifter_dtype;
 #define SHIFTER_Q8_RELU 1u
 #define SHIFTER_Q8_ACCUMULATE 2u

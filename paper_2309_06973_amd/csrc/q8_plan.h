@@ -128,8 +128,8 @@ constexpr uint32_t Q8_WHOLE_ROWS = 2048;
 //    16384 x 512 x 512      76.0  57.2    83.9  72.0     113      198
 //    256 x 2048 x 512        5.8   6.0     6.1   6.2     8.3     13.0
 // (on random digits; the first on those of a real gradient 690 with 128x256)
-// Q8_GRAD_SMALL: no digits and no workspace, sums in 64-bit floating point (which the vector units add as fast as 32-bit).
-enum Q8GradientKernel { Q8_GRAD_SMALL = -1, Q8_GRAD_64x64, Q8_GRAD_64x64_DEEP, Q8_GRAD_64x128, Q8_GRAD_64x128_DEEP,
+// Q8_GRAD_SMALL and _WIDE: no digits and no workspace, sums in 64-bit floating point, in one launch.
+enum Q8GradientKernel { Q8_GRAD_WIDE = -2, Q8_GRAD_SMALL = -1, Q8_GRAD_64x64, Q8_GRAD_64x64_DEEP, Q8_GRAD_64x128, Q8_GRAD_64x128_DEEP,
                         Q8_GRAD_64x256, Q8_GRAD_128x256, Q8_GRAD_KERNELS };
 constexpr double Q8_ALONE = -1.0;       // in the place of `shared`: only where every block has a unit
 constexpr Q8TileCost Q8_GRAD_TILES[] = {{64, 64, 3.5, 0.57, 0.62, 0.43},
@@ -141,12 +141,12 @@ constexpr Q8TileCost Q8_GRAD_TILES[] = {{64, 64, 3.5, 0.57, 0.62, 0.43},
 // Where tiles are few the rows are split among `parts` blocks a tile; their sums, fp32, are joined by a launch of its own,
 // which costs that and the traffic.
 constexpr uint64_t Q8_PARTS = 32;
-// Few rows, and few products in all, go to the small kernel's one launch.  us, that / digits and tiles: 1 x 64 x 64 4.1 / 10.7,
-// 1 x 4096 x 4096 17.7 / 34.5, 16 x 4096 x 4096 24.3 / 34.4, 32 x 4096 x 4096 36.3 / 34.4; 64 x 512 x 512 6.6 / 11.7,
-// 64 x 2048 x 2048 20.6 / 17.2, 128 x 1024 x 1024 16.9 / 12.3.
-constexpr uint64_t Q8_SMALL_ROWS = 16, Q8_SMALL_ROWS_MOST = 64, Q8_SMALL_WORK = 1ull << 27;
+// Little work, and few rows of whatever size, go to one launch.  us, that / digits and tiles: 64 x 512 x 512 3.3 / 9.3, 300 x 300 x 300
+// 4.4 / 9.5, 500 x 250 x 333 6.0 / 12, 1000 x 100 x 200 9.1 / 12, 128 x 1024 x 1024 9.6 / 9.6, 64 x 1400 x 1400 11.8 / 11.6,
+// 256 x 1024 x 1024 14.5 / 11.5; 16 x 4096 x 4096 24.8 / 27.8 (1 x 4096 x 4096 15.5).
+constexpr uint64_t Q8_SMALL_ROWS = 1024, Q8_SMALL_RESULTS = 1ull << 20, Q8_SMALL_WORK = 1ull << 27, Q8_WIDE_ROWS = 16;
 constexpr bool q8_small(uint64_t m, uint64_t n, uint64_t k) {
-    return m <= Q8_SMALL_ROWS || (m <= Q8_SMALL_ROWS_MOST && m * n * k <= Q8_SMALL_WORK);
+    return m <= Q8_SMALL_ROWS && n * k <= Q8_SMALL_RESULTS && m * n * k <= Q8_SMALL_WORK;
 }
 constexpr double q8_join_us(uint64_t parts, uint64_t n, uint64_t k) {
     return parts > 1 ? 3.5 + 2.0e-6 * (double)parts * (double)n * (double)k : 0.0;
@@ -171,8 +171,8 @@ inline Q8GradientPlan q8_gradient_plan(uint64_t m, uint64_t n, uint64_t k) {
     p.sums = p.codes + k * p.ld;
     p.parts = 1;
     p.part_rows = (uint32_t)p.ld;
-    if (q8_small(m, n, k)) {
-        p.kernel = Q8_GRAD_SMALL;
+    if (q8_small(m, n, k) || m <= Q8_WIDE_ROWS) {
+        p.kernel = q8_small(m, n, k) ? Q8_GRAD_SMALL : Q8_GRAD_WIDE;
         p.bytes = 0;
         return p;
     }

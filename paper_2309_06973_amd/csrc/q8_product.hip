@@ -783,53 +783,142 @@ __global__ __launch_bounds__(64 * WA * WB) void q8_gradient_kernel(Q8GradientArg
     }
 }
 
-// Few rows: one launch, no digits.  A block has 4 I columns of g and 256 of the checkpoint, a thread I by four of the
-// sums, which are 64-bit: products of a p and a code are exact in them, and the vector units add them fast enough.
-// All p of the block's columns lie in LDS; the codes come 16 rows at a time, the next ones on their way.  64 x 512 x 512
-// takes 6.6 us, a third of it the launch and the rest four trips to memory and 64 rows of additions in a thread; 1 x 4096 x
-// 4096 17.7 us, the 67 MB of dW at 3.8 TB/s.  The same with the rows split over blocks and joined was slower (9 us).
-template <typename T, uint32_t I>
-__global__ __launch_bounds__(BLOCK) void q8_gradient_small_kernel(Q8GradientArgs a) {
-    constexpr uint32_t MOST = Q8_SMALL_ROWS_MOST, COLS = 4 * I, DEEP = 16;
-    __shared__ double s_p[MOST][COLS];
+typedef double v4d __attribute__((ext_vector_type(4)));
+
+// Little work: one launch, no digits and no workspace, 64-bit products on the matrix units (as fast as the vector units', but
+// an operand serves 16 of them), in which a p times a code is exact.  A block has 16 FA columns of g and 16 FB of the
+// checkpoint; its WAVES wavefronts take 16 rows in turn, read straight into registers, the next ones on their way while these
+// are multiplied, and join their sums in LDS.  64 x 512 x 512 takes 3.3 us, little more than a launch; 300 x 300 x 300 4.4,
+// 512 x 512 x 512 9.5, where eight turns of 0.8 us, as long as a trip to memory, follow one another.
+template <typename T, uint32_t FA, uint32_t FB, uint32_t WAVES>
+__global__ __launch_bounds__(64 * WAVES) void q8_gradient_small_kernel(Q8GradientArgs a) {
+    constexpr uint32_t ROWS = 16, STEPS = ROWS / 4;                      // of a turn; four rows a step
+    typedef uint8_t codes __attribute__((ext_vector_type(FB), aligned(FB)));
+    __shared__ double s_sum[WAVES][FA * 4][FB][64];
+    const uint32_t across = (a.k + 16u * FB - 1u) / (16u * FB), n0 = blockIdx.x / across * (16u * FA), k0 = blockIdx.x % across * (16u * FB);
+    const uint32_t lane = threadIdx.x & 63u, wave = uniform_u32(threadIdx.x >> 6), col = lane & 15u, row = lane / 16u;
+    const uint32_t k = k0 + col * FB, pad = (a.k + Q8_ALIGN - 1u) & ~(Q8_ALIGN - 1u);
+    const int8_t* q = a.q + min(k, pad - FB);                            // columns behind the last one: in the row's padding
+    const T* g[FA];
+#pragma unroll
+    for (uint32_t i = 0; i < FA; ++i) g[i] = static_cast<const T*>(a.g) + min(n0 + 16u * i + col, a.n - 1u);
+    T e[STEPS][FA];
+    codes c[STEPS];
+    float s[STEPS];
+    auto fetch = [&](uint32_t from) {
+#pragma unroll
+        for (uint32_t x = 0; x < STEPS; ++x) {
+            const uint64_t m = min(from + 4u * x + row, a.m - 1u);       // behind the last one: it again
+#pragma unroll
+            for (uint32_t i = 0; i < FA; ++i) e[x][i] = g[i][m * a.ld_g];
+            c[x] = *reinterpret_cast<const codes*>(q + m * a.ld_q);
+            s[x] = a.s[m];
+        }
+    };
+    v4d acc[FA][FB];
+#pragma unroll
+    for (uint32_t i = 0; i < FA; ++i)
+#pragma unroll
+        for (uint32_t j = 0; j < FB; ++j) acc[i][j] = v4d{0.0, 0.0, 0.0, 0.0};
+    uint32_t from = wave * ROWS;
+    if (from < a.m) fetch(from);
+    while (from < a.m) {
+        double p[STEPS][FA], b[STEPS][FB];
+#pragma unroll
+        for (uint32_t x = 0; x < STEPS; ++x) {
+            const bool there = from + 4u * x + row < a.m;                // rows behind the last one count as zero
+#pragma unroll
+            for (uint32_t i = 0; i < FA; ++i) p[x][i] = there ? (double)__fmul_rn((float)e[x][i], s[x]) : 0.0;
+#pragma unroll
+            for (uint32_t j = 0; j < FB; ++j) b[x][j] = (double)(int8_t)c[x][j];
+        }
+        from += WAVES * ROWS;
+        if (from < a.m) fetch(from);
+#pragma unroll
+        for (uint32_t x = 0; x < STEPS; ++x)
+#pragma unroll
+            for (uint32_t i = 0; i < FA; ++i)
+#pragma unroll
+                for (uint32_t j = 0; j < FB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f64_16x16x4f64(p[x][i], b[x][j], acc[i][j], 0, 0, 0);
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < FA; ++i)
+#pragma unroll
+        for (uint32_t j = 0; j < FB; ++j)
+#pragma unroll
+            for (uint32_t x = 0; x < 4; ++x) s_sum[wave][i * 4u + x][j][lane] = acc[i][j][x];
+    __syncthreads();
+    // row 4 x + lane / 16 of 16 is in the x-th number of a lane
+#pragma unroll
+    for (uint32_t u = 0; u < FA * 4u; u += WAVES) {
+        const uint32_t at = u + wave;
+        if (at >= FA * 4u) break;
+        double sum[FB];
+#pragma unroll
+        for (uint32_t j = 0; j < FB; ++j) {
+            sum[j] = s_sum[0][at][j][lane];
+#pragma unroll
+            for (uint32_t w = 1; w < WAVES; ++w) sum[j] += s_sum[w][at][j][lane];
+        }
+        const uint32_t n = n0 + at / 4u * 16u + at % 4u * 4u + row;
+        if (n >= a.n || k >= a.k) continue;
+        float* to = a.dw + (uint64_t)n * a.ld_dw + k;
+        const uint8_t* mask = a.mask + (uint64_t)n * a.ld_mask + k;
+        float v[FB];
+#pragma unroll
+        for (uint32_t j = 0; j < FB; ++j) {
+            // a column with a p that is not finite: NaN in the whole row, as where digits are made
+            v[j] = isfinite(sum[j]) ? (float)sum[j] : __uint_as_float(0x7fc00000u);
+            if (k + j >= a.k) continue;
+            const float old = a.accumulate ? to[j] : 0.0f;
+            v[j] = !a.mask || mask[j] ? (a.accumulate ? old + v[j] : v[j]) : old;
+        }
+        if (k + FB <= a.k) {
+            typedef float loose __attribute__((ext_vector_type(FB), aligned(4)));
+            loose w;
+#pragma unroll
+            for (uint32_t j = 0; j < FB; ++j) w[j] = v[j];
+            *reinterpret_cast<loose*>(to) = w;
+        } else {
+#pragma unroll
+            for (uint32_t j = 0; j < FB; ++j)
+                if (k + j < a.k) to[j] = v[j];
+        }
+    }
+}
+
+// Up to 16 rows and a large dW, whose writing is the time: a block has 16 columns of g, their p in LDS, and 256 of the
+// checkpoint; a thread 4 x 4 of the sums, 64-bit on the vector units.  1 x 4096 x 4096 15.5 us, the 67 MB of dW at 4.3 TB/s
+// (25 with the kernel above and a wavefront a block).
+template <typename T>
+__global__ __launch_bounds__(BLOCK) void q8_gradient_wide_kernel(Q8GradientArgs a) {
+    constexpr uint32_t I = 4, COLS = 4 * I, DEEP = Q8_WIDE_ROWS;
+    __shared__ double s_p[DEEP][COLS];
     const uint32_t across = (a.k + 255u) / 256u, n0 = blockIdx.x / across * COLS, k0 = blockIdx.x % across * 256u;
     const uint32_t lane = threadIdx.x & 63u, wave = uniform_u32(threadIdx.x >> 6), k = k0 + lane * 4u;
     const bool there = k < a.k;                                          // the codes behind the last column are in the row's padding
     uint32_t q[DEEP];
-    auto codes = [&](uint32_t from) {
 #pragma unroll
-        for (uint32_t r = 0; r < DEEP; ++r)
-            q[r] = there ? *reinterpret_cast<const uint32_t*>(a.q + (uint64_t)min(from + r, a.m - 1u) * a.ld_q + k) : 0u;
-    };
-    if (a.m) codes(0);
-    const uint32_t rows = (a.m + DEEP - 1u) / DEEP * DEEP;               // those behind the last one count as zero
-#pragma unroll
-    for (uint32_t i = 0; i < MOST * COLS; i += BLOCK) {
-        const uint32_t r = (i + threadIdx.x) / COLS, c = (i + threadIdx.x) % COLS;
-        if (i / COLS >= rows || r >= MOST) break;
-        const uint32_t m = min(r, a.m - 1u);
-        const float p = __fmul_rn((float)static_cast<const T*>(a.g)[(uint64_t)m * a.ld_g + min(n0 + c, a.n - 1u)], a.s[m]);
-        s_p[r][c] = r < a.m ? (double)p : 0.0;
-    }
+    for (uint32_t r = 0; r < DEEP; ++r)
+        q[r] = there && a.m ? *reinterpret_cast<const uint32_t*>(a.q + (uint64_t)min(r, a.m - 1u) * a.ld_q + k) : 0u;
+    static_assert(DEEP * COLS == BLOCK, "a p a thread");
+    const uint32_t m = threadIdx.x / COLS, c = threadIdx.x % COLS;
+    float mine = 0.0f;                                                   // rows behind the last one count as zero
+    if (m < a.m) mine = __fmul_rn((float)static_cast<const T*>(a.g)[(uint64_t)m * a.ld_g + min(n0 + c, a.n - 1u)], a.s[m]);
+    s_p[m][c] = (double)mine;
     __syncthreads();
     double acc[I][4] = {};
-    for (uint32_t from = 0; from < rows; from += DEEP) {
-        uint32_t now[DEEP];
 #pragma unroll
-        for (uint32_t r = 0; r < DEEP; ++r) now[r] = q[r];
-        if (from + DEEP < rows) codes(from + DEEP);
+    for (uint32_t r = 0; r < DEEP; ++r) {
+        if (r % 4u == 0 && r >= a.m) break;
+        double p[I];
 #pragma unroll
-        for (uint32_t r = 0; r < DEEP; ++r) {
-            if (r % 4u == 0 && from + r >= a.m) break;
-            double p[I];
+        for (uint32_t i = 0; i < I; ++i) p[i] = s_p[r][wave * I + i];
 #pragma unroll
-            for (uint32_t i = 0; i < I; ++i) p[i] = s_p[from + r][wave * I + i];
+        for (uint32_t j = 0; j < 4; ++j) {
+            const double c = (double)(int8_t)(q[r] >> (8u * j));
 #pragma unroll
-            for (uint32_t j = 0; j < 4; ++j) {
-                const double c = (double)(int8_t)(now[r] >> (8u * j));
-#pragma unroll
-                for (uint32_t i = 0; i < I; ++i) acc[i][j] = fma(p[i], c, acc[i][j]);
-            }
+            for (uint32_t i = 0; i < I; ++i) acc[i][j] = fma(p[i], c, acc[i][j]);
         }
     }
     if (!there) return;
@@ -862,19 +951,24 @@ __global__ __launch_bounds__(BLOCK) void q8_gradient_small_kernel(Q8GradientArgs
     }
 }
 
-template <typename T, uint32_t I>
+template <typename T, uint32_t FA, uint32_t FB, uint32_t WAVES>
 static void launch_gradient_small_as(shifter_ctx* ctx, const Q8GradientArgs& g) {
-    const uint64_t blocks = (uint64_t)((g.n + 4u * I - 1u) / (4u * I)) * ((g.k + 255u) / 256u);
-    q8_gradient_small_kernel<T, I><<<(uint32_t)blocks, BLOCK, 0, ctx->stream>>>(g);
+    const uint64_t blocks = (uint64_t)((g.n + 16u * FA - 1u) / (16u * FA)) * ((g.k + 16u * FB - 1u) / (16u * FB));
+    q8_gradient_small_kernel<T, FA, FB, WAVES><<<(uint32_t)blocks, 64 * WAVES, 0, ctx->stream>>>(g);
 }
 template <typename T>
-static void launch_gradient_small(shifter_ctx* ctx, const Q8GradientArgs& g) {
+static void launch_gradient_small(shifter_ctx* ctx, const Q8GradientArgs& g, Q8GradientKernel kernel) {
     ProfileScope ps(ctx, K_Q8_GRADIENT);
-    // the fewer blocks there would be, the narrower they are: a compute unit each, as far as the columns go
-    const uint64_t sixteens = (uint64_t)((g.n + 15u) / 16u) * ((g.k + 255u) / 256u);
-    if (sixteens >= 256u) launch_gradient_small_as<T, 4>(ctx, g);
-    else if (sixteens >= 128u) launch_gradient_small_as<T, 2>(ctx, g);
-    else launch_gradient_small_as<T, 1>(ctx, g);
+    if (kernel == Q8_GRAD_WIDE) {
+        const uint64_t blocks = (uint64_t)((g.n + 15u) / 16u) * ((g.k + 255u) / 256u);
+        q8_gradient_wide_kernel<T><<<(uint32_t)blocks, BLOCK, 0, ctx->stream>>>(g);
+    } else if ((uint64_t)((g.n + 15u) / 16u) * ((g.k + 31u) / 32u) <= 1024u) {
+        // up to four narrow blocks a compute unit, then wider ones: us, narrow / wide, 64 x 512 x 512 3.3 / 3.7, 300 x 300 x 300
+        // 4.4 / 7.5, 64 x 1024 x 1024 7.6 / 6.7, 128 x 1024 x 1024 11.2 / 9.6
+        launch_gradient_small_as<T, 1, 2, 8>(ctx, g);
+    } else {
+        launch_gradient_small_as<T, 2, 2, 4>(ctx, g);
+    }
 }
 
 template <typename T, uint32_t THREADS>
@@ -939,10 +1033,10 @@ static void launch_gradient_as(shifter_ctx* ctx, const Q8GradientArgs& g, const 
 
 void launch_q8_gradient(shifter_ctx* ctx, int dtype, const Q8GradientArgs& g) {
     const Q8GradientPlan pl = q8_gradient_plan(g.m, g.n, g.k);
-    if (pl.kernel == Q8_GRAD_SMALL) {
-        if (dtype == SHIFTER_F32) launch_gradient_small<float>(ctx, g);
-        else if (dtype == SHIFTER_BF16) launch_gradient_small<__bf16>(ctx, g);
-        else launch_gradient_small<_Float16>(ctx, g);
+    if (pl.kernel < 0) {
+        if (dtype == SHIFTER_F32) launch_gradient_small<float>(ctx, g, pl.kernel);
+        else if (dtype == SHIFTER_BF16) launch_gradient_small<__bf16>(ctx, g, pl.kernel);
+        else launch_gradient_small<_Float16>(ctx, g, pl.kernel);
         return;
     }
     {

@@ -20,7 +20,7 @@ PRODUCT = {"few": [(1, 40, 8192), (16, 4096, 8200), (5, 100, 12289), (9, 64, 409
            "128x256": [(2048, 4096, 1025), (1999, 4090, 2100), (2040, 4096, 700), (4096, 4096, 513)],
            "256x256": [(4000, 4090, 1500), (4081, 3900, 1900)]}
 GRADIENT = {"64x64": [(700, 1500, 1000), (2047, 1500, 700), (1300, 1999, 900), (129, 4097, 1023)],
-            "64x64 deep": [(256, 2048, 512), (130, 1000, 1000), (3000, 500, 400), (20000, 60, 50), (1025, 513, 700)],
+            "64x64 deep": [(256, 2048, 512), (150, 1000, 1000), (3000, 500, 400), (20000, 60, 50), (1025, 513, 700)],
             "64x128": [(512, 4096, 1024), (300, 3000, 1500), (1500, 2000, 2049)],
             "64x128 deep": [(2048, 1873, 977), (1700, 1900, 1000), (2047, 1900, 1024)],
             "64x256": [(2048, 2048, 2048), (1800, 2000, 2047)],
@@ -82,8 +82,19 @@ def test_gradient_tiles(ops, m, n, k):
 @pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
 def test_digits(ops, m, dtype):
     """Digits of all rows at once by 256, 512 and 1024 threads, and in slices."""
-    check_gradient(ops, m, 250, 260, dtype, seed=m, gap=m % 3, shift=m % 2)
+    check_gradient(ops, m, 1060, 1010, dtype, seed=m, gap=m % 3, shift=m % 2)
     check_gradient(ops, m, 5, 300, dtype, seed=m)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("m,n,k", [(1, 1, 1), (3, 15, 17), (15, 16, 32), (16, 17, 33), (17, 33, 31), (63, 64, 1), (127, 1, 64), (128, 49, 50),
+                                   (129, 100, 100), (1000, 90, 70), (1024, 362, 361), (64, 1024, 1024), (40, 1500, 690), (5, 997, 1050),
+                                   (2, 1100, 1000), (16, 1030, 1025), (7, 4, 300000), (13, 300000, 4)])
+def test_little_work(ops, m, n, k, dtype):
+    """One launch in 64 bits: both widths of its blocks, and few rows of a large result."""
+    check_gradient(ops, m, n, k, dtype, seed=m + n + k)
+    check_gradient(ops, m, n, k, dtype, seed=m + n + k, mask=True, accumulate=True, gap=1 + m % 2, shift=1)
 
 
 @pytest.mark.gpu
@@ -95,8 +106,8 @@ def test_recorded_workspace():
         ops = Q8()
         gen = torch.Generator(device="cuda").manual_seed(5)
         rand = lambda *s: torch.randn(*s, generator=gen, device="cuda")
-        g, x = rand(700, 300), ops.quantize(rand(700, 200))
-        g2, x2 = rand(900, 310), ops.quantize(rand(900, 190))
+        g, x = rand(1700, 300), ops.quantize(rand(1700, 200))
+        g2, x2 = rand(1900, 310), ops.quantize(rand(1900, 190))
         want, want2 = ops.weight_grad(g, x), ops.weight_grad(g2, x2)
         graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(graph, stream=stream):
@@ -112,3 +123,11 @@ def test_recorded_workspace():
             torch.cuda.synchronize()
             assert torch.equal(recorded, want) and torch.equal(got2, want2)
         ops.close()
+
+
+@pytest.mark.gpu
+def test_no_rows_of_a_large_result(ops):
+    g, x = torch.zeros((0, 1100), device="cuda"), ops.quantize(torch.zeros((0, 1000), device="cuda"))
+    assert (ops.weight_grad(g, x) == 0).all()
+    old = torch.randn((1100, 1000), device="cuda")
+    assert torch.equal(ops.weight_grad(g, x, out=old.clone(), accumulate=True), old)
