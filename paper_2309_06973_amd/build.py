@@ -39,7 +39,7 @@ def _binding_commands():
                 *(a for h in headers for a in ("-isystem", h)), "-I", os.path.join(ROOT, "include"),
                 "-c", os.path.join(CSRC, "q8_bind.cpp"), "-o", obj]
     link = ["g++", "-shared", obj, "-L", PKG, "-lshifter", *("-L" + p for p in cpp_extension.library_paths()),
-            "-lc10", "-ltorch_cpu", "-ltorch_python", "-Wl,-rpath,$ORIGIN", "-Wl,--allow-shlib-undefined", "-o", BINDING]
+            "-lc10", "-ltorch_cpu", "-ltorch_hip", "-ltorch_python", "-Wl,-rpath,$ORIGIN", "-Wl,--allow-shlib-undefined", "-o", BINDING]
     return compile_, link
 
 

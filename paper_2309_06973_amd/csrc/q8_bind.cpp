@@ -7,6 +7,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/hip/EmptyTensor.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -95,8 +96,13 @@ const float* vector_of(const Handle& h, PyObject* o, uint64_t n, const char* wha
     return static_cast<const float*>(v.data_ptr());
 }
 
+// A new tensor straight from the device's allocator (at::empty finds its way there in 0.3 us more).
+at::Tensor new_tensor(const Handle& h, at::IntArrayRef sizes, at::ScalarType t) {
+    return at::Tensor(at::detail::empty_cuda(sizes, t, c10::Device(c10::DeviceType::CUDA, h.device), std::nullopt));
+}
+
 at::Tensor new_rows(const Handle& h, uint64_t rows, uint64_t cols, at::ScalarType t) {
-    return at::empty({(int64_t)rows, (int64_t)cols}, at::TensorOptions().dtype(t).device(c10::DeviceType::CUDA, h.device));
+    return new_tensor(h, {(int64_t)rows, (int64_t)cols}, t);
 }
 
 // An 8-bit matrix as the C ABI takes it.
@@ -138,7 +144,7 @@ PyObject* new_codes(const Handle& h, uint64_t rows, uint64_t cols, Codes& m) {
     m.cols = cols;
     m.ld = (cols + 15u) / 16u * 16u;
     const int64_t bytes = (int64_t)(rows * m.ld);
-    at::Tensor q = at::empty({bytes + 4 * (int64_t)rows}, at::TensorOptions().dtype(at::kChar).device(c10::DeviceType::CUDA, h.device));
+    at::Tensor q = new_tensor(h, {bytes + 4 * (int64_t)rows}, at::kChar);
     at::Tensor scale = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(q.storage()), q.key_set(), caffe2::TypeMeta::Make<float>());
     scale.unsafeGetTensorImpl()->set_storage_offset(bytes / 4);
     scale.unsafeGetTensorImpl()->set_sizes_contiguous({(int64_t)rows});
