@@ -1,8 +1,8 @@
 // The 8-bit operators from Python: checks of tensors, new results and the call into the C ABI.
 //
 // A call's kernel takes a few microseconds, as much as a handful of calls into torch from Python:
-// 1 x 2048 bf16, us a call with all this in Python and ctypes / here: quantise 7.7 / 4.9, read back 6.4 / 4.3, norm
-// with residual 11.0 / 5.2, of which a launch is 2.7.  No stream is looked up here: the handle has asked torch for it.
+// 1 x 2048 bf16, us a call with all this in Python and ctypes / here: quantise 7.7 / 4.0, read back 6.4 / 4.0, norm
+// with residual 11.0 / 4.8, of which a launch is 3.2.  No stream is looked up here: the handle has asked torch for it.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 

@@ -2,14 +2,15 @@
 //
 // The product   c = sa sb (A B') + bias    of two 8-bit matrices, and the weight gradient
 // dW = (g s)' Q from an 8-bit checkpoint Q.  Both are sums over the bytes of two rows that
-// lie side by side in memory, exact in 32-bit integers, so no result depends on how the work
-// is split; they share one tiled loop.
+// lie side by side in memory, exact in 32-bit integers, so a product's result does not depend on how the
+// work is split (a gradient's rows split into parts round once a part); they share one tiled loop.
 //
 // The gradient's other factor is p = g s in fp32.  Per column it is brought to 24-bit whole
 // numbers v (the column's largest |p| becomes 8355711 = 127 (2^16 + 2^8 + 1)), and those to three
 // balanced digits, v = d2 2^16 + d1 2^8 + d0, digits from -128 to 127.  Three integer products
 // with the same Q give the sum to fp32 accuracy at 1.5 times the cost of one bf16 product (the
-// matrix units take 8-bit integers twice as fast), where fp32 products run at a sixteenth.
+// matrix units take 8-bit integers twice as fast), where fp32 products run at a sixteenth.  Where there
+// is little work, 64-bit products in one launch are faster than the two that digits need.
 #include <algorithm>
 #include <type_traits>
 
