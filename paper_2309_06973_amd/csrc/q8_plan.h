@@ -53,9 +53,9 @@ inline const char* q8_bad_codes(const void* q, const void* scale, uint64_t rows,
     return nullptr;
 }
 
-// The product's kernels.  Tiles of rows x columns, a block each; Q8_FEW: no tiles, the weights are read straight into
-// registers by blocks of 16 columns and all rows.
-enum Q8Kernel { Q8_FEW, Q8_TILE_64x64, Q8_TILE_64x128, Q8_TILE_128x128, Q8_TILE_128x256, Q8_TILE_256x256, Q8_KERNELS };
+// The product's kernels.  Tiles of rows x columns, a block each; Q8_FEW and Q8_GROUPS: no tiles, both factors are read straight
+// into registers by blocks of 16 columns and all of a few rows, or groups of them.
+enum Q8Kernel { Q8_FEW, Q8_GROUPS, Q8_TILE_64x64, Q8_TILE_64x128, Q8_TILE_128x128, Q8_TILE_128x256, Q8_TILE_256x256, Q8_KERNELS };
 struct Q8TileCost {
     uint32_t rows, cols;
     // us: a launch and a tile's ends; then a stage of 128 bytes: a tile alone on the chip, one on each compute unit, and, where
@@ -101,8 +101,20 @@ inline double q8_tile_us(const Q8TileCost& c, uint64_t m, uint64_t n, uint64_t k
 // 32 x 8192 x 8192 24.1 / 16.8, 64 x 4096 x 4096 12.2 / 10.1).
 constexpr uint64_t Q8_FEW_ROWS = 16, Q8_FEW_ROWS_MOST = 48, Q8_FEW_WEIGHTS = 1ull << 24;
 
+// Few results go the same way whatever their rows, in groups of 16 F rows, F as small as leaves a block a compute unit, or 3.  us,
+// with F = 1, 2 and 3 / 64 x 64 tiles: 100 x 500 x 8000 7.2 9.4 11.7 / 16.4 (224 blocks with F = 1), 128 x 256 x 4096 5.5 7.4 9.2 / 9.7,
+// 64 x 1024 x 1024 3.1 3.6 4.1 / 4.7, 500 x 300 x 2000 5.4 6.0 4.4 / 6.5 (209 blocks with F = 3), 2000 x 64 x 4000 7.0 5.9 7.2 / 9.5 (252
+// with F = 2); beyond a block a unit, 512 x 512 x 4096 16.2 13.7 17.4 / 9.7.
+inline uint64_t q8_group_blocks(uint64_t m, uint64_t n, uint64_t f) { return (n + 15u) / 16u * ((m + 16u * f - 1u) / (16u * f)); }
+inline uint32_t q8_group(uint64_t m, uint64_t n) {
+    for (uint32_t f = 1; f < 3; ++f)
+        if (m <= 16u * f || q8_group_blocks(m, n, f) <= (uint64_t)Q8_UNITS) return f;
+    return 3;
+}
+
 inline Q8Kernel q8_kernel_for(uint64_t m, uint64_t n, uint64_t k) {
     if (m <= Q8_FEW_ROWS || (m <= Q8_FEW_ROWS_MOST && n * k <= Q8_FEW_WEIGHTS)) return Q8_FEW;
+    if (q8_group_blocks(m, n, 3) <= (uint64_t)Q8_UNITS) return Q8_GROUPS;
     int best = 0;
     for (int i = 1; i < Q8_TILES_N; ++i)
         if (q8_tile_us(Q8_TILES[i], m, n, k) < q8_tile_us(Q8_TILES[best], m, n, k)) best = i;

@@ -294,8 +294,8 @@ static void launch_product_as(shifter_ctx* ctx, const Q8ProductArgs& g) {
     q8_product_kernel<T, WA, WB, FA, FB, NS, STEP, GROUP><<<(uint32_t)tiles, Tl::THREADS, 0, ctx->stream>>>(g);
 }
 
-// Few tokens: the weights are read once, straight into registers, and that read is the time.  A block has 16
-// columns of the result and all of the up to 16 F tokens; its WAVES wavefronts take pieces of 128 bytes of the
+// Few tokens, or few results: the weights are read once (by each group of tokens), straight into registers, and that read is the
+// time.  A block has 16 columns of the result and 16 F tokens; its WAVES wavefronts take pieces of 128 bytes of the
 // rows in turn and join their sums in LDS.  (Weights are the first factor of the 16 x 16 x 64 products: a
 // lane then holds four neighbouring columns of one token.)  1 x 4096 x 4096 takes 5.3 us, 6.3 with the weights in no cache, of
 // which 3.4 are their 16.8 MB at a large copy's rate, 5.0 TB/s; 1 x 8192 x 8192 14.6 us, 4.6 TB/s; 48 x 3277 x 3541 7.6 and 9.6 us.
@@ -305,16 +305,16 @@ __global__ __launch_bounds__(64 * WAVES) void q8_product_few_kernel(Q8ProductArg
     constexpr uint32_t PIECE = 128, DEPTH = 4;                           // bytes; pieces under way
     __shared__ v4i s_sum[WAVES][F][64];
     const uint32_t lane = threadIdx.x & 63u, wave = uniform_u32(threadIdx.x >> 6);
-    const uint32_t n0 = blockIdx.x * 16u, at = lane / 16u * UNIT;
+    const uint32_t n0 = blockIdx.x * 16u, m0 = blockIdx.y * 16u * F, at = lane / 16u * UNIT;
     const int8_t* b = g.b + (uint64_t)min(n0 + (lane & 15u), g.n - 1u) * g.ld_b;
     const int8_t* a[F];
 #pragma unroll
-    for (uint32_t f = 0; f < F; ++f) a[f] = g.a + (uint64_t)min(16u * f + (lane & 15u), g.m - 1u) * g.ld_a;
+    for (uint32_t f = 0; f < F; ++f) a[f] = g.a + (uint64_t)min(m0 + 16u * f + (lane & 15u), g.m - 1u) * g.ld_a;
     v4i acc[F];
 #pragma unroll
     for (uint32_t f = 0; f < F; ++f) acc[f] = v4i{0, 0, 0, 0};
     // what the sums are finished with is on its way while they are made
-    const uint32_t m = wave * 16u + (lane & 15u), n = n0 + lane / 16u * 4u;
+    const uint32_t m = m0 + wave * 16u + (lane & 15u), n = n0 + lane / 16u * 4u;
     float sa = 0.0f, sb[4], bias[4];
     if (wave < F) {
         sa = g.sa[min(m, g.m - 1u)];
@@ -385,20 +385,23 @@ __global__ __launch_bounds__(64 * WAVES) void q8_product_few_kernel(Q8ProductArg
 
 template <typename T, uint32_t F, uint32_t WAVES>
 static void launch_product_few(shifter_ctx* ctx, const Q8ProductArgs& g) {
-    q8_product_few_kernel<T, F, WAVES><<<(g.n + 15u) / 16u, 64 * WAVES, 0, ctx->stream>>>(g);
+    q8_product_few_kernel<T, F, WAVES><<<dim3((g.n + 15u) / 16u, (g.m + 16u * F - 1u) / (16u * F)), 64 * WAVES, 0, ctx->stream>>>(g);
 }
 
 template <typename T>
 static void launch_product_of(shifter_ctx* ctx, const Q8ProductArgs& g) {
     switch (q8_kernel_for(g.m, g.n, g.k)) {
         case Q8_FEW:
+        case Q8_GROUPS: {
+            const uint32_t f = q8_group(g.m, g.n);
             // long rows and a block a compute unit: more wavefronts (1 x 4096 x 14336 14.1 -> 13.6 us, 8 x 1024 x 16384 15.6 -> 14.5;
             // but 1 x 8192 x 4200 9.0 -> 10.0, 16 x 8192 x 8192 20.1 -> 20.5)
-            if (g.m <= 16 && g.k >= 8192 && g.n <= 4096) launch_product_few<T, 1, 16>(ctx, g);
-            else if (g.m <= 16) launch_product_few<T, 1, 8>(ctx, g);
-            else if (g.m <= 32) launch_product_few<T, 2, 16>(ctx, g);
+            if (f == 1 && g.k >= 8192 && q8_group_blocks(g.m, g.n, 1) <= 256u) launch_product_few<T, 1, 16>(ctx, g);
+            else if (f == 1) launch_product_few<T, 1, 8>(ctx, g);
+            else if (f == 2) launch_product_few<T, 2, 16>(ctx, g);
             else launch_product_few<T, 3, 16>(ctx, g);
             break;
+        }
         case Q8_TILE_64x64: launch_product_as<T, 2, 2, 1, 1, 4, 128, 16>(ctx, g); break;
         case Q8_TILE_64x128: launch_product_as<T, 2, 4, 1, 1, 3, 128, 8>(ctx, g); break;
         case Q8_TILE_128x128: launch_product_as<T, 2, 4, 2, 1, 3, 128, 8>(ctx, g); break;

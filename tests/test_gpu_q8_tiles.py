@@ -14,7 +14,9 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 PRODUCT = {"few": [(1, 40, 8192), (16, 4096, 8200), (5, 100, 12289), (9, 64, 4095), (16, 33, 3000), (1, 20, 1025), (1, 20, 2049),
                    (1, 20, 3100), (17, 300, 2049), (30, 70, 4097), (48, 129, 3541), (40, 16, 6145)],
-           "64x64": [(100, 500, 127), (128, 640, 512), (65, 257, 513), (300, 129, 640)],
+           "groups": [(100, 500, 8200), (128, 640, 512), (65, 257, 513), (300, 129, 640), (500, 300, 2000), (2000, 64, 4001), (12000, 16, 100),
+                      (49, 1000, 127), (50, 2040, 1), (4000, 33, 260), (5000, 17, 9000)],
+           "64x64": [(256, 1024, 127), (300, 1000, 640), (257, 1023, 513), (512, 640, 385)],
            "64x128": [(512, 4096, 384), (512, 4096, 385), (777, 2900, 400), (640, 3500, 130), (1000, 2500, 513)],
            "128x128": [(2000, 1990, 1300), (1100, 3541, 2100), (1024, 4096, 1500)],
            "128x256": [(2048, 4096, 1025), (1999, 4090, 2100), (2040, 4096, 700), (4096, 4096, 513)],
@@ -69,6 +71,19 @@ def ops():
 @pytest.mark.parametrize("m,n,k", [s for v in PRODUCT.values() for s in v])
 def test_product_tiles(ops, m, n, k):
     check_product(ops, m, n, k, "bf16", seed=m + n + k, bias=True, ends=k % 2 == 1)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("k", [0, 1, 3, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 256, 257, 500, 1000])
+def test_product_tile_sums(ops, k):
+    check_product(ops, 300 + k % 7, 1000 + k % 5, k, "fp32", seed=k, bias=True, relu=k % 2 == 0, gap=k % 3, extra=16 * (k % 2))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("e", [0, 1, 15, 16, 17, 31, 33, 63])
+def test_product_tile_edges(ops, e):
+    check_product(ops, 320 + e, 960 + e, 200, "bf16", seed=e, gap=e % 3)
+    check_product(ops, 513 - e, 2049 - e, 130, "fp16", seed=e, bias=True)
 
 
 @pytest.mark.gpu
