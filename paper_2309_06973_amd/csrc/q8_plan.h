@@ -73,7 +73,7 @@ struct Q8TileCost {
 //    2048 x 2048 x 2048    16.9     13.4     12.8     16.2     24.8
 //    4096 x 1024 x 8192    53.0     43.7     37.7     45.5     73.4
 //    16384 x 100 x 2048     9.4      9.1     11.4     16.8     26.4
-// The costs below say these within 15 %; the kernel of the least cost is taken.
+// The costs below say these within 20 %; the kernel of the least cost is taken.
 constexpr int Q8_TILES_N = 5;
 constexpr Q8TileCost Q8_TILES[Q8_TILES_N] = {{64, 64, 3.2, 0.21, 0.235, 0.20},
                                              {64, 128, 3.2, 0.265, 0.36, 0.325},
@@ -154,9 +154,9 @@ constexpr Q8TileCost Q8_GRAD_TILES[] = {{64, 64, 3.5, 0.57, 0.62, 0.43},
 // which costs that and the traffic.
 constexpr uint64_t Q8_PARTS = 32;
 // Little work, and few rows of whatever size, go to one launch.  us, that / digits and tiles: 64 x 512 x 512 3.3 / 9.3, 300 x 300 x 300
-// 4.4 / 9.5, 500 x 250 x 333 6.0 / 12, 1000 x 100 x 200 9.1 / 12, 128 x 1024 x 1024 9.6 / 9.6, 64 x 1400 x 1400 11.8 / 11.6,
-// 256 x 1024 x 1024 14.5 / 11.5; 16 x 4096 x 4096 24.8 / 27.8 (1 x 4096 x 4096 15.5).
-constexpr uint64_t Q8_SMALL_ROWS = 1024, Q8_SMALL_RESULTS = 1ull << 20, Q8_SMALL_WORK = 1ull << 27, Q8_WIDE_ROWS = 16;
+// 4.4 / 9.5, 500 x 250 x 333 5.8 / 12, 1000 x 100 x 200 7.1 / 14, 2000 x 250 x 260 16 / 21, 128 x 1024 x 1024
+// 9.6 / 9.6, 64 x 1400 x 1400 11.8 / 11.6, 256 x 1024 x 1024 14.5 / 11.5; 16 x 4096 x 4096 24.8 / 27.8 (1 x 4096 x 4096 15.5).
+constexpr uint64_t Q8_SMALL_ROWS = 2048, Q8_SMALL_RESULTS = 1ull << 20, Q8_SMALL_WORK = 1ull << 27, Q8_WIDE_ROWS = 16;
 constexpr bool q8_small(uint64_t m, uint64_t n, uint64_t k) {
     return m <= Q8_SMALL_ROWS && n * k <= Q8_SMALL_RESULTS && m * n * k <= Q8_SMALL_WORK;
 }

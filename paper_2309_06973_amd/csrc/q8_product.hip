@@ -793,7 +793,8 @@ typedef double v4d __attribute__((ext_vector_type(4)));
 // an operand serves 16 of them), in which a p times a code is exact.  A block has 16 FA columns of g and 16 FB of the
 // checkpoint; its WAVES wavefronts take 16 rows in turn, read straight into registers, the next ones on their way while these
 // are multiplied, and join their sums in LDS.  64 x 512 x 512 takes 3.3 us, little more than a launch; 300 x 300 x 300 4.4,
-// 512 x 512 x 512 9.5, where eight turns of 0.8 us, as long as a trip to memory, follow one another.
+// 512 x 512 x 512 9.5,
+// where the matrix units' rate and the conversions bound it: as fast with 32 rows a turn.
 template <typename T, uint32_t FA, uint32_t FB, uint32_t WAVES>
 __global__ __launch_bounds__(64 * WAVES) void q8_gradient_small_kernel(Q8GradientArgs a) {
     constexpr uint32_t ROWS = 16, STEPS = ROWS / 4;                      // of a turn; four rows a step
@@ -966,9 +967,12 @@ static void launch_gradient_small(shifter_ctx* ctx, const Q8GradientArgs& g, Q8G
     if (kernel == Q8_GRAD_WIDE) {
         const uint64_t blocks = (uint64_t)((g.n + 15u) / 16u) * ((g.k + 255u) / 256u);
         q8_gradient_wide_kernel<T><<<(uint32_t)blocks, BLOCK, 0, ctx->stream>>>(g);
+    } else if ((uint64_t)((g.n + 15u) / 16u) * ((g.k + 15u) / 16u) <= 256u) {
+        // a narrowest block a compute unit, up to four narrow ones, then wider ones: us with 16 x 16, 16 x 32 and 32 x 32 results,
+        // 1000 x 100 x 200 7.1 8.9 19, 2000 x 250 x 260 20 16 35, 64 x 512 x 512 3.6 3.4 3.7, 300 x 300 x 300 5.0 4.5 7.5,
+        // 64 x 1024 x 1024 9.1 7.1 6.5, 128 x 1024 x 1024 13 11 9.2
+        launch_gradient_small_as<T, 1, 1, 8>(ctx, g);
     } else if ((uint64_t)((g.n + 15u) / 16u) * ((g.k + 31u) / 32u) <= 1024u) {
-        // up to four narrow blocks a compute unit, then wider ones: us, narrow / wide, 64 x 512 x 512 3.3 / 3.7, 300 x 300 x 300
-        // 4.4 / 7.5, 64 x 1024 x 1024 7.6 / 6.7, 128 x 1024 x 1024 11.2 / 9.6
         launch_gradient_small_as<T, 1, 2, 8>(ctx, g);
     } else {
         launch_gradient_small_as<T, 2, 2, 4>(ctx, g);

@@ -256,7 +256,7 @@ def test_refusals(ops):
                dict(out=torch.zeros((4, 7), device=DEV)), dict(out=torch.zeros((6, 4), device=DEV).t())):
         with pytest.raises(ValueError):
             ops.matmul(a, b, **kw)
-    tall, _, _ = matrix(1300, 40, 3)
+    tall, _, _ = matrix(2300, 40, 3)
     g = torch.zeros((4, 6), device=DEV)
     for kw in (dict(mask=torch.zeros((6, 39), dtype=torch.uint8, device=DEV)), dict(mask=torch.zeros((6, 40), device=DEV)),
                dict(mask=torch.zeros((6, 40), dtype=torch.uint8)), dict(accumulate=True),
@@ -278,7 +278,7 @@ def test_refusals(ops):
     d = torch.zeros((6, 40), device=DEV)
     for w, n, what in ((work, 100, "too small"), (None, 1 << 20, "256"), (work[1:], 1 << 19, "256")):
         with pytest.raises(S.ShifterError) as e:
-            S.shifter_weight_grad_q8(ops.ctx, torch.zeros((1300, 6), device=DEV), 0, 6, tall.q, 48, tall.scale, 1300, 6, 40,
+            S.shifter_weight_grad_q8(ops.ctx, torch.zeros((2300, 6), device=DEV), 0, 6, tall.q, 48, tall.scale, 2300, 6, 40,
                                      None, 0, 0, d, 40, w, n)
         assert e.value.code == S.SHIFTER_ERR_INVALID_ARG and what in str(e.value)
 

@@ -104,7 +104,7 @@ def test_digits(ops, m, dtype):
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
 @pytest.mark.parametrize("m,n,k", [(1, 1, 1), (3, 15, 17), (15, 16, 32), (16, 17, 33), (17, 33, 31), (63, 64, 1), (127, 1, 64), (128, 49, 50),
-                                   (129, 100, 100), (1000, 90, 70), (1024, 362, 361), (64, 1024, 1024), (40, 1500, 690), (5, 997, 1050),
+                                   (129, 100, 100), (1000, 90, 70), (1024, 362, 361), (2048, 256, 255), (2047, 257, 250), (300, 256, 256), (300, 257, 256), (64, 1024, 1024), (40, 1500, 690), (5, 997, 1050),
                                    (2, 1100, 1000), (16, 1030, 1025), (7, 4, 300000), (13, 300000, 4)])
 def test_little_work(ops, m, n, k, dtype):
     """One launch in 64 bits: both widths of its blocks, and few rows of a large result."""
@@ -121,8 +121,8 @@ def test_recorded_workspace():
         ops = Q8()
         gen = torch.Generator(device="cuda").manual_seed(5)
         rand = lambda *s: torch.randn(*s, generator=gen, device="cuda")
-        g, x = rand(1700, 300), ops.quantize(rand(1700, 200))
-        g2, x2 = rand(1900, 310), ops.quantize(rand(1900, 190))
+        g, x = rand(2700, 300), ops.quantize(rand(2700, 200))
+        g2, x2 = rand(2900, 310), ops.quantize(rand(2900, 190))
         want, want2 = ops.weight_grad(g, x), ops.weight_grad(g2, x2)
         graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(graph, stream=stream):

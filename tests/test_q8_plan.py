@@ -70,7 +70,7 @@ int main() {
         for (uint64_t n : ns)
             for (uint64_t k : ns) {
                 const Q8GradientPlan g = q8_gradient_plan(m, n, k);
-                const bool is_small = m <= 16 || (m <= 1024 && n * k <= 1ull << 20 && m * n * k <= 1ull << 27);
+                const bool is_small = m <= 16 || (m <= 2048 && n * k <= 1ull << 20 && m * n * k <= 1ull << 27);
                 if ((g.kernel < 0) != is_small || (is_small && g.bytes != 0)) { printf("small %llu %llu %llu\n", (unsigned long long)m, (unsigned long long)n, (unsigned long long)k); ++bad; }
                 if (is_small) continue;
                 bool ok = m > 0 && g.ld >= m && g.ld < m + 128 && g.ld % 128 == 0 && g.slices <= Q8_SLICES && g.slice_rows % Q8_SLICE_ROWS == 0;
@@ -115,7 +115,7 @@ def test_checks_and_plan(tmp_path):
 def test_layout_call_and_calls_without_a_context():
     assert S.shifter_weight_grad_q8_layout(0, 5, 5) == 0
     assert S.shifter_weight_grad_q8_layout(16, 5000, 7000) == S.shifter_weight_grad_q8_layout(60, 50, 70) == 0
-    assert S.shifter_weight_grad_q8_layout(1100, 5, 7) >= 1152 * (3 * 5 + 7)
+    assert S.shifter_weight_grad_q8_layout(2100, 5, 7) >= 2176 * (3 * 5 + 7)
     with pytest.raises(S.ShifterError) as e:
         S.shifter_weight_grad_q8_layout(S.SHIFTER_Q8_MAX_SUM + 1, 5, 5)
     assert e.value.code == S.SHIFTER_ERR_CAPACITY
