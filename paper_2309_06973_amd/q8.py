@@ -12,6 +12,7 @@ import os
 from typing import Optional
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import shifter as S
 
@@ -136,6 +137,7 @@ class _Linear(torch.autograd.Function):
         return x @ weight.t()
 
     @staticmethod
+    @once_differentiable                   # weight_grad's result has no graph
     def backward(ctx, g):
         q, scale, weight, *mask = ctx.saved_tensors
         g = g if g.dim() == 2 and (g.shape[1] < 2 or g.stride(1) == 1) and (g.shape[0] < 2 or g.stride(0) >= g.shape[1]) \
@@ -150,5 +152,6 @@ class _Linear(torch.autograd.Function):
 def checkpointed_linear(x: torch.Tensor, weight: torch.Tensor, ops: Q8, mask: Optional[torch.Tensor] = None):
     """x times weight transposed, keeping x for the backward pass in 8 bits (a quarter of its fp32
     size): the product and x's gradient are torch's, the weights' gradient comes from the 8-bit
-    rows.  mask: uint8 [out, in], weights that were pruned get no gradient."""
+    rows.  mask: uint8 [out, in], weights that were pruned get no gradient.  Second derivatives are
+    an error."""
     return _Linear.apply(x, weight, ops, mask)
