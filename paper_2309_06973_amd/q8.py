@@ -12,7 +12,6 @@ import os
 from typing import Optional
 
 import torch
-from torch.autograd.function import once_differentiable
 
 from . import shifter as S
 
@@ -128,30 +127,45 @@ class Q8:
         return self._calls.weight_grad(*self._enter(), g, x, mask, torch.float32, out, accumulate, self._room)
 
 
+class _WeightGrad(torch.autograd.Function):
+    """weight_grad where it may be differentiated again: an error then.  `link` ties the result to the layer, so
+    that the way from it to the layer's operands leads through here."""
+    @staticmethod
+    def forward(ctx, g, link, ops, x, mask):
+        return ops.weight_grad(g, x, mask=mask)
+
+    @staticmethod
+    def backward(ctx, v):
+        raise RuntimeError("checkpointed_linear: the weights' gradient has no derivative of its own")
+
+
 class _Linear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, ops, mask):
         kept = ops.quantize(x)
-        ctx.save_for_backward(kept.q, kept.scale, weight, *(() if mask is None else (mask,)))
+        link = x.new_empty(0)
+        ctx.save_for_backward(kept.q, kept.scale, weight, link, *(() if mask is None else (mask,)))
         ctx.ops, ctx.cols = ops, kept.cols
-        return x @ weight.t()
+        ctx.set_materialize_grads(False)
+        return x @ weight.t(), link
 
     @staticmethod
-    @once_differentiable                   # weight_grad's result has no graph
-    def backward(ctx, g):
-        q, scale, weight, *mask = ctx.saved_tensors
+    def backward(ctx, g, _):
+        if g is None:
+            return None, None, None, None
+        q, scale, weight, link, *mask = ctx.saved_tensors
         g = g if g.dim() == 2 and (g.shape[1] < 2 or g.stride(1) == 1) and (g.shape[0] < 2 or g.stride(0) >= g.shape[1]) \
             else g.contiguous()
         dx = g @ weight if ctx.needs_input_grad[0] else None
         dw = None
         if ctx.needs_input_grad[1]:
-            dw = ctx.ops.weight_grad(g, Q8Matrix(q, scale, ctx.cols), mask=mask[0] if mask else None).to(weight.dtype)
+            dw = _WeightGrad.apply(g, link, ctx.ops, Q8Matrix(q, scale, ctx.cols), mask[0] if mask else None).to(weight.dtype)
         return dx, dw, None, None
 
 
 def checkpointed_linear(x: torch.Tensor, weight: torch.Tensor, ops: Q8, mask: Optional[torch.Tensor] = None):
     """x times weight transposed, keeping x for the backward pass in 8 bits (a quarter of its fp32
     size): the product and x's gradient are torch's, the weights' gradient comes from the 8-bit
-    rows.  mask: uint8 [out, in], weights that were pruned get no gradient.  Second derivatives are
-    an error."""
-    return _Linear.apply(x, weight, ops, mask)
+    rows.  mask: uint8 [out, in], weights that were pruned get no gradient.  The
+    weights' gradient can not be differentiated again, which is an error; x's can."""
+    return _Linear.apply(x, weight, ops, mask)[0]

@@ -29,14 +29,46 @@ def operands(m, n, k, seed=0, **kw):
     return [torch.randn(*s, generator=g).to(**kw).requires_grad_() for s in ((m, k), (n, k))]
 
 
-def test_second_derivatives_are_refused():
+def gradients(x, w, layer, loss):
+    return torch.autograd.grad(loss(layer(x, w)), (x, w), create_graph=True)
+
+
+def ours(x, w):
+    return checkpointed_linear(x, w, OPS)
+
+
+LOSSES = {"square": lambda y: y.square().sum(), "linear": lambda y: y.sum()}
+
+
+@pytest.mark.parametrize("loss", LOSSES)
+@pytest.mark.parametrize("beside", [False, True])
+def test_second_derivatives_of_the_weights_gradient_are_refused(loss, beside):
     """A penalty on the gradients: those of the weights have no derivative of their own, which is an error and not a
-    term left out in silence."""
+    term left out in silence, also where the penalty reaches the operands on other ways."""
     x, w = operands(6, 5, 4)
-    dx, dw = torch.autograd.grad(checkpointed_linear(x, w, OPS).square().sum(), (x, w), create_graph=True)
-    with pytest.raises(RuntimeError, match="once_differentiable"):
-        torch.autograd.grad(dx.square().sum() + dw.square().sum(), (x, w))
-    # first derivatives do not mind the graph
-    x2, w2 = (t.detach().requires_grad_() for t in (x, w))
-    for a, b in zip((dx, dw), torch.autograd.grad(checkpointed_linear(x2, w2, OPS).square().sum(), (x2, w2))):
+    dx, dw = gradients(x, w, ours, LOSSES[loss])
+    penalty = dx.square().sum() + dw.square().sum() + (LOSSES[loss](x @ w.t()) if beside else 0.0)
+    for inputs in ((x,), (w,), (x, w)):
+        with pytest.raises(RuntimeError, match="no derivative of its own"):
+            torch.autograd.grad(penalty, inputs, retain_graph=True, allow_unused=True)
+    with pytest.raises(RuntimeError, match="no derivative of its own"):
+        penalty.backward()
+
+
+@pytest.mark.parametrize("loss", LOSSES)
+def test_second_derivatives_of_the_inputs_gradient(loss):
+    """They are torch's, but for what goes on to the weights, from the 8-bit input: half a code of each row off at most.
+    First derivatives do not mind the graph."""
+    x, w = operands(6, 5, 4)
+    dx, dw = gradients(x, w, ours, LOSSES[loss])
+    plain = gradients(x, w, lambda x, w: x @ w.t(), LOSSES[loss])
+    got, want = (torch.autograd.grad(d.square().sum(), (x, w), allow_unused=True) for d in (dx, plain[0]))
+    for a, b in zip(got[:1], want[:1]):
+        assert (a is None or not a.any()) if b is None else torch.equal(a, b)
+    scale = OPS.quantize(x.detach()).scale[:, None]
+    # the way through y in the square's case: y's gradient is 2 y, dx is 2 y w, the penalty's with respect to y 4 dx w'
+    off = ((4.0 * dx.detach() @ w.detach().t()).abs().t() @ (0.5 * scale).expand(6, 4)) if loss == "square" else 0.0
+    assert ((got[1] - want[1]).abs() <= off + 32 * Q.U32 * want[1].abs().max()).all()
+    for a, b in zip((dx, dw), torch.autograd.grad(LOSSES[loss](ours(x, w)), (x, w))):
         assert torch.equal(a, b)
+    assert torch.equal(dx, plain[0])
