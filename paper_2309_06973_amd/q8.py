@@ -1,8 +1,8 @@
 """8-bit matrices next to the prune-and-compact pass: a rebuilt variant's linear layers served
 in 8 bits, and 8-bit activations kept for the backward pass while a masked network trains on.
 
-Every step runs in libshifter's HIP kernels on the stream that was current when the handle was
-made; a call's checks, its new tensors and the way into the C ABI are _q8.so's (csrc/q8_bind.cpp).
+Every step runs in libshifter's HIP kernels on the stream that was current when the handle (or
+the context that it was given) was made; a call's checks, its new tensors and the way into the C ABI are _q8.so's (csrc/q8_bind.cpp).
 Raises if no ROCm device is visible."""
 from __future__ import annotations
 
@@ -59,8 +59,9 @@ def load_calls():
 
 
 class Q8:
-    """The 8-bit operators on one device and stream.  Matrices of elements are two-dimensional
-    fp32, bf16 or fp16 tensors whose columns lie side by side; their rows may have any stride.
+    """The 8-bit operators on one device and stream: the current one, or those of a given context.
+    Matrices of elements are two-dimensional fp32, bf16 or fp16 tensors whose columns lie side by
+    side; their rows may have any stride.
     Results are new tensors unless ``out`` (or ``h``) says where they go.  Recorded into a graph,
     calls of one handle share a workspace apart from that of calls made at once: replays of such graphs
     go one after another, on whatever stream."""
@@ -68,11 +69,13 @@ class Q8:
     def __init__(self, device: int = 0, ctx=None):
         if not torch.cuda.is_available():
             raise RuntimeError("no ROCm device visible: the 8-bit operators have no CPU path")
+        if ctx is not None and ctx.device != device:
+            raise ValueError(f"the context's device is {ctx.device}, not {device}")
         self.dev = torch.device("cuda", device)
         torch.cuda.set_device(self.dev)
-        self.stream = torch.cuda.current_stream(self.dev).cuda_stream
         self.own = ctx is None
-        self.ctx = ctx or S.shifter_create(device, self.stream)
+        self.ctx = ctx or S.shifter_create(device, torch.cuda.current_stream(self.dev).cuda_stream)
+        self.stream = self.ctx.stream
         self.work = None
         self.recorded = []                 # workspaces of recorded calls, which use them at every replay
         self._calls = load_calls()
@@ -85,7 +88,7 @@ class Q8:
     def _enter(self):
         """New tensors belong to torch's current stream; the kernels run on the handle's."""
         if _raw_stream(self.dev.index) != self.stream:
-            raise RuntimeError("this handle runs on the stream it was made on: make one under the other stream")
+            raise RuntimeError("this handle runs on the stream it (or its context) was made on: make one under the other stream")
         return self.ctx.handle.value, self.dev.index
 
     def _room(self, need: int) -> torch.Tensor:

@@ -220,8 +220,9 @@ def _ptr(t) -> Optional[int]:
 
 # --------------------------------------------------------------------------- objects
 class Context:
-    def __init__(self, handle):
+    def __init__(self, handle, device: int = 0, stream: int = 0):
         self.handle = handle
+        self.device, self.stream = device, stream      # what its kernels run on
 
 
 class Model:
@@ -236,7 +237,7 @@ class Model:
 def shifter_create(device: int = 0, hip_stream: int = 0) -> Context:
     h = C.c_void_p()
     _check(load_library().shifter_create(C.byref(h), device, C.c_void_p(hip_stream or None)))
-    return Context(h)
+    return Context(h, device, hip_stream or 0)
 
 
 def shifter_destroy(ctx: Context) -> None:
