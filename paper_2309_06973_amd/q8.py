@@ -159,7 +159,8 @@ class _Linear(torch.autograd.Function):
         q, scale, weight, link, *mask = ctx.saved_tensors
         g = g if g.dim() == 2 and (g.shape[1] < 2 or g.stride(1) == 1) and (g.shape[0] < 2 or g.stride(0) >= g.shape[1]) \
             else g.contiguous()
-        dx = g @ weight if ctx.needs_input_grad[0] else None
+        # under autocast the product had the type that g has
+        dx = g @ weight.to(g.dtype) if ctx.needs_input_grad[0] else None
         dw = None
         if ctx.needs_input_grad[1]:
             dw = _WeightGrad.apply(g, link, ctx.ops, Q8Matrix(q, scale, ctx.cols), mask[0] if mask else None).to(weight.dtype)

@@ -72,3 +72,27 @@ def test_second_derivatives_of_the_inputs_gradient(loss):
     for a, b in zip((dx, dw), torch.autograd.grad(LOSSES[loss](ours(x, w)), (x, w))):
         assert torch.equal(a, b)
     assert torch.equal(dx, plain[0])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("inside", [False, True])
+def test_autocast(dtype, inside):
+    """The product in bf16 as torch's own; gradients in the operands' types, whether the backward pass runs in the region or not."""
+    x, w = operands(6, 5, 4)
+    x = x.detach().to(dtype).requires_grad_()
+    grads = []
+    for layer in (ours, lambda x, w: x @ w.t()):
+        x.grad = w.grad = None
+        with torch.autocast("cpu", dtype=torch.bfloat16):
+            y = layer(x, w)
+            loss = y.float().square().sum()
+            if inside:
+                loss.backward()
+        if not inside:
+            loss.backward()
+        grads.append((y.detach(), x.grad, w.grad))
+    (y, dx, dw), (y2, dx2, _) = grads
+    assert y.dtype == torch.bfloat16 and torch.equal(y, y2)
+    assert dx.dtype == dtype and torch.equal(dx, dx2)
+    m = OPS.quantize(x.detach())
+    assert dw.dtype == torch.float32 and torch.equal(dw, OPS.weight_grad((2.0 * y.float()).bfloat16(), m))
