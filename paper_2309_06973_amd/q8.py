@@ -126,7 +126,7 @@ class Q8:
                     out: Optional[torch.Tensor] = None, accumulate: bool = False) -> torch.Tensor:
         """g transposed times the values of x: the fp32 gradient [g's columns, x.cols] of a linear
         layer's weights.  mask: uint8, what of the gradient is kept (as apply_mask writes it);
-        accumulate: added to ``out``."""
+        accumulate: added to ``out``.  Up to SHIFTER_Q8_MAX_SUM rows a call."""
         return self._calls.weight_grad(*self._enter(), g, x, mask, torch.float32, out, accumulate, self._room)
 
 
@@ -135,7 +135,13 @@ class _WeightGrad(torch.autograd.Function):
     that the way from it to the layer's operands leads through here."""
     @staticmethod
     def forward(ctx, g, link, ops, x, mask):
-        return ops.weight_grad(g, x, mask=mask)
+        most, dw = S.SHIFTER_Q8_MAX_SUM, None
+        if x.rows <= most:
+            return ops.weight_grad(g, x, mask=mask)
+        for i in range(0, x.rows, most):       # as many rows as a sum holds, the next ones added
+            dw = ops.weight_grad(g[i:i + most], Q8Matrix(x.q[i:i + most], x.scale[i:i + most], x.cols), mask=mask, out=dw,
+                                 accumulate=dw is not None)
+        return dw
 
     @staticmethod
     def backward(ctx, v):

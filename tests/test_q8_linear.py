@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from oracle import q8_oracle as Q
+from paper_2309_06973_amd import shifter as S
 from paper_2309_06973_amd.q8 import Q8Matrix, checkpointed_linear
 
 
@@ -16,9 +17,13 @@ class Definition:
         codes[:, :q.shape[1]] = q
         return Q8Matrix(torch.from_numpy(codes), torch.from_numpy(np.atleast_1d(s).astype(np.float32)), q.shape[1])
 
-    def weight_grad(self, g, x, mask=None):
+    def weight_grad(self, g, x, mask=None, out=None, accumulate=False):
+        assert g.shape[0] == x.rows <= S.SHIFTER_Q8_MAX_SUM
         d, _ = Q.weight_grad(g, x.q[:, :x.cols].numpy(), x.scale.numpy(), None if mask is None else mask.numpy())
-        return torch.from_numpy(d).float()
+        d = torch.from_numpy(d).float()
+        if out is None:
+            return d
+        return out.copy_(torch.where(mask == 0, out, out + d) if accumulate and mask is not None else out + d if accumulate else d)
 
 
 OPS = Definition()
@@ -96,3 +101,21 @@ def test_autocast(dtype, inside):
     assert dx.dtype == dtype and torch.equal(dx, dx2)
     m = OPS.quantize(x.detach())
     assert dw.dtype == torch.float32 and torch.equal(dw, OPS.weight_grad((2.0 * y.float()).bfloat16(), m))
+
+
+@pytest.mark.parametrize("rows", [7, 8, 9, 16, 17, 30])
+@pytest.mark.parametrize("masked", [False, True])
+def test_more_rows_than_one_sum_holds(monkeypatch, rows, masked):
+    """The weights' gradient of more rows than a call takes is that of several, added up: an fp32 rounding a part more."""
+    x, w = operands(rows, 5, 4)
+    mask = (torch.arange(20).view(5, 4) % 3 > 0).to(torch.uint8) if masked else None
+    y = checkpointed_linear(x, w, OPS, mask)
+    g = torch.randn(y.shape, generator=torch.Generator().manual_seed(1))
+    monkeypatch.setattr(S, "SHIFTER_Q8_MAX_SUM", 8)
+    dx, dw = torch.autograd.grad(y, (x, w), g)
+    q, s = Q.quantize(x)
+    want, _ = Q.weight_grad(g, q, s.astype(np.float32), None if mask is None else mask.numpy())
+    size, _ = Q.weight_grad(g.abs(), np.abs(q), s.astype(np.float32))
+    parts = -(-rows // 8)
+    assert (np.abs(Q.f64(dw) - want) <= 2 * parts * Q.U32 * size).all()
+    assert torch.equal(dx, g @ w.detach())
