@@ -130,6 +130,11 @@ class Q8:
         return self._calls.weight_grad(*self._enter(), g, x, mask, torch.float32, out, accumulate, self._room)
 
 
+def _rows(x: torch.Tensor) -> torch.Tensor:
+    """x with its columns side by side and its rows one after another."""
+    return x if (x.shape[1] < 2 or x.stride(1) == 1) and (x.shape[0] < 2 or x.stride(0) >= x.shape[1]) else x.contiguous()
+
+
 class _WeightGrad(torch.autograd.Function):
     """weight_grad where it may be differentiated again: an error then.  `link` ties the result to the layer, so
     that the way from it to the layer's operands leads through here."""
@@ -151,7 +156,7 @@ class _WeightGrad(torch.autograd.Function):
 class _Linear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, ops, mask):
-        kept = ops.quantize(x)
+        kept = ops.quantize(_rows(x))
         link = x.new_empty(0)
         ctx.save_for_backward(kept.q, kept.scale, weight, link, *(() if mask is None else (mask,)))
         ctx.ops, ctx.cols = ops, kept.cols
@@ -163,8 +168,7 @@ class _Linear(torch.autograd.Function):
         if g is None:
             return None, None, None, None
         q, scale, weight, link, *mask = ctx.saved_tensors
-        g = g if g.dim() == 2 and (g.shape[1] < 2 or g.stride(1) == 1) and (g.shape[0] < 2 or g.stride(0) >= g.shape[1]) \
-            else g.contiguous()
+        g = _rows(g)
         # under autocast the product had the type that g has
         dx = g @ weight.to(g.dtype) if ctx.needs_input_grad[0] else None
         dw = None
@@ -174,8 +178,11 @@ class _Linear(torch.autograd.Function):
 
 
 def checkpointed_linear(x: torch.Tensor, weight: torch.Tensor, ops: Q8, mask: Optional[torch.Tensor] = None):
-    """x times weight transposed, keeping x for the backward pass in 8 bits (a quarter of its fp32
-    size): the product and x's gradient are torch's, the weights' gradient comes from the 8-bit
-    rows.  mask: uint8 [out, in], weights that were pruned get no gradient.  The
+    """x [..., in] times weight [out, in] transposed, keeping x for the backward pass in 8 bits (a
+    quarter of its fp32 size): the product and x's gradient are torch's, the weights' gradient comes
+    from the 8-bit rows.  mask: uint8 [out, in], weights that were pruned get no gradient.  The
     weights' gradient can not be differentiated again, which is an error; x's can."""
-    return _Linear.apply(x, weight, ops, mask)[0]
+    if x.dim() == 2:
+        return _Linear.apply(x, weight, ops, mask)[0]
+    rows = x.reshape(x.shape[:-1].numel(), x.shape[-1])
+    return _Linear.apply(rows, weight, ops, mask)[0].view(*x.shape[:-1], weight.shape[0])

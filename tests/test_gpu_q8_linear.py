@@ -71,3 +71,14 @@ def test_second_derivatives(ops):
     size = 8.0 * x64.abs() @ w64.abs().t() @ w64.abs() @ w64.abs().t() @ w64.abs()
     # four products of sums of 40 to 50 terms, a half step a term and product
     assert ((got.double() - want).abs() <= 4 * 52 * Q.U32 * size).all()
+
+
+def test_layouts_of_the_input(ops):
+    x, w = operands(90, 50, 41)
+    g = torch.randn(90, 50, device=DEV)
+    for y_of, rows in ((lambda t: t.t().contiguous().t(), x), (lambda t: t.view(6, 15, 41), x),
+                       (lambda t: t.view(9, 10, 41).transpose(0, 1), x.view(9, 10, 41).transpose(0, 1).reshape(90, 41))):
+        y = checkpointed_linear(y_of(x), w, ops)
+        dx, dw = torch.autograd.grad(y, (x, w), g.view(y.shape))
+        assert y.shape == y_of(x).shape[:-1] + (50,) and dx.shape == x.shape
+        assert near(dw, g, rows)

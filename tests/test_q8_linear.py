@@ -12,10 +12,11 @@ class Definition:
     """quantize and weight_grad of Q8, from the definition in 64 bits."""
 
     def quantize(self, x):
+        assert x.dim() == 2 and (x.shape[1] < 2 or x.stride(1) == 1) and (x.shape[0] < 2 or x.stride(0) >= x.shape[1])
         q, s = Q.quantize(x)
-        codes = np.zeros((q.shape[0], -(-q.shape[1] // 16) * 16), dtype=np.int8)
-        codes[:, :q.shape[1]] = q
-        return Q8Matrix(torch.from_numpy(codes), torch.from_numpy(np.atleast_1d(s).astype(np.float32)), q.shape[1])
+        codes = torch.zeros((q.shape[0], -(-q.shape[1] // 16) * 16), dtype=torch.int8)
+        codes[:, :q.shape[1]] = torch.from_numpy(q)
+        return Q8Matrix(codes, torch.from_numpy(np.atleast_1d(s).astype(np.float32)), q.shape[1])
 
     def weight_grad(self, g, x, mask=None, out=None, accumulate=False):
         assert g.shape[0] == x.rows <= S.SHIFTER_Q8_MAX_SUM
@@ -119,3 +120,31 @@ def test_more_rows_than_one_sum_holds(monkeypatch, rows, masked):
     parts = -(-rows // 8)
     assert (np.abs(Q.f64(dw) - want) <= 2 * parts * Q.U32 * size).all()
     assert torch.equal(dx, g @ w.detach())
+
+
+def layouts(x):
+    """The values of x [24, 4] in shapes and orders that a layer meets."""
+    yield "columns apart", x.t().contiguous().t()
+    yield "every other column", torch.stack([x, -x], 2).view(24, 8)[:, ::2]
+    yield "one row for all", x[:1].expand(24, 4)
+    yield "batch of sequences", x.view(2, 3, 4, 4)
+    yield "sequences first", x.view(4, 6, 4).transpose(0, 1)
+    yield "one token", x[3]
+    yield "one token, columns apart", torch.stack([x, x], 2)[5, :, 0]
+    yield "no tokens", x[:0].view(3, 0, 4)
+
+
+@pytest.mark.parametrize("which", range(8))
+def test_layouts_of_the_input(which):
+    base, w = operands(24, 5, 4)
+    name, x = list(layouts(base.detach()))[which]
+    x = x.requires_grad_()
+    y = checkpointed_linear(x, w, OPS)
+    # four or five terms, a rounding each and one for each sum, in whatever order the products take
+    near = lambda got, a, b: (got.detach().double() - a.double() @ b.double()).abs() <= 5 * Q.U32 * (a.abs().double() @ b.abs().double())
+    assert near(y, x.detach(), w.detach().t()).all(), name
+    g = torch.randn(y.shape, generator=torch.Generator().manual_seed(2))
+    dx, dw = torch.autograd.grad(y, (x, w), g)
+    assert dx.shape == x.shape and near(dx, g, w.detach()).all()
+    rows = x.detach().reshape(-1, 4).contiguous()
+    assert torch.equal(dw, OPS.weight_grad(g.reshape(-1, 5), OPS.quantize(rows)))
