@@ -48,6 +48,11 @@ void here(const Handle& h, const at::Tensor& x, const char* what) {
     TORCH_CHECK_VALUE(d.is_cuda() && d.index() == h.device, what, " is not on cuda:", (int)h.device);
 }
 
+// What a caller gave has been written: autograd has to see it.
+void written(const at::Tensor& x) {
+    if (!x.is_inference()) x.unsafeGetTensorImpl()->bump_version();
+}
+
 int code_of(at::ScalarType t) {
     switch (t) {
         case at::kFloat: return SHIFTER_F32;
@@ -170,6 +175,14 @@ PyObject* room(const Handle& h, uint64_t rows, uint64_t cols, PyObject* out, Cod
     return out;
 }
 
+// A given 8-bit matrix has been written.
+void written(PyObject* out) {
+    if (is_none(out)) return;
+    const Owned q(PyObject_GetAttr(out, g_q)), scale(PyObject_GetAttr(out, g_scale));
+    written(tensor_of(q.p, "out"));
+    written(tensor_of(scale.p, "out"));
+}
+
 // The same for elements: their type is out's, or dtype.
 at::Tensor result(const Handle& h, uint64_t rows, uint64_t cols, PyObject* dtype, PyObject* out, Rows& r) {
     at::Tensor x;
@@ -185,8 +198,10 @@ at::Tensor result(const Handle& h, uint64_t rows, uint64_t cols, PyObject* dtype
     return x;
 }
 
+// What a call returns once it has been enqueued.
 PyObject* wrap(PyObject* out, at::Tensor&& x) {
     if (is_none(out)) return THPVariable_Wrap(std::move(x));
+    written(x);
     Py_INCREF(out);
     return out;
 }
@@ -241,6 +256,7 @@ PyObject* quantize(PyObject* const* a) {
     Codes m;
     Owned out(room(h, x.rows, x.cols, a[4], m));
     enqueue(a[0], [&] { return shifter_quantize_q8(h.ctx, x.p, x.dtype, x.ld, x.rows, x.cols, flags, m.q, m.ld, m.scale); });
+    written(a[4]);
     return out.release();
 }
 
@@ -284,6 +300,7 @@ PyObject* rms_norm(PyObject* const* a) {
         return shifter_rms_norm_q8(h.ctx, x.p, x.ld, residual.p, residual.ld, x.dtype, x.rows, x.cols, weight, (float)eps, stream.p,
                                    stream.ld, m.q, m.ld, m.scale);
     });
+    written(a[7]);
     Owned held(is_none(a[5]) ? (Py_INCREF(a[2]), a[2]) : wrap(a[6], std::move(sum)));
     Owned both(PyTuple_New(2));
     PyTuple_SET_ITEM(both.p, 0, out.release());
