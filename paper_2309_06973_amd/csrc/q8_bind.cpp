@@ -7,6 +7,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/core/grad_mode.h>
 #include <ATen/hip/EmptyTensor.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
@@ -48,7 +49,18 @@ void here(const Handle& h, const at::Tensor& x, const char* what) {
     TORCH_CHECK_VALUE(d.is_cuda() && d.index() == h.device, what, " is not on cuda:", (int)h.device);
 }
 
-// What a caller gave has been written: autograd has to see it.
+// Results have no graph.  An 8-bit matrix is a constant to autograd, as whole numbers are; where elements are made from
+// elements, the gradient of those would be lost without a word.
+void constant(const at::Tensor& x, const char* what) {
+    TORCH_CHECK_VALUE(!(x.requires_grad() && at::GradMode::is_enabled()), what,
+                      " needs a gradient, which this call does not pass on: detach it, or call under torch.no_grad()");
+}
+
+// What a caller gives to be written: autograd has to see that it was.
+void writable(const at::Tensor& x, const char* what) {
+    TORCH_CHECK_VALUE(!(x.requires_grad() && at::GradMode::is_enabled()), what,
+                      " needs a gradient, and is written without a graph: detach it, or call under torch.no_grad()");
+}
 void written(const at::Tensor& x) {
     if (!x.is_inference()) x.unsafeGetTensorImpl()->bump_version();
 }
@@ -192,6 +204,7 @@ at::Tensor result(const Handle& h, uint64_t rows, uint64_t cols, PyObject* dtype
         x = new_rows(h, rows, cols, reinterpret_cast<THPDtype*>(dtype)->scalar_type);
     } else {
         x = tensor_of(out, "out");
+        writable(x, "out");
         same(x, rows, cols, x.scalar_type(), "out");
     }
     r = rows_of(h, x, "out");
@@ -274,6 +287,11 @@ PyObject* dequantize(PyObject* const* a) {
 PyObject* rms_norm(PyObject* const* a) {
     const Handle h = handle_of(a);
     const at::Tensor& tx = tensor_of(a[2], "x");
+    if (!is_none(a[5])) {                      // without a residual the stream is x itself, with its graph
+        constant(tx, "x");
+        constant(tensor_of(a[5], "residual"), "residual");
+        if (!is_none(a[6])) writable(tensor_of(a[6], "h"), "h");
+    }
     const Rows x = rows_of(h, tx, "x");
     const float* weight = vector_of(h, a[3], x.cols, "weight");
     const double eps = PyFloat_AsDouble(a[4]);
@@ -311,6 +329,7 @@ PyObject* rms_norm(PyObject* const* a) {
 // ctx, device, a, b, bias, relu, dtype, out -> elements
 PyObject* matmul(PyObject* const* v) {
     const Handle h = handle_of(v);
+    if (!is_none(v[4])) constant(tensor_of(v[4], "bias"), "bias");
     const Codes a = codes_of(h, v[2], "a"), b = codes_of(h, v[3], "b");
     TORCH_CHECK_VALUE(a.cols == b.cols, "a and b have different numbers of columns");
     const float* bias = is_none(v[4]) ? nullptr : vector_of(h, v[4], b.rows, "bias");
@@ -326,7 +345,9 @@ PyObject* matmul(PyObject* const* v) {
 // ctx, device, g, x, mask, dtype, out, accumulate, room -> dw.  room(bytes) gives a workspace, where one is needed.
 PyObject* weight_grad(PyObject* const* a) {
     const Handle h = handle_of(a);
-    const Rows g = rows_of(h, tensor_of(a[2], "g"), "g");
+    const at::Tensor& tg = tensor_of(a[2], "g");
+    constant(tg, "g");
+    const Rows g = rows_of(h, tg, "g");
     const Codes x = codes_of(h, a[3], "x");
     TORCH_CHECK_VALUE(x.rows == g.rows, "g and x have different numbers of rows");
     Rows mask, r;
