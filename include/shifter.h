@@ -683,7 +683,8 @@ int shifter_compact_batch_masked(shifter_ctx* ctx, const shifter_model* model, c
  * shifter_quantize_q8    each row of x by itself: a = max |f(x)|, scale = a / 127,
  *                        code = 127 f(x) / a rounded to the nearest whole number, ties to even;
  *                        f is the identity, or ReLU with SHIFTER_Q8_RELU.  Codes are exact:
- *                        the rounding is that of the real quotient.  A row of zeros has
+ *                        the rounding is that of the real quotient.  The scale is one step
+ *                        of fp32 less where 127 of it would overflow (a is the largest finite number).  A row of zeros has
  *                        scale 0; a row with a value that is not finite (behind f) has codes 0
  *                        and scale NaN, so that every use of it becomes NaN.
  *                        Rows are a linear tensor's output channels (d_w + offset, stride

@@ -142,13 +142,16 @@ __device__ __forceinline__ void row_reduce(uint32_t& top, double& sum) {
 }
 
 // The row's scale.  A row with a value that is not finite has no codes: its scale is NaN, so that whatever
-// reads the row becomes NaN instead of a wrong number.
+// reads the row becomes NaN instead of a wrong number.  The largest value has to come back as a number: next to the largest
+// there is, 127 times the rounded scale can leave them (a / 127 does for that one a alone), and a scale one step less does not.
 template <bool NORM>
 __device__ __forceinline__ float row_scale(uint32_t top, double sum, const Q8RowsArgs& g) {
     if (top >= 0x7f800000u) return __uint_as_float(0x7fc00000u);
     const float a = __uint_as_float(top);
     if (a == 0.0f) return 0.0f;
-    return NORM ? (float)((double)a / (127.0 * sqrt(sum / (double)g.cols + (double)g.eps))) : a / 127.0f;
+    const float s = NORM ? (float)((double)a / (127.0 * sqrt(sum / (double)g.cols + (double)g.eps))) : a / 127.0f;
+    const float less = __uint_as_float(__float_as_uint(s) - 1u);         // s > 0, or the tiniest a: 0 then, and 127 s is a number
+    return isinf(__fmul_rn(127.0f, s)) && !isinf(__fmul_rn(127.0f, less)) ? less : s;
 }
 
 enum Q8Form { Q8_PLAIN, Q8_NORM, Q8_NORM_ADD };
