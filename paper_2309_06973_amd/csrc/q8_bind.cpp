@@ -233,6 +233,12 @@ bool truth(PyObject* o) {
     return v != 0;
 }
 
+void check(int rc, PyObject* ctx) {
+    if (rc == SHIFTER_OK) return;
+    const Owned none(PyObject_CallFunction(g_failed, "iO", rc, ctx));       // raises
+    TORCH_CHECK(false, "call failed with code ", rc);
+}
+
 // The call itself, without the interpreter's lock (a full queue makes a launch wait).
 template <typename F>
 void enqueue(PyObject* ctx, F call) {
@@ -240,9 +246,7 @@ void enqueue(PyObject* ctx, F call) {
     Py_BEGIN_ALLOW_THREADS
     rc = call();
     Py_END_ALLOW_THREADS
-    if (rc == SHIFTER_OK) return;
-    const Owned none(PyObject_CallFunction(g_failed, "iO", rc, ctx));       // raises
-    TORCH_CHECK(false, "call failed with code ", rc);
+    check(rc, ctx);
 }
 
 // A function of N arguments whose exceptions become Python's.
@@ -361,7 +365,7 @@ PyObject* weight_grad(PyObject* const* a) {
     TORCH_CHECK_VALUE(is_none(a[6]) || tensor_of(a[6], "out").scalar_type() == at::kFloat, "out must be float32");
     at::Tensor dw = result(h, g.cols, x.cols, a[5], a[6], r);
     uint64_t need = 0;
-    enqueue(Py_None, [&] { return shifter_weight_grad_q8_layout(g.rows, g.cols, x.cols, &need); });
+    check(shifter_weight_grad_q8_layout(g.rows, g.cols, x.cols, &need), Py_None);
     void* work = nullptr;
     PyObject* held = nullptr;
     if (need) {
@@ -370,10 +374,9 @@ PyObject* weight_grad(PyObject* const* a) {
     }
     const Owned keep(held ? held : (Py_INCREF(Py_None), Py_None));
     if (held) work = tensor_of(held, "work").data_ptr();
-    enqueue(a[0], [&] {
-        return shifter_weight_grad_q8(h.ctx, g.p, g.dtype, g.ld, x.q, x.ld, x.scale, g.rows, g.cols, x.cols,
-                                      static_cast<const uint8_t*>(mask.p), mask.ld, flags, static_cast<float*>(r.p), r.ld, work, need);
-    });
+    // with the interpreter's lock: the launches share the handle's workspace, and another thread's stay out from between them
+    check(shifter_weight_grad_q8(h.ctx, g.p, g.dtype, g.ld, x.q, x.ld, x.scale, g.rows, g.cols, x.cols,
+                                 static_cast<const uint8_t*>(mask.p), mask.ld, flags, static_cast<float*>(r.p), r.ld, work, need), a[0]);
     return wrap(a[6], std::move(dw));
 }
 

@@ -63,10 +63,14 @@ class Q8:
     Matrices of elements are two-dimensional fp32, bf16 or fp16 tensors whose columns lie side by
     side; their rows may have any stride.
     Results are new tensors unless ``out`` (or ``h``) says where they go, and have no graph of
-    autograd's: 8-bit matrices are constants to it, and elements (h, a bias, g) that need a gradient
-    are refused unless under torch.no_grad().  Recorded into a graph,
-    calls of one handle share a workspace apart from that of calls made at once: replays of such graphs
-    go one after another, on whatever stream."""
+    autograd's: 8-bit matrices are constants to it, and elements that need a gradient (x and residual
+    of a norm, a bias, g) are refused unless under torch.no_grad().
+
+    Recorded into a graph, calls of one handle share a workspace apart from that of calls made at
+    once: replays of such graphs go one after another, on whatever stream.  The handle is one host
+    thread's at a time, as the C interface asks for; the launches of a weight_grad, which share the
+    workspace, follow one another whatever other threads call (autograd runs backward passes on
+    threads of its own)."""
 
     def __init__(self, device: int = 0, ctx=None):
         if not torch.cuda.is_available():
@@ -95,13 +99,15 @@ class Q8:
 
     def _room(self, need: int) -> torch.Tensor:
         """A workspace of `need` bytes at least, kept from call to call; recorded calls have their own."""
-        if torch.cuda.is_current_stream_capturing():
-            if not self.recorded or self.recorded[-1].numel() < need:
-                self.recorded.append(torch.empty(need, dtype=torch.uint8, device=self.dev))
-            return self.recorded[-1]
-        if self.work is None or self.work.numel() < need:
-            self.work = torch.empty(need, dtype=torch.uint8, device=self.dev)
-        return self.work
+        recording = torch.cuda.is_current_stream_capturing()
+        work = (self.recorded[-1] if self.recorded else None) if recording else self.work
+        if work is None or work.numel() < need:            # what is returned is this call's, whatever other threads leave here
+            work = torch.empty(need, dtype=torch.uint8, device=self.dev)
+            if recording:
+                self.recorded.append(work)
+            else:
+                self.work = work
+        return work
 
     # ---- the operators --------------------------------------------------------------
     def quantize(self, x: torch.Tensor, relu: bool = False, out: Optional[Q8Matrix] = None) -> Q8Matrix:

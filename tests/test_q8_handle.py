@@ -64,3 +64,58 @@ def test_a_pipelines_context():
     there.close()
     ops.close()                                # leaves the context
     S.shifter_destroy(ctx)
+
+
+@pytest.mark.parametrize("recording", [False, True])
+def test_a_workspace_is_as_large_as_asked_for(device, monkeypatch, recording):
+    """Another host thread that puts a smaller one in the place of a call's workspace, right behind its allocation, does not
+    leave the call with less than it asked for."""
+    made = lambda n, **kw: types.SimpleNamespace(numel=lambda: n)
+
+    class Interrupted(q8.Q8):
+        @property
+        def work(self):
+            return self.held
+
+        @work.setter
+        def work(self, w):
+            self.held = w and made(10)
+
+    class Recorded(list):
+        def append(self, w):
+            super().append(w)
+            super().append(made(10))
+
+    ops = Interrupted(ctx=context(0, 7))
+    ops.recorded = Recorded()
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: recording)
+    monkeypatch.setattr(torch, "empty", made)
+    assert ops._room(100).numel() == 100
+
+
+@pytest.mark.gpu
+def test_two_threads():
+    """Gradients of two host threads on one handle: a call's launches follow one another."""
+    import threading
+    ops = q8.Q8()
+    g = torch.Generator(device="cuda").manual_seed(1)
+    pairs = [(torch.randn(m, n, generator=g, device="cuda"), ops.quantize(torch.randn(m, k, generator=g, device="cuda")))
+             for m, n, k in ((2500, 300, 200), (2700, 290, 310))]
+    want = [ops.weight_grad(a, b) for a, b in pairs]
+    got, failed = [[], []], []
+
+    def work(i):
+        try:
+            for _ in range(100):
+                got[i].append(ops.weight_grad(*pairs[i]))
+        except Exception as e:                 # pragma: no cover
+            failed.append(e)
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not failed
+    assert all(torch.equal(d, want[i]) for i in range(2) for d in got[i])
+    ops.close()
