@@ -698,8 +698,9 @@ int shifter_compact_batch_masked(shifter_ctx* ctx, const shifter_model* model, c
  *                        64 bits.  A row of zeros has scale 0 (also where eps is 0).
  * shifter_matmul_q8      c[m][n] = sa[m] sb[n] sum_k qa[m][k] qb[n][k] + bias[n], ReLU with
  *                        SHIFTER_Q8_RELU, rounded to the element type.  The sum is exact in 32-bit integers:
- *                        k up to SHIFTER_Q8_MAX_SUM, else SHIFTER_ERR_CAPACITY (also for m x n of about 2^35 and more,
- *                        or n of 2^26, which a launch does not hold).  d_bias may be NULL.
+ *                        k up to SHIFTER_Q8_MAX_SUM, else SHIFTER_ERR_CAPACITY (also where m times n, both rounded up to
+ *                        multiples of 64, is 2^35 or more, and for n above 2^26 - 16 with m up to 48: a launch does not
+ *                        hold those).  d_bias may be NULL.
  *                        For k = 0 the sum is 0.  The result does not depend on the device's state or on how the
  *                        work is split.
  * shifter_weight_grad_q8 dw[n][k] = sum over the m rows of g[m][n] scale[m] q[m][k], the gradient of a linear
@@ -712,7 +713,10 @@ int shifter_compact_batch_masked(shifter_ctx* ctx, const shifter_model* model, c
  *                        times the sum of |q| over its column k, plus a few roundings of the terms and of the result.  A column with
  *                        a p that is not finite has NaN in its whole row of dw (masked entries aside).
  *                        m up to SHIFTER_Q8_MAX_SUM, else SHIFTER_ERR_CAPACITY; more rows go in several calls with
- *                        SHIFTER_Q8_ACCUMULATE.
+ *                        SHIFTER_Q8_ACCUMULATE.  The same, from the layout call too, for sizes that a launch does not hold:
+ *                        with m up to 16, n rounded up to 16 times k to 256, of 2^36 and more; with m above 16, n times k, both
+ *                        rounded up to multiples of 64, of 2^35 and more, n from 2^26 to 2^28 on (the more rows, the sooner) and k
+ *                        times m of about 2^38 and more.
  *                        d_work: work_bytes of shifter_weight_grad_q8_layout, 256-byte aligned; NULL where that says
  *                        0, as it does for few rows and for little work. */
 typedef enum { SHIFTER_F32 = 0, SHIFTER_BF16 = 1, SHIFTER_F16 = 2 } shifter_dtype;

@@ -1776,6 +1776,8 @@ extern "C" int shifter_weight_grad_q8_layout(uint64_t m, uint64_t n, uint64_t k,
         return fail(nullptr, SHIFTER_ERR_CAPACITY, "weight_grad_q8_layout: sums of more than 131071 products do not fit 32 bits");
     if (n > Q8_MAX_ROWS || k > Q8_MAX_ROWS)
         return fail(nullptr, SHIFTER_ERR_INVALID_ARG, "weight_grad_q8_layout: more than 2^31 - 1 rows or columns");
+    if (const char* why = q8_gradient_too_many(m, n, k))
+        return fail(nullptr, SHIFTER_ERR_CAPACITY, std::string("weight_grad_q8_layout: ") + why);
     *h_work_bytes = q8_gradient_plan(m, n, k).bytes;
     return SHIFTER_OK;
 }
@@ -1793,6 +1795,7 @@ extern "C" int shifter_weight_grad_q8(shifter_ctx* ctx, const void* d_g, int dty
     if (d_mask) Q8_REFUSE("weight_grad_q8", q8_bad_rows(d_mask, 1, n, k, ld_mask));
     if (m > SHIFTER_Q8_MAX_SUM)
         return fail(ctx, SHIFTER_ERR_CAPACITY, "weight_grad_q8: sums of more than 131071 products do not fit 32 bits");
+    if (const char* why = q8_gradient_too_many(m, n, k)) return fail(ctx, SHIFTER_ERR_CAPACITY, std::string("weight_grad_q8: ") + why);
     const uint64_t need = q8_gradient_plan(m, n, k).bytes;
     if (work_bytes < need)
         return fail(ctx, SHIFTER_ERR_INVALID_ARG,
@@ -1800,7 +1803,6 @@ extern "C" int shifter_weight_grad_q8(shifter_ctx* ctx, const void* d_g, int dty
     if (need && (!d_work || misaligned(d_work, 256)))
         return fail(ctx, SHIFTER_ERR_INVALID_ARG, "weight_grad_q8: the workspace must be 256-byte aligned");
     if (n == 0 || k == 0) return SHIFTER_OK;
-    if (const char* why = q8_too_many(n, k)) return fail(ctx, SHIFTER_ERR_CAPACITY, std::string("weight_grad_q8: ") + why);
     Q8GradientArgs a{};
     a.g = d_g; a.q = d_q; a.s = d_scale; a.mask = d_mask;
     a.ld_g = ld_g; a.ld_q = ld_q; a.ld_mask = ld_mask; a.ld_dw = ld_dw;

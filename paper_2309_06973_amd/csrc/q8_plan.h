@@ -22,14 +22,6 @@ constexpr uint64_t q8_pad(uint64_t cols) { return (cols + Q8_ALIGN - 1u) & ~(uin
 
 inline bool q8_off(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1u)) != 0; }
 
-// A launch holds less than 2^32 threads.  The largest tiles that could be meant have 64 x 64 results and 512 threads, the
-// smallest blocks 16 columns; results of so many do not fit that.
-inline const char* q8_too_many(uint64_t rows, uint64_t cols) {
-    const uint64_t tiles = ((rows + 63u) / 64u) * ((cols + 63u) / 64u), strips = (cols + 15u) / 16u;
-    return tiles >= (1ull << 23) || strips >= (1ull << 22) || (rows + 15u) / 16u * ((cols + 255u) / 256u) >= (1ull << 24)
-               ? "a result of more tiles than a launch holds" : nullptr;
-}
-
 // What is wrong with a matrix of elements of `size` bytes, or nullptr.
 inline const char* q8_bad_rows(const void* p, uintptr_t size, uint64_t rows, uint64_t cols, uint64_t ld) {
     if (rows > Q8_MAX_ROWS || cols > Q8_MAX_ROWS) return "more than 2^31 - 1 rows or columns";
@@ -112,6 +104,15 @@ inline uint32_t q8_group(uint64_t m, uint64_t n) {
     return 3;
 }
 
+// A launch holds less than 2^32 threads along an axis.  Results whose tiles do not fit that: the smallest tiles have 64 x 64
+// results, the largest blocks 512 threads; blocks of 16 columns for few rows up to 1024.
+constexpr uint64_t Q8_LAUNCH = 1ull << 32;
+inline bool q8_tiles_fit(uint64_t rows, uint64_t cols) { return (rows + 63u) / 64u * ((cols + 63u) / 64u) * 512u < Q8_LAUNCH; }
+inline const char* q8_too_many(uint64_t m, uint64_t n) {
+    return !q8_tiles_fit(m, n) || (m <= Q8_FEW_ROWS_MOST && (n + 15u) / 16u * 1024u >= Q8_LAUNCH) ? "a result of more tiles than a launch holds"
+                                                                                                   : nullptr;
+}
+
 inline Q8Kernel q8_kernel_for(uint64_t m, uint64_t n, uint64_t k) {
     if (m <= Q8_FEW_ROWS || (m <= Q8_FEW_ROWS_MOST && n * k <= Q8_FEW_WEIGHTS)) return Q8_FEW;
     if (q8_group_blocks(m, n, 3) <= (uint64_t)Q8_UNITS) return Q8_GROUPS;
@@ -170,11 +171,51 @@ struct Q8GradientPlan {
     uint32_t slices, slice_rows;              // 0 slices: up to Q8_WHOLE_ROWS rows
     uint64_t tops, slice_tops, digits, codes, sums, bytes;      // offsets, and the whole
 };
+// The rows of the transposed operands, and the slices that more than Q8_WHOLE_ROWS of them are read in.
+constexpr uint64_t q8_gradient_ld(uint64_t m) { return (m + 127u) & ~(uint64_t)127u; }
+inline uint32_t q8_slice_rows(uint64_t m) {
+    const uint64_t per = (m + Q8_SLICES * Q8_SLICE_ROWS - 1u) / (Q8_SLICES * Q8_SLICE_ROWS);
+    return (uint32_t)(Q8_SLICE_ROWS * (per ? per : 1u));
+}
+// The grids that make the operands.  Threads of a block that holds columns whole; blocks of `threads` that turn the checkpoint, 128
+// rows and columns by each 256 of them; blocks of the slices' columns; of the digits, whose blocks each read the slices: as many
+// times 128 rows a block as leave 2048 blocks.
+constexpr uint32_t q8_columns_threads(uint64_t ld) { return ld <= 512 ? 256u : ld <= 1024 ? 512u : 1024u; }
+constexpr uint64_t q8_columns_blocks(uint64_t n) { return (n + 15u) / 16u; }
+constexpr uint64_t q8_turn_blocks(uint64_t k, uint64_t ld, uint32_t threads) {
+    return ((k + 127u) / 128u * (ld / 128u) + threads / 256u - 1u) / (threads / 256u);
+}
+constexpr uint64_t q8_tops_blocks(uint64_t n, uint64_t slices) { return (n + 511u) / 512u * slices; }
+inline uint32_t q8_digits_deep(uint64_t n, uint64_t ld) {
+    const uint64_t deep = (n + 63u) / 64u * (ld / 128u) / 2048u;
+    return deep < 1u ? 1u : deep > 8u ? 8u : (uint32_t)deep;
+}
+inline uint64_t q8_digits_blocks(uint64_t n, uint64_t ld) {
+    const uint64_t deep = q8_digits_deep(n, ld);
+    return (n + 63u) / 64u * ((ld / 128u + deep - 1u) / deep);
+}
+
+// The same for the gradient: its tiles, or the blocks of few rows, and what makes the tiles' operands.  m, n and k are less than 2^31.
+inline const char* q8_gradient_too_many(uint64_t m, uint64_t n, uint64_t k) {
+    bool fits = true;
+    if (q8_small(m, n, k)) {
+    } else if (m <= Q8_WIDE_ROWS) {
+        fits = (n + 15u) / 16u * ((k + 255u) / 256u) * 256u < Q8_LAUNCH;
+    } else {
+        const uint64_t ld = q8_gradient_ld(m), threads = q8_columns_threads(ld), rows = q8_slice_rows(m);
+        fits = q8_tiles_fit(n, k);
+        if (m <= Q8_WHOLE_ROWS) fits = fits && (q8_columns_blocks(n) + q8_turn_blocks(k, ld, (uint32_t)threads)) * threads < Q8_LAUNCH;
+        else
+            fits = fits && (q8_tops_blocks(n, (m + rows - 1u) / rows) + q8_turn_blocks(k, ld, 256)) * 256u < Q8_LAUNCH &&
+                   q8_digits_blocks(n, ld) * 256u < Q8_LAUNCH;
+    }
+    return fits ? nullptr : "a gradient of more tiles than a launch holds";
+}
+
 inline Q8GradientPlan q8_gradient_plan(uint64_t m, uint64_t n, uint64_t k) {
     Q8GradientPlan p;
-    p.ld = (m + 127u) & ~(uint64_t)127u;
-    const uint64_t per = (m + Q8_SLICES * Q8_SLICE_ROWS - 1u) / (Q8_SLICES * Q8_SLICE_ROWS);
-    p.slice_rows = (uint32_t)(Q8_SLICE_ROWS * (per ? per : 1u));
+    p.ld = q8_gradient_ld(m);
+    p.slice_rows = q8_slice_rows(m);
     p.slices = m <= Q8_WHOLE_ROWS ? 0u : (uint32_t)((m + p.slice_rows - 1u) / p.slice_rows);
     p.tops = 0;
     p.slice_tops = 4u * n;

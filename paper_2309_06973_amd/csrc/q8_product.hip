@@ -474,10 +474,6 @@ __device__ __forceinline__ void turn_codes(const Q8GradientArgs& a, const Q8Grad
     if (there)
         store_turned(tid, lds, min(128u, a.k - k0), reinterpret_cast<int8_t*>(a.work + pl.codes) + (uint64_t)k0 * pl.ld + m0, pl.ld);
 }
-static uint32_t turn_blocks(const Q8GradientArgs& a, const Q8GradientPlan& pl, uint32_t threads) {
-    const uint32_t tiles = (a.k + 127u) / 128u * (uint32_t)(pl.ld / TURN_ROWS), each = threads / BLOCK;
-    return (tiles + each - 1u) / each;
-}
 
 // What a column's digits are made with, from its largest |p|.  No factor: zeros, or a column that is not finite.
 struct ColumnScale {
@@ -981,20 +977,21 @@ static void launch_gradient_small(shifter_ctx* ctx, const Q8GradientArgs& g, Q8G
 
 template <typename T, uint32_t THREADS>
 static void launch_columns(shifter_ctx* ctx, const Q8GradientArgs& g, const Q8GradientPlan& pl) {
-    const uint32_t blocks = (g.n + 15u) / 16u;
-    q8_columns_kernel<T, THREADS><<<blocks + turn_blocks(g, pl, THREADS), THREADS, 0, ctx->stream>>>(g, pl, blocks);
+    const uint32_t blocks = (uint32_t)q8_columns_blocks(g.n);
+    q8_columns_kernel<T, THREADS><<<blocks + (uint32_t)q8_turn_blocks(g.k, pl.ld, THREADS), THREADS, 0, ctx->stream>>>(g, pl, blocks);
 }
 
 template <typename T>
 static void launch_digits(shifter_ctx* ctx, const Q8GradientArgs& g, const Q8GradientPlan& pl) {
-    if (pl.ld <= 512) return launch_columns<T, 256>(ctx, g, pl);
-    if (pl.ld <= 1024) return launch_columns<T, 512>(ctx, g, pl);
-    if (pl.ld <= Q8_WHOLE_ROWS) return launch_columns<T, 1024>(ctx, g, pl);
-    const uint32_t across = (g.n + 63u) / 64u, tiles = (uint32_t)(pl.ld / TURN_ROWS), tops = (g.n + 511u) / 512u * pl.slices;
-    q8_tops_kernel<T><<<tops + turn_blocks(g, pl, BLOCK), BLOCK, 0, ctx->stream>>>(g, pl, tops);
-    // every block reads its columns' slices: as many rows a block as leave 2048 blocks
-    const uint32_t deep = std::min(8u, std::max(1u, (uint32_t)((uint64_t)across * tiles / 2048u)));
-    q8_digits_kernel<T><<<across * ((tiles + deep - 1u) / deep), BLOCK, 0, ctx->stream>>>(g, pl, deep);
+    if (g.m <= Q8_WHOLE_ROWS) {
+        const uint32_t threads = q8_columns_threads(pl.ld);
+        if (threads == 256) return launch_columns<T, 256>(ctx, g, pl);
+        if (threads == 512) return launch_columns<T, 512>(ctx, g, pl);
+        return launch_columns<T, 1024>(ctx, g, pl);
+    }
+    const uint32_t tops = (uint32_t)q8_tops_blocks(g.n, pl.slices);
+    q8_tops_kernel<T><<<tops + (uint32_t)q8_turn_blocks(g.k, pl.ld, BLOCK), BLOCK, 0, ctx->stream>>>(g, pl, tops);
+    q8_digits_kernel<T><<<(uint32_t)q8_digits_blocks(g.n, pl.ld), BLOCK, 0, ctx->stream>>>(g, pl, q8_digits_deep(g.n, pl.ld));
 }
 
 // The parts' sums joined, in 64 bits so that only the parts' own roundings count; under the mask, or added to dw.
