@@ -190,6 +190,10 @@ def checkpointed_linear(x: torch.Tensor, weight: torch.Tensor, ops: Q8, mask: Op
     quarter of its fp32 size): the product and x's gradient are torch's, the weights' gradient comes
     from the 8-bit rows.  mask: uint8 [out, in], weights that were pruned get no gradient.  The
     weights' gradient can not be differentiated again, which is an error; x's can."""
+    if mask is not None:
+        if mask.dtype != torch.uint8 or mask.shape != weight.shape or mask.device != weight.device:
+            raise ValueError("mask must be uint8, of the weights' shape and on their device")
+        mask = _rows(mask)
     if x.dim() == 2:
         return _Linear.apply(x, weight, ops, mask)[0]
     rows = x.reshape(x.shape[:-1].numel(), x.shape[-1])

@@ -20,6 +20,7 @@ class Definition:
 
     def weight_grad(self, g, x, mask=None, out=None, accumulate=False):
         assert g.shape[0] == x.rows <= S.SHIFTER_Q8_MAX_SUM
+        assert mask is None or (mask.dtype == torch.uint8 and mask.stride(1) == 1 and mask.stride(0) >= mask.shape[1])
         d, _ = Q.weight_grad(g, x.q[:, :x.cols].numpy(), x.scale.numpy(), None if mask is None else mask.numpy())
         d = torch.from_numpy(d).float()
         if out is None:
@@ -148,3 +149,18 @@ def test_layouts_of_the_input(which):
     assert dx.shape == x.shape and near(dx, g, w.detach()).all()
     rows = x.detach().reshape(-1, 4).contiguous()
     assert torch.equal(dw, OPS.weight_grad(g.reshape(-1, 5), OPS.quantize(rows)))
+
+
+def test_masks():
+    """One that the backward pass could not use is refused where it is given; the order of its memory does not matter."""
+    x, w = operands(6, 5, 4)
+    mask = (torch.arange(20).view(5, 4) % 3 > 0).to(torch.uint8)
+    for bad in (mask.bool(), mask.float(), mask[:4], mask[:, :3], mask.t(), mask.to("meta")):
+        with pytest.raises(ValueError, match="mask"):
+            checkpointed_linear(x, w, OPS, bad)
+    want = torch.autograd.grad(checkpointed_linear(x, w, OPS, mask).sum(), (w,))[0]
+    for same in (mask.t().contiguous().t(), torch.stack([mask, 1 - mask], 2)[:, :, 0]):
+        assert torch.equal(torch.autograd.grad(checkpointed_linear(x, w, OPS, same).sum(), (w,))[0], want)
+    row = torch.ones(1, 4, dtype=torch.uint8).expand(5, 4)
+    assert torch.equal(torch.autograd.grad(checkpointed_linear(x, w, OPS, row).sum(), (w,))[0],
+                       torch.autograd.grad(checkpointed_linear(x, w, OPS).sum(), (w,))[0])
