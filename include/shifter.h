@@ -697,7 +697,8 @@ int shifter_compact_batch_masked(shifter_ctx* ctx, const shifter_model* model, c
  *                        scale = a / (127 sqrt(mean(h^2) + eps)); the mean of squares is summed in
  *                        64 bits.  A row of zeros has scale 0 (also where eps is 0).
  * shifter_matmul_q8      c[m][n] = sa[m] sb[n] sum_k qa[m][k] qb[n][k] + bias[n], ReLU with
- *                        SHIFTER_Q8_RELU, rounded to the element type.  The sum is exact in 32-bit integers:
+ *                        SHIFTER_Q8_RELU, rounded to the element type.  The sum is exact in 32-bit integers, then
+ *                        (sum sa[m]) sb[n] + bias[n] is worked out in fp32, where sum sa[m] has to stay in its range:
  *                        k up to SHIFTER_Q8_MAX_SUM, else SHIFTER_ERR_CAPACITY (also where m times n, both rounded up to
  *                        multiples of 64, is 2^35 or more, and for n above 2^26 - 16 with m up to 48: a launch does not
  *                        hold those).  d_bias may be NULL.
@@ -710,7 +711,10 @@ int shifter_compact_batch_masked(shifter_ctx* ctx, const shifter_model* model, c
  *                        what d_dw holds (masked entries keep what they hold).
  *                        p = fl32(g * scale) is held as a 24-bit whole number relative to the largest |p| of its
  *                        column n and summed exactly: the error of an entry is at most that largest |p| / 8355711
- *                        times the sum of |q| over its column k, plus a few roundings of the terms and of the result.  A column with
+ *                        times the sum of |q| over its column k, plus a few roundings of the terms and of the result.  (Few rows and
+ *                        little work are summed in 64 bits, without that rounding.)  A p far below its column's largest
+ *                        keeps few bits: rows 10^4 and more above the others are for a call of their own, added with
+ *                        SHIFTER_Q8_ACCUMULATE.  A column with
  *                        a p that is not finite has NaN in its whole row of dw (masked entries aside).
  *                        m up to SHIFTER_Q8_MAX_SUM, else SHIFTER_ERR_CAPACITY; more rows go in several calls with
  *                        SHIFTER_Q8_ACCUMULATE.  The same, from the layout call too, for sizes that a launch does not hold:

@@ -65,7 +65,8 @@ struct Q8TileCost {
 //    2048 x 2048 x 2048    16.9     13.4     12.8     16.2     24.8
 //    4096 x 1024 x 8192    53.0     43.7     37.7     45.5     73.4
 //    16384 x 100 x 2048     9.4      9.1     11.4     16.8     26.4
-// The costs below say these within 20 %; the kernel of the least cost is taken.
+// The costs below say these within 17 %; the kernel of the least cost is taken, the fastest one in all these rows but 777 x 1873 x 977
+// (64x64 for 64x128).
 constexpr int Q8_TILES_N = 5;
 constexpr Q8TileCost Q8_TILES[Q8_TILES_N] = {{64, 64, 3.2, 0.21, 0.235, 0.20},
                                              {64, 128, 3.2, 0.265, 0.36, 0.325},
@@ -140,7 +141,9 @@ constexpr uint32_t Q8_WHOLE_ROWS = 2048;
 //    8192 x 1000 x 300      40.9  31.9    47.0  38.9    61.0      106
 //    16384 x 512 x 512      76.0  57.2    83.9  72.0     113      198
 //    256 x 2048 x 512        5.8   6.0     6.1   6.2     8.3     13.0
-// (on random digits; the first on those of a real gradient 690 with 128x256)
+// (on random digits).  The costs below say these within 11 % from 3000 rows on; fewer rows cost more than they say, up to 27 %, and
+// with three stages up to 47 % (512 x 4096 x 1024).  3000 x 1500 x 700 takes 64x64, 11 % slower than the fastest, 256 x 2048 x 512
+// 64x64 deep, 3 %; the first four rows take the fastest, the other two are split as below.
 // Q8_GRAD_SMALL and _WIDE: no digits and no workspace, sums in 64-bit floating point, in one launch.
 enum Q8GradientKernel { Q8_GRAD_WIDE = -2, Q8_GRAD_SMALL = -1, Q8_GRAD_64x64, Q8_GRAD_64x64_DEEP, Q8_GRAD_64x128, Q8_GRAD_64x128_DEEP,
                         Q8_GRAD_64x256, Q8_GRAD_128x256, Q8_GRAD_KERNELS };
@@ -152,7 +155,12 @@ constexpr Q8TileCost Q8_GRAD_TILES[] = {{64, 64, 3.5, 0.57, 0.62, 0.43},
                                         {64, 256, 5.0, 0.85, 1.32, 0.0},
                                         {128, 256, 7.0, 1.50, 2.29, 0.0}};
 // Where tiles are few the rows are split among `parts` blocks a tile; their sums, fp32, are joined by a launch of its own,
-// which costs that and the traffic.
+// which costs that and the traffic.  us of both by parts, with the tiles that are taken:
+//    m x n x k                       1     2     4     8    16    32
+//    8192 x 1000 x 300   64x64     41.5  28.8  25.3  29.8  34.9  44.6   (4 taken; 64x128 deep would take 21.6)
+//    16384 x 512 x 512   64x128 d. 72.2  42.5  27.4  26.9  34.4  49.8   (8 taken)
+//    20000 x 60 x 50     64x64 d.  67.4  40.5  25.5  19.0  17.3  20.2   (32 taken)
+//    4100 x 260 x 520    64x64     18.8  17.5  14.3  14.6  15.7  20.9   (8 taken)
 constexpr uint64_t Q8_PARTS = 32;
 // Little work, and few rows of whatever size, go to one launch.  us, that / digits and tiles: 64 x 512 x 512 3.3 / 9.3, 300 x 300 x 300
 // 4.4 / 9.5, 500 x 250 x 333 5.8 / 12, 1000 x 100 x 200 7.1 / 14, 2000 x 250 x 260 16 / 21, 128 x 1024 x 1024

@@ -8,9 +8,14 @@
 // The gradient's other factor is p = g s in fp32.  Per column it is brought to 24-bit whole
 // numbers v (the column's largest |p| becomes 8355711 = 127 (2^16 + 2^8 + 1)), and those to three
 // balanced digits, v = d2 2^16 + d1 2^8 + d0, digits from -128 to 127.  Three integer products
-// with the same Q give the sum to fp32 accuracy at 1.5 times the cost of one bf16 product (the
-// matrix units take 8-bit integers twice as fast), where fp32 products run at a sixteenth.  Where there
-// is little work, 64-bit products in one launch are faster than the two that digits need.
+// with the same Q give the sum of v q exactly at 1.5 times the cost of one bf16 product (the
+// matrix units take 8-bit integers twice as fast), where fp32 products run at a sixteenth.  What that
+// rounds to fewer bits is p, once: a p that is 2^j below its column's largest keeps 24 - j of its bits, so
+// the column's largest bounds the error of all its sums.  Norm-wise, 4096 rows behind a ReLU: 5e-7 with rows whose
+// sizes spread by e^1, 1.7e-6 by e^2 (fp32 products 3e-7); with one row 10^4 above the others 3e-4 in the entries where that
+// row has nothing, with 10^6 4e-2.  Such rows are for a call of their own (SHIFTER_Q8_ACCUMULATE), whose columns have their own
+// largest.  Where there is little work, 64-bit products in one launch, without that rounding, are faster than the two
+// launches that digits need.
 #include <algorithm>
 #include <type_traits>
 
@@ -230,9 +235,10 @@ __device__ __forceinline__ void store_rows(const int8_t* from, uint32_t pitch, T
 }
 
 // c[m][n] = (sum over k of A[m][k] B[n][k]) sa[m] sb[n] + bias[n]: the sum exact, then two roundings in fp32 and the one to
-// c's type.  8192 x 8192 x 8192 to bf16 takes 420 to 445 us, 2.5 to 2.6 POP/s, against 2.42 of the library's bare integer product:
-// the matrix units are busy 69 % of the time and the card lowers its clock to 1.6 GHz under them, so that power is the
-// bound.  A band of GROUP tiles keeps memory out of the way: 0.8 GB are read, 1.8 TB/s.  Eight wavefronts of 128 x 64 each
+// c's type.  8192 x 8192 x 8192 to bf16 takes 425 us on the same operands again and again and 445 on new ones (434 to 555 under a
+// profiler), 2.5 to 2.6 POP/s, against 2.42 of the library's bare integer product: the matrix units are busy in 71 % of the
+// cycles, and there are 1.66 GHz of those under this load where the chip has up to 2.4; LDS reads conflict in 1 % of their
+// cycles.  A band of GROUP tiles keeps memory out of the way: 0.8 GB are read, 1.8 TB/s.  Eight wavefronts of 128 x 64 each
 // for 256 x 256: four of 128 x 128 would read a fifth less LDS but spill (505 us or more).
 template <typename T, uint32_t WA, uint32_t WB, uint32_t FA, uint32_t FB, uint32_t NS, uint32_t STEP, uint32_t GROUP>
 __global__ __launch_bounds__(64 * WA * WB) void q8_product_kernel(Q8ProductArgs g) {
@@ -508,9 +514,9 @@ __device__ __forceinline__ void digit_words(uint32_t a, uint32_t b, uint32_t c, 
 
 // Digits of 16 columns and all rows by a block that holds them in registers, eight columns of four rows a thread: g is
 // read once, and what a thread has of a column leaves as four bytes.  Neighbouring blocks, which share lines of g, are
-// on one chiplet.  Behind the blocks for digits come those that turn the checkpoint.  100 x 512 with 512 columns of checkpoint
-// takes 3.5 us, little more than a launch (with eight rows a thread, and a column's unit made by every thread, 5.5);
-// 2048 x 1873 (bf16, odd stride) and 977 10.4 us for 23 MB, 2048 x 4096 and 4096 13 us for 58 MB, 4.5 TB/s.
+// on one chiplet.  Behind the blocks for digits come those that turn the checkpoint.  300 x 1100 with 1000 columns of checkpoint
+// takes 5 us, little more than a launch; 2048 x 1873 (bf16, odd stride) and 977 12 to 14 us for 23 MB, 1.8 TB/s: 118 blocks for
+// digits and 32 for the checkpoint leave units idle; 2048 x 4096 and 4096 13.5 us for 58 MB, 4.3 TB/s.
 template <typename T, uint32_t THREADS>
 __global__ __launch_bounds__(THREADS) void q8_columns_kernel(Q8GradientArgs a, Q8GradientPlan pl, uint32_t blocks) {
     constexpr uint32_t COLS = 16, DEEP = 4;                              // a block's columns, a thread's rows
@@ -605,7 +611,7 @@ __device__ __forceinline__ void column_tops(const Q8GradientArgs& a, uint32_t n,
 }
 
 // The columns' largest over one slice of rows, 512 columns a block and eight a thread; behind those blocks, the
-// ones that turn the checkpoint.  16384 x 4096 bf16 and as much checkpoint take 54 us: 271 MB, 5 TB/s.
+// ones that turn the checkpoint.  16384 x 4096 bf16 and as much checkpoint take 52 to 58 us: 271 MB, 5 TB/s.
 template <typename T>
 __global__ __launch_bounds__(BLOCK) void q8_tops_kernel(Q8GradientArgs a, Q8GradientPlan pl, uint32_t blocks) {
     __shared__ uint32_t lds[128 * TURN_PITCH];
@@ -628,7 +634,7 @@ __global__ __launch_bounds__(BLOCK) void q8_tops_kernel(Q8GradientArgs a, Q8Grad
 
 // The digits of 64 columns and `deep` times 128 rows, the rows of a column side by side: a thread has eight columns
 // of four rows at a time, and the next ones on their way while it works.  g is read again here because a column's unit is not
-// known before its last row: 16384 x 4096 bf16 takes 70 us, 341 MB, 4.9 TB/s.
+// known before its last row: 16384 x 4096 bf16 takes 68 to 73 us, 341 MB, 4.8 TB/s.
 template <typename T>
 __global__ __launch_bounds__(BLOCK) void q8_digits_kernel(Q8GradientArgs a, Q8GradientPlan pl, uint32_t deep) {
     __shared__ uint32_t lds[3 * 64 * TURN_PITCH];
@@ -728,10 +734,10 @@ __device__ __forceinline__ void store_gradient(const int8_t* from, uint32_t pitc
 
 // dW[n][k] = unit[n] (2^16 D2 + 2^8 D1 + D0), Dp the exact sum of digit plane p of column n times column k of the codes.  One
 // tile of Q serves the three planes, whose sums all stay in registers: 128 x 256 of them fill eight wavefronts' 192
-// accumulators.  16384 x 4096 x 4096 takes 640 to 675 us, 2.5 POP/s over the three products: power, as in the product (with
-// stages of 128 bytes, two for four of 64, 650 to 690).  2048 x 1873 x 977 takes 19 us on tiles of 64 x 128, one on a compute
-// unit: its LDS is read and written 0.5 us for each of 16 stages, so eight wavefronts, of which one reads while another
-// multiplies, take 16.4 us where four with half as many reads take 19 to 20; the rest is a launch, the digits' and the mask's way from memory.
+// accumulators.  16384 x 4096 x 4096 takes 640 to 690 us, 2.5 POP/s over the three products: the matrix units are busy in 69 % of
+// the cycles, at 1.73 GHz as in the product, and LDS reads do not conflict.  2048 x 1873 x 977 takes 20 to 22 us on tiles of 64 x 128,
+// one on a compute unit, the matrix units busy in 36 % of its cycles and the LDS in 27 %: eight wavefronts, of which one reads while
+// another multiplies, take 17.2 us on random digits where four of 64 x 64 take 18.8; the rest is a launch, the digits' and the mask's way from memory.
 template <uint32_t WA, uint32_t WB, uint32_t FA, uint32_t FB, uint32_t NS, uint32_t STEP, uint32_t GROUP>
 __global__ __launch_bounds__(64 * WA * WB) void q8_gradient_kernel(Q8GradientArgs g, Q8GradientPlan pl) {
 

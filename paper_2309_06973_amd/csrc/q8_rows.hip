@@ -6,7 +6,7 @@
 // p is the row itself, its ReLU, or fl(h * weight) of the norm: the norm's common factor
 // 1 / sqrt(mean(h^2) + eps) cancels in the codes and appears in the scale alone, so a row is
 // coded without waiting for its sum of squares.  Codes are exact, that is the same on every
-// machine and for every order of work: see q8_code.
+// machine and for every order of work: see q8_codes.
 //
 // Streaming work: each row is read once into registers, reduced and written.
 #include <algorithm>
@@ -190,8 +190,8 @@ __device__ __forceinline__ void row_values(const Q8RowsArgs& g, uint64_t row, ui
 
 // TPR threads a row, NV times eight elements in the registers of each.  A block takes rows in turn: the norm's
 // weights stay in registers, and the next row is on its way while this one is reduced and coded.  One pass: a row's largest
-// (and mean square) is known before the row leaves the registers.  Memory bounds it: 8192 x 8192 bf16 39 us (201 MB, 5.1
-// TB/s), 16384 x 4096 bf16 with residual 87 us (470 MB, 5.4 TB/s), 3277 x 3541 fp32 11.6 us; single rows of 2048 3 us,
+// (and mean square) is known before the row leaves the registers.  Memory bounds it: 8192 x 8192 bf16 40 to 45 us (201 MB, 4.8
+// TB/s), 16384 x 4096 bf16 with residual 83 to 96 us (470 MB, 5.1 TB/s), 3277 x 3541 fp32 11.5 us; single rows of 2048 3 us,
 // a launch and two trips to memory.  Fewer than 256 threads where a row has no work for them: 65536 x 200 with 16 a row
 // 23 us, with 64 39.
 template <typename T, int FORM, uint32_t TPR, uint32_t NV>
@@ -337,8 +337,8 @@ void launch_q8_rows(shifter_ctx* ctx, int dtype, const Q8RowsArgs& g) {
     else launch_rows_of<_Float16>(ctx, g);
 }
 
-// Eight elements a thread at a time: code * scale, rounded to the element type once.  8192 x 8192 to bf16 takes 30 to 35 us,
-// 201 MB at 5.7 to 6.6 TB/s.
+// Eight elements a thread at a time: code * scale, rounded to the element type once.  8192 x 8192 to bf16 takes 30 to 37 us,
+// 201 MB at 5.4 to 6.6 TB/s (the codes may be in cache).
 template <typename T>
 __global__ __launch_bounds__(BLOCK) void q8_read_kernel(const int8_t* __restrict__ q, uint64_t ld_q,
                                                         const float* __restrict__ scale, uint32_t rows,
