@@ -11,6 +11,7 @@
 #include <ATen/hip/EmptyTensor.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
+#include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "shifter.h"
@@ -49,17 +50,22 @@ void here(const Handle& h, const at::Tensor& x, const char* what) {
     TORCH_CHECK_VALUE(d.is_cuda() && d.index() == h.device, what, " is not on cuda:", (int)h.device);
 }
 
-// Results have no graph.  An 8-bit matrix is a constant to autograd, as whole numbers are; where elements are made from
-// elements, the gradient of those would be lost without a word.
-void constant(const at::Tensor& x, const char* what) {
-    TORCH_CHECK_VALUE(!(x.requires_grad() && at::GradMode::is_enabled()), what,
-                      " needs a gradient, which this call does not pass on: detach it, or call under torch.no_grad()");
+// No operator passes gradients on.  An 8-bit matrix is a constant to autograd, as whole numbers are; where elements are made
+// from elements that need a gradient, that would be lost without a word.
+bool needs_gradient(const at::Tensor& x) { return x.defined() && x.requires_grad() && at::GradMode::is_enabled(); }
+
+// A new result of such elements has an error for its backward pass.
+at::Tensor tied(at::Tensor&& result, const at::Tensor& a, const at::Tensor& b, const char* fn) {
+    if (!needs_gradient(a) && !needs_gradient(b)) return std::move(result);
+    torch::autograd::variable_list all{std::move(result), a, b};
+    const auto error = std::make_shared<torch::autograd::DelayedError>(std::string("q8.") + fn + " passes no gradients on", 3);
+    return (*error)(std::move(all))[0];
 }
 
-// What a caller gives to be written: autograd has to see that it was.
-void writable(const at::Tensor& x, const char* what) {
-    TORCH_CHECK_VALUE(!(x.requires_grad() && at::GradMode::is_enabled()), what,
-                      " needs a gradient, and is written without a graph: detach it, or call under torch.no_grad()");
+// What a caller gives to be written has no such place: neither it nor what it is made from may need a gradient.
+void constant(const at::Tensor& x, const char* what) {
+    TORCH_CHECK_VALUE(!needs_gradient(x), what, " needs a gradient, which a call that writes a given tensor does not pass on: "
+                      "detach it, or call under torch.no_grad()");
 }
 void written(const at::Tensor& x) {
     if (!x.is_inference()) x.unsafeGetTensorImpl()->bump_version();
@@ -204,7 +210,7 @@ at::Tensor result(const Handle& h, uint64_t rows, uint64_t cols, PyObject* dtype
         x = new_rows(h, rows, cols, reinterpret_cast<THPDtype*>(dtype)->scalar_type);
     } else {
         x = tensor_of(out, "out");
-        writable(x, "out");
+        constant(x, "out");
         same(x, rows, cols, x.scalar_type(), "out");
     }
     r = rows_of(h, x, "out");
@@ -291,10 +297,10 @@ PyObject* dequantize(PyObject* const* a) {
 PyObject* rms_norm(PyObject* const* a) {
     const Handle h = handle_of(a);
     const at::Tensor& tx = tensor_of(a[2], "x");
-    if (!is_none(a[5])) {                      // without a residual the stream is x itself, with its graph
+    if (!is_none(a[5]) && !is_none(a[6])) {    // without a residual the stream is x itself, with its graph
         constant(tx, "x");
         constant(tensor_of(a[5], "residual"), "residual");
-        if (!is_none(a[6])) writable(tensor_of(a[6], "h"), "h");
+        constant(tensor_of(a[6], "h"), "h");
     }
     const Rows x = rows_of(h, tx, "x");
     const float* weight = vector_of(h, a[3], x.cols, "weight");
@@ -323,6 +329,7 @@ PyObject* rms_norm(PyObject* const* a) {
                                    stream.ld, m.q, m.ld, m.scale);
     });
     written(a[7]);
+    if (!is_none(a[5]) && is_none(a[6])) sum = tied(std::move(sum), tx, tensor_of(a[5], "residual"), "rms_norm");
     Owned held(is_none(a[5]) ? (Py_INCREF(a[2]), a[2]) : wrap(a[6], std::move(sum)));
     Owned both(PyTuple_New(2));
     PyTuple_SET_ITEM(both.p, 0, out.release());
@@ -333,7 +340,7 @@ PyObject* rms_norm(PyObject* const* a) {
 // ctx, device, a, b, bias, relu, dtype, out -> elements
 PyObject* matmul(PyObject* const* v) {
     const Handle h = handle_of(v);
-    if (!is_none(v[4])) constant(tensor_of(v[4], "bias"), "bias");
+    if (!is_none(v[4]) && !is_none(v[7])) constant(tensor_of(v[4], "bias"), "bias");
     const Codes a = codes_of(h, v[2], "a"), b = codes_of(h, v[3], "b");
     TORCH_CHECK_VALUE(a.cols == b.cols, "a and b have different numbers of columns");
     const float* bias = is_none(v[4]) ? nullptr : vector_of(h, v[4], b.rows, "bias");
@@ -343,6 +350,7 @@ PyObject* matmul(PyObject* const* v) {
     enqueue(v[0], [&] {
         return shifter_matmul_q8(h.ctx, a.q, a.ld, a.scale, b.q, b.ld, b.scale, a.rows, b.rows, a.cols, bias, flags, r.p, r.dtype, r.ld);
     });
+    if (!is_none(v[4]) && is_none(v[7])) c = tied(std::move(c), tensor_of(v[4], "bias"), at::Tensor(), "matmul");
     return wrap(v[7], std::move(c));
 }
 
@@ -350,7 +358,7 @@ PyObject* matmul(PyObject* const* v) {
 PyObject* weight_grad(PyObject* const* a) {
     const Handle h = handle_of(a);
     const at::Tensor& tg = tensor_of(a[2], "g");
-    constant(tg, "g");
+    if (!is_none(a[6])) constant(tg, "g");
     const Rows g = rows_of(h, tg, "g");
     const Codes x = codes_of(h, a[3], "x");
     TORCH_CHECK_VALUE(x.rows == g.rows, "g and x have different numbers of rows");
@@ -377,6 +385,7 @@ PyObject* weight_grad(PyObject* const* a) {
     // with the interpreter's lock: the launches share the handle's workspace, and another thread's stay out from between them
     check(shifter_weight_grad_q8(h.ctx, g.p, g.dtype, g.ld, x.q, x.ld, x.scale, g.rows, g.cols, x.cols,
                                  static_cast<const uint8_t*>(mask.p), mask.ld, flags, static_cast<float*>(r.p), r.ld, work, need), a[0]);
+    if (is_none(a[6])) dw = tied(std::move(dw), tg, at::Tensor(), "weight_grad");
     return wrap(a[6], std::move(dw));
 }
 

@@ -62,9 +62,10 @@ class Q8:
     """The 8-bit operators on one device and stream: the current one, or those of a given context.
     Matrices of elements are two-dimensional fp32, bf16 or fp16 tensors whose columns lie side by
     side; their rows may have any stride.
-    Results are new tensors unless ``out`` (or ``h``) says where they go, and have no graph of
-    autograd's: 8-bit matrices are constants to it, and elements that need a gradient (x and residual
-    of a norm, a bias, g) are refused unless under torch.no_grad().
+    Results are new tensors unless ``out`` (or ``h``) says where they go.  Gradients are not passed
+    on: 8-bit matrices are constants to autograd, and a new tensor made from elements that need a
+    gradient (x and residual of a norm, a bias, g) has an error for its backward pass.  With ``out``
+    or ``h`` such elements are refused, unless under torch.no_grad().
 
     Recorded into a graph, calls of one handle share a workspace apart from that of calls made at
     once: replays of such graphs go one after another, on whatever stream.  The handle is one host
