@@ -144,18 +144,22 @@ def _rows(x: torch.Tensor) -> torch.Tensor:
     return x if (x.shape[1] < 2 or x.stride(1) == 1) and (x.shape[0] < 2 or x.stride(0) >= x.shape[1]) else x.contiguous()
 
 
+def _weight_grad(g: torch.Tensor, ops: Q8, x: Q8Matrix, mask: Optional[torch.Tensor]) -> torch.Tensor:
+    most, dw = S.SHIFTER_Q8_MAX_SUM, None
+    if x.rows <= most:
+        return ops.weight_grad(g, x, mask=mask)
+    for i in range(0, x.rows, most):           # as many rows as a sum holds, the next ones added
+        dw = ops.weight_grad(g[i:i + most], Q8Matrix(x.q[i:i + most], x.scale[i:i + most], x.cols), mask=mask, out=dw,
+                             accumulate=dw is not None)
+    return dw
+
+
 class _WeightGrad(torch.autograd.Function):
-    """weight_grad where it may be differentiated again: an error then.  `link` ties the result to the layer, so
-    that the way from it to the layer's operands leads through here."""
+    """The weights' gradient where it may be differentiated again: an error then.  `link` ties the result to the layer,
+    so that the way from it to the layer's operands leads through here."""
     @staticmethod
     def forward(ctx, g, link, ops, x, mask):
-        most, dw = S.SHIFTER_Q8_MAX_SUM, None
-        if x.rows <= most:
-            return ops.weight_grad(g, x, mask=mask)
-        for i in range(0, x.rows, most):       # as many rows as a sum holds, the next ones added
-            dw = ops.weight_grad(g[i:i + most], Q8Matrix(x.q[i:i + most], x.scale[i:i + most], x.cols), mask=mask, out=dw,
-                                 accumulate=dw is not None)
-        return dw
+        return _weight_grad(g, ops, x, mask)
 
     @staticmethod
     def backward(ctx, v):
@@ -182,7 +186,9 @@ class _Linear(torch.autograd.Function):
         dx = g @ weight.to(g.dtype) if ctx.needs_input_grad[0] else None
         dw = None
         if ctx.needs_input_grad[1]:
-            dw = _WeightGrad.apply(g, link, ctx.ops, Q8Matrix(q, scale, ctx.cols), mask[0] if mask else None).to(weight.dtype)
+            operands = ctx.ops, Q8Matrix(q, scale, ctx.cols), mask[0] if mask else None
+            dw = _WeightGrad.apply(g, link, *operands) if torch.is_grad_enabled() else _weight_grad(g, *operands)
+            dw = dw.to(weight.dtype)
         return dx, dw, None, None
 
 
