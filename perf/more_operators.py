@@ -205,7 +205,7 @@ def _run_own(s):
         if s["top"]:
             outputs.update(top=r.top, index=r.index)
         if s["train"]:
-            outputs["grad"] = ops.log_probs_grad(s["x"], s["target"], r.lse, s["g_logp"], entropy=r.entropy,
+            outputs["grad"] = ops.log_probs_grad(s["x"], s["target"], r.norm, s["g_logp"], entropy=r.entropy,
                                                  g_entropy=s["g_entropy"], scale=s["scale"])
         return outputs
     if s["kind"] == "clip":
