@@ -743,6 +743,72 @@ int shifter_weight_grad_q8(shifter_ctx* ctx, const void* d_g, int dtype, uint64_
                            const uint8_t* d_mask, uint64_t ld_mask, uint32_t flags, float* d_dw,
                            uint64_t ld_dw, void* d_work, uint64_t work_bytes);
 
+/* --- what a network answers with, and what it is trained on ----------------------------- */
+
+/* The ends of a training step between two prunings (Phase 1, Sec. III-C), and of serving: log
+ * probabilities of rows of logits with their gradient, the norm of a network's gradients and
+ * their clipping, and low-rank adapters beside a projection.  None of these calls needs a model;
+ * all of them only enqueue kernels, allocate nothing and can be recorded into a HIP graph.
+ * Element matrices are as those of the 8-bit calls: any start, any stride from a row's length on.
+ *
+ * shifter_log_probs      z = scale x for each of the rows of x, and with log p = z - lse
+ *                        d_norm     rows x 2: m = max x, and log sum e^(scale (x - m))
+ *                        d_lse      log sum e^z
+ *                        d_logp     log p of column d_target[row]: 0 where that is negative (a position that is
+ *                                   left out), NaN where it is not below cols.  NULL with d_target NULL.
+ *                        d_entropy  -sum p log p, or NULL
+ *                        d_top, d_index  rows x top: the largest logits' log p and columns, largest first, of equal
+ *                                   ones the lower column first; NaN counts as minus infinity there.  top up to
+ *                                   SHIFTER_LOG_PROBS_MAX_TOP and up to cols.
+ *                        A logit of minus infinity has probability 0 and adds nothing to the entropy.  A row with NaN or
+ *                        +infinity has NaN everywhere; one that is minus infinity throughout has lse minus infinity and NaN
+ *                        elsewhere; columns and what is left out stay as above.  scale is finite and positive.
+ *                        d_work: work_bytes of shifter_log_probs_layout, NULL where that says 0; see below.
+ * shifter_log_probs_grad dx = scale (g_logp ([column = target] - p) + g_lse p - g_entropy p (log p + entropy)), rounded to
+ *                        x's type, from the gradients of the outputs above (rows each; NULL: none) and norm and entropy as
+ *                        shifter_log_probs wrote them.  d_target NULL: no g_logp.  A row whose target is negative takes
+ *                        no g_logp; one whose target is not below cols is NaN; one whose factors are all 0 is zeros,
+ *                        whatever x holds.  d_dx may be d_x with the same stride.
+ *
+ * Workspaces start on 256 bytes.  Their first SHIFTER_LEARN_ZERO bytes are zero before the first call that is given one; every
+ * call leaves them zero, so that one workspace does for calls of whatever sizes and operators, one after another.  Calls
+ * that may run at the same time have a workspace each. */
+#define SHIFTER_LEARN_ZERO 2048u
+#define SHIFTER_LOG_PROBS_MAX_TOP 32u
+typedef struct {
+    const void* d_x;
+    uint64_t ld_x, rows, cols;
+    const int64_t* d_target;
+    float* d_norm;
+    float* d_lse;
+    float* d_logp;
+    float* d_entropy;
+    float* d_top;
+    int64_t* d_index;
+    void* d_work;
+    uint64_t work_bytes;
+    int dtype;                  /* shifter_dtype of x */
+    uint32_t top;
+    float scale;
+} shifter_log_probs_args;
+typedef struct {
+    const void* d_x;
+    uint64_t ld_x, rows, cols;
+    const int64_t* d_target;
+    const float* d_norm;
+    const float* d_entropy;     /* with d_g_entropy */
+    const float* d_g_logp;
+    const float* d_g_lse;
+    const float* d_g_entropy;
+    void* d_dx;
+    uint64_t ld_dx;
+    int dtype;                  /* of x and dx */
+    float scale;
+} shifter_log_probs_grad_args;
+int shifter_log_probs_layout(uint64_t rows, uint64_t cols, uint32_t top, uint64_t* h_work_bytes);
+int shifter_log_probs(shifter_ctx* ctx, const shifter_log_probs_args* args);
+int shifter_log_probs_grad(shifter_ctx* ctx, const shifter_log_probs_grad_args* args);
+
 /* --- measurement ------------------------------------------------------------------- */
 
 /* Per-kernel timing with HIP events on the context's stream.  While enabled every

@@ -11,6 +11,7 @@
 
 #include "chain.h"
 #include "internal.h"
+#include "learn.h"
 #include "q8.h"
 
 using namespace shifter;
@@ -23,7 +24,8 @@ const char* const kKernelNames[K_COUNT] = {
     "deflate_chunk", "codec_scan", "codec_pack", "inflate_chunk",
     "mask_scan_batch", "expand_levels",
     "spec_sample", "spec_pass", "spec_hist_locate", "spec_filter_rank", "spec_fixup",
-    "q8_rows", "q8_read", "q8_norm", "q8_product", "q8_digits", "q8_gradient"};
+    "q8_rows", "q8_read", "q8_norm", "q8_product", "q8_digits", "q8_gradient",
+    "log_probs", "log_probs_grad", "grad_norm", "grad_clip", "adapters_down", "adapters_up", "adapters_turn", "adapters_grad"};
 
 ProfileScope::ProfileScope(shifter_ctx* c, int id) : ctx(c), idx(-1) {
     if (!c->profiling) return;
@@ -1811,4 +1813,78 @@ extern "C" int shifter_weight_grad_q8(shifter_ctx* ctx, const void* d_g, int dty
     a.work = static_cast<uint8_t*>(d_work);
     launch_q8_gradient(ctx, dtype, a);
     return after_launch(ctx, "weight_grad_q8");
+}
+
+// ---- what a network answers with, and what it is trained on ---------------------------
+
+static_assert(SHIFTER_LOG_PROBS_MAX_TOP == LOGP_MAX_TOP && SHIFTER_LEARN_ZERO == LEARN_TICKETS, "the limits the header names");
+
+static const char* log_probs_bad_sizes(uint64_t rows, uint64_t cols, uint64_t top) {
+    if (rows > Q8_MAX_ROWS || cols > Q8_MAX_ROWS) return "more than 2^31 - 1 rows or columns";
+    if (top > LOGP_MAX_TOP) return "more than 32 alternatives";
+    if (top > cols) return "more alternatives than columns";
+    return nullptr;
+}
+static bool bad_scale(float scale) { return !(scale > 0.0f) || !std::isfinite(scale); }
+
+extern "C" int shifter_log_probs_layout(uint64_t rows, uint64_t cols, uint32_t top, uint64_t* h_work_bytes) {
+    if (!h_work_bytes) return fail(nullptr, SHIFTER_ERR_INVALID_ARG, "log_probs_layout: NULL argument");
+    *h_work_bytes = 0;
+    if (const char* why = log_probs_bad_sizes(rows, cols, top))
+        return fail(nullptr, SHIFTER_ERR_INVALID_ARG, std::string("log_probs_layout: ") + why);
+    *h_work_bytes = log_probs_plan(rows, cols, top).bytes;
+    return SHIFTER_OK;
+}
+
+extern "C" int shifter_log_probs(shifter_ctx* ctx, const shifter_log_probs_args* a) {
+    if (!a) return fail(ctx, SHIFTER_ERR_INVALID_ARG, "log_probs: NULL argument");
+    int rc = q8_enter(ctx, "log_probs", a->dtype, 0, 0);
+    if (rc) return rc;
+    Q8_REFUSE("log_probs", log_probs_bad_sizes(a->rows, a->cols, a->top));
+    Q8_REFUSE("log_probs", q8_bad_rows(a->d_x, element_size(a->dtype), a->rows, a->cols, a->ld_x));
+    if (bad_scale(a->scale)) return fail(ctx, SHIFTER_ERR_INVALID_ARG, "log_probs: scale must be finite and positive");
+    if (a->rows == 0) return SHIFTER_OK;
+    if (!a->d_norm || !a->d_lse || (a->d_target && !a->d_logp) || (a->top && (!a->d_top || !a->d_index)))
+        return fail(ctx, SHIFTER_ERR_INVALID_ARG, "log_probs: NULL pointer argument");
+    if (a->d_logp && !a->d_target) return fail(ctx, SHIFTER_ERR_INVALID_ARG, "log_probs: d_logp without d_target");
+    if (misaligned(a->d_norm, 4) || misaligned(a->d_lse, 4) || misaligned(a->d_logp, 4) || misaligned(a->d_entropy, 4) || misaligned(a->d_top, 4) ||
+        misaligned(a->d_target, 8) || misaligned(a->d_index, 8))
+        return fail(ctx, SHIFTER_ERR_INVALID_ARG, "log_probs: a pointer is not aligned to its elements");
+    const uint64_t need = log_probs_plan(a->rows, a->cols, a->top).bytes;
+    if (a->work_bytes < need)
+        return fail(ctx, SHIFTER_ERR_INVALID_ARG, "log_probs: workspace too small, needs " + std::to_string(need) + " bytes");
+    if (need && (!a->d_work || misaligned(a->d_work, 256)))
+        return fail(ctx, SHIFTER_ERR_INVALID_ARG, "log_probs: the workspace must be 256-byte aligned");
+    LogProbsArgs g{};
+    g.x = a->d_x; g.ld_x = a->ld_x; g.rows = (uint32_t)a->rows; g.cols = (uint32_t)a->cols; g.top = a->top;
+    g.target = a->d_target; g.scale = a->scale;
+    g.norm = a->d_norm; g.lse = a->d_lse; g.logp = a->d_logp; g.entropy = a->d_entropy; g.top_logp = a->d_top; g.index = a->d_index;
+    g.work = static_cast<uint8_t*>(a->d_work);
+    launch_log_probs(ctx, a->dtype, g);
+    return after_launch(ctx, "log_probs");
+}
+
+extern "C" int shifter_log_probs_grad(shifter_ctx* ctx, const shifter_log_probs_grad_args* a) {
+    if (!a) return fail(ctx, SHIFTER_ERR_INVALID_ARG, "log_probs_grad: NULL argument");
+    int rc = q8_enter(ctx, "log_probs_grad", a->dtype, 0, 0);
+    if (rc) return rc;
+    const uintptr_t size = element_size(a->dtype);
+    Q8_REFUSE("log_probs_grad", q8_bad_rows(a->d_x, size, a->rows, a->cols, a->ld_x));
+    Q8_REFUSE("log_probs_grad", q8_bad_rows(a->d_dx, size, a->rows, a->cols, a->ld_dx));
+    if (bad_scale(a->scale)) return fail(ctx, SHIFTER_ERR_INVALID_ARG, "log_probs_grad: scale must be finite and positive");
+    if (a->d_dx == a->d_x && a->ld_dx != a->ld_x && a->rows > 1 && a->cols)
+        return fail(ctx, SHIFTER_ERR_INVALID_ARG, "log_probs_grad: d_dx is d_x with another stride");
+    if (a->rows == 0 || a->cols == 0) return SHIFTER_OK;
+    if (!a->d_norm || (a->d_g_entropy && !a->d_entropy))
+        return fail(ctx, SHIFTER_ERR_INVALID_ARG, "log_probs_grad: NULL pointer argument");
+    if (a->d_g_logp && !a->d_target) return fail(ctx, SHIFTER_ERR_INVALID_ARG, "log_probs_grad: d_g_logp without d_target");
+    if (misaligned(a->d_norm, 4) || misaligned(a->d_entropy, 4) || misaligned(a->d_g_logp, 4) || misaligned(a->d_g_lse, 4) ||
+        misaligned(a->d_g_entropy, 4) || misaligned(a->d_target, 8))
+        return fail(ctx, SHIFTER_ERR_INVALID_ARG, "log_probs_grad: a pointer is not aligned to its elements");
+    LogProbsGradArgs g{};
+    g.x = a->d_x; g.ld_x = a->ld_x; g.ld_dx = a->ld_dx; g.rows = (uint32_t)a->rows; g.cols = (uint32_t)a->cols;
+    g.target = a->d_target; g.scale = a->scale; g.norm = a->d_norm; g.entropy = a->d_entropy;
+    g.g_logp = a->d_g_logp; g.g_entropy = a->d_g_entropy; g.g_lse = a->d_g_lse; g.dx = a->d_dx;
+    launch_log_probs_grad(ctx, a->dtype, g);
+    return after_launch(ctx, "log_probs_grad");
 }

@@ -174,6 +174,7 @@ enum KernelId {
     K_MASK_SCAN_BATCH, K_EXPAND_LEVELS,
     K_SPEC_SAMPLE, K_SPEC_PASS, K_SPEC_FINISH, K_SPEC_FINISH2, K_SPEC_FIXUP,
     K_Q8_ROWS, K_Q8_READ, K_Q8_NORM, K_Q8_PRODUCT, K_Q8_DIGITS, K_Q8_GRADIENT,
+    K_LOG_PROBS, K_LOG_PROBS_GRAD, K_GRAD_NORM, K_GRAD_CLIP, K_ADAPTERS_DOWN, K_ADAPTERS_UP, K_ADAPTERS_TURN, K_ADAPTERS_GRAD,
     K_COUNT
 };
 extern const char* const kKernelNames[K_COUNT];

@@ -1,0 +1,501 @@
+// Log probabilities of given targets, entropies and the likeliest alternatives of rows of logits, and their gradient.
+//
+//   z = scale x,  lse = log sum e^z,  log p = z - lse,  H = -sum p log p
+//
+// One read of x: a thread holds m = max x, s = sum 2^d and u = sum d 2^d with d = (x - m) scale log2 e of what it has seen,
+// and scales s and u when m grows (u' = f (u + D s) for a step of D, f = 2^D).  Sums of two threads join in the same way.  Then
+// lse = scale m + log s and H = log s - (u log 2) / s: no difference of large numbers, u <= 0.  m, s and u are in 32 bits, what is
+// worked out of them in 64.  A logit of minus infinity has no probability and adds nothing, also where all d 2^d
+// would be 0 times infinity; +infinity and NaN make s NaN, and with it whatever the row gives.
+//
+// Alternatives are the largest in the order of (logit, lower index), as one 64-bit number.  While a row is read each thread keeps
+// the largest logit of its own and the eight columns that hold it.  The k-th largest of 64 groups of threads is a bound that
+// k logits at least reach and hardly more than k do (24 of random ones for k = 20), and only the threads that do are looked at again, from the
+// cache: their logits above the bound are ranked by counting.  That leaves one maximum a logit in the loop.
+//
+// Memory bounds long rows; see the figures at the kernels.
+#include <algorithm>
+#include <cmath>
+
+#include "dev_common.h"
+#include "learn.h"
+#include "q8_eight.h"
+
+namespace shifter {
+
+constexpr float LOG2E = 1.44269504088896341f;
+constexpr double LN2 = 0.693147180559945309;
+constexpr float LEAST = -3.402823466e38f;          // where m starts: a row of minus infinities has s = 0
+constexpr float FAR = -1000.0f;                    // 2^FAR is 0 in 32 bits
+
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+
+struct Sums {
+    float m, s, u;
+};
+
+// The sums of both.  The same to the bit whichever comes first, so that all lanes that exchange theirs hold the same.
+template <bool H>
+__device__ __forceinline__ Sums join(const Sums& a, const Sums& b, float c) {
+    const bool first = a.m >= b.m;
+    const float m = first ? a.m : b.m, less = first ? b.m : a.m, s = first ? b.s : a.s;
+    const float d = (less - m) * c, f = exp2_of(d);
+    Sums r;
+    r.m = m;
+    r.s = fmaf(f, s, first ? a.s : b.s);
+    r.u = 0.0f;
+    if constexpr (H) r.u = fmaf(f, fmaf(fmaxf(d, FAR), s, first ? b.u : a.u), first ? a.u : b.u);
+    return r;
+}
+
+// Logits in order as whole numbers, both zeros alike, NaN last with minus infinity; with the column, lower ones first.
+__device__ __forceinline__ uint32_t order_of(float x) {
+    const uint32_t b = __float_as_uint(x + 0.0f);
+    if ((b & 0x7fffffffu) > 0x7f800000u) return 0x007fffffu;
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float logit_of(uint32_t order) {
+    return __uint_as_float(order & 0x80000000u ? order & 0x7fffffffu : ~order);
+}
+__device__ __forceinline__ uint64_t place_of(uint32_t order, uint32_t col) { return (uint64_t)order << 32 | (uint32_t)~col; }
+
+// What a thread has seen of a row.
+struct Best {
+    float x = -INFINITY;
+    uint32_t at = 0xffffffffu;         // first of the eight columns that hold it
+};
+
+// n logits, in pieces of 8 whose first columns are c0, c0 + step, ...
+template <uint32_t N, bool H, bool TOP>
+__device__ __forceinline__ void take(const float (&f)[N], uint32_t c0, uint32_t step, float c, Sums& a, Best& best) {
+    float most = a.m;
+#pragma unroll
+    for (uint32_t p = 0; p < N / 8; ++p) {
+        float top = fmaxf(fmaxf(fmaxf(f[8 * p], f[8 * p + 1]), fmaxf(f[8 * p + 2], f[8 * p + 3])),
+                          fmaxf(fmaxf(f[8 * p + 4], f[8 * p + 5]), fmaxf(f[8 * p + 6], f[8 * p + 7])));
+        most = fmaxf(most, top);
+        if constexpr (TOP) {
+            if (top > best.x || best.at == 0xffffffffu) {
+                best.x = fmaxf(top, -INFINITY);
+                best.at = c0 + p * step;
+            }
+        }
+    }
+    const float d = (a.m - most) * c, g = exp2_of(d);
+    if constexpr (H) a.u = g * fmaf(fmaxf(d, FAR), a.s, a.u);
+    a.s *= g;
+    a.m = most;
+#pragma unroll
+    for (uint32_t i = 0; i < N; ++i) {
+        const float t = (f[i] - most) * c, e = exp2_of(t);
+        a.s += e;
+        if constexpr (H) a.u = fmaf(e, fmaxf(t, FAR), a.u);
+    }
+}
+
+// The columns [c0, end) of a row by TPR threads, U pieces of 8 columns of each under way.
+template <typename T, uint32_t TPR, uint32_t U, bool H, bool TOP>
+__device__ __forceinline__ void scan(const T* row, uint32_t c0, uint32_t end, uint32_t t, float c, Sums& a, Best& best) {
+    constexpr uint32_t STEP = 8 * TPR;
+    uint32_t at = c0;
+    for (; at + U * STEP <= end; at += U * STEP) {
+        Eight<T> e[U];
+        float f[8 * U];
+#pragma unroll
+        for (uint32_t p = 0; p < U; ++p) e[p].load(row + at + p * STEP + 8 * t);
+#pragma unroll
+        for (uint32_t p = 0; p < U; ++p) {
+            float g[8];
+            e[p].floats(g);
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i) f[8 * p + i] = g[i];
+        }
+        take<8 * U, H, TOP>(f, at + 8 * t, STEP, c, a, best);
+    }
+    for (at += 8 * t; at < end; at += STEP) {
+        float f[8];
+        if (at + 8 <= end) {
+            Eight<T> e;
+            e.load(row + at);
+            e.floats(f);
+        } else {
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i) f[i] = at + i < end ? (float)row[at + i] : -INFINITY;
+        }
+        take<8, H, TOP>(f, at, STEP, c, a, best);
+    }
+}
+
+// The TPR threads of a row together.
+template <uint32_t TPR>
+__device__ __forceinline__ void meet() {
+    if constexpr (TPR > 64) {
+        __syncthreads();
+    } else {                            // a wavefront's LDS accesses are done in order
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// LDS of a row.  CAP: places that are ranked at once.
+template <uint32_t TPR, bool TOP>
+struct RowShared {
+    static constexpr uint32_t WAVES = TPR > 64 ? TPR / 64 : 1, CAP = !TOP ? 1 : TPR == 16 ? 128 : TPR == 64 ? 512 : 1024;
+    Sums sums[WAVES];
+    uint64_t group[WAVES][TOP && TPR > 64 ? 64 : 1];
+    uint64_t place[CAP];
+    uint64_t bound;
+    uint32_t count, last;
+};
+
+template <uint32_t TPR, bool H, bool TOP>
+__device__ __forceinline__ Sums sum_up(Sums a, uint32_t t, float c, RowShared<TPR, TOP>& sh) {
+#pragma unroll
+    for (uint32_t d = 1; d < (TPR < 64 ? TPR : 64); d <<= 1) {
+        Sums b;
+        b.m = __shfl_xor(a.m, d, 64);
+        b.s = __shfl_xor(a.s, d, 64);
+        if constexpr (H) b.u = __shfl_xor(a.u, d, 64);
+        a = join<H>(a, b, c);
+    }
+    if constexpr (TPR > 64) {
+        if ((t & 63u) == 0) sh.sums[t / 64] = a;
+        meet<TPR>();
+        a = sh.sums[0];
+#pragma unroll
+        for (uint32_t w = 1; w < TPR / 64; ++w) a = join<H>(a, sh.sums[w], c);
+    }
+    return a;
+}
+
+// The k-th largest of the numbers that the `lanes` lanes of a group of a wavefront hold, or a lower one that no further lane
+// reaches; 0 where fewer than k hold one.  Zero is none.
+template <uint32_t LANES>
+__device__ __forceinline__ uint64_t kth_of(uint64_t v, uint32_t k) {
+    const uint32_t lane = threadIdx.x & 63u;
+    const uint64_t mine = LANES == 64 ? ~0ull : ((1ull << (LANES & 63u)) - 1ull) << (lane / LANES * LANES);
+    uint64_t bound = 0;
+    bool done = false;
+    if constexpr (LANES == 64) done = (uint32_t)__popcll(__ballot(v != 0)) < k;
+    else done = (uint32_t)__popcll(__ballot(v != 0) & mine) < k;
+    for (uint64_t bit = 1ull << 63; bit; bit >>= 1) {
+        const uint32_t n = (uint32_t)__popcll(__ballot(v >= (bound | bit)) & mine);
+        if (!done && n >= k) bound |= bit;
+        if (!done && n == k) done = true;
+        if (__ballot(!done) == 0) break;
+    }
+    return bound;
+}
+
+// Puts the places that `v` holds and that reach the bound on the list, as far as there is room.
+template <uint32_t TPR, bool TOP>
+__device__ __forceinline__ void list(RowShared<TPR, TOP>& sh, uint64_t v, uint64_t bound) {
+    if (v < bound || v == 0) return;
+    const uint32_t n = atomicAdd(&sh.count, 1u);
+    if (n < RowShared<TPR, TOP>::CAP) sh.place[n] = v;
+}
+
+// The k largest of the places that find(bound) lists, place(rank, v) for each.  Where more than the list holds reach the
+// bound, the k-th of those that are on it is a higher one that at least k reach, and they are looked for again: the list's others are
+// out each time.
+template <uint32_t TPR, bool TOP, typename Find, typename Put>
+__device__ __forceinline__ void rank(RowShared<TPR, TOP>& sh, uint32_t t, uint32_t k, uint64_t bound, Find find, Put put) {
+    constexpr uint32_t CAP = RowShared<TPR, TOP>::CAP;
+    for (;;) {
+        if (t == 0) sh.count = 0;
+        meet<TPR>();
+        find(bound);
+        meet<TPR>();
+        const uint32_t n = sh.count, held = min(n, CAP);
+        for (uint32_t i = t; i < held; i += TPR) {
+            const uint64_t v = sh.place[i];
+            uint32_t above = 0;
+            for (uint32_t j = 0; j < held; ++j) above += sh.place[j] > v;
+            if (n <= CAP) {
+                if (above < k) put(above, v);
+            } else if (above == k - 1) {
+                sh.bound = v;
+            }
+        }
+        meet<TPR>();
+        if (n <= CAP) return;
+        bound = sh.bound;
+    }
+}
+
+// A row's results from its sums, by its threads: t its thread, x_t the target's logit.
+struct RowEnd {
+    double most, log_s;                // scale m, log s
+    __device__ __forceinline__ RowEnd(const Sums& a, float scale) : most((double)a.m * scale), log_s(log((double)a.s)) {}
+    __device__ __forceinline__ float of(float x, float m, float scale) const {
+        return (float)(((double)x - (double)m) * scale - log_s);
+    }
+};
+
+template <typename T, uint32_t TPR, bool H, bool TOP>
+__global__ __launch_bounds__(TPR < BLOCK ? BLOCK : TPR) void log_probs_kernel(LogProbsArgs g, LogProbsPlan plan) {
+    constexpr uint32_t AT_ONCE = TPR < BLOCK ? BLOCK / TPR : 1u, U = TPR >= 256 ? (sizeof(T) == 2 ? 4 : 2) : 1;
+    __shared__ RowShared<TPR, TOP> shared[AT_ONCE];
+    const uint32_t t = threadIdx.x % TPR;
+    RowShared<TPR, TOP>& sh = shared[threadIdx.x / TPR];
+    const float c = g.scale * LOG2E;
+    const uint64_t all = (uint64_t)g.rows * plan.parts;
+    for (uint64_t i = (uint64_t)blockIdx.x * AT_ONCE + threadIdx.x / TPR; i < all; i += (uint64_t)gridDim.x * AT_ONCE) {
+        const uint64_t r = plan.parts == 1 ? i : i / plan.parts;
+        const uint32_t part = (uint32_t)(i - r * plan.parts), c0 = part * plan.part_cols, end = min(c0 + plan.part_cols, g.cols);
+        const T* row = static_cast<const T*>(g.x) + r * g.ld_x;
+        // the target's logit is on its way while the row is read
+        int64_t target = -1;
+        float x_t = 0.0f;
+        if (g.target && t == 0) {
+            target = g.target[r];
+            if (target >= 0 && target < (int64_t)g.cols) x_t = (float)row[target];
+        }
+        Sums a{LEAST, 0.0f, 0.0f};
+        Best best;
+        scan<T, TPR, U, H, TOP>(row, c0, end, t, c, a, best);
+        a = sum_up<TPR, H, TOP>(a, t, c, sh);
+
+        uint64_t bound = 0;
+        // the part's own alternatives: as many as are asked for, or all that it has
+        const uint32_t k = TOP ? min(g.top, end - c0) : 0u;
+        auto find = [&](uint64_t least) {
+            if constexpr (TPR < 64) {
+                for (uint32_t at = c0 + 8 * t; at < end; at += 8 * TPR)
+                    for (uint32_t e = at; e < min(at + 8u, end); ++e) list(sh, place_of(order_of((float)row[e]), e), least);
+            } else {
+                const uint32_t pieces = (end - c0 + 8 * TPR - 1) / (8 * TPR), lane = t & 63u;
+                uint64_t seen = __ballot(best.at != 0xffffffffu && place_of(order_of(best.x), best.at) >= least);
+                for (; seen; seen &= seen - 1) {
+                    const uint32_t whose = (t & ~63u) + (uint32_t)__ffsll((unsigned long long)seen) - 1u;
+                    for (uint32_t p = lane; p < pieces; p += 64) {
+                        const uint32_t at = c0 + 8 * (p * TPR + whose);
+                        if (at + 8 <= end) {
+                            Eight<T> e;
+                            float f[8];
+                            e.load(row + at);
+                            e.floats(f);
+#pragma unroll
+                            for (uint32_t j = 0; j < 8; ++j) list(sh, place_of(order_of(f[j]), at + j), least);
+                        } else {
+                            for (uint32_t j = at; j < end; ++j) list(sh, place_of(order_of((float)row[j]), j), least);
+                        }
+                    }
+                }
+            }
+        };
+        if constexpr (TOP) {
+            // the last column that may hold a thread's largest: a place that its logits reach
+            const uint64_t v = best.at == 0xffffffffu ? 0ull : place_of(order_of(best.x), min(best.at + 7u, end - 1u));
+            if constexpr (TPR <= 64) {
+                bound = kth_of<TPR>(v, k);
+            } else {
+                sh.group[t / 64][t & 63u] = v;
+                meet<TPR>();
+                if (t < 64) {
+                    uint64_t most = v;
+#pragma unroll
+                    for (uint32_t w = 1; w < TPR / 64; ++w) most = max(most, sh.group[w][t]);
+                    most = kth_of<64>(most, k);
+                    if (t == 0) sh.bound = most;
+                }
+                meet<TPR>();
+                bound = sh.bound;
+            }
+        }
+
+        auto finish = [&](const Sums& s) {
+            const RowEnd e(s, g.scale);
+            if (t == 0) {
+                g.norm[2 * r] = s.m;
+                g.norm[2 * r + 1] = (float)e.log_s;
+                g.lse[r] = (float)(e.most + e.log_s);
+                if (g.logp) g.logp[r] = target < 0 ? 0.0f : target < (int64_t)g.cols ? e.of(x_t, s.m, g.scale) : NAN;
+                if (H) g.entropy[r] = (float)(e.log_s - LN2 * (double)s.u / (double)s.s);
+            }
+        };
+        auto put = [&](const Sums& s, uint32_t n, uint64_t v) {
+            const float x = logit_of((uint32_t)(v >> 32));
+            g.top_logp[r * g.top + n] = RowEnd(s, g.scale).of(x, s.m, g.scale);
+            g.index[r * g.top + n] = (int64_t)(uint32_t)~(uint32_t)v;
+        };
+        if (plan.parts == 1) {
+            finish(a);
+            if constexpr (TOP) rank(sh, t, k, bound, find, [&](uint32_t n, uint64_t v) { put(a, n, v); });
+            else meet<TPR>();
+            continue;
+        }
+        if constexpr (TPR > 64) {
+            const uint32_t entry = 2 + g.top;          // words of 8 bytes
+            unsigned long long* left = reinterpret_cast<unsigned long long*>(g.work + LEARN_TICKETS) + r * plan.parts * entry;
+            unsigned long long* mine = left + (uint64_t)part * entry;
+            auto leave = [](unsigned long long* p, uint64_t v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
+            auto found = [](const unsigned long long* p) { return (uint64_t)__hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
+            if (t == 0) {
+                leave(mine, (uint64_t)__float_as_uint(a.s) << 32 | __float_as_uint(a.m));
+                leave(mine + 1, __float_as_uint(a.u));
+            }
+            if constexpr (TOP) {
+                for (uint32_t n = k + t; n < g.top; n += TPR) leave(mine + 2 + n, 0);
+                rank(sh, t, k, bound, find, [&](uint32_t n, uint64_t v) { leave(mine + 2 + n, v); });
+            }
+            uint32_t* ticket = reinterpret_cast<uint32_t*>(g.work) + r;
+            if (last_block(ticket, plan.parts, &sh.last)) {
+                // the counter is as it was before the call, for the next one
+                if (t == 0) __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                const uint32_t lane = t & 63u;
+                Sums b{LEAST, 0.0f, 0.0f};
+                uint64_t first = 0;
+                if (lane < plan.parts) {               // every wavefront by itself
+                    const uint64_t ms = found(left + (uint64_t)lane * entry);
+                    b.m = __uint_as_float((uint32_t)ms);
+                    b.s = __uint_as_float((uint32_t)(ms >> 32));
+                    b.u = __uint_as_float((uint32_t)found(left + (uint64_t)lane * entry + 1));
+                    if (TOP) first = found(left + (uint64_t)lane * entry + 2);
+                }
+#pragma unroll
+                for (uint32_t d = 1; d < 64; d <<= 1) {
+                    Sums o;
+                    o.m = __shfl_xor(b.m, d, 64);
+                    o.s = __shfl_xor(b.s, d, 64);
+                    if constexpr (H) o.u = __shfl_xor(b.u, d, 64);
+                    b = join<H>(b, o, c);
+                }
+                finish(b);
+                if constexpr (TOP) {
+                    bound = kth_of<64>(first, g.top);
+                    auto lists = [&](uint64_t least) {
+                        for (uint32_t n = t; n < plan.parts * g.top; n += TPR)
+                            list(sh, found(left + (uint64_t)(n / g.top) * entry + 2 + n % g.top), least);
+                    };
+                    rank(sh, t, g.top, bound, lists, [&](uint32_t n, uint64_t v) { put(b, n, v); });
+                }
+            }
+            meet<TPR>();
+        }
+    }
+}
+
+template <typename T, uint32_t TPR>
+static void launch_log_probs_as(shifter_ctx* ctx, const LogProbsArgs& g, const LogProbsPlan& p) {
+    constexpr uint32_t AT_ONCE = TPR < BLOCK ? BLOCK / TPR : 1u, THREADS = TPR < BLOCK ? BLOCK : TPR;
+    const uint64_t blocks = ((uint64_t)g.rows * p.parts + AT_ONCE - 1u) / AT_ONCE;
+    const uint32_t grid = (uint32_t)std::min<uint64_t>(blocks, LOGP_MAX_BLOCKS);
+    if (g.top && g.entropy) log_probs_kernel<T, TPR, true, true><<<grid, THREADS, 0, ctx->stream>>>(g, p);
+    else if (g.top) log_probs_kernel<T, TPR, false, true><<<grid, THREADS, 0, ctx->stream>>>(g, p);
+    else if (g.entropy) log_probs_kernel<T, TPR, true, false><<<grid, THREADS, 0, ctx->stream>>>(g, p);
+    else log_probs_kernel<T, TPR, false, false><<<grid, THREADS, 0, ctx->stream>>>(g, p);
+}
+
+template <typename T>
+static void launch_log_probs_of(shifter_ctx* ctx, const LogProbsArgs& g) {
+    const LogProbsPlan p = log_probs_plan(g.rows, g.cols, g.top);
+    if (p.threads == 16) launch_log_probs_as<T, 16>(ctx, g, p);
+    else if (p.threads == 64) launch_log_probs_as<T, 64>(ctx, g, p);
+    else launch_log_probs_as<T, 256>(ctx, g, p);
+}
+
+void launch_log_probs(shifter_ctx* ctx, int dtype, const LogProbsArgs& g) {
+    if (g.rows == 0) return;
+    ProfileScope ps(ctx, K_LOG_PROBS);
+    if (dtype == SHIFTER_F32) launch_log_probs_of<float>(ctx, g);
+    else if (dtype == SHIFTER_BF16) launch_log_probs_of<__bf16>(ctx, g);
+    else launch_log_probs_of<_Float16>(ctx, g);
+}
+
+// The gradient, in one read of x: p = 2^((scale (x - m) - log s) log2 e) once more, from the row's m and log s: lse, their sum,
+// would have lost log s where all that is left of a row is the type's lowest value.  A row whose factors are all 0 is zeros,
+// whatever it holds.
+template <typename T, uint32_t TPR, bool H>
+__global__ __launch_bounds__(BLOCK) void log_probs_grad_kernel(LogProbsGradArgs g, uint32_t parts, uint32_t part_cols) {
+    constexpr uint32_t AT_ONCE = BLOCK / TPR, U = 2;
+    const uint32_t t = threadIdx.x % TPR;
+    const uint64_t all = (uint64_t)g.rows * parts;
+    for (uint64_t i = (uint64_t)blockIdx.x * AT_ONCE + threadIdx.x / TPR; i < all; i += (uint64_t)gridDim.x * AT_ONCE) {
+        const uint64_t r = parts == 1 ? i : i / parts;
+        const uint32_t c0 = (uint32_t)(i - r * parts) * part_cols, end = min(c0 + part_cols, g.cols);
+        const T* row = static_cast<const T*>(g.x) + r * g.ld_x;
+        T* out = static_cast<T*>(g.dx) + r * g.ld_dx;
+        const int64_t target = g.target ? g.target[r] : -1;
+        float one = g.g_logp && target >= 0 ? g.g_logp[r] * g.scale : 0.0f;
+        if (target >= (int64_t)g.cols) one = NAN;
+        const float m = g.norm[2 * r], log_s = g.norm[2 * r + 1], all_p = (g.g_lse ? g.g_lse[r] * g.scale : 0.0f) - one;
+        float h = 0.0f, by_h = 0.0f;
+        if constexpr (H) {
+            h = g.entropy[r];
+            by_h = -g.g_entropy[r] * g.scale;
+        }
+        const bool none = all_p == 0.0f && one == 0.0f && by_h == 0.0f;
+        auto value = [&](float x, uint32_t col) {
+            const float d = fmaf(x - m, g.scale, -log_s), p = exp2_of(d * LOG2E);
+            float v = all_p;
+            if constexpr (H) v = fmaf(by_h, fmaxf(d, LEAST) + h, v);
+            v *= p;
+            return col == (uint32_t)target && target >= 0 ? v + one : v;
+        };
+        auto piece = [&](uint32_t at, const Eight<T>& e) {
+            float f[8];
+            e.floats(f);
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) f[j] = value(f[j], at + j);
+            Eight<T> o;
+            o.from(f);
+            o.store(out + at);
+        };
+        if (none) {
+            const float zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+            Eight<T> o;
+            o.from(zero);
+            for (uint32_t at = c0 + 8 * t; at < end; at += 8 * TPR) {
+                if (at + 8 <= end) o.store(out + at);
+                else for (uint32_t j = at; j < end; ++j) out[j] = (T)0.0f;
+            }
+            continue;
+        }
+        uint32_t at = c0;
+        for (; at + U * 8 * TPR <= end; at += U * 8 * TPR) {
+            Eight<T> e[U];
+#pragma unroll
+            for (uint32_t p = 0; p < U; ++p) e[p].load(row + at + 8 * (p * TPR + t));
+#pragma unroll
+            for (uint32_t p = 0; p < U; ++p) piece(at + 8 * (p * TPR + t), e[p]);
+        }
+        for (at += 8 * t; at < end; at += 8 * TPR) {
+            if (at + 8 <= end) {
+                Eight<T> e;
+                e.load(row + at);
+                piece(at, e);
+            } else {
+                for (uint32_t j = at; j < end; ++j) out[j] = (T)value((float)row[j], j);
+            }
+        }
+    }
+}
+
+template <typename T, uint32_t TPR>
+static void launch_log_probs_grad_as(shifter_ctx* ctx, const LogProbsGradArgs& g, uint32_t parts, uint32_t part_cols) {
+    const uint64_t blocks = ((uint64_t)g.rows * parts + BLOCK / TPR - 1u) / (BLOCK / TPR);
+    const uint32_t grid = (uint32_t)std::min<uint64_t>(blocks, LOGP_MAX_BLOCKS);
+    if (g.g_entropy) log_probs_grad_kernel<T, TPR, true><<<grid, BLOCK, 0, ctx->stream>>>(g, parts, part_cols);
+    else log_probs_grad_kernel<T, TPR, false><<<grid, BLOCK, 0, ctx->stream>>>(g, parts, part_cols);
+}
+
+template <typename T>
+static void launch_log_probs_grad_of(shifter_ctx* ctx, const LogProbsGradArgs& g) {
+    const uint32_t cols8 = (g.cols + 7u) & ~7u;
+    if (g.cols <= 256) return launch_log_probs_grad_as<T, 16>(ctx, g, 1, cols8);
+    if (g.cols <= 1024) return launch_log_probs_grad_as<T, 64>(ctx, g, 1, cols8);
+    // parts of 8192 columns at least: blocks that end evenly where rows are long and few
+    const uint32_t parts = std::max(1u, g.cols / 8192u), each = ((g.cols + parts - 1u) / parts + 7u) & ~7u;
+    launch_log_probs_grad_as<T, 256>(ctx, g, (g.cols + each - 1u) / each, each);
+}
+
+void launch_log_probs_grad(shifter_ctx* ctx, int dtype, const LogProbsGradArgs& g) {
+    if (g.rows == 0 || g.cols == 0) return;
+    ProfileScope ps(ctx, K_LOG_PROBS_GRAD);
+    if (dtype == SHIFTER_F32) launch_log_probs_grad_of<float>(ctx, g);
+    else if (dtype == SHIFTER_BF16) launch_log_probs_grad_of<__bf16>(ctx, g);
+    else launch_log_probs_grad_of<_Float16>(ctx, g);
+}
+
+}  // namespace shifter

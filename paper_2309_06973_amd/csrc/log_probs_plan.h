@@ -1,0 +1,46 @@
+// Log probabilities: how a call's rows are shared out, its workspace and the checks of its sizes.  Plain C++: the host
+// and the tests share it.
+#pragma once
+
+#include "q8_plan.h"
+
+namespace shifter {
+
+constexpr uint32_t LOGP_MAX_TOP = 32;              // alternatives of a row
+constexpr uint32_t LOGP_MAX_PARTS = 64;            // parts of a row: a wavefront joins them
+constexpr uint64_t LOGP_SHARED_ROWS = 512;         // only fewer rows than these are shared by blocks
+// The front of a workspace of a call whose blocks join their sums: counters, zero before a call and after it.
+constexpr uint64_t LEARN_TICKETS = 4 * LOGP_SHARED_ROWS;
+constexpr uint64_t LOGP_MAX_BLOCKS = 1u << 21;     // a launch holds less than 2^32 threads; blocks take further rows in turn
+
+struct LogProbsPlan {
+    uint32_t threads;      // of a row's part: 16 or 64, several rows a block; 256 or 1024, a block
+    uint32_t parts;        // blocks that share a row; the last of them joins their sums
+    uint32_t part_cols;    // columns of a part, a multiple of 8
+    uint64_t bytes;        // of the workspace, 0: none needed
+};
+
+inline uint64_t logp_entry(uint32_t top) { return 16u + 8u * (uint64_t)top; }      // what a part leaves: its sums, its alternatives
+
+// Rows up to 256 columns have 16 threads each, up to 1024 a wavefront, longer ones a block; and where there are too few
+// rows to fill the chip, several blocks.
+inline LogProbsPlan log_probs_plan(uint64_t rows, uint64_t cols, uint32_t top) {
+    LogProbsPlan p{};
+    p.parts = 1;
+    p.part_cols = (uint32_t)((cols + 7u) & ~7ull);
+    if (cols <= 256 && top <= 8) p.threads = 16;
+    else if (cols <= 1024) p.threads = 64;
+    else p.threads = 256;
+    if (cols > 8192 && rows < LOGP_SHARED_ROWS) {
+        uint64_t parts = (LOGP_SHARED_ROWS + rows - 1u) / (rows ? rows : 1u);
+        if (parts > cols / 4096u) parts = cols / 4096u;
+        if (parts > LOGP_MAX_PARTS) parts = LOGP_MAX_PARTS;
+        const uint64_t each = ((cols + parts - 1u) / parts + 7u) & ~7ull;
+        p.part_cols = (uint32_t)each;
+        p.parts = (uint32_t)((cols + each - 1u) / each);
+    }
+    if (p.parts > 1) p.bytes = LEARN_TICKETS + rows * p.parts * logp_entry(top);
+    return p;
+}
+
+}  // namespace shifter

@@ -389,6 +389,149 @@ PyObject* weight_grad(PyObject* const* a) {
     return wrap(a[6], std::move(dw));
 }
 
+// ---- what a network answers with, and what it is trained on ----
+
+// A workspace of `need` bytes at least, from room(need); nothing where none is needed.
+struct Work {
+    PyObject* held = nullptr;
+    void* p = nullptr;
+    Work(PyObject* room, uint64_t need) {
+        if (!need) return;
+        held = PyObject_CallFunction(room, "K", (unsigned long long)need);
+        if (!held) throw PythonError();
+        p = tensor_of(held, "work").data_ptr();
+    }
+    Work(const Work&) = delete;
+    ~Work() { Py_XDECREF(held); }
+};
+
+float number_of(PyObject* o) {
+    const double v = PyFloat_AsDouble(o);
+    if (PyErr_Occurred()) throw PythonError();
+    return (float)v;
+}
+
+// A vector of whole numbers, one a row: targets, adapters.
+const int64_t* numbers_of(const Handle& h, PyObject* o, uint64_t n, const char* what) {
+    const at::Tensor& v = tensor_of(o, what);
+    TORCH_CHECK_VALUE(v.scalar_type() == at::kLong && v.dim() == 1 && (uint64_t)v.size(0) == n && v.is_contiguous(), what,
+                      " must be a contiguous int64 vector of ", n);
+    here(h, v, what);
+    return static_cast<const int64_t*>(v.data_ptr());
+}
+
+// ctx, device, x, target, scale, entropy, top, room -> (logp, lse, entropy, top, index, norm), None for what is not asked for
+PyObject* log_probs(PyObject* const* a) {
+    const Handle h = handle_of(a);
+    const at::Tensor& tx = tensor_of(a[2], "x");
+    const Rows x = rows_of(h, tx, "x");
+    shifter_log_probs_args g{};
+    g.d_x = x.p;
+    g.ld_x = x.ld;
+    g.rows = x.rows;
+    g.cols = x.cols;
+    g.dtype = x.dtype;
+    g.scale = number_of(a[4]);
+    const bool entropy = truth(a[5]);
+    const long top = PyLong_AsLong(a[6]);
+    if (PyErr_Occurred()) throw PythonError();
+    TORCH_CHECK_VALUE(top >= 0 && top <= (long)SHIFTER_LOG_PROBS_MAX_TOP && (uint64_t)top <= x.cols, "top must be 0 to ",
+                      SHIFTER_LOG_PROBS_MAX_TOP, " and not above the columns");
+    g.top = (uint32_t)top;
+    const bool given = !is_none(a[3]);
+    if (given) g.d_target = numbers_of(h, a[3], x.rows, "target");
+    const int64_t rows = (int64_t)x.rows;
+    at::Tensor out[6];
+    // the vectors in one allocation
+    out[5] = new_tensor(h, {rows * (3 + given + entropy)}, at::kFloat);
+    float* at = static_cast<float*>(out[5].data_ptr());
+    int64_t used = 2 * rows;
+    auto vector = [&](at::Tensor& v) {
+        v = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(out[5].storage()), out[5].key_set(), out[5].dtype());
+        v.unsafeGetTensorImpl()->set_storage_offset(used);
+        v.unsafeGetTensorImpl()->set_sizes_contiguous({rows});
+        float* p = at + used;
+        used += rows;
+        return p;
+    };
+    g.d_norm = at;
+    g.d_lse = vector(out[1]);
+    if (given) g.d_logp = vector(out[0]);
+    if (entropy) g.d_entropy = vector(out[2]);
+    out[5].unsafeGetTensorImpl()->set_sizes_contiguous({rows, 2});
+    if (top) {
+        out[3] = new_tensor(h, {rows, top}, at::kFloat);
+        out[4] = new_tensor(h, {rows, top}, at::kLong);
+    }
+    g.d_top = top ? static_cast<float*>(out[3].data_ptr()) : nullptr;
+    g.d_index = top ? static_cast<int64_t*>(out[4].data_ptr()) : nullptr;
+    check(shifter_log_probs_layout(g.rows, g.cols, g.top, &g.work_bytes), Py_None);
+    const Work work(a[7], g.work_bytes);
+    g.d_work = work.p;
+    enqueue(a[0], [&] { return shifter_log_probs(h.ctx, &g); });
+    Owned all(PyTuple_New(6));
+    for (int i = 0; i < 6; ++i) {
+        if (!out[i].defined()) {
+            Py_INCREF(Py_None);
+            PyTuple_SET_ITEM(all.p, i, Py_None);
+        } else {
+            PyTuple_SET_ITEM(all.p, i, THPVariable_Wrap(i != 4 ? tied(std::move(out[i]), tx, at::Tensor(), "log_probs") : std::move(out[i])));
+        }
+    }
+    return all.release();
+}
+
+// ctx, device, x, target, norm, g_logp, g_lse, entropy, g_entropy, scale, out -> dx
+PyObject* log_probs_grad(PyObject* const* a) {
+    const Handle h = handle_of(a);
+    const at::Tensor& tx = tensor_of(a[2], "x");
+    if (!is_none(a[10])) {
+        constant(tx, "x");
+        for (int i : {5, 6, 8})
+            if (!is_none(a[i])) constant(tensor_of(a[i], "a gradient"), "a gradient");
+    }
+    const Rows x = rows_of(h, tx, "x");
+    shifter_log_probs_grad_args g{};
+    g.d_x = x.p;
+    g.ld_x = x.ld;
+    g.rows = x.rows;
+    g.cols = x.cols;
+    g.dtype = x.dtype;
+    if (!is_none(a[3])) g.d_target = numbers_of(h, a[3], x.rows, "target");
+    const at::Tensor& norm = tensor_of(a[4], "norm");
+    TORCH_CHECK_VALUE(norm.scalar_type() == at::kFloat && norm.dim() == 2 && (uint64_t)norm.size(0) == x.rows && norm.size(1) == 2 &&
+                      norm.is_contiguous(), "norm must be a contiguous float32 tensor of ", x.rows, " rows of 2");
+    here(h, norm, "norm");
+    g.d_norm = static_cast<const float*>(norm.data_ptr());
+    if (!is_none(a[5])) g.d_g_logp = vector_of(h, a[5], x.rows, "g_logp");
+    if (!is_none(a[6])) g.d_g_lse = vector_of(h, a[6], x.rows, "g_lse");
+    if (!is_none(a[8])) {
+        TORCH_CHECK_VALUE(!is_none(a[7]), "g_entropy without entropy");
+        g.d_entropy = vector_of(h, a[7], x.rows, "entropy");
+        g.d_g_entropy = vector_of(h, a[8], x.rows, "g_entropy");
+    }
+    TORCH_CHECK_VALUE(!g.d_g_logp || g.d_target || x.rows == 0, "g_logp without target");
+    g.scale = number_of(a[9]);
+    at::Tensor dx;
+    if (is_none(a[10])) {
+        dx = new_rows(h, x.rows, x.cols, tx.scalar_type());
+    } else {
+        dx = tensor_of(a[10], "out");
+        constant(dx, "out");
+        same(dx, x.rows, x.cols, tx.scalar_type(), "out");
+    }
+    const Rows r = rows_of(h, dx, "out");
+    g.d_dx = r.p;
+    g.ld_dx = r.ld;
+    enqueue(a[0], [&] { return shifter_log_probs_grad(h.ctx, &g); });
+    if (is_none(a[10])) {
+        dx = tied(std::move(dx), tx, is_none(a[5]) ? at::Tensor() : tensor_of(a[5], "g_logp"), "log_probs_grad");
+        for (int i : {6, 8})
+            if (!is_none(a[i])) dx = tied(std::move(dx), tensor_of(a[i], "a gradient"), at::Tensor(), "log_probs_grad");
+    }
+    return wrap(a[10], std::move(dx));
+}
+
 // Q8Matrix, failed(code, ctx): what the functions below make and raise.
 PyObject* bind(PyObject* const* a) {
     Py_INCREF(a[0]);
@@ -400,7 +543,7 @@ PyObject* bind(PyObject* const* a) {
 
 #define Q8_ENTRY(name, n) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&entry<n, name>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {Q8_ENTRY(bind, 2), Q8_ENTRY(quantize, 5), Q8_ENTRY(dequantize, 5), Q8_ENTRY(rms_norm, 8),
-                         Q8_ENTRY(matmul, 8), Q8_ENTRY(weight_grad, 9), {nullptr, nullptr, 0, nullptr}};
+                         Q8_ENTRY(matmul, 8), Q8_ENTRY(weight_grad, 9), Q8_ENTRY(log_probs, 8), Q8_ENTRY(log_probs_grad, 11), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_q8", "The 8-bit operators' calls; see q8.py.", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
 

@@ -9,7 +9,7 @@ from __future__ import annotations
 import importlib.machinery
 import importlib.util
 import os
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -41,6 +41,16 @@ class Q8Matrix:
         self.ld = q.stride(0) if self.rows > 1 and cols else pad
         if self.rows and cols and q.storage_offset() + (self.rows - 1) * self.ld + pad > q.untyped_storage().nbytes():
             raise ValueError("the last row's buffer ends before its columns rounded up to 16")
+
+
+class LogProbs(NamedTuple):
+    """What Q8.log_probs returns; None for what was not asked for."""
+    logp: Optional[torch.Tensor]           # [rows] of the targets
+    lse: torch.Tensor                      # [rows] log sum exp
+    entropy: Optional[torch.Tensor]        # [rows]
+    top: Optional[torch.Tensor]            # [rows, top] log probabilities, largest first
+    index: Optional[torch.Tensor]          # [rows, top] their columns
+    norm: torch.Tensor                     # [rows, 2] what log_probs_grad works from: max x, log sum exp (z - scale max x)
 
 
 def load_calls():
@@ -85,6 +95,7 @@ class Q8:
         self.stream = self.ctx.stream
         self.work = None
         self.recorded = []                 # workspaces of recorded calls, which use them at every replay
+        self.joined, self.recorded_joined = None, []       # the same for calls whose blocks join their sums: they start with zeros
         self._calls = load_calls()
 
     def close(self):
@@ -108,6 +119,19 @@ class Q8:
                 self.recorded.append(work)
             else:
                 self.work = work
+        return work
+
+    def _joined(self, need: int) -> torch.Tensor:
+        """The same for the calls that find zeros at its front and leave zeros there: none else may write it."""
+        recording = torch.cuda.is_current_stream_capturing()
+        work = (self.recorded_joined[-1] if self.recorded_joined else None) if recording else self.joined
+        if work is None or work.numel() < need:
+            work = torch.empty(need, dtype=torch.uint8, device=self.dev)
+            work[:S.SHIFTER_LEARN_ZERO].zero_()            # a kernel; recorded too, and replayed before the call that needs it
+            if recording:
+                self.recorded_joined.append(work)
+            else:
+                self.joined = work
         return work
 
     # ---- the operators --------------------------------------------------------------
@@ -137,6 +161,22 @@ class Q8:
         layer's weights.  mask: uint8, what of the gradient is kept (as apply_mask writes it);
         accumulate: added to ``out``.  Up to SHIFTER_Q8_MAX_SUM rows a call."""
         return self._calls.weight_grad(*self._enter(), g, x, mask, torch.float32, out, accumulate, self._room)
+
+    def log_probs(self, x: torch.Tensor, target: Optional[torch.Tensor] = None, scale: float = 1.0, entropy: bool = False,
+                  top: int = 0) -> LogProbs:
+        """Of each row z = scale * x: log sum exp z, the log probability of column target[row] (int64; 0 where
+        it is negative, NaN where it is not below the columns), the entropy, and the ``top`` largest log
+        probabilities (up to SHIFTER_LOG_PROBS_MAX_TOP; equal logits: the lower column first) with their columns.  All
+        numbers are fp32.  Minus infinity has probability 0; a row with NaN or infinity is NaN."""
+        return LogProbs(*self._calls.log_probs(*self._enter(), x, target, scale, entropy, top, self._joined))
+
+    def log_probs_grad(self, x: torch.Tensor, target: Optional[torch.Tensor], norm: torch.Tensor,
+                       g_logp: Optional[torch.Tensor] = None, g_lse: Optional[torch.Tensor] = None,
+                       entropy: Optional[torch.Tensor] = None, g_entropy: Optional[torch.Tensor] = None, scale: float = 1.0,
+                       out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """x's gradient in x's type, from the gradients of log_probs' results (fp32 vectors, None: none); norm, and
+        entropy with g_entropy, as log_probs gave them.  ``out`` may be x."""
+        return self._calls.log_probs_grad(*self._enter(), x, target, norm, g_logp, g_lse, entropy, g_entropy, scale, out)
 
 
 def _rows(x: torch.Tensor) -> torch.Tensor:
@@ -205,3 +245,50 @@ def checkpointed_linear(x: torch.Tensor, weight: torch.Tensor, ops: Q8, mask: Op
         return _Linear.apply(x, weight, ops, mask)[0]
     rows = x.reshape(x.shape[:-1].numel(), x.shape[-1])
     return _Linear.apply(rows, weight, ops, mask)[0].view(*x.shape[:-1], weight.shape[0])
+
+
+def _recording(what: str, *tensors: torch.Tensor):
+    """A backward pass is recorded by recording the gradient's own call."""
+    if torch.cuda.is_current_stream_capturing() and torch.is_grad_enabled() and any(t.requires_grad for t in tensors):
+        raise RuntimeError(f"{what} can not be recorded where a gradient is needed: record the handle's calls, the gradient's too")
+
+
+class _LogProbsGrad(torch.autograd.Function):
+    """x's gradient where it may be differentiated again: an error then."""
+    @staticmethod
+    def forward(ctx, x, g_logp, g_entropy, g_lse, ops, target, norm, entropy, scale):
+        return ops.log_probs_grad(x, target, norm, g_logp, g_lse, entropy, g_entropy, scale)
+
+    @staticmethod
+    def backward(ctx, v):
+        raise RuntimeError("target_log_probs: x's gradient has no derivative of its own")
+
+
+class _LogProbs(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, target, ops, scale):
+        r = ops.log_probs(x, target, scale=scale, entropy=True)
+        ctx.save_for_backward(x, target, r.norm, r.entropy)
+        ctx.ops, ctx.scale = ops, scale
+        ctx.set_materialize_grads(False)
+        return r.logp, r.entropy, r.lse
+
+    @staticmethod
+    def backward(ctx, *grads):
+        x, target, norm, entropy = ctx.saved_tensors
+        if all(g is None for g in grads):
+            return None, None, None, None
+        g_logp, g_entropy, g_lse = (None if g is None else g.contiguous() for g in grads)
+        dx = _LogProbsGrad.apply(x, g_logp, g_entropy, g_lse, ctx.ops, target, norm, entropy.detach(), ctx.scale)
+        return dx, None, None, None
+
+
+def target_log_probs(x: torch.Tensor, target: torch.Tensor, ops: Q8, scale: float = 1.0):
+    """(log probabilities of the targets, entropies, log sum exp) of the rows of scale * x [..., columns], fp32 [...]:
+    Q8.log_probs with its gradient.  target: int64 [...], negative: left out (0, without gradient).  The gradient can
+    not be differentiated again, which is an error, and not be recorded: log_probs and log_probs_grad can."""
+    if target.shape != x.shape[:-1]:
+        raise ValueError("target must have x's shape without its last dimension")
+    _recording("target_log_probs", x)
+    rows = _rows(x.reshape(target.numel(), x.shape[-1]))
+    return tuple(t.view(target.shape) for t in _LogProbs.apply(rows, target.reshape(-1).contiguous(), ops, scale))

@@ -71,6 +71,21 @@ class PortfolioArgs(C.Structure):
                 ("cap_v", C.c_uint64)]
 
 
+class LogProbsArgs(C.Structure):
+    _fields_ = [("d_x", C.c_void_p), ("ld_x", C.c_uint64), ("rows", C.c_uint64), ("cols", C.c_uint64),
+                ("d_target", C.c_void_p), ("d_norm", C.c_void_p), ("d_lse", C.c_void_p),
+                ("d_logp", C.c_void_p), ("d_entropy", C.c_void_p), ("d_top", C.c_void_p), ("d_index", C.c_void_p),
+                ("d_work", C.c_void_p), ("work_bytes", C.c_uint64), ("dtype", C.c_int),
+                ("top", C.c_uint32), ("scale", C.c_float)]
+
+
+class LogProbsGradArgs(C.Structure):
+    _fields_ = [("d_x", C.c_void_p), ("ld_x", C.c_uint64), ("rows", C.c_uint64), ("cols", C.c_uint64),
+                ("d_target", C.c_void_p), ("d_norm", C.c_void_p), ("d_entropy", C.c_void_p),
+                ("d_g_logp", C.c_void_p), ("d_g_lse", C.c_void_p), ("d_g_entropy", C.c_void_p),
+                ("d_dx", C.c_void_p), ("ld_dx", C.c_uint64), ("dtype", C.c_int), ("scale", C.c_float)]
+
+
 _fold_fields = operator.attrgetter("tensor", "gamma", "beta", "mean", "var", "bias", "out_offset")
 _fold_row = struct.Struct("=IiiiiiQ").pack      # a FoldDesc
 
@@ -133,6 +148,9 @@ EXPORTS = {
                                C.c_void_p, C.c_uint64, C.c_uint64, C.c_uint64, C.c_void_p,
                                C.c_uint64, C.c_uint32, C.c_void_p, C.c_uint64, C.c_void_p,
                                C.c_uint64],
+    "shifter_log_probs_layout": [C.c_uint64, C.c_uint64, C.c_uint32, C.POINTER(C.c_uint64)],
+    "shifter_log_probs": [C.c_void_p, C.POINTER(LogProbsArgs)],
+    "shifter_log_probs_grad": [C.c_void_p, C.POINTER(LogProbsGradArgs)],
     "shifter_apply_mask": [C.c_void_p] * 8,
     "shifter_dead_channel_scan": [C.c_void_p] * 5,
     "shifter_propagate_groups": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint32,
@@ -496,6 +514,33 @@ def shifter_weight_grad_q8(ctx: Context, d_g, dtype: int, ld_g: int, d_q, ld_q: 
                                                  work_bytes), ctx.handle)
 
 
+SHIFTER_LEARN_ZERO = 2048
+SHIFTER_LOG_PROBS_MAX_TOP = 32
+
+
+def _filled(struct, fields):
+    """A call's argument structure: tensors become their addresses."""
+    return struct(**{n: v.data_ptr() if hasattr(v, "data_ptr") else v for n, v in fields.items()})
+
+
+def shifter_log_probs_layout(rows: int, cols: int, top: int) -> int:
+    """Bytes of workspace that shifter_log_probs takes for these sizes."""
+    out = C.c_uint64()
+    _check(load_library().shifter_log_probs_layout(rows, cols, top, C.byref(out)))
+    return int(out.value)
+
+
+def shifter_log_probs(ctx: Context, **fields) -> None:
+    """fields: those of LogProbsArgs; what is left out is 0 or NULL."""
+    _check(load_library().shifter_log_probs(ctx.handle, C.byref(_filled(LogProbsArgs, fields))), ctx.handle)
+
+
+def shifter_log_probs_grad(ctx: Context, **fields) -> None:
+    """fields: those of LogProbsGradArgs; what is left out is 0 or NULL."""
+    _check(load_library().shifter_log_probs_grad(ctx.handle, C.byref(_filled(LogProbsGradArgs, fields))),
+           ctx.handle)
+
+
 def shifter_portfolio_begin(ctx: Context, model: Model, d_w, d_vecs, n_prune: Sequence[int],
                             flags: int, d_thr, d_w_sparse, w_stride: int, d_mask, mask_stride: int,
                             d_out_alive, d_in_alive, d_group_alive, d_index_map, d_keep,
@@ -683,7 +728,7 @@ def shifter_profile_enable(ctx: Context, on: bool) -> None:
 
 def shifter_profile_read(ctx: Context):
     """Returns {kernel name: (launch count, total ms)} since the last read."""
-    cap = 32
+    cap = 64
     names = (C.c_char_p * cap)()
     counts = (C.c_uint32 * cap)()
     ms = (C.c_double * cap)()
