@@ -770,6 +770,16 @@ int shifter_weight_grad_q8(shifter_ctx* ctx, const void* d_g, int dtype, uint64_
  *                        no g_logp; one whose target is not below cols is NaN; one whose factors are all 0 is zeros,
  *                        whatever x holds.  d_dx may be d_x with the same stride.
  *
+ * shifter_grad_norm      d_norm = sqrt of the sum of the squares of all elements of `count` tensors, worked out in 64 bits and
+ *                        rounded once; where a tensor has a mask (as shifter_apply_mask writes them), elements
+ *                        whose byte is 0 do not count, whatever they hold.  0 for no elements.
+ * shifter_clip_grad_norm the same, and each tensor times min(1, max_norm / (norm + 1e-6)) to its d_out, rounded to its
+ *                        type; masked elements become 0.  A norm that is NaN makes all others NaN, an infinite one makes
+ *                        finite elements 0 and others NaN.  max_norm is not negative.  d_out may be d_g; apart from that no
+ *                        tensor that is written may overlap another one.
+ *                        Tensors are runs of elements of any start, with types of their own; h_grads is a host array that is
+ *                        not used after the call returns.  d_out is not read by shifter_grad_norm.
+ *
  * Workspaces start on 256 bytes.  Their first SHIFTER_LEARN_ZERO bytes are zero before the first call that is given one; every
  * call leaves them zero, so that one workspace does for calls of whatever sizes and operators, one after another.  Calls
  * that may run at the same time have a workspace each. */
@@ -805,6 +815,18 @@ typedef struct {
     int dtype;                  /* of x and dx */
     float scale;
 } shifter_log_probs_grad_args;
+typedef struct {
+    const void* d_g;
+    void* d_out;
+    const uint8_t* d_mask;      /* or NULL */
+    uint64_t n;
+    int dtype;                  /* shifter_dtype of d_g and d_out */
+} shifter_grad;
+int shifter_grad_norm_layout(uint64_t count, uint64_t* h_work_bytes);
+int shifter_grad_norm(shifter_ctx* ctx, const shifter_grad* h_grads, uint64_t count, float* d_norm, void* d_work,
+                      uint64_t work_bytes);
+int shifter_clip_grad_norm(shifter_ctx* ctx, const shifter_grad* h_grads, uint64_t count, float max_norm,
+                           float* d_norm, void* d_work, uint64_t work_bytes);
 int shifter_log_probs_layout(uint64_t rows, uint64_t cols, uint32_t top, uint64_t* h_work_bytes);
 int shifter_log_probs(shifter_ctx* ctx, const shifter_log_probs_args* args);
 int shifter_log_probs_grad(shifter_ctx* ctx, const shifter_log_probs_grad_args* args);

@@ -84,3 +84,15 @@ class Logs:
         want[none] = 0.0
         off[none] = 0.0
         return want * self.scale, off * self.scale * (1 + 2 * U) + 2 * U * np.abs(want * self.scale)
+
+
+def clipped(grads, max_norm, masks=None):
+    """(norm, results) in float64."""
+    kept = [g.detach().cpu().double() if masks is None or masks[i] is None else
+            torch.where(masks[i].cpu() != 0, g.detach().cpu().double(), 0.0) for i, g in enumerate(grads)]
+    norm = float(torch.sqrt(sum((k * k).sum() for k in kept) + torch.zeros((), dtype=torch.float64)))
+    by = max_norm / (norm + 1e-6)
+    factor = 1.0 if by >= 1.0 else by              # NaN stays
+    return norm, [torch.where(k == 0, k, k * factor) if np.isfinite(factor) else
+                  (k * factor if masks is None or masks[i] is None else torch.where(masks[i].cpu() != 0, k * factor, 0.0))
+                  for i, k in enumerate(kept)]

@@ -1888,3 +1888,51 @@ extern "C" int shifter_log_probs_grad(shifter_ctx* ctx, const shifter_log_probs_
     launch_log_probs_grad(ctx, a->dtype, g);
     return after_launch(ctx, "log_probs_grad");
 }
+
+extern "C" int shifter_grad_norm_layout(uint64_t count, uint64_t* h_work_bytes) {
+    if (!h_work_bytes) return fail(nullptr, SHIFTER_ERR_INVALID_ARG, "grad_norm_layout: NULL argument");
+    *h_work_bytes = 0;
+    if (count >> 32) return fail(nullptr, SHIFTER_ERR_INVALID_ARG, "grad_norm_layout: 2^32 tensors or more");
+    *h_work_bytes = grad_norm_bytes(count);
+    return SHIFTER_OK;
+}
+
+static int grad_norm_call(shifter_ctx* ctx, const char* fn, const shifter_grad* h, uint64_t count, bool clip, float max_norm,
+                          float* d_norm, void* d_work, uint64_t work_bytes) {
+    int rc = q8_enter(ctx, fn, SHIFTER_F32, 0, 0);
+    if (rc) return rc;
+    const std::string name = std::string(fn) + ": ";
+    if ((count && !h) || !d_norm || !d_work) return fail(ctx, SHIFTER_ERR_INVALID_ARG, name + "NULL pointer argument");
+    if (count >> 32) return fail(ctx, SHIFTER_ERR_INVALID_ARG, name + "2^32 tensors or more");
+    if (misaligned(d_norm, 4)) return fail(ctx, SHIFTER_ERR_INVALID_ARG, name + "a pointer is not aligned to its elements");
+    if (clip && !(max_norm >= 0.0f)) return fail(ctx, SHIFTER_ERR_INVALID_ARG, name + "max_norm must not be negative");
+    if (const char* why = grad_bad(h, count, clip)) return fail(ctx, SHIFTER_ERR_INVALID_ARG, name + why);
+    if (work_bytes < grad_norm_bytes(count))
+        return fail(ctx, SHIFTER_ERR_INVALID_ARG, name + "workspace too small, needs " + std::to_string(grad_norm_bytes(count)) + " bytes");
+    if (misaligned(d_work, 256)) return fail(ctx, SHIFTER_ERR_INVALID_ARG, name + "the workspace must be 256-byte aligned");
+    std::vector<shifter_grad> all;
+    all.reserve(count);
+    for (uint64_t i = 0; i < count; ++i)
+        if (h[i].n) all.push_back(h[i]);
+    if (clip && grad_overlap(all)) return fail(ctx, SHIFTER_ERR_INVALID_ARG, name + "a tensor that is written overlaps another one");
+    launch_grad_norm(ctx, all, clip, max_norm, d_norm, static_cast<uint8_t*>(d_work));
+    return after_launch(ctx, fn);
+}
+
+extern "C" int shifter_grad_norm(shifter_ctx* ctx, const shifter_grad* h_grads, uint64_t count, float* d_norm, void* d_work,
+                                 uint64_t work_bytes) {
+    try {
+        return grad_norm_call(ctx, "grad_norm", h_grads, count, false, 0.0f, d_norm, d_work, work_bytes);
+    } catch (const std::bad_alloc&) {
+        return SHIFTER_ERR_OOM;
+    }
+}
+
+extern "C" int shifter_clip_grad_norm(shifter_ctx* ctx, const shifter_grad* h_grads, uint64_t count, float max_norm, float* d_norm,
+                                      void* d_work, uint64_t work_bytes) {
+    try {
+        return grad_norm_call(ctx, "clip_grad_norm", h_grads, count, true, max_norm, d_norm, d_work, work_bytes);
+    } catch (const std::bad_alloc&) {
+        return SHIFTER_ERR_OOM;
+    }
+}

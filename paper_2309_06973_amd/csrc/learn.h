@@ -2,6 +2,7 @@
 #pragma once
 
 #include "internal.h"
+#include "grad_norm_plan.h"
 #include "log_probs_plan.h"
 
 namespace shifter {
@@ -32,5 +33,8 @@ struct LogProbsGradArgs {
     void* dx;
 };
 void launch_log_probs_grad(shifter_ctx* ctx, int dtype, const LogProbsGradArgs& a);
+
+// The norm of all tensors to d_norm; with clip, the tensors times min(1, max_norm / (norm + 1e-6)) as well.
+void launch_grad_norm(shifter_ctx* ctx, const std::vector<shifter_grad>& all, bool clip, float max_norm, float* norm, uint8_t* work);
 
 }  // namespace shifter

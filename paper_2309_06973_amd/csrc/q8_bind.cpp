@@ -532,6 +532,61 @@ PyObject* log_probs_grad(PyObject* const* a) {
     return wrap(a[10], std::move(dx));
 }
 
+// The items of a list or tuple.
+struct Items {
+    Owned seq;
+    Items(PyObject* o, const char* what) : seq(PySequence_Fast(o, what)) {}
+    Py_ssize_t size() const { return PySequence_Fast_GET_SIZE(seq.p); }
+    PyObject* operator[](Py_ssize_t i) const { return PySequence_Fast_GET_ITEM(seq.p, i); }
+};
+
+// ctx, device, grads, masks, max_norm, out, room -> norm.  max_norm None: the norm alone.
+PyObject* grad_norm(PyObject* const* a) {
+    const Handle h = handle_of(a);
+    const bool clip = !is_none(a[4]);
+    const float max_norm = clip ? number_of(a[4]) : 0.0f;
+    const Items grads(a[2], "grads must be a list of tensors");
+    const Items masks(is_none(a[3]) ? a[2] : a[3], "masks must be a list");
+    const Items out(is_none(a[5]) ? a[2] : a[5], "out must be a list of tensors");
+    const Py_ssize_t n = grads.size();
+    TORCH_CHECK_VALUE(masks.size() == n && out.size() == n, "masks and out must have an entry for each of grads");
+    TORCH_CHECK_VALUE(!clip || max_norm >= 0.0f, "max_norm must not be negative");
+    std::vector<shifter_grad> list((size_t)n);
+    for (Py_ssize_t i = 0; i < n; ++i) {
+        const at::Tensor& g = tensor_of(grads[i], "a gradient");
+        const int code = g.layout() == at::kStrided ? code_of(g.scalar_type()) : -1;
+        TORCH_CHECK_VALUE(code >= 0, "gradient ", i, " must be fp32, bf16 or fp16");
+        TORCH_CHECK_VALUE(g.is_non_overlapping_and_dense(), "gradient ", i, " has gaps between its elements");
+        constant(g, "a gradient");
+        here(h, g, "a gradient");
+        shifter_grad& e = list[(size_t)i];
+        e = shifter_grad{g.data_ptr(), nullptr, nullptr, (uint64_t)g.numel(), code};
+        auto alike = [&](const at::Tensor& t, at::ScalarType type, const char* what) {
+            TORCH_CHECK_VALUE(t.layout() == at::kStrided && t.scalar_type() == type && t.sizes() == g.sizes() &&
+                              (g.numel() < 2 || t.strides() == g.strides()), what, " ", i, " must be ", type,
+                              " of its gradient's shape and layout in memory");
+            here(h, t, what);
+            return t.data_ptr();
+        };
+        if (!is_none(a[3]) && !is_none(masks[i])) e.d_mask = static_cast<const uint8_t*>(alike(tensor_of(masks[i], "a mask"), at::kByte, "mask"));
+        if (!clip) continue;
+        const at::Tensor& t = tensor_of(out[i], "out");
+        constant(t, "out");
+        e.d_out = alike(t, g.scalar_type(), "out");
+    }
+    uint64_t need = 0;
+    check(shifter_grad_norm_layout((uint64_t)n, &need), Py_None);
+    const Work work(a[6], need);
+    at::Tensor norm = new_tensor(h, {}, at::kFloat);
+    float* p = static_cast<float*>(norm.data_ptr());
+    // with the interpreter's lock: the launches share the handle's workspace, and another thread's stay out from between them
+    check(clip ? shifter_clip_grad_norm(h.ctx, list.data(), (uint64_t)n, max_norm, p, work.p, need)
+               : shifter_grad_norm(h.ctx, list.data(), (uint64_t)n, p, work.p, need), a[0]);
+    if (clip)
+        for (Py_ssize_t i = 0; i < n; ++i) written(tensor_of(out[i], "out"));
+    return THPVariable_Wrap(std::move(norm));
+}
+
 // Q8Matrix, failed(code, ctx): what the functions below make and raise.
 PyObject* bind(PyObject* const* a) {
     Py_INCREF(a[0]);
@@ -543,7 +598,8 @@ PyObject* bind(PyObject* const* a) {
 
 #define Q8_ENTRY(name, n) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&entry<n, name>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {Q8_ENTRY(bind, 2), Q8_ENTRY(quantize, 5), Q8_ENTRY(dequantize, 5), Q8_ENTRY(rms_norm, 8),
-                         Q8_ENTRY(matmul, 8), Q8_ENTRY(weight_grad, 9), Q8_ENTRY(log_probs, 8), Q8_ENTRY(log_probs_grad, 11), {nullptr, nullptr, 0, nullptr}};
+                         Q8_ENTRY(matmul, 8), Q8_ENTRY(weight_grad, 9), Q8_ENTRY(log_probs, 8), Q8_ENTRY(log_probs_grad, 11),
+                         Q8_ENTRY(grad_norm, 7), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_q8", "The 8-bit operators' calls; see q8.py.", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
 

@@ -178,6 +178,17 @@ class Q8:
         entropy with g_entropy, as log_probs gave them.  ``out`` may be x."""
         return self._calls.log_probs_grad(*self._enter(), x, target, norm, g_logp, g_lse, entropy, g_entropy, scale, out)
 
+    def grad_norm(self, grads, masks=None) -> torch.Tensor:
+        """The norm of all elements of a list of tensors (fp32, bf16, fp16, mixed as they come; any shape and dense layout), a
+        0-dimensional fp32 tensor worked out in 64 bits.  masks: a list of uint8 tensors or None, laid out as
+        their gradients: what is kept of each (as apply_mask writes them)."""
+        return self._calls.grad_norm(*self._enter(), grads, masks, None, None, self._joined)
+
+    def clip_grad_norm(self, grads, max_norm: float, masks=None, out=None) -> torch.Tensor:
+        """The same norm, and the gradients times min(1, max_norm / (norm + 1e-6)), masked elements 0, written in place or to
+        the tensors of ``out`` (laid out as their gradients).  What is written may not overlap anything else."""
+        return self._calls.grad_norm(*self._enter(), grads, masks, float(max_norm), out, self._joined)
+
 
 def _rows(x: torch.Tensor) -> torch.Tensor:
     """x with its columns side by side and its rows one after another."""

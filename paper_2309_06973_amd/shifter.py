@@ -86,6 +86,11 @@ class LogProbsGradArgs(C.Structure):
                 ("d_dx", C.c_void_p), ("ld_dx", C.c_uint64), ("dtype", C.c_int), ("scale", C.c_float)]
 
 
+class Grad(C.Structure):
+    _fields_ = [("d_g", C.c_void_p), ("d_out", C.c_void_p), ("d_mask", C.c_void_p), ("n", C.c_uint64),
+                ("dtype", C.c_int)]
+
+
 _fold_fields = operator.attrgetter("tensor", "gamma", "beta", "mean", "var", "bias", "out_offset")
 _fold_row = struct.Struct("=IiiiiiQ").pack      # a FoldDesc
 
@@ -151,6 +156,10 @@ EXPORTS = {
     "shifter_log_probs_layout": [C.c_uint64, C.c_uint64, C.c_uint32, C.POINTER(C.c_uint64)],
     "shifter_log_probs": [C.c_void_p, C.POINTER(LogProbsArgs)],
     "shifter_log_probs_grad": [C.c_void_p, C.POINTER(LogProbsGradArgs)],
+    "shifter_grad_norm_layout": [C.c_uint64, C.POINTER(C.c_uint64)],
+    "shifter_grad_norm": [C.c_void_p, C.POINTER(Grad), C.c_uint64, C.c_void_p, C.c_void_p, C.c_uint64],
+    "shifter_clip_grad_norm": [C.c_void_p, C.POINTER(Grad), C.c_uint64, C.c_float, C.c_void_p, C.c_void_p,
+                               C.c_uint64],
     "shifter_apply_mask": [C.c_void_p] * 8,
     "shifter_dead_channel_scan": [C.c_void_p] * 5,
     "shifter_propagate_groups": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint32,
@@ -539,6 +548,26 @@ def shifter_log_probs_grad(ctx: Context, **fields) -> None:
     """fields: those of LogProbsGradArgs; what is left out is 0 or NULL."""
     _check(load_library().shifter_log_probs_grad(ctx.handle, C.byref(_filled(LogProbsGradArgs, fields))),
            ctx.handle)
+
+
+def shifter_grad_norm_layout(count: int) -> int:
+    """Bytes of workspace that shifter_grad_norm and shifter_clip_grad_norm take for so many tensors."""
+    out = C.c_uint64()
+    _check(load_library().shifter_grad_norm_layout(count, C.byref(out)))
+    return int(out.value)
+
+
+def shifter_grad_norm(ctx: Context, grads: Sequence[Grad], d_norm, d_work, work_bytes: int) -> None:
+    arr = (Grad * max(len(grads), 1))(*grads)
+    _check(load_library().shifter_grad_norm(ctx.handle, arr, len(grads), _ptr(d_norm), _ptr(d_work),
+                                            work_bytes), ctx.handle)
+
+
+def shifter_clip_grad_norm(ctx: Context, grads: Sequence[Grad], max_norm: float, d_norm, d_work,
+                           work_bytes: int) -> None:
+    arr = (Grad * max(len(grads), 1))(*grads)
+    _check(load_library().shifter_clip_grad_norm(ctx.handle, arr, len(grads), max_norm, _ptr(d_norm),
+                                                 _ptr(d_work), work_bytes), ctx.handle)
 
 
 def shifter_portfolio_begin(ctx: Context, model: Model, d_w, d_vecs, n_prune: Sequence[int],

@@ -1,0 +1,237 @@
+"""The norm of many tensors and their clipping against the definition in 64 bits.
+
+The sum of squares is worked out in 64 bits, n elements off by n 2^-53 of it at most, and rounded once: U relatively.  A result
+is a 64-bit product rounded to fp32, U, and to the element's type, half a step, or half the smallest step."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import learn_oracle as L
+from paper_2309_06973_amd import shifter as S
+from paper_2309_06973_amd.q8 import Q8
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+DTYPES = [torch.float32, torch.bfloat16, torch.float16]
+INF, NAN = float("inf"), float("nan")
+
+
+@pytest.fixture(scope="module")
+def ops():
+    o = Q8()
+    yield o
+    torch.cuda.synchronize()
+    o.close()
+
+
+def make(sizes, dtypes, seed, shift=0, size=1.0):
+    """Tensors in one arena, one behind the other from element `shift` on, their masks too."""
+    g = torch.Generator().manual_seed(seed)
+    grads, masks = [], []
+    for i, n in enumerate(sizes):
+        t = dtypes[i % len(dtypes)]
+        grads.append((size * torch.randn(n + shift, generator=g)).to(t).to(DEV)[shift:])
+        masks.append((torch.rand(n + shift, generator=g) < 0.5).to(torch.uint8).to(DEV)[shift:])
+    return grads, masks
+
+
+def check(norm, results, grads, max_norm, masks=None):
+    want, clipped = L.clipped(grads, max_norm, masks)
+    n = sum(g.numel() for g in grads)
+    got = float(norm)
+    assert norm.shape == () and norm.dtype == torch.float32
+    assert got == want or (math.isnan(got) and math.isnan(want)) or abs(got - want) <= (1.001 * L.U + n * 2.0 ** -52) * want + L.LEAST[torch.float32]
+    for r, w, g in zip(results or (), clipped, grads):
+        x = r.detach().cpu().double()
+        assert r.shape == g.shape and torch.equal(torch.isnan(x), torch.isnan(w))
+        ok = torch.isfinite(w)
+        assert torch.equal(x[~ok & ~torch.isnan(w)], w[~ok & ~torch.isnan(w)])
+        off = (L.HALF_STEP[r.dtype] + 1.01 * L.U + n * 2.0 ** -52) * w[ok].abs() + L.LEAST[r.dtype]
+        assert ((x[ok] - w[ok]).abs() <= off).all()
+
+
+LISTS = [[], [0], [1], [7], [8], [9], [0, 3, 0], [8191, 8192, 8193], [1] * 30, [2048, 2047, 2049, 4096, 16384], [100003, 5, 77777], [24576, 65536 + 3],
+         [163 * 3] * 163, [17] * 164, [33] * 165, [5] * 500, [20000] * 340, [17000001]]
+
+
+@pytest.mark.parametrize("masked", [False, True])
+@pytest.mark.parametrize("which", range(len(LISTS)))
+def test_lists(ops, which, masked):
+    sizes = LISTS[which]
+    for dtypes, shift in ((DTYPES[:1], 0), (DTYPES, 1), (DTYPES[1:2], 3)):
+        print(f"clip_grad_norm {len(sizes)} tensors of {sizes[:3]} masked={masked} shift={shift} {dtypes}", flush=True)
+        grads, masks = make(sizes, dtypes, which + shift, shift)
+        if not masked:
+            masks = None
+        elif len(sizes) > 2:
+            masks[1] = None                     # some have masks
+        before = [g.clone() for g in grads]
+        check(ops.grad_norm(grads, masks=masks), None, grads, 1.0, masks)
+        norm = float(ops.grad_norm(grads, masks=masks))
+        for max_norm in (0.25 * norm, 2.0 * norm + 1.0):
+            out = [torch.full_like(g, 5.0) for g in grads]
+            n = ops.clip_grad_norm(grads, max_norm, masks=masks, out=out)
+            check(n, out, grads, np.float64(np.float32(max_norm)), masks)
+            assert all(torch.equal(a, b) for a, b in zip(grads, before))
+            same = [g.clone() for g in grads]
+            m = ops.clip_grad_norm(same, max_norm, masks=masks)
+            assert torch.equal(m, n) and all(torch.equal(a, b) for a, b in zip(same, out))
+
+
+def test_what_lies_around_is_left(ops):
+    buf = torch.full((70000,), 3.0, device=DEV)
+    grads = [buf[5:12], buf[20:16410], buf[20000:20001], buf[30001:47013]]
+    inside = torch.zeros(70000, dtype=torch.bool, device=DEV)
+    for a, b in ((5, 12), (20, 16410), (20000, 20001), (30001, 47013)):
+        inside[a:b] = True
+    ops.clip_grad_norm(grads, 1e-3)
+    assert (buf[~inside] == 3).all() and (buf[inside] < 1).all()
+
+
+def test_shapes_and_layouts(ops):
+    g = torch.randn(16, 8, 3, 3, device=DEV).to(memory_format=torch.channels_last)
+    m = (torch.rand(16, 8, 3, 3, device=DEV) < 0.5).to(torch.uint8).to(memory_format=torch.channels_last)
+    h = torch.randn(5, 7, device=DEV, dtype=torch.bfloat16).t()
+    s = torch.tensor(2.0, device=DEV)
+    out = [torch.empty_like(x) for x in (g, h, s)]
+    check(ops.clip_grad_norm((g, h, s), 0.5, masks=[m, None, None], out=out), out, [g, h, s], 0.5, [m, None, None])
+
+
+def test_ends_of_the_numbers(ops):
+    """Squares beyond fp32's range both ways, and factors below its smallest number."""
+    big = torch.full((1000,), 3e38, device=DEV)
+    tiny = torch.full((1000,), 1e-40, device=DEV)
+    for grads in ([big], [tiny], [big, tiny]):
+        for max_norm in (1.0, 1e-30, 1e30):
+            out = [torch.empty_like(g) for g in grads]
+            if len(grads) == 1 and grads[0] is tiny:
+                check(ops.clip_grad_norm(grads, max_norm, out=out), out, grads, float(np.float32(max_norm)))
+                continue
+            want, clipped = L.clipped(grads, float(np.float32(max_norm)))
+            n = ops.clip_grad_norm(grads, max_norm, out=out)
+            assert float(n) == INF                                    # rounded to fp32; what is clipped goes by the 64-bit norm
+            for r, w in zip(out, clipped):
+                x = r.cpu().double()
+                assert ((x - w).abs() <= 2.01 * L.U * w.abs() + 2 ** -149).all()
+    z = [torch.zeros(10, device=DEV)]
+    assert float(ops.clip_grad_norm(z, 0.0)) == 0 and (z[0] == 0).all()
+    v = [torch.ones(10, device=DEV)]
+    ops.clip_grad_norm(v, 0.0)
+    assert (v[0] == 0).all()
+    v = [torch.ones(10, device=DEV)]
+    ops.clip_grad_norm(v, INF)
+    assert (v[0] == 1).all()
+
+
+@pytest.mark.parametrize("bad", [NAN, INF, -INF])
+def test_values_that_are_not_finite(ops, bad):
+    grads, masks = make([9000, 77], DTYPES[:2], 3)
+    grads[0][8500] = bad
+    masks[0][8500] = 0
+    out = [torch.empty_like(g) for g in grads]
+    check(ops.clip_grad_norm(grads, 1.0, masks=masks, out=out), out, grads, 1.0, masks)        # it is masked: as if it were not there
+    assert out[0][8500] == 0 and all(torch.isfinite(o).all() for o in out)
+    masks[0][8500] = 1
+    n = ops.clip_grad_norm(grads, 1.0, masks=masks, out=out)
+    assert not math.isfinite(float(n)) and torch.isnan(out[0][8500])
+    kept = masks[1] != 0
+    assert torch.isnan(out[1][kept]).all() if math.isnan(bad) else (out[1][kept] == 0).all()
+    assert (out[1][~kept] == 0).all()
+
+
+def test_far_offsets(ops):
+    """A tensor of more than 2^32 bytes and 2^31 elements."""
+    n = (1 << 31) + 12345
+    g = torch.zeros(n, dtype=torch.bfloat16, device=DEV)
+    g[-3:] = 4.0
+    g[5] = 1.0
+    assert float(ops.grad_norm([g])) == 7.0
+    assert float(ops.clip_grad_norm([g], 3.5)) == 7.0
+    assert torch.equal(g[-4:].float(), torch.tensor([0, 2.0, 2.0, 2.0], device=DEV)) and float(g[5]) == 0.5
+
+
+def test_the_same_every_time(ops):
+    grads, masks = make([100003] * 30 + [17] * 200, DTYPES, 9)
+    first = ops.grad_norm(grads, masks=masks)
+    for _ in range(20):
+        assert torch.equal(ops.grad_norm(grads, masks=masks), first)
+        ops.log_probs(torch.zeros(2, 30000, device=DEV), top=3)        # another operator in the same workspace
+
+
+def test_recorded(ops):
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        own = Q8()
+        grads, masks = make([50000, 3, 8192] + [100] * 200, DTYPES, 4)
+        out = [torch.empty_like(g) for g in grads]
+        graphs = []
+        own.grad_norm(grads)
+        torch.cuda.synchronize()
+        for _ in range(2):
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=stream):
+                norm = own.clip_grad_norm(grads, 1.0, masks=masks, out=out)
+            graphs.append((g, norm))
+        for i in range(4):
+            for x in grads:
+                x.mul_(1.5).add_(0.25)
+            for g, norm in graphs:
+                for o in out:
+                    o.fill_(9.0)
+                g.replay()
+                torch.cuda.synchronize()
+                check(norm, out, grads, 1.0, masks)
+                want = [torch.empty_like(x) for x in grads]
+                assert torch.equal(own.clip_grad_norm(grads, 1.0, masks=masks, out=want), norm)
+                assert all(torch.equal(a, b) for a, b in zip(out, want))
+        torch.cuda.synchronize()
+        own.close()
+
+
+def test_a_written_tensor_has_a_new_version(ops):
+    g = [torch.ones(5, device=DEV), torch.ones(3, device=DEV)]
+    a, b = g[0]._version, g[1]._version
+    ops.grad_norm(g)
+    assert (g[0]._version, g[1]._version) == (a, b)
+    ops.clip_grad_norm(g, 1.0)
+    assert g[0]._version > a and g[1]._version > b
+
+
+def test_refusals(ops):
+    one = lambda n=10, **kw: torch.ones(n, device=DEV, **kw)
+    buf = one(100)
+    for call, what in ((lambda: ops.clip_grad_norm([buf, buf], 1.0), "overlaps"),
+                       (lambda: ops.clip_grad_norm([buf[:10], buf[9:20]], 1.0), "overlaps"),
+                       (lambda: ops.clip_grad_norm([buf[:10], one()], 1.0, out=[one(), buf[9:19]]), "overlaps"),
+                       (lambda: ops.clip_grad_norm([buf[:10]], 1.0, out=[buf[1:11]]), "overlaps"),
+                       (lambda: ops.clip_grad_norm([one(), one()], 1.0, out=[buf[:10], buf[:10]]), "overlaps")):
+        with pytest.raises(S.ShifterError, match=what):
+            call()
+    assert (buf == 1).all()
+    assert float(ops.grad_norm([buf, buf])) == pytest.approx(math.sqrt(200), rel=1e-7)       # reading twice is fine
+    leaf = one(requires_grad=True)
+    for call, what in ((lambda: ops.clip_grad_norm([one().double()], 1.0), "fp32, bf16 or fp16"),
+                       (lambda: ops.clip_grad_norm([buf.view(10, 10)[:, :5]], 1.0), "gaps"),
+                       (lambda: ops.clip_grad_norm([buf[:1].expand(5)], 1.0), "gaps"),
+                       (lambda: ops.grad_norm([one()], masks=[one()]), "mask 0"),
+                       (lambda: ops.grad_norm([one()], masks=[torch.ones(9, dtype=torch.uint8, device=DEV)]), "mask 0"),
+                       (lambda: ops.grad_norm([one()], masks=[]), "an entry for each"),
+                       (lambda: ops.clip_grad_norm([one()], 1.0, out=[one().bfloat16()]), "out 0"),
+                       (lambda: ops.clip_grad_norm([one()], -1.0), "negative"), (lambda: ops.clip_grad_norm([one()], NAN), "negative"),
+                       (lambda: ops.grad_norm([torch.ones(3)]), "not on cuda"), (lambda: ops.clip_grad_norm([leaf], 1.0), "needs a gradient"),
+                       (lambda: ops.grad_norm([leaf]), "needs a gradient"), (lambda: ops.grad_norm([None]), "tensor")):
+        with pytest.raises(ValueError, match=what):
+            call()
+    with torch.no_grad():
+        ops.clip_grad_norm([leaf], 1.0)
+    need = S.shifter_grad_norm_layout(1)
+    work, norm = torch.zeros(need, dtype=torch.uint8, device=DEV), one(1)
+    e = lambda **kw: S.Grad(**{**dict(d_g=buf.data_ptr(), d_out=buf.data_ptr(), n=10, dtype=0), **kw})
+    for grad, w, b, what in ((e(), work, need - 1, "too small"), (e(), None, need, "NULL"), (e(dtype=7), work, need, "element type"),
+                             (e(d_g=None), work, need, "NULL"), (e(d_g=buf.data_ptr() + 2), work, need, "aligned"),
+                             (e(n=1 << 40), work, need, "2\\^40"), (e(d_out=None), work, need, "NULL")):
+        with pytest.raises(S.ShifterError, match=what):
+            S.shifter_clip_grad_norm(ops.ctx, [grad], 1.0, norm, w, b)
