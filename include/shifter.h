@@ -780,7 +780,22 @@ int shifter_weight_grad_q8(shifter_ctx* ctx, const void* d_g, int dtype, uint64_
  *                        Tensors are runs of elements of any start, with types of their own; h_grads is a host array that is
  *                        not used after the call returns.  d_out is not read by shifter_grad_norm.
  *
- * Workspaces start on 256 bytes.  Their first SHIFTER_LEARN_ZERO bytes are zero before the first call that is given one; every
+ * shifter_adapters       out_r = y_r + scale[i] (x_r A_i') B_i', i = d_which[r], rounded once to y's type: A (adapters x rank x k) and
+ *                        B (adapters x n x rank) lie without gaps and have x's element type; x is elements, or an 8-bit
+ *                        matrix (d_q_scale not NULL: d_x are its codes, ld_x its stride).  A row whose number is negative
+ *                        has no adapter: out_r is y_r; one whose number is not below `adapters` is NaN.  d_scale NULL: 1.
+ *                        Sums are in 32 bits.  d_out may be d_y with the same stride.  d_down, or NULL: m x rank, gets
+ *                        scale[i] x_r A_i' (0 without an adapter) for the gradient.  What a row gives depends on its own
+ *                        numbers and adapter alone.
+ * shifter_adapters_grad  from g, the gradient of out, of x's element type: up_r = scale[i] g_r B_i, dx_r = up_r A_i (of that type, 0
+ *                        without an adapter; d_dx may be NULL), dA_i = sum up_r' x_r, dB_i = sum g_r' down_r over the rows of adapter i,
+ *                        fp32, 0 for an adapter without rows.  Rows whose number is not below `adapters` count for none.  d_down: as
+ *                        shifter_adapters wrote it, or NULL: worked out again.  y's gradient is g itself.
+ *                        rank 1 to SHIFTER_ADAPTERS_MAX_RANK; SHIFTER_ERR_CAPACITY for more than 2^27 rows and for adapters of 2^30
+ *                        columns or so all together.
+ *
+ * Workspaces start on 256 bytes.  The first SHIFTER_LEARN_ZERO bytes of those of shifter_log_probs, shifter_grad_norm and
+ * shifter_clip_grad_norm are zero before the first call that is given one; every such
  * call leaves them zero, so that one workspace does for calls of whatever sizes and operators, one after another.  Calls
  * that may run at the same time have a workspace each. */
 #define SHIFTER_LEARN_ZERO 2048u
@@ -815,6 +830,51 @@ typedef struct {
     int dtype;                  /* of x and dx */
     float scale;
 } shifter_log_probs_grad_args;
+#define SHIFTER_ADAPTERS_MAX_RANK 128u
+typedef struct {
+    const void* d_x;
+    uint64_t ld_x;
+    const float* d_q_scale;     /* m, or NULL: x is elements */
+    uint64_t m, n, k, rank, adapters;
+    const void* d_a;
+    const void* d_b;
+    const int64_t* d_which;
+    const float* d_scale;
+    const void* d_y;
+    uint64_t ld_y;
+    void* d_out;
+    uint64_t ld_out;
+    float* d_down;
+    void* d_work;
+    uint64_t work_bytes;
+    int dtype;                  /* shifter_dtype of a, b and x */
+    int y_dtype;                /* of y and out */
+} shifter_adapters_args;
+typedef struct {
+    const void* d_x;
+    uint64_t ld_x;
+    const float* d_q_scale;
+    uint64_t m, n, k, rank, adapters;
+    const void* d_a;
+    const void* d_b;
+    const int64_t* d_which;
+    const float* d_scale;
+    const void* d_g;
+    uint64_t ld_g;
+    const float* d_down;
+    void* d_dx;
+    uint64_t ld_dx;
+    float* d_da;
+    float* d_db;
+    void* d_work;
+    uint64_t work_bytes;
+    int dtype;                  /* of a, b, x, g and dx */
+} shifter_adapters_grad_args;
+int shifter_adapters_layout(uint64_t m, uint64_t n, uint64_t k, uint64_t rank, uint64_t adapters, uint64_t* h_work_bytes);
+int shifter_adapters(shifter_ctx* ctx, const shifter_adapters_args* args);
+int shifter_adapters_grad_layout(uint64_t m, uint64_t n, uint64_t k, uint64_t rank, uint64_t adapters, int dtype,
+                                 uint64_t* h_work_bytes);
+int shifter_adapters_grad(shifter_ctx* ctx, const shifter_adapters_grad_args* args);
 typedef struct {
     const void* d_g;
     void* d_out;

@@ -96,3 +96,58 @@ def clipped(grads, max_norm, masks=None):
     return norm, [torch.where(k == 0, k, k * factor) if np.isfinite(factor) else
                   (k * factor if masks is None or masks[i] is None else torch.where(masks[i].cpu() != 0, k * factor, 0.0))
                   for i, k in enumerate(kept)]
+
+
+class Adapters:
+    """out = y + scale[i] (x a[i]') b[i]' and its gradients in float64 on the CPU, and how far a kernel may be that sums in 32
+    bits: a sum of n products is off by 2 U (n + 40) of the sum of their sizes at most (products of 16-bit factors are exact,
+    others off by U; every addition may cut instead of round; parts and wavefronts are joined in no more than 40 further
+    ones; the scales cost 2 U).  An intermediate's error goes on with the sizes of what it is multiplied with."""
+
+    def __init__(self, y, x, a, b, which, scale=None):
+        d = lambda t: t.detach().cpu().double()
+        self.y, self.x, self.a, self.b = d(y), d(x), d(a), d(b)
+        self.which = which.cpu()
+        many = self.a.shape[0]
+        self.scale = d(scale) if scale is not None else torch.ones(many, dtype=torch.float64)
+        self.many = many
+        rank = self.a.shape[1]
+        self.down, self.off_down = torch.zeros(len(self.which), rank, dtype=torch.float64), torch.zeros(len(self.which), rank, dtype=torch.float64)
+        self.out, self.off = self.y.clone(), torch.zeros_like(self.y)
+        err = lambda n: 2 * U * (n + 40)
+        k = self.a.shape[2]
+        for i, rows in self.rows():
+            c, a_, b_ = abs(self.scale[i]), self.a[i], self.b[i]
+            self.down[rows] = self.scale[i] * (self.x[rows] @ a_.t())
+            self.off_down[rows] = err(k) * c * (self.x[rows].abs() @ a_.abs().t())
+            part = self.down[rows] @ b_.t()
+            self.out[rows] += part
+            self.off[rows] = self.off_down[rows] @ b_.abs().t() + err(rank) * (self.down[rows].abs() @ b_.abs().t()) + U * self.out[rows].abs()
+        bad = self.which >= many
+        self.out[bad], self.down[bad] = float("nan"), float("nan")
+
+    def rows(self):
+        for i in range(self.many):
+            rows = torch.nonzero(self.which == i)[:, 0]
+            if len(rows):
+                yield i, rows
+
+    def grads(self, g):
+        """{name: (gradient, bound)}."""
+        g = g.detach().cpu().double()
+        err = lambda n: 2 * U * (n + 40)
+        zero = lambda t: torch.zeros(t.shape, dtype=torch.float64)
+        dx, dx_off, da, da_off, db, db_off = (zero(t) for t in (self.x, self.x, self.a, self.a, self.b, self.b))
+        n, rank = self.b.shape[1:]
+        for i, rows in self.rows():
+            c, a, b, x = abs(self.scale[i]), self.a[i], self.b[i], self.x[rows]
+            up = self.scale[i] * (g[rows] @ b)
+            up_off = err(n) * c * (g[rows].abs() @ b.abs())
+            dx[rows] = up @ a
+            dx_off[rows] = up_off @ a.abs() + err(rank) * (up.abs() @ a.abs())
+            da[i] = up.t() @ x
+            da_off[i] = up_off.t() @ x.abs() + err(len(rows)) * (up.abs().t() @ x.abs())
+            db[i] = g[rows].t() @ self.down[rows]
+            db_off[i] = g[rows].abs().t() @ self.off_down[rows] + err(len(rows)) * (g[rows].abs().t() @ self.down[rows].abs())
+        dx[self.which >= self.many] = float("nan")
+        return dict(dx=(dx, dx_off), da=(da, da_off), db=(db, db_off))

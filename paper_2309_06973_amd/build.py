@@ -16,7 +16,7 @@ LIB = os.path.join(PKG, "libshifter.so")
 BINDING = os.path.join(PKG, "_q8.so")
 SOURCES = ["api.hip", "select.hip", "spec_select.hip", "spec_multi.hip", "mask_scan.hip", "batch.hip", "plan_compact.hip",
            "fixpoint.hip", "fold.hip", "codec.hip", "q8_rows.hip", "q8_product.hip",
-           "log_probs.hip", "grad_norm.hip"]
+           "log_probs.hip", "grad_norm.hip", "adapters.hip"]
 FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-Wall",
          "-Wno-unused-result",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

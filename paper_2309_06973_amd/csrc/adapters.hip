@@ -1,0 +1,650 @@
+// Low-rank adapters beside a projection that rows of many requests share:
+//
+//   out_r = y_r + c_i (x_r A_i') B_i',   i = which[r]
+//
+// and their gradients.  The product over the long side, s_r = c_i x_r A_i', is the narrow one: rank numbers a row, held in 32 bits.
+// It is multiplied with B_i in 32 bits as well (the matrix units take fp32 at a sixteenth of bf16's rate, which up to
+// rank 32 or so is still above what memory delivers), so that out is rounded once.
+//
+// Rows are taken in tiles of 16 as they come, whatever requests they belong to: a tile is multiplied with each adapter that
+// one of its rows has, and each row keeps the result of its own.  So rows need no sorting, a run of rows of one request costs
+// one product, and nothing that one request's adapter holds, infinities and NaN too, reaches another's rows.
+#include <algorithm>
+#include <cmath>
+
+#include "dev_common.h"
+#include "learn.h"
+#include "q8_eight.h"
+
+namespace shifter {
+
+typedef float v4f __attribute__((ext_vector_type(4)));
+constexpr int NO_ADAPTER = -1, BAD_ADAPTER = -2;
+constexpr uint32_t ADAPT_THREADS = 256, ADAPT_WAVES = 4;
+
+__device__ __forceinline__ int adapter_of(const int64_t* which, uint64_t row, uint64_t rows, uint32_t adapters) {
+    if (row >= rows) return NO_ADAPTER;
+    const int64_t i = which[row];
+    return i < 0 ? NO_ADAPTER : i < (int64_t)adapters ? (int)i : BAD_ADAPTER;
+}
+
+// acc[i][j] += sum over 32 columns of a[i] b[j]: lane l holds eight columns, 8 (l / 16) on, of row l % 16 of each, and
+// rows 4 (l / 16) on of column l % 16 of the result.
+__device__ __forceinline__ v4f mma(const Eight<__bf16>& a, const Eight<__bf16>& b, v4f acc) {
+    typedef __bf16 vec __attribute__((ext_vector_type(8)));
+    vec u, v;
+    __builtin_memcpy(&u, a.w, 16);
+    __builtin_memcpy(&v, b.w, 16);
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(u, v, acc, 0, 0, 0);
+}
+__device__ __forceinline__ v4f mma(const Eight<_Float16>& a, const Eight<_Float16>& b, v4f acc) {
+    typedef _Float16 vec __attribute__((ext_vector_type(8)));
+    vec u, v;
+    __builtin_memcpy(&u, a.w, 16);
+    __builtin_memcpy(&v, b.w, 16);
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(u, v, acc, 0, 0, 0);
+}
+__device__ __forceinline__ v4f mma(const Eight<float>& a, const Eight<float>& b, v4f acc) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.w[i]), __uint_as_float(b.w[i]), acc, 0, 0, 0);
+    return acc;
+}
+
+// The next adapter that a row of the tiles still waits for, the same in all lanes; false: none.
+template <uint32_t RT>
+__device__ __forceinline__ bool next_adapter(int (&waits)[RT], int* which) {
+#pragma unroll
+    for (uint32_t i = 0; i < RT; ++i) {
+        const uint64_t who = __ballot(waits[i] >= 0);
+        if (who) {
+            const int a = __builtin_amdgcn_readlane(waits[i], (int)__ffsll((unsigned long long)who) - 1);
+#pragma unroll
+            for (uint32_t j = 0; j < RT; ++j)
+                if (waits[j] == a) waits[j] = NO_ADAPTER;
+            *which = a;
+            return true;
+        }
+    }
+    return false;
+}
+
+// 16 neighbouring columns of a row, as two operands.
+template <typename T>
+struct Sixteen {
+    Eight<T> h[2];
+    __device__ __forceinline__ void load(const T* p) {
+        h[0].load(p);
+        h[1].load(p + 8);
+    }
+    __device__ __forceinline__ void load_end(const T* row, uint32_t c, uint32_t cols) {     // zeros behind the row's end
+#pragma unroll
+        for (uint32_t i = 0; i < 2; ++i) {
+            fetch8(row, c + 8 * i, cols, h[i]);
+            place8(c + 8 * i, cols, h[i]);
+        }
+    }
+};
+// Codes as numbers of type T, which holds them exactly.
+template <typename T>
+__device__ __forceinline__ void codes_as(uint4 w, Sixteen<T>& s) {
+    const uint32_t word[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (uint32_t i = 0; i < 2; ++i) {
+        float f[8];
+#pragma unroll
+        for (uint32_t j = 0; j < 8; ++j) f[j] = (float)(int8_t)(word[2 * i + j / 4] >> (8 * (j % 4)));
+        s.h[i].from(f);
+    }
+}
+
+// s[part][r] = c_i x_r A_i' over the part's columns; 0 for a row without an adapter, NaN for one whose adapter there is not.
+// A block has RT tiles of 16 rows and 16 RF ranks; its wavefronts take steps of 64 columns in turn and join their sums.  Both factors
+// come straight from memory into the operands: a lane's 16 columns of a row lie side by side.
+template <typename T, bool CODES, uint32_t RF, uint32_t RT>
+__global__ __launch_bounds__(ADAPT_THREADS) void adapters_down_kernel(AdaptersDownArgs g) {
+    __shared__ v4f s_sum[ADAPT_WAVES][RF * RT][64];
+    const uint32_t lane = threadIdx.x & 63u, wave = uniform_u32(threadIdx.x >> 6), col = 16u * (lane / 16u), r16 = lane & 15u;
+    const uint64_t m0 = (uint64_t)blockIdx.x * 16u * RT;
+    const uint32_t part = blockIdx.y, rank0 = blockIdx.z * 16u * RF;
+    const uint32_t steps = (g.k + ADAPT_STEP - 1u) / ADAPT_STEP, whole = g.k / ADAPT_STEP;
+    const uint32_t s0 = (uint32_t)((uint64_t)steps * part / g.parts), s1 = (uint32_t)((uint64_t)steps * (part + 1u) / g.parts);
+    int id[RT], waits[RT];
+    const T* x[RT];
+    const int8_t* q[RT];
+#pragma unroll
+    for (uint32_t i = 0; i < RT; ++i) {
+        const uint64_t row = m0 + 16u * i + r16, at = min(row, (uint64_t)g.m - 1u);
+        id[i] = waits[i] = adapter_of(g.which, row, g.m, g.adapters);
+        x[i] = static_cast<const T*>(g.x) + at * g.ld_x;
+        q[i] = static_cast<const int8_t*>(g.x) + at * g.ld_x;
+    }
+    v4f sum[RT][RF];
+#pragma unroll
+    for (uint32_t i = 0; i < RT; ++i)
+#pragma unroll
+        for (uint32_t f = 0; f < RF; ++f) sum[i][f] = v4f{0, 0, 0, 0};
+    int which;
+    while (next_adapter<RT>(waits, &which)) {
+        const T* a[RF];
+#pragma unroll
+        for (uint32_t f = 0; f < RF; ++f)
+            a[f] = static_cast<const T*>(g.a) + ((uint64_t)which * g.rank + min(rank0 + 16u * f + r16, g.rank - 1u)) * g.k;
+        v4f acc[RT][RF];
+#pragma unroll
+        for (uint32_t i = 0; i < RT; ++i)
+#pragma unroll
+            for (uint32_t f = 0; f < RF; ++f) acc[i][f] = v4f{0, 0, 0, 0};
+        struct Operands {
+            Sixteen<T> x[RT], a[RF];
+            uint4 q[RT];
+        };
+        auto fetch = [&](uint32_t s, Operands& o) {
+            const uint32_t c = s * ADAPT_STEP + col;
+#pragma unroll
+            for (uint32_t i = 0; i < RT; ++i) {
+                if (CODES) o.q[i] = *reinterpret_cast<const uint4*>(q[i] + c);
+                else o.x[i].load(x[i] + c);
+            }
+#pragma unroll
+            for (uint32_t f = 0; f < RF; ++f) o.a[f].load(a[f] + c);
+        };
+        auto multiply = [&](Operands& o) {
+#pragma unroll
+            for (uint32_t i = 0; i < RT; ++i) {
+                if (CODES) codes_as(o.q[i], o.x[i]);
+#pragma unroll
+                for (uint32_t f = 0; f < RF; ++f)
+#pragma unroll
+                    for (uint32_t h = 0; h < 2; ++h) acc[i][f] = mma(o.a[f].h[h], o.x[i].h[h], acc[i][f]);
+            }
+        };
+        Operands o;
+        const uint32_t end = min(s1, whole);
+        uint32_t s = s0 + wave;
+        if (s < end) fetch(s, o);
+        for (; s < end; s += ADAPT_WAVES) {
+            Operands next;
+            if (s + ADAPT_WAVES < end) fetch(s + ADAPT_WAVES, next);
+            multiply(o);
+            o = next;
+        }
+        if (s1 > whole && (s1 - 1u - s0) % ADAPT_WAVES == wave) {        // the step that a row ends in
+            const uint32_t c = whole * ADAPT_STEP + col;
+#pragma unroll
+            for (uint32_t i = 0; i < RT; ++i) {
+                if (CODES) {
+                    uint32_t w[4] = {0, 0, 0, 0};
+                    if (c < g.k) {
+                        const uint4 v = *reinterpret_cast<const uint4*>(q[i] + c);
+                        w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+                        const int32_t n = (int32_t)(g.k - c);            // what a row holds behind its end is not read as codes
+#pragma unroll
+                        for (int32_t e = 0; e < 4; ++e) {
+                            const int32_t b = min(max(n - 4 * e, 0), 4);
+                            w[e] &= b == 4 ? ~0u : (1u << (8 * b)) - 1u;
+                        }
+                    }
+                    o.q[i] = make_uint4(w[0], w[1], w[2], w[3]);
+                } else {
+                    o.x[i].load_end(x[i], c, g.k);
+                }
+            }
+#pragma unroll
+            for (uint32_t f = 0; f < RF; ++f) o.a[f].load_end(a[f], c, g.k);
+            multiply(o);
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < RT; ++i)
+#pragma unroll
+            for (uint32_t f = 0; f < RF; ++f)
+                if (id[i] == which) sum[i][f] = acc[i][f];
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < RT; ++i)
+#pragma unroll
+        for (uint32_t f = 0; f < RF; ++f) s_sum[wave][i * RF + f][lane] = sum[i][f];
+    __syncthreads();
+    const uint32_t pad = (g.rank + 15u) & ~15u;
+#pragma unroll
+    for (uint32_t u = 0; u < RF * RT; ++u) {
+        if (u % ADAPT_WAVES != wave) continue;
+        const uint32_t i = u / RF, f = u % RF, r = rank0 + 16u * f + 4u * (lane / 16u);
+        const uint64_t row = m0 + 16u * i + r16;
+        if (row >= g.m || rank0 + 16u * f >= pad) continue;
+        v4f v = (s_sum[0][u][lane] + s_sum[1][u][lane]) + (s_sum[2][u][lane] + s_sum[3][u][lane]);
+        float by = 1.0f;
+        if (id[i] >= 0) {
+            if (g.scale) by = g.scale[id[i]];
+            if (CODES) by *= g.x_scale[row];
+        }
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e) v[e] = id[i] == BAD_ADAPTER ? NAN : id[i] < 0 || r + e >= g.rank ? 0.0f : v[e] * by;
+        *reinterpret_cast<v4f*>(g.s + ((uint64_t)part * g.m + row) * pad + r) = v;
+    }
+}
+
+template <typename T, bool CODES, uint32_t RF>
+static void launch_down_as(shifter_ctx* ctx, const AdaptersDownArgs& g) {
+    constexpr uint32_t MORE = RF == 1 ? 4 : 2;
+    const uint32_t tiles = adapt_tiles(g.m, g.rank), groups = (uint32_t)((adapt_pad(g.rank) / 16u + RF - 1u) / RF);
+    const dim3 grid((uint32_t)((g.m + 16u * tiles - 1u) / (16u * tiles)), g.parts, groups);
+    if (tiles == 1) adapters_down_kernel<T, CODES, RF, 1><<<grid, ADAPT_THREADS, 0, ctx->stream>>>(g);
+    else adapters_down_kernel<T, CODES, RF, MORE><<<grid, ADAPT_THREADS, 0, ctx->stream>>>(g);
+}
+template <typename T, bool CODES>
+static void launch_down_of(shifter_ctx* ctx, const AdaptersDownArgs& g) {
+    const uint64_t pad = adapt_pad(g.rank);
+    if (pad <= 16) launch_down_as<T, CODES, 1>(ctx, g);
+    else if (pad <= 32) launch_down_as<T, CODES, 2>(ctx, g);
+    else launch_down_as<T, CODES, 4>(ctx, g);      // 64 ranks a block
+}
+static void launch_down(shifter_ctx* ctx, int dtype, const AdaptersDownArgs& g) {
+    ProfileScope ps(ctx, K_ADAPTERS_DOWN);
+    if (dtype == SHIFTER_F32) g.x_scale ? launch_down_of<float, true>(ctx, g) : launch_down_of<float, false>(ctx, g);
+    else if (dtype == SHIFTER_BF16) g.x_scale ? launch_down_of<__bf16, true>(ctx, g) : launch_down_of<__bf16, false>(ctx, g);
+    else g.x_scale ? launch_down_of<_Float16, true>(ctx, g) : launch_down_of<_Float16, false>(ctx, g);
+}
+
+// Four neighbouring numbers of a row of B, from rank r on, zeros behind its end.
+template <typename T>
+__device__ __forceinline__ v4f four_of(const T* row, uint32_t r, uint32_t rank) {
+    if (r + 4u <= rank) {
+        typedef T vec __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+        const vec v = *reinterpret_cast<const vec*>(row + r);
+        return v4f{(float)v[0], (float)v[1], (float)v[2], (float)v[3]};
+    }
+    v4f f;
+#pragma unroll
+    for (uint32_t e = 0; e < 4; ++e) f[e] = r + e < rank ? (float)row[r + e] : 0.0f;
+    return f;
+}
+
+// out_r = y_r + s_r B_i'.  A wavefront has RT tiles of 16 rows and 64 columns; the columns of its four products are interleaved so that a
+// lane ends with 16 neighbouring columns of a row, which it adds to y and writes.  s, the sums of all parts, is in LDS.
+template <typename T, typename Y, uint32_t RT>
+__global__ __launch_bounds__(ADAPT_THREADS) void adapters_up_kernel(AdaptersUpArgs g) {
+    extern __shared__ __align__(16) float s_rows[];        // [16 RT][pad + 4]
+    const uint32_t lane = threadIdx.x & 63u, wave = uniform_u32(threadIdx.x >> 6), group = lane / 16u, r16 = lane & 15u;
+    const uint64_t m0 = (uint64_t)blockIdx.x * 16u * RT;
+    const uint32_t pad = (g.rank + 15u) & ~15u, pitch = pad + 4u, fours = pad / 4u;
+    const uint32_t rows = (uint32_t)min((uint64_t)(16u * RT), g.m - m0);
+    for (uint32_t u = threadIdx.x; u < 16u * RT * fours; u += ADAPT_THREADS) {
+        const uint32_t row = u / fours, r = u % fours * 4u;
+        v4f v{0, 0, 0, 0};
+        if (row < rows) {
+            const float* p = g.s + (m0 + row) * pad + r;
+            for (uint32_t i = 0; i < g.parts; ++i) v += *reinterpret_cast<const v4f*>(p + (uint64_t)i * g.m * pad);
+            if (g.down && blockIdx.y == 0)
+                for (uint32_t e = 0; e < 4; ++e)
+                    if (r + e < g.down_cols) g.down[(m0 + row) * g.down_cols + r + e] = v[e];
+        }
+        *reinterpret_cast<v4f*>(s_rows + row * pitch + r) = v;
+    }
+    __syncthreads();
+    int id[RT];
+#pragma unroll
+    for (uint32_t i = 0; i < RT; ++i) id[i] = adapter_of(g.which, m0 + 16u * i + r16, g.m, g.adapters);
+    for (uint32_t n0 = (blockIdx.y * ADAPT_WAVES + wave) * 64u; n0 < g.n; n0 += gridDim.y * ADAPT_WAVES * 64u) {
+        // y is on its way while the products are made
+        const uint32_t c = n0 + 16u * group;
+        const bool full = c + 16u <= g.n;
+        Sixteen<Y> y[RT];
+        if (g.y && full) {
+#pragma unroll
+            for (uint32_t i = 0; i < RT; ++i)
+                y[i].load(static_cast<const Y*>(g.y) + min(m0 + 16u * i + r16, (uint64_t)g.m - 1u) * g.ld_y + c);
+        }
+        v4f sum[RT][4];
+#pragma unroll
+        for (uint32_t i = 0; i < RT; ++i)
+#pragma unroll
+            for (uint32_t t = 0; t < 4; ++t) sum[i][t] = v4f{0, 0, 0, 0};
+        int waits[RT], which;
+#pragma unroll
+        for (uint32_t i = 0; i < RT; ++i) waits[i] = id[i];
+        while (next_adapter<RT>(waits, &which)) {
+            v4f acc[RT][4];
+#pragma unroll
+            for (uint32_t i = 0; i < RT; ++i)
+#pragma unroll
+                for (uint32_t t = 0; t < 4; ++t) acc[i][t] = v4f{0, 0, 0, 0};
+            const T* b[4];
+#pragma unroll
+            for (uint32_t t = 0; t < 4; ++t) {
+                const uint32_t at = n0 + 16u * (r16 / 4u) + 4u * t + r16 % 4u;
+                b[t] = static_cast<const T*>(g.b) + ((uint64_t)which * g.n + min(at, g.n - 1u)) * g.rank;
+            }
+            for (uint32_t r = 4u * group; r < pad; r += 16u) {
+                v4f s[RT], v[4];
+#pragma unroll
+                for (uint32_t t = 0; t < 4; ++t) v[t] = four_of(b[t], r, g.rank);
+#pragma unroll
+                for (uint32_t i = 0; i < RT; ++i) s[i] = *reinterpret_cast<const v4f*>(s_rows + (16u * i + r16) * pitch + r);
+#pragma unroll
+                for (uint32_t e = 0; e < 4; ++e)
+#pragma unroll
+                    for (uint32_t i = 0; i < RT; ++i)
+#pragma unroll
+                        for (uint32_t t = 0; t < 4; ++t) acc[i][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[t][e], s[i][e], acc[i][t], 0, 0, 0);
+            }
+#pragma unroll
+            for (uint32_t i = 0; i < RT; ++i)
+#pragma unroll
+                for (uint32_t t = 0; t < 4; ++t)
+                    if (id[i] == which) sum[i][t] = acc[i][t];
+        }
+        if (c >= g.n) continue;
+#pragma unroll
+        for (uint32_t i = 0; i < RT; ++i) {
+            const uint64_t row = m0 + 16u * i + r16;
+            // a row without an adapter is y, and stays as it is in place
+            if (row >= g.m || (id[i] == NO_ADAPTER && g.y == g.out)) continue;
+            Y* out = static_cast<Y*>(g.out) + row * g.ld_out + c;
+            float f[2][8];
+            if (g.y && full) {
+                y[i].h[0].floats(f[0]);
+                y[i].h[1].floats(f[1]);
+            } else {
+#pragma unroll
+                for (uint32_t j = 0; j < 16; ++j)
+                    f[j / 8][j % 8] = g.y && c + j < g.n ? (float)static_cast<const Y*>(g.y)[row * g.ld_y + c + j] : 0.0f;
+            }
+            if (id[i] != NO_ADAPTER) {
+#pragma unroll
+                for (uint32_t j = 0; j < 16; ++j) f[j / 8][j % 8] = id[i] == BAD_ADAPTER ? NAN : f[j / 8][j % 8] + sum[i][j / 4][j % 4];
+            }
+            if (full) {
+#pragma unroll
+                for (uint32_t h = 0; h < 2; ++h) {
+                    Eight<Y> e;
+                    e.from(f[h]);
+                    e.store(out + 8 * h);
+                }
+            } else {
+#pragma unroll
+                for (uint32_t j = 0; j < 16; ++j)
+                    if (c + j < g.n) out[j] = (Y)f[j / 8][j % 8];
+            }
+        }
+    }
+}
+
+template <typename T, typename Y>
+static void launch_up_of(shifter_ctx* ctx, const AdaptersUpArgs& g) {
+    const uint32_t tiles = g.m <= 256 ? 1 : 4;
+    const uint32_t blocks = (uint32_t)((g.m + 16u * tiles - 1u) / (16u * tiles)), groups = std::max(1u, (g.n + 255u) / 256u);
+    const dim3 grid(blocks, std::min(groups, std::max(1u, 2048u / blocks)));
+    const uint32_t lds = (uint32_t)(16u * tiles * (adapt_pad(g.rank) + 4u) * sizeof(float));
+    if (tiles == 1) adapters_up_kernel<T, Y, 1><<<grid, ADAPT_THREADS, lds, ctx->stream>>>(g);
+    else adapters_up_kernel<T, Y, 4><<<grid, ADAPT_THREADS, lds, ctx->stream>>>(g);
+}
+template <typename T>
+static void launch_up_as(shifter_ctx* ctx, int y_dtype, const AdaptersUpArgs& g) {
+    if (y_dtype == SHIFTER_F32) launch_up_of<T, float>(ctx, g);
+    else if (y_dtype == SHIFTER_BF16) launch_up_of<T, __bf16>(ctx, g);
+    else launch_up_of<T, _Float16>(ctx, g);
+}
+static void launch_up(shifter_ctx* ctx, int dtype, int y_dtype, const AdaptersUpArgs& g) {
+    ProfileScope ps(ctx, K_ADAPTERS_UP);
+    if (dtype == SHIFTER_F32) launch_up_as<float>(ctx, y_dtype, g);
+    else if (dtype == SHIFTER_BF16) launch_up_as<__bf16>(ctx, y_dtype, g);
+    else launch_up_as<_Float16>(ctx, y_dtype, g);
+}
+
+void launch_adapters(shifter_ctx* ctx, int dtype, int y_dtype, const AdaptersArgs& g) {
+    const AdaptersPlan p = adapters_plan(g.m, g.k, g.rank);
+    AdaptersDownArgs d{};
+    d.x = g.x; d.ld_x = g.ld_x; d.x_scale = g.x_scale; d.a = g.a; d.which = g.which; d.scale = g.scale;
+    d.m = g.m; d.k = g.k; d.rank = g.rank; d.adapters = g.adapters; d.parts = p.parts;
+    d.s = reinterpret_cast<float*>(g.work);
+    launch_down(ctx, dtype, d);
+    AdaptersUpArgs u{};
+    u.s = d.s; u.parts = p.parts; u.b = g.b; u.which = g.which; u.m = g.m; u.n = g.n; u.rank = g.rank; u.adapters = g.adapters;
+    u.y = g.y; u.ld_y = g.ld_y; u.out = g.out; u.ld_out = g.ld_out; u.down = g.down; u.down_cols = g.rank;
+    launch_up(ctx, dtype, y_dtype, u);
+}
+
+// ---- gradients ----
+//
+//   up_r = c_i g_r B_i,   dx_r = up_r A_i,   dA_i = sum up_r' x_r,   dB_i = sum g_r' down_r   (down_r = c_i x_r A_i')
+//
+// up and dx are the products above with the adapters turned.  The sums over rows take fp32 products as well: both factors are rows as they
+// lie, a lane's eight neighbouring columns are one operand of eight products.
+
+// Blocks up to `adapters`: the rows of an adapter in order, behind those of the ones before it.  Further ones turn 64 columns of an
+// adapter: A [rank][k] to [k][rank], or B [n][rank] to [rank][n].
+template <typename T>
+__global__ __launch_bounds__(ADAPT_THREADS) void adapters_turn_kernel(AdaptersTurnArgs g) {
+    __shared__ T s_tile[ADAPT_MAX_RANK * 65];
+    __shared__ uint32_t s_before[ADAPT_WAVES], s_mine[ADAPT_WAVES];
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+    uint64_t b = blockIdx.x;
+    if (b < g.adapters) {
+        uint32_t before = 0;                   // rows of adapters before this one
+        for (uint64_t r = threadIdx.x; r < g.m; r += ADAPT_THREADS) {
+            const int id = adapter_of(g.which, r, g.m, g.adapters);
+            before += id >= 0 && id < (int)b;
+        }
+        for (uint32_t d = 1; d < 64; d <<= 1) before += __shfl_xor(before, d, 64);
+        if (lane == 0) s_before[wave] = before;
+        __syncthreads();
+        uint32_t at = s_before[0] + s_before[1] + s_before[2] + s_before[3];
+        if (threadIdx.x == 0) g.first[b] = at;
+        for (uint64_t r0 = 0; r0 < g.m; r0 += ADAPT_THREADS) {
+            const bool mine = adapter_of(g.which, r0 + threadIdx.x, g.m, g.adapters) == (int)b;
+            const uint64_t who = __ballot(mine);
+            __syncthreads();
+            if (lane == 0) s_mine[wave] = (uint32_t)__popcll(who);
+            __syncthreads();
+            uint32_t to = at + (uint32_t)__popcll(who & ((1ull << lane) - 1ull));
+            for (uint32_t w = 0; w < wave; ++w) to += s_mine[w];
+            if (mine) g.rows[to] = (uint32_t)(r0 + threadIdx.x);
+            at += s_mine[0] + s_mine[1] + s_mine[2] + s_mine[3];
+        }
+        if (threadIdx.x == 0 && b + 1 == g.adapters) g.first[g.adapters] = at;
+        return;
+    }
+    b -= g.adapters;
+    const uint32_t tiles_a = (g.k + 63u) / 64u, tiles_b = (g.n + 63u) / 64u;
+    const bool of_a = b < (uint64_t)tiles_a * g.adapters;
+    if (!of_a) b -= (uint64_t)tiles_a * g.adapters;
+    const uint32_t tiles = of_a ? tiles_a : tiles_b, cols = of_a ? g.k : g.n;
+    const uint64_t i = b / tiles;
+    const uint32_t c0 = (uint32_t)(b % tiles) * 64u, width = min(64u, cols - c0), all = width * g.rank;
+    if (of_a) {
+        const T* from = static_cast<const T*>(g.a) + i * g.rank * cols;
+        T* to = static_cast<T*>(g.a_turned) + (i * cols + c0) * g.rank;
+        for (uint32_t u = threadIdx.x; u < 64u * g.rank; u += ADAPT_THREADS)
+            if (u % 64u < width) s_tile[u / 64u * 65u + u % 64u] = from[(uint64_t)(u / 64u) * cols + c0 + u % 64u];
+        __syncthreads();
+        for (uint32_t u = threadIdx.x; u < all; u += ADAPT_THREADS) to[u] = s_tile[u % g.rank * 65u + u / g.rank];
+    } else {
+        const T* from = static_cast<const T*>(g.b) + (i * cols + c0) * g.rank;
+        T* to = static_cast<T*>(g.b_turned) + i * g.rank * cols + c0;
+        for (uint32_t u = threadIdx.x; u < all; u += ADAPT_THREADS) s_tile[u % g.rank * 65u + u / g.rank] = from[u];
+        __syncthreads();
+        for (uint32_t u = threadIdx.x; u < 64u * g.rank; u += ADAPT_THREADS)
+            if (u % 64u < width) to[(uint64_t)(u / 64u) * cols + u % 64u] = s_tile[u / 64u * 65u + u % 64u];
+    }
+}
+
+// Sums over the rows of an adapter, of the part blockIdx.y of them: 128 columns of dA_i = sum up' x or, further blocks, of
+// dB_i = sum g' down, 16 RF ranks at a time.  Wavefronts take 16 rows in turn and join their sums in LDS.
+template <typename T, bool CODES, uint32_t RF>
+__global__ __launch_bounds__(ADAPT_THREADS) void adapters_grad_kernel(AdaptersSumArgs g) {
+    constexpr uint32_t DEPTH = 4;              // four rows each
+    __shared__ v4f s_sum[2][8 * RF][64];
+    const uint32_t lane = threadIdx.x & 63u, wave = uniform_u32(threadIdx.x >> 6), group = lane / 16u, r16 = lane & 15u;
+    const uint32_t slabs_a = (g.k + ADAPT_SLAB - 1u) / ADAPT_SLAB, slabs = slabs_a + (g.n + ADAPT_SLAB - 1u) / ADAPT_SLAB;
+    const uint32_t adapter = blockIdx.x / slabs, nth_slab = blockIdx.x - adapter * slabs;
+    const bool of_a = nth_slab < slabs_a;
+    const uint32_t slab = of_a ? nth_slab : nth_slab - slabs_a, cols = of_a ? g.k : g.n;
+    const uint32_t c = slab * ADAPT_SLAB + 8u * r16;
+    const float* s = of_a ? g.up : g.down;
+    const uint64_t ld_s = of_a ? g.ld_up : g.ld_down;
+    const uint32_t from = g.first[adapter], count = g.first[adapter + 1] - from;
+    const uint32_t each = ((count + g.parts - 1u) / g.parts + 15u) & ~15u, q0 = min(blockIdx.y * each, count), q1 = min(q0 + each, count);
+    const uint32_t* list = g.rows + from;
+    for (uint32_t rank0 = 0; rank0 < g.rank; rank0 += 16u * RF) {
+        v4f acc[RF][8];
+#pragma unroll
+        for (uint32_t f = 0; f < RF; ++f)
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) acc[f][j] = v4f{0, 0, 0, 0};
+        for (uint32_t at = q0 + wave * 4u * DEPTH; at < q1; at += ADAPT_WAVES * 4u * DEPTH) {
+            Eight<T> v[DEPTH];
+            uint2 w[DEPTH];
+            float p[DEPTH][RF];
+            const bool codes = CODES && of_a;
+#pragma unroll
+            for (uint32_t d = 0; d < DEPTH; ++d) {
+                const uint32_t nth = at + 4u * d + group;
+                const uint64_t row = list[min(nth, q1 - 1u)];
+                if (codes) {
+                    // a row's codes are there up to a multiple of 16
+                    w[d] = c < cols ? *reinterpret_cast<const uint2*>(static_cast<const int8_t*>(g.x) + row * g.ld_x + c) : make_uint2(0u, 0u);
+                } else {
+                    const T* from_row = of_a ? static_cast<const T*>(g.x) + row * g.ld_x : static_cast<const T*>(g.g) + row * g.ld_g;
+                    fetch8(from_row, c, cols, v[d]);
+                }
+                const float by = codes ? g.x_scale[row] : 1.0f;
+#pragma unroll
+                for (uint32_t f = 0; f < RF; ++f) {
+                    const uint32_t r = rank0 + 16u * f + r16;
+                    const float one = s[row * ld_s + min(r, g.rank - 1u)] * by;
+                    p[d][f] = nth < q1 ? one : 0.0f;
+                }
+            }
+#pragma unroll
+            for (uint32_t d = 0; d < DEPTH; ++d) {
+                float x[8];
+                if (codes) {
+#pragma unroll
+                    for (uint32_t j = 0; j < 8; ++j) x[j] = (float)(int8_t)((j < 4 ? w[d].x : w[d].y) >> (8 * (j % 4)));
+                } else {
+                    place8(c, cols, v[d]);
+                    v[d].floats(x);
+                }
+                if (at + 4u * d + group >= q1) {           // behind the last row: its numbers once more, which do not count
+#pragma unroll
+                    for (uint32_t j = 0; j < 8; ++j) x[j] = 0.0f;
+                }
+#pragma unroll
+                for (uint32_t f = 0; f < RF; ++f)
+#pragma unroll
+                    for (uint32_t j = 0; j < 8; ++j) acc[f][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(p[d][f], x[j], acc[f][j], 0, 0, 0);
+            }
+        }
+        // wavefronts 2 and 3 to 0 and 1, then 1 to 0
+#pragma unroll
+        for (uint32_t half = 2; half > 0; half >>= 1) {
+            __syncthreads();
+            if (wave >= half && wave < 2 * half) {
+#pragma unroll
+                for (uint32_t f = 0; f < RF; ++f)
+#pragma unroll
+                    for (uint32_t j = 0; j < 8; ++j) s_sum[wave - half][8 * f + j][lane] = acc[f][j];
+            }
+            __syncthreads();
+            if (wave < half) {
+#pragma unroll
+                for (uint32_t f = 0; f < RF; ++f)
+#pragma unroll
+                    for (uint32_t j = 0; j < 8; ++j) acc[f][j] += s_sum[wave][8 * f + j][lane];
+            }
+        }
+        if (wave != 0) continue;
+        // lane: ranks 4 group on, columns c on
+        float* out = g.parts == 1 ? (of_a ? g.da : g.db) + (uint64_t)adapter * cols * g.rank
+                                  : g.partial + (((uint64_t)blockIdx.y * g.adapters + adapter) * (g.k + g.n) + (of_a ? 0 : g.k)) * g.rank;
+#pragma unroll
+        for (uint32_t f = 0; f < RF; ++f)
+#pragma unroll
+            for (uint32_t e = 0; e < 4; ++e) {
+                const uint32_t r = rank0 + 16u * f + 4u * group + e;
+                if (r >= g.rank) continue;
+#pragma unroll
+                for (uint32_t j = 0; j < 8; ++j)
+                    if (c + j < cols) out[of_a ? (uint64_t)r * cols + c + j : (uint64_t)(c + j) * g.rank + r] = acc[f][j][e];
+            }
+    }
+}
+
+// The parts' sums of all adapters, in order.
+__global__ __launch_bounds__(ADAPT_THREADS) void adapters_join_kernel(AdaptersSumArgs g) {
+    const uint64_t of_a = (uint64_t)g.k * g.rank, each = of_a + (uint64_t)g.n * g.rank, all = each * g.adapters;
+    for (uint64_t u = (uint64_t)blockIdx.x * ADAPT_THREADS + threadIdx.x; u < all; u += (uint64_t)gridDim.x * ADAPT_THREADS) {
+        float v = g.partial[u];
+        for (uint32_t p = 1; p < g.parts; ++p) v += g.partial[(uint64_t)p * all + u];
+        const uint64_t i = u / each, at = u - i * each;
+        if (at < of_a) g.da[i * of_a + at] = v;
+        else g.db[i * (each - of_a) + at - of_a] = v;
+    }
+}
+
+template <typename T, bool CODES>
+static void launch_sums_as(shifter_ctx* ctx, const AdaptersSumArgs& g) {
+    const dim3 grid(((g.k + ADAPT_SLAB - 1u) / ADAPT_SLAB + (g.n + ADAPT_SLAB - 1u) / ADAPT_SLAB) * g.adapters, g.parts);
+    const uint64_t pad = adapt_pad(g.rank);
+    if (pad <= 16) adapters_grad_kernel<T, CODES, 1><<<grid, ADAPT_THREADS, 0, ctx->stream>>>(g);
+    else if (pad <= 32) adapters_grad_kernel<T, CODES, 2><<<grid, ADAPT_THREADS, 0, ctx->stream>>>(g);
+    else adapters_grad_kernel<T, CODES, 4><<<grid, ADAPT_THREADS, 0, ctx->stream>>>(g);
+}
+
+template <typename T>
+static void launch_gradients(shifter_ctx* ctx, int dtype, const AdaptersGradArgs& g) {
+    const AdaptersGradPlan p = adapters_grad_plan(g.m, g.n, g.k, g.rank, g.adapters, sizeof(T));
+    auto at = [&](uint64_t offset) { return g.work + offset; };
+    const uint32_t pad = (uint32_t)adapt_pad(g.rank);
+    AdaptersTurnArgs t{};
+    t.which = g.which; t.a = g.a; t.b = g.b; t.m = g.m; t.n = g.n; t.k = g.k; t.rank = g.rank; t.adapters = g.adapters;
+    t.a_turned = at(p.a); t.b_turned = at(p.b);
+    t.rows = reinterpret_cast<uint32_t*>(at(p.rows)); t.first = reinterpret_cast<uint32_t*>(at(p.first));
+    if (g.adapters) {
+        ProfileScope ps(ctx, K_ADAPTERS_TURN);
+        const uint64_t blocks = g.adapters * (1ull + (g.k + 63u) / 64u + (g.n + 63u) / 64u);
+        adapters_turn_kernel<T><<<(uint32_t)blocks, ADAPT_THREADS, 0, ctx->stream>>>(t);
+    }
+    AdaptersDownArgs d{};
+    d.which = g.which; d.scale = g.scale; d.m = g.m; d.rank = g.rank; d.adapters = g.adapters;
+    d.s = reinterpret_cast<float*>(at(p.sums));
+    AdaptersUpArgs u{};
+    u.s = d.s; u.which = g.which; u.m = g.m; u.rank = g.rank; u.adapters = g.adapters;
+    const float* down = g.down;
+    uint64_t ld_down = g.rank;
+    if (!down && g.m) {                        // once more; its sums are joined by a pass that writes no columns
+        d.x = g.x; d.ld_x = g.ld_x; d.x_scale = g.x_scale; d.a = g.a; d.k = g.k; d.parts = p.parts_x;
+        launch_down(ctx, dtype, d);
+        u.parts = p.parts_x; u.n = 0; u.b = g.b; u.down = reinterpret_cast<float*>(at(p.down)); u.down_cols = pad;
+        launch_up(ctx, dtype, dtype, u);
+        down = u.down;
+        ld_down = pad;
+    }
+    d.x = g.g; d.ld_x = g.ld_g; d.x_scale = nullptr; d.a = at(p.b); d.k = g.n; d.parts = p.parts_g;
+    if (g.m) launch_down(ctx, dtype, d);
+    u.parts = p.parts_g; u.n = g.dx ? g.k : 0; u.b = at(p.a); u.out = g.dx; u.ld_out = g.ld_dx;
+    u.down = reinterpret_cast<float*>(at(p.up)); u.down_cols = pad;
+    if (g.m) launch_up(ctx, dtype, dtype, u);
+    if (g.adapters == 0 || (g.n == 0 && g.k == 0)) return;
+    AdaptersSumArgs s{};
+    s.x = g.x; s.ld_x = g.ld_x; s.x_scale = g.x_scale; s.g = g.g; s.ld_g = g.ld_g;
+    s.up = u.down; s.ld_up = pad; s.down = down; s.ld_down = ld_down;
+    s.rows = t.rows; s.first = t.first; s.n = g.n; s.k = g.k; s.rank = g.rank; s.adapters = g.adapters; s.parts = p.parts_rows;
+    s.da = g.da; s.db = g.db; s.partial = reinterpret_cast<float*>(at(p.partial));
+    ProfileScope ps(ctx, K_ADAPTERS_GRAD);
+    if (g.x_scale) launch_sums_as<T, true>(ctx, s);
+    else launch_sums_as<T, false>(ctx, s);
+    if (s.parts > 1) {
+        const uint64_t all = (uint64_t)g.adapters * (g.k + g.n) * g.rank;
+        adapters_join_kernel<<<(uint32_t)std::min<uint64_t>((all + ADAPT_THREADS - 1u) / ADAPT_THREADS, 4096), ADAPT_THREADS, 0, ctx->stream>>>(s);
+    }
+}
+
+void launch_adapters_grad(shifter_ctx* ctx, int dtype, const AdaptersGradArgs& g) {
+    if (dtype == SHIFTER_F32) launch_gradients<float>(ctx, dtype, g);
+    else if (dtype == SHIFTER_BF16) launch_gradients<__bf16>(ctx, dtype, g);
+    else launch_gradients<_Float16>(ctx, dtype, g);
+}
+
+}  // namespace shifter

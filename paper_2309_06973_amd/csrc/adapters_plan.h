@@ -1,0 +1,89 @@
+// Low-rank adapters: how a call is shared out, its workspace and the checks of its sizes.  Plain C++: the host and the
+// tests share it.
+#pragma once
+
+#include "log_probs_plan.h"
+
+namespace shifter {
+
+constexpr uint32_t ADAPT_MAX_RANK = 128;
+constexpr uint64_t ADAPT_MAX_ROWS = 1ull << 27;    // tiles of 16 rows, 256 threads each: less than 2^32 threads
+constexpr uint32_t ADAPT_STEP = 64;                // columns of a step of the products over long rows
+constexpr uint32_t ADAPT_SLAB = 128;               // columns of a block of the gradient's sums over rows
+
+inline uint64_t adapt_pad(uint64_t rank) { return (rank + 15u) & ~15ull; }
+
+// Tiles of 16 rows that a block works on together: they share what it reads of an adapter.
+inline uint32_t adapt_tiles(uint64_t m, uint32_t rank) { return m <= 256 ? 1u : adapt_pad(rank) <= 16 ? 4u : 2u; }
+
+// Blocks that share the k columns of a tile's rows; each leaves its sums.
+inline uint32_t adapt_parts(uint64_t m, uint64_t k, uint32_t rank) {
+    const uint64_t rows = 16u * adapt_tiles(m, rank), blocks = (m + rows - 1u) / rows, steps = (k + ADAPT_STEP - 1u) / ADAPT_STEP;
+    uint64_t parts = blocks ? 512u / blocks : 1u;
+    if (parts > steps / 4u) parts = steps / 4u;    // each of a block's four wavefronts has a step
+    return parts < 1 ? 1u : parts > 32 ? 32u : (uint32_t)parts;
+}
+
+struct AdaptersPlan {
+    uint32_t parts;
+    uint64_t bytes;
+};
+inline AdaptersPlan adapters_plan(uint64_t m, uint64_t k, uint32_t rank) {
+    AdaptersPlan p{};
+    p.parts = adapt_parts(m, k, rank);
+    p.bytes = p.parts * m * adapt_pad(rank) * 4u;
+    return p;
+}
+
+// The gradient's workspace: offsets of its pieces.
+struct AdaptersGradPlan {
+    uint32_t parts_x, parts_g;         // of x A' and of g B
+    uint32_t parts_rows;               // blocks that share an adapter's rows
+    uint64_t down, up;                 // [m][pad]: x A' where it is not given, and g B
+    uint64_t sums;                     // [parts][m][pad]
+    uint64_t a, b;                     // the adapters, turned: [adapters][k][rank], [adapters][rank][n]
+    uint64_t rows, first;              // rows sorted by their adapter; each adapter's first, and the number of all
+    uint64_t partial;                  // [parts_rows][adapters][k + n][rank]
+    uint64_t bytes;
+};
+inline AdaptersGradPlan adapters_grad_plan(uint64_t m, uint64_t n, uint64_t k, uint32_t rank, uint64_t adapters, uint64_t size) {
+    AdaptersGradPlan p{};
+    const uint64_t pad = adapt_pad(rank);
+    p.parts_x = adapt_parts(m, k, rank);
+    p.parts_g = adapt_parts(m, n, rank);
+    const uint64_t slabs = ((k + ADAPT_SLAB - 1u) / ADAPT_SLAB + (n + ADAPT_SLAB - 1u) / ADAPT_SLAB) * (adapters ? adapters : 1u);
+    uint64_t parts = slabs ? 512u / slabs : 1u;
+    if (parts > m / 64u) parts = m / 64u;
+    p.parts_rows = parts < 1 ? 1u : parts > 16 ? 16u : (uint32_t)parts;
+    uint64_t at = 0;
+    auto take = [&](uint64_t bytes) {
+        const uint64_t was = at;
+        at += (bytes + 255u) & ~255ull;
+        return was;
+    };
+    p.down = take(m * pad * 4u);
+    p.up = take(m * pad * 4u);
+    p.sums = take((p.parts_x > p.parts_g ? p.parts_x : p.parts_g) * m * pad * 4u);
+    p.a = take(adapters * k * rank * size);
+    p.b = take(adapters * n * rank * size);
+    p.rows = take(4u * m);
+    p.first = take(4u * (adapters + 1u));
+    p.partial = take(p.parts_rows > 1 ? p.parts_rows * adapters * (k + n) * rank * 4u : 0u);
+    p.bytes = at;
+    return p;
+}
+
+// What is wrong with the sizes, or nullptr; *capacity: they are more than a call holds.
+inline const char* adapters_bad_sizes(uint64_t m, uint64_t n, uint64_t k, uint64_t rank, uint64_t adapters, bool* capacity) {
+    *capacity = false;
+    if (rank < 1 || rank > ADAPT_MAX_RANK) return "a rank that is not 1 to 128";
+    if (n > Q8_MAX_ROWS || k > Q8_MAX_ROWS || adapters > (1u << 24)) return "more than 2^31 - 1 columns or 2^24 adapters";
+    *capacity = true;
+    if (m > ADAPT_MAX_ROWS) return "more than 2^27 rows";
+    // the gradient's blocks of 64 columns of all adapters, 256 threads each
+    if (adapters * (1u + (k + 63u) / 64u + (n + 63u) / 64u) >= 1ull << 24) return "more columns of all adapters than a launch holds";
+    *capacity = false;
+    return nullptr;
+}
+
+}  // namespace shifter

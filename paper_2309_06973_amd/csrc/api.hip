@@ -1817,7 +1817,8 @@ extern "C" int shifter_weight_grad_q8(shifter_ctx* ctx, const void* d_g, int dty
 
 // ---- what a network answers with, and what it is trained on ---------------------------
 
-static_assert(SHIFTER_LOG_PROBS_MAX_TOP == LOGP_MAX_TOP && SHIFTER_LEARN_ZERO == LEARN_TICKETS, "the limits the header names");
+static_assert(SHIFTER_LOG_PROBS_MAX_TOP == LOGP_MAX_TOP && SHIFTER_LEARN_ZERO == LEARN_TICKETS && SHIFTER_ADAPTERS_MAX_RANK == ADAPT_MAX_RANK,
+              "the limits the header names");
 
 static const char* log_probs_bad_sizes(uint64_t rows, uint64_t cols, uint64_t top) {
     if (rows > Q8_MAX_ROWS || cols > Q8_MAX_ROWS) return "more than 2^31 - 1 rows or columns";
@@ -1935,4 +1936,96 @@ extern "C" int shifter_clip_grad_norm(shifter_ctx* ctx, const shifter_grad* h_gr
     } catch (const std::bad_alloc&) {
         return SHIFTER_ERR_OOM;
     }
+}
+
+extern "C" int shifter_adapters_layout(uint64_t m, uint64_t n, uint64_t k, uint64_t rank, uint64_t adapters, uint64_t* h_work_bytes) {
+    if (!h_work_bytes) return fail(nullptr, SHIFTER_ERR_INVALID_ARG, "adapters_layout: NULL argument");
+    *h_work_bytes = 0;
+    bool capacity;
+    if (const char* why = adapters_bad_sizes(m, n, k, rank, adapters, &capacity))
+        return fail(nullptr, capacity ? SHIFTER_ERR_CAPACITY : SHIFTER_ERR_INVALID_ARG, std::string("adapters_layout: ") + why);
+    *h_work_bytes = adapters_plan(m, k, (uint32_t)rank).bytes;
+    return SHIFTER_OK;
+}
+
+extern "C" int shifter_adapters_grad_layout(uint64_t m, uint64_t n, uint64_t k, uint64_t rank, uint64_t adapters, int dtype,
+                                            uint64_t* h_work_bytes) {
+    if (!h_work_bytes) return fail(nullptr, SHIFTER_ERR_INVALID_ARG, "adapters_grad_layout: NULL argument");
+    *h_work_bytes = 0;
+    if (dtype != SHIFTER_F32 && dtype != SHIFTER_BF16 && dtype != SHIFTER_F16)
+        return fail(nullptr, SHIFTER_ERR_INVALID_ARG, "adapters_grad_layout: unknown element type");
+    bool capacity;
+    if (const char* why = adapters_bad_sizes(m, n, k, rank, adapters, &capacity))
+        return fail(nullptr, capacity ? SHIFTER_ERR_CAPACITY : SHIFTER_ERR_INVALID_ARG, std::string("adapters_grad_layout: ") + why);
+    *h_work_bytes = adapters_grad_plan(m, n, k, (uint32_t)rank, adapters, element_size(dtype)).bytes;
+    return SHIFTER_OK;
+}
+
+// What both calls take: sizes, x, the adapters and the numbers of the rows' adapters.
+template <typename Args>
+static int adapters_enter(shifter_ctx* ctx, const char* fn, const Args* a) {
+    if (!a) return fail(ctx, SHIFTER_ERR_INVALID_ARG, std::string(fn) + ": NULL argument");
+    int rc = q8_enter(ctx, fn, a->dtype, 0, 0);
+    if (rc) return rc;
+    const std::string name = std::string(fn) + ": ";
+    auto refuse = [&](const char* why) { return fail(ctx, SHIFTER_ERR_INVALID_ARG, name + why); };
+    bool capacity;
+    if (const char* why = adapters_bad_sizes(a->m, a->n, a->k, a->rank, a->adapters, &capacity))
+        return fail(ctx, capacity ? SHIFTER_ERR_CAPACITY : SHIFTER_ERR_INVALID_ARG, name + why);
+    const uintptr_t size = element_size(a->dtype);
+    if (const char* why = a->d_q_scale ? q8_bad_codes(a->d_x, a->d_q_scale, a->m, a->k, a->ld_x) : q8_bad_rows(a->d_x, size, a->m, a->k, a->ld_x))
+        return refuse(why);
+    if ((a->m && !a->d_which) || (a->adapters && ((a->k && !a->d_a) || (a->n && !a->d_b)))) return refuse("NULL pointer argument");
+    if (misaligned(a->d_which, 8) || misaligned(a->d_scale, 4) || misaligned(a->d_down, 4) || misaligned(a->d_a, size) || misaligned(a->d_b, size))
+        return refuse("a pointer is not aligned to its elements");
+    return SHIFTER_OK;
+}
+static int adapters_work(shifter_ctx* ctx, const char* fn, uint64_t need, const void* d_work, uint64_t work_bytes) {
+    if (work_bytes < need)
+        return fail(ctx, SHIFTER_ERR_INVALID_ARG, std::string(fn) + ": workspace too small, needs " + std::to_string(need) + " bytes");
+    if (need && (!d_work || misaligned(d_work, 256)))
+        return fail(ctx, SHIFTER_ERR_INVALID_ARG, std::string(fn) + ": the workspace must be 256-byte aligned");
+    return SHIFTER_OK;
+}
+
+extern "C" int shifter_adapters(shifter_ctx* ctx, const shifter_adapters_args* a) {
+    int rc = adapters_enter(ctx, "adapters", a);
+    if (rc || (rc = q8_enter(ctx, "adapters", a->y_dtype, 0, 0))) return rc;
+    const uintptr_t size = element_size(a->y_dtype);
+    Q8_REFUSE("adapters", q8_bad_rows(a->d_y, size, a->m, a->n, a->ld_y));
+    Q8_REFUSE("adapters", q8_bad_rows(a->d_out, size, a->m, a->n, a->ld_out));
+    if (a->d_out == a->d_y && a->ld_out != a->ld_y && a->m > 1 && a->n)
+        return fail(ctx, SHIFTER_ERR_INVALID_ARG, "adapters: d_out is d_y with another stride");
+    if ((rc = adapters_work(ctx, "adapters", adapters_plan(a->m, a->k, (uint32_t)a->rank).bytes, a->d_work, a->work_bytes))) return rc;
+    if (a->m == 0 || (a->n == 0 && !a->d_down)) return SHIFTER_OK;
+    AdaptersArgs g{};
+    g.x = a->d_x; g.x_scale = a->d_q_scale; g.a = a->d_a; g.b = a->d_b; g.which = a->d_which; g.scale = a->d_scale;
+    g.y = a->d_y; g.out = a->d_out; g.down = a->d_down; g.ld_x = a->ld_x; g.ld_y = a->ld_y; g.ld_out = a->ld_out;
+    g.m = (uint32_t)a->m; g.n = (uint32_t)a->n; g.k = (uint32_t)a->k; g.rank = (uint32_t)a->rank; g.adapters = (uint32_t)a->adapters;
+    g.work = static_cast<uint8_t*>(a->d_work);
+    launch_adapters(ctx, a->dtype, a->y_dtype, g);
+    return after_launch(ctx, "adapters");
+}
+
+extern "C" int shifter_adapters_grad(shifter_ctx* ctx, const shifter_adapters_grad_args* a) {
+    int rc = adapters_enter(ctx, "adapters_grad", a);
+    if (rc) return rc;
+    const uintptr_t size = element_size(a->dtype);
+    Q8_REFUSE("adapters_grad", q8_bad_rows(a->d_g, size, a->m, a->n, a->ld_g));
+    if (a->d_dx) Q8_REFUSE("adapters_grad", q8_bad_rows(a->d_dx, size, a->m, a->k, a->ld_dx));
+    if (a->adapters && ((a->k && !a->d_da) || (a->n && !a->d_db))) return fail(ctx, SHIFTER_ERR_INVALID_ARG, "adapters_grad: NULL pointer argument");
+    if (misaligned(a->d_da, 4) || misaligned(a->d_db, 4))
+        return fail(ctx, SHIFTER_ERR_INVALID_ARG, "adapters_grad: a pointer is not aligned to its elements");
+    if (a->m && (a->d_dx == a->d_x || a->d_dx == a->d_g) && a->d_dx)
+        return fail(ctx, SHIFTER_ERR_INVALID_ARG, "adapters_grad: d_dx is not d_x or d_g, which are read to the end");
+    const uint64_t need = adapters_grad_plan(a->m, a->n, a->k, (uint32_t)a->rank, a->adapters, size).bytes;
+    if ((rc = adapters_work(ctx, "adapters_grad", need, a->d_work, a->work_bytes))) return rc;
+    AdaptersGradArgs g{};
+    g.x = a->d_x; g.x_scale = a->d_q_scale; g.g = a->d_g; g.a = a->d_a; g.b = a->d_b; g.which = a->d_which; g.scale = a->d_scale;
+    g.down = a->d_down; g.dx = a->d_dx; g.da = a->d_da; g.db = a->d_db;
+    g.ld_x = a->ld_x; g.ld_g = a->ld_g; g.ld_dx = a->ld_dx;
+    g.m = (uint32_t)a->m; g.n = (uint32_t)a->n; g.k = (uint32_t)a->k; g.rank = (uint32_t)a->rank; g.adapters = (uint32_t)a->adapters;
+    g.work = static_cast<uint8_t*>(a->d_work);
+    launch_adapters_grad(ctx, a->dtype, g);
+    return after_launch(ctx, "adapters_grad");
 }

@@ -587,6 +587,147 @@ PyObject* grad_norm(PyObject* const* a) {
     return THPVariable_Wrap(std::move(norm));
 }
 
+// The adapters of a call, and x: elements of their type, or an 8-bit matrix.
+struct Adapted {
+    at::ScalarType type;
+    int dtype;
+    const void *x, *a, *b;
+    uint64_t ld_x, m, n, k, rank, adapters;
+    const float *q_scale = nullptr, *scale = nullptr;
+    const int64_t* which;
+    Adapted(const Handle& h, PyObject* ox, PyObject* oa, PyObject* ob, PyObject* owhich, PyObject* oscale) {
+        const at::Tensor &ta = tensor_of(oa, "a"), &tb = tensor_of(ob, "b");
+        type = ta.scalar_type();
+        dtype = code_of(type);
+        TORCH_CHECK_VALUE(dtype >= 0 && ta.dim() == 3 && ta.is_contiguous(), "a must be a contiguous fp32, bf16 or fp16 tensor of adapters, rank, columns of x");
+        adapters = (uint64_t)ta.size(0);
+        rank = (uint64_t)ta.size(1);
+        k = (uint64_t)ta.size(2);
+        TORCH_CHECK_VALUE(tb.dim() == 3 && tb.scalar_type() == type && tb.is_contiguous() && (uint64_t)tb.size(0) == adapters &&
+                          (uint64_t)tb.size(2) == rank, "b must be a contiguous tensor of adapters, columns of y, rank, of a's type");
+        n = (uint64_t)tb.size(1);
+        here(h, ta, "a");
+        here(h, tb, "b");
+        a = ta.data_ptr();
+        b = tb.data_ptr();
+        if (THPVariable_Check(ox)) {
+            const at::Tensor& tx = THPVariable_Unpack(ox);
+            TORCH_CHECK_VALUE(tx.scalar_type() == type, "x must have a's type, or be a Q8Matrix");
+            const Rows r = rows_of(h, tx, "x");
+            TORCH_CHECK_VALUE(r.cols == k, "x must have a's columns");
+            x = r.p;
+            ld_x = r.ld;
+            m = r.rows;
+        } else {
+            const Codes c = codes_of(h, ox, "x");
+            TORCH_CHECK_VALUE(c.cols == k, "x must have a's columns");
+            x = c.q;
+            ld_x = c.ld;
+            m = c.rows;
+            q_scale = c.scale;
+        }
+        which = numbers_of(h, owhich, m, "which");
+        if (!is_none(oscale)) scale = vector_of(h, oscale, adapters, "scale");
+    }
+    template <typename Args>
+    void put(Args& g) const {
+        g.d_x = x; g.ld_x = ld_x; g.d_q_scale = q_scale; g.m = m; g.n = n; g.k = k; g.rank = rank; g.adapters = adapters;
+        g.d_a = a; g.d_b = b; g.d_which = which; g.d_scale = scale; g.dtype = dtype;
+    }
+};
+
+// A float32 matrix without gaps.
+float* numbers32_of(const Handle& h, PyObject* o, uint64_t rows, uint64_t cols, const char* what) {
+    const at::Tensor& t = tensor_of(o, what);
+    same(t, rows, cols, at::kFloat, what);
+    TORCH_CHECK_VALUE(t.is_contiguous(), what, " must be contiguous");
+    here(h, t, what);
+    return static_cast<float*>(t.data_ptr());
+}
+
+// ctx, device, y, x, a, b, which, scale, out, down, room -> out
+PyObject* adapters(PyObject* const* a) {
+    const Handle h = handle_of(a);
+    const at::Tensor& ty = tensor_of(a[2], "y");
+    const int given[] = {2, 3, 4, 5, 7};           // elements that may need a gradient
+    if (!is_none(a[8]) || !is_none(a[9]))
+        for (int i : given)
+            if (THPVariable_Check(a[i])) constant(THPVariable_Unpack(a[i]), "an operand");
+    const Adapted s(h, a[3], a[4], a[5], a[6], a[7]);
+    same(ty, s.m, s.n, ty.scalar_type(), "y");
+    const Rows y = rows_of(h, ty, "y");
+    shifter_adapters_args g{};
+    s.put(g);
+    g.d_y = y.p;
+    g.ld_y = y.ld;
+    g.y_dtype = y.dtype;
+    at::Tensor out;
+    if (is_none(a[8])) {
+        out = new_rows(h, s.m, s.n, ty.scalar_type());
+    } else {
+        out = tensor_of(a[8], "out");
+        constant(out, "out");
+        same(out, s.m, s.n, ty.scalar_type(), "out");
+    }
+    const Rows r = rows_of(h, out, "out");
+    g.d_out = r.p;
+    g.ld_out = r.ld;
+    if (!is_none(a[9])) {
+        constant(tensor_of(a[9], "down"), "down");
+        g.d_down = numbers32_of(h, a[9], s.m, s.rank, "down");
+    }
+    check(shifter_adapters_layout(s.m, s.n, s.k, s.rank, s.adapters, &g.work_bytes), Py_None);
+    const Work work(a[10], g.work_bytes);
+    g.d_work = work.p;
+    // with the interpreter's lock: the launches share the handle's workspace
+    check(shifter_adapters(h.ctx, &g), a[0]);
+    if (!is_none(a[9])) written(tensor_of(a[9], "down"));
+    if (is_none(a[8]))
+        for (int i : given)
+            if (THPVariable_Check(a[i])) out = tied(std::move(out), THPVariable_Unpack(a[i]), at::Tensor(), "adapters");
+    return wrap(a[8], std::move(out));
+}
+
+// ctx, device, g, x, a, b, which, scale, down, dx wanted, room -> (dx, da, db)
+PyObject* adapters_grad(PyObject* const* a) {
+    const Handle h = handle_of(a);
+    const at::Tensor& tg = tensor_of(a[2], "g");
+    const Adapted s(h, a[3], a[4], a[5], a[6], a[7]);
+    same(tg, s.m, s.n, s.type, "g");
+    const Rows r = rows_of(h, tg, "g");
+    shifter_adapters_grad_args g{};
+    s.put(g);
+    g.d_g = r.p;
+    g.ld_g = r.ld;
+    if (!is_none(a[8])) g.d_down = numbers32_of(h, a[8], s.m, s.rank, "down");
+    at::Tensor out[3];
+    if (truth(a[9])) {
+        out[0] = new_rows(h, s.m, s.k, s.type);
+        g.d_dx = out[0].data_ptr();
+        g.ld_dx = s.k;
+    }
+    out[1] = new_tensor(h, {(int64_t)s.adapters, (int64_t)s.rank, (int64_t)s.k}, at::kFloat);
+    out[2] = new_tensor(h, {(int64_t)s.adapters, (int64_t)s.n, (int64_t)s.rank}, at::kFloat);
+    g.d_da = static_cast<float*>(out[1].data_ptr());
+    g.d_db = static_cast<float*>(out[2].data_ptr());
+    check(shifter_adapters_grad_layout(s.m, s.n, s.k, s.rank, s.adapters, s.dtype, &g.work_bytes), Py_None);
+    const Work work(a[10], g.work_bytes);
+    g.d_work = work.p;
+    check(shifter_adapters_grad(h.ctx, &g), a[0]);         // with the interpreter's lock, as above
+    Owned all(PyTuple_New(3));
+    for (int i = 0; i < 3; ++i) {
+        if (!out[i].defined()) {
+            Py_INCREF(Py_None);
+            PyTuple_SET_ITEM(all.p, i, Py_None);
+            continue;
+        }
+        for (int j : {2, 3, 4, 5, 7, 8})
+            if (THPVariable_Check(a[j])) out[i] = tied(std::move(out[i]), THPVariable_Unpack(a[j]), at::Tensor(), "adapters_grad");
+        PyTuple_SET_ITEM(all.p, i, THPVariable_Wrap(std::move(out[i])));
+    }
+    return all.release();
+}
+
 // Q8Matrix, failed(code, ctx): what the functions below make and raise.
 PyObject* bind(PyObject* const* a) {
     Py_INCREF(a[0]);
@@ -599,7 +740,7 @@ PyObject* bind(PyObject* const* a) {
 #define Q8_ENTRY(name, n) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&entry<n, name>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {Q8_ENTRY(bind, 2), Q8_ENTRY(quantize, 5), Q8_ENTRY(dequantize, 5), Q8_ENTRY(rms_norm, 8),
                          Q8_ENTRY(matmul, 8), Q8_ENTRY(weight_grad, 9), Q8_ENTRY(log_probs, 8), Q8_ENTRY(log_probs_grad, 11),
-                         Q8_ENTRY(grad_norm, 7), {nullptr, nullptr, 0, nullptr}};
+                         Q8_ENTRY(grad_norm, 7), Q8_ENTRY(adapters, 11), Q8_ENTRY(adapters_grad, 11), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_q8", "The 8-bit operators' calls; see q8.py.", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
 

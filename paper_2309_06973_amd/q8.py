@@ -189,6 +189,21 @@ class Q8:
         the tensors of ``out`` (laid out as their gradients).  What is written may not overlap anything else."""
         return self._calls.grad_norm(*self._enter(), grads, masks, float(max_norm), out, self._joined)
 
+    def adapters(self, y: torch.Tensor, x, a: torch.Tensor, b: torch.Tensor, which: torch.Tensor,
+                 scale: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                 down: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """y + scale[i] * (x a[i]') b[i]' for each row, i = which[row] (int64; negative: no adapter, not below the adapters:
+        NaN): low-rank adapters of many requests beside a projection that gave y.  x: elements of a's type, or the
+        Q8Matrix that the projection read.  a: [adapters, rank, x's columns], b: [adapters, y's columns, rank], rank up to
+        SHIFTER_ADAPTERS_MAX_RANK.  ``out`` may be y; down: fp32 [rows, rank], gets scale[i] * x a[i]' for adapters_grad."""
+        return self._calls.adapters(*self._enter(), y, x, a, b, which, scale, out, down, self._room)
+
+    def adapters_grad(self, g: torch.Tensor, x, a: torch.Tensor, b: torch.Tensor, which: torch.Tensor,
+                      scale: Optional[torch.Tensor] = None, down: Optional[torch.Tensor] = None, dx: bool = True):
+        """(gradient of x in a's type or None, of a and of b in fp32) from g, that of adapters' result, in a's type; y's is g
+        itself.  down: as adapters wrote it, or it is worked out again."""
+        return self._calls.adapters_grad(*self._enter(), g, x, a, b, which, scale, down, dx, self._room)
+
 
 def _rows(x: torch.Tensor) -> torch.Tensor:
     """x with its columns side by side and its rows one after another."""
@@ -303,3 +318,56 @@ def target_log_probs(x: torch.Tensor, target: torch.Tensor, ops: Q8, scale: floa
     _recording("target_log_probs", x)
     rows = _rows(x.reshape(target.numel(), x.shape[-1]))
     return tuple(t.view(target.shape) for t in _LogProbs.apply(rows, target.reshape(-1).contiguous(), ops, scale))
+
+
+class _AdaptersGrad(torch.autograd.Function):
+    """The gradients where they may be differentiated again: an error then."""
+    @staticmethod
+    def forward(ctx, g, x, a, b, ops, x8, which, scale, down, dx):
+        got = ops.adapters_grad(g, x if x8 is None else x8, a, b, which, scale, down, dx)
+        return got if got[0] is not None else (got[1].new_empty(0), *got[1:])
+
+    @staticmethod
+    def backward(ctx, *v):
+        raise RuntimeError("adapted: the gradients have no derivative of their own")
+
+
+class _Adapted(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, y, x, a, b, ops, x8, which, scale):
+        down = torch.empty(y.shape[0], a.shape[1], device=y.device)
+        out = ops.adapters(y, x if x8 is None else x8, a, b, which, scale, down=down)
+        ctx.save_for_backward(x, a, b, which, down, *(t for t in (scale, *((x8.q, x8.scale) if x8 is not None else ())) if t is not None))
+        ctx.ops, ctx.scaled, ctx.cols = ops, scale is not None, None if x8 is None else x8.cols
+        return out
+
+    @staticmethod
+    def backward(ctx, g):
+        x, a, b, which, down, *rest = ctx.saved_tensors
+        scale = rest.pop(0) if ctx.scaled else None
+        x8 = Q8Matrix(*rest, ctx.cols) if rest else None
+        dx = da = db = None
+        if any(ctx.needs_input_grad[1:4]):
+            dx, da, db = _AdaptersGrad.apply(_rows(g), x, a, b, ctx.ops, x8, which, scale, down, ctx.needs_input_grad[1])
+            dx = dx if ctx.needs_input_grad[1] else None
+            da, db = da.to(a.dtype), db.to(b.dtype)
+        return g, dx, da, db, None, None, None, None
+
+
+def adapted(y: torch.Tensor, x, a: torch.Tensor, b: torch.Tensor, which: torch.Tensor, ops: Q8,
+            scale: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Q8.adapters with the gradients of y, x (unless it is a Q8Matrix), a and b: y and x [..., columns] of a's type,
+    which int64 [...].  scale is a constant.  The gradients can not be differentiated again, which is an error, and not be
+    recorded: adapters and adapters_grad can."""
+    if scale is not None and scale.requires_grad and torch.is_grad_enabled():
+        raise ValueError("scale needs a gradient, which adapted does not pass on: detach it")
+    if y.dtype != a.dtype:
+        raise ValueError("y must have the adapters' type")
+    x8 = x if isinstance(x, Q8Matrix) else None
+    if which.shape != y.shape[:-1] or (x8 is None and x.shape[:-1] != which.shape):
+        raise ValueError("which must have y's and x's shape without their last dimension")
+    _recording("adapted", y, a, b, *(() if x8 is not None else (x,)))
+    flat = y.new_empty(0) if x8 is not None else _rows(x.reshape(which.numel(), x.shape[-1]))
+    out = _Adapted.apply(_rows(y.reshape(which.numel(), y.shape[-1])), flat, a.contiguous(), b.contiguous(), ops, x8,
+                         which.reshape(-1).contiguous(), scale)
+    return out.view(y.shape)

@@ -91,6 +91,24 @@ class Grad(C.Structure):
                 ("dtype", C.c_int)]
 
 
+_ADAPTED = [("d_x", C.c_void_p), ("ld_x", C.c_uint64), ("d_q_scale", C.c_void_p), ("m", C.c_uint64),
+            ("n", C.c_uint64), ("k", C.c_uint64), ("rank", C.c_uint64), ("adapters", C.c_uint64),
+            ("d_a", C.c_void_p), ("d_b", C.c_void_p), ("d_which", C.c_void_p), ("d_scale", C.c_void_p)]
+
+
+class AdaptersArgs(C.Structure):
+    _fields_ = _ADAPTED + [("d_y", C.c_void_p), ("ld_y", C.c_uint64), ("d_out", C.c_void_p),
+                           ("ld_out", C.c_uint64), ("d_down", C.c_void_p), ("d_work", C.c_void_p),
+                           ("work_bytes", C.c_uint64), ("dtype", C.c_int), ("y_dtype", C.c_int)]
+
+
+class AdaptersGradArgs(C.Structure):
+    _fields_ = _ADAPTED + [("d_g", C.c_void_p), ("ld_g", C.c_uint64), ("d_down", C.c_void_p),
+                           ("d_dx", C.c_void_p), ("ld_dx", C.c_uint64), ("d_da", C.c_void_p),
+                           ("d_db", C.c_void_p), ("d_work", C.c_void_p), ("work_bytes", C.c_uint64),
+                           ("dtype", C.c_int)]
+
+
 _fold_fields = operator.attrgetter("tensor", "gamma", "beta", "mean", "var", "bias", "out_offset")
 _fold_row = struct.Struct("=IiiiiiQ").pack      # a FoldDesc
 
@@ -160,6 +178,10 @@ EXPORTS = {
     "shifter_grad_norm": [C.c_void_p, C.POINTER(Grad), C.c_uint64, C.c_void_p, C.c_void_p, C.c_uint64],
     "shifter_clip_grad_norm": [C.c_void_p, C.POINTER(Grad), C.c_uint64, C.c_float, C.c_void_p, C.c_void_p,
                                C.c_uint64],
+    "shifter_adapters_layout": [C.c_uint64] * 5 + [C.POINTER(C.c_uint64)],
+    "shifter_adapters": [C.c_void_p, C.POINTER(AdaptersArgs)],
+    "shifter_adapters_grad_layout": [C.c_uint64] * 5 + [C.c_int, C.POINTER(C.c_uint64)],
+    "shifter_adapters_grad": [C.c_void_p, C.POINTER(AdaptersGradArgs)],
     "shifter_apply_mask": [C.c_void_p] * 8,
     "shifter_dead_channel_scan": [C.c_void_p] * 5,
     "shifter_propagate_groups": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint32,
@@ -568,6 +590,34 @@ def shifter_clip_grad_norm(ctx: Context, grads: Sequence[Grad], max_norm: float,
     arr = (Grad * max(len(grads), 1))(*grads)
     _check(load_library().shifter_clip_grad_norm(ctx.handle, arr, len(grads), max_norm, _ptr(d_norm),
                                                  _ptr(d_work), work_bytes), ctx.handle)
+
+
+SHIFTER_ADAPTERS_MAX_RANK = 128
+
+
+def shifter_adapters_layout(m: int, n: int, k: int, rank: int, adapters: int) -> int:
+    """Bytes of workspace that shifter_adapters takes for these sizes."""
+    out = C.c_uint64()
+    _check(load_library().shifter_adapters_layout(m, n, k, rank, adapters, C.byref(out)))
+    return int(out.value)
+
+
+def shifter_adapters(ctx: Context, **fields) -> None:
+    """fields: those of AdaptersArgs; what is left out is 0 or NULL."""
+    _check(load_library().shifter_adapters(ctx.handle, C.byref(_filled(AdaptersArgs, fields))), ctx.handle)
+
+
+def shifter_adapters_grad_layout(m: int, n: int, k: int, rank: int, adapters: int, dtype: int) -> int:
+    """Bytes of workspace that shifter_adapters_grad takes for these sizes."""
+    out = C.c_uint64()
+    _check(load_library().shifter_adapters_grad_layout(m, n, k, rank, adapters, dtype, C.byref(out)))
+    return int(out.value)
+
+
+def shifter_adapters_grad(ctx: Context, **fields) -> None:
+    """fields: those of AdaptersGradArgs; what is left out is 0 or NULL."""
+    _check(load_library().shifter_adapters_grad(ctx.handle, C.byref(_filled(AdaptersGradArgs, fields))),
+           ctx.handle)
 
 
 def shifter_portfolio_begin(ctx: Context, model: Model, d_w, d_vecs, n_prune: Sequence[int],
