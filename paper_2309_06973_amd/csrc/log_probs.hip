@@ -16,6 +16,7 @@
 // Memory bounds long rows; see the figures at the kernels.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "dev_common.h"
 #include "learn.h"
@@ -65,17 +66,17 @@ struct Best {
     uint32_t at = 0xffffffffu;         // first of the eight columns that hold it
 };
 
-// n logits, in pieces of 8 whose first columns are c0, c0 + step, ...
-template <uint32_t N, bool H, bool TOP>
-__device__ __forceinline__ void take(const float (&f)[N], uint32_t c0, uint32_t step, float c, Sums& a, Best& best) {
+// U pieces of 8 logits whose first columns are c0, c0 + step, ..., of a row that ends at `end`.
+template <uint32_t U, bool H, bool TOP>
+__device__ __forceinline__ void take(const float (&f)[8 * U], uint32_t c0, uint32_t step, uint32_t end, float c, Sums& a, Best& best) {
     float most = a.m;
 #pragma unroll
-    for (uint32_t p = 0; p < N / 8; ++p) {
-        float top = fmaxf(fmaxf(fmaxf(f[8 * p], f[8 * p + 1]), fmaxf(f[8 * p + 2], f[8 * p + 3])),
-                          fmaxf(fmaxf(f[8 * p + 4], f[8 * p + 5]), fmaxf(f[8 * p + 6], f[8 * p + 7])));
+    for (uint32_t p = 0; p < U; ++p) {
+        const float top = fmaxf(fmaxf(fmaxf(f[8 * p], f[8 * p + 1]), fmaxf(f[8 * p + 2], f[8 * p + 3])),
+                                fmaxf(fmaxf(f[8 * p + 4], f[8 * p + 5]), fmaxf(f[8 * p + 6], f[8 * p + 7])));
         most = fmaxf(most, top);
         if constexpr (TOP) {
-            if (top > best.x || best.at == 0xffffffffu) {
+            if ((top > best.x || best.at == 0xffffffffu) && c0 + p * step < end) {
                 best.x = fmaxf(top, -INFINITY);
                 best.at = c0 + p * step;
             }
@@ -86,44 +87,39 @@ __device__ __forceinline__ void take(const float (&f)[N], uint32_t c0, uint32_t 
     a.s *= g;
     a.m = most;
 #pragma unroll
-    for (uint32_t i = 0; i < N; ++i) {
+    for (uint32_t i = 0; i < 8 * U; ++i) {
         const float t = (f[i] - most) * c, e = exp2_of(t);
         a.s += e;
         if constexpr (H) a.u = fmaf(e, fmaxf(t, FAR), a.u);
     }
 }
 
-// The columns [c0, end) of a row by TPR threads, U pieces of 8 columns of each under way.
+// The columns [c0, end) of a row by TPR threads, U pieces of 8 columns of each under way, the last of which stay in `e`.  Pieces behind
+// the end and the one that holds it are fetched from inside the row, so that no load stands in a branch.
 template <typename T, uint32_t TPR, uint32_t U, bool H, bool TOP>
-__device__ __forceinline__ void scan(const T* row, uint32_t c0, uint32_t end, uint32_t t, float c, Sums& a, Best& best) {
+__device__ __forceinline__ void scan(const T* row, uint32_t c0, uint32_t end, uint32_t t, float c, Sums& a, Best& best,
+                                     Eight<T> (&e)[U]) {
     constexpr uint32_t STEP = 8 * TPR;
-    uint32_t at = c0;
-    for (; at + U * STEP <= end; at += U * STEP) {
-        Eight<T> e[U];
+    auto batch = [&](uint32_t at, auto last) {
         float f[8 * U];
 #pragma unroll
-        for (uint32_t p = 0; p < U; ++p) e[p].load(row + at + p * STEP + 8 * t);
+        for (uint32_t p = 0; p < U; ++p) {
+            if constexpr (last.value) fetch8(row, at + p * STEP, end, e[p]);
+            else e[p].load(row + at + p * STEP);
+        }
 #pragma unroll
         for (uint32_t p = 0; p < U; ++p) {
             float g[8];
+            if constexpr (last.value) place8(at + p * STEP, end, e[p]);
             e[p].floats(g);
 #pragma unroll
-            for (uint32_t i = 0; i < 8; ++i) f[8 * p + i] = g[i];
+            for (uint32_t i = 0; i < 8; ++i) f[8 * p + i] = !last.value || at + p * STEP + i < end ? g[i] : -INFINITY;
         }
-        take<8 * U, H, TOP>(f, at + 8 * t, STEP, c, a, best);
-    }
-    for (at += 8 * t; at < end; at += STEP) {
-        float f[8];
-        if (at + 8 <= end) {
-            Eight<T> e;
-            e.load(row + at);
-            e.floats(f);
-        } else {
-#pragma unroll
-            for (uint32_t i = 0; i < 8; ++i) f[i] = at + i < end ? (float)row[at + i] : -INFINITY;
-        }
-        take<8, H, TOP>(f, at, STEP, c, a, best);
-    }
+        take<U, H, TOP>(f, at, STEP, last.value ? end : 0xffffffffu, c, a, best);
+    };
+    uint32_t at = c0;
+    for (; at + U * STEP <= end; at += U * STEP) batch(at + 8 * t, std::false_type{});
+    if (at < end) batch(at + 8 * t, std::true_type{});
 }
 
 // The TPR threads of a row together.
@@ -143,21 +139,41 @@ struct RowShared {
     static constexpr uint32_t WAVES = TPR > 64 ? TPR / 64 : 1, CAP = !TOP ? 1 : TPR == 16 ? 128 : TPR == 64 ? 512 : 1024;
     Sums sums[WAVES];
     uint64_t group[WAVES][TOP && TPR > 64 ? 64 : 1];
-    uint64_t place[CAP];
+    uint64_t place[CAP + 8];
     uint64_t bound;
-    uint32_t count, last;
+    uint32_t count, winners, last;
+    uint16_t winner[TOP && TPR > 64 ? TPR : 1];
 };
+
+// The lane's value that DPP pattern CTRL pairs it with: neighbours by 1 and 2, mirrors of 8 and 16.
+template <int CTRL>
+__device__ __forceinline__ float beside(float v) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+template <int CTRL, bool H>
+__device__ __forceinline__ void join_beside(Sums& a, float c) {
+    a = join<H>(a, Sums{beside<CTRL>(a.m), beside<CTRL>(a.s), H ? beside<CTRL>(a.u) : 0.0f}, c);
+}
+// The sums of a wavefront's lanes, or of 16 of them, in all of these.
+template <uint32_t LANES, bool H>
+__device__ __forceinline__ Sums sum_lanes(Sums a, float c) {
+    join_beside<0xB1, H>(a, c);
+    join_beside<0x4E, H>(a, c);
+    join_beside<0x141, H>(a, c);
+    join_beside<0x140, H>(a, c);
+    if constexpr (LANES == 64) {
+        auto of = [&](int lane) {
+            auto one = [&](float v) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); };
+            return Sums{one(a.m), one(a.s), H ? one(a.u) : 0.0f};
+        };
+        a = join<H>(join<H>(of(0), of(16), c), join<H>(of(32), of(48), c), c);
+    }
+    return a;
+}
 
 template <uint32_t TPR, bool H, bool TOP>
 __device__ __forceinline__ Sums sum_up(Sums a, uint32_t t, float c, RowShared<TPR, TOP>& sh) {
-#pragma unroll
-    for (uint32_t d = 1; d < (TPR < 64 ? TPR : 64); d <<= 1) {
-        Sums b;
-        b.m = __shfl_xor(a.m, d, 64);
-        b.s = __shfl_xor(a.s, d, 64);
-        if constexpr (H) b.u = __shfl_xor(a.u, d, 64);
-        a = join<H>(a, b, c);
-    }
+    a = sum_lanes<(TPR < 64 ? TPR : 64), H>(a, c);
     if constexpr (TPR > 64) {
         if ((t & 63u) == 0) sh.sums[t / 64] = a;
         meet<TPR>();
@@ -168,31 +184,60 @@ __device__ __forceinline__ Sums sum_up(Sums a, uint32_t t, float c, RowShared<TP
     return a;
 }
 
-// The k-th largest of the numbers that the `lanes` lanes of a group of a wavefront hold, or a lower one that no further lane
-// reaches; 0 where fewer than k hold one.  Zero is none.
+// The k-th largest of the numbers that the lanes of a wavefront (of a group of 16 of them) hold, or a lower one that no further
+// lane reaches; 0 where fewer than k hold one.  Zero is none.  Bit by bit, the upper word first: mostly that is enough.
 template <uint32_t LANES>
 __device__ __forceinline__ uint64_t kth_of(uint64_t v, uint32_t k) {
-    const uint32_t lane = threadIdx.x & 63u;
-    const uint64_t mine = LANES == 64 ? ~0ull : ((1ull << (LANES & 63u)) - 1ull) << (lane / LANES * LANES);
-    uint64_t bound = 0;
-    bool done = false;
-    if constexpr (LANES == 64) done = (uint32_t)__popcll(__ballot(v != 0)) < k;
-    else done = (uint32_t)__popcll(__ballot(v != 0) & mine) < k;
-    for (uint64_t bit = 1ull << 63; bit; bit >>= 1) {
-        const uint32_t n = (uint32_t)__popcll(__ballot(v >= (bound | bit)) & mine);
-        if (!done && n >= k) bound |= bit;
-        if (!done && n == k) done = true;
-        if (__ballot(!done) == 0) break;
+    const uint32_t high = (uint32_t)(v >> 32), low = (uint32_t)v;
+    uint32_t top = 0, rest = 0;
+    if constexpr (LANES == 64) {
+        if ((uint32_t)__popcll(__ballot(v != 0)) < k) return 0;
+        for (uint32_t bit = 1u << 31; bit; bit >>= 1) {
+            const uint32_t n = (uint32_t)__popcll(__ballot(high >= (top | bit)));
+            if (n >= k) top |= bit;
+            if (n == k) return (uint64_t)top << 32;
+        }
+        const uint64_t over = __ballot(high > top);
+        for (uint32_t bit = 1u << 31; bit; bit >>= 1) {
+            const uint32_t n = (uint32_t)__popcll(over | __ballot(high == top && low >= (rest | bit)));
+            if (n >= k) rest |= bit;
+            if (n == k) break;
+        }
+    } else {                            // a bound for each group, until all have theirs
+        const uint64_t mine = ((1ull << LANES) - 1ull) << ((threadIdx.x & 63u) / LANES * LANES);
+        bool done = (uint32_t)__popcll(__ballot(v != 0) & mine) < k;
+        for (uint32_t bit = 1u << 31; bit && __ballot(!done); bit >>= 1) {
+            const uint32_t n = (uint32_t)__popcll(__ballot(high >= (top | bit)) & mine);
+            if (!done && n >= k) top |= bit;
+            done = done || n == k;
+        }
+        if (__ballot(!done)) {
+            const uint64_t over = __ballot(high > top) & mine;
+            for (uint32_t bit = 1u << 31; bit && __ballot(!done); bit >>= 1) {
+                const uint32_t n = (uint32_t)__popcll(over | (__ballot(high == top && low >= (rest | bit)) & mine));
+                if (!done && n >= k) rest |= bit;
+                done = done || n == k;
+            }
+        }
     }
-    return bound;
+    return (uint64_t)top << 32 | rest;
 }
 
-// Puts the places that `v` holds and that reach the bound on the list, as far as there is room.
+// Puts a place that reaches the bound on the list, if there is room.  Zero is none.
 template <uint32_t TPR, bool TOP>
 __device__ __forceinline__ void list(RowShared<TPR, TOP>& sh, uint64_t v, uint64_t bound) {
     if (v < bound || v == 0) return;
     const uint32_t n = atomicAdd(&sh.count, 1u);
     if (n < RowShared<TPR, TOP>::CAP) sh.place[n] = v;
+}
+// The same for the eight columns from `at` on of a row that ends at `end`.
+template <typename T, uint32_t TPR, bool TOP>
+__device__ __forceinline__ void list8(RowShared<TPR, TOP>& sh, const Eight<T>& e, uint32_t at, uint32_t end, uint64_t bound) {
+    float f[8];
+    e.floats(f);
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i)
+        if (at + i < end) list(sh, place_of(order_of(f[i]), at + i), bound);
 }
 
 // The k largest of the places that find(bound) lists, place(rank, v) for each.  Where more than the list holds reach the
@@ -210,7 +255,13 @@ __device__ __forceinline__ void rank(RowShared<TPR, TOP>& sh, uint32_t t, uint32
         for (uint32_t i = t; i < held; i += TPR) {
             const uint64_t v = sh.place[i];
             uint32_t above = 0;
-            for (uint32_t j = 0; j < held; ++j) above += sh.place[j] > v;
+            for (uint32_t j = 0; j < held; j += 8) {
+                uint64_t w[8];
+#pragma unroll
+                for (uint32_t e = 0; e < 8; ++e) w[e] = sh.place[j + e];
+#pragma unroll
+                for (uint32_t e = 0; e < 8; ++e) above += (uint32_t)(j + e < held) & (uint32_t)(w[e] > v);
+            }
             if (n <= CAP) {
                 if (above < k) put(above, v);
             } else if (above == k - 1) {
@@ -234,7 +285,7 @@ struct RowEnd {
 
 template <typename T, uint32_t TPR, bool H, bool TOP>
 __global__ __launch_bounds__(TPR < BLOCK ? BLOCK : TPR) void log_probs_kernel(LogProbsArgs g, LogProbsPlan plan) {
-    constexpr uint32_t AT_ONCE = TPR < BLOCK ? BLOCK / TPR : 1u, U = TPR >= 256 ? (sizeof(T) == 2 ? 4 : 2) : 1;
+    constexpr uint32_t AT_ONCE = TPR < BLOCK ? BLOCK / TPR : 1u, U = TPR > 64 ? (sizeof(T) == 2 ? 4 : 2) : 2;
     __shared__ RowShared<TPR, TOP> shared[AT_ONCE];
     const uint32_t t = threadIdx.x % TPR;
     RowShared<TPR, TOP>& sh = shared[threadIdx.x / TPR];
@@ -244,42 +295,40 @@ __global__ __launch_bounds__(TPR < BLOCK ? BLOCK : TPR) void log_probs_kernel(Lo
         const uint64_t r = plan.parts == 1 ? i : i / plan.parts;
         const uint32_t part = (uint32_t)(i - r * plan.parts), c0 = part * plan.part_cols, end = min(c0 + plan.part_cols, g.cols);
         const T* row = static_cast<const T*>(g.x) + r * g.ld_x;
-        // the target's logit is on its way while the row is read
         int64_t target = -1;
-        float x_t = 0.0f;
-        if (g.target && t == 0) {
-            target = g.target[r];
-            if (target >= 0 && target < (int64_t)g.cols) x_t = (float)row[target];
-        }
+        if (g.target && t == 0) target = g.target[r];
         Sums a{LEAST, 0.0f, 0.0f};
         Best best;
-        scan<T, TPR, U, H, TOP>(row, c0, end, t, c, a, best);
+        Eight<T> e[U];
+        scan<T, TPR, U, H, TOP>(row, c0, end, t, c, a, best, e);
+        // the target's logit is on its way while the sums are joined
+        float x_t = 0.0f;
+        if (target >= 0 && target < (int64_t)g.cols) x_t = (float)row[target];
         a = sum_up<TPR, H, TOP>(a, t, c, sh);
 
         uint64_t bound = 0;
         // the part's own alternatives: as many as are asked for, or all that it has
         const uint32_t k = TOP ? min(g.top, end - c0) : 0u;
         auto find = [&](uint64_t least) {
-            if constexpr (TPR < 64) {
-                for (uint32_t at = c0 + 8 * t; at < end; at += 8 * TPR)
-                    for (uint32_t e = at; e < min(at + 8u, end); ++e) list(sh, place_of(order_of((float)row[e]), e), least);
-            } else {
-                const uint32_t pieces = (end - c0 + 8 * TPR - 1) / (8 * TPR), lane = t & 63u;
-                uint64_t seen = __ballot(best.at != 0xffffffffu && place_of(order_of(best.x), best.at) >= least);
-                for (; seen; seen &= seen - 1) {
-                    const uint32_t whose = (t & ~63u) + (uint32_t)__ffsll((unsigned long long)seen) - 1u;
-                    for (uint32_t p = lane; p < pieces; p += 64) {
-                        const uint32_t at = c0 + 8 * (p * TPR + whose);
-                        if (at + 8 <= end) {
-                            Eight<T> e;
-                            float f[8];
-                            e.load(row + at);
-                            e.floats(f);
+            static_assert(TPR > 64 || U * 8 * TPR == 16 * TPR, "as many columns as the plan gives so many threads");
+            const bool wins = best.at != 0xffffffffu && place_of(order_of(best.x), best.at) >= least;
+            if constexpr (TPR <= 64) {             // a thread still holds all that it has seen
+                if (!wins) return;
 #pragma unroll
-                            for (uint32_t j = 0; j < 8; ++j) list(sh, place_of(order_of(f[j]), at + j), least);
-                        } else {
-                            for (uint32_t j = at; j < end; ++j) list(sh, place_of(order_of((float)row[j]), j), least);
-                        }
+                for (uint32_t p = 0; p < U; ++p) list8(sh, e[p], c0 + 8 * (p * TPR + t), end, least);
+            } else {                    // all pieces of the threads that do, by all threads
+                if (t == 0) sh.winners = 0;
+                meet<TPR>();
+                if (wins) sh.winner[atomicAdd(&sh.winners, 1u)] = (uint16_t)t;
+                meet<TPR>();
+                const uint32_t pieces = (end - c0 + 8 * TPR - 1) / (8 * TPR), todo = pieces * sh.winners;
+                for (uint32_t i = t; i < todo; i += TPR) {
+                    const uint32_t w = i / pieces, at = c0 + 8 * ((i - w * pieces) * TPR + sh.winner[w]);
+                    if (at < end) {
+                        Eight<T> x;
+                        fetch8(row, at, end, x);
+                        place8(at, end, x);
+                        list8(sh, x, at, end, least);
                     }
                 }
             }
@@ -304,8 +353,7 @@ __global__ __launch_bounds__(TPR < BLOCK ? BLOCK : TPR) void log_probs_kernel(Lo
             }
         }
 
-        auto finish = [&](const Sums& s) {
-            const RowEnd e(s, g.scale);
+        auto finish = [&](const Sums& s, const RowEnd& e) {
             if (t == 0) {
                 g.norm[2 * r] = s.m;
                 g.norm[2 * r + 1] = (float)e.log_s;
@@ -314,14 +362,15 @@ __global__ __launch_bounds__(TPR < BLOCK ? BLOCK : TPR) void log_probs_kernel(Lo
                 if (H) g.entropy[r] = (float)(e.log_s - LN2 * (double)s.u / (double)s.s);
             }
         };
-        auto put = [&](const Sums& s, uint32_t n, uint64_t v) {
+        auto put = [&](const Sums& s, const RowEnd& e, uint32_t n, uint64_t v) {
             const float x = logit_of((uint32_t)(v >> 32));
-            g.top_logp[r * g.top + n] = RowEnd(s, g.scale).of(x, s.m, g.scale);
+            g.top_logp[r * g.top + n] = e.of(x, s.m, g.scale);
             g.index[r * g.top + n] = (int64_t)(uint32_t)~(uint32_t)v;
         };
         if (plan.parts == 1) {
-            finish(a);
-            if constexpr (TOP) rank(sh, t, k, bound, find, [&](uint32_t n, uint64_t v) { put(a, n, v); });
+            const RowEnd e(a, g.scale);
+            finish(a, e);
+            if constexpr (TOP) rank(sh, t, k, bound, find, [&](uint32_t n, uint64_t v) { put(a, e, n, v); });
             else meet<TPR>();
             continue;
         }
@@ -351,24 +400,21 @@ __global__ __launch_bounds__(TPR < BLOCK ? BLOCK : TPR) void log_probs_kernel(Lo
                     b.m = __uint_as_float((uint32_t)ms);
                     b.s = __uint_as_float((uint32_t)(ms >> 32));
                     b.u = __uint_as_float((uint32_t)found(left + (uint64_t)lane * entry + 1));
-                    if (TOP) first = found(left + (uint64_t)lane * entry + 2);
                 }
-#pragma unroll
-                for (uint32_t d = 1; d < 64; d <<= 1) {
-                    Sums o;
-                    o.m = __shfl_xor(b.m, d, 64);
-                    o.s = __shfl_xor(b.s, d, 64);
-                    if constexpr (H) o.u = __shfl_xor(b.u, d, 64);
-                    b = join<H>(b, o, c);
+                if constexpr (TOP) {                   // the best of each part, 33 or more, or all
+                    const uint32_t each = min(g.top, 64u / plan.parts);
+                    if (lane < plan.parts * each) first = found(left + (uint64_t)(lane / each) * entry + 2 + lane % each);
                 }
-                finish(b);
+                b = sum_lanes<64, H>(b, c);
+                const RowEnd e(b, g.scale);
+                finish(b, e);
                 if constexpr (TOP) {
                     bound = kth_of<64>(first, g.top);
                     auto lists = [&](uint64_t least) {
                         for (uint32_t n = t; n < plan.parts * g.top; n += TPR)
                             list(sh, found(left + (uint64_t)(n / g.top) * entry + 2 + n % g.top), least);
                     };
-                    rank(sh, t, g.top, bound, lists, [&](uint32_t n, uint64_t v) { put(b, n, v); });
+                    rank(sh, t, g.top, bound, lists, [&](uint32_t n, uint64_t v) { put(b, e, n, v); });
                 }
             }
             meet<TPR>();
@@ -412,8 +458,9 @@ __global__ __launch_bounds__(BLOCK) void log_probs_grad_kernel(LogProbsGradArgs 
     const uint32_t t = threadIdx.x % TPR;
     const uint64_t all = (uint64_t)g.rows * parts;
     for (uint64_t i = (uint64_t)blockIdx.x * AT_ONCE + threadIdx.x / TPR; i < all; i += (uint64_t)gridDim.x * AT_ONCE) {
-        const uint64_t r = parts == 1 ? i : i / parts;
-        const uint32_t c0 = (uint32_t)(i - r * parts) * part_cols, end = min(c0 + part_cols, g.cols);
+        // from the last row to the first: the last ones are in the last-level cache still, where the sums have just been made
+        const uint64_t nth = parts == 1 ? i : i / parts, r = g.rows - 1u - nth;
+        const uint32_t c0 = (uint32_t)(i - nth * parts) * part_cols, end = min(c0 + part_cols, g.cols);
         const T* row = static_cast<const T*>(g.x) + r * g.ld_x;
         T* out = static_cast<T*>(g.dx) + r * g.ld_dx;
         const int64_t target = g.target ? g.target[r] : -1;

@@ -2,12 +2,15 @@
 // and the tests share it.
 #pragma once
 
+#include <algorithm>
+
 #include "q8_plan.h"
 
 namespace shifter {
 
 constexpr uint32_t LOGP_MAX_TOP = 32;              // alternatives of a row
 constexpr uint32_t LOGP_MAX_PARTS = 64;            // parts of a row: a wavefront joins them
+constexpr uint64_t LOGP_PART = 8192;               // columns of a part: 256 threads, four pieces of eight
 constexpr uint64_t LOGP_SHARED_ROWS = 512;         // only fewer rows than these are shared by blocks
 // The front of a workspace of a call whose blocks join their sums: counters, zero before a call and after it.
 constexpr uint64_t LEARN_TICKETS = 4 * LOGP_SHARED_ROWS;
@@ -22,8 +25,11 @@ struct LogProbsPlan {
 
 inline uint64_t logp_entry(uint32_t top) { return 16u + 8u * (uint64_t)top; }      // what a part leaves: its sums, its alternatives
 
-// Rows up to 256 columns have 16 threads each, up to 1024 a wavefront, longer ones a block; and where there are too few
-// rows to fill the chip, several blocks.
+// Rows up to 256 columns have 16 threads each, up to 1024 a wavefront, longer ones 256 threads; and where there are too few
+// rows to fill the chip, several such blocks, each of which fetches its 8192 columns at once.  us of bf16 with 20 alternatives, by blocks a
+// row: 1 x 50001 1: 13.9, 6 (two fetches each): 14.8, 8: 13.4, 24: 14.9; 1 x 131072 1: 23.0, 8: 14.5, 16: 14.4, 32: 15.4;
+// 128 x 131072 1: 29.3, 4: 21.6, 8: 21.7; 300 x 131072 1: 38.0, 2: 33.9, 4: 35.3; 8 x 10000 1: 11.3, 2: 14.4.  512 threads a block are
+// faster where one block has a long row (300 x 131072 32.4), and slower elsewhere (128 x 131072 23.0, 1000 x 2000 25.4 for 14.2).
 inline LogProbsPlan log_probs_plan(uint64_t rows, uint64_t cols, uint32_t top) {
     LogProbsPlan p{};
     p.parts = 1;
@@ -31,10 +37,9 @@ inline LogProbsPlan log_probs_plan(uint64_t rows, uint64_t cols, uint32_t top) {
     if (cols <= 256 && top <= 8) p.threads = 16;
     else if (cols <= 1024) p.threads = 64;
     else p.threads = 256;
-    if (cols > 8192 && rows < LOGP_SHARED_ROWS) {
+    if (cols > 2 * LOGP_PART && rows < LOGP_SHARED_ROWS) {
         uint64_t parts = (LOGP_SHARED_ROWS + rows - 1u) / (rows ? rows : 1u);
-        if (parts > cols / 4096u) parts = cols / 4096u;
-        if (parts > LOGP_MAX_PARTS) parts = LOGP_MAX_PARTS;
+        parts = std::min<uint64_t>({parts, (cols + LOGP_PART - 1u) / LOGP_PART, LOGP_MAX_PARTS});
         const uint64_t each = ((cols + parts - 1u) / parts + 7u) & ~7ull;
         p.part_cols = (uint32_t)each;
         p.parts = (uint32_t)((cols + each - 1u) / each);
