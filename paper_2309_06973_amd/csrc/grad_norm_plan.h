@@ -11,8 +11,10 @@
 namespace shifter {
 
 // A launch takes its tensors as arguments (4 KB of them), 24 bytes each: nothing is copied to the device and a recorded
-// call keeps them.  Elements go to blocks in chunks, none of which has two tensors' elements.
-constexpr uint32_t GRAD_CHUNK = 8192;              // elements
+// call keeps them.  Elements are counted in chunks, none of which has two tensors' elements; each block takes a run of
+// chunks, as many as any other block or one less.
+constexpr uint32_t GRAD_CHUNK = 2048;              // elements: eight for each thread of a block
+constexpr uint32_t GRAD_SMALL = 4096;              // eights of elements, of all tensors, that one block holds
 constexpr uint32_t GRAD_LIST = 164;                // tensors of a launch
 constexpr uint32_t GRAD_BLOCKS = 2048;             // of a launch at most; each leaves one sum
 constexpr uint64_t GRAD_HEAD = 256;                // bytes between the counters and the sums: the norm in 64 bits
@@ -29,8 +31,8 @@ static_assert(GRAD_CHUNK <= 8192 && sizeof(GradList) <= 4000, "13 bits; 4 KB of 
 inline uint64_t grad_launches(uint64_t count) { return count == 0 ? 1 : (count + GRAD_LIST - 1) / GRAD_LIST; }
 inline uint64_t grad_norm_bytes(uint64_t count) { return LEARN_TICKETS + GRAD_HEAD + 8ull * GRAD_BLOCKS * grad_launches(count); }
 
-// The tensors [from, from + GRAD_LIST) of a list without empty ones.
-inline void grad_list(const std::vector<shifter_grad>& all, uint64_t from, GradList* l) {
+// The tensors [from, from + GRAD_LIST) of a list without empty ones, in chunks of so many elements.
+inline void grad_list(const std::vector<shifter_grad>& all, uint64_t from, uint32_t chunk, GradList* l) {
     l->n = (uint32_t)std::min<uint64_t>(GRAD_LIST, all.size() - from);
     l->chunks = 0;
     for (uint32_t i = 0; i < l->n; ++i) {
@@ -41,9 +43,16 @@ inline void grad_list(const std::vector<shifter_grad>& all, uint64_t from, GradL
             l->high[j][i] = (uint16_t)(at[j] >> 32);
         }
         l->first[i] = l->chunks;
-        l->last[i] = (uint16_t)((g.n - 1) % GRAD_CHUNK | (uint32_t)g.dtype << 13);
-        l->chunks += (uint32_t)((g.n + GRAD_CHUNK - 1) / GRAD_CHUNK);
+        l->last[i] = (uint16_t)((g.n - 1) % chunk | (uint32_t)g.dtype << 13);
+        l->chunks += (uint32_t)((g.n + chunk - 1) / chunk);
     }
+}
+
+// Whether one block does it all, the elements in its registers.
+inline bool grad_small(const std::vector<shifter_grad>& all) {
+    uint64_t eights = 0;
+    for (const shifter_grad& g : all) eights += g.n > 8ull * GRAD_SMALL ? GRAD_SMALL + 1u : (g.n + 7u) / 8u;
+    return all.size() <= GRAD_LIST && eights <= GRAD_SMALL;
 }
 
 // What is wrong with a list, or nullptr.
@@ -61,7 +70,7 @@ inline const char* grad_bad(const shifter_grad* h, uint64_t count, bool write) {
         if (g.n >> 40) return "2^40 elements or more";
         chunks += (g.n + GRAD_CHUNK - 1) / GRAD_CHUNK;
     }
-    return chunks >> 31 ? "2^44 elements or more" : nullptr;
+    return chunks >> 31 ? "2^42 elements or more" : nullptr;
 }
 
 // Whether a tensor that is written lies over another one, or over its own elements in another place.

@@ -487,7 +487,7 @@ __global__ __launch_bounds__(BLOCK) void log_probs_grad_kernel(LogProbsGradArgs 
             for (uint32_t j = 0; j < 8; ++j) f[j] = value(f[j], at + j);
             Eight<T> o;
             o.from(f);
-            o.store(out + at);
+            o.store_through(out + at);       // past the caches, which hold what is read next (8192 x 32768 with its sums 273 -> 258 us)
         };
         if (none) {
             const float zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};

@@ -26,6 +26,12 @@ struct Eight {
 #pragma unroll
         for (uint32_t x = 0; x < WORDS / 4u; ++x) q[x] = vec{w[4u * x], w[4u * x + 1u], w[4u * x + 2u], w[4u * x + 3u]};
     }
+    __device__ __forceinline__ void store_through(T* p) const {          // not kept in the caches
+        typedef uint32_t vec __attribute__((ext_vector_type(4), aligned(2)));
+        vec* q = reinterpret_cast<vec*>(p);
+#pragma unroll
+        for (uint32_t x = 0; x < WORDS / 4u; ++x) __builtin_nontemporal_store(vec{w[4u * x], w[4u * x + 1u], w[4u * x + 2u], w[4u * x + 3u]}, q + x);
+    }
     // the elements from the n-th on, zeros behind them: n < 8
     __device__ __forceinline__ void drop(uint32_t n) {
         const uint32_t bits = n * 8u * sizeof(T), words = bits / 32u, rest = bits % 32u;
