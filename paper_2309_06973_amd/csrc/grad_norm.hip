@@ -131,7 +131,7 @@ __device__ __forceinline__ void squares(const GradRun& r, double (&sum)[4]) {
             sum[i % 4] = fma(x, x, sum[i % 4]);
         }
     };
-    if (r.mask) each8<T, true, 2>(r, add);
+    if (r.mask) each8<T, true, 4>(r, add);
     else each8<T, false, 4>(r, add);
 }
 

@@ -16,7 +16,7 @@ namespace shifter {
 constexpr uint32_t GRAD_CHUNK = 2048;              // elements: eight for each thread of a block
 constexpr uint32_t GRAD_SMALL = 4096;              // eights of elements, of all tensors, that one block holds
 constexpr uint32_t GRAD_LIST = 164;                // tensors of a launch
-constexpr uint32_t GRAD_BLOCKS = 2048;             // of a launch at most; each leaves one sum
+constexpr uint32_t GRAD_BLOCKS = 512;              // of a launch at most; each leaves one sum
 constexpr uint64_t GRAD_HEAD = 256;                // bytes between the counters and the sums: the norm in 64 bits
 
 struct GradList {
