@@ -98,15 +98,26 @@ __device__ __forceinline__ void codes_as(uint4 w, Sixteen<T>& s) {
     }
 }
 
+// The adapter of the block: of few rows, each block takes one of the adapters that a tile's rows have, the job-th of them.  False: there
+// are not so many.
+__device__ __forceinline__ bool adapter_of_job(int id, uint32_t job, int* which) {
+    int waits[1] = {id};
+    for (uint32_t j = 0;; ++j) {
+        if (!next_adapter<1>(waits, which)) return false;
+        if (j == job) return true;
+    }
+}
+
 // s[part][r] = c_i x_r A_i' over the part's columns; 0 for a row without an adapter, NaN for one whose adapter there is not.
 // A block has RT tiles of 16 rows and 16 RF ranks; its wavefronts take steps of 64 columns in turn and join their sums.  Both factors
 // come straight from memory into the operands: a lane's 16 columns of a row lie side by side.
-template <typename T, bool CODES, uint32_t RF, uint32_t RT>
+template <typename T, bool CODES, uint32_t RF, uint32_t RT, bool JOBS>
 __global__ __launch_bounds__(ADAPT_THREADS) void adapters_down_kernel(AdaptersDownArgs g) {
+    static_assert(!JOBS || RT == 1, "a tile of a job");
     __shared__ v4f s_sum[ADAPT_WAVES][RF * RT][64];
     const uint32_t lane = threadIdx.x & 63u, wave = uniform_u32(threadIdx.x >> 6), col = 16u * (lane / 16u), r16 = lane & 15u;
     const uint64_t m0 = (uint64_t)blockIdx.x * 16u * RT;
-    const uint32_t part = blockIdx.y, rank0 = blockIdx.z * 16u * RF;
+    const uint32_t part = blockIdx.y, job = blockIdx.z / g.groups, rank0 = (blockIdx.z - job * g.groups) * 16u * RF;
     const uint32_t steps = (g.k + ADAPT_STEP - 1u) / ADAPT_STEP, whole = g.k / ADAPT_STEP;
     const uint32_t s0 = (uint32_t)((uint64_t)steps * part / g.parts), s1 = (uint32_t)((uint64_t)steps * (part + 1u) / g.parts);
     int id[RT], waits[RT];
@@ -124,8 +135,9 @@ __global__ __launch_bounds__(ADAPT_THREADS) void adapters_down_kernel(AdaptersDo
     for (uint32_t i = 0; i < RT; ++i)
 #pragma unroll
         for (uint32_t f = 0; f < RF; ++f) sum[i][f] = v4f{0, 0, 0, 0};
-    int which;
-    while (next_adapter<RT>(waits, &which)) {
+    int which = NO_ADAPTER;
+    if (JOBS && !adapter_of_job(id[0], job, &which) && job != 0) return;
+    while (JOBS ? which >= 0 : next_adapter<RT>(waits, &which)) {
         const T* a[RF];
 #pragma unroll
         for (uint32_t f = 0; f < RF; ++f)
@@ -199,6 +211,7 @@ __global__ __launch_bounds__(ADAPT_THREADS) void adapters_down_kernel(AdaptersDo
 #pragma unroll
             for (uint32_t f = 0; f < RF; ++f)
                 if (id[i] == which) sum[i][f] = acc[i][f];
+        if (JOBS) break;
     }
 #pragma unroll
     for (uint32_t i = 0; i < RT; ++i)
@@ -212,6 +225,7 @@ __global__ __launch_bounds__(ADAPT_THREADS) void adapters_down_kernel(AdaptersDo
         const uint32_t i = u / RF, f = u % RF, r = rank0 + 16u * f + 4u * (lane / 16u);
         const uint64_t row = m0 + 16u * i + r16;
         if (row >= g.m || rank0 + 16u * f >= pad) continue;
+        if (JOBS && id[i] != which && (id[i] >= 0 || job != 0)) continue;
         v4f v = (s_sum[0][u][lane] + s_sum[1][u][lane]) + (s_sum[2][u][lane] + s_sum[3][u][lane]);
         float by = 1.0f;
         if (id[i] >= 0) {
@@ -226,11 +240,12 @@ __global__ __launch_bounds__(ADAPT_THREADS) void adapters_down_kernel(AdaptersDo
 
 template <typename T, bool CODES, uint32_t RF>
 static void launch_down_as(shifter_ctx* ctx, const AdaptersDownArgs& g) {
-    constexpr uint32_t MORE = RF == 1 ? 4 : 2;
-    const uint32_t tiles = adapt_tiles(g.m, g.rank), groups = (uint32_t)((adapt_pad(g.rank) / 16u + RF - 1u) / RF);
-    const dim3 grid((uint32_t)((g.m + 16u * tiles - 1u) / (16u * tiles)), g.parts, groups);
-    if (tiles == 1) adapters_down_kernel<T, CODES, RF, 1><<<grid, ADAPT_THREADS, 0, ctx->stream>>>(g);
-    else adapters_down_kernel<T, CODES, RF, MORE><<<grid, ADAPT_THREADS, 0, ctx->stream>>>(g);
+    constexpr uint32_t MORE = RF == 4 ? 1 : 2;
+    const uint32_t tiles = adapt_tiles(g.m, g.rank), jobs = adapt_jobs(g.m, g.adapters);
+    const dim3 grid((uint32_t)((g.m + 16u * tiles - 1u) / (16u * tiles)), g.parts, g.groups * jobs);
+    if (jobs > 1) adapters_down_kernel<T, CODES, RF, 1, true><<<grid, ADAPT_THREADS, 0, ctx->stream>>>(g);
+    else if (tiles == 1) adapters_down_kernel<T, CODES, RF, 1, false><<<grid, ADAPT_THREADS, 0, ctx->stream>>>(g);
+    else adapters_down_kernel<T, CODES, RF, MORE, false><<<grid, ADAPT_THREADS, 0, ctx->stream>>>(g);
 }
 template <typename T, bool CODES>
 static void launch_down_of(shifter_ctx* ctx, const AdaptersDownArgs& g) {
@@ -239,7 +254,8 @@ static void launch_down_of(shifter_ctx* ctx, const AdaptersDownArgs& g) {
     else if (pad <= 32) launch_down_as<T, CODES, 2>(ctx, g);
     else launch_down_as<T, CODES, 4>(ctx, g);      // 64 ranks a block
 }
-static void launch_down(shifter_ctx* ctx, int dtype, const AdaptersDownArgs& g) {
+static void launch_down(shifter_ctx* ctx, int dtype, AdaptersDownArgs g) {
+    g.groups = (uint32_t)(adapt_pad(g.rank) + 63u) / 64u;
     ProfileScope ps(ctx, K_ADAPTERS_DOWN);
     if (dtype == SHIFTER_F32) g.x_scale ? launch_down_of<float, true>(ctx, g) : launch_down_of<float, false>(ctx, g);
     else if (dtype == SHIFTER_BF16) g.x_scale ? launch_down_of<__bf16, true>(ctx, g) : launch_down_of<__bf16, false>(ctx, g);
@@ -260,124 +276,128 @@ __device__ __forceinline__ v4f four_of(const T* row, uint32_t r, uint32_t rank) 
     return f;
 }
 
-// out_r = y_r + s_r B_i'.  A wavefront has RT tiles of 16 rows and 64 columns; the columns of its four products are interleaved so that a
-// lane ends with 16 neighbouring columns of a row, which it adds to y and writes.  s, the sums of all parts, is in LDS.
-template <typename T, typename Y, uint32_t RT>
+// out_r = y_r + s_r B_i'.  A wavefront has a tile of 16 rows and takes 64 columns at a time; the columns of its four products are
+// interleaved so that a lane ends with 16 neighbouring columns of a row, which it adds to y and writes.  The next columns' y is on
+// its way meanwhile.  s, the sums of all parts, is in LDS.
+template <typename T, typename Y, bool JOBS>
 __global__ __launch_bounds__(ADAPT_THREADS) void adapters_up_kernel(AdaptersUpArgs g) {
-    extern __shared__ __align__(16) float s_rows[];        // [16 RT][pad + 4]
+    extern __shared__ __align__(16) float s_rows[];        // [16][pad + 4]
     const uint32_t lane = threadIdx.x & 63u, wave = uniform_u32(threadIdx.x >> 6), group = lane / 16u, r16 = lane & 15u;
-    const uint64_t m0 = (uint64_t)blockIdx.x * 16u * RT;
-    const uint32_t pad = (g.rank + 15u) & ~15u, pitch = pad + 4u, fours = pad / 4u;
-    const uint32_t rows = (uint32_t)min((uint64_t)(16u * RT), g.m - m0);
-    for (uint32_t u = threadIdx.x; u < 16u * RT * fours; u += ADAPT_THREADS) {
-        const uint32_t row = u / fours, r = u % fours * 4u;
+    const uint64_t m0 = (uint64_t)blockIdx.x * 16u, row = m0 + r16;
+    const uint32_t pad = (g.rank + 15u) & ~15u, pitch = pad + 4u, fours = pad / 4u, job = blockIdx.z;
+    const int id = adapter_of(g.which, row, g.m, g.adapters);
+    int mine = NO_ADAPTER;
+    if (JOBS && !adapter_of_job(id, job, &mine) && job != 0) return;
+    const uint32_t rows = (uint32_t)min((uint64_t)16u, g.m - m0);
+    for (uint32_t u = threadIdx.x; u < 16u * fours; u += ADAPT_THREADS) {
+        const uint32_t at = u / fours, r = u % fours * 4u;
         v4f v{0, 0, 0, 0};
-        if (row < rows) {
-            const float* p = g.s + (m0 + row) * pad + r;
-            for (uint32_t i = 0; i < g.parts; ++i) v += *reinterpret_cast<const v4f*>(p + (uint64_t)i * g.m * pad);
-            if (g.down && blockIdx.y == 0)
+        if (at < rows) {
+            const float* p = g.s + (m0 + at) * pad + r;
+            for (uint32_t i0 = 0; i0 < g.parts; i0 += 8) {
+                v4f w[8];
+#pragma unroll
+                for (uint32_t i = 0; i < 8; ++i) w[i] = *reinterpret_cast<const v4f*>(p + (uint64_t)min(i0 + i, g.parts - 1u) * g.m * pad);
+#pragma unroll
+                for (uint32_t i = 0; i < 8; ++i)
+                    if (i0 + i < g.parts) v += w[i];
+            }
+            if (g.down && blockIdx.y == 0 && job == 0)
                 for (uint32_t e = 0; e < 4; ++e)
-                    if (r + e < g.down_cols) g.down[(m0 + row) * g.down_cols + r + e] = v[e];
+                    if (r + e < g.down_cols) g.down[(m0 + at) * g.down_cols + r + e] = v[e];
         }
-        *reinterpret_cast<v4f*>(s_rows + row * pitch + r) = v;
+        *reinterpret_cast<v4f*>(s_rows + at * pitch + r) = v;
     }
     __syncthreads();
-    int id[RT];
-#pragma unroll
-    for (uint32_t i = 0; i < RT; ++i) id[i] = adapter_of(g.which, m0 + 16u * i + r16, g.m, g.adapters);
-    for (uint32_t n0 = (blockIdx.y * ADAPT_WAVES + wave) * 64u; n0 < g.n; n0 += gridDim.y * ADAPT_WAVES * 64u) {
-        // y is on its way while the products are made
+    const float* s_row = s_rows + r16 * pitch;
+    // which rows this block writes: one without an adapter is y, and stays as it is in place
+    const bool writes = row < g.m && !(id == NO_ADAPTER && g.y == g.out) && (!JOBS || (id >= 0 ? id == mine : job == 0));
+    const Y* y_row = static_cast<const Y*>(g.y) + min(row, (uint64_t)g.m - 1u) * g.ld_y;
+    const uint32_t step = gridDim.y * ADAPT_WAVES * 64u;
+    Sixteen<Y> y;
+    auto fetch = [&](uint32_t n0) {
         const uint32_t c = n0 + 16u * group;
-        const bool full = c + 16u <= g.n;
-        Sixteen<Y> y[RT];
-        if (g.y && full) {
+        if (!g.y) return;
+        if (c + 16u <= g.n) y.load(y_row + c);
+        else if (c < g.n) y.load_end(y_row, c, g.n);
+    };
+    uint32_t n0 = (blockIdx.y * ADAPT_WAVES + wave) * 64u;
+    if (n0 < g.n) fetch(n0);
+    for (; n0 < g.n; n0 += step) {
+        const uint32_t c = n0 + 16u * group;
+        float f[16];
+        v4f sum[4];
 #pragma unroll
-            for (uint32_t i = 0; i < RT; ++i)
-                y[i].load(static_cast<const Y*>(g.y) + min(m0 + 16u * i + r16, (uint64_t)g.m - 1u) * g.ld_y + c);
-        }
-        v4f sum[RT][4];
-#pragma unroll
-        for (uint32_t i = 0; i < RT; ++i)
-#pragma unroll
-            for (uint32_t t = 0; t < 4; ++t) sum[i][t] = v4f{0, 0, 0, 0};
-        int waits[RT], which;
-#pragma unroll
-        for (uint32_t i = 0; i < RT; ++i) waits[i] = id[i];
-        while (next_adapter<RT>(waits, &which)) {
-            v4f acc[RT][4];
-#pragma unroll
-            for (uint32_t i = 0; i < RT; ++i)
-#pragma unroll
-                for (uint32_t t = 0; t < 4; ++t) acc[i][t] = v4f{0, 0, 0, 0};
+        for (uint32_t t = 0; t < 4; ++t) sum[t] = v4f{0, 0, 0, 0};
+        int waits[1] = {id}, which = mine;
+        while (JOBS ? which >= 0 : next_adapter<1>(waits, &which)) {
+            v4f acc[4];
             const T* b[4];
 #pragma unroll
             for (uint32_t t = 0; t < 4; ++t) {
+                acc[t] = v4f{0, 0, 0, 0};
                 const uint32_t at = n0 + 16u * (r16 / 4u) + 4u * t + r16 % 4u;
                 b[t] = static_cast<const T*>(g.b) + ((uint64_t)which * g.n + min(at, g.n - 1u)) * g.rank;
             }
             for (uint32_t r = 4u * group; r < pad; r += 16u) {
-                v4f s[RT], v[4];
+                v4f v[4];
 #pragma unroll
                 for (uint32_t t = 0; t < 4; ++t) v[t] = four_of(b[t], r, g.rank);
-#pragma unroll
-                for (uint32_t i = 0; i < RT; ++i) s[i] = *reinterpret_cast<const v4f*>(s_rows + (16u * i + r16) * pitch + r);
+                const v4f s = *reinterpret_cast<const v4f*>(s_row + r);
 #pragma unroll
                 for (uint32_t e = 0; e < 4; ++e)
 #pragma unroll
-                    for (uint32_t i = 0; i < RT; ++i)
-#pragma unroll
-                        for (uint32_t t = 0; t < 4; ++t) acc[i][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[t][e], s[i][e], acc[i][t], 0, 0, 0);
+                    for (uint32_t t = 0; t < 4; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[t][e], s[e], acc[t], 0, 0, 0);
             }
 #pragma unroll
-            for (uint32_t i = 0; i < RT; ++i)
-#pragma unroll
-                for (uint32_t t = 0; t < 4; ++t)
-                    if (id[i] == which) sum[i][t] = acc[i][t];
+            for (uint32_t t = 0; t < 4; ++t)
+                if (id == which) sum[t] = acc[t];
+            if (JOBS) break;
         }
-        if (c >= g.n) continue;
+        if (g.y) {
+            float h[8];
+            y.h[0].floats(h);
 #pragma unroll
-        for (uint32_t i = 0; i < RT; ++i) {
-            const uint64_t row = m0 + 16u * i + r16;
-            // a row without an adapter is y, and stays as it is in place
-            if (row >= g.m || (id[i] == NO_ADAPTER && g.y == g.out)) continue;
-            Y* out = static_cast<Y*>(g.out) + row * g.ld_out + c;
-            float f[2][8];
-            if (g.y && full) {
-                y[i].h[0].floats(f[0]);
-                y[i].h[1].floats(f[1]);
-            } else {
+            for (uint32_t j = 0; j < 8; ++j) f[j] = h[j];
+            y.h[1].floats(h);
 #pragma unroll
-                for (uint32_t j = 0; j < 16; ++j)
-                    f[j / 8][j % 8] = g.y && c + j < g.n ? (float)static_cast<const Y*>(g.y)[row * g.ld_y + c + j] : 0.0f;
+            for (uint32_t j = 0; j < 8; ++j) f[8 + j] = h[j];
+        } else {
+#pragma unroll
+            for (uint32_t j = 0; j < 16; ++j) f[j] = 0.0f;
+        }
+        if (n0 + step < g.n) fetch(n0 + step);
+        if (!writes || c >= g.n) continue;
+        if (id != NO_ADAPTER) {
+#pragma unroll
+            for (uint32_t j = 0; j < 16; ++j) f[j] = id == BAD_ADAPTER ? NAN : f[j] + sum[j / 4][j % 4];
+        }
+        Y* out = static_cast<Y*>(g.out) + row * g.ld_out + c;
+        if (c + 16u <= g.n) {
+#pragma unroll
+            for (uint32_t h = 0; h < 2; ++h) {
+                float w[8];
+#pragma unroll
+                for (uint32_t j = 0; j < 8; ++j) w[j] = f[8 * h + j];
+                Eight<Y> e;
+                e.from(w);
+                e.store(out + 8 * h);
             }
-            if (id[i] != NO_ADAPTER) {
+        } else {
 #pragma unroll
-                for (uint32_t j = 0; j < 16; ++j) f[j / 8][j % 8] = id[i] == BAD_ADAPTER ? NAN : f[j / 8][j % 8] + sum[i][j / 4][j % 4];
-            }
-            if (full) {
-#pragma unroll
-                for (uint32_t h = 0; h < 2; ++h) {
-                    Eight<Y> e;
-                    e.from(f[h]);
-                    e.store(out + 8 * h);
-                }
-            } else {
-#pragma unroll
-                for (uint32_t j = 0; j < 16; ++j)
-                    if (c + j < g.n) out[j] = (Y)f[j / 8][j % 8];
-            }
+            for (uint32_t j = 0; j < 16; ++j)
+                if (c + j < g.n) out[j] = (Y)f[j];
         }
     }
 }
 
 template <typename T, typename Y>
 static void launch_up_of(shifter_ctx* ctx, const AdaptersUpArgs& g) {
-    const uint32_t tiles = g.m <= 256 ? 1 : 4;
-    const uint32_t blocks = (uint32_t)((g.m + 16u * tiles - 1u) / (16u * tiles)), groups = std::max(1u, (g.n + 255u) / 256u);
-    const dim3 grid(blocks, std::min(groups, std::max(1u, 2048u / blocks)));
-    const uint32_t lds = (uint32_t)(16u * tiles * (adapt_pad(g.rank) + 4u) * sizeof(float));
-    if (tiles == 1) adapters_up_kernel<T, Y, 1><<<grid, ADAPT_THREADS, lds, ctx->stream>>>(g);
-    else adapters_up_kernel<T, Y, 4><<<grid, ADAPT_THREADS, lds, ctx->stream>>>(g);
+    const uint32_t jobs = adapt_jobs(g.m, g.adapters), blocks = (uint32_t)((g.m + 15u) / 16u), groups = std::max(1u, (g.n + 255u) / 256u);
+    const dim3 grid(blocks, std::min(groups, std::max(1u, ADAPT_UP_BLOCKS / blocks)), jobs);
+    const uint32_t lds = (uint32_t)(16u * (adapt_pad(g.rank) + 4u) * sizeof(float));
+    if (jobs > 1) adapters_up_kernel<T, Y, true><<<grid, ADAPT_THREADS, lds, ctx->stream>>>(g);
+    else adapters_up_kernel<T, Y, false><<<grid, ADAPT_THREADS, lds, ctx->stream>>>(g);
 }
 template <typename T>
 static void launch_up_as(shifter_ctx* ctx, int y_dtype, const AdaptersUpArgs& g) {

@@ -9,12 +9,19 @@ namespace shifter {
 constexpr uint32_t ADAPT_MAX_RANK = 128;
 constexpr uint64_t ADAPT_MAX_ROWS = 1ull << 27;    // tiles of 16 rows, 256 threads each: less than 2^32 threads
 constexpr uint32_t ADAPT_STEP = 64;                // columns of a step of the products over long rows
+constexpr uint64_t ADAPT_FEW_ROWS = 256;
+constexpr uint32_t ADAPT_UP_BLOCKS = 2048;         // of the product with B, as far as there are columns
 constexpr uint32_t ADAPT_SLAB = 128;               // columns of a block of the gradient's sums over rows
 
 inline uint64_t adapt_pad(uint64_t rank) { return (rank + 15u) & ~15ull; }
 
 // Tiles of 16 rows that a block works on together: they share what it reads of an adapter.
-inline uint32_t adapt_tiles(uint64_t m, uint32_t rank) { return m <= 256 ? 1u : adapt_pad(rank) <= 16 ? 4u : 2u; }
+inline uint32_t adapt_tiles(uint64_t m, uint32_t rank) { return m <= ADAPT_FEW_ROWS || adapt_pad(rank) > 32 ? 1u : 2u; }
+
+// Blocks that share a tile of few rows, one for each adapter that its rows may have.
+inline uint32_t adapt_jobs(uint64_t m, uint64_t adapters) {
+    return m > ADAPT_FEW_ROWS ? 1u : (uint32_t)std::max<uint64_t>(1u, std::min<uint64_t>({16u, m, adapters}));
+}
 
 // Blocks that share the k columns of a tile's rows; each leaves its sums.
 inline uint32_t adapt_parts(uint64_t m, uint64_t k, uint32_t rank) {

@@ -78,6 +78,7 @@ struct AdaptersDownArgs {
     float* s;                  // [parts][m][rank padded to 16]
     uint64_t ld_x;
     uint32_t m, k, rank, adapters, parts;
+    uint32_t groups;           // of up to 64 ranks, a block each
 };
 struct AdaptersUpArgs {
     const float* s;
