@@ -3,14 +3,14 @@
 //   out_r = y_r + c_i (x_r A_i') B_i',   i = which[r]
 //
 // and their gradients.  The product over the long side, s_r = c_i x_r A_i', is the narrow one: rank numbers a row, held in 32 bits.
-// It is multiplied with B_i in 32 bits as well (the matrix units take fp32 at a sixteenth of bf16's rate, which up to
-// rank 32 or so is still above what memory delivers), so that out is rounded once.
+// It is multiplied with B_i in all of these bits, so that out is rounded once.
 //
 // Rows are taken in tiles of 16 as they come, whatever requests they belong to: a tile is multiplied with each adapter that
 // one of its rows has, and each row keeps the result of its own.  So rows need no sorting, a run of rows of one request costs
 // one product, and nothing that one request's adapter holds, infinities and NaN too, reaches another's rows.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "dev_common.h"
 #include "learn.h"
@@ -69,19 +69,19 @@ __device__ __forceinline__ bool next_adapter(int (&waits)[RT], int* which) {
     return false;
 }
 
-// 16 neighbouring columns of a row, as two operands.
+// Two times eight neighbouring columns of a row, `apart` columns from one to the other, as two operands.
 template <typename T>
 struct Sixteen {
     Eight<T> h[2];
-    __device__ __forceinline__ void load(const T* p) {
+    __device__ __forceinline__ void load(const T* p, uint32_t apart) {
         h[0].load(p);
-        h[1].load(p + 8);
+        h[1].load(p + apart);
     }
-    __device__ __forceinline__ void load_end(const T* row, uint32_t c, uint32_t cols) {     // zeros behind the row's end
+    __device__ __forceinline__ void load_end(const T* row, uint32_t c, uint32_t apart, uint32_t cols) {     // zeros behind the row's end
 #pragma unroll
         for (uint32_t i = 0; i < 2; ++i) {
-            fetch8(row, c + 8 * i, cols, h[i]);
-            place8(c + 8 * i, cols, h[i]);
+            fetch8(row, c + apart * i, cols, h[i]);
+            place8(c + apart * i, cols, h[i]);
         }
     }
 };
@@ -110,12 +110,14 @@ __device__ __forceinline__ bool adapter_of_job(int id, uint32_t job, int* which)
 
 // s[part][r] = c_i x_r A_i' over the part's columns; 0 for a row without an adapter, NaN for one whose adapter there is not.
 // A block has RT tiles of 16 rows and 16 RF ranks; its wavefronts take steps of 64 columns in turn and join their sums.  Both factors
-// come straight from memory into the operands: a lane's 16 columns of a row lie side by side.
+// come straight from memory into the operands: a lane has twice eight columns, so that four lanes read 64 bytes of a row side by side (the
+// 16 codes of a lane are one read, and its columns of A lie as they do).
 template <typename T, bool CODES, uint32_t RF, uint32_t RT, bool JOBS>
 __global__ __launch_bounds__(ADAPT_THREADS) void adapters_down_kernel(AdaptersDownArgs g) {
     static_assert(!JOBS || RT == 1, "a tile of a job");
     __shared__ v4f s_sum[ADAPT_WAVES][RF * RT][64];
-    const uint32_t lane = threadIdx.x & 63u, wave = uniform_u32(threadIdx.x >> 6), col = 16u * (lane / 16u), r16 = lane & 15u;
+    const uint32_t lane = threadIdx.x & 63u, wave = uniform_u32(threadIdx.x >> 6), col = (CODES ? 16u : 8u) * (lane / 16u), r16 = lane & 15u;
+    constexpr uint32_t APART = CODES ? 8 : 32;
     const uint64_t m0 = (uint64_t)blockIdx.x * 16u * RT;
     const uint32_t part = blockIdx.y, job = blockIdx.z / g.groups, rank0 = (blockIdx.z - job * g.groups) * 16u * RF;
     const uint32_t steps = (g.k + ADAPT_STEP - 1u) / ADAPT_STEP, whole = g.k / ADAPT_STEP;
@@ -156,10 +158,10 @@ __global__ __launch_bounds__(ADAPT_THREADS) void adapters_down_kernel(AdaptersDo
 #pragma unroll
             for (uint32_t i = 0; i < RT; ++i) {
                 if (CODES) o.q[i] = *reinterpret_cast<const uint4*>(q[i] + c);
-                else o.x[i].load(x[i] + c);
+                else o.x[i].load(x[i] + c, APART);
             }
 #pragma unroll
-            for (uint32_t f = 0; f < RF; ++f) o.a[f].load(a[f] + c);
+            for (uint32_t f = 0; f < RF; ++f) o.a[f].load(a[f] + c, APART);
         };
         auto multiply = [&](Operands& o) {
 #pragma unroll
@@ -199,11 +201,11 @@ __global__ __launch_bounds__(ADAPT_THREADS) void adapters_down_kernel(AdaptersDo
                     }
                     o.q[i] = make_uint4(w[0], w[1], w[2], w[3]);
                 } else {
-                    o.x[i].load_end(x[i], c, g.k);
+                    o.x[i].load_end(x[i], c, APART, g.k);
                 }
             }
 #pragma unroll
-            for (uint32_t f = 0; f < RF; ++f) o.a[f].load_end(a[f], c, g.k);
+            for (uint32_t f = 0; f < RF; ++f) o.a[f].load_end(a[f], c, APART, g.k);
             multiply(o);
         }
 #pragma unroll
@@ -262,142 +264,360 @@ static void launch_down(shifter_ctx* ctx, int dtype, AdaptersDownArgs g) {
     else g.x_scale ? launch_down_of<_Float16, true>(ctx, g) : launch_down_of<_Float16, false>(ctx, g);
 }
 
-// Four neighbouring numbers of a row of B, from rank r on, zeros behind its end.
-template <typename T>
-__device__ __forceinline__ v4f four_of(const T* row, uint32_t r, uint32_t rank) {
-    if (r + 4u <= rank) {
-        typedef T vec __attribute__((ext_vector_type(4), aligned(sizeof(T))));
-        const vec v = *reinterpret_cast<const vec*>(row + r);
-        return v4f{(float)v[0], (float)v[1], (float)v[2], (float)v[3]};
-    }
-    v4f f;
+// Four neighbouring ranks of a column of B and of a row of s, as operands of products over 16 ranks: lane l holds four, 4 (l / 16) on, of
+// row or column l % 16.
+//
+// The matrix units take fp32 at a sixteenth of bf16's rate: 16 ranks of a tile are four products of 32 cycles.  s is cut into three bf16 of
+// 8 bits each instead, which are all of its 24, and a bf16 B is multiplied with them as it is, two pieces to a product of 16 cycles; an fp16
+// B is two bf16, of 8 and 3 bits, three products.  All products of pieces are exact and summed in 32 bits.
+__device__ __forceinline__ uint2 high_halves(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return make_uint2(__builtin_amdgcn_perm(b, a, 0x07060302), __builtin_amdgcn_perm(d, c, 0x07060302));
+}
+__device__ __forceinline__ v4f mma_pieces(uint2 a0, uint2 a1, uint2 b0, uint2 b1, v4f acc) {
+    typedef __bf16 vec __attribute__((ext_vector_type(8)));
+    const uint32_t u[4] = {a0.x, a0.y, a1.x, a1.y}, v[4] = {b0.x, b0.y, b1.x, b1.y};
+    vec p, q;
+    __builtin_memcpy(&p, u, 16);
+    __builtin_memcpy(&q, v, 16);
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(p, q, acc, 0, 0, 0);
+}
+// The upper 8 bits of four numbers' 24, and what is left of them.
+__device__ __forceinline__ uint2 upper_of(v4f& v) {
+    uint32_t w[4];
 #pragma unroll
-    for (uint32_t e = 0; e < 4; ++e) f[e] = r + e < rank ? (float)row[r + e] : 0.0f;
-    return f;
+    for (uint32_t e = 0; e < 4; ++e) {
+        w[e] = __float_as_uint(v[e]) & 0xffff0000u;
+        v[e] = isinf(v[e]) ? 0.0f : v[e] - __uint_as_float(w[e]);
+    }
+    return high_halves(w[0], w[1], w[2], w[3]);
+}
+struct SPieces {
+    uint2 p[3];
+    __device__ __forceinline__ void from(v4f v) {
+        p[0] = upper_of(v);
+        p[1] = upper_of(v);
+        p[2] = high_halves(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+    }
+};
+// n of four elements at p, zeros behind them.
+template <bool EVEN, typename T>
+__device__ __forceinline__ void four_of(const T* p, int32_t n, uint32_t (&w)[sizeof(T)]) {
+    if (EVEN || n >= 4) {
+        typedef T vec __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+        const vec v = *reinterpret_cast<const vec*>(p);
+        __builtin_memcpy(w, &v, sizeof(v));
+    } else {
+        T v[4];
+#pragma unroll
+        for (int32_t e = 0; e < 4; ++e) v[e] = e < n ? p[e] : (T)0.0f;
+        __builtin_memcpy(w, v, sizeof(v));
+    }
+}
+template <typename T>
+struct BFour {
+    uint2 p;
+    typedef SPieces S;
+    template <bool EVEN>
+    __device__ __forceinline__ void load(const T* row, uint32_t r, uint32_t rank) {
+        uint32_t w[2];
+        four_of<EVEN>(row + r, (int32_t)(rank - r), w);
+        p = make_uint2(w[0], w[1]);
+    }
+    __device__ __forceinline__ v4f multiply(const S& s, v4f acc) const {
+        acc = mma_pieces(p, p, s.p[0], s.p[1], acc);
+        return mma_pieces(p, make_uint2(0, 0), s.p[2], make_uint2(0, 0), acc);
+    }
+};
+template <>
+struct BFour<_Float16> {
+    uint2 high, low;
+    typedef SPieces S;
+    template <bool EVEN>
+    __device__ __forceinline__ void load(const _Float16* row, uint32_t r, uint32_t rank) {
+        uint32_t w[2];
+        four_of<EVEN>(row + r, (int32_t)(rank - r), w);
+        _Float16 h[4];
+        __builtin_memcpy(h, w, 8);
+        v4f v{(float)h[0], (float)h[1], (float)h[2], (float)h[3]};
+        high = upper_of(v);
+        low = upper_of(v);
+    }
+    __device__ __forceinline__ v4f multiply(const S& s, v4f acc) const {
+        acc = mma_pieces(high, high, s.p[0], s.p[1], acc);
+        acc = mma_pieces(high, low, s.p[2], s.p[0], acc);
+        return mma_pieces(low, low, s.p[1], s.p[2], acc);
+    }
+};
+template <>
+struct BFour<float> {
+    v4f v;
+    struct S {
+        v4f v;
+        __device__ __forceinline__ void from(v4f x) { v = x; }
+    };
+    template <bool EVEN>
+    __device__ __forceinline__ void load(const float* row, uint32_t r, uint32_t rank) {
+        uint32_t w[4];
+        four_of<EVEN>(row + r, (int32_t)(rank - r), w);
+        __builtin_memcpy(&v, w, 16);
+    }
+    __device__ __forceinline__ v4f multiply(const S& s, v4f acc) const {
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(v[e], s.v[e], acc, 0, 0, 0);
+        return acc;
+    }
+};
+
+// out_r = y_r + s_r B_i'.  A wavefront multiplies tiles of 16 rows with 64 columns; the columns of a tile's four products are
+// interleaved so that a lane ends with twice eight neighbouring columns of a row, which it adds to y and writes: 32 half + 8 group on.
+template <typename T, typename Y>
+struct UpTile {
+    uint32_t lane = threadIdx.x & 63u, group = lane / 16u, r16 = lane & 15u;
+
+    // The row of B that product t takes as its column i = lane % 16.
+    __device__ __forceinline__ const T* b_row(const AdaptersUpArgs& g, int which, uint32_t n0, uint32_t t) const {
+        const uint32_t at = n0 + 32u * (t / 2u) + 8u * (r16 / 4u) + 4u * (t % 2u) + r16 % 4u;
+        return static_cast<const T*>(g.b) + ((uint64_t)which * g.n + min(at, g.n - 1u)) * g.rank;
+    }
+    __device__ __forceinline__ uint32_t col(uint32_t n0, uint32_t half) const { return n0 + 32u * half + 8u * group; }
+    // FULL: all 64 columns are there.
+    template <bool FULL>
+    __device__ __forceinline__ void fetch(const AdaptersUpArgs& g, uint64_t row, uint32_t n0, Eight<Y> (&y)[2]) const {
+        if (!g.y) return;
+        const Y* y_row = static_cast<const Y*>(g.y) + min(row, (uint64_t)g.m - 1u) * g.ld_y;
+#pragma unroll
+        for (uint32_t h = 0; h < 2; ++h) {
+            const uint32_t c = col(n0, h);
+            if (FULL) {
+                y[h].load(y_row + c);
+            } else {
+                fetch8(y_row, c, g.n, y[h]);
+                place8(c, g.n, y[h]);
+            }
+        }
+    }
+    // A row without an adapter is y, and stays as it is in place.
+    __device__ __forceinline__ static bool stays(const AdaptersUpArgs& g, int id) { return id == NO_ADAPTER && g.y == g.out; }
+    template <bool FULL>
+    __device__ __forceinline__ void write(const AdaptersUpArgs& g, uint64_t row, bool writes, int id, uint32_t n0, const Eight<Y> (&y)[2], v4f (&sum)[4]) const {
+        if (__ballot(id < 0)) {
+            const float none = g.y ? -0.0f : 0.0f;         // y as it is, its zeros' signs too
+#pragma unroll
+            for (uint32_t t = 0; t < 4; ++t)
+#pragma unroll
+                for (uint32_t e = 0; e < 4; ++e) sum[t][e] = id == BAD_ADAPTER ? NAN : id < 0 ? none : sum[t][e];
+        }
+        if (!writes) return;
+        Y* out_row = static_cast<Y*>(g.out) + row * g.ld_out;
+#pragma unroll
+        for (uint32_t h = 0; h < 2; ++h) {
+            const uint32_t c = col(n0, h);
+            float f[8];
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) f[j] = sum[2 * h + j / 4][j % 4];
+            if (g.y) {
+                float w[8];
+                y[h].floats(w);
+#pragma unroll
+                for (uint32_t j = 0; j < 8; ++j) f[j] += w[j];
+            }
+            if (FULL || c + 8u <= g.n) {
+                Eight<Y> e;
+                e.from(f);
+                e.store(out_row + c);
+            } else {
+#pragma unroll
+                for (uint32_t j = 0; j < 8; ++j)
+                    if (c + j < g.n) out_row[c + j] = (Y)f[j];
+            }
+        }
+    }
+};
+// s's four numbers of a row from rank r on: the sum of the parts'.
+__device__ __forceinline__ v4f sum_of_parts(const AdaptersUpArgs& g, uint64_t row, uint32_t r, uint32_t pad) {
+    const float* p = g.s + row * pad + r;
+    const uint64_t next = (uint64_t)g.m * pad;
+    constexpr uint32_t MOST = 8;           // under way
+    v4f v = *reinterpret_cast<const v4f*>(p);
+    for (uint32_t i0 = 1; i0 < g.parts; i0 += MOST) {
+        v4f w[MOST];
+#pragma unroll
+        for (uint32_t i = 0; i < MOST; ++i)
+            if (i0 + i < g.parts) w[i] = *reinterpret_cast<const v4f*>(p + (i0 + i) * next);
+#pragma unroll
+        for (uint32_t i = 0; i < MOST; ++i)
+            if (i0 + i < g.parts) v += w[i];
+    }
+    return v;
+}
+__device__ __forceinline__ void keep_down(const AdaptersUpArgs& g, uint64_t row, uint32_t r, v4f v) {
+#pragma unroll
+    for (uint32_t e = 0; e < 4; ++e)
+        if (r + e < g.down_cols) g.down[row * g.down_cols + r + e] = v[e];
 }
 
-// out_r = y_r + s_r B_i'.  A wavefront has a tile of 16 rows and takes 64 columns at a time; the columns of its four products are
-// interleaved so that a lane ends with 16 neighbouring columns of a row, which it adds to y and writes.  The next columns' y is on
-// its way meanwhile.  s, the sums of all parts, is in LDS.
-template <typename T, typename Y, bool JOBS>
+// A tile of rows for each block, whose wavefronts take 64 columns in turn: for few rows, and for ranks above 32.  s is in LDS.
+template <typename T, typename Y, bool JOBS, bool EVEN>
 __global__ __launch_bounds__(ADAPT_THREADS) void adapters_up_kernel(AdaptersUpArgs g) {
     extern __shared__ __align__(16) float s_rows[];        // [16][pad + 4]
-    const uint32_t lane = threadIdx.x & 63u, wave = uniform_u32(threadIdx.x >> 6), group = lane / 16u, r16 = lane & 15u;
-    const uint64_t m0 = (uint64_t)blockIdx.x * 16u, row = m0 + r16;
+    const UpTile<T, Y> tile;
+    const uint32_t wave = uniform_u32(threadIdx.x >> 6);
+    const uint64_t m0 = (uint64_t)blockIdx.x * 16u, row = m0 + tile.r16;
     const uint32_t pad = (g.rank + 15u) & ~15u, pitch = pad + 4u, fours = pad / 4u, job = blockIdx.z;
     const int id = adapter_of(g.which, row, g.m, g.adapters);
     int mine = NO_ADAPTER;
     if (JOBS && !adapter_of_job(id, job, &mine) && job != 0) return;
-    const uint32_t rows = (uint32_t)min((uint64_t)16u, g.m - m0);
     for (uint32_t u = threadIdx.x; u < 16u * fours; u += ADAPT_THREADS) {
         const uint32_t at = u / fours, r = u % fours * 4u;
         v4f v{0, 0, 0, 0};
-        if (at < rows) {
-            const float* p = g.s + (m0 + at) * pad + r;
-            for (uint32_t i0 = 0; i0 < g.parts; i0 += 8) {
-                v4f w[8];
-#pragma unroll
-                for (uint32_t i = 0; i < 8; ++i) w[i] = *reinterpret_cast<const v4f*>(p + (uint64_t)min(i0 + i, g.parts - 1u) * g.m * pad);
-#pragma unroll
-                for (uint32_t i = 0; i < 8; ++i)
-                    if (i0 + i < g.parts) v += w[i];
-            }
-            if (g.down && blockIdx.y == 0 && job == 0)
-                for (uint32_t e = 0; e < 4; ++e)
-                    if (r + e < g.down_cols) g.down[(m0 + at) * g.down_cols + r + e] = v[e];
+        if (m0 + at < g.m) {
+            v = sum_of_parts(g, m0 + at, r, pad);
+            if (g.down && blockIdx.y == 0 && job == 0) keep_down(g, m0 + at, r, v);
         }
         *reinterpret_cast<v4f*>(s_rows + at * pitch + r) = v;
     }
     __syncthreads();
-    const float* s_row = s_rows + r16 * pitch;
-    // which rows this block writes: one without an adapter is y, and stays as it is in place
-    const bool writes = row < g.m && !(id == NO_ADAPTER && g.y == g.out) && (!JOBS || (id >= 0 ? id == mine : job == 0));
-    const Y* y_row = static_cast<const Y*>(g.y) + min(row, (uint64_t)g.m - 1u) * g.ld_y;
-    const uint32_t step = gridDim.y * ADAPT_WAVES * 64u;
-    Sixteen<Y> y;
-    auto fetch = [&](uint32_t n0) {
-        const uint32_t c = n0 + 16u * group;
-        if (!g.y) return;
-        if (c + 16u <= g.n) y.load(y_row + c);
-        else if (c < g.n) y.load_end(y_row, c, g.n);
-    };
-    uint32_t n0 = (blockIdx.y * ADAPT_WAVES + wave) * 64u;
-    if (n0 < g.n) fetch(n0);
-    for (; n0 < g.n; n0 += step) {
-        const uint32_t c = n0 + 16u * group;
-        float f[16];
+    const float* s_row = s_rows + tile.r16 * pitch;
+    const bool writes = row < g.m && !tile.stays(g, id) && (!JOBS || (id >= 0 ? id == mine : job == 0));
+    auto columns = [&](uint32_t n0, auto full) {
+        Eight<Y> y[2];
+        tile.template fetch<full.value>(g, row, n0, y);
         v4f sum[4];
 #pragma unroll
         for (uint32_t t = 0; t < 4; ++t) sum[t] = v4f{0, 0, 0, 0};
         int waits[1] = {id}, which = mine;
+        bool first = true;
         while (JOBS ? which >= 0 : next_adapter<1>(waits, &which)) {
             v4f acc[4];
             const T* b[4];
 #pragma unroll
             for (uint32_t t = 0; t < 4; ++t) {
                 acc[t] = v4f{0, 0, 0, 0};
-                const uint32_t at = n0 + 16u * (r16 / 4u) + 4u * t + r16 % 4u;
-                b[t] = static_cast<const T*>(g.b) + ((uint64_t)which * g.n + min(at, g.n - 1u)) * g.rank;
+                b[t] = tile.b_row(g, which, n0, t);
             }
-            for (uint32_t r = 4u * group; r < pad; r += 16u) {
-                v4f v[4];
+            for (uint32_t r = 4u * tile.group; r < pad; r += 16u) {
+                BFour<T> v[4];
+                typename BFour<T>::S s;
 #pragma unroll
-                for (uint32_t t = 0; t < 4; ++t) v[t] = four_of(b[t], r, g.rank);
-                const v4f s = *reinterpret_cast<const v4f*>(s_row + r);
+                for (uint32_t t = 0; t < 4; ++t) v[t].template load<EVEN>(b[t], r, g.rank);
+                s.from(*reinterpret_cast<const v4f*>(s_row + r));
 #pragma unroll
-                for (uint32_t e = 0; e < 4; ++e)
-#pragma unroll
-                    for (uint32_t t = 0; t < 4; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[t][e], s[e], acc[t], 0, 0, 0);
+                for (uint32_t t = 0; t < 4; ++t) acc[t] = v[t].multiply(s, acc[t]);
             }
+            // the first one's are overwritten where a row has another
 #pragma unroll
             for (uint32_t t = 0; t < 4; ++t)
-                if (id == which) sum[t] = acc[t];
+                if (first || id == which) sum[t] = acc[t];
+            first = false;
             if (JOBS) break;
         }
-        if (g.y) {
-            float h[8];
-            y.h[0].floats(h);
-#pragma unroll
-            for (uint32_t j = 0; j < 8; ++j) f[j] = h[j];
-            y.h[1].floats(h);
-#pragma unroll
-            for (uint32_t j = 0; j < 8; ++j) f[8 + j] = h[j];
-        } else {
-#pragma unroll
-            for (uint32_t j = 0; j < 16; ++j) f[j] = 0.0f;
-        }
-        if (n0 + step < g.n) fetch(n0 + step);
-        if (!writes || c >= g.n) continue;
-        if (id != NO_ADAPTER) {
-#pragma unroll
-            for (uint32_t j = 0; j < 16; ++j) f[j] = id == BAD_ADAPTER ? NAN : f[j] + sum[j / 4][j % 4];
-        }
-        Y* out = static_cast<Y*>(g.out) + row * g.ld_out + c;
-        if (c + 16u <= g.n) {
-#pragma unroll
-            for (uint32_t h = 0; h < 2; ++h) {
-                float w[8];
-#pragma unroll
-                for (uint32_t j = 0; j < 8; ++j) w[j] = f[8 * h + j];
-                Eight<Y> e;
-                e.from(w);
-                e.store(out + 8 * h);
-            }
-        } else {
-#pragma unroll
-            for (uint32_t j = 0; j < 16; ++j)
-                if (c + j < g.n) out[j] = (Y)f[j];
-        }
+        tile.template write<full.value>(g, row, writes, id, n0, y, sum);
+    };
+    const uint32_t step = gridDim.y * ADAPT_WAVES * 64u;
+    for (uint32_t n0 = (blockIdx.y * ADAPT_WAVES + wave) * 64u; n0 < g.n; n0 += step) {
+        if (n0 + 64u <= g.n) columns(n0, std::true_type{});
+        else columns(n0, std::false_type{});
     }
+}
+
+// 64 columns for each wavefront, which takes tiles of rows in turn and keeps its columns of B in registers as long as the rows have the same
+// adapter; the next tile's s and y are on their way meanwhile.  Nothing in the loop of a full tile of one adapter is in a lane's branch: with
+// the ends of rows and columns looked after there, prompts of 8192 rows took 46 us.
+template <typename T, typename Y, uint32_t NF, bool EVEN>
+__global__ __launch_bounds__(ADAPT_THREADS) void adapters_up_rows_kernel(AdaptersUpArgs g) {
+    constexpr uint32_t PAD = 16 * NF;
+    const UpTile<T, Y> tile;
+    const uint32_t n0 = (blockIdx.x * ADAPT_WAVES + uniform_u32(threadIdx.x >> 6)) * 64u;
+    const bool live = n0 < g.n, keeps = g.down && n0 == 0;
+    if (!live && !keeps) return;
+    const uint32_t tiles = (g.m + 15u) / 16u;
+    auto rows = [&](auto full) {
+        struct Operands {
+            int id;
+            v4f s[2][NF];              // of two parts: added up where they are used, so that no fetch waits
+            Eight<Y> y[2];
+        };
+        auto fetch = [&](uint32_t t, Operands& o) {
+            const uint64_t row = (uint64_t)t * 16u + tile.r16, at = min(row, (uint64_t)g.m - 1u);
+            o.id = adapter_of(g.which, row, g.m, g.adapters);
+#pragma unroll
+            for (uint32_t f = 0; f < NF; ++f) {
+                const float* p = g.s + at * PAD + 16u * f + 4u * tile.group;
+                o.s[0][f] = *reinterpret_cast<const v4f*>(p);
+                o.s[1][f] = v4f{0, 0, 0, 0};
+                if (g.parts > 1) o.s[1][f] = *reinterpret_cast<const v4f*>(p + (uint64_t)g.m * PAD);
+            }
+            if (full.value || live) tile.template fetch<full.value>(g, row, n0, o.y);
+        };
+        uint32_t t = blockIdx.y;
+        Operands next;
+        if (t < tiles) fetch(t, next);
+        int held = NO_ADAPTER;
+        BFour<T> b[NF][4];
+        for (; t < tiles; t += gridDim.y) {
+            const Operands o = next;
+            const uint64_t row = (uint64_t)t * 16u + tile.r16;
+            if (t + gridDim.y < tiles) fetch(t + gridDim.y, next);
+            if (keeps) {
+                if (row < g.m) {
+#pragma unroll
+                    for (uint32_t f = 0; f < NF; ++f) keep_down(g, row, 16u * f + 4u * tile.group, o.s[0][f] + o.s[1][f]);
+                }
+                if (!live) continue;
+            }
+            typename BFour<T>::S s[NF];
+#pragma unroll
+            for (uint32_t f = 0; f < NF; ++f) s[f].from(o.s[0][f] + o.s[1][f]);
+            v4f sum[4];
+            int waits[1] = {o.id}, which;
+            bool first = true;
+            while (next_adapter<1>(waits, &which)) {
+                if (which != held) {
+                    held = which;
+#pragma unroll
+                    for (uint32_t i = 0; i < 4; ++i)
+#pragma unroll
+                        for (uint32_t f = 0; f < NF; ++f) b[f][i].template load<EVEN>(tile.b_row(g, which, n0, i), 16u * f + 4u * tile.group, g.rank);
+                    // waited for here, or the compiler waits for all that is under way wherever B is used
+                    __builtin_amdgcn_s_waitcnt(0x0f70);
+                }
+                v4f acc[4];
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i) acc[i] = v4f{0, 0, 0, 0};
+#pragma unroll
+                for (uint32_t f = 0; f < NF; ++f)
+#pragma unroll
+                    for (uint32_t i = 0; i < 4; ++i) acc[i] = b[f][i].multiply(s[f], acc[i]);
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i)
+                    if (first || o.id == which) sum[i] = acc[i];
+                first = false;
+            }
+            tile.template write<full.value>(g, row, row < g.m && !tile.stays(g, o.id), o.id, n0, o.y, sum);
+        }
+    };
+    if (n0 + 64u <= g.n) rows(std::true_type{});
+    else rows(std::false_type{});
 }
 
 template <typename T, typename Y>
 static void launch_up_of(shifter_ctx* ctx, const AdaptersUpArgs& g) {
-    const uint32_t jobs = adapt_jobs(g.m, g.adapters), blocks = (uint32_t)((g.m + 15u) / 16u), groups = std::max(1u, (g.n + 255u) / 256u);
-    const dim3 grid(blocks, std::min(groups, std::max(1u, ADAPT_UP_BLOCKS / blocks)), jobs);
-    const uint32_t lds = (uint32_t)(16u * (adapt_pad(g.rank) + 4u) * sizeof(float));
-    if (jobs > 1) adapters_up_kernel<T, Y, true><<<grid, ADAPT_THREADS, lds, ctx->stream>>>(g);
-    else adapters_up_kernel<T, Y, false><<<grid, ADAPT_THREADS, lds, ctx->stream>>>(g);
+    const uint32_t jobs = adapt_jobs(g.m, g.adapters), tiles = (uint32_t)((g.m + 15u) / 16u), groups = std::max(1u, (g.n + 255u) / 256u);
+    const uint64_t pad = adapt_pad(g.rank);
+    if (g.m > ADAPT_FEW_ROWS && pad <= 32) {
+        const dim3 grid(groups, std::min(tiles, std::max(1u, ADAPT_UP_BLOCKS / groups)));
+        if (pad == 16 && g.rank == pad) adapters_up_rows_kernel<T, Y, 1, true><<<grid, ADAPT_THREADS, 0, ctx->stream>>>(g);
+        else if (pad == 16) adapters_up_rows_kernel<T, Y, 1, false><<<grid, ADAPT_THREADS, 0, ctx->stream>>>(g);
+        else if (g.rank == pad) adapters_up_rows_kernel<T, Y, 2, true><<<grid, ADAPT_THREADS, 0, ctx->stream>>>(g);
+        else adapters_up_rows_kernel<T, Y, 2, false><<<grid, ADAPT_THREADS, 0, ctx->stream>>>(g);
+        return;
+    }
+    const dim3 grid(tiles, std::min(groups, std::max(1u, ADAPT_UP_BLOCKS / tiles)), jobs);
+    const uint32_t lds = (uint32_t)(16u * (pad + 4u) * sizeof(float));
+    if (jobs > 1 && g.rank == pad) adapters_up_kernel<T, Y, true, true><<<grid, ADAPT_THREADS, lds, ctx->stream>>>(g);
+    else if (jobs > 1) adapters_up_kernel<T, Y, true, false><<<grid, ADAPT_THREADS, lds, ctx->stream>>>(g);
+    else if (g.rank == pad) adapters_up_kernel<T, Y, false, true><<<grid, ADAPT_THREADS, lds, ctx->stream>>>(g);
+    else adapters_up_kernel<T, Y, false, false><<<grid, ADAPT_THREADS, lds, ctx->stream>>>(g);
 }
 template <typename T>
 static void launch_up_as(shifter_ctx* ctx, int y_dtype, const AdaptersUpArgs& g) {

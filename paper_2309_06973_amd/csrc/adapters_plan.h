@@ -9,14 +9,15 @@ namespace shifter {
 constexpr uint32_t ADAPT_MAX_RANK = 128;
 constexpr uint64_t ADAPT_MAX_ROWS = 1ull << 27;    // tiles of 16 rows, 256 threads each: less than 2^32 threads
 constexpr uint32_t ADAPT_STEP = 64;                // columns of a step of the products over long rows
-constexpr uint64_t ADAPT_FEW_ROWS = 256;
+constexpr uint64_t ADAPT_FEW_ROWS = 256, ADAPT_TWO_TILES = 2048;
+constexpr uint32_t ADAPT_MANY_ROWS_PARTS = 2;      // with more rows, their product with B holds so many in registers
 constexpr uint32_t ADAPT_UP_BLOCKS = 2048;         // of the product with B, as far as there are columns
 constexpr uint32_t ADAPT_SLAB = 128;               // columns of a block of the gradient's sums over rows
 
 inline uint64_t adapt_pad(uint64_t rank) { return (rank + 15u) & ~15ull; }
 
 // Tiles of 16 rows that a block works on together: they share what it reads of an adapter.
-inline uint32_t adapt_tiles(uint64_t m, uint32_t rank) { return m <= ADAPT_FEW_ROWS || adapt_pad(rank) > 32 ? 1u : 2u; }
+inline uint32_t adapt_tiles(uint64_t m, uint32_t rank) { return adapt_pad(rank) > 32 || m < ADAPT_TWO_TILES ? 1u : 2u; }
 
 // Blocks that share a tile of few rows, one for each adapter that its rows may have.
 inline uint32_t adapt_jobs(uint64_t m, uint64_t adapters) {
@@ -28,7 +29,8 @@ inline uint32_t adapt_parts(uint64_t m, uint64_t k, uint32_t rank) {
     const uint64_t rows = 16u * adapt_tiles(m, rank), blocks = (m + rows - 1u) / rows, steps = (k + ADAPT_STEP - 1u) / ADAPT_STEP;
     uint64_t parts = blocks ? 512u / blocks : 1u;
     if (parts > steps / 4u) parts = steps / 4u;    // each of a block's four wavefronts has a step
-    return parts < 1 ? 1u : parts > 32 ? 32u : (uint32_t)parts;
+    const uint64_t most = m > ADAPT_FEW_ROWS ? ADAPT_MANY_ROWS_PARTS : 32u;
+    return parts < 1 ? 1u : parts > most ? (uint32_t)most : (uint32_t)parts;
 }
 
 struct AdaptersPlan {
