@@ -28,6 +28,9 @@ __device__ __forceinline__ int adapter_of(const int64_t* which, uint64_t row, ui
     return i < 0 ? NO_ADAPTER : i < (int64_t)adapters ? (int)i : BAD_ADAPTER;
 }
 
+// The nth row of an order.
+__device__ __forceinline__ uint64_t row_of(const uint32_t* order, uint64_t nth) { return order ? order[nth] : nth; }
+
 // acc[i][j] += sum over 32 columns of a[i] b[j]: lane l holds eight columns, 8 (l / 16) on, of row l % 16 of each, and
 // rows 4 (l / 16) on of column l % 16 of the result.
 __device__ __forceinline__ v4f mma(const Eight<__bf16>& a, const Eight<__bf16>& b, v4f acc) {
@@ -112,23 +115,28 @@ __device__ __forceinline__ bool adapter_of_job(int id, uint32_t job, int* which)
 // A block has RT tiles of 16 rows and 16 RF ranks; its wavefronts take steps of 64 columns in turn and join their sums.  Both factors
 // come straight from memory into the operands: a lane has twice eight columns, so that four lanes read 64 bytes of a row side by side (the
 // 16 codes of a lane are one read, and its columns of A lie as they do).
-template <typename T, bool CODES, uint32_t RF, uint32_t RT, bool JOBS>
+// Blocks share the adapters of a tile's rows (g.jobs of them; of a tile of one adapter all but one end at once), and write the rows of
+// theirs: a tile of several would take several times as long as the others, and the kernel with it (prompts of 8192 rows with five
+// borders 21 us for 13).
+template <typename T, bool CODES, uint32_t RF, uint32_t RT>
 __global__ __launch_bounds__(ADAPT_THREADS) void adapters_down_kernel(AdaptersDownArgs g) {
-    static_assert(!JOBS || RT == 1, "a tile of a job");
     __shared__ v4f s_sum[ADAPT_WAVES][RF * RT][64];
     const uint32_t lane = threadIdx.x & 63u, wave = uniform_u32(threadIdx.x >> 6), col = (CODES ? 16u : 8u) * (lane / 16u), r16 = lane & 15u;
     constexpr uint32_t APART = CODES ? 8 : 32;
-    const uint64_t m0 = (uint64_t)blockIdx.x * 16u * RT;
-    const uint32_t part = blockIdx.y, job = blockIdx.z / g.groups, rank0 = (blockIdx.z - job * g.groups) * 16u * RF;
+    const uint32_t tile = blockIdx.x, job = blockIdx.z / g.groups;
+    const uint64_t m0 = (uint64_t)tile * 16u * RT;
+    const uint32_t part = blockIdx.y, rank0 = (blockIdx.z - job * g.groups) * 16u * RF;
     const uint32_t steps = (g.k + ADAPT_STEP - 1u) / ADAPT_STEP, whole = g.k / ADAPT_STEP;
     const uint32_t s0 = (uint32_t)((uint64_t)steps * part / g.parts), s1 = (uint32_t)((uint64_t)steps * (part + 1u) / g.parts);
     int id[RT], waits[RT];
+    uint32_t row[RT];
     const T* x[RT];
     const int8_t* q[RT];
 #pragma unroll
     for (uint32_t i = 0; i < RT; ++i) {
-        const uint64_t row = m0 + 16u * i + r16, at = min(row, (uint64_t)g.m - 1u);
-        id[i] = waits[i] = adapter_of(g.which, row, g.m, g.adapters);
+        const uint64_t nth = m0 + 16u * i + r16, at = row_of(g.order, min(nth, (uint64_t)g.m - 1u));
+        row[i] = (uint32_t)at;
+        id[i] = waits[i] = nth < g.m ? adapter_of(g.which, at, g.m, g.adapters) : NO_ADAPTER;
         x[i] = static_cast<const T*>(g.x) + at * g.ld_x;
         q[i] = static_cast<const int8_t*>(g.x) + at * g.ld_x;
     }
@@ -137,9 +145,13 @@ __global__ __launch_bounds__(ADAPT_THREADS) void adapters_down_kernel(AdaptersDo
     for (uint32_t i = 0; i < RT; ++i)
 #pragma unroll
         for (uint32_t f = 0; f < RF; ++f) sum[i][f] = v4f{0, 0, 0, 0};
-    int which = NO_ADAPTER;
-    if (JOBS && !adapter_of_job(id[0], job, &which) && job != 0) return;
-    while (JOBS ? which >= 0 : next_adapter<RT>(waits, &which)) {
+    bool mine[RT];                         // rows without an adapter are the first one's
+#pragma unroll
+    for (uint32_t i = 0; i < RT; ++i) mine[i] = job == 0 && id[i] < 0;
+    int which;
+    uint32_t nth = 0;
+    while (next_adapter<RT>(waits, &which)) {
+        if (nth++ % g.jobs != job) continue;
         const T* a[RF];
 #pragma unroll
         for (uint32_t f = 0; f < RF; ++f)
@@ -173,15 +185,14 @@ __global__ __launch_bounds__(ADAPT_THREADS) void adapters_down_kernel(AdaptersDo
                     for (uint32_t h = 0; h < 2; ++h) acc[i][f] = mma(o.a[f].h[h], o.x[i].h[h], acc[i][f]);
             }
         };
-        Operands o;
+        Operands o, next;
         const uint32_t end = min(s1, whole);
         uint32_t s = s0 + wave;
-        if (s < end) fetch(s, o);
+        if (s < end) fetch(s, next);
         for (; s < end; s += ADAPT_WAVES) {
-            Operands next;
+            o = next;
             if (s + ADAPT_WAVES < end) fetch(s + ADAPT_WAVES, next);
             multiply(o);
-            o = next;
         }
         if (s1 > whole && (s1 - 1u - s0) % ADAPT_WAVES == wave) {        // the step that a row ends in
             const uint32_t c = whole * ADAPT_STEP + col;
@@ -213,8 +224,10 @@ __global__ __launch_bounds__(ADAPT_THREADS) void adapters_down_kernel(AdaptersDo
 #pragma unroll
             for (uint32_t f = 0; f < RF; ++f)
                 if (id[i] == which) sum[i][f] = acc[i][f];
-        if (JOBS) break;
+#pragma unroll
+        for (uint32_t i = 0; i < RT; ++i) mine[i] = mine[i] || id[i] == which;
     }
+    if (job >= nth && job != 0) return;    // all wavefronts alike
 #pragma unroll
     for (uint32_t i = 0; i < RT; ++i)
 #pragma unroll
@@ -225,29 +238,29 @@ __global__ __launch_bounds__(ADAPT_THREADS) void adapters_down_kernel(AdaptersDo
     for (uint32_t u = 0; u < RF * RT; ++u) {
         if (u % ADAPT_WAVES != wave) continue;
         const uint32_t i = u / RF, f = u % RF, r = rank0 + 16u * f + 4u * (lane / 16u);
-        const uint64_t row = m0 + 16u * i + r16;
-        if (row >= g.m || rank0 + 16u * f >= pad) continue;
-        if (JOBS && id[i] != which && (id[i] >= 0 || job != 0)) continue;
+        const uint64_t nth = m0 + 16u * i + r16;
+        if (nth >= g.m || rank0 + 16u * f >= pad) continue;
+        if (!mine[i]) continue;
         v4f v = (s_sum[0][u][lane] + s_sum[1][u][lane]) + (s_sum[2][u][lane] + s_sum[3][u][lane]);
         float by = 1.0f;
         if (id[i] >= 0) {
             if (g.scale) by = g.scale[id[i]];
-            if (CODES) by *= g.x_scale[row];
+            if (CODES) by *= g.x_scale[row[i]];
         }
 #pragma unroll
         for (uint32_t e = 0; e < 4; ++e) v[e] = id[i] == BAD_ADAPTER ? NAN : id[i] < 0 || r + e >= g.rank ? 0.0f : v[e] * by;
-        *reinterpret_cast<v4f*>(g.s + ((uint64_t)part * g.m + row) * pad + r) = v;
+        *reinterpret_cast<v4f*>(g.s + ((uint64_t)part * g.m + nth) * pad + r) = v;
     }
 }
 
 template <typename T, bool CODES, uint32_t RF>
 static void launch_down_as(shifter_ctx* ctx, const AdaptersDownArgs& g) {
-    constexpr uint32_t MORE = RF == 4 ? 1 : 2;
-    const uint32_t tiles = adapt_tiles(g.m, g.rank), jobs = adapt_jobs(g.m, g.adapters);
-    const dim3 grid((uint32_t)((g.m + 16u * tiles - 1u) / (16u * tiles)), g.parts, g.groups * jobs);
-    if (jobs > 1) adapters_down_kernel<T, CODES, RF, 1, true><<<grid, ADAPT_THREADS, 0, ctx->stream>>>(g);
-    else if (tiles == 1) adapters_down_kernel<T, CODES, RF, 1, false><<<grid, ADAPT_THREADS, 0, ctx->stream>>>(g);
-    else adapters_down_kernel<T, CODES, RF, MORE, false><<<grid, ADAPT_THREADS, 0, ctx->stream>>>(g);
+    const uint32_t tiles = adapt_tiles(g.m, g.rank);
+    const uint32_t blocks = (uint32_t)((g.m + 16u * tiles - 1u) / (16u * tiles));
+    const dim3 grid(blocks, g.parts, g.groups * g.jobs);
+    if constexpr (RF < 4)
+        if (tiles == 2) return adapters_down_kernel<T, CODES, RF, 2><<<grid, ADAPT_THREADS, 0, ctx->stream>>>(g);
+    adapters_down_kernel<T, CODES, RF, 1><<<grid, ADAPT_THREADS, 0, ctx->stream>>>(g);
 }
 template <typename T, bool CODES>
 static void launch_down_of(shifter_ctx* ctx, const AdaptersDownArgs& g) {
@@ -258,6 +271,7 @@ static void launch_down_of(shifter_ctx* ctx, const AdaptersDownArgs& g) {
 }
 static void launch_down(shifter_ctx* ctx, int dtype, AdaptersDownArgs g) {
     g.groups = (uint32_t)(adapt_pad(g.rank) + 63u) / 64u;
+    g.jobs = adapt_down_jobs(g.m, g.adapters);
     ProfileScope ps(ctx, K_ADAPTERS_DOWN);
     if (dtype == SHIFTER_F32) g.x_scale ? launch_down_of<float, true>(ctx, g) : launch_down_of<float, false>(ctx, g);
     else if (dtype == SHIFTER_BF16) g.x_scale ? launch_down_of<__bf16, true>(ctx, g) : launch_down_of<__bf16, false>(ctx, g);
@@ -462,9 +476,9 @@ __global__ __launch_bounds__(ADAPT_THREADS) void adapters_up_kernel(AdaptersUpAr
     extern __shared__ __align__(16) float s_rows[];        // [16][pad + 4]
     const UpTile<T, Y> tile;
     const uint32_t wave = uniform_u32(threadIdx.x >> 6);
-    const uint64_t m0 = (uint64_t)blockIdx.x * 16u, row = m0 + tile.r16;
+    const uint64_t m0 = (uint64_t)blockIdx.x * 16u, nth = m0 + tile.r16, row = row_of(g.order, min(nth, (uint64_t)g.m - 1u));
     const uint32_t pad = (g.rank + 15u) & ~15u, pitch = pad + 4u, fours = pad / 4u, job = blockIdx.z;
-    const int id = adapter_of(g.which, row, g.m, g.adapters);
+    const int id = nth < g.m ? adapter_of(g.which, row, g.m, g.adapters) : NO_ADAPTER;
     int mine = NO_ADAPTER;
     if (JOBS && !adapter_of_job(id, job, &mine) && job != 0) return;
     for (uint32_t u = threadIdx.x; u < 16u * fours; u += ADAPT_THREADS) {
@@ -472,13 +486,13 @@ __global__ __launch_bounds__(ADAPT_THREADS) void adapters_up_kernel(AdaptersUpAr
         v4f v{0, 0, 0, 0};
         if (m0 + at < g.m) {
             v = sum_of_parts(g, m0 + at, r, pad);
-            if (g.down && blockIdx.y == 0 && job == 0) keep_down(g, m0 + at, r, v);
+            if (g.down && blockIdx.y == 0 && job == 0) keep_down(g, row_of(g.order, m0 + at), r, v);
         }
         *reinterpret_cast<v4f*>(s_rows + at * pitch + r) = v;
     }
     __syncthreads();
     const float* s_row = s_rows + tile.r16 * pitch;
-    const bool writes = row < g.m && !tile.stays(g, id) && (!JOBS || (id >= 0 ? id == mine : job == 0));
+    const bool writes = nth < g.m && !tile.stays(g, id) && (!JOBS || (id >= 0 ? id == mine : job == 0));
     auto columns = [&](uint32_t n0, auto full) {
         Eight<Y> y[2];
         tile.template fetch<full.value>(g, row, n0, y);
@@ -534,11 +548,14 @@ __global__ __launch_bounds__(ADAPT_THREADS) void adapters_up_rows_kernel(Adapter
     auto rows = [&](auto full) {
         struct Operands {
             int id;
+            uint64_t row;
             v4f s[2][NF];              // of two parts: added up where they are used, so that no fetch waits
             Eight<Y> y[2];
         };
-        auto fetch = [&](uint32_t t, Operands& o) {
-            const uint64_t row = (uint64_t)t * 16u + tile.r16, at = min(row, (uint64_t)g.m - 1u);
+        auto row_at = [&](uint32_t t) { return row_of(g.order, min((uint64_t)t * 16u + tile.r16, (uint64_t)g.m - 1u)); };
+        auto fetch = [&](uint32_t t, uint64_t row, Operands& o) {
+            const uint64_t at = min((uint64_t)t * 16u + tile.r16, (uint64_t)g.m - 1u);
+            o.row = row;
             o.id = adapter_of(g.which, row, g.m, g.adapters);
 #pragma unroll
             for (uint32_t f = 0; f < NF; ++f) {
@@ -551,17 +568,20 @@ __global__ __launch_bounds__(ADAPT_THREADS) void adapters_up_rows_kernel(Adapter
         };
         uint32_t t = blockIdx.y;
         Operands next;
-        if (t < tiles) fetch(t, next);
+        if (t < tiles) fetch(t, row_at(t), next);
+        uint64_t later = row_at(min(t + gridDim.y, tiles - 1u));           // where the next tile's rows are is known a tile ahead
         int held = NO_ADAPTER;
         BFour<T> b[NF][4];
         for (; t < tiles; t += gridDim.y) {
-            const Operands o = next;
-            const uint64_t row = (uint64_t)t * 16u + tile.r16;
-            if (t + gridDim.y < tiles) fetch(t + gridDim.y, next);
+            Operands o = next;
+            const bool there = (uint64_t)t * 16u + tile.r16 < g.m;
+            if (!there) o.id = NO_ADAPTER;
+            if (t + gridDim.y < tiles) fetch(t + gridDim.y, later, next);
+            later = row_at(min(t + 2u * gridDim.y, tiles - 1u));
             if (keeps) {
-                if (row < g.m) {
+                if (there) {
 #pragma unroll
-                    for (uint32_t f = 0; f < NF; ++f) keep_down(g, row, 16u * f + 4u * tile.group, o.s[0][f] + o.s[1][f]);
+                    for (uint32_t f = 0; f < NF; ++f) keep_down(g, o.row, 16u * f + 4u * tile.group, o.s[0][f] + o.s[1][f]);
                 }
                 if (!live) continue;
             }
@@ -593,7 +613,7 @@ __global__ __launch_bounds__(ADAPT_THREADS) void adapters_up_rows_kernel(Adapter
                     if (first || o.id == which) sum[i] = acc[i];
                 first = false;
             }
-            tile.template write<full.value>(g, row, row < g.m && !tile.stays(g, o.id), o.id, n0, o.y, sum);
+            tile.template write<full.value>(g, o.row, there && !tile.stays(g, o.id), o.id, n0, o.y, sum);
         }
     };
     if (n0 + 64u <= g.n) rows(std::true_type{});
@@ -632,15 +652,88 @@ static void launch_up(shifter_ctx* ctx, int dtype, int y_dtype, const AdaptersUp
     else launch_up_as<_Float16>(ctx, y_dtype, g);
 }
 
+// The rows in the order of their adapters, those without one at the end, by one block: rows are counted by adapter in LDS, each with its
+// place among the ones counted before it.  The order of an adapter's rows is not always the same, which no row's result depends on.
+constexpr uint32_t SORT_THREADS = 1024, SORT_EACH = 8;
+__global__ __launch_bounds__(SORT_THREADS) void adapters_sort_kernel(const int64_t* which, uint32_t m, uint32_t adapters, uint32_t* order) {
+    constexpr uint32_t BINS = (uint32_t)ADAPT_SORT_MOST + 2u, PER = (BINS + SORT_THREADS - 1u) / SORT_THREADS;
+    __shared__ uint32_t s_bin[PER * SORT_THREADS];
+    __shared__ uint64_t smem[SORT_THREADS / 64 + 1];
+    for (uint32_t i = threadIdx.x; i < PER * SORT_THREADS; i += SORT_THREADS) s_bin[i] = 0;
+    __syncthreads();
+    uint32_t bin[SORT_EACH], place[SORT_EACH];
+    auto count = [&](uint64_t r0) {
+#pragma unroll
+        for (uint32_t e = 0; e < SORT_EACH; ++e) {
+            const uint64_t r = r0 + e * SORT_THREADS + threadIdx.x;
+            const int id = adapter_of(which, r, m, adapters);
+            bin[e] = r >= m ? BINS : id < 0 ? adapters : (uint32_t)id;
+        }
+#pragma unroll
+        for (uint32_t e = 0; e < SORT_EACH; ++e) {
+            // rows of one adapter side by side go as one addition
+            const bool want = bin[e] != BINS;
+            const uint64_t todo = __ballot(want);
+            if (todo == 0) break;
+            const uint32_t first = (uint32_t)__ffsll((unsigned long long)todo) - 1u, lane = threadIdx.x & 63u;
+            const uint32_t leader = (uint32_t)__builtin_amdgcn_readlane((int)bin[e], (int)first);
+            const uint64_t peers = __ballot(want && bin[e] == leader);
+            uint32_t base = 0;
+            if (lane == first) base = atomicAdd(&s_bin[leader], (uint32_t)__popcll(peers));
+            base = (uint32_t)__builtin_amdgcn_readlane((int)base, (int)first);
+            if (want && bin[e] == leader) place[e] = base + (uint32_t)__popcll(peers & ((1ull << lane) - 1ull));
+            else if (want) place[e] = atomicAdd(&s_bin[bin[e]], 1u);
+        }
+    };
+    auto firsts = [&] {                    // of the bins, in the place of their numbers
+        uint64_t sum = 0, all;
+        uint32_t c[PER];
+        __syncthreads();
+#pragma unroll
+        for (uint32_t i = 0; i < PER; ++i) sum += c[i] = s_bin[threadIdx.x * PER + i];
+        uint64_t at = block_excl_scan_u64<SORT_THREADS>(sum, smem, &all);
+#pragma unroll
+        for (uint32_t i = 0; i < PER; ++i) {
+            s_bin[threadIdx.x * PER + i] = (uint32_t)at;
+            at += c[i];
+        }
+        __syncthreads();
+    };
+    if (m <= SORT_THREADS * SORT_EACH) {
+        count(0);
+        firsts();
+#pragma unroll
+        for (uint32_t e = 0; e < SORT_EACH; ++e)
+            if (bin[e] != BINS) order[s_bin[bin[e]] + place[e]] = e * SORT_THREADS + threadIdx.x;
+        return;
+    }
+    // more rows than the threads hold: counted once, and once more from the bins' first places on
+    for (uint64_t r0 = 0; r0 < m; r0 += SORT_THREADS * SORT_EACH) count(r0);
+    firsts();
+    for (uint64_t r0 = 0; r0 < m; r0 += SORT_THREADS * SORT_EACH) {
+        count(r0);
+#pragma unroll
+        for (uint32_t e = 0; e < SORT_EACH; ++e)
+            if (bin[e] != BINS) order[place[e]] = (uint32_t)(r0 + e * SORT_THREADS + threadIdx.x);
+    }
+}
+
 void launch_adapters(shifter_ctx* ctx, int dtype, int y_dtype, const AdaptersArgs& g) {
-    const AdaptersPlan p = adapters_plan(g.m, g.k, g.rank);
+    const AdaptersPlan p = adapters_plan(g.m, g.k, g.rank, g.adapters);
+    uint32_t* order = nullptr;
+    if (adapt_sorted(g.m, g.adapters)) {
+        ProfileScope ps(ctx, K_ADAPTERS_TURN);
+        order = reinterpret_cast<uint32_t*>(g.work + p.order);
+        adapters_sort_kernel<<<1, SORT_THREADS, 0, ctx->stream>>>(g.which, g.m, g.adapters, order);
+    }
     AdaptersDownArgs d{};
     d.x = g.x; d.ld_x = g.ld_x; d.x_scale = g.x_scale; d.a = g.a; d.which = g.which; d.scale = g.scale;
     d.m = g.m; d.k = g.k; d.rank = g.rank; d.adapters = g.adapters; d.parts = p.parts;
+    d.order = order;
     d.s = reinterpret_cast<float*>(g.work);
     launch_down(ctx, dtype, d);
     AdaptersUpArgs u{};
-    u.s = d.s; u.parts = p.parts; u.b = g.b; u.which = g.which; u.m = g.m; u.n = g.n; u.rank = g.rank; u.adapters = g.adapters;
+    u.s = d.s; u.order = order; u.parts = p.parts; u.b = g.b; u.which = g.which; u.m = g.m; u.n = g.n; u.rank = g.rank; u.adapters = g.adapters;
     u.y = g.y; u.ld_y = g.ld_y; u.out = g.out; u.ld_out = g.ld_out; u.down = g.down; u.down_cols = g.rank;
     launch_up(ctx, dtype, y_dtype, u);
 }
@@ -652,7 +745,7 @@ void launch_adapters(shifter_ctx* ctx, int dtype, int y_dtype, const AdaptersArg
 // up and dx are the products above with the adapters turned.  The sums over rows take fp32 products as well: both factors are rows as they
 // lie, a lane's eight neighbouring columns are one operand of eight products.
 
-// Blocks up to `adapters`: the rows of an adapter in order, behind those of the ones before it.  Further ones turn 64 columns of an
+// Blocks up to `adapters`: the rows of an adapter in order, behind those of the ones before it; at the end those of none.  Further ones turn 64 columns of an
 // adapter: A [rank][k] to [k][rank], or B [n][rank] to [rank][n].
 template <typename T>
 __global__ __launch_bounds__(ADAPT_THREADS) void adapters_turn_kernel(AdaptersTurnArgs g) {
@@ -660,32 +753,49 @@ __global__ __launch_bounds__(ADAPT_THREADS) void adapters_turn_kernel(AdaptersTu
     __shared__ uint32_t s_before[ADAPT_WAVES], s_mine[ADAPT_WAVES];
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
     uint64_t b = blockIdx.x;
-    if (b < g.adapters) {
-        uint32_t before = 0;                   // rows of adapters before this one
-        for (uint64_t r = threadIdx.x; r < g.m; r += ADAPT_THREADS) {
+    if (b <= g.adapters) {
+        // the last bin: rows without an adapter, or with one that is not there
+        auto bin_of = [&](uint64_t r) {
             const int id = adapter_of(g.which, r, g.m, g.adapters);
-            before += id >= 0 && id < (int)b;
+            return r >= g.m ? ~0u : id < 0 ? g.adapters : (uint32_t)id;
+        };
+        constexpr uint32_t EACH = 8;           // neighbouring rows of a thread
+        uint32_t before = 0;                   // rows of bins before this one
+        for (uint64_t r0 = 0; r0 < g.m; r0 += ADAPT_THREADS * EACH) {
+            uint32_t bin[EACH];
+#pragma unroll
+            for (uint32_t e = 0; e < EACH; ++e) bin[e] = bin_of(r0 + e * ADAPT_THREADS + threadIdx.x);
+#pragma unroll
+            for (uint32_t e = 0; e < EACH; ++e) before += bin[e] < b;
         }
         for (uint32_t d = 1; d < 64; d <<= 1) before += __shfl_xor(before, d, 64);
         if (lane == 0) s_before[wave] = before;
         __syncthreads();
         uint32_t at = s_before[0] + s_before[1] + s_before[2] + s_before[3];
         if (threadIdx.x == 0) g.first[b] = at;
-        for (uint64_t r0 = 0; r0 < g.m; r0 += ADAPT_THREADS) {
-            const bool mine = adapter_of(g.which, r0 + threadIdx.x, g.m, g.adapters) == (int)b;
-            const uint64_t who = __ballot(mine);
+        for (uint64_t r0 = 0; r0 < g.m; r0 += ADAPT_THREADS * EACH) {
+            const uint64_t r = r0 + threadIdx.x * EACH;
+            uint32_t mine = 0, n = 0;
+#pragma unroll
+            for (uint32_t e = 0; e < EACH; ++e) mine |= (uint32_t)(bin_of(r + e) == b) << e;
+            n = (uint32_t)__popc(mine);
+            uint32_t upto = n;                 // this lane's and those before it
+#pragma unroll
+            for (uint32_t d = 1; d < 64; d <<= 1) {
+                const uint32_t o = __shfl_up(upto, d, 64);
+                if (lane >= d) upto += o;
+            }
             __syncthreads();
-            if (lane == 0) s_mine[wave] = (uint32_t)__popcll(who);
+            if (lane == 63) s_mine[wave] = upto;
             __syncthreads();
-            uint32_t to = at + (uint32_t)__popcll(who & ((1ull << lane) - 1ull));
+            uint32_t to = at + upto - n;
             for (uint32_t w = 0; w < wave; ++w) to += s_mine[w];
-            if (mine) g.rows[to] = (uint32_t)(r0 + threadIdx.x);
+            for (; mine; mine &= mine - 1u) g.rows[to++] = (uint32_t)r + (uint32_t)__ffs(mine) - 1u;
             at += s_mine[0] + s_mine[1] + s_mine[2] + s_mine[3];
         }
-        if (threadIdx.x == 0 && b + 1 == g.adapters) g.first[g.adapters] = at;
         return;
     }
-    b -= g.adapters;
+    b -= g.adapters + 1u;
     const uint32_t tiles_a = (g.k + 63u) / 64u, tiles_b = (g.n + 63u) / 64u;
     const bool of_a = b < (uint64_t)tiles_a * g.adapters;
     if (!of_a) b -= (uint64_t)tiles_a * g.adapters;
@@ -726,54 +836,84 @@ __global__ __launch_bounds__(ADAPT_THREADS) void adapters_grad_kernel(AdaptersSu
     const uint32_t from = g.first[adapter], count = g.first[adapter + 1] - from;
     const uint32_t each = ((count + g.parts - 1u) / g.parts + 15u) & ~15u, q0 = min(blockIdx.y * each, count), q1 = min(q0 + each, count);
     const uint32_t* list = g.rows + from;
+    const bool codes = CODES && of_a, full = slab * ADAPT_SLAB + ADAPT_SLAB <= cols;
+    const uint8_t* rows_x = static_cast<const uint8_t*>(of_a ? g.x : g.g);
+    const uint64_t pitch = (of_a ? g.ld_x : g.ld_g) * (codes ? 1u : sizeof(T));
+    struct Operands {
+        Eight<T> v[DEPTH];
+        uint2 w[DEPTH];
+        float p[DEPTH][RF], by[DEPTH];
+    };
     for (uint32_t rank0 = 0; rank0 < g.rank; rank0 += 16u * RF) {
         v4f acc[RF][8];
 #pragma unroll
         for (uint32_t f = 0; f < RF; ++f)
 #pragma unroll
             for (uint32_t j = 0; j < 8; ++j) acc[f][j] = v4f{0, 0, 0, 0};
-        for (uint32_t at = q0 + wave * 4u * DEPTH; at < q1; at += ADAPT_WAVES * 4u * DEPTH) {
-            Eight<T> v[DEPTH];
-            uint2 w[DEPTH];
-            float p[DEPTH][RF];
-            const bool codes = CODES && of_a;
+        uint32_t rank_at[RF];
+#pragma unroll
+        for (uint32_t f = 0; f < RF; ++f) rank_at[f] = min(rank0 + 16u * f + r16, g.rank - 1u);
+        auto rows_at = [&](uint32_t at, uint32_t (&row)[DEPTH]) {
+#pragma unroll
+            for (uint32_t d = 0; d < DEPTH; ++d) row[d] = list[min(at + 4u * d + group, q1 - 1u)];
+        };
+        auto fetch = [&](const uint32_t (&row)[DEPTH], Operands& o) {
 #pragma unroll
             for (uint32_t d = 0; d < DEPTH; ++d) {
-                const uint32_t nth = at + 4u * d + group;
-                const uint64_t row = list[min(nth, q1 - 1u)];
-                if (codes) {
-                    // a row's codes are there up to a multiple of 16
-                    w[d] = c < cols ? *reinterpret_cast<const uint2*>(static_cast<const int8_t*>(g.x) + row * g.ld_x + c) : make_uint2(0u, 0u);
+                const uint8_t* from_row = rows_x + row[d] * pitch;
+                if (codes) {                   // they are there up to a multiple of 16
+                    o.w[d] = make_uint2(0u, 0u);
+                    if (full || c < cols) o.w[d] = *reinterpret_cast<const uint2*>(from_row + c);
+                    o.by[d] = g.x_scale[row[d]];
+                } else if (full) {
+                    o.v[d].load(reinterpret_cast<const T*>(from_row) + c);
                 } else {
-                    const T* from_row = of_a ? static_cast<const T*>(g.x) + row * g.ld_x : static_cast<const T*>(g.g) + row * g.ld_g;
-                    fetch8(from_row, c, cols, v[d]);
+                    fetch8(reinterpret_cast<const T*>(from_row), c, cols, o.v[d]);
                 }
-                const float by = codes ? g.x_scale[row] : 1.0f;
 #pragma unroll
-                for (uint32_t f = 0; f < RF; ++f) {
-                    const uint32_t r = rank0 + 16u * f + r16;
-                    const float one = s[row * ld_s + min(r, g.rank - 1u)] * by;
-                    p[d][f] = nth < q1 ? one : 0.0f;
-                }
+                for (uint32_t f = 0; f < RF; ++f) o.p[d][f] = s[row[d] * ld_s + rank_at[f]];
+            }
+        };
+        // the next rows are on their way while these are multiplied, and where the ones after them are is known
+        constexpr uint32_t TURN = ADAPT_WAVES * 4u * DEPTH;
+        uint32_t at = q0 + wave * 4u * DEPTH, row[DEPTH];
+        Operands next;
+        if (at < q1) {
+            rows_at(at, row);
+            fetch(row, next);
+            rows_at(at + TURN, row);
+        }
+        for (; at < q1; at += TURN) {
+            const Operands o = next;
+            if (at + TURN < q1) {
+                fetch(row, next);
+                rows_at(at + 2u * TURN, row);
             }
 #pragma unroll
             for (uint32_t d = 0; d < DEPTH; ++d) {
                 float x[8];
                 if (codes) {
 #pragma unroll
-                    for (uint32_t j = 0; j < 8; ++j) x[j] = (float)(int8_t)((j < 4 ? w[d].x : w[d].y) >> (8 * (j % 4)));
+                    for (uint32_t j = 0; j < 8; ++j) x[j] = (float)(int8_t)((j < 4 ? o.w[d].x : o.w[d].y) >> (8 * (j % 4)));
                 } else {
-                    place8(c, cols, v[d]);
-                    v[d].floats(x);
+                    Eight<T> v = o.v[d];
+                    if (!full) place8(c, cols, v);
+                    v.floats(x);
                 }
-                if (at + 4u * d + group >= q1) {           // behind the last row: its numbers once more, which do not count
+                float p[RF];
 #pragma unroll
-                    for (uint32_t j = 0; j < 8; ++j) x[j] = 0.0f;
+                for (uint32_t f = 0; f < RF; ++f) p[f] = codes ? o.p[d][f] * o.by[d] : o.p[d][f];
+                if (at + 4u * DEPTH > q1) {    // behind the last row: its numbers once more, which do not count
+                    const bool in = at + 4u * d + group < q1;
+#pragma unroll
+                    for (uint32_t f = 0; f < RF; ++f) p[f] = in ? p[f] : 0.0f;
+#pragma unroll
+                    for (uint32_t j = 0; j < 8; ++j) x[j] = in ? x[j] : 0.0f;
                 }
 #pragma unroll
                 for (uint32_t f = 0; f < RF; ++f)
 #pragma unroll
-                    for (uint32_t j = 0; j < 8; ++j) acc[f][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(p[d][f], x[j], acc[f][j], 0, 0, 0);
+                    for (uint32_t j = 0; j < 8; ++j) acc[f][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(p[f], x[j], acc[f][j], 0, 0, 0);
             }
         }
         // wavefronts 2 and 3 to 0 and 1, then 1 to 0
@@ -798,16 +938,40 @@ __global__ __launch_bounds__(ADAPT_THREADS) void adapters_grad_kernel(AdaptersSu
         // lane: ranks 4 group on, columns c on
         float* out = g.parts == 1 ? (of_a ? g.da : g.db) + (uint64_t)adapter * cols * g.rank
                                   : g.partial + (((uint64_t)blockIdx.y * g.adapters + adapter) * (g.k + g.n) + (of_a ? 0 : g.k)) * g.rank;
+        typedef float loose __attribute__((ext_vector_type(4), aligned(4)));
 #pragma unroll
-        for (uint32_t f = 0; f < RF; ++f)
+        for (uint32_t f = 0; f < RF; ++f) {
+            const uint32_t r = rank0 + 16u * f + 4u * group;
+            if (of_a) {
 #pragma unroll
-            for (uint32_t e = 0; e < 4; ++e) {
-                const uint32_t r = rank0 + 16u * f + 4u * group + e;
-                if (r >= g.rank) continue;
+                for (uint32_t e = 0; e < 4; ++e) {
+                    if (r + e >= g.rank) continue;
+                    float* to = out + (uint64_t)(r + e) * cols + c;
+                    if (full) {
 #pragma unroll
-                for (uint32_t j = 0; j < 8; ++j)
-                    if (c + j < cols) out[of_a ? (uint64_t)r * cols + c + j : (uint64_t)(c + j) * g.rank + r] = acc[f][j][e];
+                        for (uint32_t h = 0; h < 2; ++h)
+                            reinterpret_cast<loose*>(to)[h] = loose{acc[f][4 * h][e], acc[f][4 * h + 1][e], acc[f][4 * h + 2][e], acc[f][4 * h + 3][e]};
+                    } else {
+#pragma unroll
+                        for (uint32_t j = 0; j < 8; ++j)
+                            if (c + j < cols) to[j] = acc[f][j][e];
+                    }
+                }
+            } else {
+#pragma unroll
+                for (uint32_t j = 0; j < 8; ++j) {
+                    if (c + j >= cols) continue;
+                    float* to = out + (uint64_t)(c + j) * g.rank + r;
+                    if (r + 4u <= g.rank) {
+                        *reinterpret_cast<loose*>(to) = loose{acc[f][j][0], acc[f][j][1], acc[f][j][2], acc[f][j][3]};
+                    } else {
+#pragma unroll
+                        for (uint32_t e = 0; e < 4; ++e)
+                            if (r + e < g.rank) to[e] = acc[f][j][e];
+                    }
+                }
             }
+        }
     }
 }
 
@@ -841,16 +1005,18 @@ static void launch_gradients(shifter_ctx* ctx, int dtype, const AdaptersGradArgs
     t.which = g.which; t.a = g.a; t.b = g.b; t.m = g.m; t.n = g.n; t.k = g.k; t.rank = g.rank; t.adapters = g.adapters;
     t.a_turned = at(p.a); t.b_turned = at(p.b);
     t.rows = reinterpret_cast<uint32_t*>(at(p.rows)); t.first = reinterpret_cast<uint32_t*>(at(p.first));
-    if (g.adapters) {
+    {
         ProfileScope ps(ctx, K_ADAPTERS_TURN);
-        const uint64_t blocks = g.adapters * (1ull + (g.k + 63u) / 64u + (g.n + 63u) / 64u);
+        const uint64_t blocks = 1ull + g.adapters * (1ull + (g.k + 63u) / 64u + (g.n + 63u) / 64u);
         adapters_turn_kernel<T><<<(uint32_t)blocks, ADAPT_THREADS, 0, ctx->stream>>>(t);
     }
     AdaptersDownArgs d{};
     d.which = g.which; d.scale = g.scale; d.m = g.m; d.rank = g.rank; d.adapters = g.adapters;
     d.s = reinterpret_cast<float*>(at(p.sums));
+    // the lists are there anyway: rows are taken in their order where tiles as they come could have many adapters
+    d.order = adapt_sorted(g.m, g.adapters) ? t.rows : nullptr;
     AdaptersUpArgs u{};
-    u.s = d.s; u.which = g.which; u.m = g.m; u.rank = g.rank; u.adapters = g.adapters;
+    u.s = d.s; u.order = d.order; u.which = g.which; u.m = g.m; u.rank = g.rank; u.adapters = g.adapters;
     const float* down = g.down;
     uint64_t ld_down = g.rank;
     if (!down && g.m) {                        // once more; its sums are joined by a pass that writes no columns

@@ -7,7 +7,8 @@
 namespace shifter {
 
 constexpr uint32_t ADAPT_MAX_RANK = 128;
-constexpr uint64_t ADAPT_MAX_ROWS = 1ull << 27;    // tiles of 16 rows, 256 threads each: less than 2^32 threads
+constexpr uint64_t ADAPT_MAX_ROWS = 1ull << 25;    // tiles of 16 rows, up to four blocks of 256 threads each: less than 2^32 threads
+constexpr uint64_t ADAPT_SORT_FROM = 8, ADAPT_SORT_MOST = 4094;
 constexpr uint32_t ADAPT_STEP = 64;                // columns of a step of the products over long rows
 constexpr uint64_t ADAPT_FEW_ROWS = 256, ADAPT_TWO_TILES = 2048;
 constexpr uint32_t ADAPT_MANY_ROWS_PARTS = 2;      // with more rows, their product with B holds so many in registers
@@ -24,6 +25,14 @@ inline uint32_t adapt_jobs(uint64_t m, uint64_t adapters) {
     return m > ADAPT_FEW_ROWS ? 1u : (uint32_t)std::max<uint64_t>(1u, std::min<uint64_t>({16u, m, adapters}));
 }
 
+// The same for the product over long rows, of any number of rows.
+inline uint32_t adapt_down_jobs(uint64_t m, uint64_t adapters) {
+    return m <= ADAPT_FEW_ROWS ? adapt_jobs(m, adapters) : adapters >= 2 ? 2u : 1u;
+}
+
+// Whether the rows are put in order of their adapters first: one more launch, of 6 to 9 us, where tiles of rows as they come could have many.
+inline bool adapt_sorted(uint64_t m, uint64_t adapters) { return m > ADAPT_FEW_ROWS && adapters >= ADAPT_SORT_FROM && adapters <= ADAPT_SORT_MOST; }
+
 // Blocks that share the k columns of a tile's rows; each leaves its sums.
 inline uint32_t adapt_parts(uint64_t m, uint64_t k, uint32_t rank) {
     const uint64_t rows = 16u * adapt_tiles(m, rank), blocks = (m + rows - 1u) / rows, steps = (k + ADAPT_STEP - 1u) / ADAPT_STEP;
@@ -35,12 +44,14 @@ inline uint32_t adapt_parts(uint64_t m, uint64_t k, uint32_t rank) {
 
 struct AdaptersPlan {
     uint32_t parts;
+    uint64_t order;                    // rows in the order of their adapters, behind the sums
     uint64_t bytes;
 };
-inline AdaptersPlan adapters_plan(uint64_t m, uint64_t k, uint32_t rank) {
+inline AdaptersPlan adapters_plan(uint64_t m, uint64_t k, uint32_t rank, uint64_t adapters) {
     AdaptersPlan p{};
     p.parts = adapt_parts(m, k, rank);
-    p.bytes = p.parts * m * adapt_pad(rank) * 4u;
+    p.order = p.parts * m * adapt_pad(rank) * 4u;
+    p.bytes = p.order + (adapt_sorted(m, adapters) ? 4u * m : 0u);
     return p;
 }
 
@@ -76,7 +87,7 @@ inline AdaptersGradPlan adapters_grad_plan(uint64_t m, uint64_t n, uint64_t k, u
     p.a = take(adapters * k * rank * size);
     p.b = take(adapters * n * rank * size);
     p.rows = take(4u * m);
-    p.first = take(4u * (adapters + 1u));
+    p.first = take(4u * (adapters + 2u));
     p.partial = take(p.parts_rows > 1 ? p.parts_rows * adapters * (k + n) * rank * 4u : 0u);
     p.bytes = at;
     return p;
@@ -88,7 +99,7 @@ inline const char* adapters_bad_sizes(uint64_t m, uint64_t n, uint64_t k, uint64
     if (rank < 1 || rank > ADAPT_MAX_RANK) return "a rank that is not 1 to 128";
     if (n > Q8_MAX_ROWS || k > Q8_MAX_ROWS || adapters > (1u << 24)) return "more than 2^31 - 1 columns or 2^24 adapters";
     *capacity = true;
-    if (m > ADAPT_MAX_ROWS) return "more than 2^27 rows";
+    if (m > ADAPT_MAX_ROWS) return "more than 2^25 rows";
     // the gradient's blocks of 64 columns of all adapters, 256 threads each
     if (adapters * (1u + (k + 63u) / 64u + (n + 63u) / 64u) >= 1ull << 24) return "more columns of all adapters than a launch holds";
     *capacity = false;

@@ -1944,7 +1944,7 @@ extern "C" int shifter_adapters_layout(uint64_t m, uint64_t n, uint64_t k, uint6
     bool capacity;
     if (const char* why = adapters_bad_sizes(m, n, k, rank, adapters, &capacity))
         return fail(nullptr, capacity ? SHIFTER_ERR_CAPACITY : SHIFTER_ERR_INVALID_ARG, std::string("adapters_layout: ") + why);
-    *h_work_bytes = adapters_plan(m, k, (uint32_t)rank).bytes;
+    *h_work_bytes = adapters_plan(m, k, (uint32_t)rank, adapters).bytes;
     return SHIFTER_OK;
 }
 
@@ -1996,7 +1996,7 @@ extern "C" int shifter_adapters(shifter_ctx* ctx, const shifter_adapters_args* a
     Q8_REFUSE("adapters", q8_bad_rows(a->d_out, size, a->m, a->n, a->ld_out));
     if (a->d_out == a->d_y && a->ld_out != a->ld_y && a->m > 1 && a->n)
         return fail(ctx, SHIFTER_ERR_INVALID_ARG, "adapters: d_out is d_y with another stride");
-    if ((rc = adapters_work(ctx, "adapters", adapters_plan(a->m, a->k, (uint32_t)a->rank).bytes, a->d_work, a->work_bytes))) return rc;
+    if ((rc = adapters_work(ctx, "adapters", adapters_plan(a->m, a->k, (uint32_t)a->rank, a->adapters).bytes, a->d_work, a->work_bytes))) return rc;
     if (a->m == 0 || (a->n == 0 && !a->d_down)) return SHIFTER_OK;
     AdaptersArgs g{};
     g.x = a->d_x; g.x_scale = a->d_q_scale; g.a = a->d_a; g.b = a->d_b; g.which = a->d_which; g.scale = a->d_scale;

@@ -75,13 +75,15 @@ struct AdaptersDownArgs {
     const void* a;
     const int64_t* which;
     const float* scale;
-    float* s;                  // [parts][m][rank padded to 16]
+    const uint32_t* order;     // the rows in the order that they are taken in, or nullptr: as they come
+    float* s;                  // [parts][m][rank padded to 16], in that order
     uint64_t ld_x;
     uint32_t m, k, rank, adapters, parts;
-    uint32_t groups;           // of up to 64 ranks, a block each
+    uint32_t groups, jobs;     // of up to 64 ranks, a block each; blocks that share a tile's adapters
 };
 struct AdaptersUpArgs {
     const float* s;
+    const uint32_t* order;
     const void* b;
     const int64_t* which;
     const void* y;             // or nullptr: 0

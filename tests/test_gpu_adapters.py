@@ -311,7 +311,7 @@ def test_refusals(ops):
     with pytest.raises(ValueError, match="g must have"):
         ops.adapters_grad(y.bfloat16(), x, a, b, num)
     with pytest.raises(S.ShifterError) as e:
-        S.shifter_adapters_layout((1 << 27) + 1, 1, 1, 1, 1)
+        S.shifter_adapters_layout((1 << 25) + 1, 1, 1, 1, 1)
     assert e.value.code == S.SHIFTER_ERR_CAPACITY
     with pytest.raises(S.ShifterError, match="more columns of all adapters") as e:
         S.shifter_adapters_grad_layout(1, 1 << 20, 1 << 20, 1, 1 << 10, 0)
