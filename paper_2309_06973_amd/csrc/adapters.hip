@@ -819,10 +819,14 @@ __global__ __launch_bounds__(ADAPT_THREADS) void adapters_turn_kernel(AdaptersTu
     }
 }
 
-// Sums over the rows of an adapter, of the part blockIdx.y of them: 128 columns of dA_i = sum up' x or, further blocks, of
+// An adapter's parts have places of their own among `parts + adapters`: the ones before it that its rows' first number gives, and one more for
+// each adapter before it, whose last part may not be whole.
+__device__ __forceinline__ uint64_t part_of(uint32_t first, uint32_t adapter, uint32_t rows_each) { return first / rows_each + adapter; }
+
+// Sums over the rows of an adapter, rows_each of them from blockIdx.y rows_each on: 128 columns of dA_i = sum up' x or, further blocks, of
 // dB_i = sum g' down, 16 RF ranks at a time.  Wavefronts take 16 rows in turn and join their sums in LDS.
 template <typename T, bool CODES, uint32_t RF>
-__global__ __launch_bounds__(ADAPT_THREADS) void adapters_grad_kernel(AdaptersSumArgs g) {
+__global__ __launch_bounds__(ADAPT_THREADS, 3) void adapters_grad_kernel(AdaptersSumArgs g) {
     constexpr uint32_t DEPTH = 4;              // four rows each
     __shared__ v4f s_sum[2][8 * RF][64];
     const uint32_t lane = threadIdx.x & 63u, wave = uniform_u32(threadIdx.x >> 6), group = lane / 16u, r16 = lane & 15u;
@@ -834,7 +838,8 @@ __global__ __launch_bounds__(ADAPT_THREADS) void adapters_grad_kernel(AdaptersSu
     const float* s = of_a ? g.up : g.down;
     const uint64_t ld_s = of_a ? g.ld_up : g.ld_down;
     const uint32_t from = g.first[adapter], count = g.first[adapter + 1] - from;
-    const uint32_t each = ((count + g.parts - 1u) / g.parts + 15u) & ~15u, q0 = min(blockIdx.y * each, count), q1 = min(q0 + each, count);
+    const uint32_t q0 = min(blockIdx.y * g.rows_each, count), q1 = min(q0 + g.rows_each, count);
+    if (g.parts > 1 && q0 == q1) return;       // all wavefronts alike
     const uint32_t* list = g.rows + from;
     const bool codes = CODES && of_a, full = slab * ADAPT_SLAB + ADAPT_SLAB <= cols;
     const uint8_t* rows_x = static_cast<const uint8_t*>(of_a ? g.x : g.g);
@@ -844,7 +849,8 @@ __global__ __launch_bounds__(ADAPT_THREADS) void adapters_grad_kernel(AdaptersSu
         uint2 w[DEPTH];
         float p[DEPTH][RF], by[DEPTH];
     };
-    for (uint32_t rank0 = 0; rank0 < g.rank; rank0 += 16u * RF) {
+    {
+        const uint32_t rank0 = blockIdx.z * 16u * RF;
         v4f acc[RF][8];
 #pragma unroll
         for (uint32_t f = 0; f < RF; ++f)
@@ -934,10 +940,10 @@ __global__ __launch_bounds__(ADAPT_THREADS) void adapters_grad_kernel(AdaptersSu
                     for (uint32_t j = 0; j < 8; ++j) acc[f][j] += s_sum[wave][8 * f + j][lane];
             }
         }
-        if (wave != 0) continue;
+        if (wave != 0) return;
         // lane: ranks 4 group on, columns c on
         float* out = g.parts == 1 ? (of_a ? g.da : g.db) + (uint64_t)adapter * cols * g.rank
-                                  : g.partial + (((uint64_t)blockIdx.y * g.adapters + adapter) * (g.k + g.n) + (of_a ? 0 : g.k)) * g.rank;
+                                  : g.partial + ((part_of(from, adapter, g.rows_each) + blockIdx.y) * (g.k + g.n) + (of_a ? 0 : g.k)) * g.rank;
         typedef float loose __attribute__((ext_vector_type(4), aligned(4)));
 #pragma unroll
         for (uint32_t f = 0; f < RF; ++f) {
@@ -975,25 +981,30 @@ __global__ __launch_bounds__(ADAPT_THREADS) void adapters_grad_kernel(AdaptersSu
     }
 }
 
-// The parts' sums of all adapters, in order.
+// The parts' sums of all adapters, in order; 0 for an adapter without rows.
 __global__ __launch_bounds__(ADAPT_THREADS) void adapters_join_kernel(AdaptersSumArgs g) {
-    const uint64_t of_a = (uint64_t)g.k * g.rank, each = of_a + (uint64_t)g.n * g.rank, all = each * g.adapters;
-    for (uint64_t u = (uint64_t)blockIdx.x * ADAPT_THREADS + threadIdx.x; u < all; u += (uint64_t)gridDim.x * ADAPT_THREADS) {
-        float v = g.partial[u];
-        for (uint32_t p = 1; p < g.parts; ++p) v += g.partial[(uint64_t)p * all + u];
-        const uint64_t i = u / each, at = u - i * each;
-        if (at < of_a) g.da[i * of_a + at] = v;
-        else g.db[i * (each - of_a) + at - of_a] = v;
+    const uint64_t of_a = (uint64_t)g.k * g.rank, each = of_a + (uint64_t)g.n * g.rank;
+    const uint32_t adapter = blockIdx.y, from = g.first[adapter], count = g.first[adapter + 1] - from, parts = (count + g.rows_each - 1u) / g.rows_each;
+    const float* p = g.partial + part_of(from, adapter, g.rows_each) * each;
+    for (uint64_t u = (uint64_t)blockIdx.x * ADAPT_THREADS + threadIdx.x; u < each; u += (uint64_t)gridDim.x * ADAPT_THREADS) {
+        float v = 0.0f, w[4];
+        for (uint32_t i0 = 0; i0 < parts; i0 += 4) {
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i)
+                if (i0 + i < parts) w[i] = p[(i0 + i) * each + u];
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i)
+                if (i0 + i < parts) v += w[i];
+        }
+        if (u < of_a) g.da[adapter * of_a + u] = v;
+        else g.db[adapter * (each - of_a) + u - of_a] = v;
     }
 }
 
 template <typename T, bool CODES>
 static void launch_sums_as(shifter_ctx* ctx, const AdaptersSumArgs& g) {
-    const dim3 grid(((g.k + ADAPT_SLAB - 1u) / ADAPT_SLAB + (g.n + ADAPT_SLAB - 1u) / ADAPT_SLAB) * g.adapters, g.parts);
-    const uint64_t pad = adapt_pad(g.rank);
-    if (pad <= 16) adapters_grad_kernel<T, CODES, 1><<<grid, ADAPT_THREADS, 0, ctx->stream>>>(g);
-    else if (pad <= 32) adapters_grad_kernel<T, CODES, 2><<<grid, ADAPT_THREADS, 0, ctx->stream>>>(g);
-    else adapters_grad_kernel<T, CODES, 4><<<grid, ADAPT_THREADS, 0, ctx->stream>>>(g);
+    const dim3 grid(((g.k + ADAPT_SLAB - 1u) / ADAPT_SLAB + (g.n + ADAPT_SLAB - 1u) / ADAPT_SLAB) * g.adapters, g.parts, (uint32_t)adapt_pad(g.rank) / 16u);
+    adapters_grad_kernel<T, CODES, 1><<<grid, ADAPT_THREADS, 0, ctx->stream>>>(g);
 }
 
 template <typename T>
@@ -1036,14 +1047,15 @@ static void launch_gradients(shifter_ctx* ctx, int dtype, const AdaptersGradArgs
     AdaptersSumArgs s{};
     s.x = g.x; s.ld_x = g.ld_x; s.x_scale = g.x_scale; s.g = g.g; s.ld_g = g.ld_g;
     s.up = u.down; s.ld_up = pad; s.down = down; s.ld_down = ld_down;
-    s.rows = t.rows; s.first = t.first; s.n = g.n; s.k = g.k; s.rank = g.rank; s.adapters = g.adapters; s.parts = p.parts_rows;
+    s.rows = t.rows; s.first = t.first; s.n = g.n; s.k = g.k; s.rank = g.rank; s.adapters = g.adapters; s.parts = p.parts_rows; s.rows_each = p.rows_each;
     s.da = g.da; s.db = g.db; s.partial = reinterpret_cast<float*>(at(p.partial));
     ProfileScope ps(ctx, K_ADAPTERS_GRAD);
     if (g.x_scale) launch_sums_as<T, true>(ctx, s);
     else launch_sums_as<T, false>(ctx, s);
     if (s.parts > 1) {
-        const uint64_t all = (uint64_t)g.adapters * (g.k + g.n) * g.rank;
-        adapters_join_kernel<<<(uint32_t)std::min<uint64_t>((all + ADAPT_THREADS - 1u) / ADAPT_THREADS, 4096), ADAPT_THREADS, 0, ctx->stream>>>(s);
+        const uint64_t each = (uint64_t)(g.k + g.n) * g.rank;
+        const dim3 grid((uint32_t)std::min<uint64_t>((each + ADAPT_THREADS - 1u) / ADAPT_THREADS, 1024), g.adapters);
+        adapters_join_kernel<<<grid, ADAPT_THREADS, 0, ctx->stream>>>(s);
     }
 }
 

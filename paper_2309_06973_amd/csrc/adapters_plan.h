@@ -9,6 +9,7 @@ namespace shifter {
 constexpr uint32_t ADAPT_MAX_RANK = 128;
 constexpr uint64_t ADAPT_MAX_ROWS = 1ull << 25;    // tiles of 16 rows, up to four blocks of 256 threads each: less than 2^32 threads
 constexpr uint64_t ADAPT_SORT_FROM = 8, ADAPT_SORT_MOST = 4094;
+constexpr uint64_t ADAPT_FEW_ADAPTERS = 8;
 constexpr uint32_t ADAPT_STEP = 64;                // columns of a step of the products over long rows
 constexpr uint64_t ADAPT_FEW_ROWS = 256, ADAPT_TWO_TILES = 2048;
 constexpr uint32_t ADAPT_MANY_ROWS_PARTS = 2;      // with more rows, their product with B holds so many in registers
@@ -58,12 +59,12 @@ inline AdaptersPlan adapters_plan(uint64_t m, uint64_t k, uint32_t rank, uint64_
 // The gradient's workspace: offsets of its pieces.
 struct AdaptersGradPlan {
     uint32_t parts_x, parts_g;         // of x A' and of g B
-    uint32_t parts_rows;               // blocks that share an adapter's rows
+    uint32_t parts_rows, rows_each;    // blocks that share an adapter's rows, if it has them all; rows of one
     uint64_t down, up;                 // [m][pad]: x A' where it is not given, and g B
     uint64_t sums;                     // [parts][m][pad]
     uint64_t a, b;                     // the adapters, turned: [adapters][k][rank], [adapters][rank][n]
     uint64_t rows, first;              // rows sorted by their adapter; each adapter's first, and the number of all
-    uint64_t partial;                  // [parts_rows][adapters][k + n][rank]
+    uint64_t partial;                  // [parts_rows + adapters][k + n][rank]: see adapters_grad_kernel
     uint64_t bytes;
 };
 inline AdaptersGradPlan adapters_grad_plan(uint64_t m, uint64_t n, uint64_t k, uint32_t rank, uint64_t adapters, uint64_t size) {
@@ -71,10 +72,12 @@ inline AdaptersGradPlan adapters_grad_plan(uint64_t m, uint64_t n, uint64_t k, u
     const uint64_t pad = adapt_pad(rank);
     p.parts_x = adapt_parts(m, k, rank);
     p.parts_g = adapt_parts(m, n, rank);
-    const uint64_t slabs = ((k + ADAPT_SLAB - 1u) / ADAPT_SLAB + (n + ADAPT_SLAB - 1u) / ADAPT_SLAB) * (adapters ? adapters : 1u);
+    // Few adapters may have any share of the rows: as many parts as would do for one that has all.
+    const uint64_t slabs = ((k + ADAPT_SLAB - 1u) / ADAPT_SLAB + (n + ADAPT_SLAB - 1u) / ADAPT_SLAB) * (adapters > ADAPT_FEW_ADAPTERS ? adapters : 1u);
     uint64_t parts = slabs ? 512u / slabs : 1u;
-    if (parts > m / 64u) parts = m / 64u;
-    p.parts_rows = parts < 1 ? 1u : parts > 16 ? 16u : (uint32_t)parts;
+    parts = std::max<uint64_t>(1u, std::min<uint64_t>({parts, m / 64u, 16u}));
+    p.rows_each = (uint32_t)((((m + parts - 1u) / parts) + 15u) & ~15ull);
+    p.parts_rows = m ? (uint32_t)((m + p.rows_each - 1u) / p.rows_each) : 1u;
     uint64_t at = 0;
     auto take = [&](uint64_t bytes) {
         const uint64_t was = at;
@@ -88,7 +91,7 @@ inline AdaptersGradPlan adapters_grad_plan(uint64_t m, uint64_t n, uint64_t k, u
     p.b = take(adapters * n * rank * size);
     p.rows = take(4u * m);
     p.first = take(4u * (adapters + 2u));
-    p.partial = take(p.parts_rows > 1 ? p.parts_rows * adapters * (k + n) * rank * 4u : 0u);
+    p.partial = take(p.parts_rows > 1 ? (p.parts_rows + adapters) * (k + n) * rank * 4u : 0u);
     p.bytes = at;
     return p;
 }

@@ -105,7 +105,7 @@ struct AdaptersSumArgs {
     uint64_t ld_x, ld_g, ld_up, ld_down;
     const uint32_t *rows, *first;
     float *da, *db, *partial;
-    uint32_t n, k, rank, adapters, parts;
+    uint32_t n, k, rank, adapters, parts, rows_each;
 };
 
 }  // namespace shifter
