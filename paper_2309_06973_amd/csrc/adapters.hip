@@ -119,7 +119,7 @@ __device__ __forceinline__ bool adapter_of_job(int id, uint32_t job, int* which)
 // theirs: a tile of several would take several times as long as the others, and the kernel with it (prompts of 8192 rows with five
 // borders 21 us for 13).
 template <typename T, bool CODES, uint32_t RF, uint32_t RT>
-__global__ __launch_bounds__(ADAPT_THREADS) void adapters_down_kernel(AdaptersDownArgs g) {
+__global__ __launch_bounds__(ADAPT_THREADS, RT * RF > 2 ? 2 : 3) void adapters_down_kernel(AdaptersDownArgs g) {
     __shared__ v4f s_sum[ADAPT_WAVES][RF * RT][64];
     const uint32_t lane = threadIdx.x & 63u, wave = uniform_u32(threadIdx.x >> 6), col = (CODES ? 16u : 8u) * (lane / 16u), r16 = lane & 15u;
     constexpr uint32_t APART = CODES ? 8 : 32;
@@ -316,6 +316,11 @@ struct SPieces {
 // n of four elements at p, zeros behind them.
 template <bool EVEN, typename T>
 __device__ __forceinline__ void four_of(const T* p, int32_t n, uint32_t (&w)[sizeof(T)]) {
+    if (!EVEN) {
+#pragma unroll
+        for (uint32_t i = 0; i < sizeof(T); ++i) w[i] = 0u;
+        if (n <= 0) return;
+    }
     if (EVEN || n >= 4) {
         typedef T vec __attribute__((ext_vector_type(4), aligned(sizeof(T))));
         const vec v = *reinterpret_cast<const vec*>(p);
@@ -472,7 +477,7 @@ __device__ __forceinline__ void keep_down(const AdaptersUpArgs& g, uint64_t row,
 
 // A tile of rows for each block, whose wavefronts take 64 columns in turn: for few rows, and for ranks above 32.  s is in LDS.
 template <typename T, typename Y, bool JOBS, bool EVEN>
-__global__ __launch_bounds__(ADAPT_THREADS) void adapters_up_kernel(AdaptersUpArgs g) {
+__global__ __launch_bounds__(ADAPT_THREADS, 3) void adapters_up_kernel(AdaptersUpArgs g) {
     extern __shared__ __align__(16) float s_rows[];        // [16][pad + 4]
     const UpTile<T, Y> tile;
     const uint32_t wave = uniform_u32(threadIdx.x >> 6);
@@ -538,7 +543,7 @@ __global__ __launch_bounds__(ADAPT_THREADS) void adapters_up_kernel(AdaptersUpAr
 // adapter; the next tile's s and y are on their way meanwhile.  Nothing in the loop of a full tile of one adapter is in a lane's branch: with
 // the ends of rows and columns looked after there, prompts of 8192 rows took 46 us.
 template <typename T, typename Y, uint32_t NF, bool EVEN>
-__global__ __launch_bounds__(ADAPT_THREADS) void adapters_up_rows_kernel(AdaptersUpArgs g) {
+__global__ __launch_bounds__(ADAPT_THREADS, 3) void adapters_up_rows_kernel(AdaptersUpArgs g) {
     constexpr uint32_t PAD = 16 * NF;
     const UpTile<T, Y> tile;
     const uint32_t n0 = (blockIdx.x * ADAPT_WAVES + uniform_u32(threadIdx.x >> 6)) * 64u;
