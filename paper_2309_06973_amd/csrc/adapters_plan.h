@@ -104,7 +104,7 @@ inline const char* adapters_bad_sizes(uint64_t m, uint64_t n, uint64_t k, uint64
     *capacity = true;
     if (m > ADAPT_MAX_ROWS) return "more than 2^25 rows";
     // the gradient's blocks of 64 columns of all adapters, 256 threads each
-    if (adapters * (1u + (k + 63u) / 64u + (n + 63u) / 64u) >= 1ull << 24) return "more columns of all adapters than a launch holds";
+    if (adapters * (1u + (k + 63u) / 64u + (n + 63u) / 64u) + 1u >= 1ull << 24) return "more columns of all adapters than a launch holds";
     *capacity = false;
     return nullptr;
 }

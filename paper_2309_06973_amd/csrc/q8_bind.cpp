@@ -468,7 +468,7 @@ PyObject* log_probs(PyObject* const* a) {
     check(shifter_log_probs_layout(g.rows, g.cols, g.top, &g.work_bytes), Py_None);
     const Work work(a[7], g.work_bytes);
     g.d_work = work.p;
-    enqueue(a[0], [&] { return shifter_log_probs(h.ctx, &g); });
+    check(shifter_log_probs(h.ctx, &g), a[0]);     // with the interpreter's lock: calls of several launches have the same workspace
     Owned all(PyTuple_New(6));
     for (int i = 0; i < 6; ++i) {
         if (!out[i].defined()) {

@@ -125,13 +125,15 @@ class Q8:
         """The same for the calls that find zeros at its front and leave zeros there: none else may write it."""
         recording = torch.cuda.is_current_stream_capturing()
         work = (self.recorded_joined[-1] if self.recorded_joined else None) if recording else self.joined
-        if work is None or work.numel() < need:
+        new = work is None or work.numel() < need
+        if new:
             work = torch.empty(need, dtype=torch.uint8, device=self.dev)
-            work[:S.SHIFTER_LEARN_ZERO].zero_()            # a kernel; recorded too, and replayed before the call that needs it
             if recording:
                 self.recorded_joined.append(work)
             else:
                 self.joined = work
+        if new or recording:           # recorded with each call: what a capture records is not done, and any graph may be replayed first
+            work[:S.SHIFTER_LEARN_ZERO].zero_()
         return work
 
     # ---- the operators --------------------------------------------------------------

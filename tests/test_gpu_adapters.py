@@ -117,6 +117,28 @@ def test_gradients(ops, which, dtype, codes):
         assert none is None and torch.equal(da, da2) and torch.equal(db, db2)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m, n, k, rank, adapters", [(257, 70, 64, 16, 8), (600, 200, 150, 16, 9), (3000, 130, 70, 20, 40), (2048, 64, 65, 32, 300), (9001, 65, 40, 8, 12),
+                                                    (700, 300, 33, 50, 4094), (700, 300, 33, 12, 4095)])
+def test_rows_in_the_order_of_their_adapters(ops, m, n, k, rank, adapters, dtype):
+    """More rows than a wavefront's tiles for each of many adapters, forward and back; more rows than the order's block holds."""
+    for pattern, codes in (("random", False), ("runs", True), ("one", False), ("none", False)):
+        print(f"in order m={m} n={n} k={k} rank={rank} adapters={adapters} {dtype} codes={codes} {pattern}", flush=True)
+        y, x, values, a, b, num, scale = setup(ops, m, n, k, rank, adapters, dtype, pattern, codes)
+        num[3] = adapters                    # names none
+        ref = L.Adapters(y, values, a, b, num, scale)
+        down = torch.full((m, rank), 9.0, device=DEV)
+        out = ops.adapters(y, x, a, b, num, scale=scale, down=down)
+        near(out, ref.out, ref.off, dtype, "out")
+        near(down, ref.down, ref.off_down, torch.float32, "down")
+        z = y.clone()
+        assert torch.equal(ops.adapters(z, x, a, b, num, scale=scale, out=z)[num < adapters], out[num < adapters])
+        g = rand(m, n, dtype=dtype, seed=9)
+        for kept in (down, None):
+            for name, got, t in zip(("dx", "da", "db"), ops.adapters_grad(g, x, a, b, num, scale=scale, down=kept), (dtype, torch.float32, torch.float32)):
+                near(got, *ref.grads(g)[name], t, name)
+
+
 def test_no_rows_and_no_columns(ops):
     for m, n, k, adapters in ((0, 5, 7, 2), (3, 0, 7, 2), (3, 5, 0, 2), (3, 5, 7, 0), (0, 0, 0, 0)):
         y, x, a, b = torch.ones(m, n, device=DEV), torch.ones(m, k, device=DEV), torch.ones(adapters, 4, k, device=DEV), torch.ones(adapters, n, 4, device=DEV)
@@ -257,12 +279,13 @@ def test_second_derivative_and_lost_gradients(ops):
         adapted(y, x, a, b, num[:3], ops)
 
 
-def test_recorded(ops):
+@pytest.mark.parametrize("many", [5, 20])
+def test_recorded(ops, many):
     stream = torch.cuda.Stream()
     stream.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(stream):
         own = Q8()
-        y, x, _, a, b, num, scale = setup(own, 300, 500, 700, 16, 5, torch.bfloat16, "random")
+        y, x, _, a, b, num, scale = setup(own, 300, 500, 700, 16, many, torch.bfloat16, "random")
         g = rand(300, 500, dtype=torch.bfloat16, seed=5)
         down = torch.empty(300, 16, device=DEV)
         own.adapters_grad(g, x, a, b, num)
@@ -276,7 +299,7 @@ def test_recorded(ops):
             graphs.append((graph, (out, *grads)))
         for i in range(4):
             x.copy_(rand(300, 700, dtype=torch.bfloat16, seed=30 + i))
-            num.copy_(numbers(300, 5, "random", 40 + i))
+            num.copy_(numbers(300, many, "random", 40 + i))
             for graph, got in graphs:
                 for t in got:
                     t.fill_(3.0)

@@ -178,6 +178,7 @@ def test_recorded(ops):
         for i in range(4):
             for x in grads:
                 x.mul_(1.5).add_(0.25)
+            graphs.reverse()                       # the one recorded last is replayed first
             for g, norm in graphs:
                 for o in out:
                     o.fill_(9.0)

@@ -287,6 +287,7 @@ def test_recorded(ops):
                 d = own.log_probs_grad(x, t, r.norm, g_logp=one)
             graphs.append((g, r, d))
         for i in range(4):
+            graphs.reverse()                       # the one recorded last is replayed first
             y = make(3, 50001, torch.bfloat16, 20 + i)
             x.copy_(y)
             want = own.log_probs(x, t, entropy=True, top=20)
