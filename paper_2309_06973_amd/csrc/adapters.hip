@@ -7,7 +7,11 @@
 //
 // Rows are taken in tiles of 16 as they come, whatever requests they belong to: a tile is multiplied with each adapter that
 // one of its rows has, and each row keeps the result of its own.  So rows need no sorting, a run of rows of one request costs
-// one product, and nothing that one request's adapter holds, infinities and NaN too, reaches another's rows.
+// one product, and nothing that one request's adapter holds, infinities and NaN too, reaches another's rows.  More rows of many adapters are put
+// in the adapters' order first, as a list that the kernels go by: nothing is moved.
+//
+// 8192 rows of 4096 in 8 bits to 4096 in bf16, rank 16, six runs: 50 to 52 us, of which the product over long rows takes 16 (34 MB; 11 for
+// one adapter) and the one with B 30 (134 MB, 4.5 TB/s).  One row: two launches, 3.7 and 4.6 us.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -113,8 +117,9 @@ __device__ __forceinline__ bool adapter_of_job(int id, uint32_t job, int* which)
 
 // s[part][r] = c_i x_r A_i' over the part's columns; 0 for a row without an adapter, NaN for one whose adapter there is not.
 // A block has RT tiles of 16 rows and 16 RF ranks; its wavefronts take steps of 64 columns in turn and join their sums.  Both factors
-// come straight from memory into the operands: a lane has twice eight columns, so that four lanes read 64 bytes of a row side by side (the
-// 16 codes of a lane are one read, and its columns of A lie as they do).
+// come straight from memory into the operands (a lane has twice eight columns, so that four lanes read 64 bytes of a row side by side; the
+// 16 codes of a lane are one read, and its columns of A lie as they do).  16 rows by 64 bytes are read at a time, 128 to 256 bytes of a row by
+// the block: 8192 x 4096 bf16 with one adapter 17 us, 4 TB/s, as long as a library product of that shape (20).
 // Blocks share the adapters of a tile's rows (g.jobs of them; of a tile of one adapter all but one end at once), and write the rows of
 // theirs: a tile of several would take several times as long as the others, and the kernel with it (prompts of 8192 rows with five
 // borders 21 us for 13).
@@ -748,7 +753,9 @@ void launch_adapters(shifter_ctx* ctx, int dtype, int y_dtype, const AdaptersArg
 //   up_r = c_i g_r B_i,   dx_r = up_r A_i,   dA_i = sum up_r' x_r,   dB_i = sum g_r' down_r   (down_r = c_i x_r A_i')
 //
 // up and dx are the products above with the adapters turned.  The sums over rows take fp32 products as well: both factors are rows as they
-// lie, a lane's eight neighbouring columns are one operand of eight products.
+// lie, a lane's eight neighbouring columns are one operand of eight products.  A training step of 4096 x 2048 x 2048 with rank 32 and three
+// adapters, forward and back, is seven launches, 88 us: the products over long rows 2 x 11, with A and B 2 x 16, turning 9, the sums over rows 24 and
+// their join 4.
 
 // Blocks up to `adapters`: the rows of an adapter in order, behind those of the ones before it; at the end those of none.  Further ones turn 64 columns of an
 // adapter: A [rank][k] to [k][rank], or B [n][rank] to [rank][n].

@@ -8,17 +8,27 @@ namespace shifter {
 
 constexpr uint32_t ADAPT_MAX_RANK = 128;
 constexpr uint64_t ADAPT_MAX_ROWS = 1ull << 25;    // tiles of 16 rows, up to four blocks of 256 threads each: less than 2^32 threads
+// From so many adapters on (up to those that fit the block's LDS) more than a few rows are put in order first, whatever order they have.  us of
+// 8192 rows, 4096 x 4096 with rank 16, in order / as they come: 4 adapters of random rows 77 / 101, of runs 70 / 59; 8: 79 / 160, 73 / 62;
+// 16: 81 / 260, 79 / 63.
 constexpr uint64_t ADAPT_SORT_FROM = 8, ADAPT_SORT_MOST = 4094;
+// Up to so many adapters the gradient's sums over rows are cut into parts as if one adapter had all the rows; beyond, as if all had as many.
+// us of a training step of 4096 x 2048 x 2048 with rank 32, as one / as all: 3 adapters 87 / 94, 8 98 / 121, 16 110 / 109, 32 134 / 106.
 constexpr uint64_t ADAPT_FEW_ADAPTERS = 8;
 constexpr uint32_t ADAPT_STEP = 64;                // columns of a step of the products over long rows
-constexpr uint64_t ADAPT_FEW_ROWS = 256, ADAPT_TWO_TILES = 2048;
+// Up to ADAPT_FEW_ROWS rows each adapter of a tile has blocks of its own; beyond, tiles are taken with all of theirs, or in the order of the
+// adapters.  us of 4096 x 4096 with rank 16, apart / together: 256 rows of 32 adapters as they come 33.7 / 20.2, 1024 of them 83 / 19.3;
+// 256 rows in six runs 10.2 / 11.8, 1024 16.7 / 13.7.
+// From ADAPT_TWO_TILES rows on a block has two tiles of the product over long rows (1024 rows in three runs, one tile / two: 13.9 / 17.4,
+// 2048 20.1 / 19.4, 4096 34.3 / 31.5).
+constexpr uint64_t ADAPT_FEW_ROWS = 128, ADAPT_TWO_TILES = 2048;
 constexpr uint32_t ADAPT_MANY_ROWS_PARTS = 2;      // with more rows, their product with B holds so many in registers
-constexpr uint32_t ADAPT_UP_BLOCKS = 2048;         // of the product with B, as far as there are columns
+constexpr uint32_t ADAPT_UP_BLOCKS = 2048;         // of the product with B, as far as there are columns (1024 and 4096: within 4 %)
 constexpr uint32_t ADAPT_SLAB = 128;               // columns of a block of the gradient's sums over rows
 
 inline uint64_t adapt_pad(uint64_t rank) { return (rank + 15u) & ~15ull; }
 
-// Tiles of 16 rows that a block works on together: they share what it reads of an adapter.
+// Tiles of 16 rows that a block works on together: they share what it reads of an adapter.  (Two tiles of 64 ranks do not fit the registers.)
 inline uint32_t adapt_tiles(uint64_t m, uint32_t rank) { return adapt_pad(rank) > 32 || m < ADAPT_TWO_TILES ? 1u : 2u; }
 
 // Blocks that share a tile of few rows, one for each adapter that its rows may have.
@@ -31,7 +41,7 @@ inline uint32_t adapt_down_jobs(uint64_t m, uint64_t adapters) {
     return m <= ADAPT_FEW_ROWS ? adapt_jobs(m, adapters) : adapters >= 2 ? 2u : 1u;
 }
 
-// Whether the rows are put in order of their adapters first: one more launch, of 6 to 9 us, where tiles of rows as they come could have many.
+// Whether the rows are put in order of their adapters first: one more launch, of 6 to 11 us, where tiles of rows as they come could have many.
 inline bool adapt_sorted(uint64_t m, uint64_t adapters) { return m > ADAPT_FEW_ROWS && adapters >= ADAPT_SORT_FROM && adapters <= ADAPT_SORT_MOST; }
 
 // Blocks that share the k columns of a tile's rows; each leaves its sums.

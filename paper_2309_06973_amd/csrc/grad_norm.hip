@@ -4,7 +4,10 @@
 // Two streaming passes, a launch each (for up to GRAD_LIST tensors).  Squares are summed in 64 bits: no square overflows or is lost, and a
 // sum's error is far below the one rounding of the result, whatever the order.  The order is fixed all the same: each block
 // leaves the sum of its chunks, and the last block of the launch adds those up.  The second pass takes the chunks from the
-// last to the first, so that what the first pass left in the last-level cache (256 MB) is read from there.
+// last to the first, so that what the first pass left in the last-level cache (256 MB) is read from there.  268 M fp32 in 17 tensors
+// to others: 212 + 424 us, 3.2 GB at 5.0 TB/s, a large copy's rate; 25.5 M fp32 in 161 with masks 43 + 42 us (127 and 229 MB, from memory,
+// which holds other tensors' results in its cache still).  512 blocks with long runs: with 2048 the search for a block's first tensor and its
+// ends cost as much as its elements (161 tensors 90 us for 85).
 #include <cmath>
 #include <type_traits>
 

@@ -1,4 +1,4 @@
-// What a network is trained on and answers with: what the host hands to the kernels.
+// Log probabilities, gradient norms and adapters: what the host hands to the kernels.
 #pragma once
 
 #include "internal.h"

@@ -1,4 +1,4 @@
-// The 8-bit operators from Python: checks of tensors, new results and the call into the C ABI.
+// The 8-bit operators and those beside them from Python: checks of tensors, new results and the call into the C ABI.
 //
 // A call's kernel takes a few microseconds, as much as a handful of calls into torch from Python:
 // 1 x 2048 bf16, us a call with all this in Python and ctypes / here: quantise 7.7 / 4.0, read back 6.4 / 4.0, norm

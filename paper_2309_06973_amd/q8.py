@@ -1,5 +1,7 @@
 """8-bit matrices next to the prune-and-compact pass: a rebuilt variant's linear layers served
-in 8 bits, and 8-bit activations kept for the backward pass while a masked network trains on.
+in 8 bits, and 8-bit activations kept for the backward pass while a masked network trains on.  Beside
+them, what such a network is trained on and answers with: log probabilities and their gradient, the norm of
+all gradients and their clipping, and low-rank adapters of many requests with their gradients.
 
 Every step runs in libshifter's HIP kernels on the stream that was current when the handle (or
 the context that it was given) was made; a call's checks, its new tensors and the way into the C ABI are _q8.so's (csrc/q8_bind.cpp).
@@ -69,17 +71,17 @@ def load_calls():
 
 
 class Q8:
-    """The 8-bit operators on one device and stream: the current one, or those of a given context.
+    """The 8-bit operators and those beside them on one device and stream: the current one, or those of a given context.
     Matrices of elements are two-dimensional fp32, bf16 or fp16 tensors whose columns lie side by
     side; their rows may have any stride.
     Results are new tensors unless ``out`` (or ``h``) says where they go.  Gradients are not passed
     on: 8-bit matrices are constants to autograd, and a new tensor made from elements that need a
     gradient (x and residual of a norm, a bias, g) has an error for its backward pass.  With ``out``
-    or ``h`` such elements are refused, unless under torch.no_grad().
+    or ``h`` such elements are refused, unless under torch.no_grad().  The module's functions do pass gradients on.
 
     Recorded into a graph, calls of one handle share a workspace apart from that of calls made at
     once: replays of such graphs go one after another, on whatever stream.  The handle is one host
-    thread's at a time, as the C interface asks for; the launches of a weight_grad, which share the
+    thread's at a time, as the C interface asks for; the launches of a call that has several, which share a
     workspace, follow one another whatever other threads call (autograd runs backward passes on
     threads of its own)."""
 

@@ -232,17 +232,17 @@ def test_adapters_workspaces(plan):
     rng = random.Random(5)
     size = lambda most: int(2 ** rng.uniform(0, most))
     sizes = [(size(20), size(14), size(14), rng.randint(1, 128), rng.choice([1, 2, 7, 8, 64, 500])) for _ in range(1500)]
-    sizes += [(m, 4096, 4096, 16, a) for m in (1, 16, 255, 256, 257, 2047, 2048, 8192) for a in (1, 7, 8, 4094, 4095)]
+    sizes += [(m, 4096, 4096, 16, a) for m in (1, 16, 127, 128, 129, 256, 2047, 2048, 8192) for a in (1, 7, 8, 4094, 4095)]
     for (m, n, k, rank, many), line in zip(sizes, plan("a", [x for s in sizes for x in s])):
         if line == "bad":
             assert many * (1 + up(k, 64) + up(n, 64)) >= 1 << 24
             continue
         parts, total, tiles, jobs, down_jobs, order, ordered, px, pg, pr, each, down, over, sums, a, b, rows, partial, everything = map(int, line.split())
         pad = up(rank, 16) * 16
-        assert order >= parts * m * pad * 4 and total >= order + (4 * m if ordered else 0) and 1 <= parts <= (32 if m <= 256 else 2)
-        assert parts <= max(1, up(k, 64)) and px == parts and ordered == (m > 256 and 8 <= many <= 4094)
+        assert order >= parts * m * pad * 4 and total >= order + (4 * m if ordered else 0) and 1 <= parts <= (32 if m <= 128 else 2)
+        assert parts <= max(1, up(k, 64)) and px == parts and ordered == (m > 128 and 8 <= many <= 4094)
         # a tile of few rows: no more adapters than blocks that share it
-        assert jobs == (1 if m > 256 else max(1, min(16, m, many))) and (m > 256 or down_jobs == jobs) and tiles in (1, 2)
+        assert jobs == (1 if m > 128 else max(1, min(16, m, many))) and (m > 128 or down_jobs == jobs) and tiles in (1, 2)
         assert (tiles == 1 or rank <= 32) and up(m, 16 * tiles) * 256 < 1 << 32
         assert each % 16 == 0 and pr == max(1, up(m, each)) and pr <= 16
         # pieces one behind the other
