@@ -762,7 +762,7 @@ int shifter_weight_grad_q8(shifter_ctx* ctx, const void* d_g, int dtype, uint64_
  *                                   SHIFTER_LOG_PROBS_MAX_TOP and up to cols.
  *                        A logit of minus infinity has probability 0 and adds nothing to the entropy.  A row with NaN or
  *                        +infinity has NaN everywhere; one that is minus infinity throughout has lse minus infinity and NaN
- *                        elsewhere; columns and what is left out stay as above.  scale is finite and positive.
+ *                        elsewhere; columns and what is left out stay as above.  scale is positive, up to 2^64.
  *                        d_work: work_bytes of shifter_log_probs_layout, NULL where that says 0; see below.
  * shifter_log_probs_grad dx = scale (g_logp ([column = target] - p) + g_lse p - g_entropy p (log p + entropy)), rounded to
  *                        x's type, from the gradients of the outputs above (rows each; NULL: none) and norm and entropy as
@@ -780,7 +780,7 @@ int shifter_weight_grad_q8(shifter_ctx* ctx, const void* d_g, int dtype, uint64_
  *                        Tensors are runs of elements of any start, with types of their own; h_grads is a host array that is
  *                        not used after the call returns.  d_out is not read by shifter_grad_norm.
  *
- * shifter_adapters       out_r = y_r + scale[i] (x_r A_i') B_i', i = d_which[r], rounded once to y's type: A (adapters x rank x k) and
+ * shifter_adapters       out_r = y_r + scale[i] (x_r A_i') B_i', i = d_which[r], rounded to y's type: A (adapters x rank x k) and
  *                        B (adapters x n x rank) lie without gaps and have x's element type; x is elements, or an 8-bit
  *                        matrix (d_q_scale not NULL: d_x are its codes, ld_x its stride).  A row whose number is negative
  *                        has no adapter: out_r is y_r; one whose number is not below `adapters` is NaN.  d_scale NULL: 1.

@@ -1826,7 +1826,7 @@ static const char* log_probs_bad_sizes(uint64_t rows, uint64_t cols, uint64_t to
     if (top > cols) return "more alternatives than columns";
     return nullptr;
 }
-static bool bad_scale(float scale) { return !(scale > 0.0f) || !std::isfinite(scale); }
+static bool bad_scale(float scale) { return !(scale > 0.0f && scale <= 0x1p64f); }
 
 extern "C" int shifter_log_probs_layout(uint64_t rows, uint64_t cols, uint32_t top, uint64_t* h_work_bytes) {
     if (!h_work_bytes) return fail(nullptr, SHIFTER_ERR_INVALID_ARG, "log_probs_layout: NULL argument");
@@ -1843,7 +1843,7 @@ extern "C" int shifter_log_probs(shifter_ctx* ctx, const shifter_log_probs_args*
     if (rc) return rc;
     Q8_REFUSE("log_probs", log_probs_bad_sizes(a->rows, a->cols, a->top));
     Q8_REFUSE("log_probs", q8_bad_rows(a->d_x, element_size(a->dtype), a->rows, a->cols, a->ld_x));
-    if (bad_scale(a->scale)) return fail(ctx, SHIFTER_ERR_INVALID_ARG, "log_probs: scale must be finite and positive");
+    if (bad_scale(a->scale)) return fail(ctx, SHIFTER_ERR_INVALID_ARG, "log_probs: scale must be positive, up to 2^64");
     if (a->rows == 0) return SHIFTER_OK;
     if (!a->d_norm || !a->d_lse || (a->d_target && !a->d_logp) || (a->top && (!a->d_top || !a->d_index)))
         return fail(ctx, SHIFTER_ERR_INVALID_ARG, "log_probs: NULL pointer argument");
@@ -1872,7 +1872,7 @@ extern "C" int shifter_log_probs_grad(shifter_ctx* ctx, const shifter_log_probs_
     const uintptr_t size = element_size(a->dtype);
     Q8_REFUSE("log_probs_grad", q8_bad_rows(a->d_x, size, a->rows, a->cols, a->ld_x));
     Q8_REFUSE("log_probs_grad", q8_bad_rows(a->d_dx, size, a->rows, a->cols, a->ld_dx));
-    if (bad_scale(a->scale)) return fail(ctx, SHIFTER_ERR_INVALID_ARG, "log_probs_grad: scale must be finite and positive");
+    if (bad_scale(a->scale)) return fail(ctx, SHIFTER_ERR_INVALID_ARG, "log_probs_grad: scale must be positive, up to 2^64");
     if (a->d_dx == a->d_x && a->ld_dx != a->ld_x && a->rows > 1 && a->cols)
         return fail(ctx, SHIFTER_ERR_INVALID_ARG, "log_probs_grad: d_dx is d_x with another stride");
     if (a->rows == 0 || a->cols == 0) return SHIFTER_OK;

@@ -17,7 +17,7 @@ constexpr uint64_t LEARN_TICKETS = 4 * LOGP_SHARED_ROWS;
 constexpr uint64_t LOGP_MAX_BLOCKS = 1u << 21;     // a launch holds less than 2^32 threads; blocks take further rows in turn
 
 struct LogProbsPlan {
-    uint32_t threads;      // of a row's part: 16 or 64, several rows a block; 256 or 1024, a block
+    uint32_t threads;      // of a row's part: 16 or 64, several rows a block; 256, a block
     uint32_t parts;        // blocks that share a row; the last of them joins their sums
     uint32_t part_cols;    // columns of a part, a multiple of 8
     uint64_t bytes;        // of the workspace, 0: none needed

@@ -171,7 +171,7 @@ class Q8:
         """Of each row z = scale * x: log sum exp z, the log probability of column target[row] (int64; 0 where
         it is negative, NaN where it is not below the columns), the entropy, and the ``top`` largest log
         probabilities (up to SHIFTER_LOG_PROBS_MAX_TOP; equal logits: the lower column first) with their columns.  All
-        numbers are fp32.  Minus infinity has probability 0; a row with NaN or infinity is NaN."""
+        numbers are fp32.  Minus infinity has probability 0; a row with NaN or infinity is NaN.  scale: above 0, up to 2^64."""
         return LogProbs(*self._calls.log_probs(*self._enter(), x, target, scale, entropy, top, self._joined))
 
     def log_probs_grad(self, x: torch.Tensor, target: Optional[torch.Tensor], norm: torch.Tensor,

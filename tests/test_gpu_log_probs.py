@@ -327,7 +327,8 @@ def test_what_the_interface_refuses(ops):
     work = torch.zeros(need, dtype=torch.uint8, device=DEV)
     for change, what in ((dict(), "workspace too small"), (dict(d_work=work, work_bytes=need - 1), "too small"),
                          (dict(d_work=work.data_ptr() + 8, work_bytes=need), "256-byte"), (dict(dtype=5), "element type"),
-                         (dict(scale=0.0), "scale"), (dict(scale=NAN), "scale"), (dict(scale=-1.0), "scale"), (dict(top=33), "32 alternatives"),
+                         (dict(scale=0.0), "scale"), (dict(scale=NAN), "scale"), (dict(scale=-1.0), "scale"), (dict(scale=2.0 ** 65), "scale"),
+                         (dict(top=33), "32 alternatives"),
                          (dict(cols=3, top=4), "more alternatives"), (dict(ld_x=100), "stride"), (dict(d_lse=None), "NULL"),
                          (dict(d_logp=None), "NULL"), (dict(d_target=None), "without d_target"), (dict(top=2), "NULL"),
                          (dict(d_lse=v.data_ptr() + 2), "aligned")):
