@@ -483,7 +483,7 @@ __global__ __launch_bounds__(BLOCK) void log_probs_grad_kernel(LogProbsGradArgs 
         auto value = [&](float x, uint32_t col) {
             const float d = fmaf(x - m, g.scale, -log_s), p = exp2_of(d * LOG2E);
             float v = all_p;
-            if constexpr (H) v = fmaf(by_h, fmaxf(d, LEAST) + h, v);
+            if constexpr (H) v = fmaf(by_h, fmaxf(d, FAR) + h, v);      // where p is 0, times 0 whatever by_h is
             v *= p;
             return col == (uint32_t)target && target >= 0 ? v + one : v;
         };

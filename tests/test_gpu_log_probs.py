@@ -216,6 +216,20 @@ def test_gradient_of_masked_rows(ops):
         assert torch.isfinite(got[0]).all() and (got[4].abs() <= L.U).all() and torch.isnan(got[1]).all()
 
 
+@pytest.mark.parametrize("low", [-INF, torch.finfo(torch.float32).min, -1e30])
+def test_large_entropy_gradient_of_masked_places(ops, low):
+    """What has no probability gives 0, however large the entropy's gradient."""
+    for cols in (100, 900, 3000):
+        x, t = make(5, cols, torch.float32, 3), torch.tensor([1, -1, 2, 3, 6], device=DEV)
+        x[:, 1::3] = low
+        ref = L.Logs(x)
+        norm, h = (torch.from_numpy(v).float().to(DEV) for v in (ref.norm, ref.entropy))
+        some = dict(g_logp=torch.full((5,), -3.0, device=DEV), g_entropy=torch.tensor([1.5, -2.0, 100.0, 1e4, -1e20], device=DEV))
+        got = ops.log_probs_grad(x, t, norm, entropy=h, **some)
+        check_grad(got, ref, torch.float32, t, **some)
+        assert (got[1:, 1::3] == 0).all() and got[0, 1] == -3 and (got[0, 4::3] == 0).all()
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_autograd(ops, dtype):
     """Through torch's graph, leading dimensions and all; against the formula's and against differences."""
