@@ -11,7 +11,7 @@
 // in the adapters' order first, as a list that the kernels go by: nothing is moved.
 //
 // 8192 rows of 4096 in 8 bits to 4096 in bf16, rank 16, six runs: 50 to 52 us, of which the product over long rows takes 16 (34 MB; 11 for
-// one adapter) and the one with B 30 (134 MB, 4.5 TB/s).  One row: two launches, 3.7 and 4.6 us.
+// one adapter) and the one with B 30 (134 MB, 4.5 TB/s).  One row: one launch, 7.6 us.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -103,6 +103,22 @@ __device__ __forceinline__ void codes_as(uint4 w, Sixteen<T>& s) {
         for (uint32_t j = 0; j < 8; ++j) f[j] = (float)(int8_t)(word[2 * i + j / 4] >> (8 * (j % 4)));
         s.h[i].from(f);
     }
+}
+
+// The 16 codes from column c on, zeros behind the row's end: what it holds there is not read as codes.
+__device__ __forceinline__ uint4 codes_end(const int8_t* q, uint32_t c, uint32_t cols) {
+    uint32_t w[4] = {0, 0, 0, 0};
+    if (c < cols) {
+        const uint4 v = *reinterpret_cast<const uint4*>(q + c);
+        w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+        const int32_t n = (int32_t)(cols - c);
+#pragma unroll
+        for (int32_t e = 0; e < 4; ++e) {
+            const int32_t b = min(max(n - 4 * e, 0), 4);
+            w[e] &= b == 4 ? ~0u : (1u << (8 * b)) - 1u;
+        }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 // The adapter of the block: of few rows, each block takes one of the adapters that a tile's rows have, the job-th of them.  False: there
@@ -204,18 +220,7 @@ __global__ __launch_bounds__(ADAPT_THREADS, RT * RF > 2 ? 2 : 3) void adapters_d
 #pragma unroll
             for (uint32_t i = 0; i < RT; ++i) {
                 if (CODES) {
-                    uint32_t w[4] = {0, 0, 0, 0};
-                    if (c < g.k) {
-                        const uint4 v = *reinterpret_cast<const uint4*>(q[i] + c);
-                        w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
-                        const int32_t n = (int32_t)(g.k - c);            // what a row holds behind its end is not read as codes
-#pragma unroll
-                        for (int32_t e = 0; e < 4; ++e) {
-                            const int32_t b = min(max(n - 4 * e, 0), 4);
-                            w[e] &= b == 4 ? ~0u : (1u << (8 * b)) - 1u;
-                        }
-                    }
-                    o.q[i] = make_uint4(w[0], w[1], w[2], w[3]);
+                    o.q[i] = codes_end(q[i], c, g.k);
                 } else {
                     o.x[i].load_end(x[i], c, APART, g.k);
                 }
@@ -662,6 +667,160 @@ static void launch_up(shifter_ctx* ctx, int dtype, int y_dtype, const AdaptersUp
     else launch_up_as<_Float16>(ctx, y_dtype, g);
 }
 
+// Both products in one launch, for a few rows of small adapters: each block works out s for itself, its wavefronts taking steps of 64 columns
+// in turn, and multiplies it with its columns of B, which are on their way meanwhile, as y is.  One row of 4096 in 8 bits to 4096 with rank 16 7.6 us
+// (9.3 in two launches), 512 to 512 6.3 (9.4): a launch, three trips to memory one after the other, and 131 KB of A by each of 16 blocks.
+constexpr uint32_t ONE_THREADS = 1024, ONE_WAVES = ONE_THREADS / 64;
+struct AdaptersOneArgs {
+    AdaptersDownArgs d;
+    AdaptersUpArgs u;
+};
+template <typename T, bool CODES, typename Y, uint32_t NF>
+__global__ __launch_bounds__(ONE_THREADS) void adapters_one_kernel(AdaptersOneArgs g) {
+    __shared__ v4f s_sum[ONE_WAVES][NF][64];
+    const UpTile<T, Y> tile;
+    const uint32_t wave = uniform_u32(threadIdx.x >> 6), job = blockIdx.z, rank = g.u.rank, k = g.d.k;
+    const uint64_t nth = (uint64_t)blockIdx.x * 16u + tile.r16, row = min(nth, (uint64_t)g.u.m - 1u);
+    const int id = nth < g.u.m ? adapter_of(g.u.which, row, g.u.m, g.u.adapters) : NO_ADAPTER;
+    int mine = NO_ADAPTER;
+    if (!adapter_of_job(id, job, &mine)) {         // all wavefronts alike
+        if (job != 0) return;
+        mine = NO_ADAPTER;
+    }
+    uint32_t n0 = (wave * gridDim.y + blockIdx.y) * 64u;
+    const bool full = n0 + 64u <= g.u.n;
+    BFour<T> b[NF][4];
+    Eight<Y> y[2];
+    auto fetch_b = [&] {
+#pragma unroll
+        for (uint32_t t = 0; t < 4; ++t)
+#pragma unroll
+            for (uint32_t f = 0; f < NF; ++f) b[f][t].template load<false>(tile.b_row(g.u, mine, n0, t), 16u * f + 4u * tile.group, rank);
+    };
+    if (n0 < g.u.n) {
+        if (full) tile.template fetch<true>(g.u, row, n0, y);
+        else tile.template fetch<false>(g.u, row, n0, y);
+        if (mine >= 0) fetch_b();
+    }
+    if (mine >= 0) {
+        constexpr uint32_t APART = CODES ? 8 : 32;
+        const uint32_t col = (CODES ? 16u : 8u) * tile.group, whole = k / ADAPT_STEP;
+        const T* x = static_cast<const T*>(g.d.x) + row * g.d.ld_x;
+        const int8_t* q = static_cast<const int8_t*>(g.d.x) + row * g.d.ld_x;
+        const T* a[NF];
+        v4f acc[NF];
+#pragma unroll
+        for (uint32_t f = 0; f < NF; ++f) {
+            a[f] = static_cast<const T*>(g.d.a) + ((uint64_t)mine * rank + min(16u * f + tile.r16, rank - 1u)) * k;
+            acc[f] = v4f{0, 0, 0, 0};
+        }
+        auto multiply = [&](const Sixteen<T>& v, const Sixteen<T> (&w)[NF]) {
+#pragma unroll
+            for (uint32_t f = 0; f < NF; ++f)
+#pragma unroll
+                for (uint32_t h = 0; h < 2; ++h) acc[f] = mma(w[f].h[h], v.h[h], acc[f]);
+        };
+        constexpr uint32_t DEPTH = sizeof(T) == 2 ? 4 / NF : 1;        // steps under way
+        uint32_t s = wave;
+        auto steps = [&](auto depth) {
+            constexpr uint32_t D = depth.value;
+            Sixteen<T> v[D], w[D][NF];
+            uint4 code[D];
+#pragma unroll
+            for (uint32_t i = 0; i < D; ++i) {
+                const uint32_t c = (s + i * ONE_WAVES) * ADAPT_STEP + col;
+                if (CODES) code[i] = *reinterpret_cast<const uint4*>(q + c);
+                else v[i].load(x + c, APART);
+#pragma unroll
+                for (uint32_t f = 0; f < NF; ++f) w[i][f].load(a[f] + c, APART);
+            }
+#pragma unroll
+            for (uint32_t i = 0; i < D; ++i) {
+                if (CODES) codes_as(code[i], v[i]);
+                multiply(v[i], w[i]);
+            }
+            s += D * ONE_WAVES;
+        };
+        while (s + (DEPTH - 1u) * ONE_WAVES < whole) steps(std::integral_constant<uint32_t, DEPTH>{});
+        while (s < whole) steps(std::integral_constant<uint32_t, 1>{});
+        if (whole * ADAPT_STEP < k && whole % ONE_WAVES == wave) {         // the step that a row ends in
+            const uint32_t c = whole * ADAPT_STEP + col;
+            Sixteen<T> v, w[NF];
+            if (CODES) codes_as(codes_end(q, c, k), v);
+            else v.load_end(x, c, APART, k);
+#pragma unroll
+            for (uint32_t f = 0; f < NF; ++f) w[f].load_end(a[f], c, APART, k);
+            multiply(v, w);
+        }
+#pragma unroll
+        for (uint32_t f = 0; f < NF; ++f) s_sum[wave][f][tile.lane] = acc[f];
+    }
+    __syncthreads();
+    v4f v[NF];
+    float by = 1.0f;
+    if (id >= 0) {
+        if (g.d.scale) by = g.d.scale[id];
+        if (CODES) by *= g.d.x_scale[row];
+    }
+    typename BFour<T>::S s[NF];
+#pragma unroll
+    for (uint32_t f = 0; f < NF; ++f) {
+        v[f] = v4f{0, 0, 0, 0};
+        if (mine >= 0) {
+#pragma unroll
+            for (uint32_t w = 0; w < ONE_WAVES; ++w) v[f] += s_sum[w][f][tile.lane];
+        }
+        const uint32_t r = 16u * f + 4u * tile.group;
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e) v[f][e] = id == BAD_ADAPTER ? NAN : id < 0 || r + e >= rank ? 0.0f : v[f][e] * by;
+        s[f].from(v[f]);
+    }
+    const bool own = nth < g.u.m && (id >= 0 ? id == mine : job == 0);
+    if (g.u.down && own && blockIdx.y == 0 && wave == 0) {
+#pragma unroll
+        for (uint32_t f = 0; f < NF; ++f) keep_down(g.u, row, 16u * f + 4u * tile.group, v[f]);
+    }
+    const bool writes = own && !tile.stays(g.u, id);
+    for (bool first = true; n0 < g.u.n; n0 += gridDim.y * ONE_WAVES * 64u, first = false) {
+        if (!first) {
+            tile.template fetch<false>(g.u, row, n0, y);
+            if (mine >= 0) fetch_b();
+        }
+        v4f sum[4];
+#pragma unroll
+        for (uint32_t t = 0; t < 4; ++t) sum[t] = v4f{0, 0, 0, 0};
+        if (mine >= 0) {
+#pragma unroll
+            for (uint32_t f = 0; f < NF; ++f)
+#pragma unroll
+                for (uint32_t t = 0; t < 4; ++t) sum[t] = b[f][t].multiply(s[f], sum[t]);
+        }
+        if (n0 + 64u <= g.u.n) tile.template write<true>(g.u, row, writes, id, n0, y, sum);
+        else tile.template write<false>(g.u, row, writes, id, n0, y, sum);
+    }
+}
+
+template <typename T, bool CODES, typename Y>
+static void launch_one_of(shifter_ctx* ctx, const AdaptersOneArgs& g) {
+    const uint32_t tiles = (g.u.m + 15u) / 16u, jobs = adapt_jobs(g.u.m, g.u.adapters);
+    const dim3 grid(tiles, adapt_one_blocks(g.u.m, g.u.n, g.u.adapters), jobs);
+    if (g.u.rank <= 16) adapters_one_kernel<T, CODES, Y, 1><<<grid, ONE_THREADS, 0, ctx->stream>>>(g);
+    else adapters_one_kernel<T, CODES, Y, 2><<<grid, ONE_THREADS, 0, ctx->stream>>>(g);
+}
+template <typename T>
+static void launch_one_as(shifter_ctx* ctx, int y_dtype, const AdaptersOneArgs& g) {
+    const bool codes = g.d.x_scale != nullptr;
+    if (y_dtype == SHIFTER_F32) codes ? launch_one_of<T, true, float>(ctx, g) : launch_one_of<T, false, float>(ctx, g);
+    else if (y_dtype == SHIFTER_BF16) codes ? launch_one_of<T, true, __bf16>(ctx, g) : launch_one_of<T, false, __bf16>(ctx, g);
+    else codes ? launch_one_of<T, true, _Float16>(ctx, g) : launch_one_of<T, false, _Float16>(ctx, g);
+}
+static void launch_one(shifter_ctx* ctx, int dtype, int y_dtype, const AdaptersOneArgs& g) {
+    ProfileScope ps(ctx, K_ADAPTERS_UP);
+    if (dtype == SHIFTER_F32) launch_one_as<float>(ctx, y_dtype, g);
+    else if (dtype == SHIFTER_BF16) launch_one_as<__bf16>(ctx, y_dtype, g);
+    else launch_one_as<_Float16>(ctx, y_dtype, g);
+}
+
 // The rows in the order of their adapters, those without one at the end, by one block: rows are counted by adapter in LDS, each with its
 // place among the ones counted before it.  The order of an adapter's rows is not always the same, which no row's result depends on.
 constexpr uint32_t SORT_THREADS = 1024, SORT_EACH = 8;
@@ -741,10 +900,11 @@ void launch_adapters(shifter_ctx* ctx, int dtype, int y_dtype, const AdaptersArg
     d.m = g.m; d.k = g.k; d.rank = g.rank; d.adapters = g.adapters; d.parts = p.parts;
     d.order = order;
     d.s = reinterpret_cast<float*>(g.work);
-    launch_down(ctx, dtype, d);
     AdaptersUpArgs u{};
     u.s = d.s; u.order = order; u.parts = p.parts; u.b = g.b; u.which = g.which; u.m = g.m; u.n = g.n; u.rank = g.rank; u.adapters = g.adapters;
     u.y = g.y; u.ld_y = g.ld_y; u.out = g.out; u.ld_out = g.ld_out; u.down = g.down; u.down_cols = g.rank;
+    if (adapt_one(g.m, g.k, g.ld_x, g.rank, g.adapters, dtype == SHIFTER_F32 ? 4 : 2)) return launch_one(ctx, dtype, y_dtype, AdaptersOneArgs{d, u});
+    launch_down(ctx, dtype, d);
     launch_up(ctx, dtype, y_dtype, u);
 }
 

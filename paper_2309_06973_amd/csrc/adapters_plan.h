@@ -24,6 +24,7 @@ constexpr uint32_t ADAPT_STEP = 64;                // columns of a step of the p
 constexpr uint64_t ADAPT_FEW_ROWS = 128, ADAPT_TWO_TILES = 2048;
 constexpr uint32_t ADAPT_MANY_ROWS_PARTS = 2;      // with more rows, their product with B holds so many in registers
 constexpr uint32_t ADAPT_UP_BLOCKS = 2048;         // of the product with B, as far as there are columns (1024 and 4096: within 4 %)
+constexpr uint64_t ADAPT_ONE_BYTES = 144u << 10;
 constexpr uint32_t ADAPT_SLAB = 128;               // columns of a block of the gradient's sums over rows
 
 inline uint64_t adapt_pad(uint64_t rank) { return (rank + 15u) & ~15ull; }
@@ -39,6 +40,22 @@ inline uint32_t adapt_jobs(uint64_t m, uint64_t adapters) {
 // The same for the product over long rows, of any number of rows.
 inline uint32_t adapt_down_jobs(uint64_t m, uint64_t adapters) {
     return m <= ADAPT_FEW_ROWS ? adapt_jobs(m, adapters) : adapters >= 2 ? 2u : 1u;
+}
+
+// Whether one launch does for both products: each of its blocks reads a tile's rows and their adapter's A, which is less than a second launch
+// costs up to ADAPT_ONE_BYTES of rows that start on 16 bytes.  us of two launches / one, bf16, square: one row, rank 16, 1024 columns 10.1 / 6.7,
+// 2048 9.6 / 7.2, 4096 (139 KB) 9.8 / 8.8, 8192 with rank 8 (147 KB) 10.7 / 10.0; eight rows, 2048 9.6 / 7.2, 4096 (197 KB) 9.7 / 9.6; sixteen rows, 2048
+// 9.6 / 8.4, 4096 (262 KB) 9.8 / 11.1; fp32, one row, 2048 (139 KB) 9.6 / 8.7, eight (197 KB) 10.3 / 10.0.  48 rows of 32 adapters, 2048 10.0 / 8.4; 128
+// 12.2 / 9.7.  Rows of 3541 in fp16, which start anywhere: 48 of 32 adapters with rank 4 13.3 / 19.9.  It needs no workspace.
+inline bool adapt_one(uint64_t m, uint64_t k, uint64_t ld_x, uint32_t rank, uint64_t adapters, uint64_t size) {
+    return m <= ADAPT_FEW_ROWS && rank <= 32 && adapters >= 1 && k % 8u == 0 && ld_x % 8u == 0 &&
+           (rank + std::min<uint64_t>(m, 16u)) * k * size <= ADAPT_ONE_BYTES;
+}
+// Its blocks that share the columns of a tile's rows and adapter.  More than 256 blocks take a compute unit's turn each (128 rows of 32 adapters,
+// 4096 x 1024: 256 9.9 us, 512 13.8, 1024 21.0).
+inline uint32_t adapt_one_blocks(uint64_t m, uint64_t n, uint64_t adapters) {
+    const uint64_t shared = (m + 15u) / 16u * adapt_jobs(m, adapters), groups = (n + 255u) / 256u;
+    return (uint32_t)std::max<uint64_t>(1u, std::min<uint64_t>(groups, 256u / shared));
 }
 
 // Whether the rows are put in order of their adapters first: one more launch, of 6 to 11 us, where tiles of rows as they come could have many.

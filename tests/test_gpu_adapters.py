@@ -98,6 +98,27 @@ def test_adapters(ops, which, dtype, codes):
 
 @pytest.mark.parametrize("codes", [False, True])
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m, n, k, rank, adapters", [(1, 4096, 4096, 16, 8), (1, 4097, 4104, 16, 8), (1, 17000, 64, 31, 2), (3, 1000, 3880, 16, 1), (8, 63, 3000, 32, 9), (16, 300, 1024, 1, 40),
+                                                    (17, 1025, 8, 12, 3), (48, 2500, 1088, 16, 32), (128, 5000, 1000, 20, 40), (129, 300, 1000, 20, 40), (100, 70, 0, 8, 5)])
+def test_few_rows_of_small_adapters(ops, m, n, k, rank, adapters, dtype, codes):
+    """Around what one launch does for, columns that end anywhere, rows that name no adapter among others."""
+    for pattern, gap, shift in (("random", 0, 0), ("runs", 8, 3), ("one", 4, 0)):
+        print(f"few rows m={m} n={n} k={k} rank={rank} adapters={adapters} {dtype} codes={codes} {pattern} gap={gap}", flush=True)
+        y, x, values, a, b, num, scale = setup(ops, m, n, k, rank, adapters, dtype, pattern, codes, torch.bfloat16, gap, shift)
+        if m > 2:
+            num[1], num[2] = -1, adapters
+        ref = L.Adapters(y, values, a, b, num, scale)
+        down = torch.full((m, rank), 9.0, device=DEV)
+        out = ops.adapters(y, x, a, b, num, scale=scale, down=down)
+        near(out, ref.out, ref.off, torch.bfloat16, "out")
+        near(down, ref.down, ref.off_down, torch.float32, "down")
+        z = y.clone()
+        ops.adapters(z, x, a, b, num, scale=scale, out=z)
+        assert torch.equal(torch.nan_to_num(z), torch.nan_to_num(out))
+
+
+@pytest.mark.parametrize("codes", [False, True])
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("which", range(len(SIZES)))
 def test_gradients(ops, which, dtype, codes):
     m, n, k, rank, adapters = SIZES[which]

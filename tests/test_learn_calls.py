@@ -143,6 +143,9 @@ int main(int n, char** v) {
             for (int i = 2; i + 2 < n; i += 3) all.push_back({(void*)at(i), (void*)at(i + 1), nullptr, at(i + 2), SHIFTER_F32});
             printf("%d\n", (int)grad_overlap(all));
         } break;
+        case 'e': for (int i = 2; i + 6 < n; i += 7) // rows, columns of y, of x, x's stride, rank, adapters, bytes of an element
+            printf("%d %u\n", (int)adapt_one(at(i), at(i + 2), at(i + 3), (uint32_t)at(i + 4), at(i + 5), at(i + 6)), adapt_one_blocks(at(i), at(i + 1), at(i + 5)));
+        break;
         case 'a': for (int i = 2; i + 4 < n; i += 5) {
             const uint64_t m = at(i), nn = at(i + 1), k = at(i + 2), many = at(i + 4);
             const uint32_t rank = (uint32_t)at(i + 3);
@@ -225,6 +228,22 @@ def test_tensors_that_overlap(plan):
         want = any((a[3] or b[3]) and a[1] < b[2] and b[1] < a[2] for x, a in enumerate(spans) for b in spans[x + 1:])
         assert int(plan("o", [v for e in grads for v in e])[0]) == want
         seen[want] += 1
+    assert min(seen) > 50
+
+
+def test_adapters_in_one_launch(plan):
+    rng = random.Random(6)
+    size = lambda most: int(2 ** rng.uniform(0, most))
+    sizes = [(size(8), size(14), size(12), rng.randint(0, 8), rng.randint(1, 40), rng.choice([0, 1, 7, 8, 64]), rng.choice([2, 4])) for _ in range(2000)]
+    sizes += [(m, n, 4096, 0, 16, 8, 2) for m in (1, 2, 3, 16, 128, 129) for n in (0, 1, 256, 257, 4096, 1 << 31)]
+    sizes = [(m, n, k // 8 * 8 if i % 2 else k, k + gap, rank, many, b) for i, (m, n, k, gap, rank, many, b) in enumerate(sizes)]
+    seen = [0, 0]
+    for (m, n, k, ld, rank, many, b), line in zip(sizes, plan("e", [x for s in sizes for x in s])):
+        one, blocks = map(int, line.split())
+        # whole pieces of eight of A and x, and not many of them
+        assert one == (m <= 128 and rank <= 32 and many > 0 and k % 8 == 0 and ld % 8 == 0 and (rank + min(m, 16)) * k * b <= 147456)
+        assert 1 <= blocks <= max(1, up(n, 256)) and blocks * up(m, 16) * (1 if m > 128 else max(1, min(16, m, many))) <= max(256, up(m, 16) * 16)
+        seen[one] += 1
     assert min(seen) > 50
 
 
