@@ -784,9 +784,9 @@ int shifter_weight_grad_q8(shifter_ctx* ctx, const void* d_g, int dtype, uint64_
  *                        B (adapters x n x rank) lie without gaps and have x's element type; x is elements, or an 8-bit
  *                        matrix (d_q_scale not NULL: d_x are its codes, ld_x its stride).  A row whose number is negative
  *                        has no adapter: out_r is y_r; one whose number is not below `adapters` is NaN.  d_scale NULL: 1.
- *                        Sums are in 32 bits.  d_out may be d_y with the same stride.  d_down, or NULL: m x rank, gets
- *                        scale[i] x_r A_i' (0 without an adapter) for the gradient.  What a row gives depends on its own
- *                        numbers and adapter alone.
+ *                        Sums are in 32 bits; infinities in B may give NaN.  d_out may be d_y with the same stride, and both
+ *                        may be d_x.  d_down, or NULL: m x rank, gets scale[i] x_r A_i' (0 without an adapter) for the gradient.
+ *                        What a row gives depends on its own numbers and adapter alone.
  * shifter_adapters_grad  from g, the gradient of out, of x's element type: up_r = scale[i] g_r B_i, dx_r = up_r A_i (of that type, 0
  *                        without an adapter; d_dx may be NULL), dA_i = sum up_r' x_r, dB_i = sum g_r' down_r over the rows of adapter i,
  *                        fp32, 0 for an adapter without rows.  Rows whose number is not below `adapters` count for none.  d_down: as

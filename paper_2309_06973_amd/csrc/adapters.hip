@@ -903,7 +903,12 @@ void launch_adapters(shifter_ctx* ctx, int dtype, int y_dtype, const AdaptersArg
     AdaptersUpArgs u{};
     u.s = d.s; u.order = order; u.parts = p.parts; u.b = g.b; u.which = g.which; u.m = g.m; u.n = g.n; u.rank = g.rank; u.adapters = g.adapters;
     u.y = g.y; u.ld_y = g.ld_y; u.out = g.out; u.ld_out = g.ld_out; u.down = g.down; u.down_cols = g.rank;
-    if (adapt_one(g.m, g.k, g.ld_x, g.rank, g.adapters, dtype == SHIFTER_F32 ? 4 : 2)) return launch_one(ctx, dtype, y_dtype, AdaptersOneArgs{d, u});
+    // x may be y, and written in place: not while blocks read it
+    auto last = [&](uint64_t ld, uint64_t cols, uint64_t size) { return ((g.m - 1u) * ld + cols) * size; };
+    const uintptr_t x = reinterpret_cast<uintptr_t>(g.x), out = reinterpret_cast<uintptr_t>(g.out);
+    const uint64_t size = dtype == SHIFTER_F32 ? 4 : 2, y_size = y_dtype == SHIFTER_F32 ? 4 : 2;
+    const bool apart = out >= x + last(g.ld_x, g.k, g.x_scale ? 1 : size) || x >= out + last(g.ld_out, g.n, y_size);
+    if (apart && adapt_one(g.m, g.k, g.ld_x, g.rank, g.adapters, size)) return launch_one(ctx, dtype, y_dtype, AdaptersOneArgs{d, u});
     launch_down(ctx, dtype, d);
     launch_up(ctx, dtype, y_dtype, u);
 }

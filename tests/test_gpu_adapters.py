@@ -117,6 +117,20 @@ def test_few_rows_of_small_adapters(ops, m, n, k, rank, adapters, dtype, codes):
         assert torch.equal(torch.nan_to_num(z), torch.nan_to_num(out))
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m, n, rank", [(1, 64, 3), (5, 2048, 16), (100, 1000, 8), (128, 4096, 4), (16, 300, 40), (300, 512, 16)])
+def test_x_is_y_in_place(ops, m, n, rank, dtype):
+    x, _, _, a, b, num, scale = setup(ops, m, n, n, rank, 5, dtype, "random")
+    num = num.clamp(min=0)
+    want = ops.adapters(x, x, a, b, num, scale=scale)
+    ref = L.Adapters(x, x, a, b, num, scale)
+    near(want, ref.out, ref.off, dtype, "out")
+    for _ in range(5):
+        z = x.clone()
+        ops.adapters(z, z, a, b, num, scale=scale, out=z)
+        near(z, ref.out, ref.off, dtype, "in place")
+
+
 @pytest.mark.parametrize("codes", [False, True])
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("which", range(len(SIZES)))
