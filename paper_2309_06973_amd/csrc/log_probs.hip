@@ -471,21 +471,21 @@ __global__ __launch_bounds__(BLOCK) void log_probs_grad_kernel(LogProbsGradArgs 
         const T* row = static_cast<const T*>(g.x) + r * g.ld_x;
         T* out = static_cast<T*>(g.dx) + r * g.ld_dx;
         const int64_t target = g.target ? g.target[r] : -1;
-        float one = g.g_logp && target >= 0 ? g.g_logp[r] * g.scale : 0.0f;
+        float one = g.g_logp && target >= 0 ? g.g_logp[r] : 0.0f;
         if (target >= (int64_t)g.cols) one = NAN;
-        const float m = g.norm[2 * r], log_s = g.norm[2 * r + 1], all_p = (g.g_lse ? g.g_lse[r] * g.scale : 0.0f) - one;
+        const float m = g.norm[2 * r], log_s = g.norm[2 * r + 1], all_p = (g.g_lse ? g.g_lse[r] : 0.0f) - one;
         float h = 0.0f, by_h = 0.0f;
         if constexpr (H) {
             h = g.entropy[r];
-            by_h = -g.g_entropy[r] * g.scale;
+            by_h = -g.g_entropy[r];
         }
         const bool none = all_p == 0.0f && one == 0.0f && by_h == 0.0f;
         auto value = [&](float x, uint32_t col) {
             const float d = fmaf(x - m, g.scale, -log_s), p = exp2_of(d * LOG2E);
-            float v = all_p;
-            if constexpr (H) v = fmaf(by_h, fmaxf(d, FAR) + h, v);      // where p is 0, times 0 whatever by_h is
-            v *= p;
-            return col == (uint32_t)target && target >= 0 ? v + one : v;
+            // p first and the scale last: no factor of a row comes to the end of fp32 before p makes it small, and where p is 0 this is 0
+            float v = all_p * p;
+            if constexpr (H) v = fmaf(by_h, p * (fmaxf(d, FAR) + h), v);
+            return (col == (uint32_t)target && target >= 0 ? v + one : v) * g.scale;
         };
         auto piece = [&](uint32_t at, const Eight<T>& e) {
             float f[8];
