@@ -1858,7 +1858,7 @@ extern "C" int shifter_log_probs(shifter_ctx* ctx, const shifter_log_probs_args*
         return fail(ctx, SHIFTER_ERR_INVALID_ARG, "log_probs: the workspace must be 256-byte aligned");
     LogProbsArgs g{};
     g.x = a->d_x; g.ld_x = a->ld_x; g.rows = (uint32_t)a->rows; g.cols = (uint32_t)a->cols; g.top = a->top;
-    g.target = a->d_target; g.scale = a->scale;
+    g.target = a->d_target; g.scale = a->scale; g.unit = log_probs_unit(a->scale); g.by = a->scale / g.unit;
     g.norm = a->d_norm; g.lse = a->d_lse; g.logp = a->d_logp; g.entropy = a->d_entropy; g.top_logp = a->d_top; g.index = a->d_index;
     g.work = static_cast<uint8_t*>(a->d_work);
     launch_log_probs(ctx, a->dtype, g);
@@ -1884,7 +1884,8 @@ extern "C" int shifter_log_probs_grad(shifter_ctx* ctx, const shifter_log_probs_
         return fail(ctx, SHIFTER_ERR_INVALID_ARG, "log_probs_grad: a pointer is not aligned to its elements");
     LogProbsGradArgs g{};
     g.x = a->d_x; g.ld_x = a->ld_x; g.ld_dx = a->ld_dx; g.rows = (uint32_t)a->rows; g.cols = (uint32_t)a->cols;
-    g.target = a->d_target; g.scale = a->scale; g.norm = a->d_norm; g.entropy = a->d_entropy;
+    g.target = a->d_target; g.scale = a->scale; g.unit = log_probs_unit(a->scale); g.by = a->scale / g.unit;
+    g.norm = a->d_norm; g.entropy = a->d_entropy;
     g.g_logp = a->d_g_logp; g.g_entropy = a->d_g_entropy; g.g_lse = a->d_g_lse; g.dx = a->d_dx;
     launch_log_probs_grad(ctx, a->dtype, g);
     return after_launch(ctx, "log_probs_grad");

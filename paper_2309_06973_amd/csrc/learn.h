@@ -13,7 +13,7 @@ struct LogProbsArgs {
     uint64_t ld_x;
     uint32_t rows, cols, top;
     const int64_t* target;     // rows, or nullptr
-    float scale;
+    float scale, unit, by;     // log_probs_unit(scale); the scale of logits in that unit
     float* norm;               // [rows][2]: max x, log sum e^(z - scale max x)
     float *lse, *logp, *entropy;   // rows; logp nullptr without targets, entropy nullptr: not asked for
     float* top_logp;           // [rows][top]
@@ -28,7 +28,7 @@ struct LogProbsGradArgs {
     uint64_t ld_x, ld_dx;
     uint32_t rows, cols;
     const int64_t* target;
-    float scale;
+    float scale, unit, by;
     const float* norm;         // [rows][2]
     const float *entropy, *g_logp, *g_entropy, *g_lse;   // rows each, or nullptr
     void* dx;

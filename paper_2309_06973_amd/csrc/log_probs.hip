@@ -31,16 +31,23 @@ constexpr float FAR = -1000.0f;                    // 2^FAR is 0 in 32 bits
 
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// d of two logits.  Both are taken in `unit`, 1 or less, as their difference may be beyond fp32 where the scale brings it back; a power of two, so that
+// nothing is rounded but the difference and the product, and with 1 the difference is x - m to the bit.
+struct Distance {
+    float unit, c;                     // c: log2 e times the scale, of logits in that unit
+    __device__ __forceinline__ float operator()(float x, float m) const { return fmaf(x, unit, -(m * unit)) * c; }
+};
+
 struct Sums {
     float m, s, u;
 };
 
 // The sums of both.  The same to the bit whichever comes first, so that all lanes that exchange theirs hold the same.
 template <bool H>
-__device__ __forceinline__ Sums join(const Sums& a, const Sums& b, float c) {
+__device__ __forceinline__ Sums join(const Sums& a, const Sums& b, const Distance& c) {
     const bool first = a.m >= b.m;
     const float m = first ? a.m : b.m, less = first ? b.m : a.m, s = first ? b.s : a.s;
-    const float d = (less - m) * c, f = exp2_of(d);
+    const float d = c(less, m), f = exp2_of(d);
     Sums r;
     r.m = m;
     r.s = fmaf(f, s, first ? a.s : b.s);
@@ -68,7 +75,7 @@ struct Best {
 
 // U pieces of 8 logits whose first columns are c0, c0 + step, ..., of a row that ends at `end`.
 template <uint32_t U, bool H, bool TOP>
-__device__ __forceinline__ void take(const float (&f)[8 * U], uint32_t c0, uint32_t step, uint32_t end, float c, Sums& a, Best& best) {
+__device__ __forceinline__ void take(const float (&f)[8 * U], uint32_t c0, uint32_t step, uint32_t end, const Distance& c, Sums& a, Best& best) {
     float most = a.m;
 #pragma unroll
     for (uint32_t p = 0; p < U; ++p) {
@@ -82,13 +89,13 @@ __device__ __forceinline__ void take(const float (&f)[8 * U], uint32_t c0, uint3
             }
         }
     }
-    const float d = (a.m - most) * c, g = exp2_of(d);
+    const float d = c(a.m, most), g = exp2_of(d);
     if constexpr (H) a.u = g * fmaf(fmaxf(d, FAR), a.s, a.u);
     a.s *= g;
     a.m = most;
 #pragma unroll
     for (uint32_t i = 0; i < 8 * U; ++i) {
-        const float t = (f[i] - most) * c, e = exp2_of(t);
+        const float t = c(f[i], most), e = exp2_of(t);
         a.s += e;
         if constexpr (H) a.u = fmaf(e, fmaxf(t, FAR), a.u);
     }
@@ -97,7 +104,7 @@ __device__ __forceinline__ void take(const float (&f)[8 * U], uint32_t c0, uint3
 // The columns [c0, end) of a row by TPR threads, U pieces of 8 columns of each under way, the last of which stay in `e`.  Pieces behind
 // the end and the one that holds it are fetched from inside the row, so that no load stands in a branch.
 template <typename T, uint32_t TPR, uint32_t U, bool H, bool TOP>
-__device__ __forceinline__ void scan(const T* row, uint32_t c0, uint32_t end, uint32_t t, float c, Sums& a, Best& best,
+__device__ __forceinline__ void scan(const T* row, uint32_t c0, uint32_t end, uint32_t t, const Distance& c, Sums& a, Best& best,
                                      Eight<T> (&e)[U]) {
     constexpr uint32_t STEP = 8 * TPR;
     auto batch = [&](uint32_t at, auto last) {
@@ -151,12 +158,12 @@ __device__ __forceinline__ float beside(float v) {
     return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
 }
 template <int CTRL, bool H>
-__device__ __forceinline__ void join_beside(Sums& a, float c) {
+__device__ __forceinline__ void join_beside(Sums& a, const Distance& c) {
     a = join<H>(a, Sums{beside<CTRL>(a.m), beside<CTRL>(a.s), H ? beside<CTRL>(a.u) : 0.0f}, c);
 }
 // The sums of a wavefront's lanes, or of 16 of them, in all of these.
 template <uint32_t LANES, bool H>
-__device__ __forceinline__ Sums sum_lanes(Sums a, float c) {
+__device__ __forceinline__ Sums sum_lanes(Sums a, const Distance& c) {
     join_beside<0xB1, H>(a, c);
     join_beside<0x4E, H>(a, c);
     join_beside<0x141, H>(a, c);
@@ -172,7 +179,7 @@ __device__ __forceinline__ Sums sum_lanes(Sums a, float c) {
 }
 
 template <uint32_t TPR, bool H, bool TOP>
-__device__ __forceinline__ Sums sum_up(Sums a, uint32_t t, float c, RowShared<TPR, TOP>& sh) {
+__device__ __forceinline__ Sums sum_up(Sums a, uint32_t t, const Distance& c, RowShared<TPR, TOP>& sh) {
     a = sum_lanes<(TPR < 64 ? TPR : 64), H>(a, c);
     if constexpr (TPR > 64) {
         if ((t & 63u) == 0) sh.sums[t / 64] = a;
@@ -294,7 +301,7 @@ __global__ __launch_bounds__(TPR < BLOCK ? BLOCK : TPR) void log_probs_kernel(Lo
     __shared__ RowShared<TPR, TOP> shared[AT_ONCE];
     const uint32_t t = threadIdx.x % TPR;
     RowShared<TPR, TOP>& sh = shared[threadIdx.x / TPR];
-    const float c = g.scale * LOG2E;
+    const Distance c{g.unit, g.by * LOG2E};
     const uint64_t all = (uint64_t)g.rows * plan.parts;
     for (uint64_t i = (uint64_t)blockIdx.x * AT_ONCE + threadIdx.x / TPR; i < all; i += (uint64_t)gridDim.x * AT_ONCE) {
         const uint64_t r = plan.parts == 1 ? i : i / plan.parts;
@@ -454,7 +461,7 @@ void launch_log_probs(shifter_ctx* ctx, int dtype, const LogProbsArgs& g) {
     else launch_log_probs_of<_Float16>(ctx, g);
 }
 
-// The gradient, in one read of x: p = 2^((scale (x - m) - log s) log2 e) once more, from the row's m and log s: lse, their sum,
+// The gradient, in one read of x: p = 2^((scale (x - m) - log s) log2 e) once more, x - m in the same unit, from the row's m and log s: lse, their sum,
 // would have lost log s where all that is left of a row is the type's lowest value.  A row whose factors are all 0 is zeros,
 // whatever it holds.  Memory bounds it: 8192 x 32768 bf16, a fifth of the rows left out, 147 us with 430 MB read (some 200 of them from the
 // last-level cache) and 537 written.  Threads a row as for the sums, where 16, 64 and 256 are within a tenth of each other but for
@@ -473,7 +480,7 @@ __global__ __launch_bounds__(BLOCK) void log_probs_grad_kernel(LogProbsGradArgs 
         const int64_t target = g.target ? g.target[r] : -1;
         float one = g.g_logp && target >= 0 ? g.g_logp[r] : 0.0f;
         if (target >= (int64_t)g.cols) one = NAN;
-        const float m = g.norm[2 * r], log_s = g.norm[2 * r + 1], all_p = (g.g_lse ? g.g_lse[r] : 0.0f) - one;
+        const float m = g.norm[2 * r] * g.unit, log_s = g.norm[2 * r + 1], all_p = (g.g_lse ? g.g_lse[r] : 0.0f) - one;
         float h = 0.0f, by_h = 0.0f;
         if constexpr (H) {
             h = g.entropy[r];
@@ -481,7 +488,7 @@ __global__ __launch_bounds__(BLOCK) void log_probs_grad_kernel(LogProbsGradArgs 
         }
         const bool none = all_p == 0.0f && one == 0.0f && by_h == 0.0f;
         auto value = [&](float x, uint32_t col) {
-            const float d = fmaf(x - m, g.scale, -log_s), p = exp2_of(d * LOG2E);
+            const float d = fmaf(fmaf(x, g.unit, -m), g.by, -log_s), p = exp2_of(d * LOG2E);
             // p first and the scale last: no factor of a row comes to the end of fp32 before p makes it small, and where p is 0 this is 0
             float v = all_p * p;
             if constexpr (H) v = fmaf(by_h, p * (fmaxf(d, FAR) + h), v);

@@ -16,6 +16,11 @@ constexpr uint64_t LOGP_SHARED_ROWS = 512;         // only fewer rows than these
 constexpr uint64_t LEARN_TICKETS = 4 * LOGP_SHARED_ROWS;
 constexpr uint64_t LOGP_MAX_BLOCKS = 1u << 21;     // a launch holds less than 2^32 threads; blocks take further rows in turn
 
+// What a logit is multiplied with before differences are taken.  From 2^-64 on, logits whose difference is beyond fp32 (2^128 and more) are 2^64 and
+// more apart with the scale: minus infinity gives the same, no probability.  Below, the difference counts, and in 2^-64 it stays within 2^65;
+// what falls below fp32's steps there is less than 2^-148 with the scale.
+inline float log_probs_unit(float scale) { return scale < 0x1p-64f ? 0x1p-64f : 1.0f; }
+
 struct LogProbsPlan {
     uint32_t threads;      // of a row's part: 16 or 64, several rows a block; 256, a block
     uint32_t parts;        // blocks that share a row; the last of them joins their sums
