@@ -776,7 +776,7 @@ int shifter_weight_grad_q8(shifter_ctx* ctx, const void* d_g, int dtype, uint64_
  * shifter_clip_grad_norm the same, and each tensor times min(1, max_norm / (norm + 1e-6)) to its d_out, rounded to its
  *                        type; masked elements become 0.  A norm that is NaN makes all others NaN, an infinite one makes
  *                        finite elements 0 and others NaN.  max_norm is not negative.  d_out may be d_g; apart from that no
- *                        tensor that is written may overlap another one.
+ *                        tensor that is written may overlap another one or a mask.
  *                        Tensors are runs of elements of any start, with types of their own; h_grads is a host array that is
  *                        not used after the call returns.  d_out is not read by shifter_grad_norm.
  *

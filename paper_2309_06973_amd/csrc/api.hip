@@ -1916,7 +1916,7 @@ static int grad_norm_call(shifter_ctx* ctx, const char* fn, const shifter_grad* 
     all.reserve(count);
     for (uint64_t i = 0; i < count; ++i)
         if (h[i].n) all.push_back(h[i]);
-    if (clip && grad_overlap(all)) return fail(ctx, SHIFTER_ERR_INVALID_ARG, name + "a tensor that is written overlaps another one");
+    if (clip && grad_overlap(all)) return fail(ctx, SHIFTER_ERR_INVALID_ARG, name + "a tensor that is written overlaps another one or a mask");
     launch_grad_norm(ctx, all, clip, max_norm, d_norm, static_cast<uint8_t*>(d_work));
     return after_launch(ctx, fn);
 }

@@ -73,20 +73,21 @@ inline const char* grad_bad(const shifter_grad* h, uint64_t count, bool write) {
     return chunks >> 31 ? "2^42 elements or more" : nullptr;
 }
 
-// Whether a tensor that is written lies over another one, or over its own elements in another place.
+// Whether a tensor that is written lies over another one, over its own elements in another place or over a mask: blocks would read what others have
+// written already.
 inline bool grad_overlap(const std::vector<shifter_grad>& all) {
     struct Span {
         uint64_t from, to;
-        uint32_t of;
         bool written;
     };
     std::vector<Span> spans;
-    spans.reserve(2 * all.size());
+    spans.reserve(3 * all.size());
     for (uint32_t i = 0; i < all.size(); ++i) {
         const uint64_t bytes = all[i].n * (all[i].dtype == SHIFTER_F32 ? 4 : 2), g = reinterpret_cast<uint64_t>(all[i].d_g),
-                       out = reinterpret_cast<uint64_t>(all[i].d_out);
-        spans.push_back({out, out + bytes, i, true});
-        if (out != g) spans.push_back({g, g + bytes, i, false});
+                       out = reinterpret_cast<uint64_t>(all[i].d_out), mask = reinterpret_cast<uint64_t>(all[i].d_mask);
+        spans.push_back({out, out + bytes, true});
+        if (out != g) spans.push_back({g, g + bytes, false});
+        if (mask) spans.push_back({mask, mask + all[i].n, false});
     }
     std::sort(spans.begin(), spans.end(), [](const Span& a, const Span& b) { return a.from < b.from; });
     uint64_t any = 0, written = 0;                 // ends of what came before
