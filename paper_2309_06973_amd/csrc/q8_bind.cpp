@@ -540,6 +540,14 @@ struct Items {
     PyObject* operator[](Py_ssize_t i) const { return PySequence_Fast_GET_ITEM(seq.p, i); }
 };
 
+// Whether both, of one shape and without gaps, have their elements in the same order: the strides of dimensions of one element say nothing.
+bool in_order(const at::Tensor& a, const at::Tensor& b) {
+    if (a.numel() < 2) return true;
+    for (int64_t i = 0; i < a.dim(); ++i)
+        if (a.size(i) != 1 && a.stride(i) != b.stride(i)) return false;
+    return true;
+}
+
 // ctx, device, grads, masks, max_norm, out, room -> norm.  max_norm None: the norm alone.
 PyObject* grad_norm(PyObject* const* a) {
     const Handle h = handle_of(a);
@@ -562,8 +570,7 @@ PyObject* grad_norm(PyObject* const* a) {
         shifter_grad& e = list[(size_t)i];
         e = shifter_grad{g.data_ptr(), nullptr, nullptr, (uint64_t)g.numel(), code};
         auto alike = [&](const at::Tensor& t, at::ScalarType type, const char* what) {
-            TORCH_CHECK_VALUE(t.layout() == at::kStrided && t.scalar_type() == type && t.sizes() == g.sizes() &&
-                              (g.numel() < 2 || t.strides() == g.strides()), what, " ", i, " must be ", type,
+            TORCH_CHECK_VALUE(t.layout() == at::kStrided && t.scalar_type() == type && t.sizes() == g.sizes() && in_order(g, t), what, " ", i, " must be ", type,
                               " of its gradient's shape and layout in memory");
             here(h, t, what);
             return t.data_ptr();
