@@ -339,7 +339,7 @@ class _AdaptersGrad(torch.autograd.Function):
 class _Adapted(torch.autograd.Function):
     @staticmethod
     def forward(ctx, y, x, a, b, ops, x8, which, scale):
-        down = torch.empty(y.shape[0], a.shape[1], device=y.device)
+        down = torch.empty(y.shape[0], a.shape[1], dtype=torch.float32, device=y.device)
         out = ops.adapters(y, x if x8 is None else x8, a, b, which, scale, down=down)
         ctx.save_for_backward(x, a, b, which, down, *(t for t in (scale, *((x8.q, x8.scale) if x8 is not None else ())) if t is not None))
         ctx.ops, ctx.scaled, ctx.cols = ops, scale is not None, None if x8 is None else x8.cols
