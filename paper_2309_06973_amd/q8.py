@@ -129,7 +129,8 @@ class Q8:
         work = (self.recorded_joined[-1] if self.recorded_joined else None) if recording else self.joined
         new = work is None or work.numel() < need
         if new:
-            work = torch.empty(need, dtype=torch.uint8, device=self.dev)
+            with torch.inference_mode(False):      # or only calls in that mode could write it
+                work = torch.empty(need, dtype=torch.uint8, device=self.dev)
             if recording:
                 self.recorded_joined.append(work)
             else:
