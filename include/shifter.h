@@ -786,7 +786,9 @@ int shifter_weight_grad_q8(shifter_ctx* ctx, const void* d_g, int dtype, uint64_
  *                        has no adapter: out_r is y_r; one whose number is not below `adapters` is NaN.  d_scale NULL: 1.
  *                        Sums are in 32 bits; infinities in B may give NaN.  d_out may be d_y with the same stride, and both
  *                        may be d_x.  d_down, or NULL: m x rank, gets scale[i] x_r A_i' (0 without an adapter) for the gradient.
- *                        What a row gives depends on its own numbers and adapter alone.
+ *                        What a row gives depends on its own numbers and adapter alone, whatever the other rows hold and in whatever order
+ *                        they come: to the bit in calls of the same sizes, strides and types that are alike in whether d_out lies over
+ *                        d_x.  Other calls may add the same products up in another order.
  * shifter_adapters_grad  from g, the gradient of out, of x's element type: up_r = scale[i] g_r B_i, dx_r = up_r A_i (of that type, 0
  *                        without an adapter; d_dx may be NULL), dA_i = sum up_r' x_r, dB_i = sum g_r' down_r over the rows of adapter i,
  *                        fp32, 0 for an adapter without rows.  Rows whose number is not below `adapters` count for none.  d_down: as
