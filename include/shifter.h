@@ -784,7 +784,8 @@ int shifter_weight_grad_q8(shifter_ctx* ctx, const void* d_g, int dtype, uint64_
  *                        B (adapters x n x rank) lie without gaps and have x's element type; x is elements, or an 8-bit
  *                        matrix (d_q_scale not NULL: d_x are its codes, ld_x its stride).  A row whose number is negative
  *                        has no adapter: out_r is y_r; one whose number is not below `adapters` is NaN.  d_scale NULL: 1.
- *                        Sums are in 32 bits; infinities in B may give NaN.  d_out may be d_y with the same stride, and both
+ *                        Sums are in 32 bits; infinities in B may give NaN, and so may
+ *                        scale[i] x_r A_i' where that is infinite.  d_out may be d_y with the same stride, and both
  *                        may be d_x.  d_down, or NULL: m x rank, gets scale[i] x_r A_i' (0 without an adapter) for the gradient.
  *                        What a row gives depends on its own numbers and adapter alone, whatever the other rows hold and in whatever order
  *                        they come: to the bit in calls of the same sizes, strides and types that are alike in whether d_out lies over
