@@ -1001,11 +1001,11 @@ __global__ __launch_bounds__(ADAPT_THREADS) void adapters_turn_kernel(AdaptersTu
 __device__ __forceinline__ uint64_t part_of(uint32_t first, uint32_t adapter, uint32_t rows_each) { return first / rows_each + adapter; }
 
 // Sums over the rows of an adapter, rows_each of them from blockIdx.y rows_each on: 128 columns of dA_i = sum up' x or, further blocks, of
-// dB_i = sum g' down, 16 RF ranks at a time.  Wavefronts take 16 rows in turn and join their sums in LDS.
-template <typename T, bool CODES, uint32_t RF>
+// dB_i = sum g' down, 16 ranks a block.  Wavefronts take 16 rows in turn and join their sums in LDS.
+template <typename T, bool CODES>
 __global__ __launch_bounds__(ADAPT_THREADS, 3) void adapters_grad_kernel(AdaptersSumArgs g) {
     constexpr uint32_t DEPTH = 4;              // four rows each
-    __shared__ v4f s_sum[2][8 * RF][64];
+    __shared__ v4f s_sum[2][8][64];
     const uint32_t lane = threadIdx.x & 63u, wave = uniform_u32(threadIdx.x >> 6), group = lane / 16u, r16 = lane & 15u;
     const uint32_t slabs_a = (g.k + ADAPT_SLAB - 1u) / ADAPT_SLAB, slabs = slabs_a + (g.n + ADAPT_SLAB - 1u) / ADAPT_SLAB;
     const uint32_t adapter = blockIdx.x / slabs, nth_slab = blockIdx.x - adapter * slabs;
@@ -1024,135 +1024,115 @@ __global__ __launch_bounds__(ADAPT_THREADS, 3) void adapters_grad_kernel(Adapter
     struct Operands {
         Eight<T> v[DEPTH];
         uint2 w[DEPTH];
-        float p[DEPTH][RF], by[DEPTH];
+        float p[DEPTH], by[DEPTH];
     };
-    {
-        const uint32_t rank0 = blockIdx.z * 16u * RF;
-        v4f acc[RF][8];
+    const uint32_t rank0 = blockIdx.z * 16u, rank_at = min(rank0 + r16, g.rank - 1u);
+    v4f acc[8];
 #pragma unroll
-        for (uint32_t f = 0; f < RF; ++f)
+    for (uint32_t j = 0; j < 8; ++j) acc[j] = v4f{0, 0, 0, 0};
+    auto rows_at = [&](uint32_t at, uint32_t (&row)[DEPTH]) {
 #pragma unroll
-            for (uint32_t j = 0; j < 8; ++j) acc[f][j] = v4f{0, 0, 0, 0};
-        uint32_t rank_at[RF];
+        for (uint32_t d = 0; d < DEPTH; ++d) row[d] = list[min(at + 4u * d + group, q1 - 1u)];
+    };
+    auto fetch = [&](const uint32_t (&row)[DEPTH], Operands& o) {
 #pragma unroll
-        for (uint32_t f = 0; f < RF; ++f) rank_at[f] = min(rank0 + 16u * f + r16, g.rank - 1u);
-        auto rows_at = [&](uint32_t at, uint32_t (&row)[DEPTH]) {
-#pragma unroll
-            for (uint32_t d = 0; d < DEPTH; ++d) row[d] = list[min(at + 4u * d + group, q1 - 1u)];
-        };
-        auto fetch = [&](const uint32_t (&row)[DEPTH], Operands& o) {
-#pragma unroll
-            for (uint32_t d = 0; d < DEPTH; ++d) {
-                const uint8_t* from_row = rows_x + row[d] * pitch;
-                if (codes) {                   // they are there up to a multiple of 16
-                    o.w[d] = make_uint2(0u, 0u);
-                    if (full || c < cols) o.w[d] = *reinterpret_cast<const uint2*>(from_row + c);
-                    o.by[d] = g.x_scale[row[d]];
-                } else if (full) {
-                    o.v[d].load(reinterpret_cast<const T*>(from_row) + c);
-                } else {
-                    fetch8(reinterpret_cast<const T*>(from_row), c, cols, o.v[d]);
-                }
-#pragma unroll
-                for (uint32_t f = 0; f < RF; ++f) o.p[d][f] = s[row[d] * ld_s + rank_at[f]];
+        for (uint32_t d = 0; d < DEPTH; ++d) {
+            const uint8_t* from_row = rows_x + row[d] * pitch;
+            if (codes) {                   // they are there up to a multiple of 16
+                o.w[d] = make_uint2(0u, 0u);
+                if (full || c < cols) o.w[d] = *reinterpret_cast<const uint2*>(from_row + c);
+                o.by[d] = g.x_scale[row[d]];
+            } else if (full) {
+                o.v[d].load(reinterpret_cast<const T*>(from_row) + c);
+            } else {
+                fetch8(reinterpret_cast<const T*>(from_row), c, cols, o.v[d]);
             }
-        };
-        // the next rows are on their way while these are multiplied, and where the ones after them are is known
-        constexpr uint32_t TURN = ADAPT_WAVES * 4u * DEPTH;
-        uint32_t at = q0 + wave * 4u * DEPTH, row[DEPTH];
-        Operands next;
-        if (at < q1) {
-            rows_at(at, row);
+            o.p[d] = s[row[d] * ld_s + rank_at];
+        }
+    };
+    // the next rows are on their way while these are multiplied, and where the ones after them are is known
+    constexpr uint32_t TURN = ADAPT_WAVES * 4u * DEPTH;
+    uint32_t at = q0 + wave * 4u * DEPTH, row[DEPTH];
+    Operands next;
+    if (at < q1) {
+        rows_at(at, row);
+        fetch(row, next);
+        rows_at(at + TURN, row);
+    }
+    for (; at < q1; at += TURN) {
+        const Operands o = next;
+        if (at + TURN < q1) {
             fetch(row, next);
-            rows_at(at + TURN, row);
+            rows_at(at + 2u * TURN, row);
         }
-        for (; at < q1; at += TURN) {
-            const Operands o = next;
-            if (at + TURN < q1) {
-                fetch(row, next);
-                rows_at(at + 2u * TURN, row);
+#pragma unroll
+        for (uint32_t d = 0; d < DEPTH; ++d) {
+            float x[8];
+            if (codes) {
+#pragma unroll
+                for (uint32_t j = 0; j < 8; ++j) x[j] = (float)(int8_t)((j < 4 ? o.w[d].x : o.w[d].y) >> (8 * (j % 4)));
+            } else {
+                Eight<T> v = o.v[d];
+                if (!full) place8(c, cols, v);
+                v.floats(x);
+            }
+            float p = codes ? o.p[d] * o.by[d] : o.p[d];
+            if (at + 4u * DEPTH > q1) {    // behind the last row: its numbers once more, which do not count
+                const bool in = at + 4u * d + group < q1;
+                p = in ? p : 0.0f;
+#pragma unroll
+                for (uint32_t j = 0; j < 8; ++j) x[j] = in ? x[j] : 0.0f;
             }
 #pragma unroll
-            for (uint32_t d = 0; d < DEPTH; ++d) {
-                float x[8];
-                if (codes) {
-#pragma unroll
-                    for (uint32_t j = 0; j < 8; ++j) x[j] = (float)(int8_t)((j < 4 ? o.w[d].x : o.w[d].y) >> (8 * (j % 4)));
-                } else {
-                    Eight<T> v = o.v[d];
-                    if (!full) place8(c, cols, v);
-                    v.floats(x);
-                }
-                float p[RF];
-#pragma unroll
-                for (uint32_t f = 0; f < RF; ++f) p[f] = codes ? o.p[d][f] * o.by[d] : o.p[d][f];
-                if (at + 4u * DEPTH > q1) {    // behind the last row: its numbers once more, which do not count
-                    const bool in = at + 4u * d + group < q1;
-#pragma unroll
-                    for (uint32_t f = 0; f < RF; ++f) p[f] = in ? p[f] : 0.0f;
-#pragma unroll
-                    for (uint32_t j = 0; j < 8; ++j) x[j] = in ? x[j] : 0.0f;
-                }
-#pragma unroll
-                for (uint32_t f = 0; f < RF; ++f)
-#pragma unroll
-                    for (uint32_t j = 0; j < 8; ++j) acc[f][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(p[f], x[j], acc[f][j], 0, 0, 0);
-            }
+            for (uint32_t j = 0; j < 8; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(p, x[j], acc[j], 0, 0, 0);
         }
-        // wavefronts 2 and 3 to 0 and 1, then 1 to 0
+    }
+    // wavefronts 2 and 3 to 0 and 1, then 1 to 0
 #pragma unroll
-        for (uint32_t half = 2; half > 0; half >>= 1) {
-            __syncthreads();
-            if (wave >= half && wave < 2 * half) {
+    for (uint32_t half = 2; half > 0; half >>= 1) {
+        __syncthreads();
+        if (wave >= half && wave < 2 * half) {
 #pragma unroll
-                for (uint32_t f = 0; f < RF; ++f)
-#pragma unroll
-                    for (uint32_t j = 0; j < 8; ++j) s_sum[wave - half][8 * f + j][lane] = acc[f][j];
-            }
-            __syncthreads();
-            if (wave < half) {
-#pragma unroll
-                for (uint32_t f = 0; f < RF; ++f)
-#pragma unroll
-                    for (uint32_t j = 0; j < 8; ++j) acc[f][j] += s_sum[wave][8 * f + j][lane];
-            }
+            for (uint32_t j = 0; j < 8; ++j) s_sum[wave - half][j][lane] = acc[j];
         }
-        if (wave != 0) return;
-        // lane: ranks 4 group on, columns c on
-        float* out = g.parts == 1 ? (of_a ? g.da : g.db) + (uint64_t)adapter * cols * g.rank
-                                  : g.partial + ((part_of(from, adapter, g.rows_each) + blockIdx.y) * (g.k + g.n) + (of_a ? 0 : g.k)) * g.rank;
-        typedef float loose __attribute__((ext_vector_type(4), aligned(4)));
+        __syncthreads();
+        if (wave < half) {
 #pragma unroll
-        for (uint32_t f = 0; f < RF; ++f) {
-            const uint32_t r = rank0 + 16u * f + 4u * group;
-            if (of_a) {
+            for (uint32_t j = 0; j < 8; ++j) acc[j] += s_sum[wave][j][lane];
+        }
+    }
+    if (wave != 0) return;
+    // lane: ranks 4 group on, columns c on
+    float* out = g.parts == 1 ? (of_a ? g.da : g.db) + (uint64_t)adapter * cols * g.rank
+                              : g.partial + ((part_of(from, adapter, g.rows_each) + blockIdx.y) * (g.k + g.n) + (of_a ? 0 : g.k)) * g.rank;
+    typedef float loose __attribute__((ext_vector_type(4), aligned(4)));
+    const uint32_t r = rank0 + 4u * group;
+    if (of_a) {
 #pragma unroll
-                for (uint32_t e = 0; e < 4; ++e) {
-                    if (r + e >= g.rank) continue;
-                    float* to = out + (uint64_t)(r + e) * cols + c;
-                    if (full) {
+        for (uint32_t e = 0; e < 4; ++e) {
+            if (r + e >= g.rank) continue;
+            float* to = out + (uint64_t)(r + e) * cols + c;
+            if (full) {
 #pragma unroll
-                        for (uint32_t h = 0; h < 2; ++h)
-                            reinterpret_cast<loose*>(to)[h] = loose{acc[f][4 * h][e], acc[f][4 * h + 1][e], acc[f][4 * h + 2][e], acc[f][4 * h + 3][e]};
-                    } else {
-#pragma unroll
-                        for (uint32_t j = 0; j < 8; ++j)
-                            if (c + j < cols) to[j] = acc[f][j][e];
-                    }
-                }
+                for (uint32_t h = 0; h < 2; ++h)
+                    reinterpret_cast<loose*>(to)[h] = loose{acc[4 * h][e], acc[4 * h + 1][e], acc[4 * h + 2][e], acc[4 * h + 3][e]};
             } else {
 #pragma unroll
-                for (uint32_t j = 0; j < 8; ++j) {
-                    if (c + j >= cols) continue;
-                    float* to = out + (uint64_t)(c + j) * g.rank + r;
-                    if (r + 4u <= g.rank) {
-                        *reinterpret_cast<loose*>(to) = loose{acc[f][j][0], acc[f][j][1], acc[f][j][2], acc[f][j][3]};
-                    } else {
+                for (uint32_t j = 0; j < 8; ++j)
+                    if (c + j < cols) to[j] = acc[j][e];
+            }
+        }
+    } else {
 #pragma unroll
-                        for (uint32_t e = 0; e < 4; ++e)
-                            if (r + e < g.rank) to[e] = acc[f][j][e];
-                    }
-                }
+        for (uint32_t j = 0; j < 8; ++j) {
+            if (c + j >= cols) continue;
+            float* to = out + (uint64_t)(c + j) * g.rank + r;
+            if (r + 4u <= g.rank) {
+                *reinterpret_cast<loose*>(to) = loose{acc[j][0], acc[j][1], acc[j][2], acc[j][3]};
+            } else {
+#pragma unroll
+                for (uint32_t e = 0; e < 4; ++e)
+                    if (r + e < g.rank) to[e] = acc[j][e];
             }
         }
     }
@@ -1181,7 +1161,7 @@ __global__ __launch_bounds__(ADAPT_THREADS) void adapters_join_kernel(AdaptersSu
 template <typename T, bool CODES>
 static void launch_sums_as(shifter_ctx* ctx, const AdaptersSumArgs& g) {
     const dim3 grid(((g.k + ADAPT_SLAB - 1u) / ADAPT_SLAB + (g.n + ADAPT_SLAB - 1u) / ADAPT_SLAB) * g.adapters, g.parts, (uint32_t)adapt_pad(g.rank) / 16u);
-    adapters_grad_kernel<T, CODES, 1><<<grid, ADAPT_THREADS, 0, ctx->stream>>>(g);
+    adapters_grad_kernel<T, CODES><<<grid, ADAPT_THREADS, 0, ctx->stream>>>(g);
 }
 
 template <typename T>
