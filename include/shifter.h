@@ -794,6 +794,7 @@ int shifter_weight_grad_q8(shifter_ctx* ctx, const void* d_g, int dtype, uint64_
  *                        without an adapter; d_dx may be NULL), dA_i = sum up_r' x_r, dB_i = sum g_r' down_r over the rows of adapter i,
  *                        fp32, 0 for an adapter without rows.  Rows whose number is not below `adapters` count for none.  d_down: as
  *                        shifter_adapters wrote it, or NULL: worked out again.  y's gradient is g itself.
+ *                        Its work includes two reads of d_which for each adapter, with or without rows.
  *                        rank 1 to SHIFTER_ADAPTERS_MAX_RANK; SHIFTER_ERR_CAPACITY for more than 2^25 rows and for adapters of 2^30
  *                        columns or so all together.
  *

@@ -13,7 +13,8 @@ constexpr uint64_t ADAPT_MAX_ROWS = 1ull << 25;    // tiles of 16 rows, up to fo
 // 16: 81 / 260, 79 / 63.
 constexpr uint64_t ADAPT_SORT_FROM = 8, ADAPT_SORT_MOST = 4094;
 // Up to so many adapters the gradient's sums over rows are cut into parts as if one adapter had all the rows; beyond, as if all had as many.
-// us of a training step of 4096 x 2048 x 2048 with rank 32, as one / as all: 3 adapters 87 / 94, 8 98 / 121, 16 110 / 109, 32 134 / 106.
+// us of a training step of 4096 x 2048 x 2048 with rank 32, as one / as all: 3 adapters 87 / 94, 8 98 / 121, 16 110 / 109, 32 134 / 106.  That goes by
+// the adapters that are loaded, not by where the rows are: 64 of which one has all rows take 181 (105 where all have as many, 79 with one loaded).
 constexpr uint64_t ADAPT_FEW_ADAPTERS = 8;
 constexpr uint32_t ADAPT_STEP = 64;                // columns of a step of the products over long rows
 // Up to ADAPT_FEW_ROWS rows each adapter of a tile has blocks of its own; beyond, tiles are taken with all of theirs, or in the order of the
@@ -22,7 +23,10 @@ constexpr uint32_t ADAPT_STEP = 64;                // columns of a step of the p
 // From ADAPT_TWO_TILES rows on a block has two tiles of the product over long rows (1024 rows in three runs, one tile / two: 13.9 / 17.4,
 // 2048 20.1 / 19.4, 4096 34.3 / 31.5).
 constexpr uint64_t ADAPT_FEW_ROWS = 128, ADAPT_TWO_TILES = 2048;
-constexpr uint32_t ADAPT_MANY_ROWS_PARTS = 2;      // with more rows, their product with B holds so many in registers
+// With more rows, their product with B holds so many parts in registers.  us, one part / two, 4096 x 4096 with rank 16 and six adapters, 8 bits: 129
+// rows 12.1 / 9.9, 512 13.1 / 10.8, 1024 15.3 / 12.9, 2048 23.6 / 19.0, 4096 31.5 / 28.9, 8192 46.3 / 44.7; a training step of 2048 x 2048, rank 32: 1024
+// rows 47.3 / 43.3, 4096 of one adapter 81.2 / 78.5, of three 83.1 / 86.4.
+constexpr uint32_t ADAPT_MANY_ROWS_PARTS = 2;
 constexpr uint32_t ADAPT_UP_BLOCKS = 2048;         // of the product with B, as far as there are columns (1024 and 4096: within 4 %)
 constexpr uint64_t ADAPT_ONE_BYTES = 144u << 10;
 constexpr uint32_t ADAPT_SLAB = 128;               // columns of a block of the gradient's sums over rows

@@ -291,8 +291,8 @@ struct RowEnd {
 };
 
 // One launch: where blocks share a row, the last of them to end joins what all have left.  8192 x 32768 bf16 without alternatives or
-// entropy 92 us (537 MB, 5.8 TB/s), 2048 x 50001 fp16 with entropy 51 (205 MB, 4.0 TB/s: eleven instructions a logit and an exponential),
-// 128 x 131072 bf16 with entropy and 20 alternatives 21.6, without alternatives 10.8 (34 MB, 3.1 TB/s).  A single row of 50001 with 20
+// entropy 91 us by itself (537 MB, 5.9 TB/s), 112 behind a gradient whose results are still on their way to memory (4.8), 2048 x 50001 fp16 with entropy 51 (205 MB, 4.0 TB/s: eleven instructions a logit and an exponential),
+// 128 x 131072 bf16 with entropy and 20 alternatives 20.4, without alternatives 10.1 (34 MB, 3.3 TB/s).  A single row of 50001 with 20
 // takes 14.0, 6.2 without: a launch and one trip to memory, and with alternatives two rankings of some 24 places and the trip between
 // blocks, each step of which waits for the one before.
 template <typename T, uint32_t TPR, bool H, bool TOP>
@@ -463,8 +463,8 @@ void launch_log_probs(shifter_ctx* ctx, int dtype, const LogProbsArgs& g) {
 
 // The gradient, in one read of x: p = 2^((scale (x - m) - log s) log2 e) once more, x - m in the same unit, from the row's m and log s: lse, their sum,
 // would have lost log s where all that is left of a row is the type's lowest value.  A row whose factors are all 0 is zeros,
-// whatever it holds.  Memory bounds it: 8192 x 32768 bf16, a fifth of the rows left out, 147 us with 430 MB read (some 200 of them from the
-// last-level cache) and 537 written.  Threads a row as for the sums, where 16, 64 and 256 are within a tenth of each other but for
+// whatever it holds.  Memory bounds it: 8192 x 32768 bf16, a fifth of the rows left out, 144 to 155 us right behind the sums, with 430 MB read and 537
+// written (183, with no row left out, where the logits are in no cache).  Threads a row as for the sums, where 16, 64 and 256 are within a tenth of each other but for
 // rows of 200 (8192 x 200 10.5 us with 16, 14.4 with 256).
 template <typename T, uint32_t TPR, bool H>
 __global__ __launch_bounds__(BLOCK) void log_probs_grad_kernel(LogProbsGradArgs g, uint32_t parts, uint32_t part_cols) {

@@ -32,7 +32,8 @@ inline uint64_t logp_entry(uint32_t top) { return 16u + 8u * (uint64_t)top; }   
 
 // Rows up to 256 columns have 16 threads each, up to 1024 a wavefront (more alternatives than groups of 16 give a bound for: a wavefront too),
 // longer ones 256 threads.  us in fp32, 16 threads / 64: 10000 x 200 with five alternatives 9.1 / 18.7, 65536 x 100 13.9 / 45.0,
-// 10000 x 256 5.7 / 8.9; 64 / 256: 4096 x 1000 6.4 / 12.8, with five 10.4 / 27.1.  And where there are too few
+// 10000 x 256 5.7 / 8.9 (10000 x 200 with 16 threads, without alternatives and with five: fp32 5.1 8.9, bf16 5.2 12.2, fp16 5.0 11.8, which have more equal
+// logits to be told apart by their columns); 64 / 256: 4096 x 1000 6.4 / 12.8, with five 10.4 / 27.1.  And where there are too few
 // rows to fill the chip, several such blocks, each of which fetches its 8192 columns at once.  us of bf16 with 20 alternatives, by blocks a
 // row: 1 x 50001 1: 13.9, 6 (two fetches each): 14.8, 8: 13.4, 24: 14.9; 1 x 131072 1: 23.0, 8: 14.5, 16: 14.4, 32: 15.4;
 // 128 x 131072 1: 29.3, 4: 21.6, 8: 21.7; 300 x 131072 1: 38.0, 2: 33.9, 4: 35.3; 8 x 10000 1: 11.3, 2: 14.4.  512 threads a block are
