@@ -480,11 +480,14 @@ __global__ __launch_bounds__(BLOCK) void log_probs_grad_kernel(LogProbsGradArgs 
         const int64_t target = g.target ? g.target[r] : -1;
         float one = g.g_logp && target >= 0 ? g.g_logp[r] : 0.0f;
         if (target >= (int64_t)g.cols) one = NAN;
-        const float m = g.norm[2 * r] * g.unit, log_s = g.norm[2 * r + 1], all_p = (g.g_lse ? g.g_lse[r] : 0.0f) - one;
+        const float m = g.norm[2 * r] * g.unit, log_s = g.norm[2 * r + 1], of_lse = g.g_lse ? g.g_lse[r] : 0.0f;
+        const float by = isinf(of_lse - one) ? 0.5f : 1.0f, scale = g.scale / by;      // factors that only their difference takes beyond fp32: halves of them
+        one *= by;
+        const float all_p = of_lse * by - one;
         float h = 0.0f, by_h = 0.0f;
         if constexpr (H) {
             h = g.entropy[r];
-            by_h = -g.g_entropy[r];
+            by_h = -g.g_entropy[r] * by;
         }
         const bool none = all_p == 0.0f && one == 0.0f && by_h == 0.0f;
         auto value = [&](float x, uint32_t col) {
@@ -492,7 +495,7 @@ __global__ __launch_bounds__(BLOCK) void log_probs_grad_kernel(LogProbsGradArgs 
             // p first and the scale last: no factor of a row comes to the end of fp32 before p makes it small, and where p is 0 this is 0
             float v = all_p * p;
             if constexpr (H) v = fmaf(by_h, p * (fmaxf(d, FAR) + h), v);
-            return (col == (uint32_t)target && target >= 0 ? v + one : v) * g.scale;
+            return (col == (uint32_t)target && target >= 0 ? v + one : v) * scale;
         };
         auto piece = [&](uint32_t at, const Eight<T>& e) {
             float f[8];

@@ -1,11 +1,12 @@
 """The gradient of log probabilities where its factors, or their products with the scale, come to the end of fp32: places
 without probability give 0, others what the formula gives as long as that is a number of the type."""
+import numpy as np
 import pytest
 import torch
 
 from oracle import learn_oracle as L
 from paper_2309_06973_amd.q8 import Q8
-from test_gpu_log_probs import check_grad, make
+from test_gpu_log_probs import check_grad, make, near
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -53,6 +54,22 @@ def test_products_with_the_scale_beyond_fp32(ops, cols):
     got = ops.log_probs_grad(x, t, norm, g_logp=torch.full((5,), 1e25, device=DEV), scale=scale)
     assert (got[:, 1::3] == 0).all() and not torch.isnan(got).any()
     assert (got[1] == 0).all() and got[0, 0] == INF and (got[0, 3::3] <= 0).all()
+
+
+@pytest.mark.parametrize("cols", [100, 900, 3000])
+def test_factors_whose_difference_is_beyond_fp32(ops, cols):
+    for scale in (1.0, 0.25):
+        x, t, ref, norm, h = setup(cols, -INF, scale)
+        big = torch.tensor([3e38, -3e38, 3e38, -2e38, 1e38], device=DEV)
+        for some in (dict(g_logp=big, g_lse=-big), dict(g_logp=big, g_lse=-big, g_entropy=big / 16)):
+            got = ops.log_probs_grad(x, t, norm, entropy=h, scale=scale, **some)
+            assert (got[:, 1::3] == 0).all()
+            # one place of a row is -4e38 by the formula (p 0.68 or 0.66 of -6e38): infinite in fp32
+            want, off = ref.grad(t, **some)
+            beyond = np.abs(want) > 3.41e38
+            assert beyond.sum() == (scale == 1.0 and cols != 900)
+            want[beyond] = np.copysign(np.inf, want[beyond])
+            near(got, want, off + L.U * np.abs(want), "grad")
 
 
 @pytest.mark.parametrize("scale", [2.0 ** -100, 1e-38])
